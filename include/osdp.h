@@ -90,6 +90,11 @@ extern "C" {
 
 #define OSDP_DTYPE_BF16 0
 #define OSDP_DTYPE_FP32 1
+#define OSDP_DTYPE_E4M3 2             /* optimiser states only: 8-bit codes with a scale per OSDP_ADAMW_BLOCK elements */
+
+#define OSDP_NORM_NONE 0
+#define OSDP_NORM_RMS 1
+#define OSDP_NORM_LAYER 2
 
 #define OSDP_OP_LINEAR_FWD 0
 #define OSDP_OP_LINEAR_BWD 1
@@ -342,6 +347,109 @@ int osdp_split_mlp_bwd(const void *dy, const void *x, const void *w_flat, int64_
                        int k_split, int act, void *dx, void *dw_flat, int64_t dw_off_w1,
                        int64_t dw_off_w2, int dw_dtype, int flags, float *db1, float *db2,
                        void *ws, size_t ws_bytes, void *stream);
+
+/* ---- Between two blocks: norms, gate and residual sum.  (Addition beside the paper's method: what a transformer block
+ * needs around its split linear layers.)  For every row (token) of D channels
+ *
+ *     p = N_post(y),    r = alpha * x + beta * gate (.) p,    u = N_pre(r)
+ *
+ * y is the output of the block before, x the residual stream, r the new residual stream, u the input of the next block.
+ * N is  v / sqrt(mean(v^2) + eps) * w  (OSDP_NORM_RMS) or  (v - mean) / sqrt(var + eps) * w + b  (OSDP_NORM_LAYER, var
+ * without Bessel's correction), or nothing (OSDP_NORM_NONE).  Everything between the inputs and the outputs is fp32:
+ * u and the statistics are those of the unrounded r.
+ *   x, r [M,D] resid_dtype (bf16 or fp32); y, u [M,D] bf16; w_*, b_*, gate [D] fp32.
+ *   y NULL: r = alpha * x (the norm in front of the first block); post, w_post, b_post and gate are then not used.
+ *   post OSDP_NORM_NONE: p = y.  pre OSDP_NORM_NONE: u is not written (may be NULL), nor are its statistics.
+ *   w_* NULL: ones; b_* NULL: zeros (b_* must be NULL for OSDP_NORM_RMS); gate NULL: ones.
+ *   r may be NULL (not written) and may be x itself; r and u must not overlap y otherwise.
+ *   u_scale NULL: u is bf16.  u_scale [M] fp32: u is int8, the row divided by its scale = max |u| / 127 and rounded to
+ *   the nearest integer, ties to even: the input that osdp_split_linear_fwd_i8 takes.  A row without a magnitude
+ *   has scale 0 and zeros; a row with an infinity or a NaN has a scale that is not finite (the products come out NaN).
+ *   stats [M,4] fp32 or NULL: mean and 1 / sqrt(...) of N_post, then of N_pre (mean 0 for RMS; 0, 0 for an absent norm):
+ *   what the backward needs.
+ * D is a multiple of 8 and at most OSDP_BLOCK_NORM_MAX_D; M may be 0 (nothing is launched).  bf16 matrices are 16-byte
+ * aligned, fp32 matrices and vectors 32-byte, int8 u 8-byte.  alpha, beta, eps_* finite, eps_* >= 0. */
+#define OSDP_BLOCK_NORM_MAX_D 16384
+int osdp_block_norm_fwd(const void *x, const void *y, int64_t M, int64_t D, int resid_dtype, int post, const float *w_post,
+                        const float *b_post, double eps_post, const float *gate, double alpha, double beta, int pre,
+                        const float *w_pre, const float *b_pre, double eps_pre, void *r, void *u, float *u_scale,
+                        float *stats, void *stream);
+
+/* Gradients of osdp_block_norm_fwd (bf16 u).  dr [M,D] resid_dtype or NULL: gradient that reaches r from elsewhere (the
+ * residual stream); du [M,D] bf16, required iff pre != OSDP_NORM_NONE; y (NULL as in the forward), r and stats as the
+ * forward read and wrote them.  With h = (v - mean) / sqrt(...) of either norm and t the gradient of r:
+ *     a = du (.) w_pre;  t = dr + (a - mean(a) [LAYER] - h_pre mean(a (.) h_pre)) / sqrt(...);  dx = alpha t
+ *     q = beta gate (.) w_post (.) t;  dy = (q - mean(q) [LAYER] - h_post mean(q (.) h_post)) / sqrt(...)
+ *     dw_post = beta gate (.) sum t (.) h_post;  db_post = beta gate (.) sum t;  dgate = beta sum t (.) p
+ *     dw_pre = sum du (.) h_pre;  db_pre = sum du          (sums over rows)
+ * dx [M,D] resid_dtype, dy [M,D] bf16, the others [D] fp32; any of them may be NULL (not wanted).  dx may be dr itself,
+ * dy may be du itself.  The sums over rows are added in a fixed order: the same call gives the same bits.  M = 0 writes
+ * zeros to the vectors.  ws: osdp_block_norm_workspace_bytes(M, D) bytes (no state is kept in it). */
+int osdp_block_norm_workspace_bytes(int64_t M, int64_t D, size_t *bytes);
+int osdp_block_norm_bwd(const void *dr, const void *du, const void *y, const void *r, const float *stats, int64_t M, int64_t D,
+                        int resid_dtype, int post, const float *w_post, const float *b_post, const float *gate, double alpha,
+                        double beta, int pre, const float *w_pre, void *dx, void *dy, float *dw_post, float *db_post,
+                        float *dgate, float *dw_pre, float *db_pre, void *ws, size_t ws_bytes, void *stream);
+
+/* ---- The optimiser step of the (flat) parameters.  (Addition beside the paper's method, whose memory model counts
+ * the optimiser states that this keeps in 32 or in 8 bits.)  A tensor of the step: */
+#define OSDP_ADAMW_BLOCK 256
+typedef struct {
+  void *param;            /* DEVICE, numel elements, contiguous, aligned to one element */
+  const void *grad;       /* DEVICE, same dtype and length */
+  int64_t numel;          /* 0: the tensor is skipped */
+  int64_t state_offset;   /* element where its states start in the flat state buffers, a multiple of OSDP_ADAMW_BLOCK */
+  double lr, weight_decay;
+} osdp_adamw_tensor;
+
+/* Where the states of n tensors start when they are laid out one after another, each padded to whole blocks of
+ * OSDP_ADAMW_BLOCK elements, and the length of a flat state buffer.  Host only; state_offset may be NULL. */
+int osdp_adamw_layout(const int64_t *numel, int n, int64_t *state_offset, int64_t *state_elems);
+
+/* out[0] = sqrt(sum of squares of all gradients), out[1] = min(1, max_norm / (out[0] + 1e-6)), the coefficient that
+ * clips them (1 for max_norm <= 0; NaN if out[0] is not finite).  `tensors` is a HOST array (grad and numel are read),
+ * out two floats on the DEVICE.  Sums are fp32 per block and fp64 over blocks, in a fixed order: the same gradients
+ * give the same bits.  No host synchronisation.  ws: zero its first 256 bytes once, as for every workspace; one
+ * workspace must not be used by two calls at the same time. */
+int osdp_grad_norm_workspace_bytes(int n_tensors, size_t *bytes);
+int osdp_grad_norm(const osdp_adamw_tensor *tensors, int n_tensors, int grad_dtype, float max_norm, float *out, void *ws,
+                   size_t ws_bytes, void *stream);
+
+/* AdamW (decoupled weight decay) over all tensors, one launch per 640 of them; `tensors` is a HOST array that the call
+ * does not keep.  Per element, t = step >= 1 and c = clip[1] (1 for clip NULL):
+ *     g = c * grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *     p = p (1 - lr wd) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32.  param_dtype (of param and grad): OSDP_DTYPE_BF16 or OSDP_DTYPE_FP32.
+ *   master   flat fp32 parameters laid out like the states, or NULL.  With it p is read and written there and param
+ *            receives its bf16 rounding; only for bf16 parameters.
+ *   state_m, state_v   flat states, zeroed before the first step, 32-byte aligned; state_dtype OSDP_DTYPE_FP32: m and v;
+ *            OSDP_DTYPE_E4M3: e4m3 codes of m and of sqrt(v), value = code * scale_m / scale_v [offset / OSDP_ADAMW_BLOCK].
+ *            A scale is the block's largest magnitude / 448; a block below 2^-100 is stored as zeros; the code of a root
+ *            above zero is at least the smallest positive one.  The step uses m and v before they are rounded.
+ *   clip     output of osdp_grad_norm or NULL.  If its coefficient is not finite nothing at all is updated.
+ * All arithmetic per element is in a fixed order; the call is deterministic. */
+int osdp_adamw_step(const osdp_adamw_tensor *tensors, int n_tensors, int param_dtype, int state_dtype, float *master,
+                    void *state_m, void *state_v, float *scale_m, float *scale_v, double beta1, double beta2, double eps,
+                    int64_t step, const float *clip, void *stream);
+
+/* ---- int8 operands with a scale per token and per output channel: the forward of a linear layer for serving.
+ *     Y[m,n] = act( (sum_k x8[m,k] w8[n,k]) * x_scale[m] * w_scale[n] + bias[n] )
+ * The sum is an int32 and therefore exact: any slicing gives the same bits.
+ *
+ * osdp_quantize_rows_i8: per row, scale = max |x| / 127, q = x / scale rounded to the nearest integer, ties to even
+ * (rows without a magnitude and rows that are not finite: as in osdp_block_norm_fwd).  x [M,K] bf16, q [M,K] int8,
+ * scale [M] fp32; K a multiple of 8, at most 131071 (a product of longer rows could leave 32 bits); x 16-byte, q 8-byte
+ * aligned; M may be 0. */
+int osdp_quantize_rows_i8(const void *x, int64_t M, int64_t K, void *q, float *scale, void *stream);
+
+/* x8 [M,K] and w8_flat (W [N,K] at element = byte offset w_offset) int8; x_scale [M], w_scale [N], bias [N] (or NULL) fp32;
+ * out [M,N] bf16.  K and w_offset multiples of 16, N of 8 (16 if the slices cut N), a slice length of K a multiple of 16;
+ * K < 131072; M may be 0.  x8, w8_flat, out, w_scale and bias 16-byte aligned.  Every slice of the operator in one
+ * call, no flags; workspace osdp_split_linear_workspace_bytes(..., OSDP_OP_LINEAR_FWD, 0).  No gradient: a model is
+ * trained in bf16 and served in int8. */
+int osdp_split_linear_fwd_i8(const void *x8, const float *x_scale, const void *w8_flat, int64_t w_offset, const float *w_scale,
+                             const float *bias, int64_t M, int64_t N, int64_t K, int k_split, int split_dim, int act, void *out,
+                             void *ws, size_t ws_bytes, void *stream);
 
 /* Failure detection (no counterpart in the paper, which does not discuss faults: the slices of Section
  * 3.3 "executed sequentially" are pipelines of asynchronous copies and tensor-core work whose stages

@@ -14,7 +14,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 
 SPLIT_OUT, SPLIT_RED = 0, 1
 ACT_NONE, ACT_GELU_TANH, ACT_GELU_ERF = 0, 1, 2
-DTYPE_BF16, DTYPE_FP32 = 0, 1
+DTYPE_BF16, DTYPE_FP32, DTYPE_E4M3 = 0, 1, 2
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+ADAMW_BLOCK, BLOCK_NORM_MAX_D = 256, 16384
 OP_LINEAR_FWD, OP_LINEAR_BWD, OP_MLP_FWD, OP_MLP_BWD = 0, 1, 2, 3
 FLAG_ACCUMULATE_DW, FLAG_CARRY_BF16, FLAG_RECOMPUTE, FLAG_PAIR_SLICES, FLAG_SLICE_MAJOR = 1, 2, 4, 8, 16
 
@@ -27,9 +29,18 @@ EXPORTS = [
     "osdp_plan_cost", "osdp_plan_search", "osdp_plan_expand_slices", "osdp_plan_search_granularity",
     "osdp_split_linear_fwd_f8", "osdp_split_linear_bwd_f8", "osdp_zdp_linear_bwd_slice_scatter",
     "osdp_zdp_mlp_fwd_slice", "osdp_zdp_mlp_bwd_slice",
+    "osdp_block_norm_fwd", "osdp_block_norm_bwd", "osdp_block_norm_workspace_bytes",
+    "osdp_adamw_layout", "osdp_adamw_step", "osdp_grad_norm", "osdp_grad_norm_workspace_bytes",
+    "osdp_quantize_rows_i8", "osdp_split_linear_fwd_i8",
 ]
 
 _lib = None
+
+
+class AdamWTensor(ctypes.Structure):
+    """osdp_adamw_tensor of the C ABI: one tensor of an optimiser step (device addresses)."""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("numel", ctypes.c_int64),
+                ("state_offset", ctypes.c_int64), ("lr", ctypes.c_double), ("weight_decay", ctypes.c_double)]
 
 
 class OsdpError(RuntimeError):
@@ -96,6 +107,17 @@ def lib():
         L.osdp_split_linear_fwd_f8.argtypes = [vp, vp, i64, f32, vp, i64, i64, i64, ci, ci, ci, ci, vp, vp, vp, sz, vp]
         L.osdp_split_linear_bwd_f8.argtypes = [vp, vp, vp, i64, f32, f32, i64, i64, i64, ci, ci, vp, vp, i64, ci, ci,
                                                vp, sz, vp]
+        dbl = ctypes.c_double
+        L.osdp_block_norm_fwd.argtypes = [vp, vp, i64, i64, ci, ci, vp, vp, dbl, vp, dbl, dbl, ci, vp, vp, dbl, vp, vp, vp, vp, vp]
+        L.osdp_block_norm_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
+        L.osdp_block_norm_bwd.argtypes = [vp, vp, vp, vp, vp, i64, i64, ci, ci, vp, vp, vp, dbl, dbl, ci, vp, vp, vp, vp, vp, vp,
+                                          vp, vp, vp, sz, vp]
+        L.osdp_adamw_layout.argtypes = [p64, ci, p64, p64]
+        L.osdp_grad_norm_workspace_bytes.argtypes = [ci, ctypes.POINTER(sz)]
+        L.osdp_grad_norm.argtypes = [vp, ci, ci, f32, vp, vp, sz, vp]
+        L.osdp_adamw_step.argtypes = [vp, ci, ci, ci, vp, vp, vp, vp, vp, dbl, dbl, dbl, i64, vp, vp]
+        L.osdp_quantize_rows_i8.argtypes = [vp, i64, i64, vp, vp, vp]
+        L.osdp_split_linear_fwd_i8.argtypes = [vp, vp, vp, i64, vp, vp, i64, i64, i64, ci, ci, ci, vp, vp, sz, vp]
         for name in EXPORTS:
             getattr(L, name)
             if name not in ("osdp_status_string",):
@@ -402,3 +424,72 @@ def osdp_zdp_mlp_bwd_slice(dy, x, w1_slice, w2_slice, ld_w2, b1, z1_saved, M, hi
                                       _ptr_array(dw1_peers), _ptr_array(dw2_peers), world, int(dw_dtype), int(flags),
                                       _ptr(db1), _ptr(db2), wp, wn, _stream(stream))
     return _ret(rc, check, "osdp_zdp_mlp_bwd_slice")
+
+
+def osdp_block_norm_fwd(x, y, M, D, resid_dtype, post, w_post, b_post, eps_post, gate, alpha, beta, pre, w_pre, b_pre, eps_pre,
+                        r, u, u_scale, stats, stream=None, check=False):
+    rc = lib().osdp_block_norm_fwd(_ptr(x), _ptr(y), M, D, resid_dtype, post, _ptr(w_post), _ptr(b_post), eps_post, _ptr(gate),
+                                   alpha, beta, pre, _ptr(w_pre), _ptr(b_pre), eps_pre, _ptr(r), _ptr(u), _ptr(u_scale),
+                                   _ptr(stats), _stream(stream))
+    return _ret(rc, check, "osdp_block_norm_fwd")
+
+
+def osdp_block_norm_workspace_bytes(M, D):
+    """Returns (status, bytes)."""
+    n = ctypes.c_size_t()
+    rc = lib().osdp_block_norm_workspace_bytes(int(M), int(D), ctypes.byref(n))
+    return rc, n.value
+
+
+def osdp_block_norm_bwd(dr, du, y, r, stats, M, D, resid_dtype, post, w_post, b_post, gate, alpha, beta, pre, w_pre, dx, dy,
+                        dw_post, db_post, dgate, dw_pre, db_pre, ws, stream=None, check=False):
+    wp, wn = _ws(ws)
+    rc = lib().osdp_block_norm_bwd(_ptr(dr), _ptr(du), _ptr(y), _ptr(r), _ptr(stats), M, D, resid_dtype, post, _ptr(w_post),
+                                   _ptr(b_post), _ptr(gate), alpha, beta, pre, _ptr(w_pre), _ptr(dx), _ptr(dy), _ptr(dw_post),
+                                   _ptr(db_post), _ptr(dgate), _ptr(dw_pre), _ptr(db_pre), wp, wn, _stream(stream))
+    return _ret(rc, check, "osdp_block_norm_bwd")
+
+
+def osdp_adamw_layout(numels):
+    """Returns (status, [state offset of each tensor], elements of a flat state buffer)."""
+    n = len(numels)
+    a, o, t = (ctypes.c_int64 * max(n, 1))(*[int(v) for v in numels]), (ctypes.c_int64 * max(n, 1))(), ctypes.c_int64()
+    rc = lib().osdp_adamw_layout(a, n, o, ctypes.byref(t))
+    return rc, list(o[:n]), t.value
+
+
+def osdp_grad_norm_workspace_bytes(n_tensors):
+    """Returns (status, bytes)."""
+    n = ctypes.c_size_t()
+    rc = lib().osdp_grad_norm_workspace_bytes(int(n_tensors), ctypes.byref(n))
+    return rc, n.value
+
+
+def osdp_grad_norm(tensors, n_tensors, grad_dtype, max_norm, out, ws, stream=None, check=False):
+    """tensors: a ctypes array of AdamWTensor, or its address (grad and numel are read)."""
+    wp, wn = _ws(ws)
+    rc = lib().osdp_grad_norm(tensors, int(n_tensors), int(grad_dtype), float(max_norm), _ptr(out), wp, wn, _stream(stream))
+    return _ret(rc, check, "osdp_grad_norm")
+
+
+def osdp_adamw_step(tensors, n_tensors, param_dtype, state_dtype, master, state_m, state_v, scale_m, scale_v, beta1, beta2, eps,
+                    step, clip, stream=None, check=False):
+    """tensors: a ctypes array of AdamWTensor, or its address."""
+    rc = lib().osdp_adamw_step(tensors, int(n_tensors), int(param_dtype), int(state_dtype), _ptr(master), _ptr(state_m),
+                               _ptr(state_v), _ptr(scale_m), _ptr(scale_v), float(beta1), float(beta2), float(eps), int(step),
+                               _ptr(clip), _stream(stream))
+    return _ret(rc, check, "osdp_adamw_step")
+
+
+def osdp_quantize_rows_i8(x, M, K, q, scale, stream=None, check=False):
+    rc = lib().osdp_quantize_rows_i8(_ptr(x), int(M), int(K), _ptr(q), _ptr(scale), _stream(stream))
+    return _ret(rc, check, "osdp_quantize_rows_i8")
+
+
+def osdp_split_linear_fwd_i8(x8, x_scale, w8_flat, w_offset, w_scale, bias, M, N, K, k_split, split_dim, act, out, ws,
+                             stream=None, check=False):
+    wp, wn = _ws(ws)
+    rc = lib().osdp_split_linear_fwd_i8(_ptr(x8), _ptr(x_scale), _ptr(w8_flat), int(w_offset), _ptr(w_scale), _ptr(bias), int(M),
+                                        int(N), int(K), int(k_split), int(split_dim), int(act), _ptr(out), wp, wn,
+                                        _stream(stream))
+    return _ret(rc, check, "osdp_split_linear_fwd_i8")

@@ -14,6 +14,8 @@
 
 #include "osdp_aux.cuh"
 #include "osdp_gemm.cuh"
+#include "osdp_i8.h"
+#include "osdp_internal.h"
 
 using namespace osdp;
 
@@ -185,8 +187,6 @@ struct ForkJoin {
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
 // ------------------------------------------------------------------------------------------------
 // Slice table (Section 3.3, step 1)
 
@@ -308,7 +308,8 @@ struct GemmCall {
   int pair_slices;  // MODE_RED: accumulate two adjacent slices per pass
   int slice_major;  // MODE_RED, all slices in the launch: sweep slice by slice with the carry (else: slices inside a tile)
   int out_is_slice; // MODE_ROWS / MODE_COLS: `epi.out` is the slice's own compact matrix, not the whole output
-  int fp8;          // operands are fp8 e4m3 (1 byte per element) instead of bf16
+  int fp8;          // operands are 8-bit (1 byte per element) instead of bf16: fp8 e4m3, or int8 with i8
+  int i8;           // (with fp8) int8 operands, int32 accumulators, epi.row_scale / epi.col_scale
   int compact;      // the launch runs next to another GEMM of the call: CTA pairs on 256-wide tiles even when few
   int n_peers;      // > 0: the output slice is reduce-added row block by row block into peer_out[0..n_peers)
   void *peer_out[8];
@@ -422,12 +423,12 @@ int make_output_maps(void *base, bool fp32, int64_t P, int64_t Q, int64_t ld, in
 
 // One kernel variant: sets its attributes once per device, sizes the grid and launches.
 // `units` = work items of the launch (tiles, summed over slices for concatenated outputs).
-template <int BN, bool A_MN, bool B_MN, bool CTA2, bool HEAVY = false, int EB = 2>
+template <int BN, bool A_MN, bool B_MN, bool CTA2, bool HEAVY = false, int EB = 2, bool I8 = false>
 int launch_variant(const GemmParams &p, int64_t units, int sms, cudaStream_t stream) {
   static std::atomic<bool> attr_done[64];
   static std::atomic<int> max_clusters[64];
   using SL = SmemLayout<BN, CTA2, HEAVY>;
-  auto kernel = gemm_kernel<BN, A_MN, B_MN, CTA2, HEAVY, EB>;
+  auto kernel = gemm_kernel<BN, A_MN, B_MN, CTA2, HEAVY, EB, I8>;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return cuda_fail(e);
@@ -478,6 +479,13 @@ template <int BN, bool CTA2>
 int launch_bn(const GemmParams &p, bool a_mn, bool b_mn, bool heavy, int64_t units, int sms, cudaStream_t stream) {
   if (p.bk == 128) {   // fp8 operands: tiles from 128 columns up (an MN-major chunk is 128 wide)
     if constexpr (BN >= 128) {
+      if (p.epi.row_scale) {   // int8: the forward's operand layout only
+        if (a_mn || b_mn) return OSDP_ERR_UNSUPPORTED;
+        if constexpr (BN <= 256) {
+          if (heavy) return launch_variant<BN, false, false, CTA2, true, 1, true>(p, units, sms, stream);
+        }
+        return launch_variant<BN, false, false, CTA2, false, 1, true>(p, units, sms, stream);
+      }
       if (!a_mn && !b_mn) return launch_variant<BN, false, false, CTA2, false, 1>(p, units, sms, stream);
       if (!a_mn && b_mn) return launch_variant<BN, false, true, CTA2, false, 1>(p, units, sms, stream);
       if (a_mn && b_mn) return launch_variant<BN, true, true, CTA2, false, 1>(p, units, sms, stream);
@@ -547,10 +555,10 @@ void make_key(const GemmCall &c, PreparedKey *k) {
   putp(e.z_save); put((uint64_t)e.ld_z); putp(e.gz); put((uint64_t)e.ld_gz); putp(e.act_out); put((uint64_t)e.ld_act_out);
   put(((uint64_t)(uint32_t)e.out_fp32) | ((uint64_t)(uint32_t)e.accumulate << 8) | ((uint64_t)(uint32_t)e.act << 16) |
       ((uint64_t)(uint32_t)e.gz_act << 24));
-  putf(e.scale);
+  putf(e.scale); putp(e.row_scale); putp(e.col_scale);
   put(((uint64_t)(uint32_t)c.carry_bf16) | ((uint64_t)(uint32_t)c.pair_slices << 8) | ((uint64_t)(uint32_t)c.slice_major << 16) |
       ((uint64_t)(uint32_t)c.out_is_slice << 24) | ((uint64_t)(uint32_t)c.fp8 << 32) | ((uint64_t)(uint32_t)c.n_peers << 40) |
-      ((uint64_t)(uint32_t)c.compact << 48));
+      ((uint64_t)(uint32_t)c.compact << 48) | ((uint64_t)(uint32_t)c.i8 << 56));
   for (int q = 0; q < 8; ++q) putp(q < c.n_peers ? c.peer_out[q] : nullptr);
   putp(c.status);
   uint64_t h = 1469598103934665603ull;
@@ -759,10 +767,10 @@ int launch_gemm(const GemmCall &c, cudaStream_t stream) {
   slot.pair = pair;
   slot.bn = bn;
   slot.items = count_items(c, tm, bn);
-  slot.heavy = (c.epi.act != ACT_NONE || gz_tma) && c.mode != MODE_RED && p.tma_epilogue && !c.fp8;
+  slot.heavy = (c.epi.act != ACT_NONE || gz_tma) && c.mode != MODE_RED && p.tma_epilogue && (!c.fp8 || c.i8);
   // A launch that gives every scheduling unit at most one tile has its whole epilogue exposed (nothing follows
   // to overlap it with): eight epilogue warps, each draining half of the tile's columns, halve that time.
-  if (slot.items <= (pair ? sms / 2 : sms) && p.tma_epilogue && !c.fp8 && (bn == 128 || bn == 256) &&
+  if (slot.items <= (pair ? sms / 2 : sms) && p.tma_epilogue && (!c.fp8 || c.i8) && (bn == 128 || bn == 256) &&
       (c.mode == MODE_NONE || c.mode == MODE_COLS || c.mode == MODE_ROWS))
     slot.heavy = true;
   slot.valid = true;
@@ -1124,6 +1132,12 @@ int bwd_impl(const void *dy, const void *x, const void *w_flat, int64_t w_offset
 // ================================================================================================
 // C ABI
 
+// What the other translation units of the library need from this one (osdp_internal.h).
+namespace osdp {
+int report_cuda(cudaError_t e) { return e == cudaSuccess ? OSDP_OK : cuda_fail(e); }
+int sm_count(int *sms) { return device_sms(sms); }
+}  // namespace osdp
+
 extern "C" {
 
 int osdp_version(void) { return OSDP_VERSION; }
@@ -1230,6 +1244,46 @@ int osdp_split_linear_fwd_f8(const void *x8, const void *w8_flat, int64_t w_offs
                              void *out, void *z_save, void *ws, size_t ws_bytes, void *stream) {
   return fwd_impl(x8, w8_flat, w_offset, bias, M, N, K, k_split, split_dim, act, flags, 0, 0, false, out, z_save, ws,
                   ws_bytes, stream, 0, 1, scale);
+}
+
+int osdp_split_linear_fwd_i8(const void *x8, const float *x_scale, const void *w8_flat, int64_t w_offset, const float *w_scale,
+                             const float *bias, int64_t M, int64_t N, int64_t K, int k_split, int split_dim, int act, void *out,
+                             void *ws, size_t ws_bytes, void *stream) {
+  if (M < 0 || K > OSDP_I8_MAX_K) return OSDP_ERR_BAD_SHAPE;
+  int64_t L = 0;
+  int rc = check_common(M > 0 ? M : 1, N, K, k_split, split_dim, act, &L);
+  if (rc) return rc;
+  if (k_split == 0) k_split = 1;
+  if ((K & 15) || w_offset < 0 || (w_offset & 15) || (k_split > 1 && (L & 15)) || (k_split > 1 && split_dim == OSDP_SPLIT_OUT && (N & 15)))
+    return OSDP_ERR_ALIGNMENT;
+  if (M == 0) return OSDP_OK;
+  if (!x8 || !x_scale || !w8_flat || !w_scale || !out) return OSDP_ERR_NULL_POINTER;
+  if (!aligned16(x8) || !aligned16(w8_flat) || !aligned16(out) || !aligned16(w_scale) || !aligned16(bias) || !aligned_to(x_scale, 4))
+    return OSDP_ERR_ALIGNMENT;
+  WsPlan plan;
+  rc = plan_workspace(M, N, K, k_split, split_dim, act, OSDP_OP_LINEAR_FWD, 0, &plan);
+  if (rc) return rc;
+  rc = check_ws(ws, ws_bytes, plan);
+  if (rc) return rc;
+  const void *w = static_cast<const char *>(w8_flat) + w_offset;
+  if (M <= OSDP_I8_FEW_TOKENS)   // exact sums: the slices make no difference to the bits
+    return launch_i8_few_tokens(x8, x_scale, w, w_scale, bias, M, N, K, act, out, static_cast<cudaStream_t>(stream));
+  GemmCall c;
+  memset(&c, 0, sizeof(c));
+  c.fp8 = c.i8 = 1;
+  c.a = Operand{x8, K, M, K, false, true};
+  c.b = Operand{w, K, N, K, false, true};
+  c.P = M; c.Q = N; c.R = K;
+  c.bn_P = M; c.bn_Q = N;
+  c.mode = (k_split == 1) ? MODE_NONE : (split_dim == OSDP_SPLIT_OUT ? MODE_COLS : MODE_RED);
+  c.L = L; c.k_total = k_split; c.s_begin = 0; c.s_end = k_split;
+  c.epi = plain_epilogue(out, N, 0);
+  c.epi.row_scale = x_scale;
+  c.epi.col_scale = w_scale;
+  c.epi.bias = bias;
+  c.epi.act = act;
+  c.status = static_cast<int *>(ws);
+  return launch_gemm(c, static_cast<cudaStream_t>(stream));
 }
 
 int osdp_split_linear_bwd_f8(const void *dy8, const void *x8, const void *w8_flat, int64_t w_offset, float scale_dx,

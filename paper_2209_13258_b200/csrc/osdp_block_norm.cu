@@ -1,0 +1,786 @@
+// Norms, gate and residual sum between two blocks, forward and backward:
+//   p = N_post(y),  r = alpha x + beta gate (.) p,  u = N_pre(r).
+// HBM-bound: the forward reads x, y and writes r, u once; the backward reads y, r, du, dr and writes dx, dy once, the
+// sums over rows (weights' gradients) are kept in registers over all rows of a thread block.
+#include "../../include/osdp.h"
+
+#include <atomic>
+#include <cmath>
+#include <mutex>
+
+#include "osdp_internal.h"
+#include "osdp_vec.cuh"
+
+namespace osdp {
+namespace {
+
+struct RowNorm {
+  int has;          // a norm at all (RMS or layer)
+  int layer;        // layer norm: subtracts the mean
+  float eps;
+  const float *w, *b;
+};
+
+// Sum of N values per thread over a team of `warps` warps (all of them call it).  `red`: two buffers of
+// [warps of the block][N4] floats used in turn, so that one barrier per call is enough: a buffer is written again only
+// after the barrier of the call in between, which every reader of the buffer has passed.
+template <int N>
+__device__ __forceinline__ void team_sum(float (&v)[N], int warps, int first_warp, int warp, int lane, int bar_id, float *red, int &turn) {
+  constexpr int N4 = (N + 3) / 4 * 4;
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = warp_sum(v[k]);
+  if (warps == 1) return;
+  float *buf = red + turn * (32 * N4);
+  turn ^= 1;
+  if (lane == 0) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) buf[warp * N4 + k] = v[k];
+  }
+  asm volatile("bar.sync %0, %1;" ::"r"(bar_id), "r"(warps * 32) : "memory");
+  float s[N4];
+#pragma unroll
+  for (int k = 0; k < N4; ++k) s[k] = 0.f;
+  for (int q = 0; q < warps; ++q) {
+#pragma unroll
+    for (int k4 = 0; k4 < N4 / 4; ++k4) {
+      const float4 f = *reinterpret_cast<const float4 *>(buf + (first_warp + q) * N4 + 4 * k4);
+      s[4 * k4] += f.x;
+      s[4 * k4 + 1] += f.y;
+      s[4 * k4 + 2] += f.z;
+      s[4 * k4 + 3] += f.w;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = s[k];
+}
+
+// ------------------------------------------------------------------------------------------------ forward
+
+struct FwdArgs {
+  const void *x;
+  const __nv_bfloat16 *y;
+  void *r;
+  void *u;
+  float *u_scale;
+  float4 *stats;
+  const float *gate;
+  float alpha, beta;
+  RowNorm post, pre;
+  long long M;
+  int D;
+  int warps;       // of a row's team
+};
+
+__device__ __forceinline__ void weights8(const float *w, int col, float fill, float (&f)[8]) {
+  if (w) {
+    const float4 a = __ldg(reinterpret_cast<const float4 *>(w + col)), b = __ldg(reinterpret_cast<const float4 *>(w + col + 4));
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = fill;
+  }
+}
+
+// A team of `warps` warps owns a row; a lane holds V vectors of eight adjacent channels, vector j at channel
+// (j * 32 * warps + lane of the team) * 8, so that a warp's accesses are whole lines.  The row stays in registers
+// between the two norms: sums are taken over the values themselves (mean first, then squared distances from it), not
+// as differences of moments.
+template <typename RT, int V>
+__global__ void __launch_bounds__(V == 4 ? 512 : 1024) block_norm_fwd_kernel(const __grid_constant__ FwdArgs a) {
+  __shared__ __align__(16) float red[2 * 32 * 4];
+  pdl_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int team = warp / a.warps, first_warp = team * a.warps;
+  const int tl = (warp - first_warp) * 32 + lane, TL = a.warps * 32;
+  const int teams = (blockDim.x >> 5) / a.warps;
+  const long long row = (long long)blockIdx.x * teams + team;
+  if (row >= a.M) return;
+  int turn = 0;
+  auto sum1 = [&](float s) {
+    float v[1] = {s};
+    team_sum<1>(v, a.warps, first_warp, warp, lane, 1 + team, red, turn);
+    return v[0];
+  };
+  pdl_wait();
+  const float inv_d = 1.0f / (float)a.D;
+  const RT *xr = static_cast<const RT *>(a.x) + row * a.D;
+  float v[V][8];     // r, then u
+  uint4 yv[V];
+  bool act[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const int col = (j * TL + tl) * 8;
+    act[j] = col < a.D;
+    yv[j] = make_uint4(0u, 0u, 0u, 0u);
+    if (act[j]) {
+      if (a.y) yv[j] = load16(a.y + row * a.D + col);
+      load8(xr + col, v[j]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[j][k] = 0.f;
+    }
+  }
+  float4 st = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (a.y) {
+    float mean = 0.f, rstd = 1.f;
+    if (a.post.has) {
+      if (a.post.layer) {
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          float f[8];
+          widen8(yv[j], f);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s += f[k];
+        }
+        mean = sum1(s) * inv_d;
+      }
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        float f[8];
+        widen8(yv[j], f);
+        if (act[j]) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s = fmaf(f[k] - mean, f[k] - mean, s);
+        }
+      }
+      rstd = rsqrtf(fmaf(sum1(s), inv_d, a.post.eps));
+      st.x = mean;
+      st.y = rstd;
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      if (!act[j]) continue;
+      const int col = (j * TL + tl) * 8;
+      float f[8], w[8], b[8], g[8];
+      widen8(yv[j], f);
+      weights8(a.post.w, col, 1.f, w);
+      weights8(a.post.b, col, 0.f, b);
+      weights8(a.gate, col, 1.f, g);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float p = fmaf((f[k] - mean) * rstd, w[k], b[k]);
+        v[j][k] = fmaf(a.beta * g[k], p, a.alpha * v[j][k]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[j][k] *= a.alpha;
+  }
+  if (a.r) {
+    RT *rr = static_cast<RT *>(a.r) + row * a.D;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (act[j]) store8(rr + (j * TL + tl) * 8, v[j]);
+  }
+  if (a.pre.has) {
+    float mean = 0.f;
+    if (a.pre.layer) {
+      float s = 0.f;
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += v[j][k];
+      mean = sum1(s) * inv_d;
+    }
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      if (act[j]) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s = fmaf(v[j][k] - mean, v[j][k] - mean, s);
+      }
+    }
+    const float rstd = rsqrtf(fmaf(sum1(s), inv_d, a.pre.eps));
+    st.z = mean;
+    st.w = rstd;
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+      if (!act[j]) continue;
+      const int col = (j * TL + tl) * 8;
+      float w[8], b[8];
+      weights8(a.pre.w, col, 1.f, w);
+      weights8(a.pre.b, col, 0.f, b);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        v[j][k] = fmaf((v[j][k] - mean) * rstd, w[k], b[k]);
+        top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(v[j][k]) & 0x7FFFFFFFu));
+      }
+      if (!a.u_scale) store8(static_cast<__nv_bfloat16 *>(a.u) + row * a.D + col, v[j]);
+    }
+    if (a.u_scale) {
+      top = warp_max_abs(top);
+      if (a.warps > 1) {
+        float *buf = red + turn * (32 * 4);
+        if (lane == 0) buf[warp * 4] = top;
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(TL) : "memory");
+        for (int q = 0; q < a.warps; ++q)
+          top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(buf[(first_warp + q) * 4])));
+      }
+      const float inv = int8_inverse(top);
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (act[j])
+          *reinterpret_cast<uint2 *>(static_cast<int8_t *>(a.u) + row * a.D + (j * TL + tl) * 8) = to_int8x8(v[j], inv);
+      if (tl == 0) a.u_scale[row] = int8_scale(top);
+    }
+  }
+  if (a.stats && tl == 0) a.stats[row] = st;
+}
+
+// ------------------------------------------------------------------------------------------------ backward
+
+constexpr int BWD_MAX_BLOCKS = 160;   // partial sums over rows that the workspace holds
+constexpr int BWD_THREADS = 512;
+
+struct BwdArgs {
+  const void *dr;
+  const __nv_bfloat16 *du, *y;
+  const void *r;
+  const float4 *stats;
+  const float *w_post, *gate, *w_pre;
+  float alpha, beta;
+  int post_has, post_layer, pre_has, pre_layer;
+  void *dx;
+  __nv_bfloat16 *dy;
+  float *partial;    // [units][4][D]
+  long long M;
+  int D;
+  int warps;         // of a team
+  int teams;         // of a block
+  int stages;
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// waits until at most `left` of this thread's groups are still in flight
+__device__ __forceinline__ void cp_async_wait(int left) {
+  switch (left) {
+    case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+    case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+    case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+    case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+    default: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
+  }
+}
+constexpr int MAX_STAGES = 6;
+
+// Rows are dealt to teams of warps in a fixed stride; a lane owns two vectors of eight adjacent channels for the whole
+// kernel and keeps the channel sums in registers.  What it needs of the next rows it copies itself, asynchronously, into
+// its own slots of a ring in shared memory: no thread reads another's slots, so the ring needs no barrier.
+//
+// One reduction per row.  With t = dr + rstd (a - c1 - h_pre c2), c1 = mean a, c2 = mean a h_pre, the sums that dy needs,
+// sum q t and sum q t h_post, are linear in c1 and c2, so all sums over the row's data are taken at once and combined:
+//   sum q t h_post = sum q h_post (dr + rstd a) - rstd (c1 sum q h_post + c2 sum q h_post h_pre).
+//
+// PAIR: a row is split between the two blocks of a cluster (D > 8192); partial sums go to both blocks' shared memory.
+// LAYER: either norm subtracts a mean (more sums).  WREG: weights in registers, else in shared memory.
+template <typename RT, bool LAYER, bool PAIR>
+__global__ void __launch_bounds__(BWD_THREADS, 1) block_norm_bwd_kernel(const __grid_constant__ BwdArgs a) {
+  constexpr bool WREG = !LAYER;
+  constexpr int NS = LAYER ? 8 : 4;                 // sums per row
+  constexpr int RP = sizeof(RT) / 2;                // 16-byte pieces of a residual vector
+  constexpr int PIECES = 2 + 2 * RP;                // y, du, r, dr
+  extern __shared__ __align__(16) uint8_t smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int team = warp / a.warps, first_warp = team * a.warps;
+  const int tl = (warp - first_warp) * 32 + lane, TL = a.warps * 32;
+  uint32_t rank = 0;
+  if (PAIR) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const int unit = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, units = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
+  const int half = PAIR ? (a.D / 8 + 1) / 2 * 8 : 0;                 // channels of the first block of a pair
+  const int c_begin = (int)rank * half, c_end = (PAIR && rank == 0) ? half : a.D;
+
+  float *red = reinterpret_cast<float *>(smem);                      // [2][2 blocks][16 warps][NS]
+  constexpr int RED_BYTES = 2 * 2 * 16 * 8 * 4;
+  float4 *wsm = reinterpret_cast<float4 *>(smem + RED_BYTES);        // [q, w_pre][2 vectors][2 halves][TL]
+  const int w_bytes = WREG ? 0 : 8 * TL * 16;
+  uint8_t *ring = smem + RED_BYTES + w_bytes;
+  const uint32_t ring_u32 = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
+  const int nthreads = a.warps * a.teams * 32;
+  const int stage_bytes = 2 * PIECES * nthreads * 16;
+
+  pdl_launch_dependents();
+  pdl_wait();
+
+  int col[2];
+  bool act[2];
+  float qreg[WREG ? 2 : 1][8], wreg[WREG ? 2 : 1][8];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    col[j] = c_begin + (j * TL + tl) * 8;
+    act[j] = col[j] < c_end;
+    float q[8], w[8], g[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) q[k] = w[k] = 0.f;
+    if (act[j]) {
+      if (a.y) {
+        weights8(a.w_post, col[j], 1.f, q);
+        weights8(a.gate, col[j], 1.f, g);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) q[k] *= a.beta * g[k];
+      }
+      if (a.pre_has) weights8(a.w_pre, col[j], 1.f, w);
+    }
+    if (WREG) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) { qreg[j][k] = q[k]; wreg[j][k] = w[k]; }
+    } else if (team == 0) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        wsm[(0 + j * 2 + h) * TL + tl] = make_float4(q[4 * h], q[4 * h + 1], q[4 * h + 2], q[4 * h + 3]);
+        wsm[(4 + j * 2 + h) * TL + tl] = make_float4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]);
+      }
+    }
+  }
+  if (!WREG) __syncthreads();
+  if (PAIR) {   // the other block runs before anything is written to its shared memory
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  auto weights = [&](int j, float (&q)[8], float (&w)[8]) {
+    if (WREG) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) { q[k] = qreg[j][k]; w[k] = wreg[j][k]; }
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float4 fq = wsm[(0 + j * 2 + h) * TL + tl], fw = wsm[(4 + j * 2 + h) * TL + tl];
+        q[4 * h] = fq.x; q[4 * h + 1] = fq.y; q[4 * h + 2] = fq.z; q[4 * h + 3] = fq.w;
+        w[4 * h] = fw.x; w[4 * h + 1] = fw.y; w[4 * h + 2] = fw.z; w[4 * h + 3] = fw.w;
+      }
+    }
+  };
+
+  const long long first = (long long)unit * a.teams + team, step = (long long)units * a.teams;
+  auto slot = [&](int stage, int j, int piece) { return stage * stage_bytes + ((j * PIECES + piece) * nthreads + (int)threadIdx.x) * 16; };
+  auto fetch = [&](long long row, int stage) {
+    if (row < a.M) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (!act[j]) continue;
+        const long long at = row * a.D + col[j];
+        if (a.y) cp_async16(ring_u32 + slot(stage, j, 0), a.y + at);
+        if (a.pre_has) {
+          cp_async16(ring_u32 + slot(stage, j, 1), a.du + at);
+#pragma unroll
+          for (int p = 0; p < RP; ++p)
+            cp_async16(ring_u32 + slot(stage, j, 2 + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.r) + at) + 16 * p);
+        }
+        if (a.dr) {
+#pragma unroll
+          for (int p = 0; p < RP; ++p)
+            cp_async16(ring_u32 + slot(stage, j, 2 + RP + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.dr) + at) + 16 * p);
+        }
+      }
+    }
+    cp_async_commit();
+  };
+  auto piece8 = [&](int stage, int j, int piece, bool there, float (&f)[8]) {   // one bf16 vector
+    if (!there) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) f[k] = 0.f;
+    } else {
+      widen8(*reinterpret_cast<const uint4 *>(ring + slot(stage, j, piece)), f);
+    }
+  };
+  auto resid8 = [&](int stage, int j, int piece, bool there, float (&f)[8]) {
+    if (RP == 1 || !there) {
+      piece8(stage, j, piece, there, f);
+    } else {
+      const float4 lo = *reinterpret_cast<const float4 *>(ring + slot(stage, j, piece)),
+                   hi = *reinterpret_cast<const float4 *>(ring + slot(stage, j, piece + 1));
+      f[0] = lo.x; f[1] = lo.y; f[2] = lo.z; f[3] = lo.w;
+      f[4] = hi.x; f[5] = hi.y; f[6] = hi.z; f[7] = hi.w;
+    }
+  };
+
+  float sumA[2][8], sumC[2][8], sumB[LAYER ? 2 : 1][8], sumE[LAYER ? 2 : 1][8];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      sumA[j][k] = sumC[j][k] = 0.f;
+      if (LAYER) sumB[j][k] = sumE[j][k] = 0.f;
+    }
+  const bool has_y = a.y != nullptr, has_dr = a.dr != nullptr, has_pre = a.pre_has != 0;
+  const float inv_d = 1.0f / (float)a.D;
+  int turn = 0;
+  for (int s = 0; s + 1 < a.stages; ++s) fetch(first + s * step, s);
+  int stage = 0, next_stage = a.stages - 1;
+  // PAIR: both blocks walk the same rows, so their barriers match
+  for (long long row = first; row < a.M; row += step) {
+    fetch(row + (a.stages - 1) * step, next_stage);
+    if (++next_stage == a.stages) next_stage = 0;
+    float4 st = a.stats ? __ldg(a.stats + row) : make_float4(0.f, 0.f, 0.f, 0.f);
+    if (!a.post_has) { st.x = 0.f; st.y = 1.f; }      // h_post = y
+    if (!has_pre) { st.z = 0.f; st.w = 0.f; }
+    cp_async_wait(a.stages - 1);
+
+    float s[NS];
+#pragma unroll
+    for (int k = 0; k < NS; ++k) s[k] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (!act[j]) continue;
+      float q[8], w[8], y[8], du[8], r[8], dr[8];
+      weights(j, q, w);
+      piece8(stage, j, 0, has_y, y);
+      piece8(stage, j, 1, has_pre, du);
+      resid8(stage, j, 2, has_pre, r);
+      resid8(stage, j, 2 + RP, has_dr, dr);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float hp = (y[k] - st.x) * st.y, hr = (r[k] - st.z) * st.w, av = du[k] * w[k];
+        const float z = q[k] * fmaf(st.w, av, dr[k]), qh = q[k] * hp;
+        s[0] = fmaf(av, hr, s[0]);
+        s[1] = fmaf(z, hp, s[1]);
+        s[2] = fmaf(qh, hr, s[2]);
+        if (LAYER) {
+          s[3] += av;
+          s[4] += z;
+          s[5] = fmaf(q[k], hr, s[5]);
+          s[6] += q[k];
+          s[7] += qh;
+        }
+      }
+    }
+    if (PAIR) {
+#pragma unroll
+      for (int k = 0; k < NS; ++k) s[k] = warp_sum(s[k]);
+      float *buf = red + turn * (2 * 16 * 8);
+      turn ^= 1;
+      if (lane < 2) {   // lane 0 writes to block 0 of the pair, lane 1 to block 1
+        const uint32_t local = static_cast<uint32_t>(__cvta_generic_to_shared(buf + (rank * 16 + warp) * NS));
+        uint32_t remote;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(lane));
+#pragma unroll
+        for (int k = 0; k < NS; k += 4)
+          asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(remote + 4 * k), "f"(s[k]), "f"(s[k + 1]), "f"(s[k + 2]), "f"(s[k + 3]) : "memory");
+      }
+      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+#pragma unroll
+      for (int k = 0; k < NS; ++k) s[k] = 0.f;
+      for (int q = 0; q < 2; ++q)
+        for (int i = 0; i < a.warps; ++i)
+#pragma unroll
+          for (int k4 = 0; k4 < NS / 4; ++k4) {
+            const float4 f = *reinterpret_cast<const float4 *>(buf + (q * 16 + i) * NS + 4 * k4);
+            s[4 * k4] += f.x; s[4 * k4 + 1] += f.y; s[4 * k4 + 2] += f.z; s[4 * k4 + 3] += f.w;
+          }
+    } else {
+      team_sum<NS>(s, a.warps, first_warp, warp, lane, 1 + team, red, turn);
+    }
+    const float c2 = s[0] * inv_d;
+    float c1 = 0.f, m1 = 0.f, m2;
+    if (LAYER) {
+      c1 = a.pre_layer ? s[3] * inv_d : 0.f;
+      m1 = a.post_layer ? (s[4] - st.w * (c1 * s[6] + c2 * s[5])) * inv_d : 0.f;
+      m2 = (s[1] - st.w * (c1 * s[7] + c2 * s[2])) * inv_d;
+    } else {
+      m2 = (s[1] - st.w * (c2 * s[2])) * inv_d;
+    }
+    if (!a.post_has) m2 = 0.f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (!act[j]) continue;
+      float q[8], w[8], y[8], du[8], r[8], dr[8];
+      weights(j, q, w);
+      piece8(stage, j, 0, has_y, y);
+      piece8(stage, j, 1, has_pre, du);
+      resid8(stage, j, 2, has_pre, r);
+      resid8(stage, j, 2 + RP, has_dr, dr);
+      float dy[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float hp = (y[k] - st.x) * st.y, hr = (r[k] - st.z) * st.w;
+        const float t = fmaf(st.w, fmaf(-hr, c2, fmaf(du[k], w[k], -c1)), dr[k]);
+        sumA[j][k] = fmaf(t, hp, sumA[j][k]);
+        sumC[j][k] = fmaf(du[k], hr, sumC[j][k]);
+        if (LAYER) {
+          sumB[j][k] += t;
+          sumE[j][k] += du[k];
+        }
+        dr[k] = a.alpha * t;
+        dy[k] = st.y * fmaf(-hp, m2, fmaf(q[k], t, -m1));
+      }
+      const long long at = row * a.D + col[j];
+      if (a.dx) store8(static_cast<RT *>(a.dx) + at, dr);
+      if (a.dy) store8(a.dy + at, dy);
+    }
+    if (++stage == a.stages) stage = 0;
+  }
+  cp_async_wait(0);
+
+  // Channel sums of the block: teams added in ascending order.
+  __syncthreads();
+  float *acc = reinterpret_cast<float *>(ring);   // [team][vector][half][TL] float4, one sum at a time
+  constexpr int NACC = LAYER ? 4 : 2;
+#pragma unroll
+  for (int q = 0; q < NACC; ++q) {
+    float4 *mine = reinterpret_cast<float4 *>(acc) + team * (4 * TL);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float *p = q == 0 ? &sumA[j][4 * h] : q == 1 ? &sumC[j][4 * h] : q == 2 ? &sumB[LAYER ? j : 0][4 * h] : &sumE[LAYER ? j : 0][4 * h];
+        mine[(j * 2 + h) * TL + tl] = make_float4(p[0], p[1], p[2], p[3]);
+      }
+    __syncthreads();
+    if (team == 0) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (!act[j]) continue;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float4 v = reinterpret_cast<float4 *>(acc)[(j * 2 + h) * TL + tl];
+          for (int t = 1; t < a.teams; ++t) {
+            const float4 o = reinterpret_cast<float4 *>(acc)[(t * 4 + j * 2 + h) * TL + tl];
+            v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+          }
+          *reinterpret_cast<float4 *>(a.partial + ((long long)unit * 4 + q) * a.D + col[j] + 4 * h) = v;
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+struct FinalArgs {
+  const float *partial;
+  int units, D, layer;
+  const float *w_post, *b_post, *gate;
+  float beta;
+  int post_has;
+  float *dw_post, *db_post, *dgate, *dw_pre, *db_pre;
+};
+
+// Adds the blocks' channel sums (in ascending order per group of blocks, then the groups in ascending order) and forms
+// the vectors' gradients.  32 channels per block, 8 groups.
+__global__ void __launch_bounds__(256) block_norm_final_kernel(const __grid_constant__ FinalArgs a) {
+  __shared__ float red[4][8][32];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
+  const int col = blockIdx.x * 32 + c;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (col < a.D) {
+    for (int u = g; u < a.units; u += 8) {
+      const float *p = a.partial + (long long)u * 4 * a.D + col;
+      s[0] += p[0];
+      s[1] += p[a.D];
+      if (a.layer) {
+        s[2] += p[2ll * a.D];
+        s[3] += p[3ll * a.D];
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) red[k][g][c] = s[k];
+  __syncthreads();
+  if (g != 0 || col >= a.D) return;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    for (int q = 1; q < 8; ++q) s[k] += red[k][q][c];
+  const float gate = a.gate ? a.gate[col] : 1.f, w = (a.post_has && a.w_post) ? a.w_post[col] : 1.f;
+  const float b = a.b_post ? a.b_post[col] : 0.f;
+  if (a.dw_post) a.dw_post[col] = a.beta * gate * s[0];
+  if (a.db_post) a.db_post[col] = a.beta * gate * s[2];
+  if (a.dgate) a.dgate[col] = a.beta * fmaf(w, s[0], b * s[2]);
+  if (a.dw_pre) a.dw_pre[col] = s[1];
+  if (a.db_pre) a.db_pre[col] = s[3];
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+constexpr int SMEM_MAX = 227 * 1024;
+constexpr int RED_BYTES_HOST = 2 * 2 * 16 * 8 * 4;
+
+template <typename RT, int V>
+int launch_fwd(const FwdArgs &args, int warps, cudaStream_t stream) {
+  FwdArgs a = args;
+  a.warps = warps;
+  const int teams = warps >= 8 ? 1 : 8 / warps;
+  return launch_overlapped(block_norm_fwd_kernel<RT, V>, dim3((unsigned)cdiv(a.M, teams)), dim3(teams * warps * 32), 0, 1, stream, a);
+}
+
+template <typename RT, bool LAYER, bool PAIR>
+int launch_bwd(const BwdArgs &args, int sms, int *units, cudaStream_t stream) {
+  BwdArgs a = args;
+  const int width = PAIR ? (a.D / 8 + 1) / 2 * 8 : a.D;
+  a.warps = (int)cdiv(width, 512);
+  a.teams = PAIR ? 1 : 16 / a.warps;
+  const int threads = a.warps * a.teams * 32;
+  const int stage = 2 * (2 + 2 * (int)(sizeof(RT) / 2)) * threads * 16;
+  const int w_bytes = LAYER ? 8 * a.warps * 32 * 16 : 0;
+  a.stages = (SMEM_MAX - RED_BYTES_HOST - w_bytes) / stage;
+  if (a.stages > MAX_STAGES) a.stages = MAX_STAGES;
+  const int smem = RED_BYTES_HOST + w_bytes + a.stages * stage;
+  int64_t n = cdiv(a.M, a.teams);
+  const int cap = PAIR ? sms / 2 : sms;
+  if (n > cap) n = cap;
+  if (n > BWD_MAX_BLOCKS) n = BWD_MAX_BLOCKS;
+  if (n < 1) n = 1;    // no rows: zeros are written
+  *units = (int)n;
+  auto kernel = block_norm_bwd_kernel<RT, LAYER, PAIR>;
+  static std::atomic<bool> ready[64];
+  static std::mutex setup;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return report_cuda(e);
+  if (!ready[dev & 63].load(std::memory_order_acquire)) {
+    std::lock_guard<std::mutex> lock(setup);
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
+    if (e != cudaSuccess) return report_cuda(e);
+    ready[dev & 63].store(true, std::memory_order_release);
+  }
+  return launch_overlapped(kernel, dim3((unsigned)(PAIR ? 2 * n : n)), dim3(threads), smem, PAIR ? 2 : 1, stream, a);
+}
+
+bool norm_kind(int k) { return k == OSDP_NORM_NONE || k == OSDP_NORM_RMS || k == OSDP_NORM_LAYER; }
+
+int check_shape(int64_t M, int64_t D, int resid_dtype, int post, int pre) {
+  if (M < 0 || D <= 0 || M > ((int64_t)1 << 31) - 1) return OSDP_ERR_BAD_SHAPE;
+  if (D & 7) return OSDP_ERR_ALIGNMENT;
+  if (D > OSDP_BLOCK_NORM_MAX_D) return OSDP_ERR_UNSUPPORTED;
+  if (resid_dtype != OSDP_DTYPE_BF16 && resid_dtype != OSDP_DTYPE_FP32) return OSDP_ERR_UNSUPPORTED;
+  if (!norm_kind(post) || !norm_kind(pre)) return OSDP_ERR_UNSUPPORTED;
+  return OSDP_OK;
+}
+
+}  // namespace
+}  // namespace osdp
+
+using namespace osdp;
+
+extern "C" {
+
+int osdp_block_norm_fwd(const void *x, const void *y, int64_t M, int64_t D, int resid_dtype, int post, const float *w_post,
+                        const float *b_post, double eps_post, const float *gate, double alpha, double beta, int pre,
+                        const float *w_pre, const float *b_pre, double eps_pre, void *r, void *u, float *u_scale,
+                        float *stats, void *stream) {
+  const int rc = check_shape(M, D, resid_dtype, post, pre);
+  if (rc) return rc;
+  if (!std::isfinite(alpha) || !std::isfinite(beta)) return OSDP_ERR_UNSUPPORTED;
+  if ((post && !(eps_post >= 0.0 && std::isfinite(eps_post))) || (pre && !(eps_pre >= 0.0 && std::isfinite(eps_pre)))) return OSDP_ERR_UNSUPPORTED;
+  if ((b_post && post != OSDP_NORM_LAYER) || (b_pre && pre != OSDP_NORM_LAYER)) return OSDP_ERR_UNSUPPORTED;
+  if (M == 0) return OSDP_OK;
+  if (!x || (pre && !u) || (!r && !pre)) return OSDP_ERR_NULL_POINTER;
+  const uintptr_t ra = resid_dtype == OSDP_DTYPE_FP32 ? 32 : 16;
+  if (!aligned_to(x, ra) || !aligned_to(r, ra) || !aligned_to(y, 16) || !aligned_to(u, u_scale ? 8 : 16) || !aligned_to(u_scale, 4) ||
+      !aligned_to(stats, 16) || !aligned_to(w_post, 16) || !aligned_to(b_post, 16) || !aligned_to(gate, 16) || !aligned_to(w_pre, 16) ||
+      !aligned_to(b_pre, 16))
+    return OSDP_ERR_ALIGNMENT;
+  FwdArgs a;
+  a.x = x;
+  a.y = static_cast<const __nv_bfloat16 *>(y);
+  a.r = r;
+  a.u = u;
+  a.u_scale = u_scale;
+  a.stats = reinterpret_cast<float4 *>(stats);
+  a.gate = gate;
+  a.alpha = (float)alpha;
+  a.beta = (float)beta;
+  a.post = RowNorm{post != OSDP_NORM_NONE, post == OSDP_NORM_LAYER, (float)eps_post, post ? w_post : nullptr, b_post};
+  a.pre = RowNorm{pre != OSDP_NORM_NONE, pre == OSDP_NORM_LAYER, (float)eps_pre, w_pre, b_pre};
+  a.M = M;
+  a.D = (int)D;
+  a.warps = 0;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  // Few rows: one vector per lane, as many warps to a row as it has vectors, for the shortest chain of instructions.
+  const bool few = D <= 8192 && M * cdiv(D, 256) <= 148 * 8;
+  if (few)
+    return resid_dtype == OSDP_DTYPE_FP32 ? launch_fwd<float, 1>(a, (int)cdiv(D, 256), s) : launch_fwd<__nv_bfloat16, 1>(a, (int)cdiv(D, 256), s);
+  return resid_dtype == OSDP_DTYPE_FP32 ? launch_fwd<float, 4>(a, (int)cdiv(D, 1024), s) : launch_fwd<__nv_bfloat16, 4>(a, (int)cdiv(D, 1024), s);
+}
+
+int osdp_block_norm_workspace_bytes(int64_t M, int64_t D, size_t *bytes) {
+  if (!bytes) return OSDP_ERR_NULL_POINTER;
+  const int rc = check_shape(M, D, OSDP_DTYPE_BF16, 0, 0);
+  if (rc) return rc;
+  *bytes = 256 + (size_t)BWD_MAX_BLOCKS * 4 * (size_t)D * sizeof(float);
+  return OSDP_OK;
+}
+
+int osdp_block_norm_bwd(const void *dr, const void *du, const void *y, const void *r, const float *stats, int64_t M, int64_t D,
+                        int resid_dtype, int post, const float *w_post, const float *b_post, const float *gate, double alpha,
+                        double beta, int pre, const float *w_pre, void *dx, void *dy, float *dw_post, float *db_post,
+                        float *dgate, float *dw_pre, float *db_pre, void *ws, size_t ws_bytes, void *stream) {
+  int rc = check_shape(M, D, resid_dtype, post, pre);
+  if (rc) return rc;
+  if (!std::isfinite(alpha) || !std::isfinite(beta)) return OSDP_ERR_UNSUPPORTED;
+  if (((b_post || db_post) && post != OSDP_NORM_LAYER) || (db_pre && pre != OSDP_NORM_LAYER)) return OSDP_ERR_UNSUPPORTED;
+  if ((dw_post && !post) || (dw_pre && !pre)) return OSDP_ERR_UNSUPPORTED;
+  if (!ws || (M > 0 && ((pre && (!du || !r)) || ((pre || (y && post)) && !stats) || (!y && (dy || dw_post || db_post || dgate)) || (!pre && !dr))))
+    return OSDP_ERR_NULL_POINTER;
+  const uintptr_t ra = resid_dtype == OSDP_DTYPE_FP32 ? 32 : 16;
+  if (!aligned_to(dr, ra) || !aligned_to(r, ra) || !aligned_to(dx, ra) || !aligned_to(du, 16) || !aligned_to(y, 16) || !aligned_to(dy, 16) ||
+      !aligned_to(stats, 16) || !aligned_to(w_post, 16) || !aligned_to(b_post, 16) || !aligned_to(gate, 16) || !aligned_to(w_pre, 16) ||
+      !aligned_to(dw_post, 4) || !aligned_to(db_post, 4) || !aligned_to(dgate, 4) || !aligned_to(dw_pre, 4) || !aligned_to(db_pre, 4) ||
+      !aligned_to(ws, 256))
+    return OSDP_ERR_ALIGNMENT;
+  size_t need = 0;
+  rc = osdp_block_norm_workspace_bytes(M, D, &need);
+  if (rc) return rc;
+  if (ws_bytes < need) return OSDP_ERR_WORKSPACE_TOO_SMALL;
+  int sms = 0;
+  rc = sm_count(&sms);
+  if (rc) return rc;
+  BwdArgs a;
+  a.dr = dr;
+  a.du = static_cast<const __nv_bfloat16 *>(du);
+  a.y = static_cast<const __nv_bfloat16 *>(y);
+  a.r = r;
+  a.stats = reinterpret_cast<const float4 *>(stats);
+  a.w_post = post ? w_post : nullptr;
+  a.gate = gate;
+  a.w_pre = w_pre;
+  a.alpha = (float)alpha;
+  a.beta = (float)beta;
+  a.post_has = post != OSDP_NORM_NONE;
+  a.post_layer = post == OSDP_NORM_LAYER;
+  a.pre_has = pre != OSDP_NORM_NONE;
+  a.pre_layer = pre == OSDP_NORM_LAYER;
+  a.dx = dx;
+  a.dy = static_cast<__nv_bfloat16 *>(dy);
+  a.partial = reinterpret_cast<float *>(static_cast<char *>(ws) + 256);
+  a.M = M;
+  a.D = (int)D;
+  a.warps = a.teams = a.stages = 0;
+  const bool layer = a.post_layer || a.pre_layer || db_post || db_pre, pair = D > 8192;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int units = 0;
+#define OSDP_BWD(RT, LAYER) (pair ? launch_bwd<RT, LAYER, true>(a, sms, &units, s) : launch_bwd<RT, LAYER, false>(a, sms, &units, s))
+  if (resid_dtype == OSDP_DTYPE_FP32) rc = layer ? OSDP_BWD(float, true) : OSDP_BWD(float, false);
+  else rc = layer ? OSDP_BWD(__nv_bfloat16, true) : OSDP_BWD(__nv_bfloat16, false);
+#undef OSDP_BWD
+  if (rc) return rc;
+  if (!dw_post && !db_post && !dgate && !dw_pre && !db_pre) return OSDP_OK;
+  FinalArgs f;
+  f.partial = a.partial;
+  f.units = units;
+  f.D = (int)D;
+  f.layer = layer;
+  f.w_post = a.w_post;
+  f.b_post = b_post;
+  f.gate = gate;
+  f.beta = a.beta;
+  f.post_has = a.post_has;
+  f.dw_post = dw_post;
+  f.db_post = db_post;
+  f.dgate = dgate;
+  f.dw_pre = dw_pre;
+  f.db_pre = db_pre;
+  return launch_overlapped(block_norm_final_kernel, dim3((unsigned)cdiv(D, 32)), dim3(256), 0, 1, s, f);
+}
+
+}  // extern "C"

@@ -55,6 +55,8 @@ struct Epilogue {
   __nv_bfloat16 *act_out;    // [P,Q] or null: also write act(gz) here
   long long ld_act_out;
   float scale;               // the accumulator is multiplied by this before anything else (fp8 operands' scales)
+  const float *row_scale;    // int8 operands: [P] and [Q], the int32 accumulator is multiplied by both
+  const float *col_scale;
 };
 
 struct GemmParams {
@@ -262,6 +264,25 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_
         ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+// int8 x int8 -> int32
+template <bool CTA2>
+__device__ __forceinline__ void umma_i8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                        uint32_t accumulate) {
+  if (CTA2)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
 // COLL: use of the tensor core's collector buffer for the A operand.  0: none.  1: this MMA leaves its A operand in
 // the buffer (fill); 2: this MMA takes A from the buffer, for the last time (lastuse).  The 256 x 512 tile issues two
 // MMAs per k-step that share A (one per 256-column group): the second does not read A from shared memory again.
@@ -336,6 +357,20 @@ __device__ __forceinline__ void scale_acc(uint32_t (&v)[32], float scale) {
   }
 }
 
+// int8 operands: int32 accumulators of one row and 32 columns -> fp32, times the row's and the columns' scales.
+// Columns come in groups of eight that lie wholly inside or outside the matrix (Q is a multiple of 8).
+__device__ __forceinline__ void dequantise_acc(uint32_t (&v)[32], float row_scale, const float *col_scale, int col, int col_end) {
+#pragma unroll
+  for (int g = 0; g < 8; ++g) {
+    float4 c = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (col + 4 * g < col_end) c = *reinterpret_cast<const float4 *>(col_scale + col + 4 * g);
+    v[4 * g + 0] = __float_as_uint((float)(int)v[4 * g + 0] * row_scale * c.x);
+    v[4 * g + 1] = __float_as_uint((float)(int)v[4 * g + 1] * row_scale * c.y);
+    v[4 * g + 2] = __float_as_uint((float)(int)v[4 * g + 2] * row_scale * c.z);
+    v[4 * g + 3] = __float_as_uint((float)(int)v[4 * g + 3] * row_scale * c.w);
+  }
+}
+
 // ------------------------------------------------------------------------------------------------
 // Descriptors
 
@@ -364,9 +399,13 @@ __device__ __forceinline__ constexpr uint32_t desc_k_advance() {
   return MN_MAJOR ? ((32 / EB) * 128) : 32;
 }
 // Instruction descriptor: bf16 x bf16 -> fp32, M = 128, N = BN.
-// (operand format field: 1 = bf16 under kind::f16, 0 = e4m3 under kind::f8f6f4; accumulator fp32)
-template <int UM, int BN, bool A_MN, bool B_MN, int EB = 2>
+// (operand format field: 1 = bf16 under kind::f16, 0 = e4m3 under kind::f8f6f4; accumulator fp32.  I8: format 1 =
+// signed 8-bit integers under kind::i8, accumulator field 2 = int32)
+template <int UM, int BN, bool A_MN, bool B_MN, int EB = 2, bool I8 = false>
 __device__ __forceinline__ constexpr uint32_t make_idesc() {
+  if (I8)
+    return (2u << 4) | (1u << 7) | (1u << 10) | ((A_MN ? 1u : 0u) << 15) | ((B_MN ? 1u : 0u) << 16) |
+           ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(UM >> 4) << 24);
   return (1u << 4) | ((EB == 2 ? 1u : 0u) << 7) | ((EB == 2 ? 1u : 0u) << 10) | ((A_MN ? 1u : 0u) << 15) |
          ((B_MN ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(UM >> 4) << 24);
 }
@@ -663,7 +702,9 @@ __device__ __forceinline__ void epilogue8(const Epilogue &e, long long row, int 
 // of the B tile (BN/2 rows), holds the accumulator of its 128 rows in its own tensor memory and
 // runs its own epilogue.  Per CTA a stage is 32 KB instead of 48 KB (6 stages instead of 4) and
 // half as many B bytes cross from L2 to shared memory per flop.
-template <int BN, bool A_MN, bool B_MN, bool CTA2, bool HEAVY = false, int EB = 2>
+// I8: int8 operands with a scale per row and per column of the output (bf16 output, whole or concatenated, or summed
+// in tensor memory over all slices).
+template <int BN, bool A_MN, bool B_MN, bool CTA2, bool HEAVY = false, int EB = 2, bool I8 = false>
 __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kernel(const __grid_constant__ GemmParams p) {
   using SL = SmemLayout<BN, CTA2, HEAVY>;
   constexpr int BKE = 128 / EB;   // reduction elements per k-block
@@ -833,7 +874,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
     // ------------------------------------------------------------------ MMA issuer (even CTA of a pair)
     // One thread runs the whole role: it waits for a round of the ring (UNIT k-blocks), issues their MMAs and
     // hands the round back with one commit.
-    constexpr uint32_t idesc = make_idesc<TM, SL::UMMA_N, A_MN, B_MN, EB>();
+    constexpr uint32_t idesc = make_idesc<TM, SL::UMMA_N, A_MN, B_MN, EB, I8>();
     if (lane == 0) {
       int grp = 0;
       uint32_t phase = 0;
@@ -869,6 +910,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
                   if (EB == 2 && SL::NG == 2 && g == 0) umma_bf16<CTA2, 1>(d, ad, bd, idesc, acc);
                   else if (EB == 2 && SL::NG == 2 && g == 1) umma_bf16<CTA2, 2>(d, ad, bd, idesc, acc);
                   else if (EB == 2) umma_bf16<CTA2>(d, ad, bd, idesc, acc);
+                  else if (I8) umma_i8<CTA2>(d, ad, bd, idesc, acc);
                   else umma_f8<CTA2>(d, ad, bd, idesc, acc);
                 }
               }
@@ -1242,8 +1284,14 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
               if (BN >= 64) tmem_ld_x32(taddr + (uint32_t)(c * 64 + 32), hi);
               tmem_ld_wait();
               if (SL::NBUF == 1 && (c + 1 == (wg + 1) * ((BN + 63) / 64 / EG) || cbase + 64 >= w.col_end)) release_accumulator();
-              scale_acc(lo, p.epi.scale);
-              if (BN >= 64) scale_acc(hi, p.epi.scale);
+              if (I8) {
+                const float rs = row < w.row_end ? __ldg(p.epi.row_scale + row) : 0.f;
+                dequantise_acc(lo, rs, p.epi.col_scale, cbase, w.col_end);
+                if (BN >= 64) dequantise_acc(hi, rs, p.epi.col_scale, cbase + 32, w.col_end);
+              } else {
+                scale_acc(lo, p.epi.scale);
+                if (BN >= 64) scale_acc(hi, p.epi.scale);
+              }
 #pragma unroll
               for (int j = 0; j < 32; ++j) { v[j] = lo[j]; v[32 + j] = hi[j]; }
             }

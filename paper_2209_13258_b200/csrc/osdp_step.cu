@@ -1,0 +1,421 @@
+// The optimiser step of the flat parameters: global gradient norm with its clipping coefficient, and AdamW over
+// many tensors in one launch, with 32-bit or 8-bit states.
+//
+//   g' = c g                       c: clipping coefficient (1 without)
+//   m  = b1 m + (1 - b1) g'        v = b2 v + (1 - b2) g'^2
+//   p  = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v) / sqrt(1 - b2^t) + eps)
+//
+// 8-bit states: 256 consecutive elements share one fp32 scale = (largest magnitude) / 448 and are kept as e4m3 codes
+// (448 is the largest e4m3 value).  The second moment is kept as its root, which halves the range that the codes have
+// to cover (2^-9 ... 448 of a root is 10 decades of v), and a root above zero is never rounded to zero: that would turn
+// a small second moment into a huge step.  The step itself uses the unrounded m and v.
+#include "../../include/osdp.h"
+
+#include <cmath>
+
+#include "osdp_internal.h"
+#include "osdp_vec.cuh"
+
+namespace osdp {
+namespace {
+
+constexpr int QB = OSDP_ADAMW_BLOCK;       // elements per 8-bit scale; one warp works on one such block
+constexpr int THREADS = 256;
+constexpr int CHUNK = 4096;                // elements of one tensor that a thread block works on
+constexpr int STATUS_BYTES = 256;
+constexpr float TINY = 7.888609052210118e-31f;   // 2^-100: a block whose largest magnitude is below it is stored as zeros
+
+struct Entry {
+  void *param;
+  const void *grad;
+  long long numel;
+  long long state;     // element offset in the flat states
+  float decay;         // 1 - lr * weight_decay
+  float size;          // lr / (1 - b1^t)
+  int first_chunk;
+  int aligned;         // param and grad allow eight-element accesses
+};
+// Tensors of one launch.  The table travels as a kernel parameter (up to 32 KB): no copy to the device, nothing to
+// keep alive, and a stream capture takes it along.  Two sizes, so that a step over a few tensors does not pay for
+// the launch of a full table.
+constexpr int TABLE_SMALL = 48, TABLE_LARGE = 640;
+template <int MAXT>
+struct Table {
+  Entry e[MAXT];
+  int n;
+  int chunks;
+};
+
+template <int MAXT>
+__device__ __forceinline__ int find_entry(const Table<MAXT> &t, int chunk) {
+  int lo = 0, hi = t.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (t.e[mid].first_chunk <= chunk) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+struct Hyper {
+  float b1, one_minus_b1, b2, one_minus_b2, eps;
+  float root_scale;    // 1 / sqrt(1 - b2^t)
+};
+
+// 256 elements -> codes and their scale.  ROOT: elements above zero keep at least the smallest code.
+template <bool ROOT>
+__device__ __forceinline__ void quantise_block(const float (&x)[8], uint8_t *codes, float *scale, int lane) {
+  float top = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t a = __float_as_uint(x[j]) & 0x7FFFFFFFu;
+    top = __uint_as_float(max(__float_as_uint(top), a));
+  }
+  top = warp_max_abs(top);
+  const bool live = !(top < TINY);
+  const float inv = live ? __fdiv_rn(448.0f, top) : 0.0f;
+  float c[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    c[j] = __fmul_rn(x[j], inv);
+    if (ROOT && live && x[j] > 0.f) c[j] = fmaxf(c[j], 0.001953125f);   // 2^-9
+  }
+  *reinterpret_cast<uint2 *>(codes + lane * 8) = encode_e4m3x8(c);
+  if (lane == 0) *scale = live ? __fmul_rn(top, 1.0f / 448.0f) : 0.0f;
+}
+
+// Each warp takes blocks of 256 consecutive elements, eight per lane, so that every array is read and written in
+// whole lines and a block's scale is a warp reduction.  HBM-bound: nothing is read twice.
+template <typename T, bool MASTER, bool E4M3, int MAXT>
+__global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ Table<MAXT> t, const Hyper h, float *master,
+                                                        void *state_m, void *state_v, float *scale_m, float *scale_v,
+                                                        const float *__restrict__ clip) {
+  pdl_launch_dependents();
+  const Entry &e = t.e[find_entry(t, blockIdx.x)];
+  const long long base = (long long)(blockIdx.x - e.first_chunk) * CHUNK;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_wait();
+  float coef = 1.0f;
+  if (clip) {
+    coef = clip[1];
+    if (!isfinite(coef)) return;   // the gradient's norm is not a number: nothing is updated
+  }
+  T *param = static_cast<T *>(e.param);
+  const T *grad = static_cast<const T *>(e.grad);
+#pragma unroll 2
+  for (int it = 0; it < CHUNK / (THREADS / 32 * QB); ++it) {
+    const long long blk = base + (it * (THREADS / 32) + warp) * QB;
+    if (blk >= e.numel) break;
+    const long long i = blk + lane * 8;                       // this lane's first element, in the tensor
+    const long long si = e.state + i;                         // ... and in the flat states (whole blocks are there)
+    const bool whole = e.aligned && i + 8 <= e.numel;
+    float w[8], g[8], m[8], v[8];
+    if (whole) {
+      load8(grad + i, g);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) g[j] = i + j < e.numel ? to_f32(grad[i + j]) : 0.f;
+    }
+    if (MASTER) {
+      load8(master + si, w);
+    } else if (whole) {
+      load8(param + i, w);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = i + j < e.numel ? to_f32(param[i + j]) : 0.f;
+    }
+    uint8_t *m8 = static_cast<uint8_t *>(state_m) + (e.state + blk), *v8 = static_cast<uint8_t *>(state_v) + (e.state + blk);
+    const long long sb = (e.state + blk) / QB;
+    if (E4M3) {
+      const uint2 cm = *reinterpret_cast<const uint2 *>(m8 + lane * 8), cv = *reinterpret_cast<const uint2 *>(v8 + lane * 8);
+      const float fm = scale_m[sb], fv = scale_v[sb];
+      decode_e4m3x8(cm, m);
+      decode_e4m3x8(cv, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        m[j] = __fmul_rn(m[j], fm);
+        v[j] = __fmul_rn(v[j], fv);
+        v[j] = __fmul_rn(v[j], v[j]);
+      }
+    } else {
+      load8(static_cast<const float *>(state_m) + si, m);
+      load8(static_cast<const float *>(state_v) + si, v);
+    }
+    float root[8];
+    // Products and sums one rounding each, never contracted: the states are then a function of the inputs alone,
+    // whatever the compiler does, and 8-bit codes do not depend on it.
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float gc = clip ? __fmul_rn(g[j], coef) : g[j];
+      m[j] = __fadd_rn(__fmul_rn(m[j], h.b1), __fmul_rn(gc, h.one_minus_b1));
+      v[j] = __fadd_rn(__fmul_rn(v[j], h.b2), __fmul_rn(__fmul_rn(gc, gc), h.one_minus_b2));
+      root[j] = __fsqrt_rn(v[j]);
+      const float den = fmaf(root[j], h.root_scale, h.eps);
+      w[j] = fmaf(w[j], e.decay, -__fdividef(m[j], den) * e.size);
+    }
+    if (MASTER) store8(master + si, w);
+    if (whole) {
+      store8(param + i, w);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (i + j < e.numel) param[i + j] = from_f32<T>(w[j]);
+    }
+    if (E4M3) {
+      quantise_block<false>(m, m8, scale_m + sb, lane);
+      quantise_block<true>(root, v8, scale_v + sb, lane);
+    } else {
+      store8(static_cast<float *>(state_m) + si, m);
+      store8(static_cast<float *>(state_v) + si, v);
+    }
+  }
+}
+
+// ---- gradient norm: one partial sum of squares per thread block, added in block order by the block that finishes
+// last (no floating-point atomics: the same gradients give the same bits).
+constexpr int NORM_BLOCKS = 592;   // 4 per SM
+
+template <typename T, int MAXT>
+__global__ void __launch_bounds__(THREADS) grad_norm_kernel(const __grid_constant__ Table<MAXT> t, float *partial, int first_partial,
+                                                            int total_partials, unsigned *ticket, float max_norm,
+                                                            float *__restrict__ out) {
+  __shared__ float red[THREADS / 32];
+  __shared__ bool last;
+  pdl_launch_dependents();
+  pdl_wait();
+  float acc[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+  for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    const Entry &e = t.e[find_entry(t, c)];
+    const long long base = (long long)(c - e.first_chunk) * CHUNK;
+    const T *grad = static_cast<const T *>(e.grad);
+#pragma unroll
+    for (int it = 0; it < CHUNK / (THREADS * 8); ++it) {
+      const long long i = base + (it * THREADS + threadIdx.x) * 8;
+      float g[8];
+      if (e.aligned && i + 8 <= e.numel) {
+        load8(grad + i, g);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] = i + j < e.numel ? to_f32(grad[i + j]) : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) acc[j] = fmaf(g[j], g[j], acc[j]);
+    }
+  }
+  float s = ((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7]));
+  s = warp_sum(s);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s = red[0];
+#pragma unroll
+    for (int k = 1; k < THREADS / 32; ++k) s += red[k];
+    partial[first_partial + blockIdx.x] = s;
+    __threadfence();
+    last = atomicAdd(ticket, 1u) == (unsigned)total_partials - 1u;
+  }
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  double d = 0.0;
+  for (int k = threadIdx.x; k < total_partials; k += THREADS) d += (double)__ldcg(partial + k);
+  __shared__ double sum[THREADS];
+  sum[threadIdx.x] = d;
+  __syncthreads();
+  for (int k = THREADS / 2; k > 0; k >>= 1) {
+    if (threadIdx.x < k) sum[threadIdx.x] += sum[threadIdx.x + k];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    const float norm = (float)sqrt(sum[0]);
+    out[0] = norm;
+    // a norm that is not finite has no coefficient: the step that reads NaN changes nothing
+    out[1] = !isfinite(norm) ? __int_as_float(0x7FC00000) : max_norm > 0.f ? fminf(max_norm / (norm + 1e-6f), 1.0f) : 1.0f;
+    *ticket = 0u;
+  }
+}
+
+int check_tensors(const osdp_adamw_tensor *t, int n, int dtype, bool need_param) {
+  if (n < 0) return OSDP_ERR_BAD_SHAPE;
+  if (n > 0 && !t) return OSDP_ERR_NULL_POINTER;
+  if (dtype != OSDP_DTYPE_BF16 && dtype != OSDP_DTYPE_FP32) return OSDP_ERR_UNSUPPORTED;
+  const uintptr_t es = dtype == OSDP_DTYPE_FP32 ? 4 : 2;
+  int64_t total = 0;
+  for (int i = 0; i < n; ++i) {
+    // 2^42 elements in all: the chunks of any table are then below 2^31
+    if (t[i].numel < 0 || t[i].numel > ((int64_t)1 << 42) - total) return OSDP_ERR_BAD_SHAPE;
+    total += t[i].numel;
+    if (t[i].numel == 0) continue;
+    if (!t[i].grad || (need_param && !t[i].param)) return OSDP_ERR_NULL_POINTER;
+    if (!aligned_to(t[i].grad, es) || (need_param && !aligned_to(t[i].param, es))) return OSDP_ERR_ALIGNMENT;
+    if (need_param && (t[i].state_offset < 0 || t[i].state_offset % QB)) return OSDP_ERR_ALIGNMENT;
+  }
+  return OSDP_OK;
+}
+
+// Fills tables with the tensors that have elements and hands each to launch(table, is_first, index of its first chunk).
+template <int MAXT, typename Fill, typename Launch>
+int for_each_table(const osdp_adamw_tensor *t, int n, int dtype, bool with_param, Fill fill, Launch launch) {
+  const uintptr_t vec = dtype == OSDP_DTYPE_FP32 ? 32 : 16;
+  Table<MAXT> tab;
+  int i = 0;
+  while (i < n) {
+    tab.n = 0;
+    int64_t chunks = 0;
+    for (; i < n && tab.n < MAXT; ++i) {
+      if (t[i].numel == 0) continue;
+      Entry &e = tab.e[tab.n++];
+      e.param = t[i].param;
+      e.grad = t[i].grad;
+      e.numel = t[i].numel;
+      e.state = t[i].state_offset;
+      e.first_chunk = (int)chunks;
+      e.aligned = aligned_to(t[i].grad, vec) && (!with_param || aligned_to(t[i].param, vec));
+      fill(t[i], e);
+      chunks += cdiv(t[i].numel, CHUNK);
+    }
+    if (tab.n == 0) break;
+    tab.chunks = (int)chunks;
+    const int rc = launch(tab);
+    if (rc) return rc;
+  }
+  return OSDP_OK;
+}
+
+template <typename T, bool MASTER, bool E4M3, int MAXT>
+int launch_adamw(const osdp_adamw_tensor *t, int n, int dtype, const Hyper &h, double beta1_t, float *master, void *m, void *v,
+                 float *sm, float *sv, const float *clip, cudaStream_t stream) {
+  return for_each_table<MAXT>(
+      t, n, dtype, true,
+      [&](const osdp_adamw_tensor &a, Entry &e) {
+        e.decay = (float)(1.0 - a.lr * a.weight_decay);
+        e.size = (float)(a.lr / (1.0 - beta1_t));
+      },
+      [&](const Table<MAXT> &tab) {
+        return launch_overlapped(adamw_kernel<T, MASTER, E4M3, MAXT>, dim3((unsigned)tab.chunks), dim3(THREADS), 0, 1, stream, tab, h,
+                                 master, m, v, sm, sv, clip);
+      });
+}
+
+template <typename T, bool MASTER, bool E4M3>
+int pick_table(const osdp_adamw_tensor *t, int n, int dtype, const Hyper &h, double b1t, float *master, void *m, void *v, float *sm,
+               float *sv, const float *clip, cudaStream_t stream) {
+  return n <= TABLE_SMALL ? launch_adamw<T, MASTER, E4M3, TABLE_SMALL>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream)
+                          : launch_adamw<T, MASTER, E4M3, TABLE_LARGE>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream);
+}
+
+template <typename T, int MAXT>
+int launch_norm(const osdp_adamw_tensor *t, int n, int dtype, float max_norm, float *out, float *partial, unsigned *ticket,
+                cudaStream_t stream) {
+  // the number of partial sums has to be known before the first launch
+  int total = 0;
+  auto blocks = [](int chunks) { return chunks < NORM_BLOCKS ? chunks : NORM_BLOCKS; };
+  auto none = [](const osdp_adamw_tensor &, Entry &) {};
+  int rc = for_each_table<MAXT>(t, n, dtype, false, none, [&](const Table<MAXT> &tab) { total += blocks(tab.chunks); return OSDP_OK; });
+  if (rc) return rc;
+  Table<MAXT> empty;
+  empty.n = 0;
+  empty.chunks = 0;
+  if (total == 0)   // no elements at all: the norm is zero
+    return launch_overlapped(grad_norm_kernel<T, MAXT>, dim3(1), dim3(THREADS), 0, 1, stream, empty, partial, 0, 1, ticket, max_norm, out);
+  int at = 0;
+  return for_each_table<MAXT>(t, n, dtype, false, none, [&](const Table<MAXT> &tab) {
+    const int b = blocks(tab.chunks);
+    const int first = at;
+    at += b;
+    return launch_overlapped(grad_norm_kernel<T, MAXT>, dim3((unsigned)b), dim3(THREADS), 0, 1, stream, tab, partial, first, total, ticket,
+                             max_norm, out);
+  });
+}
+
+size_t norm_workspace(int n) {
+  const size_t tables = (size_t)cdiv(n > 0 ? n : 1, TABLE_LARGE);
+  return STATUS_BYTES + tables * NORM_BLOCKS * sizeof(float);
+}
+
+}  // namespace
+}  // namespace osdp
+
+using namespace osdp;
+
+extern "C" {
+
+int osdp_adamw_layout(const int64_t *numel, int n, int64_t *state_offset, int64_t *state_elems) {
+  if (n < 0) return OSDP_ERR_BAD_SHAPE;
+  if ((n > 0 && !numel) || !state_elems) return OSDP_ERR_NULL_POINTER;
+  int64_t at = 0;
+  for (int i = 0; i < n; ++i) {
+    if (numel[i] < 0 || numel[i] > ((int64_t)1 << 42) - at) return OSDP_ERR_BAD_SHAPE;
+    if (state_offset) state_offset[i] = at;
+    at += cdiv(numel[i], QB) * QB;
+  }
+  *state_elems = at;
+  return OSDP_OK;
+}
+
+int osdp_grad_norm_workspace_bytes(int n_tensors, size_t *bytes) {
+  if (!bytes) return OSDP_ERR_NULL_POINTER;
+  if (n_tensors < 0) return OSDP_ERR_BAD_SHAPE;
+  *bytes = norm_workspace(n_tensors);
+  return OSDP_OK;
+}
+
+int osdp_grad_norm(const osdp_adamw_tensor *tensors, int n_tensors, int grad_dtype, float max_norm, float *out, void *ws,
+                   size_t ws_bytes, void *stream) {
+  const int rc = check_tensors(tensors, n_tensors, grad_dtype, false);
+  if (rc) return rc;
+  if (!out || !ws) return OSDP_ERR_NULL_POINTER;
+  if (std::isnan(max_norm)) return OSDP_ERR_UNSUPPORTED;
+  if (!aligned_to(ws, 256) || !aligned_to(out, 4)) return OSDP_ERR_ALIGNMENT;
+  if (ws_bytes < norm_workspace(n_tensors)) return OSDP_ERR_WORKSPACE_TOO_SMALL;
+  unsigned *ticket = reinterpret_cast<unsigned *>(static_cast<char *>(ws) + 64);
+  float *partial = reinterpret_cast<float *>(static_cast<char *>(ws) + STATUS_BYTES);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const bool small = n_tensors <= TABLE_SMALL;
+  if (grad_dtype == OSDP_DTYPE_FP32)
+    return small ? launch_norm<float, TABLE_SMALL>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s)
+                 : launch_norm<float, TABLE_LARGE>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s);
+  return small ? launch_norm<__nv_bfloat16, TABLE_SMALL>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s)
+               : launch_norm<__nv_bfloat16, TABLE_LARGE>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s);
+}
+
+int osdp_adamw_step(const osdp_adamw_tensor *tensors, int n_tensors, int param_dtype, int state_dtype, float *master,
+                    void *state_m, void *state_v, float *scale_m, float *scale_v, double beta1, double beta2, double eps,
+                    int64_t step, const float *clip, void *stream) {
+  int rc = check_tensors(tensors, n_tensors, param_dtype, true);
+  if (rc) return rc;
+  if (state_dtype != OSDP_DTYPE_FP32 && state_dtype != OSDP_DTYPE_E4M3) return OSDP_ERR_UNSUPPORTED;
+  const bool e4m3 = state_dtype == OSDP_DTYPE_E4M3;
+  if (step < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !std::isfinite(eps))
+    return OSDP_ERR_UNSUPPORTED;
+  int64_t total = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    if (!std::isfinite(tensors[i].lr) || !std::isfinite(tensors[i].weight_decay)) return OSDP_ERR_UNSUPPORTED;
+    total += tensors[i].numel;
+  }
+  if (total == 0) return OSDP_OK;
+  if (!state_m || !state_v || (e4m3 && (!scale_m || !scale_v))) return OSDP_ERR_NULL_POINTER;
+  if (!aligned_to(state_m, 32) || !aligned_to(state_v, 32) || !aligned_to(master, 32) || !aligned_to(scale_m, 4) ||
+      !aligned_to(scale_v, 4) || !aligned_to(clip, 4))
+    return OSDP_ERR_ALIGNMENT;
+  if (master && param_dtype != OSDP_DTYPE_BF16) return OSDP_ERR_UNSUPPORTED;   // fp32 parameters are their own master
+  Hyper h;
+  h.b1 = (float)beta1;
+  h.one_minus_b1 = (float)(1.0 - beta1);
+  h.b2 = (float)beta2;
+  h.one_minus_b2 = (float)(1.0 - beta2);
+  h.eps = (float)eps;
+  h.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+  const double b1t = std::pow(beta1, (double)step);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+#define OSDP_STEP(T, MASTER, E4M3) \
+  pick_table<T, MASTER, E4M3>(tensors, n_tensors, param_dtype, h, b1t, master, state_m, state_v, scale_m, scale_v, clip, s)
+  if (param_dtype == OSDP_DTYPE_FP32) return e4m3 ? OSDP_STEP(float, false, true) : OSDP_STEP(float, false, false);
+  if (master) return e4m3 ? OSDP_STEP(__nv_bfloat16, true, true) : OSDP_STEP(__nv_bfloat16, true, false);
+  return e4m3 ? OSDP_STEP(__nv_bfloat16, false, true) : OSDP_STEP(__nv_bfloat16, false, false);
+#undef OSDP_STEP
+}
+
+}  // extern "C"

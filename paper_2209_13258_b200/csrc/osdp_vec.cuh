@@ -1,0 +1,137 @@
+// Eight-element vectors in registers: loads, stores and conversions shared by the bandwidth-bound kernels.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace osdp {
+
+__device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// 32 bytes in one access (256-bit global accesses need a 32-byte aligned address).  The data of these kernels is
+// streamed: nothing of it is kept in L1.
+__device__ __forceinline__ void load32(const void *p, uint32_t (&w)[8]) {
+  asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+               : "l"(p)
+               : "memory");
+}
+__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+__device__ __forceinline__ uint4 load16(const void *p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ void widen8(const uint4 &u, float (&f)[8]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    f[2 * j] = __uint_as_float(w[j] << 16);
+    f[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ uint4 narrow8(const float (&f)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+    w[j] = *reinterpret_cast<const uint32_t *>(&h);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Eight consecutive elements of type T (__nv_bfloat16: 16-byte aligned, float: 32-byte aligned) <-> fp32.
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, float (&f)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    widen8(load16(p), f);
+  } else {
+    uint32_t w[8];
+    load32(p, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(w[j]);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store8(T *p, const float (&f)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4 *>(p) = narrow8(f);
+  } else {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = __float_as_uint(f[j]);
+    store32(p, w);
+  }
+}
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float v) {
+  if constexpr (sizeof(T) == 2) return __float2bfloat16_rn(v);
+  else return v;
+}
+
+// Eight e4m3 codes (8 bytes) <-> fp32.  Round to nearest, ties to even; beyond +-448 saturates; NaN stays NaN.
+__device__ __forceinline__ void decode_e4m3x8(const uint2 &c, float (&f)[8]) {
+  const uint32_t w[2] = {c.x, c.y};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j >> 1] >> (16 * (j & 1))), __NV_E4M3);
+    const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+    f[2 * j] = v.x;
+    f[2 * j + 1] = v.y;
+  }
+}
+__device__ __forceinline__ uint2 encode_e4m3x8(const float (&f)[8]) {
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    w[j >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f[2 * j], f[2 * j + 1]), __NV_SATFINITE, __NV_E4M3)
+                 << (16 * (j & 1));
+  return make_uint2(w[0], w[1]);
+}
+
+// int8 rows: scale = (largest magnitude) / 127; a row whose largest magnitude is below 2^-100 (its reciprocal could
+// overflow) is stored as zeros with scale 0.  An infinity or a NaN goes into the scale.
+__device__ __forceinline__ float int8_inverse(float top) { return top < 7.888609052210118e-31f ? 0.f : __fdiv_rn(127.0f, top); }
+__device__ __forceinline__ float int8_scale(float top) { return top < 7.888609052210118e-31f ? 0.f : __fdiv_rn(top, 127.0f); }
+// Eight values times `inv`, rounded to the nearest integers (ties to even), as int8.  |value * inv| <= 127 up to
+// rounding; a NaN becomes 0.
+__device__ __forceinline__ uint2 to_int8x8(const float (&f)[8], float inv) {
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int q = min(127, max(-127, __float2int_rn(f[j] * inv)));
+    w[j >> 2] |= ((uint32_t)q & 0xFFu) << (8 * (j & 3));
+  }
+  return make_uint2(w[0], w[1]);
+}
+
+// act(x) with the ABI's activation codes (0 none, 1 GeLU tanh form, 2 GeLU erf form).
+__device__ __forceinline__ float gelu1(float x, int act) {
+  if (act == 1) return 0.5f * x * (1.0f + tanhf(0.7978845608028654f * (x + 0.044715f * x * x * x)));
+  if (act == 2) return 0.5f * x * (1.0f + erff(x * 0.7071067811865476f));
+  return x;
+}
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  return v;
+}
+// Largest magnitude in the warp, `a` >= 0 or NaN (which wins: the bit patterns of non-negative floats are ordered
+// and a NaN's lies above infinity's).
+__device__ __forceinline__ float warp_max_abs(float a) {
+  return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(a) & 0x7FFFFFFFu));
+}
+
+}  // namespace osdp

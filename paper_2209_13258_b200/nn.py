@@ -293,3 +293,189 @@ class ZdpLinear(torch.nn.Module):
         if x.dtype != torch.bfloat16:
             raise TypeError("ZdpLinear takes bf16 activations")
         return _ZdpLinearFn.apply(x, self.shard, self.bias, self, *self.dp_parts)
+
+
+class _ResidualNormFn(torch.autograd.Function):
+    """(r, u) of osdp_block_norm_fwd; r is None where it would be x itself (no y, alpha 1)."""
+
+    @staticmethod
+    def forward(ctx, x, y, w_post, b_post, gate, w_pre, b_pre, layer):
+        D = layer.hidden
+        M = x.numel() // D
+        x2 = x.reshape(M, D).contiguous()
+        y2 = y.reshape(M, D).contiguous() if y is not None else None
+        need_grad = any(ctx.needs_input_grad)
+        pre = layer.pre != B.NORM_NONE
+        r = None if y is None and layer.alpha == 1.0 else torch.empty_like(x2)
+        u = torch.empty(M, D, dtype=torch.bfloat16, device=x.device) if pre else None
+        post = layer.post if y is not None else B.NORM_NONE
+        if y is None:
+            w_post = b_post = gate = None
+        stats = torch.empty(M, 4, dtype=torch.float32, device=x.device) if need_grad else None
+        B.osdp_block_norm_fwd(x2, y2, M, D, layer.resid_dtype, post, w_post, b_post, layer.eps, gate, layer.alpha, layer.beta,
+                              layer.pre, w_pre, b_pre, layer.eps, r, u, None, stats, check=True)
+        if need_grad:
+            ctx.layer, ctx.M, ctx.post, ctx.shape = layer, M, post, x.shape
+            ctx.save_for_backward(y2, (x2 if r is None else r) if pre else None, stats, w_post, b_post, gate, w_pre)
+        ctx.set_materialize_grads(False)
+        return (r.view(x.shape) if r is not None else None), (u.view(x.shape) if pre else None)
+
+    @staticmethod
+    def backward(ctx, dr, du):
+        layer, M = ctx.layer, ctx.M
+        D = layer.hidden
+        y, r, stats, w_post, b_post, gate, w_pre = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        if dr is None and du is None:
+            return (None,) * 8
+        dev = stats.device
+        pre = layer.pre if du is not None else B.NORM_NONE   # u was not used: nothing comes through its norm
+        dr = dr.reshape(M, D).contiguous() if dr is not None else None
+        du = du.reshape(M, D).contiguous() if du is not None else None
+        has_y = y is not None
+        dx = torch.empty(M, D, dtype=layer.resid_torch_dtype, device=dev) if need[0] else None
+        dy = torch.empty(M, D, dtype=torch.bfloat16, device=dev) if has_y and need[1] else None
+        vec = lambda on: torch.empty(D, dtype=torch.float32, device=dev) if on else None    # noqa: E731
+        dw_post, db_post, dgate = vec(need[2] and has_y), vec(need[3] and has_y), vec(need[4] and has_y)
+        dw_pre, db_pre = vec(need[5] and pre), vec(need[6] and pre)
+        B.osdp_block_norm_bwd(dr, du, y, r, stats, M, D, layer.resid_dtype, ctx.post, w_post, b_post, gate, layer.alpha, layer.beta,
+                              pre, w_pre if pre else None, dx, dy, dw_post, db_post, dgate, dw_pre, db_pre, layer._workspace(M), check=True)
+        return (dx.view(ctx.shape) if dx is not None else None, dy.view(ctx.shape) if dy is not None else None, dw_post, db_post,
+                dgate, dw_pre, db_pre, None)
+
+
+_NORMS = {None: B.NORM_NONE, "rms": B.NORM_RMS, "layer": B.NORM_LAYER}
+
+
+class ResidualNorm(torch.nn.Module):
+    """What stands between two blocks of a transformer, in one kernel:
+
+        r = alpha * x + beta * gate (.) N_post(y),    u = N_pre(r)
+
+    x: the residual stream (bf16, or fp32 with resid_dtype=torch.float32), y: the output of the block before (bf16), r:
+    the new residual stream, u (bf16): the input of the block after.  ``forward(x, y)`` returns (r, u);
+    ``forward(x)`` in front of the first block leaves the y term out; pre=None returns (r, None) behind the last one.
+    post / pre: "rms", "layer" or None.  gate: a learned value per channel (``gate_init``), or none with gate=False.
+    Weights, biases and gate are fp32 parameters.
+
+    ``forward_int8(x, y)`` (no gradient) returns (r, (u8, scale)): u as int8 with a scale per token, what ``Int8Linear``
+    takes, without the bf16 u in between.
+    """
+
+    def __init__(self, hidden, post="rms", pre="rms", gate=True, gate_init=1.0, alpha=1.0, beta=1.0, eps=1e-5,
+                 resid_dtype=torch.bfloat16, device="cuda"):
+        super().__init__()
+        if hidden % 8 or not 0 < hidden <= B.BLOCK_NORM_MAX_D:
+            raise ValueError("hidden must be a multiple of 8 and at most %d" % B.BLOCK_NORM_MAX_D)
+        if post not in _NORMS or pre not in _NORMS:
+            raise ValueError('post and pre are "rms", "layer" or None')
+        if resid_dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("the residual stream is bf16 or fp32")
+        self.hidden, self.post, self.pre = int(hidden), _NORMS[post], _NORMS[pre]
+        self.alpha, self.beta, self.eps = float(alpha), float(beta), float(eps)
+        self.resid_torch_dtype = resid_dtype
+        self.resid_dtype = B.DTYPE_FP32 if resid_dtype == torch.float32 else B.DTYPE_BF16
+        vec = lambda on, v: torch.nn.Parameter(torch.full((self.hidden,), float(v), device=device)) if on else None   # noqa: E731
+        self.w_post, self.b_post = vec(post, 1.0), vec(post == "layer", 0.0)
+        self.w_pre, self.b_pre = vec(pre, 1.0), vec(pre == "layer", 0.0)
+        self.gate = vec(gate, gate_init)
+        self._ws = None
+
+    def _workspace(self, M):
+        rc, need = B.osdp_block_norm_workspace_bytes(M, self.hidden)
+        if rc:
+            raise B.OsdpError(rc, "osdp_block_norm_workspace_bytes")
+        dev = next(self.parameters()).device
+        if self._ws is None or self._ws.device != dev:
+            self._ws = B.new_workspace(need, device=dev)
+        return self._ws
+
+    def _check(self, x, y):
+        if not x.is_cuda:
+            raise RuntimeError("ResidualNorm runs on CUDA only: there is no CPU path")
+        if x.dtype != self.resid_torch_dtype or (y is not None and y.dtype != torch.bfloat16):
+            raise TypeError("ResidualNorm takes x in its resid_dtype and y in bf16")
+        if x.shape[-1] != self.hidden or (y is not None and y.shape != x.shape):
+            raise ValueError("x and y are [..., hidden] of the same shape")
+
+    def forward(self, x, y=None):
+        self._check(x, y)
+        if y is None and self.alpha == 1.0 and self.pre == B.NORM_NONE:
+            return x, None
+        r, u = _ResidualNormFn.apply(x, y, self.w_post, self.b_post, self.gate, self.w_pre, self.b_pre, self)
+        return (x if r is None else r), u
+
+    @torch.no_grad()
+    def forward_int8(self, x, y=None):
+        self._check(x, y)
+        if self.pre == B.NORM_NONE:
+            raise ValueError("there is no u to quantise: pre is None")
+        D = self.hidden
+        M = x.numel() // D
+        x2 = x.reshape(M, D).contiguous()
+        y2 = y.reshape(M, D).contiguous() if y is not None else None
+        r = torch.empty_like(x2)
+        u = torch.empty(M, D, dtype=torch.int8, device=x.device)
+        s = torch.empty(M, dtype=torch.float32, device=x.device)
+        post, w_post, b_post, gate = (self.post, self.w_post, self.b_post, self.gate) if y is not None else (B.NORM_NONE, None, None, None)
+        B.osdp_block_norm_fwd(x2, y2, M, D, self.resid_dtype, post, w_post, b_post, self.eps, gate, self.alpha, self.beta, self.pre,
+                              self.w_pre, self.b_pre, self.eps, r, u, s, None, check=True)
+        return r.view(x.shape), (u.view(x.shape), s.view(x.shape[:-1]))
+
+
+def quantize_int8(x):
+    """(int8 rows, fp32 scale per row) of a bf16 tensor [..., K] (osdp_quantize_rows_i8)."""
+    K = x.shape[-1]
+    if not x.is_cuda or x.dtype != torch.bfloat16:
+        raise TypeError("quantize_int8 takes a bf16 CUDA tensor")
+    x2 = x.detach().reshape(-1, K).contiguous()
+    q = torch.empty(x2.shape, dtype=torch.int8, device=x.device)
+    s = torch.empty(x2.shape[0], dtype=torch.float32, device=x.device)
+    B.osdp_quantize_rows_i8(x2, x2.shape[0], K, q, s, check=True)
+    return q.view(x.shape), s.view(x.shape[:-1])
+
+
+class Int8Linear(torch.nn.Module):
+    """y = act(x W^T + b) for serving, with int8 weights (a scale per output channel) and int8 activations (a scale per
+    token, taken from the token itself); int32 sums, bf16 output.  No gradient.
+
+    weight8 [out, in] int8, w_scale [out] fp32, bias [out] fp32 or None.  ``from_linear`` quantises a trained
+    ``SplitLinear`` (or any bf16 weight).  ``forward`` takes bf16 activations, or the pair (int8, scale) that
+    ``ResidualNorm.forward_int8`` and ``quantize_int8`` return.
+    """
+
+    def __init__(self, weight8, w_scale, bias=None, act=B.ACT_NONE, k_split=1, split_dim=B.SPLIT_OUT):
+        super().__init__()
+        if weight8.dtype != torch.int8 or weight8.dim() != 2 or w_scale.dtype != torch.float32 or w_scale.numel() != weight8.shape[0]:
+            raise ValueError("weight8 is [out, in] int8 with one fp32 scale per row")
+        if bias is not None and (bias.dtype != torch.float32 or bias.numel() != weight8.shape[0]):
+            raise ValueError("bias is [out] fp32")
+        self.out_features, self.in_features = weight8.shape
+        if self.in_features % 16 or self.out_features % 8:
+            raise ValueError("in_features must be a multiple of 16 and out_features of 8")
+        self.register_buffer("weight8", weight8.contiguous())
+        self.register_buffer("w_scale", w_scale.contiguous())
+        self.register_buffer("bias", bias.contiguous() if bias is not None else None)
+        self.act, self.k_split, self.split_dim = int(act), int(k_split), int(split_dim)
+        self._ws = B.new_workspace(256, device=weight8.device)
+
+    @classmethod
+    def from_linear(cls, layer, **kw):
+        """From a SplitLinear, or from anything with a bf16 `weight` [out, in] and an optional `bias`."""
+        q, s = quantize_int8(layer.weight)
+        bias = layer.bias.detach().float() if layer.bias is not None else None
+        return cls(q, s, bias, act=getattr(layer, "act", B.ACT_NONE), **kw)
+
+    @torch.no_grad()
+    def forward(self, x):
+        q, s = x if isinstance(x, tuple) else quantize_int8(x)
+        if q.dtype != torch.int8 or q.shape[-1] != self.in_features:
+            raise ValueError("Int8Linear takes [..., in_features]")
+        K, N = self.in_features, self.out_features
+        M = q.numel() // K
+        if self._ws.device != q.device:
+            self._ws = B.new_workspace(256, device=q.device)
+        out = torch.empty(*q.shape[:-1], N, dtype=torch.bfloat16, device=q.device)
+        B.osdp_split_linear_fwd_i8(q.contiguous(), s.contiguous(), self.weight8, 0, self.w_scale, self.bias, M, N, K, self.k_split,
+                                   self.split_dim, self.act, out, self._ws, check=True)
+        return out

@@ -1,0 +1,143 @@
+"""AdamW over the parameters of the split layers: one kernel launch for all tensors, states in 32 or in 8 bits, and the
+gradient norm with its clipping coefficient on the device.
+
+Argument marshalling only; the arithmetic runs in ``osdp_adamw_step`` / ``osdp_grad_norm``.  CUDA only.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import binding as B
+
+
+class AdamW(torch.optim.Optimizer):
+    """Decoupled weight decay (AdamW) for contiguous CUDA parameters of one dtype, bf16 or fp32.
+
+    state_dtype  "fp32", or "e4m3": both moments as 8-bit codes with one fp32 scale per 256 elements (2.03 bytes per
+                 parameter instead of 8; the second moment is kept as its root).
+    master       bf16 parameters only: the step works on fp32 copies of the parameters (4 bytes each) and writes their
+                 rounding.  Without it an update below half a unit in the last place of a bf16 parameter is lost.
+    max_norm     clips the gradients by their global norm over all parameters of the step, without a host round trip.
+                 A step whose norm is not finite changes nothing (``grad_norm[0]`` says so).
+
+    All parameter groups are stepped together: ``lr`` and ``weight_decay`` may differ between groups, ``betas`` and
+    ``eps`` may not.  Parameters whose ``.grad`` is None are left alone.  ``steps`` counts the steps done (one count for
+    all parameters: it sets the bias correction).  States are flat over all parameters, each parameter's part starting
+    at a multiple of 256 elements (``offsets``): ``exp_avg``, ``exp_avg_sq`` (with "e4m3" the codes of the second
+    moment's root), ``exp_avg_scale``, ``exp_avg_sq_scale``, ``master``.  ``grad_norm`` [2]: the last step's norm and
+    coefficient, on the device.
+    """
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_dtype="fp32", master=False,
+                 max_norm=None):
+        if state_dtype not in ("fp32", "e4m3"):
+            raise ValueError('state_dtype is "fp32" or "e4m3"')
+        self._built = False
+        super().__init__(params, {"lr": lr, "betas": tuple(betas), "eps": eps, "weight_decay": weight_decay})
+        self._params = [p for g in self.param_groups for p in g["params"]]
+        first = self._params[0]
+        if first.dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError("AdamW takes bf16 or fp32 parameters")
+        for p in self._params:
+            if not p.is_cuda:
+                raise RuntimeError("AdamW runs on CUDA only: there is no CPU path")
+            if p.dtype != first.dtype or p.device != first.device:
+                raise TypeError("the parameters of one AdamW have one dtype and one device")
+            if not p.is_contiguous():
+                raise ValueError("AdamW takes contiguous parameters")
+        if master and first.dtype != torch.bfloat16:
+            raise ValueError("fp32 parameters are their own master")
+        self._dtype = B.DTYPE_FP32 if first.dtype == torch.float32 else B.DTYPE_BF16
+        self._state_dtype = B.DTYPE_E4M3 if state_dtype == "e4m3" else B.DTYPE_FP32
+        rc, self.offsets, total = B.osdp_adamw_layout([p.numel() for p in self._params])
+        if rc:
+            raise B.OsdpError(rc, "osdp_adamw_layout")
+        dev = first.device
+        new = lambda n, dt: torch.zeros(n, dtype=dt, device=dev)      # noqa: E731
+        sdt = torch.float8_e4m3fn if state_dtype == "e4m3" else torch.float32
+        self.exp_avg, self.exp_avg_sq = new(total, sdt), new(total, sdt)
+        blocks = total // B.ADAMW_BLOCK
+        self.exp_avg_scale, self.exp_avg_sq_scale = (new(blocks, torch.float32), new(blocks, torch.float32)) if state_dtype == "e4m3" else (None, None)
+        self.master = None
+        if master:
+            self.master = new(total, torch.float32)
+            for p, o in zip(self._params, self.offsets):
+                self.master[o:o + p.numel()].copy_(p.detach().reshape(-1))
+        self.max_norm = max_norm
+        self.grad_norm = new(2, torch.float32)
+        self.steps = 0
+        n = len(self._params)
+        self._table = (B.AdamWTensor * n)()
+        for t, p, o in zip(self._table, self._params, self.offsets):
+            t.numel, t.state_offset = p.numel(), o
+        self._ws = B.new_workspace(B.osdp_grad_norm_workspace_bytes(n)[1], device=dev)
+        self._built = True
+
+    def add_param_group(self, group):
+        if self._built:
+            raise RuntimeError("the states are laid out when the optimiser is built: pass all groups then")
+        super().add_param_group(group)
+
+    def _fill(self):
+        """The table of this step: addresses as they are now, tensors without a gradient left out."""
+        i, n = 0, 0
+        table, params, offsets = self._table, self._params, self.offsets
+        dtype, device = params[0].dtype, params[0].device
+        keep = []
+        for g in self.param_groups:
+            lr, wd = float(g["lr"]), float(g["weight_decay"])
+            for p in g["params"]:
+                d = p.grad
+                if d is not None:
+                    if d.dtype != dtype or d.device != device or d.numel() != p.numel():
+                        raise TypeError("a gradient has its parameter's dtype, device and size")
+                    if not d.is_contiguous():
+                        d = d.contiguous()
+                        keep.append(d)
+                    t = table[n]
+                    t.param, t.grad, t.numel, t.state_offset, t.lr, t.weight_decay = p.data_ptr(), d.data_ptr(), p.numel(), offsets[i], lr, wd
+                    n += 1
+                i += 1
+        return n, keep
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        betas, eps = self.param_groups[0]["betas"], self.param_groups[0]["eps"]
+        for g in self.param_groups[1:]:
+            if g["betas"] != betas or g["eps"] != eps:
+                raise ValueError("betas and eps are the same for all groups")
+        n, keep = self._fill()
+        self.steps += 1
+        with torch.cuda.device(self.exp_avg.device):
+            clip = None
+            if self.max_norm is not None:
+                clip = self.grad_norm
+                B.osdp_grad_norm(self._table, n, self._dtype, self.max_norm, clip, self._ws, check=True)
+            B.osdp_adamw_step(self._table, n, self._dtype, self._state_dtype, self.master, self.exp_avg, self.exp_avg_sq,
+                              self.exp_avg_scale, self.exp_avg_sq_scale, betas[0], betas[1], eps, self.steps, clip, check=True)
+        return loss
+
+    def state_dict(self):
+        d = super().state_dict()
+        d["flat"] = {k: getattr(self, k) for k in ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale", "master")}
+        d["steps"] = self.steps
+        return d
+
+    def load_state_dict(self, d):
+        d = dict(d)
+        flat, steps = d.pop("flat"), d.pop("steps")
+        for k, v in flat.items():
+            mine = getattr(self, k)
+            if (mine is None) != (v is None) or (v is not None and (mine.shape != v.shape or mine.dtype != v.dtype)):
+                raise ValueError("%s does not fit this optimiser" % k)
+        super().load_state_dict(d)
+        for k, v in flat.items():
+            if v is not None:
+                getattr(self, k).copy_(v)
+        self.steps = int(steps)
