@@ -126,29 +126,35 @@ def lib():
     return _lib
 
 
+# Addresses are passed as plain integers (the argtypes convert them): these run a dozen times per call.
 def _ptr(t):
-    if t is None:
-        return None
-    if isinstance(t, int):
-        return ctypes.c_void_p(t)
-    return ctypes.c_void_p(t.data_ptr())
+    if t is None or type(t) is int:
+        return t
+    return t if isinstance(t, int) else t.data_ptr()
+
+
+_raw_stream = None
 
 
 def _stream(s):
     if s is None:
-        import torch
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
-    if isinstance(s, int):
-        return ctypes.c_void_p(s)
-    return ctypes.c_void_p(s.cuda_stream)
+        global _raw_stream
+        if _raw_stream is None:
+            import torch
+            # the handle of the current stream without a Stream object around it, where this torch has it
+            get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            _raw_stream = ((lambda: get(torch.cuda.current_device())) if get is not None
+                           else (lambda: torch.cuda.current_stream().cuda_stream))
+        return _raw_stream()
+    return s if isinstance(s, int) else s.cuda_stream
 
 
 def _ws(ws):
     if ws is None:
         return None, 0
     if isinstance(ws, tuple):
-        return ctypes.c_void_p(ws[0]), int(ws[1])
-    return ctypes.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size()
+        return ws[0], int(ws[1])
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 def _ret(rc, check, where):

@@ -233,10 +233,346 @@ __global__ void __launch_bounds__(V == 4 ? 512 : 1024) block_norm_fwd_kernel(con
   if (a.stats && tl == 0) a.stats[row] = st;
 }
 
-// ------------------------------------------------------------------------------------------------ backward
+// ------------------------------------------------------------------------------------------------ teams over many rows
+//
+// Kernels for many rows: one block per SM, or a cluster of CL = 2 or 4 blocks that share their rows where a row does not
+// fit one (registers: 8192 channels; shared memory: three rows of what a kernel reads), teams of warps that take rows in a fixed stride, a lane with the same two vectors of eight channels for all of them, so
+// that weights stay in its registers.  What a lane needs of the next rows it copies itself, asynchronously, into its own
+// slots of a ring in shared memory; no thread reads another's slots, so the ring needs no barrier, and several rows per
+// team are in flight whatever the arithmetic does.  Rows are worked on in a software pipeline: a step does the last part
+// of one row and the first part of the next, whose sums over the row are then exchanged with ONE barrier, so that its
+// latency and that of the shuffles is met with independent work.
 
-constexpr int BWD_MAX_BLOCKS = 160;   // partial sums over rows that the workspace holds
-constexpr int BWD_THREADS = 512;
+constexpr int ROW_THREADS = 512;
+constexpr int MAX_STAGES = 6;
+constexpr int ROW_MAX_BLOCKS = 160;   // partial sums over rows that the workspace holds
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// waits until at most `left` (0 ... MAX_STAGES - 2) of this thread's groups are still in flight
+__device__ __forceinline__ void cp_async_wait(int left) {
+  switch (left) {
+    case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+    case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+    case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+    default: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
+  }
+}
+
+// Sums of N values over the warp; every lane returns the sum with index `idx` (a function of the lane).  Halving the
+// values at each exchange takes N - 1 + log2(32 / N) shuffles instead of 5 N.
+template <int N>
+__device__ __forceinline__ float warp_sum_scattered(float (&v)[N], int lane, int &idx) {
+  static_assert(N == 2 || N == 4 || N == 8, "");
+  idx = 0;
+  int o = 16;
+#pragma unroll
+  for (int n = N / 2; n > 0; n >>= 1, o >>= 1) {
+    const bool up = (lane & o) != 0;
+#pragma unroll
+    for (int k = 0; k < n; ++k) {
+      const float give = up ? v[k] : v[k + n];
+      v[k] = (up ? v[k + n] : v[k]) + __shfl_xor_sync(0xFFFFFFFFu, give, o);
+    }
+    idx += up ? n : 0;
+  }
+  float s = v[0];
+  for (; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+  return s;
+}
+
+// channels of a row that a block of a cluster holds (the last one may have fewer)
+__host__ __device__ constexpr int block_channels(int D, int cl) { return (D / 8 + cl - 1) / cl * 8; }
+
+struct TeamShape {
+  int warps;    // of a team
+  int teams;    // of a block
+  int stages;
+};
+
+// Where a thread stands, and the exchange of a row's partial sums.
+template <int CL, int NS>
+struct Team {
+  int warp, lane, team, first_warp, tl, TL, warps, unit, units, c_begin, c_end, turn;
+  uint32_t rank;
+  float *red;    // [2 turns][CL blocks][16 warps][NS]
+  static constexpr int RED_FLOATS = 2 * CL * 16 * NS;
+
+  __device__ __forceinline__ void init(const TeamShape &sh, int D, float *red_) {
+    warp = threadIdx.x >> 5;
+    lane = threadIdx.x & 31;
+    warps = sh.warps;
+    team = warp / warps;
+    first_warp = team * warps;
+    tl = (warp - first_warp) * 32 + lane;
+    TL = warps * 32;
+    rank = 0;
+    if (CL > 1) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    unit = (int)blockIdx.x / CL;
+    units = (int)gridDim.x / CL;
+    c_begin = min((int)rank * block_channels(D, CL), D);
+    c_end = min(c_begin + block_channels(D, CL), D);
+    red = red_;
+    turn = 0;
+  }
+  // channels that warp w of the team (0 ... warps - 1) of block `blk` holds
+  __device__ __forceinline__ float channels(int blk, int w, int D) const {
+    const int width = min(block_channels(D, CL), max(D - blk * block_channels(D, CL), 0));
+    return (float)(min(max(width - w * 256, 0), 256) + min(max(width - (TL + w * 32) * 8, 0), 256));
+  }
+  __device__ __forceinline__ float *buffer() const { return red + turn * (RED_FLOATS / 2); }
+  // Makes this warp's sums visible to the team.  A lane brings the sum with index idx; exactly the lanes with `mine`
+  // set write.  Two buffers in turn: one is written again only after the barrier of the exchange in between, which
+  // every reader of it has passed.
+  __device__ __forceinline__ void publish(float s, int idx, bool mine) {
+    float *at = buffer() + ((int)rank * 16 + warp) * NS + idx;
+    if (mine) {
+      *at = s;
+      const uint32_t local = static_cast<uint32_t>(__cvta_generic_to_shared(at));
+#pragma unroll
+      for (uint32_t q = 1; q < CL; ++q)
+        asm volatile("{\n\t.reg .b32 ra;\n\tmapa.shared::cluster.u32 ra, %0, %1;\n\tst.shared::cluster.f32 [ra], %2;\n\t}" ::"r"(local), "r"((rank + q) % CL), "f"(s) : "memory");
+    }
+  }
+  __device__ __forceinline__ void barrier() const {
+    if (CL > 1) {   // the teams of a cluster go through it together
+      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else if (warps > 1) {
+      asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(TL) : "memory");
+    } else {
+      __syncwarp();
+    }
+  }
+  // f(partial sums of one warp, block, warp of the team) for every warp that shares the row
+  template <typename F>
+  __device__ __forceinline__ void each(const float *buf, F f) const {
+#pragma unroll
+    for (int b = 0; b < CL; ++b)
+      for (int w = 0; w < warps; ++w) f(buf + (b * 16 + first_warp + w) * NS, b, w);
+  }
+};
+
+// ------------------------------------------------------------------------------------------------ forward, many rows
+
+// A step finishes row i (u), does row i + 1 up to its sums (r) and takes the sums of row i + 2's y.  The variance is
+// taken per warp about the warp's own mean and the warps' means and variances are merged, which is as safe as a second
+// pass over the row and needs no second exchange.
+template <typename RT, bool LAYER, int CL>
+__global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_fwd_rows_kernel(const __grid_constant__ FwdArgs a, const TeamShape sh) {
+  constexpr int RP = sizeof(RT) / 2;             // 16-byte pieces of a residual vector
+  constexpr int PIECES = 1 + RP;                 // y, x
+  constexpr int NS = LAYER ? 4 : 2;              // y's, r's: mean and squared distances, or squares alone
+  extern __shared__ __align__(16) uint8_t smem[];
+  Team<CL, NS> tm;
+  tm.init(sh, a.D, reinterpret_cast<float *>(smem));
+  uint8_t *ring = smem + Team<CL, NS>::RED_FLOATS * 4;
+  const uint32_t ring_u32 = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
+  const int nthreads = blockDim.x;
+  const int stage_bytes = 2 * PIECES * nthreads * 16;
+  pdl_launch_dependents();
+  pdl_wait();
+
+  int col[2];
+  bool act[2];
+  float qw[2][8], wp[2][8], qb[LAYER ? 2 : 1][8], bp[LAYER ? 2 : 1][8];   // r = alpha x + qw h + qb, u = wp h + bp
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    col[j] = tm.c_begin + (j * tm.TL + tm.tl) * 8;
+    act[j] = col[j] < tm.c_end;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      qw[j][k] = wp[j][k] = 0.f;
+      if (LAYER) qb[j][k] = bp[j][k] = 0.f;
+    }
+    if (!act[j]) continue;
+    if (a.y) {
+      float g[8];
+      weights8(a.gate, col[j], 1.f, g);
+      weights8(a.post.w, col[j], 1.f, qw[j]);
+      if (LAYER) weights8(a.post.b, col[j], 0.f, qb[j]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        qw[j][k] *= a.beta * g[k];
+        if (LAYER) qb[j][k] *= a.beta * g[k];
+      }
+    }
+    if (a.pre.has) weights8(a.pre.w, col[j], 1.f, wp[j]);
+    if (LAYER) weights8(a.pre.b, col[j], 0.f, bp[j]);
+  }
+  if (CL > 1) tm.barrier();   // the other blocks run before anything is written to their shared memory
+
+  const long long first = (long long)tm.unit * sh.teams + tm.team, step = (long long)tm.units * sh.teams;
+  const long long n = first < a.M ? (a.M - first + step - 1) / step : 0;
+  // the teams of a cluster meet at its barrier: all do as many steps as its first team, which has the most rows
+  const long long n_steps = CL == 1 ? n : (a.M - (first - tm.team) + step - 1) / step;
+  auto slot = [&](int stage, int j, int piece) { return stage * stage_bytes + ((j * PIECES + piece) * nthreads + (int)threadIdx.x) * 16; };
+  auto fetch = [&](long long i, int stage) {
+    if (i < n) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (!act[j]) continue;
+        const long long at = (first + i * step) * a.D + col[j];
+        if (a.y) cp_async16(ring_u32 + slot(stage, j, 0), a.y + at);
+#pragma unroll
+        for (int p = 0; p < RP; ++p)
+          cp_async16(ring_u32 + slot(stage, j, 1 + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.x) + at) + 16 * p);
+      }
+    }
+    cp_async_commit();
+  };
+  const float inv_d = 1.0f / (float)a.D;
+  const float my_channels = LAYER ? tm.channels((int)tm.rank, tm.warp - tm.first_warp, a.D) : 0.f;
+  const float my_inv = my_channels > 0.f ? 1.0f / my_channels : 0.f;
+  const bool has_y = a.y != nullptr, post = has_y && a.post.has, pre = a.pre.has;
+  const bool y_mean = LAYER && post && a.post.layer, r_mean = LAYER && pre && a.pre.layer;
+  float r[2][8];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) r[j][k] = 0.f;
+  float mean_y = 0.f, rstd_y = 1.f, mean_r = 0.f, rstd_r = 0.f, shown_mean_y = 0.f, shown_rstd_y = 0.f;
+
+  for (int s = 0; s + 1 < sh.stages; ++s) fetch(s, s);
+  int st_a = 0, st_b = sh.stages - 1;     // ring stages of row i (its y) and of row i - 1 (then refilled)
+  for (long long i = 0; i < n_steps + 2; ++i) {
+    if (i >= 2 && i < n + 2) {
+      // ---- row i - 2: u
+      const long long row = first + (i - 2) * step;
+      if (pre) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          if (!act[j]) continue;
+          float u[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float h = (LAYER ? r[j][k] - mean_r : r[j][k]) * rstd_r;
+            u[k] = LAYER ? fmaf(h, wp[j][k], bp[j][k]) : h * wp[j][k];
+          }
+          store8(static_cast<__nv_bfloat16 *>(a.u) + row * a.D + col[j], u);
+        }
+      }
+      if (a.stats && tm.tl == 0 && tm.rank == 0)
+        a.stats[row] = make_float4(shown_mean_y, shown_rstd_y, pre ? mean_r : 0.f, pre ? rstd_r : 0.f);
+    }
+    float part[NS];
+#pragma unroll
+    for (int k = 0; k < NS; ++k) part[k] = 0.f;
+    if (i >= 1 && i <= n) {
+      // ---- row i - 1: r
+      const long long row = first + (i - 1) * step;
+      shown_mean_y = post ? mean_y : 0.f;
+      shown_rstd_y = post ? rstd_y : 0.f;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (!act[j]) continue;
+        float x[8];
+        if (RP == 1) {
+          widen8(*reinterpret_cast<const uint4 *>(ring + slot(st_b, j, 1)), x);
+        } else {
+          const float4 lo = *reinterpret_cast<const float4 *>(ring + slot(st_b, j, 1)), hi = *reinterpret_cast<const float4 *>(ring + slot(st_b, j, PIECES - 1));
+          x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w;
+          x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) r[j][k] = a.alpha * x[k];
+        if (has_y) {
+          float y[8];
+          widen8(*reinterpret_cast<const uint4 *>(ring + slot(st_b, j, 0)), y);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float h = (LAYER ? y[k] - mean_y : y[k]) * rstd_y;
+            r[j][k] = fmaf(qw[j][k], h, LAYER ? r[j][k] + qb[j][k] : r[j][k]);
+          }
+        }
+        if (a.r) store8(static_cast<RT *>(a.r) + row * a.D + col[j], r[j]);
+        if (LAYER) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) part[2] += r[j][k];
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) part[1] = fmaf(r[j][k], r[j][k], part[1]);
+        }
+      }
+    }
+    float y[2][8];
+    if (i < n) {
+      // ---- row i: sums of y
+      cp_async_wait(sh.stages - 2);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (post && act[j]) {
+          widen8(*reinterpret_cast<const uint4 *>(ring + slot(st_a, j, 0)), y[j]);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) part[0] = LAYER ? part[0] + y[j][k] : fmaf(y[j][k], y[j][k], part[0]);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) y[j][k] = 0.f;
+        }
+      }
+    }
+    // st_b is free: row i - 1 has been read for the last time
+    fetch(i - 1 + sh.stages, st_b);
+    st_b = st_a;
+    if (++st_a == sh.stages) st_a = 0;
+    if (LAYER) {
+      const float my = y_mean ? warp_sum(part[0]) * my_inv : 0.f, mr = r_mean ? warp_sum(part[2]) * my_inv : 0.f;
+      float d[2] = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (!act[j]) continue;
+        if (i < n && post) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) d[0] = fmaf(y[j][k] - my, y[j][k] - my, d[0]);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) d[1] = fmaf(r[j][k] - mr, r[j][k] - mr, d[1]);
+      }
+      d[0] = warp_sum(d[0]);
+      d[1] = warp_sum(d[1]);
+      tm.publish(tm.lane == 0 ? my : tm.lane == 1 ? d[0] : tm.lane == 2 ? mr : d[1], tm.lane & 3, tm.lane < 4);
+    } else {
+      float two[2] = {part[0], part[1]};
+      int idx;
+      const float s = warp_sum_scattered<2>(two, tm.lane, idx);
+      tm.publish(s, idx, (tm.lane & 15) == 0);
+    }
+    const float *buf = tm.buffer();
+    tm.turn ^= 1;
+    tm.barrier();
+    if (LAYER) {
+      float sy = 0.f, sr = 0.f, vy = 0.f, vr = 0.f;
+      tm.each(buf, [&](const float *f, int b, int w) {
+        const float c = tm.channels(b, w, a.D);
+        sy = fmaf(c, f[0], sy);
+        sr = fmaf(c, f[2], sr);
+      });
+      mean_y = sy * inv_d;
+      mean_r = sr * inv_d;
+      tm.each(buf, [&](const float *f, int b, int w) {
+        const float c = tm.channels(b, w, a.D), dy = f[0] - mean_y, dr = f[2] - mean_r;
+        vy += fmaf(c * dy, dy, f[1]);
+        vr += fmaf(c * dr, dr, f[3]);
+      });
+      rstd_y = post ? rsqrtf(fmaf(vy, inv_d, a.post.eps)) : 1.f;
+      rstd_r = rsqrtf(fmaf(vr, inv_d, a.pre.eps));
+    } else {
+      float sy = 0.f, sr = 0.f;
+      tm.each(buf, [&](const float *f, int, int) {
+        sy += f[0];
+        sr += f[1];
+      });
+      rstd_y = post ? rsqrtf(fmaf(sy, inv_d, a.post.eps)) : 1.f;
+      rstd_r = rsqrtf(fmaf(sr, inv_d, a.pre.eps));
+    }
+  }
+  cp_async_wait(0);
+}
+
+// ------------------------------------------------------------------------------------------------ backward
 
 struct BwdArgs {
   const void *dr;
@@ -251,61 +587,28 @@ struct BwdArgs {
   float *partial;    // [units][4][D]
   long long M;
   int D;
-  int warps;         // of a team
-  int teams;         // of a block
-  int stages;
 };
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-// waits until at most `left` of this thread's groups are still in flight
-__device__ __forceinline__ void cp_async_wait(int left) {
-  switch (left) {
-    case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
-    case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
-    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
-    case 3: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
-    case 4: asm volatile("cp.async.wait_group 4;" ::: "memory"); break;
-    default: asm volatile("cp.async.wait_group 5;" ::: "memory"); break;
-  }
-}
-constexpr int MAX_STAGES = 6;
-
-// Rows are dealt to teams of warps in a fixed stride; a lane owns two vectors of eight adjacent channels for the whole
-// kernel and keeps the channel sums in registers.  What it needs of the next rows it copies itself, asynchronously, into
-// its own slots of a ring in shared memory: no thread reads another's slots, so the ring needs no barrier.
-//
-// One reduction per row.  With t = dr + rstd (a - c1 - h_pre c2), c1 = mean a, c2 = mean a h_pre, the sums that dy needs,
+// One exchange per row.  With t = dr + rstd (a - c1 - h_pre c2), c1 = mean a, c2 = mean a h_pre, the sums that dy needs,
 // sum q t and sum q t h_post, are linear in c1 and c2, so all sums over the row's data are taken at once and combined:
 //   sum q t h_post = sum q h_post (dr + rstd a) - rstd (c1 sum q h_post + c2 sum q h_post h_pre).
+// A step takes the sums of row i + 1 and writes the gradients of row i.  The sums over rows stay in registers.
 //
-// PAIR: a row is split between the two blocks of a cluster (D > 8192); partial sums go to both blocks' shared memory.
-// LAYER: either norm subtracts a mean (more sums).  WREG: weights in registers, else in shared memory.
-template <typename RT, bool LAYER, bool PAIR>
-__global__ void __launch_bounds__(BWD_THREADS, 1) block_norm_bwd_kernel(const __grid_constant__ BwdArgs a) {
+// LAYER: either norm subtracts a mean (more sums; the weights are then in shared memory, there are too few registers).
+template <typename RT, bool LAYER, int CL>
+__global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __grid_constant__ BwdArgs a, const TeamShape sh) {
   constexpr bool WREG = !LAYER;
   constexpr int NS = LAYER ? 8 : 4;                 // sums per row
   constexpr int RP = sizeof(RT) / 2;                // 16-byte pieces of a residual vector
   constexpr int PIECES = 2 + 2 * RP;                // y, du, r, dr
   extern __shared__ __align__(16) uint8_t smem[];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int team = warp / a.warps, first_warp = team * a.warps;
-  const int tl = (warp - first_warp) * 32 + lane, TL = a.warps * 32;
-  uint32_t rank = 0;
-  if (PAIR) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-  const int unit = PAIR ? (int)(blockIdx.x >> 1) : (int)blockIdx.x, units = PAIR ? (int)(gridDim.x >> 1) : (int)gridDim.x;
-  const int half = PAIR ? (a.D / 8 + 1) / 2 * 8 : 0;                 // channels of the first block of a pair
-  const int c_begin = (int)rank * half, c_end = (PAIR && rank == 0) ? half : a.D;
-
-  float *red = reinterpret_cast<float *>(smem);                      // [2][2 blocks][16 warps][NS]
-  constexpr int RED_BYTES = 2 * 2 * 16 * 8 * 4;
-  float4 *wsm = reinterpret_cast<float4 *>(smem + RED_BYTES);        // [q, w_pre][2 vectors][2 halves][TL]
-  const int w_bytes = WREG ? 0 : 8 * TL * 16;
-  uint8_t *ring = smem + RED_BYTES + w_bytes;
+  Team<CL, NS> tm;
+  tm.init(sh, a.D, reinterpret_cast<float *>(smem));
+  const int tl = tm.tl, TL = tm.TL;
+  float4 *wsm = reinterpret_cast<float4 *>(smem + Team<CL, NS>::RED_FLOATS * 4);   // [q, w_pre][2 vectors][2 halves][TL]
+  uint8_t *ring = reinterpret_cast<uint8_t *>(wsm) + (WREG ? 0 : 8 * TL * 16);
   const uint32_t ring_u32 = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
-  const int nthreads = a.warps * a.teams * 32;
+  const int nthreads = blockDim.x;
   const int stage_bytes = 2 * PIECES * nthreads * 16;
 
   pdl_launch_dependents();
@@ -316,8 +619,8 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) block_norm_bwd_kernel(const __
   float qreg[WREG ? 2 : 1][8], wreg[WREG ? 2 : 1][8];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    col[j] = c_begin + (j * TL + tl) * 8;
-    act[j] = col[j] < c_end;
+    col[j] = tm.c_begin + (j * TL + tl) * 8;
+    act[j] = col[j] < tm.c_end;
     float q[8], w[8], g[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) q[k] = w[k] = 0.f;
@@ -333,7 +636,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) block_norm_bwd_kernel(const __
     if (WREG) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) { qreg[j][k] = q[k]; wreg[j][k] = w[k]; }
-    } else if (team == 0) {
+    } else if (tm.team == 0) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         wsm[(0 + j * 2 + h) * TL + tl] = make_float4(q[4 * h], q[4 * h + 1], q[4 * h + 2], q[4 * h + 3]);
@@ -342,10 +645,7 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) block_norm_bwd_kernel(const __
     }
   }
   if (!WREG) __syncthreads();
-  if (PAIR) {   // the other block runs before anything is written to its shared memory
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-  }
+  if (CL > 1) tm.barrier();   // the other blocks run before anything is written to their shared memory
   auto weights = [&](int j, float (&q)[8], float (&w)[8]) {
     if (WREG) {
 #pragma unroll
@@ -360,14 +660,17 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) block_norm_bwd_kernel(const __
     }
   };
 
-  const long long first = (long long)unit * a.teams + team, step = (long long)units * a.teams;
+  const long long first = (long long)tm.unit * sh.teams + tm.team, step = (long long)tm.units * sh.teams;
+  const long long n = first < a.M ? (a.M - first + step - 1) / step : 0;
+  // the teams of a cluster meet at its barrier: all do as many steps as its first team, which has the most rows
+  const long long n_steps = CL == 1 ? n : (a.M - (first - tm.team) + step - 1) / step;
   auto slot = [&](int stage, int j, int piece) { return stage * stage_bytes + ((j * PIECES + piece) * nthreads + (int)threadIdx.x) * 16; };
-  auto fetch = [&](long long row, int stage) {
-    if (row < a.M) {
+  auto fetch = [&](long long i, int stage) {
+    if (i < n) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (!act[j]) continue;
-        const long long at = row * a.D + col[j];
+        const long long at = (first + i * step) * a.D + col[j];
         if (a.y) cp_async16(ring_u32 + slot(stage, j, 0), a.y + at);
         if (a.pre_has) {
           cp_async16(ring_u32 + slot(stage, j, 1), a.du + at);
@@ -413,121 +716,132 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) block_norm_bwd_kernel(const __
     }
   const bool has_y = a.y != nullptr, has_dr = a.dr != nullptr, has_pre = a.pre_has != 0;
   const float inv_d = 1.0f / (float)a.D;
-  int turn = 0;
-  for (int s = 0; s + 1 < a.stages; ++s) fetch(first + s * step, s);
-  int stage = 0, next_stage = a.stages - 1;
-  // PAIR: both blocks walk the same rows, so their barriers match
-  for (long long row = first; row < a.M; row += step) {
-    fetch(row + (a.stages - 1) * step, next_stage);
-    if (++next_stage == a.stages) next_stage = 0;
-    float4 st = a.stats ? __ldg(a.stats + row) : make_float4(0.f, 0.f, 0.f, 0.f);
-    if (!a.post_has) { st.x = 0.f; st.y = 1.f; }      // h_post = y
-    if (!has_pre) { st.z = 0.f; st.w = 0.f; }
-    cp_async_wait(a.stages - 1);
-
+  // h_post = (y - mp) ip, h_pre = (r - mr) ir of the rows in work (0: row i, 1: row i - 1); the mean is subtracted first:
+  // folded into the product it would leave its rounding error, which is large where the mean is
+  float ip[2] = {1.f, 1.f}, mp[2] = {0.f, 0.f}, ir[2] = {0.f, 0.f}, mr[2] = {0.f, 0.f};
+  float c1 = 0.f, c2 = 0.f, m1 = 0.f, m2 = 0.f;    // of row i - 1
+  for (int s = 0; s + 1 < sh.stages; ++s) fetch(s, s);
+  int st_a = 0, st_b = sh.stages - 1;     // ring stages of row i and of row i - 1 (then refilled)
+  for (long long i = 0; i <= n_steps; ++i) {
+    if (i < n) {
+      const float4 st = a.stats ? __ldg(a.stats + first + i * step) : make_float4(0.f, 0.f, 0.f, 0.f);
+      if (a.post_has) {
+        ip[0] = st.y;
+        mp[0] = st.x;
+      }
+      if (has_pre) {
+        ir[0] = st.w;
+        mr[0] = st.z;
+      }
+      cp_async_wait(sh.stages - 2);
+      float s[NS];
+#pragma unroll
+      for (int k = 0; k < NS; ++k) s[k] = 0.f;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (!act[j]) continue;
+        float q[8], w[8], y[8], du[8], r[8], dr[8];
+        weights(j, q, w);
+        piece8(st_a, j, 0, has_y, y);
+        piece8(st_a, j, 1, has_pre, du);
+        resid8(st_a, j, 2, has_pre, r);
+        resid8(st_a, j, 2 + RP, has_dr, dr);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float av = du[k] * w[k], z = fmaf(ir[0], av, dr[k]);
+          if (LAYER) {
+            const float hp = (y[k] - mp[0]) * ip[0], hr = (r[k] - mr[0]) * ir[0], qh = q[k] * hp;
+            s[0] = fmaf(av, hr, s[0]);
+            s[1] = fmaf(z, qh, s[1]);
+            s[2] = fmaf(qh, hr, s[2]);
+            s[3] += av;
+            s[4] = fmaf(q[k], z, s[4]);
+            s[5] = fmaf(q[k], hr, s[5]);
+            s[6] += q[k];
+            s[7] += qh;
+          } else {   // without the factors ip and ir, which are the row's
+            const float qy = q[k] * y[k];
+            s[0] = fmaf(av, r[k], s[0]);
+            s[1] = fmaf(z, qy, s[1]);
+            s[2] = fmaf(qy, r[k], s[2]);
+          }
+        }
+      }
+      int idx;
+      const float mine = warp_sum_scattered<NS>(s, tm.lane, idx);
+      tm.publish(mine, idx, (tm.lane & (32 / NS - 1)) == 0);
+    }
+    if (i > 0 && i <= n) {
+      const long long row = first + (i - 1) * step;
+      const float k1 = ir[1] * c1, k2 = ir[1] * c2, g2 = ip[1] * m2, g1 = ip[1] * m1;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (!act[j]) continue;
+        float q[8], w[8], y[8], du[8], r[8], dr[8];
+        weights(j, q, w);
+        piece8(st_b, j, 0, has_y, y);
+        piece8(st_b, j, 1, has_pre, du);
+        resid8(st_b, j, 2, has_pre, r);
+        resid8(st_b, j, 2 + RP, has_dr, dr);
+        float dy[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float hp = (LAYER ? y[k] - mp[1] : y[k]) * ip[1], hr = (LAYER ? r[k] - mr[1] : r[k]) * ir[1];
+          float t = fmaf(ir[1], du[k] * w[k], dr[k]);
+          if (LAYER) t -= k1;
+          t = fmaf(-hr, k2, t);
+          sumA[j][k] = fmaf(t, hp, sumA[j][k]);
+          sumC[j][k] = fmaf(du[k], hr, sumC[j][k]);
+          if (LAYER) {
+            sumB[j][k] += t;
+            sumE[j][k] += du[k];
+          }
+          dr[k] = a.alpha * t;
+          dy[k] = fmaf(-hp, g2, LAYER ? fmaf(q[k] * t, ip[1], -g1) : (q[k] * t) * ip[1]);
+        }
+        const long long at = row * a.D + col[j];
+        if (a.dx) store8(static_cast<RT *>(a.dx) + at, dr);
+        if (a.dy) store8(a.dy + at, dy);
+      }
+    }
+    fetch(i - 1 + sh.stages, st_b);     // row i - 1 has been read for the last time
+    st_b = st_a;
+    if (++st_a == sh.stages) st_a = 0;
+    if (i == n_steps) break;
+    const float *buf = tm.buffer();
+    tm.turn ^= 1;
+    tm.barrier();
     float s[NS];
 #pragma unroll
     for (int k = 0; k < NS; ++k) s[k] = 0.f;
+    tm.each(buf, [&](const float *f, int, int) {
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      if (!act[j]) continue;
-      float q[8], w[8], y[8], du[8], r[8], dr[8];
-      weights(j, q, w);
-      piece8(stage, j, 0, has_y, y);
-      piece8(stage, j, 1, has_pre, du);
-      resid8(stage, j, 2, has_pre, r);
-      resid8(stage, j, 2 + RP, has_dr, dr);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float hp = (y[k] - st.x) * st.y, hr = (r[k] - st.z) * st.w, av = du[k] * w[k];
-        const float z = q[k] * fmaf(st.w, av, dr[k]), qh = q[k] * hp;
-        s[0] = fmaf(av, hr, s[0]);
-        s[1] = fmaf(z, hp, s[1]);
-        s[2] = fmaf(qh, hr, s[2]);
-        if (LAYER) {
-          s[3] += av;
-          s[4] += z;
-          s[5] = fmaf(q[k], hr, s[5]);
-          s[6] += q[k];
-          s[7] += qh;
-        }
+      for (int k4 = 0; k4 < NS / 4; ++k4) {
+        const float4 v = *reinterpret_cast<const float4 *>(f + 4 * k4);
+        s[4 * k4] += v.x; s[4 * k4 + 1] += v.y; s[4 * k4 + 2] += v.z; s[4 * k4 + 3] += v.w;
       }
-    }
-    if (PAIR) {
-#pragma unroll
-      for (int k = 0; k < NS; ++k) s[k] = warp_sum(s[k]);
-      float *buf = red + turn * (2 * 16 * 8);
-      turn ^= 1;
-      if (lane < 2) {   // lane 0 writes to block 0 of the pair, lane 1 to block 1
-        const uint32_t local = static_cast<uint32_t>(__cvta_generic_to_shared(buf + (rank * 16 + warp) * NS));
-        uint32_t remote;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(local), "r"(lane));
-#pragma unroll
-        for (int k = 0; k < NS; k += 4)
-          asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(remote + 4 * k), "f"(s[k]), "f"(s[k + 1]), "f"(s[k + 2]), "f"(s[k + 3]) : "memory");
-      }
-      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-#pragma unroll
-      for (int k = 0; k < NS; ++k) s[k] = 0.f;
-      for (int q = 0; q < 2; ++q)
-        for (int i = 0; i < a.warps; ++i)
-#pragma unroll
-          for (int k4 = 0; k4 < NS / 4; ++k4) {
-            const float4 f = *reinterpret_cast<const float4 *>(buf + (q * 16 + i) * NS + 4 * k4);
-            s[4 * k4] += f.x; s[4 * k4 + 1] += f.y; s[4 * k4 + 2] += f.z; s[4 * k4 + 3] += f.w;
-          }
-    } else {
-      team_sum<NS>(s, a.warps, first_warp, warp, lane, 1 + team, red, turn);
-    }
-    const float c2 = s[0] * inv_d;
-    float c1 = 0.f, m1 = 0.f, m2;
+    });
+    ip[1] = ip[0]; mp[1] = mp[0]; ir[1] = ir[0]; mr[1] = mr[0];
     if (LAYER) {
       c1 = a.pre_layer ? s[3] * inv_d : 0.f;
-      m1 = a.post_layer ? (s[4] - st.w * (c1 * s[6] + c2 * s[5])) * inv_d : 0.f;
-      m2 = (s[1] - st.w * (c1 * s[7] + c2 * s[2])) * inv_d;
+      c2 = s[0] * inv_d;
+      m1 = a.post_layer ? (s[4] - ir[1] * (c1 * s[6] + c2 * s[5])) * inv_d : 0.f;
+      m2 = (s[1] - ir[1] * (c1 * s[7] + c2 * s[2])) * inv_d;
     } else {
-      m2 = (s[1] - st.w * (c2 * s[2])) * inv_d;
+      c2 = s[0] * ir[1] * inv_d;
+      m2 = ip[1] * (s[1] - ir[1] * ir[1] * c2 * s[2]) * inv_d;
     }
     if (!a.post_has) m2 = 0.f;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      if (!act[j]) continue;
-      float q[8], w[8], y[8], du[8], r[8], dr[8];
-      weights(j, q, w);
-      piece8(stage, j, 0, has_y, y);
-      piece8(stage, j, 1, has_pre, du);
-      resid8(stage, j, 2, has_pre, r);
-      resid8(stage, j, 2 + RP, has_dr, dr);
-      float dy[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float hp = (y[k] - st.x) * st.y, hr = (r[k] - st.z) * st.w;
-        const float t = fmaf(st.w, fmaf(-hr, c2, fmaf(du[k], w[k], -c1)), dr[k]);
-        sumA[j][k] = fmaf(t, hp, sumA[j][k]);
-        sumC[j][k] = fmaf(du[k], hr, sumC[j][k]);
-        if (LAYER) {
-          sumB[j][k] += t;
-          sumE[j][k] += du[k];
-        }
-        dr[k] = a.alpha * t;
-        dy[k] = st.y * fmaf(-hp, m2, fmaf(q[k], t, -m1));
-      }
-      const long long at = row * a.D + col[j];
-      if (a.dx) store8(static_cast<RT *>(a.dx) + at, dr);
-      if (a.dy) store8(a.dy + at, dy);
-    }
-    if (++stage == a.stages) stage = 0;
   }
   cp_async_wait(0);
 
   // Channel sums of the block: teams added in ascending order.
   __syncthreads();
-  float *acc = reinterpret_cast<float *>(ring);   // [team][vector][half][TL] float4, one sum at a time
+  float4 *acc = reinterpret_cast<float4 *>(ring);   // [team][vector][half][TL], one sum at a time
   constexpr int NACC = LAYER ? 4 : 2;
 #pragma unroll
   for (int q = 0; q < NACC; ++q) {
-    float4 *mine = reinterpret_cast<float4 *>(acc) + team * (4 * TL);
+    float4 *mine = acc + tm.team * (4 * TL);
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -536,18 +850,18 @@ __global__ void __launch_bounds__(BWD_THREADS, 1) block_norm_bwd_kernel(const __
         mine[(j * 2 + h) * TL + tl] = make_float4(p[0], p[1], p[2], p[3]);
       }
     __syncthreads();
-    if (team == 0) {
+    if (tm.team == 0) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (!act[j]) continue;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          float4 v = reinterpret_cast<float4 *>(acc)[(j * 2 + h) * TL + tl];
-          for (int t = 1; t < a.teams; ++t) {
-            const float4 o = reinterpret_cast<float4 *>(acc)[(t * 4 + j * 2 + h) * TL + tl];
+          float4 v = acc[(j * 2 + h) * TL + tl];
+          for (int t = 1; t < sh.teams; ++t) {
+            const float4 o = acc[(t * 4 + j * 2 + h) * TL + tl];
             v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
           }
-          *reinterpret_cast<float4 *>(a.partial + ((long long)unit * 4 + q) * a.D + col[j] + 4 * h) = v;
+          *reinterpret_cast<float4 *>(a.partial + ((long long)tm.unit * 4 + q) * a.D + col[j] + 4 * h) = v;
         }
       }
     }
@@ -603,7 +917,6 @@ __global__ void __launch_bounds__(256) block_norm_final_kernel(const __grid_cons
 // ------------------------------------------------------------------------------------------------ host
 
 constexpr int SMEM_MAX = 227 * 1024;
-constexpr int RED_BYTES_HOST = 2 * 2 * 16 * 8 * 4;
 
 template <typename RT, int V>
 int launch_fwd(const FwdArgs &args, int warps, cudaStream_t stream) {
@@ -613,37 +926,62 @@ int launch_fwd(const FwdArgs &args, int warps, cudaStream_t stream) {
   return launch_overlapped(block_norm_fwd_kernel<RT, V>, dim3((unsigned)cdiv(a.M, teams)), dim3(teams * warps * 32), 0, 1, stream, a);
 }
 
-template <typename RT, bool LAYER, bool PAIR>
-int launch_bwd(const BwdArgs &args, int sms, int *units, cudaStream_t stream) {
-  BwdArgs a = args;
-  const int width = PAIR ? (a.D / 8 + 1) / 2 * 8 : a.D;
-  a.warps = (int)cdiv(width, 512);
-  a.teams = PAIR ? 1 : 16 / a.warps;
-  const int threads = a.warps * a.teams * 32;
-  const int stage = 2 * (2 + 2 * (int)(sizeof(RT) / 2)) * threads * 16;
-  const int w_bytes = LAYER ? 8 * a.warps * 32 * 16 : 0;
-  a.stages = (SMEM_MAX - RED_BYTES_HOST - w_bytes) / stage;
-  if (a.stages > MAX_STAGES) a.stages = MAX_STAGES;
-  const int smem = RED_BYTES_HOST + w_bytes + a.stages * stage;
-  int64_t n = cdiv(a.M, a.teams);
-  const int cap = PAIR ? sms / 2 : sms;
+// Shape and launch of a kernel that walks many rows on clusters of CL blocks.  `pieces`: 16-byte pieces of a vector in
+// the ring, `red_bytes` and `w_bytes_per_thread`: what else it keeps in shared memory.  As many teams to a block as leave
+// room for three rows each (one being finished, one begun, one on its way); OSDP_ERR_UNSUPPORTED if not even one does.
+template <int CL, auto KERNEL, typename Args>
+int launch_rows(const Args &a, int pieces, int red_bytes, int w_bytes_per_thread, int sms, int *units, cudaStream_t stream) {
+  TeamShape sh;
+  sh.warps = (int)cdiv(block_channels(a.D, CL), 512);
+  if (sh.warps > 16) return OSDP_ERR_UNSUPPORTED;
+  const int fixed = red_bytes + w_bytes_per_thread * sh.warps * 32;
+  int stage = 0;
+  for (sh.teams = 16 / sh.warps; sh.teams > 0; --sh.teams) {
+    stage = 2 * pieces * sh.teams * sh.warps * 32 * 16;
+    sh.stages = (SMEM_MAX - fixed) / stage;
+    if (sh.stages >= 3) break;
+  }
+  if (sh.teams == 0) return OSDP_ERR_UNSUPPORTED;
+  if (sh.stages > MAX_STAGES) sh.stages = MAX_STAGES;
+  const int threads = sh.warps * sh.teams * 32;
+  int64_t n = cdiv(a.M, sh.teams);
+  const int cap = sms / CL;
   if (n > cap) n = cap;
-  if (n > BWD_MAX_BLOCKS) n = BWD_MAX_BLOCKS;
-  if (n < 1) n = 1;    // no rows: zeros are written
-  *units = (int)n;
-  auto kernel = block_norm_bwd_kernel<RT, LAYER, PAIR>;
-  static std::atomic<bool> ready[64];
-  static std::mutex setup;
+  if (n > ROW_MAX_BLOCKS) n = ROW_MAX_BLOCKS;
+  if (n < 1) n = 1;    // no rows: the backward writes zeros
+  if (units) *units = (int)n;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return report_cuda(e);
+  static std::atomic<bool> ready[64];
+  static std::mutex setup;
   if (!ready[dev & 63].load(std::memory_order_acquire)) {
     std::lock_guard<std::mutex> lock(setup);
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
+    e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
     if (e != cudaSuccess) return report_cuda(e);
     ready[dev & 63].store(true, std::memory_order_release);
   }
-  return launch_overlapped(kernel, dim3((unsigned)(PAIR ? 2 * n : n)), dim3(threads), smem, PAIR ? 2 : 1, stream, a);
+  return launch_overlapped(KERNEL, dim3((unsigned)(CL * n)), dim3(threads), fixed + sh.stages * stage, CL, stream, a, sh);
+}
+
+// The smallest cluster that the rows fit.
+template <typename RT, bool LAYER, int CL = 1>
+int launch_fwd_rows(const FwdArgs &a, int sms, cudaStream_t stream) {
+  const int rc = launch_rows<CL, block_norm_fwd_rows_kernel<RT, LAYER, CL>>(a, 1 + (int)sizeof(RT) / 2, Team<CL, LAYER ? 4 : 2>::RED_FLOATS * 4, 0,
+                                                                            sms, nullptr, stream);
+  if constexpr (CL < 2) {
+    if (rc == OSDP_ERR_UNSUPPORTED) return launch_fwd_rows<RT, LAYER, 2 * CL>(a, sms, stream);
+  }
+  return rc;
+}
+template <typename RT, bool LAYER, int CL = 1>
+int launch_bwd(const BwdArgs &a, int sms, int *units, cudaStream_t stream) {
+  const int rc = launch_rows<CL, block_norm_bwd_kernel<RT, LAYER, CL>>(a, 2 + (int)sizeof(RT), Team<CL, LAYER ? 8 : 4>::RED_FLOATS * 4,
+                                                                       LAYER ? 128 : 0, sms, units, stream);
+  if constexpr (CL < 4) {
+    if (rc == OSDP_ERR_UNSUPPORTED) return launch_bwd<RT, LAYER, 2 * CL>(a, sms, units, stream);
+  }
+  return rc;
 }
 
 bool norm_kind(int k) { return k == OSDP_NORM_NONE || k == OSDP_NORM_RMS || k == OSDP_NORM_LAYER; }
@@ -696,8 +1034,18 @@ int osdp_block_norm_fwd(const void *x, const void *y, int64_t M, int64_t D, int 
   a.D = (int)D;
   a.warps = 0;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int sms = 0;
+  const int src = sm_count(&sms);
+  if (src) return src;
   // Few rows: one vector per lane, as many warps to a row as it has vectors, for the shortest chain of instructions.
   const bool few = D <= 8192 && M * cdiv(D, 256) <= 148 * 8;
+  if (!few && !u_scale && D > 512) {
+    const bool layer = a.post.layer || a.pre.layer;
+#define OSDP_FWD(RT, LAYER) launch_fwd_rows<RT, LAYER>(a, sms, s)
+    if (resid_dtype == OSDP_DTYPE_FP32) return layer ? OSDP_FWD(float, true) : OSDP_FWD(float, false);
+    return layer ? OSDP_FWD(__nv_bfloat16, true) : OSDP_FWD(__nv_bfloat16, false);
+#undef OSDP_FWD
+  }
   if (few)
     return resid_dtype == OSDP_DTYPE_FP32 ? launch_fwd<float, 1>(a, (int)cdiv(D, 256), s) : launch_fwd<__nv_bfloat16, 1>(a, (int)cdiv(D, 256), s);
   return resid_dtype == OSDP_DTYPE_FP32 ? launch_fwd<float, 4>(a, (int)cdiv(D, 1024), s) : launch_fwd<__nv_bfloat16, 4>(a, (int)cdiv(D, 1024), s);
@@ -707,7 +1055,7 @@ int osdp_block_norm_workspace_bytes(int64_t M, int64_t D, size_t *bytes) {
   if (!bytes) return OSDP_ERR_NULL_POINTER;
   const int rc = check_shape(M, D, OSDP_DTYPE_BF16, 0, 0);
   if (rc) return rc;
-  *bytes = 256 + (size_t)BWD_MAX_BLOCKS * 4 * (size_t)D * sizeof(float);
+  *bytes = 256 + (size_t)ROW_MAX_BLOCKS * 4 * (size_t)D * sizeof(float);
   return OSDP_OK;
 }
 
@@ -755,11 +1103,10 @@ int osdp_block_norm_bwd(const void *dr, const void *du, const void *y, const voi
   a.partial = reinterpret_cast<float *>(static_cast<char *>(ws) + 256);
   a.M = M;
   a.D = (int)D;
-  a.warps = a.teams = a.stages = 0;
-  const bool layer = a.post_layer || a.pre_layer || db_post || db_pre, pair = D > 8192;
+  const bool layer = a.post_layer || a.pre_layer || db_post || db_pre;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int units = 0;
-#define OSDP_BWD(RT, LAYER) (pair ? launch_bwd<RT, LAYER, true>(a, sms, &units, s) : launch_bwd<RT, LAYER, false>(a, sms, &units, s))
+#define OSDP_BWD(RT, LAYER) launch_bwd<RT, LAYER>(a, sms, &units, s)
   if (resid_dtype == OSDP_DTYPE_FP32) rc = layer ? OSDP_BWD(float, true) : OSDP_BWD(float, false);
   else rc = layer ? OSDP_BWD(__nv_bfloat16, true) : OSDP_BWD(__nv_bfloat16, false);
 #undef OSDP_BWD
