@@ -361,7 +361,9 @@ struct Team {
 // A step finishes row i (u), does row i + 1 up to its sums (r) and takes the sums of row i + 2's y.  The variance is
 // taken per warp about the warp's own mean and the warps' means and variances are merged, which is as safe as a second
 // pass over the row and needs no second exchange.
-template <typename RT, bool LAYER, int CL>
+// LAYER: either norm subtracts a mean.  FULL: y, both norms, r and u are there (the form between two blocks); without
+// it each may be absent, which costs branches.
+template <typename RT, bool LAYER, int CL, bool FULL>
 __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_fwd_rows_kernel(const __grid_constant__ FwdArgs a, const TeamShape sh) {
   constexpr int RP = sizeof(RT) / 2;             // 16-byte pieces of a residual vector
   constexpr int PIECES = 1 + RP;                 // y, x
@@ -369,40 +371,52 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_fwd_rows_kernel(con
   extern __shared__ __align__(16) uint8_t smem[];
   Team<CL, NS> tm;
   tm.init(sh, a.D, reinterpret_cast<float *>(smem));
-  uint8_t *ring = smem + Team<CL, NS>::RED_FLOATS * 4;
+  float *count = reinterpret_cast<float *>(smem) + Team<CL, NS>::RED_FLOATS;   // channels of each warp of a team, by block
+  uint8_t *ring = reinterpret_cast<uint8_t *>(count + CL * 16);
   const uint32_t ring_u32 = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
   const int nthreads = blockDim.x;
   const int stage_bytes = 2 * PIECES * nthreads * 16;
+  if (LAYER && threadIdx.x < CL * 16) count[threadIdx.x] = tm.channels(threadIdx.x / 16, threadIdx.x % 16, a.D);
   pdl_launch_dependents();
   pdl_wait();
 
+  const bool has_y = FULL || a.y != nullptr, post = FULL || (has_y && a.post.has), pre = FULL || a.pre.has, has_r = FULL || a.r != nullptr;
   int col[2];
   bool act[2];
-  float qw[2][8], wp[2][8], qb[LAYER ? 2 : 1][8], bp[LAYER ? 2 : 1][8];   // r = alpha x + qw h + qb, u = wp h + bp
+  f2 qw[2][4], wp[2][4], qb[LAYER ? 2 : 1][4], bp[LAYER ? 2 : 1][4];   // r = alpha x + qw h + qb, u = wp h + bp
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     col[j] = tm.c_begin + (j * tm.TL + tm.tl) * 8;
     act[j] = col[j] < tm.c_end;
+    float q[8], b[8], w[8], c[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      qw[j][k] = wp[j][k] = 0.f;
-      if (LAYER) qb[j][k] = bp[j][k] = 0.f;
+    for (int k = 0; k < 8; ++k) q[k] = b[k] = w[k] = c[k] = 0.f;
+    if (act[j]) {
+      if (has_y) {
+        float g[8];
+        weights8(a.gate, col[j], 1.f, g);
+        weights8(a.post.w, col[j], 1.f, q);
+        if (LAYER) weights8(a.post.b, col[j], 0.f, b);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          q[k] *= a.beta * g[k];
+          b[k] *= a.beta * g[k];
+        }
+      }
+      if (pre) weights8(a.pre.w, col[j], 1.f, w);
+      if (LAYER) weights8(a.pre.b, col[j], 0.f, c);
     }
-    if (!act[j]) continue;
-    if (a.y) {
-      float g[8];
-      weights8(a.gate, col[j], 1.f, g);
-      weights8(a.post.w, col[j], 1.f, qw[j]);
-      if (LAYER) weights8(a.post.b, col[j], 0.f, qb[j]);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        qw[j][k] *= a.beta * g[k];
-        if (LAYER) qb[j][k] *= a.beta * g[k];
+    for (int k = 0; k < 4; ++k) {
+      qw[j][k] = pack2(q[2 * k], q[2 * k + 1]);
+      wp[j][k] = pack2(w[2 * k], w[2 * k + 1]);
+      if (LAYER) {
+        qb[j][k] = pack2(b[2 * k], b[2 * k + 1]);
+        bp[j][k] = pack2(c[2 * k], c[2 * k + 1]);
       }
     }
-    if (a.pre.has) weights8(a.pre.w, col[j], 1.f, wp[j]);
-    if (LAYER) weights8(a.pre.b, col[j], 0.f, bp[j]);
   }
+  if (LAYER) __syncthreads();
   if (CL > 1) tm.barrier();   // the other blocks run before anything is written to their shared memory
 
   const long long first = (long long)tm.unit * sh.teams + tm.team, step = (long long)tm.units * sh.teams;
@@ -410,164 +424,163 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_fwd_rows_kernel(con
   // the teams of a cluster meet at its barrier: all do as many steps as its first team, which has the most rows
   const long long n_steps = CL == 1 ? n : (a.M - (first - tm.team) + step - 1) / step;
   auto slot = [&](int stage, int j, int piece) { return stage * stage_bytes + ((j * PIECES + piece) * nthreads + (int)threadIdx.x) * 16; };
-  auto fetch = [&](long long i, int stage) {
-    if (i < n) {
+  const long long row_step = step * a.D;
+  long long f_at = first * a.D;                  // first channel of the row that is fetched next
+  long long f_row = 0;
+  auto fetch = [&](int stage) {
+    if (f_row < n) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (!act[j]) continue;
-        const long long at = (first + i * step) * a.D + col[j];
-        if (a.y) cp_async16(ring_u32 + slot(stage, j, 0), a.y + at);
+        if (has_y) cp_async16(ring_u32 + slot(stage, j, 0), a.y + f_at + col[j]);
 #pragma unroll
         for (int p = 0; p < RP; ++p)
-          cp_async16(ring_u32 + slot(stage, j, 1 + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.x) + at) + 16 * p);
+          cp_async16(ring_u32 + slot(stage, j, 1 + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.x) + f_at + col[j]) + 16 * p);
       }
     }
+    ++f_row;
+    f_at += row_step;
     cp_async_commit();
   };
   const float inv_d = 1.0f / (float)a.D;
-  const float my_channels = LAYER ? tm.channels((int)tm.rank, tm.warp - tm.first_warp, a.D) : 0.f;
+  const float my_channels = LAYER ? count[tm.rank * 16 + tm.warp - tm.first_warp] : 0.f;
   const float my_inv = my_channels > 0.f ? 1.0f / my_channels : 0.f;
-  const bool has_y = a.y != nullptr, post = has_y && a.post.has, pre = a.pre.has;
-  const bool y_mean = LAYER && post && a.post.layer, r_mean = LAYER && pre && a.pre.layer;
-  float r[2][8];
+  const float y_mean = (LAYER && post && a.post.layer) ? my_inv : 0.f, r_mean = (LAYER && pre && a.pre.layer) ? my_inv : 0.f;
+  const f2 alpha = both(a.alpha), zero = both(0.f);
+  f2 r[2][4];
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) r[j][k] = 0.f;
+    for (int k = 0; k < 4; ++k) r[j][k] = zero;
   float mean_y = 0.f, rstd_y = 1.f, mean_r = 0.f, rstd_r = 0.f, shown_mean_y = 0.f, shown_rstd_y = 0.f;
 
-  for (int s = 0; s + 1 < sh.stages; ++s) fetch(s, s);
+  for (int s = 0; s + 1 < sh.stages; ++s) fetch(s);
   int st_a = 0, st_b = sh.stages - 1;     // ring stages of row i (its y) and of row i - 1 (then refilled)
-  for (long long i = 0; i < n_steps + 2; ++i) {
+  long long at = first * a.D - 2 * row_step;   // first channel of row i - 2
+  for (long long i = 0; i < n_steps + 2; ++i, at += row_step) {
     if (i >= 2 && i < n + 2) {
       // ---- row i - 2: u
-      const long long row = first + (i - 2) * step;
       if (pre) {
+        const f2 shift = both(-mean_r), scale = both(rstd_r);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           if (!act[j]) continue;
-          float u[8];
+          f2 u[4];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float h = (LAYER ? r[j][k] - mean_r : r[j][k]) * rstd_r;
-            u[k] = LAYER ? fmaf(h, wp[j][k], bp[j][k]) : h * wp[j][k];
+          for (int k = 0; k < 4; ++k) {
+            const f2 h = mul2(LAYER ? add2(r[j][k], shift) : r[j][k], scale);
+            u[k] = LAYER ? fma2(h, wp[j][k], bp[j][k]) : mul2(h, wp[j][k]);
           }
-          store8(static_cast<__nv_bfloat16 *>(a.u) + row * a.D + col[j], u);
+          store4(static_cast<__nv_bfloat16 *>(a.u) + at + col[j], u);
         }
       }
       if (a.stats && tm.tl == 0 && tm.rank == 0)
-        a.stats[row] = make_float4(shown_mean_y, shown_rstd_y, pre ? mean_r : 0.f, pre ? rstd_r : 0.f);
+        a.stats[first + (i - 2) * step] = make_float4(shown_mean_y, shown_rstd_y, pre ? mean_r : 0.f, pre ? rstd_r : 0.f);
     }
-    float part[NS];
-#pragma unroll
-    for (int k = 0; k < NS; ++k) part[k] = 0.f;
+    f2 part_y = zero, part_r = zero;
     if (i >= 1 && i <= n) {
       // ---- row i - 1: r
-      const long long row = first + (i - 1) * step;
+      const f2 shift = both(-mean_y), scale = both(rstd_y);
       shown_mean_y = post ? mean_y : 0.f;
       shown_rstd_y = post ? rstd_y : 0.f;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (!act[j]) continue;
-        float x[8];
-        if (RP == 1) {
-          widen8(*reinterpret_cast<const uint4 *>(ring + slot(st_b, j, 1)), x);
-        } else {
-          const float4 lo = *reinterpret_cast<const float4 *>(ring + slot(st_b, j, 1)), hi = *reinterpret_cast<const float4 *>(ring + slot(st_b, j, PIECES - 1));
-          x[0] = lo.x; x[1] = lo.y; x[2] = lo.z; x[3] = lo.w;
-          x[4] = hi.x; x[5] = hi.y; x[6] = hi.z; x[7] = hi.w;
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) r[j][k] = a.alpha * x[k];
+        f2 x[4];
+        if (RP == 1)
+          widen4(*reinterpret_cast<const uint4 *>(ring + slot(st_b, j, 1)), x);
+        else
+          join4(*reinterpret_cast<const float4 *>(ring + slot(st_b, j, 1)), *reinterpret_cast<const float4 *>(ring + slot(st_b, j, PIECES - 1)), x);
         if (has_y) {
-          float y[8];
-          widen8(*reinterpret_cast<const uint4 *>(ring + slot(st_b, j, 0)), y);
+          f2 y[4];
+          widen4(*reinterpret_cast<const uint4 *>(ring + slot(st_b, j, 0)), y);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const float h = (LAYER ? y[k] - mean_y : y[k]) * rstd_y;
-            r[j][k] = fmaf(qw[j][k], h, LAYER ? r[j][k] + qb[j][k] : r[j][k]);
+          for (int k = 0; k < 4; ++k) {
+            const f2 h = mul2(LAYER ? add2(y[k], shift) : y[k], scale);
+            const f2 base = LAYER ? fma2(alpha, x[k], qb[j][k]) : mul2(alpha, x[k]);
+            r[j][k] = fma2(qw[j][k], h, base);
           }
-        }
-        if (a.r) store8(static_cast<RT *>(a.r) + row * a.D + col[j], r[j]);
-        if (LAYER) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) part[2] += r[j][k];
         } else {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) part[1] = fmaf(r[j][k], r[j][k], part[1]);
+          for (int k = 0; k < 4; ++k) r[j][k] = mul2(alpha, x[k]);
         }
+        if (has_r) store4(static_cast<RT *>(a.r) + (at + row_step) + col[j], r[j]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) part_r = LAYER ? add2(part_r, r[j][k]) : fma2(r[j][k], r[j][k], part_r);
       }
     }
-    float y[2][8];
+    f2 y[2][4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[j][k] = zero;
     if (i < n) {
       // ---- row i: sums of y
       cp_async_wait(sh.stages - 2);
+      if (post) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        if (post && act[j]) {
-          widen8(*reinterpret_cast<const uint4 *>(ring + slot(st_a, j, 0)), y[j]);
+        for (int j = 0; j < 2; ++j) {
+          if (!act[j]) continue;
+          widen4(*reinterpret_cast<const uint4 *>(ring + slot(st_a, j, 0)), y[j]);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) part[0] = LAYER ? part[0] + y[j][k] : fmaf(y[j][k], y[j][k], part[0]);
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) y[j][k] = 0.f;
+          for (int k = 0; k < 4; ++k) part_y = LAYER ? add2(part_y, y[j][k]) : fma2(y[j][k], y[j][k], part_y);
         }
       }
     }
-    // st_b is free: row i - 1 has been read for the last time
-    fetch(i - 1 + sh.stages, st_b);
+    fetch(st_b);     // row i - 1 has been read for the last time
     st_b = st_a;
     if (++st_a == sh.stages) st_a = 0;
+    float two[2] = {sum2(part_y), sum2(part_r)};
+    int idx;
+    float s = warp_sum_scattered<2>(two, tm.lane, idx);
     if (LAYER) {
-      const float my = y_mean ? warp_sum(part[0]) * my_inv : 0.f, mr = r_mean ? warp_sum(part[2]) * my_inv : 0.f;
-      float d[2] = {0.f, 0.f};
+      const float my = __shfl_sync(0xFFFFFFFFu, s, 0) * y_mean, mr = __shfl_sync(0xFFFFFFFFu, s, 16) * r_mean;
+      const f2 sy = both(-my), sr = both(-mr);
+      f2 dy = zero, dr = zero;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (!act[j]) continue;
-        if (i < n && post) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) d[0] = fmaf(y[j][k] - my, y[j][k] - my, d[0]);
+        for (int k = 0; k < 4; ++k) {
+          const f2 ey = add2(y[j][k], sy), er = add2(r[j][k], sr);
+          dy = fma2(ey, ey, dy);
+          dr = fma2(er, er, dr);
         }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) d[1] = fmaf(r[j][k] - mr, r[j][k] - mr, d[1]);
       }
-      d[0] = warp_sum(d[0]);
-      d[1] = warp_sum(d[1]);
-      tm.publish(tm.lane == 0 ? my : tm.lane == 1 ? d[0] : tm.lane == 2 ? mr : d[1], tm.lane & 3, tm.lane < 4);
+      float d[2] = {sum2(dy), sum2(dr)};
+      s = warp_sum_scattered<2>(d, tm.lane, idx);
+      // lanes 0 and 16 bring the squared distances, 1 and 17 the means
+      const bool mean_lane = (tm.lane & 1) != 0;
+      tm.publish(mean_lane ? (idx ? mr : my) : s, 2 * idx + (mean_lane ? 0 : 1), (tm.lane & 14) == 0);
     } else {
-      float two[2] = {part[0], part[1]};
-      int idx;
-      const float s = warp_sum_scattered<2>(two, tm.lane, idx);
       tm.publish(s, idx, (tm.lane & 15) == 0);
     }
     const float *buf = tm.buffer();
     tm.turn ^= 1;
     tm.barrier();
+    float vy = 0.f, vr = 0.f;
     if (LAYER) {
-      float sy = 0.f, sr = 0.f, vy = 0.f, vr = 0.f;
+      float sy = 0.f, sr = 0.f;
       tm.each(buf, [&](const float *f, int b, int w) {
-        const float c = tm.channels(b, w, a.D);
+        const float c = count[b * 16 + w];
         sy = fmaf(c, f[0], sy);
         sr = fmaf(c, f[2], sr);
       });
       mean_y = sy * inv_d;
       mean_r = sr * inv_d;
       tm.each(buf, [&](const float *f, int b, int w) {
-        const float c = tm.channels(b, w, a.D), dy = f[0] - mean_y, dr = f[2] - mean_r;
+        const float c = count[b * 16 + w], dy = f[0] - mean_y, dr = f[2] - mean_r;
         vy += fmaf(c * dy, dy, f[1]);
         vr += fmaf(c * dr, dr, f[3]);
       });
-      rstd_y = post ? rsqrtf(fmaf(vy, inv_d, a.post.eps)) : 1.f;
-      rstd_r = rsqrtf(fmaf(vr, inv_d, a.pre.eps));
     } else {
-      float sy = 0.f, sr = 0.f;
       tm.each(buf, [&](const float *f, int, int) {
-        sy += f[0];
-        sr += f[1];
+        vy += f[0];
+        vr += f[1];
       });
-      rstd_y = post ? rsqrtf(fmaf(sy, inv_d, a.post.eps)) : 1.f;
-      rstd_r = rsqrtf(fmaf(sr, inv_d, a.pre.eps));
     }
+    rstd_y = post ? rsqrtf(fmaf(vy, inv_d, a.post.eps)) : 1.f;
+    rstd_r = rsqrtf(fmaf(vr, inv_d, a.pre.eps));
   }
   cp_async_wait(0);
 }
@@ -595,7 +608,8 @@ struct BwdArgs {
 // A step takes the sums of row i + 1 and writes the gradients of row i.  The sums over rows stay in registers.
 //
 // LAYER: either norm subtracts a mean (more sums; the weights are then in shared memory, there are too few registers).
-template <typename RT, bool LAYER, int CL>
+// FULL: every input, both norms, dx and dy are there.
+template <typename RT, bool LAYER, int CL, bool FULL>
 __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __grid_constant__ BwdArgs a, const TeamShape sh) {
   constexpr bool WREG = !LAYER;
   constexpr int NS = LAYER ? 8 : 4;                 // sums per row
@@ -614,9 +628,10 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
   pdl_launch_dependents();
   pdl_wait();
 
+  const bool has_y = FULL || a.y != nullptr, has_dr = FULL || a.dr != nullptr, has_pre = FULL || a.pre_has != 0, has_post = FULL || a.post_has != 0;
   int col[2];
   bool act[2];
-  float qreg[WREG ? 2 : 1][8], wreg[WREG ? 2 : 1][8];
+  f2 qreg[WREG ? 2 : 1][4], wreg[WREG ? 2 : 1][4];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     col[j] = tm.c_begin + (j * TL + tl) * 8;
@@ -625,17 +640,20 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
 #pragma unroll
     for (int k = 0; k < 8; ++k) q[k] = w[k] = 0.f;
     if (act[j]) {
-      if (a.y) {
+      if (has_y) {
         weights8(a.w_post, col[j], 1.f, q);
         weights8(a.gate, col[j], 1.f, g);
 #pragma unroll
         for (int k = 0; k < 8; ++k) q[k] *= a.beta * g[k];
       }
-      if (a.pre_has) weights8(a.w_pre, col[j], 1.f, w);
+      if (has_pre) weights8(a.w_pre, col[j], 1.f, w);
     }
     if (WREG) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) { qreg[j][k] = q[k]; wreg[j][k] = w[k]; }
+      for (int k = 0; k < 4; ++k) {
+        qreg[j][k] = pack2(q[2 * k], q[2 * k + 1]);
+        wreg[j][k] = pack2(w[2 * k], w[2 * k + 1]);
+      }
     } else if (tm.team == 0) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -646,17 +664,16 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
   }
   if (!WREG) __syncthreads();
   if (CL > 1) tm.barrier();   // the other blocks run before anything is written to their shared memory
-  auto weights = [&](int j, float (&q)[8], float (&w)[8]) {
+  auto weights = [&](int j, f2 (&q)[4], f2 (&w)[4]) {
     if (WREG) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) { q[k] = qreg[j][k]; w[k] = wreg[j][k]; }
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float4 fq = wsm[(0 + j * 2 + h) * TL + tl], fw = wsm[(4 + j * 2 + h) * TL + tl];
-        q[4 * h] = fq.x; q[4 * h + 1] = fq.y; q[4 * h + 2] = fq.z; q[4 * h + 3] = fq.w;
-        w[4 * h] = fw.x; w[4 * h + 1] = fw.y; w[4 * h + 2] = fw.z; w[4 * h + 3] = fw.w;
+      for (int k = 0; k < 4; ++k) {
+        q[k] = qreg[j][k];
+        w[k] = wreg[j][k];
       }
+    } else {
+      join4(wsm[(0 + j * 2) * TL + tl], wsm[(1 + j * 2) * TL + tl], q);
+      join4(wsm[(4 + j * 2) * TL + tl], wsm[(5 + j * 2) * TL + tl], w);
     }
   };
 
@@ -665,67 +682,65 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
   // the teams of a cluster meet at its barrier: all do as many steps as its first team, which has the most rows
   const long long n_steps = CL == 1 ? n : (a.M - (first - tm.team) + step - 1) / step;
   auto slot = [&](int stage, int j, int piece) { return stage * stage_bytes + ((j * PIECES + piece) * nthreads + (int)threadIdx.x) * 16; };
-  auto fetch = [&](long long i, int stage) {
-    if (i < n) {
+  const long long row_step = step * a.D;
+  long long f_at = first * a.D, f_row = 0;       // first channel and number of the row that is fetched next
+  auto fetch = [&](int stage) {
+    if (f_row < n) {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (!act[j]) continue;
-        const long long at = (first + i * step) * a.D + col[j];
-        if (a.y) cp_async16(ring_u32 + slot(stage, j, 0), a.y + at);
-        if (a.pre_has) {
+        const long long at = f_at + col[j];
+        if (has_y) cp_async16(ring_u32 + slot(stage, j, 0), a.y + at);
+        if (has_pre) {
           cp_async16(ring_u32 + slot(stage, j, 1), a.du + at);
 #pragma unroll
           for (int p = 0; p < RP; ++p)
             cp_async16(ring_u32 + slot(stage, j, 2 + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.r) + at) + 16 * p);
         }
-        if (a.dr) {
+        if (has_dr) {
 #pragma unroll
           for (int p = 0; p < RP; ++p)
             cp_async16(ring_u32 + slot(stage, j, 2 + RP + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.dr) + at) + 16 * p);
         }
       }
     }
+    ++f_row;
+    f_at += row_step;
     cp_async_commit();
   };
-  auto piece8 = [&](int stage, int j, int piece, bool there, float (&f)[8]) {   // one bf16 vector
+  const f2 zero = both(0.f);
+  auto read = [&](int stage, int j, int piece, bool there, bool resid, f2 (&f)[4]) {   // one vector of eight channels
     if (!there) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) f[k] = 0.f;
+      for (int k = 0; k < 4; ++k) f[k] = zero;
+    } else if (resid && RP == 2) {
+      join4(*reinterpret_cast<const float4 *>(ring + slot(stage, j, piece)), *reinterpret_cast<const float4 *>(ring + slot(stage, j, piece + 1)), f);
     } else {
-      widen8(*reinterpret_cast<const uint4 *>(ring + slot(stage, j, piece)), f);
-    }
-  };
-  auto resid8 = [&](int stage, int j, int piece, bool there, float (&f)[8]) {
-    if (RP == 1 || !there) {
-      piece8(stage, j, piece, there, f);
-    } else {
-      const float4 lo = *reinterpret_cast<const float4 *>(ring + slot(stage, j, piece)),
-                   hi = *reinterpret_cast<const float4 *>(ring + slot(stage, j, piece + 1));
-      f[0] = lo.x; f[1] = lo.y; f[2] = lo.z; f[3] = lo.w;
-      f[4] = hi.x; f[5] = hi.y; f[6] = hi.z; f[7] = hi.w;
+      widen4(*reinterpret_cast<const uint4 *>(ring + slot(stage, j, piece)), f);
     }
   };
 
-  float sumA[2][8], sumC[2][8], sumB[LAYER ? 2 : 1][8], sumE[LAYER ? 2 : 1][8];
+  f2 sumA[2][4], sumC[2][4], sumB[LAYER ? 2 : 1][4], sumE[LAYER ? 2 : 1][4];
 #pragma unroll
   for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      sumA[j][k] = sumC[j][k] = 0.f;
-      if (LAYER) sumB[j][k] = sumE[j][k] = 0.f;
+    for (int k = 0; k < 4; ++k) {
+      sumA[j][k] = sumC[j][k] = zero;
+      if (LAYER) sumB[j][k] = sumE[j][k] = zero;
     }
-  const bool has_y = a.y != nullptr, has_dr = a.dr != nullptr, has_pre = a.pre_has != 0;
   const float inv_d = 1.0f / (float)a.D;
   // h_post = (y - mp) ip, h_pre = (r - mr) ir of the rows in work (0: row i, 1: row i - 1); the mean is subtracted first:
   // folded into the product it would leave its rounding error, which is large where the mean is
   float ip[2] = {1.f, 1.f}, mp[2] = {0.f, 0.f}, ir[2] = {0.f, 0.f}, mr[2] = {0.f, 0.f};
   float c1 = 0.f, c2 = 0.f, m1 = 0.f, m2 = 0.f;    // of row i - 1
-  for (int s = 0; s + 1 < sh.stages; ++s) fetch(s, s);
+  const f2 alpha = both(a.alpha);
+  for (int s = 0; s + 1 < sh.stages; ++s) fetch(s);
   int st_a = 0, st_b = sh.stages - 1;     // ring stages of row i and of row i - 1 (then refilled)
-  for (long long i = 0; i <= n_steps; ++i) {
+  long long at = first * a.D - row_step;  // first channel of row i - 1
+  for (long long i = 0; i <= n_steps; ++i, at += row_step) {
     if (i < n) {
-      const float4 st = a.stats ? __ldg(a.stats + first + i * step) : make_float4(0.f, 0.f, 0.f, 0.f);
-      if (a.post_has) {
+      const float4 st = (FULL || a.stats) ? __ldg(a.stats + first + i * step) : make_float4(0.f, 0.f, 0.f, 0.f);
+      if (has_post) {
         ip[0] = st.y;
         mp[0] = st.x;
       }
@@ -734,77 +749,78 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
         mr[0] = st.z;
       }
       cp_async_wait(sh.stages - 2);
-      float s[NS];
+      f2 s2[NS];
 #pragma unroll
-      for (int k = 0; k < NS; ++k) s[k] = 0.f;
+      for (int k = 0; k < NS; ++k) s2[k] = zero;
+      const f2 ir2 = both(ir[0]), ip2 = both(ip[0]), nmr = both(-mr[0]), nmp = both(-mp[0]);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (!act[j]) continue;
-        float q[8], w[8], y[8], du[8], r[8], dr[8];
+        f2 q[4], w[4], y[4], du[4], r[4], dr[4];
         weights(j, q, w);
-        piece8(st_a, j, 0, has_y, y);
-        piece8(st_a, j, 1, has_pre, du);
-        resid8(st_a, j, 2, has_pre, r);
-        resid8(st_a, j, 2 + RP, has_dr, dr);
+        read(st_a, j, 0, has_y, false, y);
+        read(st_a, j, 1, has_pre, false, du);
+        read(st_a, j, 2, has_pre, true, r);
+        read(st_a, j, 2 + RP, has_dr, true, dr);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float av = du[k] * w[k], z = fmaf(ir[0], av, dr[k]);
+        for (int k = 0; k < 4; ++k) {
+          const f2 av = mul2(du[k], w[k]), z = fma2(ir2, av, dr[k]);
           if (LAYER) {
-            const float hp = (y[k] - mp[0]) * ip[0], hr = (r[k] - mr[0]) * ir[0], qh = q[k] * hp;
-            s[0] = fmaf(av, hr, s[0]);
-            s[1] = fmaf(z, qh, s[1]);
-            s[2] = fmaf(qh, hr, s[2]);
-            s[3] += av;
-            s[4] = fmaf(q[k], z, s[4]);
-            s[5] = fmaf(q[k], hr, s[5]);
-            s[6] += q[k];
-            s[7] += qh;
+            const f2 hp = mul2(add2(y[k], nmp), ip2), hr = mul2(add2(r[k], nmr), ir2), qh = mul2(q[k], hp);
+            s2[0] = fma2(av, hr, s2[0]);
+            s2[1] = fma2(z, qh, s2[1]);
+            s2[2] = fma2(qh, hr, s2[2]);
+            s2[3] = add2(s2[3], av);
+            s2[4] = fma2(q[k], z, s2[4]);
+            s2[5] = fma2(q[k], hr, s2[5]);
+            s2[6] = add2(s2[6], q[k]);
+            s2[7] = add2(s2[7], qh);
           } else {   // without the factors ip and ir, which are the row's
-            const float qy = q[k] * y[k];
-            s[0] = fmaf(av, r[k], s[0]);
-            s[1] = fmaf(z, qy, s[1]);
-            s[2] = fmaf(qy, r[k], s[2]);
+            const f2 qy = mul2(q[k], y[k]);
+            s2[0] = fma2(av, r[k], s2[0]);
+            s2[1] = fma2(z, qy, s2[1]);
+            s2[2] = fma2(qy, r[k], s2[2]);
           }
         }
       }
+      float s[NS];
+#pragma unroll
+      for (int k = 0; k < NS; ++k) s[k] = sum2(s2[k]);
       int idx;
       const float mine = warp_sum_scattered<NS>(s, tm.lane, idx);
       tm.publish(mine, idx, (tm.lane & (32 / NS - 1)) == 0);
     }
     if (i > 0 && i <= n) {
-      const long long row = first + (i - 1) * step;
-      const float k1 = ir[1] * c1, k2 = ir[1] * c2, g2 = ip[1] * m2, g1 = ip[1] * m1;
+      const f2 ir2 = both(ir[1]), ip2 = both(ip[1]), nmr = both(-mr[1]), nmp = both(-mp[1]);
+      const f2 k1 = both(-ir[1] * c1), k2 = both(-ir[1] * c2), g2 = both(-ip[1] * m2), g1 = both(-ip[1] * m1);
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         if (!act[j]) continue;
-        float q[8], w[8], y[8], du[8], r[8], dr[8];
+        f2 q[4], w[4], y[4], du[4], r[4], dr[4], dy[4];
         weights(j, q, w);
-        piece8(st_b, j, 0, has_y, y);
-        piece8(st_b, j, 1, has_pre, du);
-        resid8(st_b, j, 2, has_pre, r);
-        resid8(st_b, j, 2 + RP, has_dr, dr);
-        float dy[8];
+        read(st_b, j, 0, has_y, false, y);
+        read(st_b, j, 1, has_pre, false, du);
+        read(st_b, j, 2, has_pre, true, r);
+        read(st_b, j, 2 + RP, has_dr, true, dr);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float hp = (LAYER ? y[k] - mp[1] : y[k]) * ip[1], hr = (LAYER ? r[k] - mr[1] : r[k]) * ir[1];
-          float t = fmaf(ir[1], du[k] * w[k], dr[k]);
-          if (LAYER) t -= k1;
-          t = fmaf(-hr, k2, t);
-          sumA[j][k] = fmaf(t, hp, sumA[j][k]);
-          sumC[j][k] = fmaf(du[k], hr, sumC[j][k]);
+        for (int k = 0; k < 4; ++k) {
+          const f2 hp = mul2(LAYER ? add2(y[k], nmp) : y[k], ip2), hr = mul2(LAYER ? add2(r[k], nmr) : r[k], ir2);
+          f2 t = fma2(ir2, mul2(du[k], w[k]), LAYER ? add2(dr[k], k1) : dr[k]);
+          t = fma2(hr, k2, t);
+          sumA[j][k] = fma2(t, hp, sumA[j][k]);
+          sumC[j][k] = fma2(du[k], hr, sumC[j][k]);
           if (LAYER) {
-            sumB[j][k] += t;
-            sumE[j][k] += du[k];
+            sumB[j][k] = add2(sumB[j][k], t);
+            sumE[j][k] = add2(sumE[j][k], du[k]);
           }
-          dr[k] = a.alpha * t;
-          dy[k] = fmaf(-hp, g2, LAYER ? fmaf(q[k] * t, ip[1], -g1) : (q[k] * t) * ip[1]);
+          dr[k] = mul2(alpha, t);
+          dy[k] = fma2(hp, g2, LAYER ? fma2(mul2(q[k], t), ip2, g1) : mul2(mul2(q[k], t), ip2));
         }
-        const long long at = row * a.D + col[j];
-        if (a.dx) store8(static_cast<RT *>(a.dx) + at, dr);
-        if (a.dy) store8(a.dy + at, dy);
+        if (FULL || a.dx) store4(static_cast<RT *>(a.dx) + at + col[j], dr);
+        if (FULL || a.dy) store4(a.dy + at + col[j], dy);
       }
     }
-    fetch(i - 1 + sh.stages, st_b);     // row i - 1 has been read for the last time
+    fetch(st_b);     // row i - 1 has been read for the last time
     st_b = st_a;
     if (++st_a == sh.stages) st_a = 0;
     if (i == n_steps) break;
@@ -831,7 +847,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
       c2 = s[0] * ir[1] * inv_d;
       m2 = ip[1] * (s[1] - ir[1] * ir[1] * c2 * s[2]) * inv_d;
     }
-    if (!a.post_has) m2 = 0.f;
+    if (!has_post) m2 = 0.f;
   }
   cp_async_wait(0);
 
@@ -846,8 +862,9 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float *p = q == 0 ? &sumA[j][4 * h] : q == 1 ? &sumC[j][4 * h] : q == 2 ? &sumB[LAYER ? j : 0][4 * h] : &sumE[LAYER ? j : 0][4 * h];
-        mine[(j * 2 + h) * TL + tl] = make_float4(p[0], p[1], p[2], p[3]);
+        const f2 *p = q == 0 ? &sumA[j][2 * h] : q == 1 ? &sumC[j][2 * h] : q == 2 ? &sumB[LAYER ? j : 0][2 * h] : &sumE[LAYER ? j : 0][2 * h];
+        const float2 lo = split2(p[0]), hi = split2(p[1]);
+        mine[(j * 2 + h) * TL + tl] = make_float4(lo.x, lo.y, hi.x, hi.y);
       }
     __syncthreads();
     if (tm.team == 0) {
@@ -967,8 +984,10 @@ int launch_rows(const Args &a, int pieces, int red_bytes, int w_bytes_per_thread
 // The smallest cluster that the rows fit.
 template <typename RT, bool LAYER, int CL = 1>
 int launch_fwd_rows(const FwdArgs &a, int sms, cudaStream_t stream) {
-  const int rc = launch_rows<CL, block_norm_fwd_rows_kernel<RT, LAYER, CL>>(a, 1 + (int)sizeof(RT) / 2, Team<CL, LAYER ? 4 : 2>::RED_FLOATS * 4, 0,
-                                                                            sms, nullptr, stream);
+  const int pieces = 1 + (int)sizeof(RT) / 2, red = (Team<CL, LAYER ? 4 : 2>::RED_FLOATS + CL * 16) * 4;
+  const bool full = a.y && a.r && a.post.has && a.pre.has;
+  const int rc = full ? launch_rows<CL, block_norm_fwd_rows_kernel<RT, LAYER, CL, true>>(a, pieces, red, 0, sms, nullptr, stream)
+                      : launch_rows<CL, block_norm_fwd_rows_kernel<RT, LAYER, CL, false>>(a, pieces, red, 0, sms, nullptr, stream);
   if constexpr (CL < 2) {
     if (rc == OSDP_ERR_UNSUPPORTED) return launch_fwd_rows<RT, LAYER, 2 * CL>(a, sms, stream);
   }
@@ -976,8 +995,10 @@ int launch_fwd_rows(const FwdArgs &a, int sms, cudaStream_t stream) {
 }
 template <typename RT, bool LAYER, int CL = 1>
 int launch_bwd(const BwdArgs &a, int sms, int *units, cudaStream_t stream) {
-  const int rc = launch_rows<CL, block_norm_bwd_kernel<RT, LAYER, CL>>(a, 2 + (int)sizeof(RT), Team<CL, LAYER ? 8 : 4>::RED_FLOATS * 4,
-                                                                       LAYER ? 128 : 0, sms, units, stream);
+  const int pieces = 2 + (int)sizeof(RT), red = Team<CL, LAYER ? 8 : 4>::RED_FLOATS * 4, w = LAYER ? 128 : 0;
+  const bool full = a.y && a.dr && a.post_has && a.pre_has && a.dx && a.dy;
+  const int rc = full ? launch_rows<CL, block_norm_bwd_kernel<RT, LAYER, CL, true>>(a, pieces, red, w, sms, units, stream)
+                      : launch_rows<CL, block_norm_bwd_kernel<RT, LAYER, CL, false>>(a, pieces, red, w, sms, units, stream);
   if constexpr (CL < 4) {
     if (rc == OSDP_ERR_UNSUPPORTED) return launch_bwd<RT, LAYER, 2 * CL>(a, sms, units, stream);
   }

@@ -49,6 +49,79 @@ __device__ __forceinline__ uint4 narrow8(const float (&f)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Two fp32 values side by side: sm_100 multiplies and adds such pairs in one instruction, which is what lets the
+// element-wise kernels keep up with the memory.
+struct f2 {
+  unsigned long long v;
+};
+__device__ __forceinline__ f2 pack2(float a, float b) {
+  f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 split2(f2 a) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+  return r;
+}
+__device__ __forceinline__ f2 both(float a) { return pack2(a, a); }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) {
+  f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b) {
+  f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
+  f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ float sum2(f2 a) {
+  const float2 s = split2(a);
+  return s.x + s.y;
+}
+__device__ __forceinline__ void widen4(const uint4 &u, f2 (&f)[4]) {
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) f[j] = pack2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u));
+}
+__device__ __forceinline__ uint4 narrow4(const f2 (&f)[4]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 v = split2(f[j]);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
+    w[j] = *reinterpret_cast<const uint32_t *>(&h);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Eight fp32 values from two 16-byte pieces, and back to memory as T.
+__device__ __forceinline__ void join4(const float4 &lo, const float4 &hi, f2 (&f)[4]) {
+  f[0] = pack2(lo.x, lo.y);
+  f[1] = pack2(lo.z, lo.w);
+  f[2] = pack2(hi.x, hi.y);
+  f[3] = pack2(hi.z, hi.w);
+}
+template <typename T>
+__device__ __forceinline__ void store4(T *p, const f2 (&f)[4]) {
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4 *>(p) = narrow4(f);
+  } else {
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 v = split2(f[j]);
+      w[2 * j] = __float_as_uint(v.x);
+      w[2 * j + 1] = __float_as_uint(v.y);
+    }
+    store32(p, w);
+  }
+}
+
 // Eight consecutive elements of type T (__nv_bfloat16: 16-byte aligned, float: 32-byte aligned) <-> fp32.
 template <typename T>
 __device__ __forceinline__ void load8(const T *p, float (&f)[8]) {
