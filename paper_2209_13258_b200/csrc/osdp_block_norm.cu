@@ -243,7 +243,10 @@ __global__ void __launch_bounds__(V == 4 ? 512 : 1024) block_norm_fwd_kernel(con
 // of one row and the first part of the next, whose sums over the row are then exchanged with ONE barrier, so that its
 // latency and that of the shuffles is met with independent work.
 
-constexpr int ROW_THREADS = 512;
+// Threads of a block: what the registers allow without spills (spilled values come back from L2, there is hardly any L1
+// beside the ring: the layer norm's backward took 1.5 times as long with 512 threads of 128 registers).
+constexpr int FWD_WARPS = 16;
+constexpr int bwd_warps(bool layer) { return layer ? 12 : 16; }
 constexpr int MAX_STAGES = 6;
 constexpr int ROW_MAX_BLOCKS = 160;   // partial sums over rows that the workspace holds
 
@@ -347,12 +350,32 @@ struct Team {
       __syncwarp();
     }
   }
-  // f(partial sums of one warp, block, warp of the team) for every warp that shares the row
-  template <typename F>
-  __device__ __forceinline__ void each(const float *buf, F f) const {
+  // The exchanged sums, added over the warps that share the row: lane l takes the warps l, l + 32, ... (block by block;
+  // `add` is given their sums and their number in count order) and the lanes' totals are added by shuffles.  A loop
+  // over the warps in every lane instead is a chain of up to 16 CL shared-memory reads per row.
+  template <int N, typename F>
+  __device__ __forceinline__ void total(const float *buf, float (&t)[N], F add) const {
 #pragma unroll
-    for (int b = 0; b < CL; ++b)
-      for (int w = 0; w < warps; ++w) f(buf + (b * 16 + first_warp + w) * NS, b, w);
+    for (int k = 0; k < N; ++k) t[k] = 0.f;
+#pragma unroll
+    for (int p = 0; p < (CL + 1) / 2; ++p) {
+      const int slot = lane + 32 * p, b = slot >> 4, w = slot & 15;
+      if (b < CL && w < warps) add(t, buf + (b * 16 + first_warp + w) * NS, b * 16 + w);
+    }
+    if (warps == 1 && CL == 1) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) t[k] = __shfl_sync(0xFFFFFFFFu, t[k], 0);
+      return;
+    }
+    int idx;
+    const float s = warp_sum_scattered<N>(t, lane, idx);
+#pragma unroll
+    for (int k = 0; k < N; ++k) t[k] = __shfl_sync(0xFFFFFFFFu, s, lane_of<N>(k));
+  }
+  // a lane that warp_sum_scattered<N> leaves with sum k
+  template <int N>
+  static __device__ __forceinline__ constexpr int lane_of(int k) {
+    return N == 2 ? (k & 1) * 16 : N == 4 ? (k >> 1) * 16 + (k & 1) * 8 : (k >> 2) * 16 + ((k >> 1) & 1) * 8 + (k & 1) * 4;
   }
 };
 
@@ -364,7 +387,7 @@ struct Team {
 // LAYER: either norm subtracts a mean.  FULL: y, both norms, r and u are there (the form between two blocks); without
 // it each may be absent, which costs branches.
 template <typename RT, bool LAYER, int CL, bool FULL>
-__global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_fwd_rows_kernel(const __grid_constant__ FwdArgs a, const TeamShape sh) {
+__global__ void __launch_bounds__(32 * FWD_WARPS, 1) block_norm_fwd_rows_kernel(const __grid_constant__ FwdArgs a, const TeamShape sh) {
   constexpr int RP = sizeof(RT) / 2;             // 16-byte pieces of a residual vector
   constexpr int PIECES = 1 + RP;                 // y, x
   constexpr int NS = LAYER ? 4 : 2;              // y's, r's: mean and squared distances, or squares alone
@@ -372,10 +395,12 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_fwd_rows_kernel(con
   Team<CL, NS> tm;
   tm.init(sh, a.D, reinterpret_cast<float *>(smem));
   float *count = reinterpret_cast<float *>(smem) + Team<CL, NS>::RED_FLOATS;   // channels of each warp of a team, by block
-  uint8_t *ring = reinterpret_cast<uint8_t *>(count + CL * 16);
+  float4 *bias = reinterpret_cast<float4 *>(count + CL * 16);                  // layer: [warp of a team][qb, bp][4][lane]
+  // ring: [warp][stage][vector][piece][lane] of 16 bytes, so that a lane's pieces are at constant distances
+  constexpr int STAGE = 2 * PIECES * 512;
+  uint8_t *ring = reinterpret_cast<uint8_t *>(bias + (LAYER ? 8 * 32 * sh.warps : 0)) + tm.warp * (STAGE * sh.stages) + tm.lane * 16;
   const uint32_t ring_u32 = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
-  const int nthreads = blockDim.x;
-  const int stage_bytes = 2 * PIECES * nthreads * 16;
+  const float4 *my_bias = bias + (tm.warp - tm.first_warp) * (8 * 32) + tm.lane;
   if (LAYER && threadIdx.x < CL * 16) count[threadIdx.x] = tm.channels(threadIdx.x / 16, threadIdx.x % 16, a.D);
   pdl_launch_dependents();
   pdl_wait();
@@ -383,7 +408,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_fwd_rows_kernel(con
   const bool has_y = FULL || a.y != nullptr, post = FULL || (has_y && a.post.has), pre = FULL || a.pre.has, has_r = FULL || a.r != nullptr;
   int col[2];
   bool act[2];
-  f2 qw[2][4], wp[2][4], qb[LAYER ? 2 : 1][4], bp[LAYER ? 2 : 1][4];   // r = alpha x + qw h + qb, u = wp h + bp
+  f2 qw[2][4], wp[2][4];   // r = alpha x + qw h + qb, u = wp h + bp
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     col[j] = tm.c_begin + (j * tm.TL + tm.tl) * 8;
@@ -410,9 +435,13 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_fwd_rows_kernel(con
     for (int k = 0; k < 4; ++k) {
       qw[j][k] = pack2(q[2 * k], q[2 * k + 1]);
       wp[j][k] = pack2(w[2 * k], w[2 * k + 1]);
-      if (LAYER) {
-        qb[j][k] = pack2(b[2 * k], b[2 * k + 1]);
-        bp[j][k] = pack2(c[2 * k], c[2 * k + 1]);
+    }
+    if (LAYER && tm.team == 0) {   // too many for the registers
+      float4 *to = bias + tm.warp * (8 * 32) + tm.lane;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        to[(j * 2 + h) * 32] = make_float4(b[4 * h], b[4 * h + 1], b[4 * h + 2], b[4 * h + 3]);
+        to[(4 + j * 2 + h) * 32] = make_float4(c[4 * h], c[4 * h + 1], c[4 * h + 2], c[4 * h + 3]);
       }
     }
   }
@@ -423,7 +452,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_fwd_rows_kernel(con
   const long long n = first < a.M ? (a.M - first + step - 1) / step : 0;
   // the teams of a cluster meet at its barrier: all do as many steps as its first team, which has the most rows
   const long long n_steps = CL == 1 ? n : (a.M - (first - tm.team) + step - 1) / step;
-  auto slot = [&](int stage, int j, int piece) { return stage * stage_bytes + ((j * PIECES + piece) * nthreads + (int)threadIdx.x) * 16; };
+  auto slot = [](int stage, int j, int piece) { return stage * STAGE + (j * PIECES + piece) * 512; };
   const long long row_step = step * a.D;
   long long f_at = first * a.D;                  // first channel of the row that is fetched next
   long long f_row = 0;
@@ -465,11 +494,12 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_fwd_rows_kernel(con
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           if (!act[j]) continue;
-          f2 u[4];
+          f2 u[4], bp[4];
+          if (LAYER) join4(my_bias[(4 + j * 2) * 32], my_bias[(5 + j * 2) * 32], bp);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const f2 h = mul2(LAYER ? add2(r[j][k], shift) : r[j][k], scale);
-            u[k] = LAYER ? fma2(h, wp[j][k], bp[j][k]) : mul2(h, wp[j][k]);
+            u[k] = LAYER ? fma2(h, wp[j][k], bp[k]) : mul2(h, wp[j][k]);
           }
           store4(static_cast<__nv_bfloat16 *>(a.u) + at + col[j], u);
         }
@@ -492,12 +522,13 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_fwd_rows_kernel(con
         else
           join4(*reinterpret_cast<const float4 *>(ring + slot(st_b, j, 1)), *reinterpret_cast<const float4 *>(ring + slot(st_b, j, PIECES - 1)), x);
         if (has_y) {
-          f2 y[4];
+          f2 y[4], qb[4];
           widen4(*reinterpret_cast<const uint4 *>(ring + slot(st_b, j, 0)), y);
+          if (LAYER) join4(my_bias[(j * 2) * 32], my_bias[(1 + j * 2) * 32], qb);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const f2 h = mul2(LAYER ? add2(y[k], shift) : y[k], scale);
-            const f2 base = LAYER ? fma2(alpha, x[k], qb[j][k]) : mul2(alpha, x[k]);
+            const f2 base = LAYER ? fma2(alpha, x[k], qb[k]) : mul2(alpha, x[k]);
             r[j][k] = fma2(qw[j][k], h, base);
           }
         } else {
@@ -558,27 +589,27 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_fwd_rows_kernel(con
     const float *buf = tm.buffer();
     tm.turn ^= 1;
     tm.barrier();
-    float vy = 0.f, vr = 0.f;
+    float v[2];
     if (LAYER) {
-      float sy = 0.f, sr = 0.f;
-      tm.each(buf, [&](const float *f, int b, int w) {
-        const float c = count[b * 16 + w];
-        sy = fmaf(c, f[0], sy);
-        sr = fmaf(c, f[2], sr);
+      float m[2];
+      tm.template total<2>(buf, m, [&](float (&t)[2], const float *f, int w) {
+        t[0] = fmaf(count[w], f[0], t[0]);
+        t[1] = fmaf(count[w], f[2], t[1]);
       });
-      mean_y = sy * inv_d;
-      mean_r = sr * inv_d;
-      tm.each(buf, [&](const float *f, int b, int w) {
-        const float c = count[b * 16 + w], dy = f[0] - mean_y, dr = f[2] - mean_r;
-        vy += fmaf(c * dy, dy, f[1]);
-        vr += fmaf(c * dr, dr, f[3]);
+      mean_y = m[0] * inv_d;
+      mean_r = m[1] * inv_d;
+      tm.template total<2>(buf, v, [&](float (&t)[2], const float *f, int w) {
+        const float dy = f[0] - mean_y, dr = f[2] - mean_r;
+        t[0] += fmaf(count[w] * dy, dy, f[1]);
+        t[1] += fmaf(count[w] * dr, dr, f[3]);
       });
     } else {
-      tm.each(buf, [&](const float *f, int, int) {
-        vy += f[0];
-        vr += f[1];
+      tm.template total<2>(buf, v, [&](float (&t)[2], const float *f, int) {
+        t[0] += f[0];
+        t[1] += f[1];
       });
     }
+    const float vy = v[0], vr = v[1];
     rstd_y = post ? rsqrtf(fmaf(vy, inv_d, a.post.eps)) : 1.f;
     rstd_r = rsqrtf(fmaf(vr, inv_d, a.pre.eps));
   }
@@ -610,7 +641,7 @@ struct BwdArgs {
 // LAYER: either norm subtracts a mean (more sums; the weights are then in shared memory, there are too few registers).
 // FULL: every input, both norms, dx and dy are there.
 template <typename RT, bool LAYER, int CL, bool FULL>
-__global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __grid_constant__ BwdArgs a, const TeamShape sh) {
+__global__ void __launch_bounds__(32 * bwd_warps(LAYER), 1) block_norm_bwd_kernel(const __grid_constant__ BwdArgs a, const TeamShape sh) {
   constexpr bool WREG = !LAYER;
   constexpr int NS = LAYER ? 8 : 4;                 // sums per row
   constexpr int RP = sizeof(RT) / 2;                // 16-byte pieces of a residual vector
@@ -619,11 +650,12 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
   Team<CL, NS> tm;
   tm.init(sh, a.D, reinterpret_cast<float *>(smem));
   const int tl = tm.tl, TL = tm.TL;
-  float4 *wsm = reinterpret_cast<float4 *>(smem + Team<CL, NS>::RED_FLOATS * 4);   // [q, w_pre][2 vectors][2 halves][TL]
-  uint8_t *ring = reinterpret_cast<uint8_t *>(wsm) + (WREG ? 0 : 8 * TL * 16);
+  float4 *wsm = reinterpret_cast<float4 *>(smem + Team<CL, NS>::RED_FLOATS * 4);   // layer: [warp of a team][q, w_pre][4][lane]
+  // ring: [warp][stage][vector][piece][lane] of 16 bytes, so that a lane's pieces are at constant distances
+  constexpr int STAGE = 2 * PIECES * 512;
+  uint8_t *ring0 = reinterpret_cast<uint8_t *>(wsm + (WREG ? 0 : 8 * TL)), *ring = ring0 + tm.warp * (STAGE * sh.stages) + tm.lane * 16;
   const uint32_t ring_u32 = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
-  const int nthreads = blockDim.x;
-  const int stage_bytes = 2 * PIECES * nthreads * 16;
+  const float4 *my_w = wsm + (tm.warp - tm.first_warp) * (8 * 32) + tm.lane;
 
   pdl_launch_dependents();
   pdl_wait();
@@ -655,10 +687,11 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
         wreg[j][k] = pack2(w[2 * k], w[2 * k + 1]);
       }
     } else if (tm.team == 0) {
+      float4 *to = wsm + tm.warp * (8 * 32) + tm.lane;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        wsm[(0 + j * 2 + h) * TL + tl] = make_float4(q[4 * h], q[4 * h + 1], q[4 * h + 2], q[4 * h + 3]);
-        wsm[(4 + j * 2 + h) * TL + tl] = make_float4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]);
+        to[(j * 2 + h) * 32] = make_float4(q[4 * h], q[4 * h + 1], q[4 * h + 2], q[4 * h + 3]);
+        to[(4 + j * 2 + h) * 32] = make_float4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]);
       }
     }
   }
@@ -672,8 +705,8 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
         w[k] = wreg[j][k];
       }
     } else {
-      join4(wsm[(0 + j * 2) * TL + tl], wsm[(1 + j * 2) * TL + tl], q);
-      join4(wsm[(4 + j * 2) * TL + tl], wsm[(5 + j * 2) * TL + tl], w);
+      join4(my_w[(j * 2) * 32], my_w[(1 + j * 2) * 32], q);
+      join4(my_w[(4 + j * 2) * 32], my_w[(5 + j * 2) * 32], w);
     }
   };
 
@@ -681,7 +714,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
   const long long n = first < a.M ? (a.M - first + step - 1) / step : 0;
   // the teams of a cluster meet at its barrier: all do as many steps as its first team, which has the most rows
   const long long n_steps = CL == 1 ? n : (a.M - (first - tm.team) + step - 1) / step;
-  auto slot = [&](int stage, int j, int piece) { return stage * stage_bytes + ((j * PIECES + piece) * nthreads + (int)threadIdx.x) * 16; };
+  auto slot = [](int stage, int j, int piece) { return stage * STAGE + (j * PIECES + piece) * 512; };
   const long long row_step = step * a.D;
   long long f_at = first * a.D, f_row = 0;       // first channel and number of the row that is fetched next
   auto fetch = [&](int stage) {
@@ -828,13 +861,11 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
     tm.turn ^= 1;
     tm.barrier();
     float s[NS];
-#pragma unroll
-    for (int k = 0; k < NS; ++k) s[k] = 0.f;
-    tm.each(buf, [&](const float *f, int, int) {
+    tm.template total<NS>(buf, s, [&](float (&t)[NS], const float *f, int) {
 #pragma unroll
       for (int k4 = 0; k4 < NS / 4; ++k4) {
         const float4 v = *reinterpret_cast<const float4 *>(f + 4 * k4);
-        s[4 * k4] += v.x; s[4 * k4 + 1] += v.y; s[4 * k4 + 2] += v.z; s[4 * k4 + 3] += v.w;
+        t[4 * k4] += v.x; t[4 * k4 + 1] += v.y; t[4 * k4 + 2] += v.z; t[4 * k4 + 3] += v.w;
       }
     });
     ip[1] = ip[0]; mp[1] = mp[0]; ir[1] = ir[0]; mr[1] = mr[0];
@@ -853,7 +884,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 1) block_norm_bwd_kernel(const __
 
   // Channel sums of the block: teams added in ascending order.
   __syncthreads();
-  float4 *acc = reinterpret_cast<float4 *>(ring);   // [team][vector][half][TL], one sum at a time
+  float4 *acc = reinterpret_cast<float4 *>(ring0);   // [team][vector][half][TL], one sum at a time
   constexpr int NACC = LAYER ? 4 : 2;
 #pragma unroll
   for (int q = 0; q < NACC; ++q) {
@@ -947,13 +978,13 @@ int launch_fwd(const FwdArgs &args, int warps, cudaStream_t stream) {
 // the ring, `red_bytes` and `w_bytes_per_thread`: what else it keeps in shared memory.  As many teams to a block as leave
 // room for three rows each (one being finished, one begun, one on its way); OSDP_ERR_UNSUPPORTED if not even one does.
 template <int CL, auto KERNEL, typename Args>
-int launch_rows(const Args &a, int pieces, int red_bytes, int w_bytes_per_thread, int sms, int *units, cudaStream_t stream) {
+int launch_rows(const Args &a, int max_warps, int pieces, int red_bytes, int w_bytes_per_thread, int sms, int *units, cudaStream_t stream) {
   TeamShape sh;
   sh.warps = (int)cdiv(block_channels(a.D, CL), 512);
-  if (sh.warps > 16) return OSDP_ERR_UNSUPPORTED;
+  if (sh.warps > max_warps) return OSDP_ERR_UNSUPPORTED;
   const int fixed = red_bytes + w_bytes_per_thread * sh.warps * 32;
   int stage = 0;
-  for (sh.teams = 16 / sh.warps; sh.teams > 0; --sh.teams) {
+  for (sh.teams = max_warps / sh.warps; sh.teams > 0; --sh.teams) {
     stage = 2 * pieces * sh.teams * sh.warps * 32 * 16;
     sh.stages = (SMEM_MAX - fixed) / stage;
     if (sh.stages >= 3) break;
@@ -984,10 +1015,10 @@ int launch_rows(const Args &a, int pieces, int red_bytes, int w_bytes_per_thread
 // The smallest cluster that the rows fit.
 template <typename RT, bool LAYER, int CL = 1>
 int launch_fwd_rows(const FwdArgs &a, int sms, cudaStream_t stream) {
-  const int pieces = 1 + (int)sizeof(RT) / 2, red = (Team<CL, LAYER ? 4 : 2>::RED_FLOATS + CL * 16) * 4;
+  const int pieces = 1 + (int)sizeof(RT) / 2, red = (Team<CL, LAYER ? 4 : 2>::RED_FLOATS + CL * 16) * 4, w = LAYER ? 128 : 0;
   const bool full = a.y && a.r && a.post.has && a.pre.has;
-  const int rc = full ? launch_rows<CL, block_norm_fwd_rows_kernel<RT, LAYER, CL, true>>(a, pieces, red, 0, sms, nullptr, stream)
-                      : launch_rows<CL, block_norm_fwd_rows_kernel<RT, LAYER, CL, false>>(a, pieces, red, 0, sms, nullptr, stream);
+  const int rc = full ? launch_rows<CL, block_norm_fwd_rows_kernel<RT, LAYER, CL, true>>(a, FWD_WARPS, pieces, red, w, sms, nullptr, stream)
+                      : launch_rows<CL, block_norm_fwd_rows_kernel<RT, LAYER, CL, false>>(a, FWD_WARPS, pieces, red, w, sms, nullptr, stream);
   if constexpr (CL < 2) {
     if (rc == OSDP_ERR_UNSUPPORTED) return launch_fwd_rows<RT, LAYER, 2 * CL>(a, sms, stream);
   }
@@ -997,8 +1028,8 @@ template <typename RT, bool LAYER, int CL = 1>
 int launch_bwd(const BwdArgs &a, int sms, int *units, cudaStream_t stream) {
   const int pieces = 2 + (int)sizeof(RT), red = Team<CL, LAYER ? 8 : 4>::RED_FLOATS * 4, w = LAYER ? 128 : 0;
   const bool full = a.y && a.dr && a.post_has && a.pre_has && a.dx && a.dy;
-  const int rc = full ? launch_rows<CL, block_norm_bwd_kernel<RT, LAYER, CL, true>>(a, pieces, red, w, sms, units, stream)
-                      : launch_rows<CL, block_norm_bwd_kernel<RT, LAYER, CL, false>>(a, pieces, red, w, sms, units, stream);
+  const int rc = full ? launch_rows<CL, block_norm_bwd_kernel<RT, LAYER, CL, true>>(a, bwd_warps(LAYER), pieces, red, w, sms, units, stream)
+                      : launch_rows<CL, block_norm_bwd_kernel<RT, LAYER, CL, false>>(a, bwd_warps(LAYER), pieces, red, w, sms, units, stream);
   if constexpr (CL < 4) {
     if (rc == OSDP_ERR_UNSUPPORTED) return launch_bwd<RT, LAYER, 2 * CL>(a, sms, units, stream);
   }
