@@ -367,8 +367,8 @@ int osdp_split_mlp_bwd(const void *dy, const void *x, const void *w_flat, int64_
  *   has scale 0 and zeros; a row with an infinity or a NaN has a scale that is not finite (the products come out NaN).
  *   stats [M,4] fp32 or NULL: mean and 1 / sqrt(...) of N_post, then of N_pre (mean 0 for RMS; 0, 0 for an absent norm):
  *   what the backward needs.
- * D is a multiple of 8 and at most OSDP_BLOCK_NORM_MAX_D; M may be 0 (nothing is launched).  bf16 matrices are 16-byte
- * aligned, fp32 matrices and vectors 32-byte, int8 u 8-byte.  alpha, beta, eps_* finite, eps_* >= 0. */
+ * D is a multiple of 8 and at most OSDP_BLOCK_NORM_MAX_D; M may be 0 (nothing is launched).  bf16 matrices, stats and vectors
+ * are 16-byte aligned, fp32 matrices 32-byte, int8 u 8-byte.  alpha, beta, eps_* finite, eps_* >= 0. */
 #define OSDP_BLOCK_NORM_MAX_D 16384
 int osdp_block_norm_fwd(const void *x, const void *y, int64_t M, int64_t D, int resid_dtype, int post, const float *w_post,
                         const float *b_post, double eps_post, const float *gate, double alpha, double beta, int pre,
@@ -442,12 +442,14 @@ int osdp_adamw_step(const osdp_adamw_tensor *tensors, int n_tensors, int param_d
  * aligned; M may be 0. */
 int osdp_quantize_rows_i8(const void *x, int64_t M, int64_t K, void *q, float *scale, void *stream);
 
-/* x8 [M,K] and w8_flat (W [N,K] at element = byte offset w_offset) int8; x_scale [M], w_scale [N], bias [N] (or NULL) fp32;
- * out [M,N] bf16.  K and w_offset multiples of 16, N of 8 (16 if the slices cut N), a slice length of K a multiple of 16;
- * K < 131072; M may be 0.  x8, w8_flat, out, w_scale and bias 16-byte aligned.  Every slice of the operator in one
- * call, no flags; workspace osdp_split_linear_workspace_bytes(..., OSDP_OP_LINEAR_FWD, 0).  No gradient: a model is
- * trained in bf16 and served in int8. */
-int osdp_split_linear_fwd_i8(const void *x8, const float *x_scale, const void *w8_flat, int64_t w_offset, const float *w_scale,
+/* x [M,K] and w8_flat (W [N,K] at element = byte offset w_offset) int8; x_scale [M], w_scale [N], bias [N] (or NULL) fp32;
+ * out [M,N] bf16.  x_scale NULL: x is [M,K] bf16 and the call quantises it, as osdp_quantize_rows_i8 does, on the way;
+ * ws then needs osdp_i8_workspace_bytes(M, K) bytes, otherwise 256 (its status word, as for every tile kernel).
+ * K and w_offset multiples of 16, N of 8 (16 if the slices cut N), a slice length of K a multiple of 16; K < 131072; M may
+ * be 0.  x, w8_flat, out, w_scale and bias 16-byte aligned.  Every slice of the operator in one call, no flags.  No
+ * gradient: a model is trained in bf16 and served in int8. */
+int osdp_i8_workspace_bytes(int64_t M, int64_t K, size_t *bytes);
+int osdp_split_linear_fwd_i8(const void *x, const float *x_scale, const void *w8_flat, int64_t w_offset, const float *w_scale,
                              const float *bias, int64_t M, int64_t N, int64_t K, int k_split, int split_dim, int act, void *out,
                              void *ws, size_t ws_bytes, void *stream);
 

@@ -31,7 +31,7 @@ EXPORTS = [
     "osdp_zdp_mlp_fwd_slice", "osdp_zdp_mlp_bwd_slice",
     "osdp_block_norm_fwd", "osdp_block_norm_bwd", "osdp_block_norm_workspace_bytes",
     "osdp_adamw_layout", "osdp_adamw_step", "osdp_grad_norm", "osdp_grad_norm_workspace_bytes",
-    "osdp_quantize_rows_i8", "osdp_split_linear_fwd_i8",
+    "osdp_quantize_rows_i8", "osdp_split_linear_fwd_i8", "osdp_i8_workspace_bytes",
 ]
 
 _lib = None
@@ -116,6 +116,7 @@ def lib():
         L.osdp_grad_norm_workspace_bytes.argtypes = [ci, ctypes.POINTER(sz)]
         L.osdp_grad_norm.argtypes = [vp, ci, ci, f32, vp, vp, sz, vp]
         L.osdp_adamw_step.argtypes = [vp, ci, ci, ci, vp, vp, vp, vp, vp, dbl, dbl, dbl, i64, vp, vp]
+        L.osdp_i8_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
         L.osdp_quantize_rows_i8.argtypes = [vp, i64, i64, vp, vp, vp]
         L.osdp_split_linear_fwd_i8.argtypes = [vp, vp, vp, i64, vp, vp, i64, i64, i64, ci, ci, ci, vp, vp, sz, vp]
         for name in EXPORTS:
@@ -492,10 +493,18 @@ def osdp_quantize_rows_i8(x, M, K, q, scale, stream=None, check=False):
     return _ret(rc, check, "osdp_quantize_rows_i8")
 
 
-def osdp_split_linear_fwd_i8(x8, x_scale, w8_flat, w_offset, w_scale, bias, M, N, K, k_split, split_dim, act, out, ws,
+def osdp_i8_workspace_bytes(M, K):
+    """Returns (status, bytes)."""
+    n = ctypes.c_size_t()
+    rc = lib().osdp_i8_workspace_bytes(int(M), int(K), ctypes.byref(n))
+    return rc, n.value
+
+
+def osdp_split_linear_fwd_i8(x, x_scale, w8_flat, w_offset, w_scale, bias, M, N, K, k_split, split_dim, act, out, ws,
                              stream=None, check=False):
+    """x_scale None: x is bf16 and is quantised by the call."""
     wp, wn = _ws(ws)
-    rc = lib().osdp_split_linear_fwd_i8(_ptr(x8), _ptr(x_scale), _ptr(w8_flat), int(w_offset), _ptr(w_scale), _ptr(bias), int(M),
+    rc = lib().osdp_split_linear_fwd_i8(_ptr(x), _ptr(x_scale), _ptr(w8_flat), int(w_offset), _ptr(w_scale), _ptr(bias), int(M),
                                         int(N), int(K), int(k_split), int(split_dim), int(act), _ptr(out), wp, wn,
                                         _stream(stream))
     return _ret(rc, check, "osdp_split_linear_fwd_i8")

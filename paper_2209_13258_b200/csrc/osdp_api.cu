@@ -478,14 +478,14 @@ int launch_variant(const GemmParams &p, int64_t units, int sms, cudaStream_t str
 template <int BN, bool CTA2>
 int launch_bn(const GemmParams &p, bool a_mn, bool b_mn, bool heavy, int64_t units, int sms, cudaStream_t stream) {
   if (p.bk == 128) {   // fp8 operands: tiles from 128 columns up (an MN-major chunk is 128 wide)
-    if constexpr (BN >= 128) {
-      if (p.epi.row_scale) {   // int8: the forward's operand layout only
-        if (a_mn || b_mn) return OSDP_ERR_UNSUPPORTED;
-        if constexpr (BN <= 256) {
-          if (heavy) return launch_variant<BN, false, false, CTA2, true, 1, true>(p, units, sms, stream);
-        }
-        return launch_variant<BN, false, false, CTA2, false, 1, true>(p, units, sms, stream);
+    if (p.epi.row_scale) {   // int8: the forward's operand layout only
+      if (a_mn || b_mn) return OSDP_ERR_UNSUPPORTED;
+      if constexpr (BN == 128 || BN == 256) {
+        if (heavy) return launch_variant<BN, false, false, CTA2, true, 1, true>(p, units, sms, stream);
       }
+      return launch_variant<BN, false, false, CTA2, false, 1, true>(p, units, sms, stream);
+    }
+    if constexpr (BN >= 128) {
       if (!a_mn && !b_mn) return launch_variant<BN, false, false, CTA2, false, 1>(p, units, sms, stream);
       if (!a_mn && b_mn) return launch_variant<BN, false, true, CTA2, false, 1>(p, units, sms, stream);
       if (a_mn && b_mn) return launch_variant<BN, true, true, CTA2, false, 1>(p, units, sms, stream);
@@ -629,7 +629,7 @@ int launch_gemm(const GemmCall &c, cudaStream_t stream) {
   if (pair || cdiv(c.bn_P, BM) * cdiv(c.bn_Q, 256) >= want) bn = 256;
   else if (cdiv(c.bn_P, BM) * cdiv(c.bn_Q, 128) >= want) bn = 128;
   const int eb = c.fp8 ? 1 : 2;
-  if (c.fp8 && bn < 128) bn = 128;
+  if (c.fp8 && !c.i8 && bn < 128) bn = 128;   // (K-major operands have no 128-wide chunks: int8 may take 64 columns)
   const int tm = pair ? 2 * BM : BM;
   // Widest tile, 256 x 512 per CTA pair: eight MMAs per k-block instead of four for the same barrier traffic of
   // the thread that issues them (which paces the main loop) and 25 % fewer operand bytes per flop, but the
@@ -1246,9 +1246,16 @@ int osdp_split_linear_fwd_f8(const void *x8, const void *w8_flat, int64_t w_offs
                   ws_bytes, stream, 0, 1, scale);
 }
 
-int osdp_split_linear_fwd_i8(const void *x8, const float *x_scale, const void *w8_flat, int64_t w_offset, const float *w_scale,
+int osdp_i8_workspace_bytes(int64_t M, int64_t K, size_t *bytes) {
+  if (!bytes) return OSDP_ERR_NULL_POINTER;
+  if (M < 0 || K <= 0 || M > ((int64_t)1 << 30) || K > OSDP_I8_MAX_K) return OSDP_ERR_BAD_SHAPE;
+  *bytes = 256 + align_up((size_t)M * 4, 256) + (size_t)M * K;
+  return OSDP_OK;
+}
+
+int osdp_split_linear_fwd_i8(const void *x, const float *x_scale, const void *w8_flat, int64_t w_offset, const float *w_scale,
                              const float *bias, int64_t M, int64_t N, int64_t K, int k_split, int split_dim, int act, void *out,
-                             void *ws, size_t ws_bytes, void *stream) {
+                             void *ws, size_t ws_bytes, void *stream_) {
   if (M < 0 || K > OSDP_I8_MAX_K) return OSDP_ERR_BAD_SHAPE;
   int64_t L = 0;
   int rc = check_common(M > 0 ? M : 1, N, K, k_split, split_dim, act, &L);
@@ -1257,21 +1264,33 @@ int osdp_split_linear_fwd_i8(const void *x8, const float *x_scale, const void *w
   if ((K & 15) || w_offset < 0 || (w_offset & 15) || (k_split > 1 && (L & 15)) || (k_split > 1 && split_dim == OSDP_SPLIT_OUT && (N & 15)))
     return OSDP_ERR_ALIGNMENT;
   if (M == 0) return OSDP_OK;
-  if (!x8 || !x_scale || !w8_flat || !w_scale || !out) return OSDP_ERR_NULL_POINTER;
-  if (!aligned16(x8) || !aligned16(w8_flat) || !aligned16(out) || !aligned16(w_scale) || !aligned16(bias) || !aligned_to(x_scale, 4))
+  if (!x || !w8_flat || !w_scale || !out || !ws) return OSDP_ERR_NULL_POINTER;
+  if (!aligned16(x) || !aligned16(w8_flat) || !aligned16(out) || !aligned16(w_scale) || !aligned16(bias) || !aligned_to(x_scale, 4) ||
+      !aligned_to(ws, 256))
     return OSDP_ERR_ALIGNMENT;
-  WsPlan plan;
-  rc = plan_workspace(M, N, K, k_split, split_dim, act, OSDP_OP_LINEAR_FWD, 0, &plan);
-  if (rc) return rc;
-  rc = check_ws(ws, ws_bytes, plan);
-  if (rc) return rc;
+  size_t need = 256;
+  if (!x_scale) {
+    rc = osdp_i8_workspace_bytes(M, K, &need);
+    if (rc) return rc;
+  }
+  if (ws_bytes < need) return OSDP_ERR_WORKSPACE_TOO_SMALL;
+  cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   const void *w = static_cast<const char *>(w8_flat) + w_offset;
-  if (M <= OSDP_I8_FEW_TOKENS)   // exact sums: the slices make no difference to the bits
-    return launch_i8_few_tokens(x8, x_scale, w, w_scale, bias, M, N, K, act, out, static_cast<cudaStream_t>(stream));
+  const bool few = M <= OSDP_I8_FEW_TOKENS;
+  if (!x_scale && !(few && i8_quantises_itself(M, K))) {
+    float *scale = reinterpret_cast<float *>(static_cast<char *>(ws) + 256);
+    void *q = static_cast<char *>(ws) + 256 + align_up((size_t)M * 4, 256);
+    rc = launch_i8_quantize(x, M, K, q, scale, stream);
+    if (rc) return rc;
+    x = q;
+    x_scale = scale;
+  }
+  if (few)   // exact sums: the slices make no difference to the bits
+    return launch_i8_few_tokens(x, x_scale, w, w_scale, bias, M, N, K, act, out, stream);
   GemmCall c;
   memset(&c, 0, sizeof(c));
   c.fp8 = c.i8 = 1;
-  c.a = Operand{x8, K, M, K, false, true};
+  c.a = Operand{x, K, M, K, false, true};
   c.b = Operand{w, K, N, K, false, true};
   c.P = M; c.Q = N; c.R = K;
   c.bn_P = M; c.bn_Q = N;
@@ -1283,7 +1302,7 @@ int osdp_split_linear_fwd_i8(const void *x8, const float *x_scale, const void *w
   c.epi.bias = bias;
   c.epi.act = act;
   c.status = static_cast<int *>(ws);
-  return launch_gemm(c, static_cast<cudaStream_t>(stream));
+  return launch_gemm(c, stream);
 }
 
 int osdp_split_linear_bwd_f8(const void *dy8, const void *x8, const void *w8_flat, int64_t w_offset, float scale_dx,

@@ -12,6 +12,7 @@
 #include "../../include/osdp.h"
 
 #include <cmath>
+#include <type_traits>
 
 #include "osdp_internal.h"
 #include "osdp_vec.cuh"
@@ -62,34 +63,88 @@ struct Hyper {
   float root_scale;    // 1 / sqrt(1 - b2^t)
 };
 
-// 256 elements -> codes and their scale.  ROOT: elements above zero keep at least the smallest code.
+// 256 elements -> codes and their scale.  ROOT: the elements are not negative, those above zero keep at least the
+// smallest code.
 template <bool ROOT>
-__device__ __forceinline__ void quantise_block(const float (&x)[8], uint8_t *codes, float *scale, int lane) {
+__device__ __forceinline__ void quantise_block(const f2 (&x)[4], uint8_t *codes, float *scale, int lane) {
   float top = 0.f;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t a = __float_as_uint(x[j]) & 0x7FFFFFFFu;
-    top = __uint_as_float(max(__float_as_uint(top), a));
+  for (int j = 0; j < 4; ++j) {
+    const float2 v = split2(x[j]);
+    top = max_abs3(top, v.x, v.y);
   }
   top = warp_max_abs(top);
   const bool live = !(top < TINY);
   const float inv = live ? __fdiv_rn(448.0f, top) : 0.0f;
-  float c[8];
+  const f2 inv2 = both(inv);
+  f2 c[4];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    c[j] = __fmul_rn(x[j], inv);
-    if (ROOT && live && x[j] > 0.f) c[j] = fmaxf(c[j], 0.001953125f);   // 2^-9
+  for (int j = 0; j < 4; ++j) {
+    c[j] = mul2(x[j], inv2);
+    if (ROOT) {
+      const float2 v = split2(x[j]);
+      float2 q = split2(c[j]);
+      constexpr float least = 0.001953125f;   // 2^-9, the smallest e4m3 value
+      q.x = (live && v.x > 0.f) ? fmaxf(q.x, least) : q.x;
+      q.y = (live && v.y > 0.f) ? fmaxf(q.y, least) : q.y;
+      c[j] = pack2(q.x, q.y);
+    }
   }
   *reinterpret_cast<uint2 *>(codes + lane * 8) = encode_e4m3x8(c);
-  if (lane == 0) *scale = live ? __fmul_rn(top, 1.0f / 448.0f) : 0.0f;
+  if (lane == 0) *scale = live ? top * (1.0f / 448.0f) : 0.0f;
 }
 
-// Each warp takes blocks of 256 consecutive elements, eight per lane, so that every array is read and written in
-// whole lines and a block's scale is a warp reduction.  HBM-bound: nothing is read twice.
+// What a lane reads of one block of 256 elements, as it lies in memory.
+template <typename T>
+struct Raw8 {
+  uint32_t w[2 * sizeof(T)];
+};
+template <typename T>
+__device__ __forceinline__ void load_raw(const T *p, Raw8<T> &r) {
+  if constexpr (sizeof(T) == 2) {
+    const uint4 v = load16(p);
+    r.w[0] = v.x; r.w[1] = v.y; r.w[2] = v.z; r.w[3] = v.w;
+  } else {
+    load32(p, r.w);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void load_raw_part(const T *p, int n, Raw8<T> &r) {   // the first n < 8 elements, then zeros; any alignment
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t lo = 2 * j < n ? reinterpret_cast<const uint16_t *>(p)[2 * j] : 0u, hi = 2 * j + 1 < n ? reinterpret_cast<const uint16_t *>(p)[2 * j + 1] : 0u;
+      r.w[j] = lo | hi << 16;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.w[j] = j < n ? reinterpret_cast<const uint32_t *>(p)[j] : 0u;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void widen_raw(const Raw8<T> &r, f2 (&f)[4]) {
+  if constexpr (sizeof(T) == 2) {
+    widen4(make_uint4(r.w[0], r.w[1], r.w[2], r.w[3]), f);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f[j] = pack2(__uint_as_float(r.w[2 * j]), __uint_as_float(r.w[2 * j + 1]));
+  }
+}
+
+template <bool E4M3>
+struct RawState {
+  uint32_t m[E4M3 ? 2 : 8], v[E4M3 ? 2 : 8];
+  float fm, fv;
+};
+
+// Each warp takes blocks of 256 consecutive elements, eight per lane, so that every array is read and written in whole
+// lines and a block's scale is a warp reduction.  All loads of BLOCKS blocks are issued before the first is used.
+// HBM-bound: nothing is read twice.
 template <typename T, bool MASTER, bool E4M3, int MAXT>
 __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ Table<MAXT> t, const Hyper h, float *master,
                                                         void *state_m, void *state_v, float *scale_m, float *scale_v,
                                                         const float *__restrict__ clip) {
+  constexpr int WARPS = THREADS / 32, PER_WARP = CHUNK / (WARPS * QB), BLOCKS = E4M3 ? PER_WARP : 1;
   pdl_launch_dependents();
   const Entry &e = t.e[find_entry(t, blockIdx.x)];
   const long long base = (long long)(blockIdx.x - e.first_chunk) * CHUNK;
@@ -102,71 +157,96 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
   }
   T *param = static_cast<T *>(e.param);
   const T *grad = static_cast<const T *>(e.grad);
-#pragma unroll 2
-  for (int it = 0; it < CHUNK / (THREADS / 32 * QB); ++it) {
-    const long long blk = base + (it * (THREADS / 32) + warp) * QB;
-    if (blk >= e.numel) break;
-    const long long i = blk + lane * 8;                       // this lane's first element, in the tensor
-    const long long si = e.state + i;                         // ... and in the flat states (whole blocks are there)
-    const bool whole = e.aligned && i + 8 <= e.numel;
-    float w[8], g[8], m[8], v[8];
-    if (whole) {
-      load8(grad + i, g);
-    } else {
+  using W = typename std::conditional<MASTER, float, T>::type;
+  const f2 b1 = both(h.b1), n1 = both(h.one_minus_b1 * coef), b2 = both(h.b2), n2 = both(h.one_minus_b2), eps = both(h.eps),
+           root_scale = both(h.root_scale), decay = both(e.decay), size = both(-e.size), coef2 = both(coef);
+#pragma unroll 1
+  for (int it = 0; it < PER_WARP; it += BLOCKS) {
+    Raw8<T> rg[BLOCKS];
+    Raw8<W> rw[BLOCKS];
+    RawState<E4M3> rs[BLOCKS];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) g[j] = i + j < e.numel ? to_f32(grad[i + j]) : 0.f;
-    }
-    if (MASTER) {
-      load8(master + si, w);
-    } else if (whole) {
-      load8(param + i, w);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = i + j < e.numel ? to_f32(param[i + j]) : 0.f;
-    }
-    uint8_t *m8 = static_cast<uint8_t *>(state_m) + (e.state + blk), *v8 = static_cast<uint8_t *>(state_v) + (e.state + blk);
-    const long long sb = (e.state + blk) / QB;
-    if (E4M3) {
-      const uint2 cm = *reinterpret_cast<const uint2 *>(m8 + lane * 8), cv = *reinterpret_cast<const uint2 *>(v8 + lane * 8);
-      const float fm = scale_m[sb], fv = scale_v[sb];
-      decode_e4m3x8(cm, m);
-      decode_e4m3x8(cv, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        m[j] = __fmul_rn(m[j], fm);
-        v[j] = __fmul_rn(v[j], fv);
-        v[j] = __fmul_rn(v[j], v[j]);
+    for (int q = 0; q < BLOCKS; ++q) {
+      const long long blk = base + ((it + q) * WARPS + warp) * QB;
+      if (blk >= e.numel) break;
+      const long long i = blk + lane * 8, si = e.state + i;   // first element in the tensor, and in the flat states (whole blocks are there)
+      const bool whole = e.aligned && i + 8 <= e.numel;
+      const int left = (int)min(max(e.numel - i, 0ll), 8ll);
+      if (whole) load_raw(grad + i, rg[q]);
+      else load_raw_part(grad + i, left, rg[q]);
+      if constexpr (MASTER) {
+        load_raw(master + si, rw[q]);
+      } else {
+        if (whole) load_raw(param + i, rw[q]);
+        else load_raw_part(param + i, left, rw[q]);
       }
-    } else {
-      load8(static_cast<const float *>(state_m) + si, m);
-      load8(static_cast<const float *>(state_v) + si, v);
+      if constexpr (E4M3) {
+        const uint2 cm = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(state_m) + si),
+                    cv = *reinterpret_cast<const uint2 *>(static_cast<const uint8_t *>(state_v) + si);
+        rs[q].m[0] = cm.x; rs[q].m[1] = cm.y;
+        rs[q].v[0] = cv.x; rs[q].v[1] = cv.y;
+        rs[q].fm = scale_m[(e.state + blk) / QB];
+        rs[q].fv = scale_v[(e.state + blk) / QB];
+      } else {
+        load32(static_cast<const float *>(state_m) + si, rs[q].m);
+        load32(static_cast<const float *>(state_v) + si, rs[q].v);
+      }
     }
-    float root[8];
-    // Products and sums one rounding each, never contracted: the states are then a function of the inputs alone,
-    // whatever the compiler does, and 8-bit codes do not depend on it.
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float gc = clip ? __fmul_rn(g[j], coef) : g[j];
-      m[j] = __fadd_rn(__fmul_rn(m[j], h.b1), __fmul_rn(gc, h.one_minus_b1));
-      v[j] = __fadd_rn(__fmul_rn(v[j], h.b2), __fmul_rn(__fmul_rn(gc, gc), h.one_minus_b2));
-      root[j] = __fsqrt_rn(v[j]);
-      const float den = fmaf(root[j], h.root_scale, h.eps);
-      w[j] = fmaf(w[j], e.decay, -__fdividef(m[j], den) * e.size);
-    }
-    if (MASTER) store8(master + si, w);
-    if (whole) {
-      store8(param + i, w);
-    } else {
+    for (int q = 0; q < BLOCKS; ++q) {
+      const long long blk = base + ((it + q) * WARPS + warp) * QB;
+      if (blk >= e.numel) break;
+      const long long i = blk + lane * 8, si = e.state + i;
+      const bool whole = e.aligned && i + 8 <= e.numel;
+      f2 w[4], g[4], m[4], v[4], root[4];
+      widen_raw(rg[q], g);
+      widen_raw(rw[q], w);
+      if constexpr (E4M3) {
+        decode_e4m3x8(make_uint2(rs[q].m[0], rs[q].m[1]), m);
+        decode_e4m3x8(make_uint2(rs[q].v[0], rs[q].v[1]), v);
+        const f2 fm = both(rs[q].fm), fv = both(rs[q].fv);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (i + j < e.numel) param[i + j] = from_f32<T>(w[j]);
-    }
-    if (E4M3) {
-      quantise_block<false>(m, m8, scale_m + sb, lane);
-      quantise_block<true>(root, v8, scale_v + sb, lane);
-    } else {
-      store8(static_cast<float *>(state_m) + si, m);
-      store8(static_cast<float *>(state_v) + si, v);
+        for (int j = 0; j < 4; ++j) {
+          m[j] = mul2(m[j], fm);
+          v[j] = mul2(v[j], fv);
+          v[j] = mul2(v[j], v[j]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          m[j] = pack2(__uint_as_float(rs[q].m[2 * j]), __uint_as_float(rs[q].m[2 * j + 1]));
+          v[j] = pack2(__uint_as_float(rs[q].v[2 * j]), __uint_as_float(rs[q].v[2 * j + 1]));
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        m[j] = fma2(n1, g[j], mul2(m[j], b1));
+        const f2 gc = mul2(g[j], coef2);
+        v[j] = fma2(mul2(gc, n2), gc, mul2(v[j], b2));
+        const float2 s = split2(v[j]);
+        root[j] = pack2(fast_sqrt(s.x), fast_sqrt(s.y));
+        const float2 d = split2(fma2(root[j], root_scale, eps));
+        const f2 upd = mul2(m[j], pack2(fast_rcp(d.x), fast_rcp(d.y)));
+        w[j] = fma2(upd, size, mul2(w[j], decay));
+      }
+      if constexpr (MASTER) store4(master + si, w);
+      if (whole) {
+        store4(param + i, w);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float2 p = split2(w[j >> 1]);
+          if (i + j < e.numel) param[i + j] = from_f32<T>((j & 1) ? p.y : p.x);
+        }
+      }
+      if constexpr (E4M3) {
+        const long long sb = (e.state + blk) / QB;
+        quantise_block<false>(m, static_cast<uint8_t *>(state_m) + (e.state + blk), scale_m + sb, lane);
+        quantise_block<true>(root, static_cast<uint8_t *>(state_v) + (e.state + blk), scale_v + sb, lane);
+      } else {
+        store4(static_cast<float *>(state_m) + si, m);
+        store4(static_cast<float *>(state_v) + si, v);
+      }
     }
   }
 }

@@ -154,23 +154,39 @@ __device__ __forceinline__ T from_f32(float v) {
 }
 
 // Eight e4m3 codes (8 bytes) <-> fp32.  Round to nearest, ties to even; beyond +-448 saturates; NaN stays NaN.
-__device__ __forceinline__ void decode_e4m3x8(const uint2 &c, float (&f)[8]) {
+__device__ __forceinline__ void decode_e4m3x8(const uint2 &c, f2 (&f)[4]) {
   const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j >> 1] >> (16 * (j & 1))), __NV_E4M3);
     const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-    f[2 * j] = v.x;
-    f[2 * j + 1] = v.y;
+    f[j] = pack2(v.x, v.y);
   }
 }
-__device__ __forceinline__ uint2 encode_e4m3x8(const float (&f)[8]) {
+__device__ __forceinline__ uint2 encode_e4m3x8(const f2 (&f)[4]) {
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    w[j >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f[2 * j], f[2 * j + 1]), __NV_SATFINITE, __NV_E4M3)
-                 << (16 * (j & 1));
+    w[j >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(split2(f[j]), __NV_SATFINITE, __NV_E4M3) << (16 * (j & 1));
   return make_uint2(w[0], w[1]);
+}
+
+// Largest of three magnitudes; a NaN wins.
+__device__ __forceinline__ float max_abs3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
+  return r;
+}
+// Square root and reciprocal of the special-function unit (relative error about 2^-22; denormals count as zero).
+__device__ __forceinline__ float fast_sqrt(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float fast_rcp(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
 
 // int8 rows: scale = (largest magnitude) / 127; a row whose largest magnitude is below 2^-100 (its reciprocal could

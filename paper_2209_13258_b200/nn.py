@@ -457,7 +457,17 @@ class Int8Linear(torch.nn.Module):
         self.register_buffer("w_scale", w_scale.contiguous())
         self.register_buffer("bias", bias.contiguous() if bias is not None else None)
         self.act, self.k_split, self.split_dim = int(act), int(k_split), int(split_dim)
-        self._ws = B.new_workspace(256, device=weight8.device)
+        self._ws = None
+
+    def _workspace(self, M, quantise):
+        need = 256
+        if quantise:
+            rc, need = B.osdp_i8_workspace_bytes(M, self.in_features)
+            if rc:
+                raise B.OsdpError(rc, "osdp_i8_workspace_bytes")
+        if self._ws is None or self._ws.numel() < need or self._ws.device != self.weight8.device:
+            self._ws = B.new_workspace(need, device=self.weight8.device)
+        return self._ws
 
     @classmethod
     def from_linear(cls, layer, **kw):
@@ -466,16 +476,22 @@ class Int8Linear(torch.nn.Module):
         bias = layer.bias.detach().float() if layer.bias is not None else None
         return cls(q, s, bias, act=getattr(layer, "act", B.ACT_NONE), **kw)
 
-    @torch.no_grad()
     def forward(self, x):
-        q, s = x if isinstance(x, tuple) else quantize_int8(x)
-        if q.dtype != torch.int8 or q.shape[-1] != self.in_features:
-            raise ValueError("Int8Linear takes [..., in_features]")
+        q, s = x if isinstance(x, tuple) else (x, None)
+        if q.dtype != (torch.bfloat16 if s is None else torch.int8) or not q.is_cuda:
+            raise TypeError("Int8Linear takes bf16 CUDA activations, or a pair (int8, fp32 scale per token)")
         K, N = self.in_features, self.out_features
+        shape = q.shape
+        if shape[-1] != K:
+            raise ValueError("Int8Linear takes [..., in_features]")
         M = q.numel() // K
-        if self._ws.device != q.device:
-            self._ws = B.new_workspace(256, device=q.device)
-        out = torch.empty(*q.shape[:-1], N, dtype=torch.bfloat16, device=q.device)
-        B.osdp_split_linear_fwd_i8(q.contiguous(), s.contiguous(), self.weight8, 0, self.w_scale, self.bias, M, N, K, self.k_split,
-                                   self.split_dim, self.act, out, self._ws, check=True)
+        if not q.is_contiguous():
+            q = q.contiguous()
+        if s is not None:
+            if s.dtype != torch.float32 or s.numel() != M:
+                raise ValueError("one fp32 scale per token")
+            s = s.contiguous()
+        out = torch.empty(shape[:-1] + (N,), dtype=torch.bfloat16, device=q.device)
+        B.osdp_split_linear_fwd_i8(q, s, self.weight8, 0, self.w_scale, self.bias, M, N, K, self.k_split, self.split_dim, self.act, out,
+                                   self._workspace(M, s is None), check=True)
         return out

@@ -5,11 +5,13 @@ Argument marshalling only; the arithmetic runs in ``osdp_adamw_step`` / ``osdp_g
 """
 from __future__ import annotations
 
-import ctypes
-
+import numpy as np
 import torch
 
 from . import binding as B
+
+_TENSOR = np.dtype([("param", np.uint64), ("grad", np.uint64), ("numel", np.int64), ("state_offset", np.int64),
+                    ("lr", np.float64), ("weight_decay", np.float64)])      # osdp_adamw_tensor
 
 
 class AdamW(torch.optim.Optimizer):
@@ -49,6 +51,7 @@ class AdamW(torch.optim.Optimizer):
                 raise ValueError("AdamW takes contiguous parameters")
         if master and first.dtype != torch.bfloat16:
             raise ValueError("fp32 parameters are their own master")
+        self._torch_dtype, self._device = first.dtype, first.device
         self._dtype = B.DTYPE_FP32 if first.dtype == torch.float32 else B.DTYPE_BF16
         self._state_dtype = B.DTYPE_E4M3 if state_dtype == "e4m3" else B.DTYPE_FP32
         rc, self.offsets, total = B.osdp_adamw_layout([p.numel() for p in self._params])
@@ -69,9 +72,12 @@ class AdamW(torch.optim.Optimizer):
         self.grad_norm = new(2, torch.float32)
         self.steps = 0
         n = len(self._params)
-        self._table = (B.AdamWTensor * n)()
-        for t, p, o in zip(self._table, self._params, self.offsets):
-            t.numel, t.state_offset = p.numel(), o
+        # the step's table of tensors, filled column by column; `_whole`: its sizes, offsets and rates are those of all
+        # parameters in order
+        self._sizes = [p.numel() for p in self._params]
+        self._group_of = [i for i, g in enumerate(self.param_groups) for _ in g["params"]]
+        self._table = np.zeros(n, dtype=_TENSOR)
+        self._whole, self._rates = False, None
         self._ws = B.new_workspace(B.osdp_grad_norm_workspace_bytes(n)[1], device=dev)
         self._built = True
 
@@ -81,47 +87,71 @@ class AdamW(torch.optim.Optimizer):
         super().add_param_group(group)
 
     def _fill(self):
-        """The table of this step: addresses as they are now, tensors without a gradient left out."""
-        i, n = 0, 0
-        table, params, offsets = self._table, self._params, self.offsets
-        dtype, device = params[0].dtype, params[0].device
-        keep = []
-        for g in self.param_groups:
-            lr, wd = float(g["lr"]), float(g["weight_decay"])
-            for p in g["params"]:
-                d = p.grad
-                if d is not None:
-                    if d.dtype != dtype or d.device != device or d.numel() != p.numel():
-                        raise TypeError("a gradient has its parameter's dtype, device and size")
-                    if not d.is_contiguous():
-                        d = d.contiguous()
-                        keep.append(d)
-                    t = table[n]
-                    t.param, t.grad, t.numel, t.state_offset, t.lr, t.weight_decay = p.data_ptr(), d.data_ptr(), p.numel(), offsets[i], lr, wd
-                    n += 1
-                i += 1
+        """The table of this step: addresses as they are now; tensors without a gradient are left out.  Returns its
+        length and the copies of gradients that were not contiguous."""
+        params, table = self._params, self._table
+        grads = [p.grad for p in params]
+        dtype = self._torch_dtype
+        for p in params:
+            if p.dtype is not dtype:
+                raise TypeError("a parameter's dtype has changed since the optimiser was built")
+        at = range(len(params))
+        if any(g is None for g in grads):
+            at = [i for i, g in enumerate(grads) if g is not None]
+            params, grads = [params[i] for i in at], [grads[i] for i in at]
+        n = len(grads)
+        keep = None
+        if not all(map(torch.Tensor.is_contiguous, grads)):
+            keep = grads = [g.contiguous() for g in grads]
+        rates = [(float(g["lr"]), float(g["weight_decay"])) for g in self.param_groups]
+        if n != len(self._params) or not self._whole or rates != self._rates:
+            table["numel"][:n] = [self._sizes[i] for i in at]
+            table["state_offset"][:n] = [self.offsets[i] for i in at]
+            table["lr"][:n] = [rates[self._group_of[i]][0] for i in at]
+            table["weight_decay"][:n] = [rates[self._group_of[i]][1] for i in at]
+            self._whole, self._rates = n == len(self._params), rates
+        table["param"][:n] = list(map(torch.Tensor.data_ptr, params))
+        table["grad"][:n] = list(map(torch.Tensor.data_ptr, grads))
         return n, keep
 
-    @torch.no_grad()
     def step(self, closure=None):
+        if self._optimizer_step_pre_hooks or self._optimizer_step_post_hooks:
+            for hook in self._optimizer_step_pre_hooks.values():
+                hook(self, (closure,), {})
+            loss = self._step(closure)
+            for hook in self._optimizer_step_post_hooks.values():
+                hook(self, (closure,), {})
+            return loss
+        return self._step(closure)
+
+    step.hooked = True       # the hooks are called here: torch's wrapper around step costs more than the launch
+
+    def _step(self, closure):
         loss = None
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
-        betas, eps = self.param_groups[0]["betas"], self.param_groups[0]["eps"]
-        for g in self.param_groups[1:]:
+        first = self.param_groups[0]
+        betas, eps = first["betas"], first["eps"]
+        for g in self.param_groups:
             if g["betas"] != betas or g["eps"] != eps:
                 raise ValueError("betas and eps are the same for all groups")
+        if torch.cuda.current_device() != self._device.index:
+            with torch.cuda.device(self._device):
+                self._launch(betas, eps)
+        else:
+            self._launch(betas, eps)
+        return loss
+
+    def _launch(self, betas, eps):
         n, keep = self._fill()
         self.steps += 1
-        with torch.cuda.device(self.exp_avg.device):
-            clip = None
-            if self.max_norm is not None:
-                clip = self.grad_norm
-                B.osdp_grad_norm(self._table, n, self._dtype, self.max_norm, clip, self._ws, check=True)
-            B.osdp_adamw_step(self._table, n, self._dtype, self._state_dtype, self.master, self.exp_avg, self.exp_avg_sq,
-                              self.exp_avg_scale, self.exp_avg_sq_scale, betas[0], betas[1], eps, self.steps, clip, check=True)
-        return loss
+        clip, table = None, self._table.ctypes.data
+        if self.max_norm is not None:
+            clip = self.grad_norm
+            B.osdp_grad_norm(table, n, self._dtype, self.max_norm, clip, self._ws, check=True)
+        B.osdp_adamw_step(table, n, self._dtype, self._state_dtype, self.master, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale,
+                          self.exp_avg_sq_scale, betas[0], betas[1], eps, self.steps, clip, check=True)
 
     def state_dict(self):
         d = super().state_dict()

@@ -102,6 +102,26 @@ def test_wide_tiles(P, M, N, K):
             check(out[lo:lo + 2048], mag, ref, act)
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 520, 8192), (1, 64, 32), (2, 2056, 8192), (3, 520, 1040), (4, 4096, 4096), (4, 264, 8192), (7, 520, 1040),
+                                   (40, 520, 1040), (300, 1024, 1040), (1, 8200, 16384), (1, 72, 16400)])
+def test_bf16_tokens_give_the_same_bits_as_quantised_ones(P, M, N, K):
+    """x_scale NULL: whichever kernel quantises, the codes are those of the quantiser."""
+    g = gen(M + K)
+    x = (torch.randn(M, K, device="cuda", generator=g) * 3).bfloat16()
+    w8, sw = codes(g, N, K), torch.rand(N, device="cuda", generator=g) * 0.01
+    bias = torch.randn(N, device="cuda", generator=g)
+    q, s = torch.empty(M, K, dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    P.osdp_quantize_rows_i8(x, M, K, q, s, check=True)
+    want = run(P, q, s, w8, sw, bias, 1)
+    ws = P.new_workspace(P.osdp_i8_workspace_bytes(M, K)[1])
+    out = Guarded((M, N), torch.bfloat16)
+    P.osdp_split_linear_fwd_i8(x, None, w8, 0, sw, bias, M, N, K, 1, 0, 1, out.t, ws, check=True)
+    torch.cuda.synchronize()
+    out.check()
+    assert torch.equal(out.t, want)
+    assert P.osdp_split_linear_fwd_i8(x, None, w8, 0, sw, bias, M, N, K, 1, 0, 1, out.t, P.new_workspace(256)) == 5
+
+
 @pytest.mark.parametrize("M,N,K", [(5, 1024, 1024), (300, 1024, 1024), (4096, 2048, 2048)])
 @pytest.mark.parametrize("split", [0, 1])
 def test_slices_give_the_same_bits(P, M, N, K, split):
