@@ -1276,7 +1276,7 @@ int osdp_split_linear_fwd_i8(const void *x, const float *x_scale, const void *w8
   if (ws_bytes < need) return OSDP_ERR_WORKSPACE_TOO_SMALL;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   const void *w = static_cast<const char *>(w8_flat) + w_offset;
-  const bool few = M <= OSDP_I8_FEW_TOKENS;
+  const bool few = i8_few_tokens(M, N, K);
   if (!x_scale && !(few && i8_quantises_itself(M, K))) {
     float *scale = reinterpret_cast<float *>(static_cast<char *>(ws) + 256);
     void *q = static_cast<char *>(ws) + 256 + align_up((size_t)M * 4, 256);

@@ -926,40 +926,49 @@ struct FinalArgs {
   float *dw_post, *db_post, *dgate, *dw_pre, *db_pre;
 };
 
-// Adds the blocks' channel sums (in ascending order per group of blocks, then the groups in ascending order) and forms
-// the vectors' gradients.  32 channels per block, 8 groups.
-__global__ void __launch_bounds__(256) block_norm_final_kernel(const __grid_constant__ FinalArgs a) {
-  __shared__ float red[4][8][32];
+// Adds the blocks' channel sums and forms the vectors' gradients.  32 channels per block; each of the 32 warps takes every
+// 32nd partial sum (ROW_MAX_BLOCKS / 32 of them, all loads issued together: the kernel is one memory latency long), the
+// warps' sums are added in ascending order.
+__global__ void __launch_bounds__(1024) block_norm_final_kernel(const __grid_constant__ FinalArgs a) {
+  __shared__ float red[4][32][33];
   pdl_launch_dependents();
   pdl_wait();
   const int c = threadIdx.x & 31, g = threadIdx.x >> 5;
   const int col = blockIdx.x * 32 + c;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  if (col < a.D) {
-    for (int u = g; u < a.units; u += 8) {
-      const float *p = a.partial + (long long)u * 4 * a.D + col;
-      s[0] += p[0];
-      s[1] += p[a.D];
-      if (a.layer) {
-        s[2] += p[2ll * a.D];
-        s[3] += p[3ll * a.D];
-      }
-    }
+  constexpr int PER = ROW_MAX_BLOCKS / 32;
+  float v[4][PER];
+#pragma unroll
+  for (int p = 0; p < PER; ++p) {
+    const int u = g + 32 * p;
+    const bool there = col < a.D && u < a.units;
+    const float *from = a.partial + (long long)u * 4 * a.D + col;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k][p] = (there && (k < 2 || a.layer)) ? from[(long long)k * a.D] : 0.f;
   }
 #pragma unroll
-  for (int k = 0; k < 4; ++k) red[k][g][c] = s[k];
-  __syncthreads();
-  if (g != 0 || col >= a.D) return;
+  for (int k = 0; k < 4; ++k) {
+    float s = v[k][0];
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    for (int q = 1; q < 8; ++q) s[k] += red[k][q][c];
+    for (int p = 1; p < PER; ++p) s += v[k][p];
+    red[k][g][c] = s;
+  }
+  __syncthreads();
+  if (g >= 4) return;
+  // warp k adds sum k over the 32 warps, then every sum is in red[k][0]
+  float s = red[g][0][c];
+#pragma unroll
+  for (int q = 1; q < 32; ++q) s += red[g][q][c];
+  red[g][0][c] = s;
+  asm volatile("bar.sync 1, 128;" ::: "memory");
+  if (g != 0 || col >= a.D) return;
+  const float sum_th = red[0][0][c], sum_dh = red[1][0][c], sum_t = red[2][0][c], sum_d = red[3][0][c];
   const float gate = a.gate ? a.gate[col] : 1.f, w = (a.post_has && a.w_post) ? a.w_post[col] : 1.f;
   const float b = a.b_post ? a.b_post[col] : 0.f;
-  if (a.dw_post) a.dw_post[col] = a.beta * gate * s[0];
-  if (a.db_post) a.db_post[col] = a.beta * gate * s[2];
-  if (a.dgate) a.dgate[col] = a.beta * fmaf(w, s[0], b * s[2]);
-  if (a.dw_pre) a.dw_pre[col] = s[1];
-  if (a.db_pre) a.db_pre[col] = s[3];
+  if (a.dw_post) a.dw_post[col] = a.beta * gate * sum_th;
+  if (a.db_post) a.db_post[col] = a.beta * gate * sum_t;
+  if (a.dgate) a.dgate[col] = a.beta * fmaf(w, sum_th, b * sum_t);
+  if (a.dw_pre) a.dw_pre[col] = sum_dh;
+  if (a.db_pre) a.db_pre[col] = sum_d;
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -1179,7 +1188,7 @@ int osdp_block_norm_bwd(const void *dr, const void *du, const void *y, const voi
   f.dgate = dgate;
   f.dw_pre = dw_pre;
   f.db_pre = db_pre;
-  return launch_overlapped(block_norm_final_kernel, dim3((unsigned)cdiv(D, 32)), dim3(256), 0, 1, s, f);
+  return launch_overlapped(block_norm_final_kernel, dim3((unsigned)cdiv(D, 32)), dim3(1024), 0, 1, s, f);
 }
 
 }  // extern "C"

@@ -2,6 +2,9 @@
 // the weights.  Products of many tokens run on the tile kernel (tcgen05.mma.kind::i8, osdp_gemm.cuh).
 #include "../../include/osdp.h"
 
+#include <atomic>
+#include <mutex>
+
 #include "osdp_i8.h"
 #include "osdp_internal.h"
 #include "osdp_vec.cuh"
@@ -44,11 +47,21 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const __nv_bfloat16 
   if (tl == 0) scale[row] = int8_scale(top);
 }
 
-// ---- Few tokens.  Y^T[weight rows x tokens] by mma.sync (int8, exact int32 sums): at this many tokens the product is
-// bound by reading W once, and mma.sync takes W from the registers that it is loaded into.
-// A block owns 8 NT weight rows; its warps take 64-byte steps of K in turn and their sums are added in shared memory.
-// A lane reads 16 consecutive bytes of a row; the four words are used as the operands of two mma whose k order is a
-// permutation of the real one, the same for W and X, which a sum over k does not notice.
+// ---- Few tokens: the product is bound by reading W once; mma.sync (int8, exact int32 sums) takes W straight from
+// registers.  (An mma.sync of 16 x 8 x 32 keeps an SM's quarter busy for about 40 cycles here, two for every 512 bytes of
+// W and 16 tokens, so the memory is the longer part up to about 16 tokens.  dp4a is no way around it: eight per token
+// and 512 bytes took 12 us per token at 32768 x 8192.)
+//
+// One block per SM.  Its 16 warps form groups of WK warps; a group walks units of 8 NT weight rows, each warp with a
+// contiguous share of K, and the warps' sums meet in shared memory at the end of a unit.  A lane copies the 16-byte
+// pieces of W that it needs itself, asynchronously, into its own slots of a ring (no barrier), stages ahead and on into
+// the next unit, so that the stream from memory does not stop at a unit's end.  A stage is Q steps of 64 bytes per row:
+// the instructions around one 64-byte step (512 bytes of W per warp) would by themselves take as long as the memory.
+// The four words of a piece are used as operands of two mma whose k order is a permutation of the real one, the same
+// for W and X, which a sum over k does not notice.
+//
+// Measured on B200, one token, 8192 x 8192 (67 MB of W): 19.5 us, what a plain sum over as many bytes takes (20 us: a
+// read that short does not reach the copy rate); 32768 x 8192: 60 us, 4470 GB/s.
 __device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
@@ -62,30 +75,93 @@ struct FewArgs {
   const float *w_scale, *bias;
   __nv_bfloat16 *out;
   int M, N, K, act;
+  int wk;                     // warps that share a unit (a power of two)
 };
-constexpr int FEW_MAX_WARPS = 8;
+constexpr int FEW_WARPS = 16;
 constexpr int FUSED_MAX_M = 4, FUSED_MAX_BYTES = 16384;   // int8 rows that a block quantises for itself
 
-// MT: 16-token tiles, NT: groups of eight weight rows per block.
-template <int MT, int NT, bool QUANT>
-__global__ void __launch_bounds__(32 * FEW_MAX_WARPS) few_tokens_kernel(const __grid_constant__ FewArgs a) {
-  constexpr int U = 8 / NT;            // steps of K whose loads are issued together: eight 16-byte loads per lane
-  __shared__ int part[FEW_MAX_WARPS][16 * MT * 8 * NT];
+// T8: groups of eight tokens, NT: groups of eight weight rows per unit.
+template <int T8, int NT>
+struct FewShape {
+  static constexpr int MT = (T8 + 1) / 2;                                 // 16-token tiles
+  static constexpr int Q = 4 / NT;                                        // 64-byte steps of a stage
+  static constexpr int STAGE = NT * Q * 512;                              // 2 KB of W per warp
+  static constexpr int STAGES = 4;
+  static constexpr int OUT = 16 * MT * 8 * NT;                            // sums of a unit
+  static constexpr int RING = FEW_WARPS * STAGES * STAGE;
+  static constexpr int TURNS = MT * NT >= 8 ? 1 : 2;                      // buffers for the warps' sums: two units in turn where there is room
+  static constexpr int PART = TURNS * FEW_WARPS * OUT * 4;
+  static constexpr int SMEM = RING + PART;                                // and the tokens, with QUANT
+};
+
+template <int T8, int NT, bool QUANT>
+__global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __grid_constant__ FewArgs a) {
+  using SH = FewShape<T8, NT>;
+  constexpr int MT = SH::MT, Q = SH::Q, S = SH::STAGES, ROWS = 8 * NT, KSTAGE = 64 * Q;
+  extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float scales[16 * MT];
   __shared__ uint32_t top[FUSED_MAX_M];
-  extern __shared__ __align__(16) int8_t xq[];
+  int8_t *xq = reinterpret_cast<int8_t *>(smem + SH::SMEM);
   pdl_launch_dependents();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, kq = (lane & 3) * 16;
-  const int n0 = blockIdx.x * (8 * NT);
-  const int K = a.K, M = a.M, N = a.N;
+  const int K = a.K, M = a.M, N = a.N, WK = a.wk;
+  const int group = warp / WK, wk = warp % WK, groups = FEW_WARPS / WK;
+  const int units = (N + ROWS - 1) / ROWS, first = (int)blockIdx.x + group * (int)gridDim.x, stride = groups * (int)gridDim.x;
   // Nothing says that the weights were not written by the kernel before this one: only a prefetch into L2, where
   // whatever is written later lands as well, may run ahead of the wait.
-  if (threadIdx.x < 8 * NT && n0 + (int)threadIdx.x < N)
-    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.w + (long long)(n0 + threadIdx.x) * K), "r"(K) : "memory");
+  if (wk == 0 && lane < ROWS && first * ROWS + lane < N)
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.w + (long long)(first * ROWS + lane) * K), "r"(K) : "memory");
   if (QUANT && threadIdx.x < FUSED_MAX_M) top[threadIdx.x] = 0u;
   pdl_wait();
-  if (QUANT) {
+
+  const int all_stages = (K + KSTAGE - 1) / KSTAGE, share = (all_stages + WK - 1) / WK;
+  const int k_first = wk * share * KSTAGE;                                // this warp's share of K: n_st stages from k_first
+  const int n_st = min(max(all_stages - wk * share, 0), share);
+  int f_unit = n_st > 0 ? first : units, f_st = 0, f_slot = 0;            // the stage that is copied next
+  const int8_t *f_w[NT];
+  auto f_rows = [&]() {   // rows past the end read the last row: in bounds, and their sums are not stored
+#pragma unroll
+    for (int n = 0; n < NT; ++n) f_w[n] = a.w + (long long)min(f_unit * ROWS + n * 8 + g, N - 1) * K + (k_first + kq);
+  };
+  f_rows();
+  uint8_t *ring = smem + warp * (S * SH::STAGE) + lane * 16;
+  const uint32_t ring_u32 = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
+  auto fetch = [&]() {
+    if (f_unit < units) {
+      const int k = k_first + f_st * KSTAGE;
+      const uint32_t to = ring_u32 + (uint32_t)(f_slot * SH::STAGE);
+      if (k + KSTAGE <= K) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int q = 0; q < Q; ++q)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (uint32_t)((n * Q + q) * 512)), "l"(f_w[n] + q * 64) : "memory");
+      } else {                     // K is a multiple of 16: a lane's piece is whole, or zeros are written
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int q = 0; q < Q; ++q) {
+            const bool there = k + kq + q * 64 < K;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + (uint32_t)((n * Q + q) * 512)), "l"(there ? f_w[n] + q * 64 : a.w), "r"(there ? 16 : 0) : "memory");
+          }
+      }
+      if (++f_st == n_st) {
+        f_st = 0;
+        f_unit += stride;
+        f_rows();
+      } else {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) f_w[n] += KSTAGE;
+      }
+    }
+    if (++f_slot == S) f_slot = 0;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll 1
+  for (int s = 0; s < S - 1; ++s) fetch();
+
+  if (QUANT) {      // while the first pieces of W are on their way
     __syncthreads();
     const __nv_bfloat16 *x = static_cast<const __nv_bfloat16 *>(a.x);
     for (int m = 0; m < M; ++m) {
@@ -109,75 +185,102 @@ __global__ void __launch_bounds__(32 * FEW_MAX_WARPS) few_tokens_kernel(const __
       }
       if (threadIdx.x == 0) scales[m] = int8_scale(t);
     }
-    __syncthreads();
   } else if (threadIdx.x < 16 * MT) {
     scales[threadIdx.x] = (int)threadIdx.x < M ? a.x_scale[threadIdx.x] : 0.f;
   }
-  // rows past the end read the last row: in bounds, and their sums are not stored
-  const int8_t *w[NT];
+  __syncthreads();
+  const int8_t *x8 = (QUANT ? xq : static_cast<const int8_t *>(a.x)) + (k_first + kq);
+  // tokens past the end read the last one: their sums are not stored
+  const int8_t *x_row[T8];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) w[n] = a.w + (long long)min(n0 + n * 8 + g, N - 1) * K;
-  const int8_t *x8 = QUANT ? xq : static_cast<const int8_t *>(a.x);
-  int acc[MT][NT][4];
-#pragma unroll
-  for (int t = 0; t < MT; ++t)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[t][n][j] = 0;
+  for (int t = 0; t < T8; ++t) x_row[t] = x8 + (long long)min(t * 8 + g, M - 1) * K;
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-  // The loop is the warp's: mma.sync needs every lane, those whose 16 bytes lie past K bring zeros (K is a multiple of
-  // 16, so a lane's 16 bytes are whole or absent).
-  for (int k0 = warp * 64; k0 < K; k0 += warps * 64 * U) {
-    uint4 b[U][NT];
+  int slot = 0, turn = 0;
+  for (int unit = first; unit < units; unit += stride, turn = (turn + 1) % SH::TURNS) {
+    int acc[MT][NT][4];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = k0 + u * warps * 64 + kq;
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) b[u][n] = k < K ? load16(w[n] + k) : zero;
-    }
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = k0 + u * warps * 64 + kq;
-      if (k0 + u * warps * 64 >= K) break;
+        for (int j = 0; j < 4; ++j) acc[t][n][j] = 0;
+#pragma unroll 1
+    for (int st = 0; st < n_st; ++st) {     // the loop is the warp's: mma.sync needs every lane
+      const int off = st * KSTAGE;
+      const bool whole = k_first + off + KSTAGE <= K;
+      fetch();
+      asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
+      const uint8_t *from = ring + slot * SH::STAGE;
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        const int m = t * 16 + g;
-        const uint4 lo = (k < K && m < M) ? *reinterpret_cast<const uint4 *>(x8 + (long long)m * K + k) : zero;
-        const uint4 hi = (k < K && m + 8 < M) ? *reinterpret_cast<const uint4 *>(x8 + (long long)(m + 8) * K + k) : zero;
+      for (int q = 0; q < Q; ++q) {
+        const bool there = whole || k_first + off + kq + q * 64 < K;
+        uint4 x[2 * MT];
+#pragma unroll
+        for (int t = 0; t < 2 * MT; ++t) x[t] = (t < T8 && there) ? *reinterpret_cast<const uint4 *>(x_row[t < T8 ? t : 0] + off + q * 64) : zero;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          mma_s8(acc[t][n], lo.x, hi.x, lo.y, hi.y, b[u][n].x, b[u][n].y);
-          mma_s8(acc[t][n], lo.z, hi.z, lo.w, hi.w, b[u][n].z, b[u][n].w);
+          const uint4 b = *reinterpret_cast<const uint4 *>(from + (n * Q + q) * 512);
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            mma_s8(acc[t][n], x[2 * t].x, x[2 * t + 1].x, x[2 * t].y, x[2 * t + 1].y, b.x, b.y);
+            mma_s8(acc[t][n], x[2 * t].z, x[2 * t + 1].z, x[2 * t].w, x[2 * t + 1].w, b.z, b.w);
+          }
         }
       }
+      if (++slot == S) slot = 0;
     }
+    int *sums = reinterpret_cast<int *>(smem + SH::RING) + (turn * FEW_WARPS + group * WK) * SH::OUT;
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)   // token g (+ 8) of the tile, weight rows 2 (lane & 3) + (0, 1) of the group
+          if (2 * t + h < T8)
+            *reinterpret_cast<int2 *>(sums + wk * SH::OUT + (t * 16 + g + 8 * h) * ROWS + n * 8 + 2 * (lane & 3)) = make_int2(acc[t][n][2 * h], acc[t][n][2 * h + 1]);
+    // with two buffers the only barrier of a unit: this buffer is written again only after the next one
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(WK * 32) : "memory");
+    for (int i = wk * 32 + lane; i < T8 * 8 * ROWS; i += WK * 32) {
+      const int m = i / ROWS, n = unit * ROWS + i % ROWS;
+      if (m >= M || n >= N) continue;
+      int s = 0;
+      for (int q = 0; q < WK; ++q) s += sums[q * SH::OUT + i];
+      float f = (float)s * scales[m] * __ldg(a.w_scale + n);
+      if (a.bias) f += __ldg(a.bias + n);
+      a.out[(long long)m * N + n] = __float2bfloat16_rn(gelu1(f, a.act));
+    }
+    if (SH::TURNS == 1) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(WK * 32) : "memory");
   }
-  constexpr int ROWS = 8 * NT;
-#pragma unroll
-  for (int t = 0; t < MT; ++t)
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)   // token g (+ 8) of the tile, weight row 2 (lane & 3) + (0, 1) of the group
-        part[warp][(t * 16 + g + 8 * (j >> 1)) * ROWS + n * 8 + 2 * (lane & 3) + (j & 1)] = acc[t][n][j];
-  __syncthreads();
-  for (int i = threadIdx.x; i < 16 * MT * ROWS; i += blockDim.x) {
-    const int m = i / ROWS, n = n0 + i % ROWS;
-    if (m >= M || n >= N) continue;
-    int s = 0;
-    for (int q = 0; q < warps; ++q) s += part[q][i];
-    float f = (float)s * scales[m] * a.w_scale[n];
-    if (a.bias) f += a.bias[n];
-    a.out[(long long)m * N + n] = __float2bfloat16_rn(gelu1(f, a.act));
-  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-template <int MT, int NT, bool QUANT>
-int launch_few(const FewArgs &a, cudaStream_t stream) {
-  const int64_t blocks = cdiv(a.N, 8 * NT);
-  const int warps = blocks < 148 * 4 ? 8 : 4;     // few blocks: more warps each, to have as many loads in flight
-  return launch_overlapped(few_tokens_kernel<MT, NT, QUANT>, dim3((unsigned)blocks), dim3(32 * warps), QUANT ? (size_t)a.M * a.K : 0, 1, stream, a);
+template <int T8, int NT, bool QUANT>
+int launch_few(const FewArgs &args, cudaStream_t stream) {
+  using SH = FewShape<T8, NT>;
+  int sms = 0;
+  const int rc = sm_count(&sms);
+  if (rc) return rc;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return report_cuda(e);
+  static std::atomic<bool> ready[64];
+  static std::mutex setup;
+  constexpr int most = SH::SMEM + (QUANT ? FUSED_MAX_BYTES : 0);
+  if (!ready[dev & 63].load(std::memory_order_acquire)) {
+    std::lock_guard<std::mutex> lock(setup);
+    e = cudaFuncSetAttribute(few_tokens_kernel<T8, NT, QUANT>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e != cudaSuccess) return report_cuda(e);
+    ready[dev & 63].store(true, std::memory_order_release);
+  }
+  FewArgs a = args;
+  // as many warps to a unit as leave each two stages of it
+  const int64_t stages = cdiv(a.K, 64 * SH::Q);
+  a.wk = FEW_WARPS;
+  while (a.wk > 1 && stages < 2 * a.wk) a.wk /= 2;
+  int64_t blocks = cdiv(a.N, 8 * NT);
+  if (blocks > sms) blocks = sms;
+  return launch_overlapped(few_tokens_kernel<T8, NT, QUANT>, dim3((unsigned)blocks), dim3(32 * FEW_WARPS),
+                           (size_t)SH::SMEM + (QUANT ? (size_t)a.M * a.K : 0), 1, stream, a);
 }
 
 int launch_quantize(const void *x, int64_t M, int64_t K, void *q, float *scale, cudaStream_t stream) {
@@ -194,16 +297,27 @@ int launch_i8_quantize(const void *x, int64_t M, int64_t K, void *q, float *scal
   return launch_quantize(x, M, K, q, scale, stream);
 }
 
+// A tile kernel's block streams 64 weight rows over all of K by itself, so its time goes with K, and with few columns most
+// SMs are idle; this one's goes with N K, and from about 16 tokens on with the mma.  Measured on B200 (us, few / tile):
+// 24 tokens 2048 x 8192 10 / 24, 8192 x 2048 10 / 13, 8192 x 8192 32 / 27; 48 tokens 2048 x 2048 7.9 / 11.5, 2048 x 8192
+// 14 / 24, 8192 x 2048 14 / 13, 8192 x 8192 49 / 28, 32768 x 8192 156 / 68; 16 tokens 32768 x 8192 74 / 67.
+bool i8_few_tokens(int64_t M, int64_t N, int64_t K) {
+  if (M > 64) return false;
+  return M <= 16 || N <= 4096 || (M <= 32 && N * K <= ((int64_t)1 << 25));
+}
+
 bool i8_quantises_itself(int64_t M, int64_t K) { return M <= FUSED_MAX_M && M * K <= FUSED_MAX_BYTES; }
 
 int launch_i8_few_tokens(const void *x, const float *x_scale, const void *w8, const float *w_scale, const float *bias, int64_t M, int64_t N,
                          int64_t K, int act, void *out, cudaStream_t stream) {
-  const FewArgs a{x, x_scale, static_cast<const int8_t *>(w8), w_scale, bias, static_cast<__nv_bfloat16 *>(out), (int)M, (int)N, (int)K, act};
+  const FewArgs a{x, x_scale, static_cast<const int8_t *>(w8), w_scale, bias, static_cast<__nv_bfloat16 *>(out), (int)M, (int)N, (int)K, act, 0};
   if (!x_scale) return launch_few<1, 1, true>(a, stream);
-  // more weight rows to a block as the tokens grow: every block reads all of x
+  // more weight rows to a unit as the tokens grow: every unit reads all of x
   if (M <= 8) return launch_few<1, 1, false>(a, stream);
-  if (M <= 16) return launch_few<1, 2, false>(a, stream);
-  return launch_few<2, 4, false>(a, stream);
+  if (M <= 16) return launch_few<2, 2, false>(a, stream);
+  if (M <= 32) return launch_few<4, 2, false>(a, stream);
+  if (M <= 48) return launch_few<6, 2, false>(a, stream);
+  return launch_few<8, 2, false>(a, stream);
 }
 
 }  // namespace osdp

@@ -6,10 +6,11 @@
 
 namespace osdp {
 
-constexpr int OSDP_I8_FEW_TOKENS = 32;      // most tokens that launch_i8_few_tokens takes
 constexpr int64_t OSDP_I8_MAX_K = 131071;   // 2^31 / 128^2 = 131072 products of the largest magnitude would overflow
 
 int launch_i8_quantize(const void *x, int64_t M, int64_t K, void *q, float *scale, cudaStream_t stream);
+// Whether launch_i8_few_tokens takes this product (64 tokens at most).
+bool i8_few_tokens(int64_t M, int64_t N, int64_t K);
 // Whether launch_i8_few_tokens takes these tokens in bf16 (x_scale NULL): each of its blocks then quantises them for
 // itself, which is cheaper than a launch of its own.
 bool i8_quantises_itself(int64_t M, int64_t K);

@@ -146,8 +146,10 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
                                                         const float *__restrict__ clip) {
   constexpr int WARPS = THREADS / 32, PER_WARP = CHUNK / (WARPS * QB), BLOCKS = E4M3 ? PER_WARP : 1;
   pdl_launch_dependents();
-  const Entry &e = t.e[find_entry(t, blockIdx.x)];
-  const long long base = (long long)(blockIdx.x - e.first_chunk) * CHUNK;
+  // After the gradient norm the last gradients that it read are still in L2: those first.
+  const int chunk = clip ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x;
+  const Entry &e = t.e[find_entry(t, chunk)];
+  const long long base = (long long)(chunk - e.first_chunk) * CHUNK;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();
   float coef = 1.0f;
@@ -254,6 +256,7 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
 // ---- gradient norm: one partial sum of squares per thread block, added in block order by the block that finishes
 // last (no floating-point atomics: the same gradients give the same bits).
 constexpr int NORM_BLOCKS = 592;   // 4 per SM
+constexpr int NORM_CHUNK = 16384;  // eight vectors per thread, all loads issued before the first is used
 
 template <typename T, int MAXT>
 __global__ void __launch_bounds__(THREADS) grad_norm_kernel(const __grid_constant__ Table<MAXT> t, float *partial, int first_partial,
@@ -263,28 +266,30 @@ __global__ void __launch_bounds__(THREADS) grad_norm_kernel(const __grid_constan
   __shared__ bool last;
   pdl_launch_dependents();
   pdl_wait();
-  float acc[8];
+  f2 acc[4];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+  for (int j = 0; j < 4; ++j) acc[j] = both(0.f);
+  constexpr int VECS = NORM_CHUNK / (THREADS * 8);
   for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
     const Entry &e = t.e[find_entry(t, c)];
-    const long long base = (long long)(c - e.first_chunk) * CHUNK;
+    const long long base = (long long)(c - e.first_chunk) * NORM_CHUNK;
     const T *grad = static_cast<const T *>(e.grad);
+    Raw8<T> raw[VECS];
 #pragma unroll
-    for (int it = 0; it < CHUNK / (THREADS * 8); ++it) {
+    for (int it = 0; it < VECS; ++it) {
       const long long i = base + (it * THREADS + threadIdx.x) * 8;
-      float g[8];
-      if (e.aligned && i + 8 <= e.numel) {
-        load8(grad + i, g);
-      } else {
+      if (e.aligned && i + 8 <= e.numel) load_raw(grad + i, raw[it]);
+      else load_raw_part(grad + i, (int)min(max(e.numel - i, 0ll), 8ll), raw[it]);
+    }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] = i + j < e.numel ? to_f32(grad[i + j]) : 0.f;
-      }
+    for (int it = 0; it < VECS; ++it) {
+      f2 g[4];
+      widen_raw(raw[it], g);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] = fmaf(g[j], g[j], acc[j]);
+      for (int j = 0; j < 4; ++j) acc[j] = fma2(g[j], g[j], acc[j]);
     }
   }
-  float s = ((acc[0] + acc[1]) + (acc[2] + acc[3])) + ((acc[4] + acc[5]) + (acc[6] + acc[7]));
+  float s = sum2(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])));
   s = warp_sum(s);
   if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
   __syncthreads();
@@ -337,7 +342,7 @@ int check_tensors(const osdp_adamw_tensor *t, int n, int dtype, bool need_param)
 
 // Fills tables with the tensors that have elements and hands each to launch(table, is_first, index of its first chunk).
 template <int MAXT, typename Fill, typename Launch>
-int for_each_table(const osdp_adamw_tensor *t, int n, int dtype, bool with_param, Fill fill, Launch launch) {
+int for_each_table(const osdp_adamw_tensor *t, int n, int dtype, bool with_param, int chunk, Fill fill, Launch launch) {
   const uintptr_t vec = dtype == OSDP_DTYPE_FP32 ? 32 : 16;
   Table<MAXT> tab;
   int i = 0;
@@ -354,7 +359,7 @@ int for_each_table(const osdp_adamw_tensor *t, int n, int dtype, bool with_param
       e.first_chunk = (int)chunks;
       e.aligned = aligned_to(t[i].grad, vec) && (!with_param || aligned_to(t[i].param, vec));
       fill(t[i], e);
-      chunks += cdiv(t[i].numel, CHUNK);
+      chunks += cdiv(t[i].numel, chunk);
     }
     if (tab.n == 0) break;
     tab.chunks = (int)chunks;
@@ -368,7 +373,7 @@ template <typename T, bool MASTER, bool E4M3, int MAXT>
 int launch_adamw(const osdp_adamw_tensor *t, int n, int dtype, const Hyper &h, double beta1_t, float *master, void *m, void *v,
                  float *sm, float *sv, const float *clip, cudaStream_t stream) {
   return for_each_table<MAXT>(
-      t, n, dtype, true,
+      t, n, dtype, true, CHUNK,
       [&](const osdp_adamw_tensor &a, Entry &e) {
         e.decay = (float)(1.0 - a.lr * a.weight_decay);
         e.size = (float)(a.lr / (1.0 - beta1_t));
@@ -393,7 +398,7 @@ int launch_norm(const osdp_adamw_tensor *t, int n, int dtype, float max_norm, fl
   int total = 0;
   auto blocks = [](int chunks) { return chunks < NORM_BLOCKS ? chunks : NORM_BLOCKS; };
   auto none = [](const osdp_adamw_tensor &, Entry &) {};
-  int rc = for_each_table<MAXT>(t, n, dtype, false, none, [&](const Table<MAXT> &tab) { total += blocks(tab.chunks); return OSDP_OK; });
+  int rc = for_each_table<MAXT>(t, n, dtype, false, NORM_CHUNK, none, [&](const Table<MAXT> &tab) { total += blocks(tab.chunks); return OSDP_OK; });
   if (rc) return rc;
   Table<MAXT> empty;
   empty.n = 0;
@@ -401,7 +406,7 @@ int launch_norm(const osdp_adamw_tensor *t, int n, int dtype, float max_norm, fl
   if (total == 0)   // no elements at all: the norm is zero
     return launch_overlapped(grad_norm_kernel<T, MAXT>, dim3(1), dim3(THREADS), 0, 1, stream, empty, partial, 0, 1, ticket, max_norm, out);
   int at = 0;
-  return for_each_table<MAXT>(t, n, dtype, false, none, [&](const Table<MAXT> &tab) {
+  return for_each_table<MAXT>(t, n, dtype, false, NORM_CHUNK, none, [&](const Table<MAXT> &tab) {
     const int b = blocks(tab.chunks);
     const int first = at;
     at += b;
