@@ -53,9 +53,9 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const __nv_bfloat16 
 // and 512 bytes took 12 us per token at 32768 x 8192.)
 //
 // One block per SM.  Its 16 warps form groups of WK warps; a group walks units of 8 NT weight rows, each warp with a
-// contiguous share of K, and the warps' sums meet in shared memory at the end of a unit.  A lane copies the 16-byte
-// pieces of W that it needs itself, asynchronously, into its own slots of a ring (no barrier), stages ahead and on into
-// the next unit, so that the stream from memory does not stop at a unit's end.  A stage is Q steps of 64 bytes per row:
+// contiguous share of K, and the warps' sums meet in shared memory at the end of a unit.  A warp copies its pieces of W
+// asynchronously into its own ring, stages ahead and on into the next unit, so that the stream from memory does not stop
+// at a unit's end; a copy instruction covers whole 128-byte lines, and a lane then picks the pieces of its mma operands.  A stage is Q steps of 64 bytes per row:
 // the instructions around one 64-byte step (512 bytes of W per warp) would by themselves take as long as the memory.
 // The four words of a piece are used as operands of two mma whose k order is a permutation of the real one, the same
 // for W and X, which a sum over k does not notice.
@@ -85,7 +85,7 @@ template <int T8, int NT>
 struct FewShape {
   static constexpr int MT = (T8 + 1) / 2;                                 // 16-token tiles
   static constexpr int Q = 4 / NT;                                        // 64-byte steps of a stage
-  static constexpr int STAGE = NT * Q * 512;                              // 2 KB of W per warp
+  static constexpr int STAGE = 8 * NT * 64 * Q;                           // 2 KB of W per warp
   static constexpr int STAGES = 4;
   static constexpr int OUT = 16 * MT * 8 * NT;                            // sums of a unit
   static constexpr int RING = FEW_WARPS * STAGES * STAGE;
@@ -119,40 +119,32 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
   const int k_first = wk * share * KSTAGE;                                // this warp's share of K: n_st stages from k_first
   const int n_st = min(max(all_stages - wk * share, 0), share);
   int f_unit = n_st > 0 ? first : units, f_st = 0, f_slot = 0;            // the stage that is copied next
-  const int8_t *f_w[NT];
+  // A copy instruction brings COPY_ROWS rows of KSTAGE bytes.  16-byte piece c of row r lies at place c ^ 4 (r & 1) of the
+  // row's 4 Q places, so that the eight lanes that read together (two rows, four pieces each) hit all banks.
+  constexpr int PIECES = 4 * Q, COPY_ROWS = 32 / PIECES, COPIES = ROWS / COPY_ROWS;
+  const int c_row = lane / PIECES, c_piece = lane % PIECES;
+  const int8_t *f_w[COPIES];
   auto f_rows = [&]() {   // rows past the end read the last row: in bounds, and their sums are not stored
 #pragma unroll
-    for (int n = 0; n < NT; ++n) f_w[n] = a.w + (long long)min(f_unit * ROWS + n * 8 + g, N - 1) * K + (k_first + kq);
+    for (int n = 0; n < COPIES; ++n) f_w[n] = a.w + (long long)min(f_unit * ROWS + n * COPY_ROWS + c_row, N - 1) * K + (k_first + c_piece * 16);
   };
   f_rows();
-  uint8_t *ring = smem + warp * (S * SH::STAGE) + lane * 16;
-  const uint32_t ring_u32 = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
+  uint8_t *ring = smem + warp * (S * SH::STAGE);
+  const uint32_t ring_u32 = static_cast<uint32_t>(__cvta_generic_to_shared(ring)) + (uint32_t)(c_row * KSTAGE + (c_piece ^ ((c_row & 1) << 2)) * 16);
   auto fetch = [&]() {
     if (f_unit < units) {
-      const int k = k_first + f_st * KSTAGE;
       const uint32_t to = ring_u32 + (uint32_t)(f_slot * SH::STAGE);
-      if (k + KSTAGE <= K) {
+      const bool there = k_first + f_st * KSTAGE + c_piece * 16 < K;   // K is a multiple of 16: a piece is whole, or zeros are written
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int q = 0; q < Q; ++q)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (uint32_t)((n * Q + q) * 512)), "l"(f_w[n] + q * 64) : "memory");
-      } else {                     // K is a multiple of 16: a lane's piece is whole, or zeros are written
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int q = 0; q < Q; ++q) {
-            const bool there = k + kq + q * 64 < K;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + (uint32_t)((n * Q + q) * 512)), "l"(there ? f_w[n] + q * 64 : a.w), "r"(there ? 16 : 0) : "memory");
-          }
-      }
+      for (int n = 0; n < COPIES; ++n)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + (uint32_t)(n * COPY_ROWS * KSTAGE)), "l"(there ? f_w[n] : a.w), "r"(there ? 16 : 0) : "memory");
       if (++f_st == n_st) {
         f_st = 0;
         f_unit += stride;
         f_rows();
       } else {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) f_w[n] += KSTAGE;
+        for (int n = 0; n < COPIES; ++n) f_w[n] += KSTAGE;
       }
     }
     if (++f_slot == S) f_slot = 0;
@@ -208,9 +200,11 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
     for (int st = 0; st < n_st; ++st) {     // the loop is the warp's: mma.sync needs every lane
       const int off = st * KSTAGE;
       const bool whole = k_first + off + KSTAGE <= K;
+      __syncwarp();      // every lane has read the slot that is filled now
       fetch();
       asm volatile("cp.async.wait_group %0;" ::"n"(S - 1) : "memory");
-      const uint8_t *from = ring + slot * SH::STAGE;
+      __syncwarp();      // every lane's copies of this stage have landed
+      const uint8_t *from = ring + slot * SH::STAGE + g * KSTAGE + kq;
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
         const bool there = whole || k_first + off + kq + q * 64 < K;
@@ -219,7 +213,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
         for (int t = 0; t < 2 * MT; ++t) x[t] = (t < T8 && there) ? *reinterpret_cast<const uint4 *>(x_row[t < T8 ? t : 0] + off + q * 64) : zero;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          const uint4 b = *reinterpret_cast<const uint4 *>(from + (n * Q + q) * 512);
+          const uint4 b = *reinterpret_cast<const uint4 *>(from + n * 8 * KSTAGE + ((q ^ (g & 1)) * 64));
 #pragma unroll
           for (int t = 0; t < MT; ++t) {
             mma_s8(acc[t][n], x[2 * t].x, x[2 * t + 1].x, x[2 * t].y, x[2 * t + 1].y, b.x, b.y);
