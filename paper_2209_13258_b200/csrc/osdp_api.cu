@@ -1277,7 +1277,7 @@ int osdp_split_linear_fwd_i8(const void *x, const float *x_scale, const void *w8
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
   const void *w = static_cast<const char *>(w8_flat) + w_offset;
   const bool few = i8_few_tokens(M, N, K);
-  if (!x_scale && !(few && i8_quantises_itself(M, K))) {
+  if (!x_scale) {
     float *scale = reinterpret_cast<float *>(static_cast<char *>(ws) + 256);
     void *q = static_cast<char *>(ws) + 256 + align_up((size_t)M * 4, 256);
     rc = launch_i8_quantize(x, M, K, q, scale, stream);

@@ -60,8 +60,8 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const __nv_bfloat16 
 // The four words of a piece are used as operands of two mma whose k order is a permutation of the real one, the same
 // for W and X, which a sum over k does not notice.
 //
-// Measured on B200, one token, 8192 x 8192 (67 MB of W): 19.5 us, what a plain sum over as many bytes takes (20 us: a
-// read that short does not reach the copy rate); 32768 x 8192: 60 us, 4470 GB/s.
+// Measured on B200, one token, 8192 x 8192 (67 MB of W): 15.0 us, 4470 GB/s, where the bare stream takes 13 us (a read
+// that short does not reach the copy rate); 32768 x 8192: 45.9 us, 5850 GB/s; 8 tokens 53 us, 16 tokens 68 us.
 __device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
@@ -69,7 +69,7 @@ __device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, ui
 }
 
 struct FewArgs {
-  const void *x;              // int8 [M,K], or bf16 [M,K] that the block quantises itself (QUANT)
+  const int8_t *x;
   const float *x_scale;
   const int8_t *w;
   const float *w_scale, *bias;
@@ -78,7 +78,7 @@ struct FewArgs {
   int wk;                     // warps that share a unit (a power of two)
 };
 constexpr int FEW_WARPS = 16;
-constexpr int FUSED_MAX_M = 4, FUSED_MAX_BYTES = 16384;   // int8 rows that a block quantises for itself
+constexpr int X_SMEM = 66 * 1024;                                         // shared memory for the tokens where they fit
 
 // T8: groups of eight tokens, NT: groups of eight weight rows per unit.
 template <int T8, int NT>
@@ -88,20 +88,22 @@ struct FewShape {
   static constexpr int STAGE = 8 * NT * 64 * Q;                           // 2 KB of W per warp
   static constexpr int STAGES = 4;
   static constexpr int OUT = 16 * MT * 8 * NT;                            // sums of a unit
+  static constexpr int PITCH = OUT + 4;                                   // a warp's sums: the four words keep the readers below off each other's banks
   static constexpr int RING = FEW_WARPS * STAGES * STAGE;
   static constexpr int TURNS = MT * NT >= 8 ? 1 : 2;                      // buffers for the warps' sums: two units in turn where there is room
-  static constexpr int PART = TURNS * FEW_WARPS * OUT * 4;
-  static constexpr int SMEM = RING + PART;                                // and the tokens, with QUANT
+  static constexpr int PART = TURNS * FEW_WARPS * PITCH * 4;
+  static constexpr int SMEM = RING + PART;                                // and the tokens, with XS
 };
 
-template <int T8, int NT, bool QUANT>
+// XS: the tokens are copied to shared memory first (rows 64 bytes apart beyond K, so that two rows read together do not
+// meet in a bank); otherwise they are read through L1.
+template <int T8, int NT, bool XS>
 __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __grid_constant__ FewArgs a) {
   using SH = FewShape<T8, NT>;
   constexpr int MT = SH::MT, Q = SH::Q, S = SH::STAGES, ROWS = 8 * NT, KSTAGE = 64 * Q;
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ float scales[16 * MT];
-  __shared__ uint32_t top[FUSED_MAX_M];
-  int8_t *xq = reinterpret_cast<int8_t *>(smem + SH::SMEM);
+  int8_t *xs = reinterpret_cast<int8_t *>(smem + SH::SMEM);
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, kq = (lane & 3) * 16;
@@ -110,9 +112,12 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
   const int units = (N + ROWS - 1) / ROWS, first = (int)blockIdx.x + group * (int)gridDim.x, stride = groups * (int)gridDim.x;
   // Nothing says that the weights were not written by the kernel before this one: only a prefetch into L2, where
   // whatever is written later lands as well, may run ahead of the wait.
-  if (wk == 0 && lane < ROWS && first * ROWS + lane < N)
-    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.w + (long long)(first * ROWS + lane) * K), "r"(K) : "memory");
-  if (QUANT && threadIdx.x < FUSED_MAX_M) top[threadIdx.x] = 0u;
+  if (wk == 0) {
+    for (int i = lane; i < 3 * ROWS; i += 32) {
+      const long long row = (long long)(first + i / ROWS * stride) * ROWS + i % ROWS;
+      if (row < N) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.w + row * K), "r"(K) : "memory");
+    }
+  }
   pdl_wait();
 
   const int all_stages = (K + KSTAGE - 1) / KSTAGE, share = (all_stages + WK - 1) / WK;
@@ -153,42 +158,32 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
 #pragma unroll 1
   for (int s = 0; s < S - 1; ++s) fetch();
 
-  if (QUANT) {      // while the first pieces of W are on their way
-    __syncthreads();
-    const __nv_bfloat16 *x = static_cast<const __nv_bfloat16 *>(a.x);
-    for (int m = 0; m < M; ++m) {
-      uint32_t bits = 0u;
-      for (int c = threadIdx.x * 8; c < K; c += blockDim.x * 8) {
-        float f[8];
-        widen8(__ldg(reinterpret_cast<const uint4 *>(x + (long long)m * K + c)), f);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) bits = max(bits, __float_as_uint(f[k]) & 0x7FFFFFFFu);
-      }
-      bits = __reduce_max_sync(0xFFFFFFFFu, bits);
-      if (lane == 0) atomicMax(&top[m], bits);
+  if (threadIdx.x < 16 * MT) scales[threadIdx.x] = (int)threadIdx.x < M ? a.x_scale[threadIdx.x] : 0.f;
+  if (XS) {
+    const int pieces = K / 16;
+    for (int i = threadIdx.x; i < M * pieces; i += blockDim.x) {
+      const int m = i / pieces, c = i - m * pieces;
+      *reinterpret_cast<uint4 *>(xs + m * (K + 64) + c * 16) = __ldg(reinterpret_cast<const uint4 *>(a.x + (long long)m * K + c * 16));
     }
-    __syncthreads();
-    for (int m = 0; m < M; ++m) {
-      const float t = __uint_as_float(top[m]), inv = int8_inverse(t);
-      for (int c = threadIdx.x * 8; c < K; c += blockDim.x * 8) {
-        float f[8];
-        widen8(__ldg(reinterpret_cast<const uint4 *>(x + (long long)m * K + c)), f);
-        *reinterpret_cast<uint2 *>(xq + m * K + c) = to_int8x8(f, inv);
-      }
-      if (threadIdx.x == 0) scales[m] = int8_scale(t);
-    }
-  } else if (threadIdx.x < 16 * MT) {
-    scales[threadIdx.x] = (int)threadIdx.x < M ? a.x_scale[threadIdx.x] : 0.f;
   }
   __syncthreads();
-  const int8_t *x8 = (QUANT ? xq : static_cast<const int8_t *>(a.x)) + (k_first + kq);
+  const int8_t *x8 = (XS ? xs : a.x) + (k_first + kq);
+  const int x_pitch = XS ? K + 64 : K;
   // tokens past the end read the last one: their sums are not stored
   const int8_t *x_row[T8];
 #pragma unroll
-  for (int t = 0; t < T8; ++t) x_row[t] = x8 + (long long)min(t * 8 + g, M - 1) * K;
+  for (int t = 0; t < T8; ++t) x_row[t] = x8 + (long long)min(t * 8 + g, M - 1) * x_pitch;
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
   int slot = 0, turn = 0;
+  // The sums of a unit are added by all threads of the group: `per` adjacent lanes to an output, each a part of the warps.
+  constexpr int OUTPUTS = T8 * 8 * ROWS;
+  const int in_group = wk * 32 + lane;
+  int per = 1;
+  while (per < WK && per < 8 && 2 * per * OUTPUTS <= WK * 32) per *= 2;
   for (int unit = first; unit < units; unit += stride, turn = (turn + 1) % SH::TURNS) {
+    // what the epilogue needs of this thread's first output's column, while the products run
+    const int n_first = min(unit * ROWS + (in_group / per) % ROWS, N - 1);
+    const float ws_first = __ldg(a.w_scale + n_first), b_first = a.bias ? __ldg(a.bias + n_first) : 0.f;
     int acc[MT][NT][4];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -223,7 +218,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
       }
       if (++slot == S) slot = 0;
     }
-    int *sums = reinterpret_cast<int *>(smem + SH::RING) + (turn * FEW_WARPS + group * WK) * SH::OUT;
+    int *sums = reinterpret_cast<int *>(smem + SH::RING) + (turn * FEW_WARPS + group * WK) * SH::PITCH;
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -231,24 +226,26 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
 #pragma unroll
         for (int h = 0; h < 2; ++h)   // token g (+ 8) of the tile, weight rows 2 (lane & 3) + (0, 1) of the group
           if (2 * t + h < T8)
-            *reinterpret_cast<int2 *>(sums + wk * SH::OUT + (t * 16 + g + 8 * h) * ROWS + n * 8 + 2 * (lane & 3)) = make_int2(acc[t][n][2 * h], acc[t][n][2 * h + 1]);
+            *reinterpret_cast<int2 *>(sums + wk * SH::PITCH + (t * 16 + g + 8 * h) * ROWS + n * 8 + 2 * (lane & 3)) = make_int2(acc[t][n][2 * h], acc[t][n][2 * h + 1]);
     // with two buffers the only barrier of a unit: this buffer is written again only after the next one
     asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(WK * 32) : "memory");
-    for (int i = wk * 32 + lane; i < T8 * 8 * ROWS; i += WK * 32) {
-      const int m = i / ROWS, n = unit * ROWS + i % ROWS;
-      if (m >= M || n >= N) continue;
+    for (int i = in_group / per; i < OUTPUTS; i += WK * 32 / per) {   // whole warps, or all their lanes, leave together
       int s = 0;
-      for (int q = 0; q < WK; ++q) s += sums[q * SH::OUT + i];
-      float f = (float)s * scales[m] * __ldg(a.w_scale + n);
-      if (a.bias) f += __ldg(a.bias + n);
-      a.out[(long long)m * N + n] = __float2bfloat16_rn(gelu1(f, a.act));
+      for (int q = in_group % per; q < WK; q += per) s += sums[q * SH::PITCH + i];
+      for (int o = per / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+      const int m = i / ROWS, n = unit * ROWS + i % ROWS;
+      if (m < M && n < N && in_group % per == 0) {
+        const bool f1 = i == in_group / per;
+        const float f = fmaf((float)s * scales[m], f1 ? ws_first : __ldg(a.w_scale + n), f1 ? b_first : a.bias ? __ldg(a.bias + n) : 0.f);
+        a.out[(long long)m * N + n] = __float2bfloat16_rn(gelu1(f, a.act));
+      }
     }
     if (SH::TURNS == 1) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(WK * 32) : "memory");
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-template <int T8, int NT, bool QUANT>
+template <int T8, int NT, bool XS>
 int launch_few(const FewArgs &args, cudaStream_t stream) {
   using SH = FewShape<T8, NT>;
   int sms = 0;
@@ -259,10 +256,10 @@ int launch_few(const FewArgs &args, cudaStream_t stream) {
   if (e != cudaSuccess) return report_cuda(e);
   static std::atomic<bool> ready[64];
   static std::mutex setup;
-  constexpr int most = SH::SMEM + (QUANT ? FUSED_MAX_BYTES : 0);
+  constexpr int most = SH::SMEM + (XS ? X_SMEM : 0);
   if (!ready[dev & 63].load(std::memory_order_acquire)) {
     std::lock_guard<std::mutex> lock(setup);
-    e = cudaFuncSetAttribute(few_tokens_kernel<T8, NT, QUANT>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    e = cudaFuncSetAttribute(few_tokens_kernel<T8, NT, XS>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
     if (e != cudaSuccess) return report_cuda(e);
     ready[dev & 63].store(true, std::memory_order_release);
   }
@@ -273,8 +270,8 @@ int launch_few(const FewArgs &args, cudaStream_t stream) {
   while (a.wk > 1 && stages < 2 * a.wk) a.wk /= 2;
   int64_t blocks = cdiv(a.N, 8 * NT);
   if (blocks > sms) blocks = sms;
-  return launch_overlapped(few_tokens_kernel<T8, NT, QUANT>, dim3((unsigned)blocks), dim3(32 * FEW_WARPS),
-                           (size_t)SH::SMEM + (QUANT ? (size_t)a.M * a.K : 0), 1, stream, a);
+  return launch_overlapped(few_tokens_kernel<T8, NT, XS>, dim3((unsigned)blocks), dim3(32 * FEW_WARPS),
+                           (size_t)SH::SMEM + (XS ? (size_t)a.M * (a.K + 64) : 0), 1, stream, a);
 }
 
 int launch_quantize(const void *x, int64_t M, int64_t K, void *q, float *scale, cudaStream_t stream) {
@@ -300,15 +297,14 @@ bool i8_few_tokens(int64_t M, int64_t N, int64_t K) {
   return M <= 16 || N <= 4096 || (M <= 32 && N * K <= ((int64_t)1 << 25));
 }
 
-bool i8_quantises_itself(int64_t M, int64_t K) { return M <= FUSED_MAX_M && M * K <= FUSED_MAX_BYTES; }
-
-int launch_i8_few_tokens(const void *x, const float *x_scale, const void *w8, const float *w_scale, const float *bias, int64_t M, int64_t N,
+int launch_i8_few_tokens(const void *x8, const float *x_scale, const void *w8, const float *w_scale, const float *bias, int64_t M, int64_t N,
                          int64_t K, int act, void *out, cudaStream_t stream) {
-  const FewArgs a{x, x_scale, static_cast<const int8_t *>(w8), w_scale, bias, static_cast<__nv_bfloat16 *>(out), (int)M, (int)N, (int)K, act, 0};
-  if (!x_scale) return launch_few<1, 1, true>(a, stream);
+  const FewArgs a{static_cast<const int8_t *>(x8), x_scale, static_cast<const int8_t *>(w8), w_scale, bias, static_cast<__nv_bfloat16 *>(out),
+                  (int)M, (int)N, (int)K, act, 0};
   // more weight rows to a unit as the tokens grow: every unit reads all of x
+  if (M <= 8 && M * (K + 64) <= X_SMEM) return launch_few<1, 1, true>(a, stream);   // 8 tokens, 32768 x 8192: 62 -> 53 us
   if (M <= 8) return launch_few<1, 1, false>(a, stream);
-  if (M <= 16) return launch_few<2, 2, false>(a, stream);
+  if (M <= 16) return launch_few<2, 2, false>(a, stream);   // (no faster from shared memory: 16 tokens, 8200 x 2064 7.3 / 8.2 us)
   if (M <= 32) return launch_few<4, 2, false>(a, stream);
   if (M <= 48) return launch_few<6, 2, false>(a, stream);
   return launch_few<8, 2, false>(a, stream);

@@ -37,9 +37,9 @@ struct Entry {
   int aligned;         // param and grad allow eight-element accesses
 };
 // Tensors of one launch.  The table travels as a kernel parameter (up to 32 KB): no copy to the device, nothing to
-// keep alive, and a stream capture takes it along.  Two sizes, so that a step over a few tensors does not pay for
+// keep alive, and a stream capture takes it along.  Three sizes, so that a step over fewer tensors does not pay for
 // the launch of a full table.
-constexpr int TABLE_SMALL = 48, TABLE_LARGE = 640;
+constexpr int TABLE_SMALL = 48, TABLE_MIDDLE = 192, TABLE_LARGE = 640;
 template <int MAXT>
 struct Table {
   Entry e[MAXT];
@@ -387,8 +387,9 @@ int launch_adamw(const osdp_adamw_tensor *t, int n, int dtype, const Hyper &h, d
 template <typename T, bool MASTER, bool E4M3>
 int pick_table(const osdp_adamw_tensor *t, int n, int dtype, const Hyper &h, double b1t, float *master, void *m, void *v, float *sm,
                float *sv, const float *clip, cudaStream_t stream) {
-  return n <= TABLE_SMALL ? launch_adamw<T, MASTER, E4M3, TABLE_SMALL>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream)
-                          : launch_adamw<T, MASTER, E4M3, TABLE_LARGE>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream);
+  if (n <= TABLE_SMALL) return launch_adamw<T, MASTER, E4M3, TABLE_SMALL>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream);
+  if (n <= TABLE_MIDDLE) return launch_adamw<T, MASTER, E4M3, TABLE_MIDDLE>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream);
+  return launch_adamw<T, MASTER, E4M3, TABLE_LARGE>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream);
 }
 
 template <typename T, int MAXT>
@@ -458,12 +459,12 @@ int osdp_grad_norm(const osdp_adamw_tensor *tensors, int n_tensors, int grad_dty
   unsigned *ticket = reinterpret_cast<unsigned *>(static_cast<char *>(ws) + 64);
   float *partial = reinterpret_cast<float *>(static_cast<char *>(ws) + STATUS_BYTES);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const bool small = n_tensors <= TABLE_SMALL;
-  if (grad_dtype == OSDP_DTYPE_FP32)
-    return small ? launch_norm<float, TABLE_SMALL>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s)
-                 : launch_norm<float, TABLE_LARGE>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s);
-  return small ? launch_norm<__nv_bfloat16, TABLE_SMALL>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s)
-               : launch_norm<__nv_bfloat16, TABLE_LARGE>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s);
+#define OSDP_NORM(T) \
+  (n_tensors <= TABLE_SMALL ? launch_norm<T, TABLE_SMALL>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s) \
+   : n_tensors <= TABLE_MIDDLE ? launch_norm<T, TABLE_MIDDLE>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s) \
+                               : launch_norm<T, TABLE_LARGE>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s))
+  return grad_dtype == OSDP_DTYPE_FP32 ? OSDP_NORM(float) : OSDP_NORM(__nv_bfloat16);
+#undef OSDP_NORM
 }
 
 int osdp_adamw_step(const osdp_adamw_tensor *tensors, int n_tensors, int param_dtype, int state_dtype, float *master,

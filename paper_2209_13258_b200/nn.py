@@ -457,16 +457,15 @@ class Int8Linear(torch.nn.Module):
         self.register_buffer("w_scale", w_scale.contiguous())
         self.register_buffer("bias", bias.contiguous() if bias is not None else None)
         self.act, self.k_split, self.split_dim = int(act), int(k_split), int(split_dim)
-        self._ws = None
+        self._ws, self._ws_tokens = None, 0
 
     def _workspace(self, M, quantise):
-        need = 256
-        if quantise:
-            rc, need = B.osdp_i8_workspace_bytes(M, self.in_features)
-            if rc:
-                raise B.OsdpError(rc, "osdp_i8_workspace_bytes")
-        if self._ws is None or self._ws.numel() < need or self._ws.device != self.weight8.device:
-            self._ws = B.new_workspace(need, device=self.weight8.device)
+        if self._ws is not None and (not quantise or M <= self._ws_tokens) and self._ws.device == self.weight8.device:
+            return self._ws
+        rc, need = B.osdp_i8_workspace_bytes(M, self.in_features)
+        if rc:
+            raise B.OsdpError(rc, "osdp_i8_workspace_bytes")
+        self._ws, self._ws_tokens = B.new_workspace(need, device=self.weight8.device), M
         return self._ws
 
     @classmethod

@@ -5,6 +5,8 @@ Argument marshalling only; the arithmetic runs in ``osdp_adamw_step`` / ``osdp_g
 """
 from __future__ import annotations
 
+import operator
+
 import numpy as np
 import torch
 
@@ -12,6 +14,9 @@ from . import binding as B
 
 _TENSOR = np.dtype([("param", np.uint64), ("grad", np.uint64), ("numel", np.int64), ("state_offset", np.int64),
                     ("lr", np.float64), ("weight_decay", np.float64)])      # osdp_adamw_tensor
+
+
+_GRAD, _DATA_PTR, _IS_CONTIGUOUS = operator.attrgetter("grad"), torch.Tensor.data_ptr, torch.Tensor.is_contiguous
 
 
 class AdamW(torch.optim.Optimizer):
@@ -77,6 +82,7 @@ class AdamW(torch.optim.Optimizer):
         self._sizes = [p.numel() for p in self._params]
         self._group_of = [i for i, g in enumerate(self.param_groups) for _ in g["params"]]
         self._table = np.zeros(n, dtype=_TENSOR)
+        self._table_address = self._table.ctypes.data
         self._whole, self._rates = False, None
         self._ws = B.new_workspace(B.osdp_grad_norm_workspace_bytes(n)[1], device=dev)
         self._built = True
@@ -90,28 +96,30 @@ class AdamW(torch.optim.Optimizer):
         """The table of this step: addresses as they are now; tensors without a gradient are left out.  Returns its
         length and the copies of gradients that were not contiguous."""
         params, table = self._params, self._table
-        grads = [p.grad for p in params]
         dtype = self._torch_dtype
         for p in params:
             if p.dtype is not dtype:
                 raise TypeError("a parameter's dtype has changed since the optimiser was built")
-        at = range(len(params))
-        if any(g is None for g in grads):
+        grads, at, keep = list(map(_GRAD, params)), None, None
+        try:
+            dense = all(map(_IS_CONTIGUOUS, grads))
+        except TypeError:                 # a None among them
             at = [i for i, g in enumerate(grads) if g is not None]
             params, grads = [params[i] for i in at], [grads[i] for i in at]
-        n = len(grads)
-        keep = None
-        if not all(map(torch.Tensor.is_contiguous, grads)):
+            dense = all(map(_IS_CONTIGUOUS, grads))
+        if not dense:
             keep = grads = [g.contiguous() for g in grads]
+        n = len(grads)
         rates = [(float(g["lr"]), float(g["weight_decay"])) for g in self.param_groups]
-        if n != len(self._params) or not self._whole or rates != self._rates:
-            table["numel"][:n] = [self._sizes[i] for i in at]
-            table["state_offset"][:n] = [self.offsets[i] for i in at]
-            table["lr"][:n] = [rates[self._group_of[i]][0] for i in at]
-            table["weight_decay"][:n] = [rates[self._group_of[i]][1] for i in at]
-            self._whole, self._rates = n == len(self._params), rates
-        table["param"][:n] = list(map(torch.Tensor.data_ptr, params))
-        table["grad"][:n] = list(map(torch.Tensor.data_ptr, grads))
+        if at is not None or not self._whole or rates != self._rates:
+            which = range(n) if at is None else at
+            table["numel"][:n] = [self._sizes[i] for i in which]
+            table["state_offset"][:n] = [self.offsets[i] for i in which]
+            table["lr"][:n] = [rates[self._group_of[i]][0] for i in which]
+            table["weight_decay"][:n] = [rates[self._group_of[i]][1] for i in which]
+            self._whole, self._rates = at is None, rates
+        table["param"][:n] = list(map(_DATA_PTR, params))
+        table["grad"][:n] = list(map(_DATA_PTR, grads))
         return n, keep
 
     def step(self, closure=None):
@@ -146,7 +154,7 @@ class AdamW(torch.optim.Optimizer):
     def _launch(self, betas, eps):
         n, keep = self._fill()
         self.steps += 1
-        clip, table = None, self._table.ctypes.data
+        clip, table = None, self._table_address
         if self.max_norm is not None:
             clip = self.grad_norm
             B.osdp_grad_norm(table, n, self._dtype, self.max_norm, clip, self._ws, check=True)
