@@ -655,7 +655,8 @@ int launch_gemm(const GemmCall &c, cudaStream_t stream) {
 
   GemmParams &p = slot.p;
   memset(&p, 0, sizeof(p));
-  rc = make_operand_maps(c.a, true, c.mode, c.L, c.k_total, BM, &p.a_main, &p.a_tail, &p.a_sc_mul, eb);
+  p.a_rows = (c.i8 && !pair && c.P < BM) ? (int)cdiv(c.P, 8) * 8 : BM;
+  rc = make_operand_maps(c.a, true, c.mode, c.L, c.k_total, p.a_rows, &p.a_main, &p.a_tail, &p.a_sc_mul, eb);
   if (rc) return rc;
   rc = make_operand_maps(c.b, false, c.mode, c.L, c.k_total, pair ? 128 : bn, &p.b_main, &p.b_tail, &p.b_sc_mul, eb);
   if (rc) return rc;

@@ -91,6 +91,7 @@ struct GemmParams {
   int carry_bf16;            // MODE_RED: the running sum is kept in `out` itself, in bf16 (no fp32 carry buffer)
   int tma_epilogue;          // 1: outputs leave through shared-memory staging + TMA; 0: direct stores
   int bk;                    // reduction elements per k-block: 128 / (bytes per operand element)
+  int a_rows;                // int8: rows of A's box (BM, or the matrix's own, rounded up to 8, where it has fewer)
   Epilogue epi;
   int *status;               // device status word or null
 };
@@ -785,6 +786,9 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
     // ------------------------------------------------------------------ TMA producer(s)
     const bool load_a = (warp == 0);
     const bool load_b = SPLIT_PRODUCER ? (warp == 3) : true;
+    // int8 with few rows of A: a copy takes its time for every row of its box, in the matrix or not, so the box is only as
+    // high as the matrix (the tile's other rows hold whatever was there; nothing of them is stored).
+    const uint32_t stage_tx = (I8 && !CTA2) ? (uint32_t)p.a_rows * 128u + SL::B_BYTES : SL::STAGE_BYTES;
     int grp = 0, sub = 0, n_sub = 0;       // round of the ring being filled, k-block inside it, k-blocks it will hold
     uint32_t phase = 0;
     uint32_t armed = 0, armed_phase = 0;   // per-round bookkeeping for the unwind path
@@ -808,7 +812,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
           if (!ok) break;
           n_sub = min(unit, tile_left);
           if (lane == 0 && load_a && (!CTA2 || rank == 0))
-            mbar_expect_tx(full_bar(grp), (uint32_t)n_sub * SL::STAGE_BYTES * (CTA2 ? 2 : 1));
+            mbar_expect_tx(full_bar(grp), (uint32_t)n_sub * stage_tx * (CTA2 ? 2 : 1));
           armed |= 1u << grp;
           armed_phase = (armed_phase & ~(1u << grp)) | (phase << grp);
         }
