@@ -350,22 +350,23 @@ struct Team {
       __syncwarp();
     }
   }
-  // The exchanged sums, added over the warps that share the row: lane l takes the warps l, l + 32, ... (block by block;
-  // `add` is given their sums and their number in count order) and the lanes' totals are added by shuffles.  A loop
-  // over the warps in every lane instead is a chain of up to 16 CL shared-memory reads per row.
+  // The exchanged sums, added over the warps that share the row (`add` is given a warp's sums and its number in count
+  // order).  Up to four warps: every lane reads them all.  More: lane l takes the warps l, l + 32, ... (block by block)
+  // and the lanes' totals are added by shuffles, where a loop would be a chain of up to 16 CL reads per row.
   template <int N, typename F>
   __device__ __forceinline__ void total(const float *buf, float (&t)[N], F add) const {
 #pragma unroll
     for (int k = 0; k < N; ++k) t[k] = 0.f;
+    if (CL == 1 && warps <= 4) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        if (w < warps) add(t, buf + (first_warp + w) * NS, w);
+      return;
+    }
 #pragma unroll
     for (int p = 0; p < (CL + 1) / 2; ++p) {
       const int slot = lane + 32 * p, b = slot >> 4, w = slot & 15;
       if (b < CL && w < warps) add(t, buf + (b * 16 + first_warp + w) * NS, b * 16 + w);
-    }
-    if (warps == 1 && CL == 1) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) t[k] = __shfl_sync(0xFFFFFFFFu, t[k], 0);
-      return;
     }
     int idx;
     const float s = warp_sum_scattered<N>(t, lane, idx);
@@ -768,11 +769,15 @@ __global__ void __launch_bounds__(32 * bwd_warps(LAYER), 1) block_norm_bwd_kerne
   float c1 = 0.f, c2 = 0.f, m1 = 0.f, m2 = 0.f;    // of row i - 1
   const f2 alpha = both(a.alpha);
   for (int s = 0; s + 1 < sh.stages; ++s) fetch(s);
+  // a row's statistics are read a step before they are used
+  const bool has_stats = FULL || a.stats;
+  float4 next_st = (has_stats && n > 0) ? __ldg(a.stats + first) : make_float4(0.f, 0.f, 0.f, 0.f);
   int st_a = 0, st_b = sh.stages - 1;     // ring stages of row i and of row i - 1 (then refilled)
   long long at = first * a.D - row_step;  // first channel of row i - 1
   for (long long i = 0; i <= n_steps; ++i, at += row_step) {
     if (i < n) {
-      const float4 st = (FULL || a.stats) ? __ldg(a.stats + first + i * step) : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float4 st = next_st;
+      if (has_stats && i + 1 < n) next_st = __ldg(a.stats + first + (i + 1) * step);
       if (has_post) {
         ip[0] = st.y;
         mp[0] = st.x;
