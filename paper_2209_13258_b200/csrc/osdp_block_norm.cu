@@ -1005,25 +1005,42 @@ int launch_rows(const Args &a, int max_warps, int pieces, int red_bytes, int w_b
   }
   if (sh.teams == 0) return OSDP_ERR_UNSUPPORTED;
   if (sh.stages > MAX_STAGES) sh.stages = MAX_STAGES;
-  const int threads = sh.warps * sh.teams * 32;
+  const int threads = sh.warps * sh.teams * 32, smem = fixed + sh.stages * stage;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return report_cuda(e);
+  static std::atomic<int> most[64];      // clusters that run at the same time (blocks, without clusters); 0: not known yet
+  static std::mutex setup;
+  int cap = most[dev & 63].load(std::memory_order_acquire);
+  if (cap == 0) {
+    std::lock_guard<std::mutex> lock(setup);
+    e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
+    if (e != cudaSuccess) return report_cuda(e);
+    cap = sms;
+    if (CL > 1) {   // fewer than sms / CL: a cluster does not cross the chip's groups of SMs
+      cudaLaunchConfig_t q = {};
+      q.gridDim = dim3((unsigned)(sms / CL * CL));
+      q.blockDim = dim3(32 * max_warps);
+      q.dynamicSmemBytes = SMEM_MAX;
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = CL;
+      attr[0].val.clusterDim.y = 1;
+      attr[0].val.clusterDim.z = 1;
+      q.attrs = attr;
+      q.numAttrs = 1;
+      e = cudaOccupancyMaxActiveClusters(&cap, KERNEL, &q);
+      if (e != cudaSuccess) return report_cuda(e);
+      if (cap < 1) return report_cuda(cudaErrorLaunchOutOfResources);
+    }
+    most[dev & 63].store(cap, std::memory_order_release);
+  }
   int64_t n = cdiv(a.M, sh.teams);
-  const int cap = sms / CL;
   if (n > cap) n = cap;
   if (n > ROW_MAX_BLOCKS) n = ROW_MAX_BLOCKS;
   if (n < 1) n = 1;    // no rows: the backward writes zeros
   if (units) *units = (int)n;
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return report_cuda(e);
-  static std::atomic<bool> ready[64];
-  static std::mutex setup;
-  if (!ready[dev & 63].load(std::memory_order_acquire)) {
-    std::lock_guard<std::mutex> lock(setup);
-    e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_MAX);
-    if (e != cudaSuccess) return report_cuda(e);
-    ready[dev & 63].store(true, std::memory_order_release);
-  }
-  return launch_overlapped(KERNEL, dim3((unsigned)(CL * n)), dim3(threads), fixed + sh.stages * stage, CL, stream, a, sh);
+  return launch_overlapped(KERNEL, dim3((unsigned)(CL * n)), dim3(threads), smem, CL, stream, a, sh);
 }
 
 // The smallest cluster that the rows fit.
