@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(V == 4 ? 512 : 1024) block_norm_fwd_kernel(con
 
 // Threads of a block: what the registers allow without spills (spilled values come back from L2, there is hardly any L1
 // beside the ring: the layer norm's backward took 1.5 times as long with 512 threads of 128 registers).
-constexpr int FWD_WARPS = 16;
+constexpr int fwd_warps(bool layer, bool fp32, int cl) { return layer && fp32 && cl > 1 ? 12 : 16; }
 constexpr int bwd_warps(bool layer) { return layer ? 12 : 16; }
 constexpr int MAX_STAGES = 6;
 constexpr int ROW_MAX_BLOCKS = 160;   // partial sums over rows that the workspace holds
@@ -340,9 +340,13 @@ struct Team {
         asm volatile("{\n\t.reg .b32 ra;\n\tmapa.shared::cluster.u32 ra, %0, %1;\n\tst.shared::cluster.f32 [ra], %2;\n\t}" ::"r"(local), "r"((rank + q) % CL), "f"(s) : "memory");
     }
   }
-  __device__ __forceinline__ void barrier() const {
-    if (CL > 1) {   // the teams of a cluster go through it together
-      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  // The exchange's barrier in two halves.  Across a cluster the first half comes right after publish(): as a release it
+  // waits for the global stores before it to be acknowledged, so a step's own stores go between the halves.
+  __device__ __forceinline__ void arrive() const {
+    if (CL > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // the teams of a cluster go through it together
+  }
+  __device__ __forceinline__ void wait() const {
+    if (CL > 1) {
       asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     } else if (warps > 1) {
       asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(TL) : "memory");
@@ -388,10 +392,12 @@ struct Team {
 // LAYER: either norm subtracts a mean.  FULL: y, both norms, r and u are there (the form between two blocks); without
 // it each may be absent, which costs branches.
 template <typename RT, bool LAYER, int CL, bool FULL>
-__global__ void __launch_bounds__(32 * FWD_WARPS, 1) block_norm_fwd_rows_kernel(const __grid_constant__ FwdArgs a, const TeamShape sh) {
+__global__ void __launch_bounds__(32 * fwd_warps(LAYER, sizeof(RT) == 4, CL), 1) block_norm_fwd_rows_kernel(const __grid_constant__ FwdArgs a, const TeamShape sh) {
   constexpr int RP = sizeof(RT) / 2;             // 16-byte pieces of a residual vector
   constexpr int PIECES = 1 + RP;                 // y, x
   constexpr int NS = LAYER ? 4 : 2;              // y's, r's: mean and squared distances, or squares alone
+  constexpr bool LATE = CL > 1;                  // a step's stores go between the halves of the barrier (Team::arrive); within
+                                                 // one block they are better early (16384 x 8192 RMS: 173 against 197 us)
   extern __shared__ __align__(16) uint8_t smem[];
   Team<CL, NS> tm;
   tm.init(sh, a.D, reinterpret_cast<float *>(smem));
@@ -447,7 +453,10 @@ __global__ void __launch_bounds__(32 * FWD_WARPS, 1) block_norm_fwd_rows_kernel(
     }
   }
   if (LAYER) __syncthreads();
-  if (CL > 1) tm.barrier();   // the other blocks run before anything is written to their shared memory
+  if (CL > 1) {   // the other blocks run before anything is written to their shared memory
+    tm.arrive();
+    tm.wait();
+  }
 
   const long long first = (long long)tm.unit * sh.teams + tm.team, step = (long long)tm.units * sh.teams;
   const long long n = first < a.M ? (a.M - first + step - 1) / step : 0;
@@ -488,13 +497,19 @@ __global__ void __launch_bounds__(32 * FWD_WARPS, 1) block_norm_fwd_rows_kernel(
   int st_a = 0, st_b = sh.stages - 1;     // ring stages of row i (its y) and of row i - 1 (then refilled)
   long long at = first * a.D - 2 * row_step;   // first channel of row i - 2
   for (long long i = 0; i < n_steps + 2; ++i, at += row_step) {
+    uint4 u_out[LATE ? 2 : 1];
+    float4 st_out;
+    auto store_u = [&](int j, const uint4 &u) { *reinterpret_cast<uint4 *>(static_cast<__nv_bfloat16 *>(a.u) + at + col[j]) = u; };
+    auto store_stats = [&](const float4 &st) {
+      if (a.stats && tm.tl == 0 && tm.rank == 0) a.stats[first + (i - 2) * step] = st;
+    };
     if (i >= 2 && i < n + 2) {
-      // ---- row i - 2: u
+      // ---- row i - 2: u (stored below)
       if (pre) {
         const f2 shift = both(-mean_r), scale = both(rstd_r);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          if (!act[j]) continue;
+          if (!LATE && !act[j]) continue;
           f2 u[4], bp[4];
           if (LAYER) join4(my_bias[(4 + j * 2) * 32], my_bias[(5 + j * 2) * 32], bp);
 #pragma unroll
@@ -502,11 +517,13 @@ __global__ void __launch_bounds__(32 * FWD_WARPS, 1) block_norm_fwd_rows_kernel(
             const f2 h = mul2(LAYER ? add2(r[j][k], shift) : r[j][k], scale);
             u[k] = LAYER ? fma2(h, wp[j][k], bp[k]) : mul2(h, wp[j][k]);
           }
-          store4(static_cast<__nv_bfloat16 *>(a.u) + at + col[j], u);
+          if (LATE) u_out[LATE ? j : 0] = narrow4(u);
+          else store_u(j, narrow4(u));
         }
       }
-      if (a.stats && tm.tl == 0 && tm.rank == 0)
-        a.stats[first + (i - 2) * step] = make_float4(shown_mean_y, shown_rstd_y, pre ? mean_r : 0.f, pre ? rstd_r : 0.f);
+      const float4 st = make_float4(shown_mean_y, shown_rstd_y, pre ? mean_r : 0.f, pre ? rstd_r : 0.f);
+      if (LATE) st_out = st;
+      else store_stats(st);
     }
     f2 part_y = zero, part_r = zero;
     if (i >= 1 && i <= n) {
@@ -536,7 +553,7 @@ __global__ void __launch_bounds__(32 * FWD_WARPS, 1) block_norm_fwd_rows_kernel(
 #pragma unroll
           for (int k = 0; k < 4; ++k) r[j][k] = mul2(alpha, x[k]);
         }
-        if (has_r) store4(static_cast<RT *>(a.r) + (at + row_step) + col[j], r[j]);
+        if (!LATE && has_r) store4(static_cast<RT *>(a.r) + (at + row_step) + col[j], r[j]);
 #pragma unroll
         for (int k = 0; k < 4; ++k) part_r = LAYER ? add2(part_r, r[j][k]) : fma2(r[j][k], r[j][k], part_r);
       }
@@ -559,9 +576,12 @@ __global__ void __launch_bounds__(32 * FWD_WARPS, 1) block_norm_fwd_rows_kernel(
         }
       }
     }
-    fetch(st_b);     // row i - 1 has been read for the last time
-    st_b = st_a;
-    if (++st_a == sh.stages) st_a = 0;
+    auto refill = [&]() {
+      fetch(st_b);     // row i - 1 has been read for the last time
+      st_b = st_a;
+      if (++st_a == sh.stages) st_a = 0;
+    };
+    if (!LATE) refill();
     float two[2] = {sum2(part_y), sum2(part_r)};
     int idx;
     float s = warp_sum_scattered<2>(two, tm.lane, idx);
@@ -587,9 +607,23 @@ __global__ void __launch_bounds__(32 * FWD_WARPS, 1) block_norm_fwd_rows_kernel(
     } else {
       tm.publish(s, idx, (tm.lane & 15) == 0);
     }
+    tm.arrive();
+    // what this step writes and fetches late, while the sums are exchanged
+    if (LATE && i >= 2 && i < n + 2) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (pre && act[j]) store_u(j, u_out[LATE ? j : 0]);
+      store_stats(st_out);
+    }
+    if (LATE && has_r && i >= 1 && i <= n) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        if (act[j]) store4(static_cast<RT *>(a.r) + (at + row_step) + col[j], r[j]);
+    }
+    if (LATE) refill();
     const float *buf = tm.buffer();
     tm.turn ^= 1;
-    tm.barrier();
+    tm.wait();
     float v[2];
     if (LAYER) {
       float m[2];
@@ -697,7 +731,10 @@ __global__ void __launch_bounds__(32 * bwd_warps(LAYER), 1) block_norm_bwd_kerne
     }
   }
   if (!WREG) __syncthreads();
-  if (CL > 1) tm.barrier();   // the other blocks run before anything is written to their shared memory
+  if (CL > 1) {   // the other blocks run before anything is written to their shared memory
+    tm.arrive();
+    tm.wait();
+  }
   auto weights = [&](int j, f2 (&q)[4], f2 (&w)[4]) {
     if (WREG) {
 #pragma unroll
@@ -828,6 +865,7 @@ __global__ void __launch_bounds__(32 * bwd_warps(LAYER), 1) block_norm_bwd_kerne
       const float mine = warp_sum_scattered<NS>(s, tm.lane, idx);
       tm.publish(mine, idx, (tm.lane & (32 / NS - 1)) == 0);
     }
+    if (i < n_steps) tm.arrive();
     if (i > 0 && i <= n) {
       const f2 ir2 = both(ir[1]), ip2 = both(ip[1]), nmr = both(-mr[1]), nmp = both(-mp[1]);
       const f2 k1 = both(-ir[1] * c1), k2 = both(-ir[1] * c2), g2 = both(-ip[1] * m2), g1 = both(-ip[1] * m1);
@@ -864,7 +902,7 @@ __global__ void __launch_bounds__(32 * bwd_warps(LAYER), 1) block_norm_bwd_kerne
     if (i == n_steps) break;
     const float *buf = tm.buffer();
     tm.turn ^= 1;
-    tm.barrier();
+    tm.wait();
     float s[NS];
     tm.template total<NS>(buf, s, [&](float (&t)[NS], const float *f, int) {
 #pragma unroll
@@ -1048,9 +1086,9 @@ template <typename RT, bool LAYER, int CL = 1>
 int launch_fwd_rows(const FwdArgs &a, int sms, cudaStream_t stream) {
   const int pieces = 1 + (int)sizeof(RT) / 2, red = (Team<CL, LAYER ? 4 : 2>::RED_FLOATS + CL * 16) * 4, w = LAYER ? 128 : 0;
   const bool full = a.y && a.r && a.post.has && a.pre.has;
-  const int rc = full ? launch_rows<CL, block_norm_fwd_rows_kernel<RT, LAYER, CL, true>>(a, FWD_WARPS, pieces, red, w, sms, nullptr, stream)
-                      : launch_rows<CL, block_norm_fwd_rows_kernel<RT, LAYER, CL, false>>(a, FWD_WARPS, pieces, red, w, sms, nullptr, stream);
-  if constexpr (CL < 2) {
+  const int rc = full ? launch_rows<CL, block_norm_fwd_rows_kernel<RT, LAYER, CL, true>>(a, fwd_warps(LAYER, sizeof(RT) == 4, CL), pieces, red, w, sms, nullptr, stream)
+                      : launch_rows<CL, block_norm_fwd_rows_kernel<RT, LAYER, CL, false>>(a, fwd_warps(LAYER, sizeof(RT) == 4, CL), pieces, red, w, sms, nullptr, stream);
+  if constexpr (CL < 4) {
     if (rc == OSDP_ERR_UNSUPPORTED) return launch_fwd_rows<RT, LAYER, 2 * CL>(a, sms, stream);
   }
   return rc;
