@@ -387,8 +387,8 @@ struct Team {
 // ------------------------------------------------------------------------------------------------ forward, many rows
 
 // A step finishes row i (u), does row i + 1 up to its sums (r) and takes the sums of row i + 2's y.  The variance is
-// taken per warp about the warp's own mean and the warps' means and variances are merged, which is as safe as a second
-// pass over the row and needs no second exchange.
+// taken per lane about the lane's own mean; lanes' and then warps' means and squared distances are merged, which is as
+// safe as a second pass over the row and needs no second exchange.
 // LAYER: either norm subtracts a mean.  FULL: y, both norms, r and u are there (the form between two blocks); without
 // it each may be absent, which costs branches.
 template <typename RT, bool LAYER, int CL, bool FULL>
@@ -484,7 +484,9 @@ __global__ void __launch_bounds__(32 * fwd_warps(LAYER, sizeof(RT) == 4, CL), 1)
   const float inv_d = 1.0f / (float)a.D;
   const float my_channels = LAYER ? count[tm.rank * 16 + tm.warp - tm.first_warp] : 0.f;
   const float my_inv = my_channels > 0.f ? 1.0f / my_channels : 0.f;
-  const float y_mean = (LAYER && post && a.post.layer) ? my_inv : 0.f, r_mean = (LAYER && pre && a.pre.layer) ? my_inv : 0.f;
+  // (an RMS norm beside a layer norm: means of zero)
+  const float lane_channels = (float)(8 * ((int)act[0] + (int)act[1])), lane_inv = act[0] ? 1.0f / lane_channels : 0.f;
+  const float y_inv = (post && a.post.layer) ? lane_inv : 0.f, r_inv = (pre && a.pre.layer) ? lane_inv : 0.f;
   const f2 alpha = both(a.alpha), zero = both(0.f);
   f2 r[2][4];
 #pragma unroll
@@ -582,12 +584,13 @@ __global__ void __launch_bounds__(32 * fwd_warps(LAYER, sizeof(RT) == 4, CL), 1)
       if (++st_a == sh.stages) st_a = 0;
     };
     if (!LATE) refill();
-    float two[2] = {sum2(part_y), sum2(part_r)};
     int idx;
-    float s = warp_sum_scattered<2>(two, tm.lane, idx);
     if (LAYER) {
-      const float my = __shfl_sync(0xFFFFFFFFu, s, 0) * y_mean, mr = __shfl_sync(0xFFFFFFFFu, s, 16) * r_mean;
-      const f2 sy = both(-my), sr = both(-mr);
+      // A lane's own mean and squared distances from it; the warp's from the lanes', with the lanes' means taken relative to
+      // lane 0's: the differences are of the size of the deviation, so nothing cancels that matters (at worst, when lane 0
+      // holds all of the variance, its share of the channels: 16 of 512), and one round of shuffles does it.
+      const float ly = sum2(part_y) * y_inv, lr = sum2(part_r) * r_inv;
+      const f2 sy = both(-ly), sr = both(-lr);
       f2 dy = zero, dr = zero;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
@@ -599,12 +602,14 @@ __global__ void __launch_bounds__(32 * fwd_warps(LAYER, sizeof(RT) == 4, CL), 1)
           dr = fma2(er, er, dr);
         }
       }
-      float d[2] = {sum2(dy), sum2(dr)};
-      s = warp_sum_scattered<2>(d, tm.lane, idx);
-      // lanes 0 and 16 bring the squared distances, 1 and 17 the means
-      const bool mean_lane = (tm.lane & 1) != 0;
-      tm.publish(mean_lane ? (idx ? mr : my) : s, 2 * idx + (mean_lane ? 0 : 1), (tm.lane & 14) == 0);
+      const float cy = __shfl_sync(0xFFFFFFFFu, ly, 0), cr = __shfl_sync(0xFFFFFFFFu, lr, 0);
+      const float ny = lane_channels * (ly - cy), nr = lane_channels * (lr - cr);
+      float four[4] = {ny, fmaf(ny, ly - cy, sum2(dy)), nr, fmaf(nr, lr - cr, sum2(dr))};
+      const float s = warp_sum_scattered<4>(four, tm.lane, idx), other = __shfl_xor_sync(0xFFFFFFFFu, s, 8);
+      tm.publish((idx & 1) ? fmaf(-other * my_inv, other, s) : fmaf(s, my_inv, (idx & 2) ? cr : cy), idx, (tm.lane & 7) == 0);
     } else {
+      float two[2] = {sum2(part_y), sum2(part_r)};
+      const float s = warp_sum_scattered<2>(two, tm.lane, idx);
       tm.publish(s, idx, (tm.lane & 15) == 0);
     }
     tm.arrive();
