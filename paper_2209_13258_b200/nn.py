@@ -339,7 +339,7 @@ class _ResidualNormFn(torch.autograd.Function):
         dw_post, db_post, dgate = vec(need[2] and has_y), vec(need[3] and has_y), vec(need[4] and has_y)
         dw_pre, db_pre = vec(need[5] and pre), vec(need[6] and pre)
         B.osdp_block_norm_bwd(dr, du, y, r, stats, M, D, layer.resid_dtype, ctx.post, w_post, b_post, gate, layer.alpha, layer.beta,
-                              pre, w_pre if pre else None, dx, dy, dw_post, db_post, dgate, dw_pre, db_pre, layer._workspace(M), check=True)
+                              pre, w_pre if pre else None, dx, dy, dw_post, db_post, dgate, dw_pre, db_pre, layer._workspace(M, dev), check=True)
         return (dx.view(ctx.shape) if dx is not None else None, dy.view(ctx.shape) if dy is not None else None, dw_post, db_post,
                 dgate, dw_pre, db_pre, None)
 
@@ -381,12 +381,11 @@ class ResidualNorm(torch.nn.Module):
         self.gate = vec(gate, gate_init)
         self._ws = None
 
-    def _workspace(self, M):
-        rc, need = B.osdp_block_norm_workspace_bytes(M, self.hidden)
-        if rc:
-            raise B.OsdpError(rc, "osdp_block_norm_workspace_bytes")
-        dev = next(self.parameters()).device
-        if self._ws is None or self._ws.device != dev:
+    def _workspace(self, M, dev):
+        if self._ws is None or self._ws.device != dev:       # its size does not depend on M
+            rc, need = B.osdp_block_norm_workspace_bytes(M, self.hidden)
+            if rc:
+                raise B.OsdpError(rc, "osdp_block_norm_workspace_bytes")
             self._ws = B.new_workspace(need, device=dev)
         return self._ws
 

@@ -27,13 +27,15 @@ class AdamW(torch.optim.Optimizer):
     master       bf16 parameters only: the step works on fp32 copies of the parameters (4 bytes each) and writes their
                  rounding.  Without it an update below half a unit in the last place of a bf16 parameter is lost.
     max_norm     clips the gradients by their global norm over all parameters of the step, without a host round trip.
-                 A step whose norm is not finite changes nothing (``grad_norm[0]`` says so).
+                 A step whose norm is not finite changes no parameter and no state (``grad_norm[0]`` says so); it counts as
+                 a step all the same, since the host does not wait to learn of it.
 
     All parameter groups are stepped together: ``lr`` and ``weight_decay`` may differ between groups, ``betas`` and
     ``eps`` may not.  Parameters whose ``.grad`` is None are left alone.  ``steps`` counts the steps done (one count for
     all parameters: it sets the bias correction).  States are flat over all parameters, each parameter's part starting
     at a multiple of 256 elements (``offsets``): ``exp_avg``, ``exp_avg_sq`` (with "e4m3" the codes of the second
-    moment's root), ``exp_avg_scale``, ``exp_avg_sq_scale``, ``master``.  ``grad_norm`` [2]: the last step's norm and
+    moment's root), ``exp_avg_scale``, ``exp_avg_sq_scale``, ``master``.  A CUDA graph of a step replays that step's
+    bias correction, rates and gradients' addresses.  ``grad_norm`` [2]: the last step's norm and
     coefficient, on the device.
     """
 
@@ -82,7 +84,6 @@ class AdamW(torch.optim.Optimizer):
         self._sizes = [p.numel() for p in self._params]
         self._group_of = [i for i, g in enumerate(self.param_groups) for _ in g["params"]]
         self._table = np.zeros(n, dtype=_TENSOR)
-        self._table_address = self._table.ctypes.data
         self._whole, self._rates = False, None
         self._ws = B.new_workspace(B.osdp_grad_norm_workspace_bytes(n)[1], device=dev)
         self._built = True
@@ -101,13 +102,10 @@ class AdamW(torch.optim.Optimizer):
             if p.dtype is not dtype:
                 raise TypeError("a parameter's dtype has changed since the optimiser was built")
         grads, at, keep = list(map(_GRAD, params)), None, None
-        try:
-            dense = all(map(_IS_CONTIGUOUS, grads))
-        except TypeError:                 # a None among them
+        if type(None) in set(map(type, grads)):
             at = [i for i, g in enumerate(grads) if g is not None]
             params, grads = [params[i] for i in at], [grads[i] for i in at]
-            dense = all(map(_IS_CONTIGUOUS, grads))
-        if not dense:
+        if not all(map(_IS_CONTIGUOUS, grads)):
             keep = grads = [g.contiguous() for g in grads]
         n = len(grads)
         rates = [(float(g["lr"]), float(g["weight_decay"])) for g in self.param_groups]
@@ -154,7 +152,7 @@ class AdamW(torch.optim.Optimizer):
     def _launch(self, betas, eps):
         n, keep = self._fill()
         self.steps += 1
-        clip, table = None, self._table_address
+        clip, table = None, self._table.__array_interface__["data"][0]
         if self.max_norm is not None:
             clip = self.grad_norm
             B.osdp_grad_norm(table, n, self._dtype, self.max_norm, clip, self._ws, check=True)
