@@ -159,6 +159,9 @@ class AdamW(torch.optim.Optimizer):
         B.osdp_adamw_step(table, n, self._dtype, self._state_dtype, self.master, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale,
                           self.exp_avg_sq_scale, betas[0], betas[1], eps, self.steps, clip, check=True)
 
+    def __getstate__(self):
+        raise TypeError("an AdamW is copied or saved through state_dict()")     # torch's copy would leave the flat states out
+
     def state_dict(self):
         d = super().state_dict()
         d["flat"] = {k: getattr(self, k) for k in ("exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale", "master")}
