@@ -63,6 +63,8 @@ struct Hyper {
   float root_scale;    // 1 / sqrt(1 - b2^t)
 };
 
+__device__ __forceinline__ bool has_zero_byte(uint32_t w) { return ((w - 0x01010101u) & ~w & 0x80808080u) != 0u; }
+
 // 256 elements -> codes and their scale.  ROOT: the elements are not negative, those above zero keep at least the
 // smallest code.
 template <bool ROOT>
@@ -79,18 +81,21 @@ __device__ __forceinline__ void quantise_block(const f2 (&x)[4], uint8_t *codes,
   const f2 inv2 = both(inv);
   f2 c[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    c[j] = mul2(x[j], inv2);
-    if (ROOT) {
+  for (int j = 0; j < 4; ++j) c[j] = mul2(x[j], inv2);
+  uint2 q = encode_e4m3x8(c);
+  if (ROOT && (has_zero_byte(q.x) || has_zero_byte(q.y))) {   // rare: an element that is zero, or very small in its block
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
       const float2 v = split2(x[j]);
-      float2 q = split2(c[j]);
+      float2 l = split2(c[j]);
       constexpr float least = 0.001953125f;   // 2^-9, the smallest e4m3 value
-      q.x = (live && v.x > 0.f) ? fmaxf(q.x, least) : q.x;
-      q.y = (live && v.y > 0.f) ? fmaxf(q.y, least) : q.y;
-      c[j] = pack2(q.x, q.y);
+      if (live && v.x > 0.f) l.x = fmaxf(l.x, least);
+      if (live && v.y > 0.f) l.y = fmaxf(l.y, least);
+      c[j] = pack2(l.x, l.y);
     }
+    q = encode_e4m3x8(c);
   }
-  *reinterpret_cast<uint2 *>(codes + lane * 8) = encode_e4m3x8(c);
+  *reinterpret_cast<uint2 *>(codes + lane * 8) = q;
   if (lane == 0) *scale = live ? top * (1.0f / 448.0f) : 0.0f;
 }
 
@@ -160,8 +165,9 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
   T *param = static_cast<T *>(e.param);
   const T *grad = static_cast<const T *>(e.grad);
   using W = typename std::conditional<MASTER, float, T>::type;
-  const f2 b1 = both(h.b1), n1 = both(h.one_minus_b1 * coef), b2 = both(h.b2), n2 = both(h.one_minus_b2), eps = both(h.eps),
-           root_scale = both(h.root_scale), decay = both(e.decay), size = both(-e.size), coef2 = both(coef);
+  // the clipping coefficient is folded into the factors of g and g^2
+  const f2 b1 = both(h.b1), n1 = both(h.one_minus_b1 * coef), b2 = both(h.b2), n2 = both(h.one_minus_b2 * coef * coef), eps = both(h.eps),
+           root_scale = both(h.root_scale), decay = both(e.decay), size = both(-e.size);
 #pragma unroll 1
   for (int it = 0; it < PER_WARP; it += BLOCKS) {
     Raw8<T> rg[BLOCKS];
@@ -223,8 +229,7 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         m[j] = fma2(n1, g[j], mul2(m[j], b1));
-        const f2 gc = mul2(g[j], coef2);
-        v[j] = fma2(mul2(gc, n2), gc, mul2(v[j], b2));
+        v[j] = fma2(mul2(g[j], n2), g[j], mul2(v[j], b2));
         const float2 s = split2(v[j]);
         root[j] = pack2(fast_sqrt(s.x), fast_sqrt(s.y));
         const float2 d = split2(fma2(root[j], root_scale, eps));
