@@ -415,11 +415,39 @@ __global__ void __launch_bounds__(32 * fwd_warps(LAYER, sizeof(RT) == 4, CL), 1)
   const bool has_y = FULL || a.y != nullptr, post = FULL || (has_y && a.post.has), pre = FULL || a.pre.has, has_r = FULL || a.r != nullptr;
   int col[2];
   bool act[2];
-  f2 qw[2][4], wp[2][4];   // r = alpha x + qw h + qb, u = wp h + bp
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     col[j] = tm.c_begin + (j * tm.TL + tm.tl) * 8;
     act[j] = col[j] < tm.c_end;
+  }
+  const long long first = (long long)tm.unit * sh.teams + tm.team, step = (long long)tm.units * sh.teams;
+  const long long n = first < a.M ? (a.M - first + step - 1) / step : 0;
+  // the teams of a cluster meet at its barrier: all do as many steps as its first team, which has the most rows
+  const long long n_steps = CL == 1 ? n : (a.M - (first - tm.team) + step - 1) / step;
+  auto slot = [](int stage, int j, int piece) { return stage * STAGE + (j * PIECES + piece) * 512; };
+  const long long row_step = step * a.D;
+  long long f_at = first * a.D;                  // first channel of the row that is fetched next
+  long long f_row = 0;
+  auto fetch = [&](int stage) {
+    if (f_row < n) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (!act[j]) continue;
+        if (has_y) cp_async16(ring_u32 + slot(stage, j, 0), a.y + f_at + col[j]);
+#pragma unroll
+        for (int p = 0; p < RP; ++p)
+          cp_async16(ring_u32 + slot(stage, j, 1 + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.x) + f_at + col[j]) + 16 * p);
+      }
+    }
+    ++f_row;
+    f_at += row_step;
+    cp_async_commit();
+  };
+  for (int s = 0; s + 1 < sh.stages; ++s) fetch(s);   // the weights come while the first rows are on their way
+
+  f2 qw[2][4], wp[2][4];   // r = alpha x + qw h + qb, u = wp h + bp
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
     float q[8], b[8], w[8], c[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) q[k] = b[k] = w[k] = c[k] = 0.f;
@@ -458,29 +486,6 @@ __global__ void __launch_bounds__(32 * fwd_warps(LAYER, sizeof(RT) == 4, CL), 1)
     tm.wait();
   }
 
-  const long long first = (long long)tm.unit * sh.teams + tm.team, step = (long long)tm.units * sh.teams;
-  const long long n = first < a.M ? (a.M - first + step - 1) / step : 0;
-  // the teams of a cluster meet at its barrier: all do as many steps as its first team, which has the most rows
-  const long long n_steps = CL == 1 ? n : (a.M - (first - tm.team) + step - 1) / step;
-  auto slot = [](int stage, int j, int piece) { return stage * STAGE + (j * PIECES + piece) * 512; };
-  const long long row_step = step * a.D;
-  long long f_at = first * a.D;                  // first channel of the row that is fetched next
-  long long f_row = 0;
-  auto fetch = [&](int stage) {
-    if (f_row < n) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        if (!act[j]) continue;
-        if (has_y) cp_async16(ring_u32 + slot(stage, j, 0), a.y + f_at + col[j]);
-#pragma unroll
-        for (int p = 0; p < RP; ++p)
-          cp_async16(ring_u32 + slot(stage, j, 1 + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.x) + f_at + col[j]) + 16 * p);
-      }
-    }
-    ++f_row;
-    f_at += row_step;
-    cp_async_commit();
-  };
   const float inv_d = 1.0f / (float)a.D;
   const float my_channels = LAYER ? count[tm.rank * 16 + tm.warp - tm.first_warp] : 0.f;
   const float my_inv = my_channels > 0.f ? 1.0f / my_channels : 0.f;
@@ -495,7 +500,6 @@ __global__ void __launch_bounds__(32 * fwd_warps(LAYER, sizeof(RT) == 4, CL), 1)
     for (int k = 0; k < 4; ++k) r[j][k] = zero;
   float mean_y = 0.f, rstd_y = 1.f, mean_r = 0.f, rstd_r = 0.f, shown_mean_y = 0.f, shown_rstd_y = 0.f;
 
-  for (int s = 0; s + 1 < sh.stages; ++s) fetch(s);
   int st_a = 0, st_b = sh.stages - 1;     // ring stages of row i (its y) and of row i - 1 (then refilled)
   long long at = first * a.D - 2 * row_step;   // first channel of row i - 2
   for (long long i = 0; i < n_steps + 2; ++i, at += row_step) {
@@ -703,11 +707,47 @@ __global__ void __launch_bounds__(32 * bwd_warps(LAYER), 1) block_norm_bwd_kerne
   const bool has_y = FULL || a.y != nullptr, has_dr = FULL || a.dr != nullptr, has_pre = FULL || a.pre_has != 0, has_post = FULL || a.post_has != 0;
   int col[2];
   bool act[2];
-  f2 qreg[WREG ? 2 : 1][4], wreg[WREG ? 2 : 1][4];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     col[j] = tm.c_begin + (j * TL + tl) * 8;
     act[j] = col[j] < tm.c_end;
+  }
+  const long long first = (long long)tm.unit * sh.teams + tm.team, step = (long long)tm.units * sh.teams;
+  const long long n = first < a.M ? (a.M - first + step - 1) / step : 0;
+  // the teams of a cluster meet at its barrier: all do as many steps as its first team, which has the most rows
+  const long long n_steps = CL == 1 ? n : (a.M - (first - tm.team) + step - 1) / step;
+  auto slot = [](int stage, int j, int piece) { return stage * STAGE + (j * PIECES + piece) * 512; };
+  const long long row_step = step * a.D;
+  long long f_at = first * a.D, f_row = 0;       // first channel and number of the row that is fetched next
+  auto fetch = [&](int stage) {
+    if (f_row < n) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        if (!act[j]) continue;
+        const long long at = f_at + col[j];
+        if (has_y) cp_async16(ring_u32 + slot(stage, j, 0), a.y + at);
+        if (has_pre) {
+          cp_async16(ring_u32 + slot(stage, j, 1), a.du + at);
+#pragma unroll
+          for (int p = 0; p < RP; ++p)
+            cp_async16(ring_u32 + slot(stage, j, 2 + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.r) + at) + 16 * p);
+        }
+        if (has_dr) {
+#pragma unroll
+          for (int p = 0; p < RP; ++p)
+            cp_async16(ring_u32 + slot(stage, j, 2 + RP + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.dr) + at) + 16 * p);
+        }
+      }
+    }
+    ++f_row;
+    f_at += row_step;
+    cp_async_commit();
+  };
+  for (int s = 0; s + 1 < sh.stages; ++s) fetch(s);   // the weights come while the first rows are on their way
+
+  f2 qreg[WREG ? 2 : 1][4], wreg[WREG ? 2 : 1][4];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
     float q[8], w[8], g[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) q[k] = w[k] = 0.f;
@@ -753,37 +793,6 @@ __global__ void __launch_bounds__(32 * bwd_warps(LAYER), 1) block_norm_bwd_kerne
     }
   };
 
-  const long long first = (long long)tm.unit * sh.teams + tm.team, step = (long long)tm.units * sh.teams;
-  const long long n = first < a.M ? (a.M - first + step - 1) / step : 0;
-  // the teams of a cluster meet at its barrier: all do as many steps as its first team, which has the most rows
-  const long long n_steps = CL == 1 ? n : (a.M - (first - tm.team) + step - 1) / step;
-  auto slot = [](int stage, int j, int piece) { return stage * STAGE + (j * PIECES + piece) * 512; };
-  const long long row_step = step * a.D;
-  long long f_at = first * a.D, f_row = 0;       // first channel and number of the row that is fetched next
-  auto fetch = [&](int stage) {
-    if (f_row < n) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        if (!act[j]) continue;
-        const long long at = f_at + col[j];
-        if (has_y) cp_async16(ring_u32 + slot(stage, j, 0), a.y + at);
-        if (has_pre) {
-          cp_async16(ring_u32 + slot(stage, j, 1), a.du + at);
-#pragma unroll
-          for (int p = 0; p < RP; ++p)
-            cp_async16(ring_u32 + slot(stage, j, 2 + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.r) + at) + 16 * p);
-        }
-        if (has_dr) {
-#pragma unroll
-          for (int p = 0; p < RP; ++p)
-            cp_async16(ring_u32 + slot(stage, j, 2 + RP + p), reinterpret_cast<const uint8_t *>(static_cast<const RT *>(a.dr) + at) + 16 * p);
-        }
-      }
-    }
-    ++f_row;
-    f_at += row_step;
-    cp_async_commit();
-  };
   const f2 zero = both(0.f);
   auto read = [&](int stage, int j, int piece, bool there, bool resid, f2 (&f)[4]) {   // one vector of eight channels
     if (!there) {
@@ -810,7 +819,6 @@ __global__ void __launch_bounds__(32 * bwd_warps(LAYER), 1) block_norm_bwd_kerne
   float ip[2] = {1.f, 1.f}, mp[2] = {0.f, 0.f}, ir[2] = {0.f, 0.f}, mr[2] = {0.f, 0.f};
   float c1 = 0.f, c2 = 0.f, m1 = 0.f, m2 = 0.f;    // of row i - 1
   const f2 alpha = both(a.alpha);
-  for (int s = 0; s + 1 < sh.stages; ++s) fetch(s);
   // a row's statistics are read a step before they are used
   const bool has_stats = FULL || a.stats;
   float4 next_st = (has_stats && n > 0) ? __ldg(a.stats + first) : make_float4(0.f, 0.f, 0.f, 0.f);
