@@ -82,12 +82,13 @@ __device__ __forceinline__ void weights8(const float *w, int col, float fill, fl
   }
 }
 
-// A team of `warps` warps owns a row; a lane holds V vectors of eight adjacent channels, vector j at channel
+// Few rows, and int8 u (which needs the row's largest magnitude before anything is written).  A team of `warps` warps
+// owns a row; a lane holds V vectors of eight adjacent channels, vector j at channel
 // (j * 32 * warps + lane of the team) * 8, so that a warp's accesses are whole lines.  The row stays in registers
 // between the two norms: sums are taken over the values themselves (mean first, then squared distances from it), not
 // as differences of moments.
 template <typename RT, int V>
-__global__ void __launch_bounds__(V == 4 ? 512 : 1024) block_norm_fwd_kernel(const __grid_constant__ FwdArgs a) {
+__global__ void __launch_bounds__(1024) block_norm_fwd_kernel(const __grid_constant__ FwdArgs a) {
   __shared__ __align__(16) float red[2 * 32 * 4];
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -1171,18 +1172,21 @@ int osdp_block_norm_fwd(const void *x, const void *y, int64_t M, int64_t D, int 
   int sms = 0;
   const int src = sm_count(&sms);
   if (src) return src;
-  // Few rows: one vector per lane, as many warps to a row as it has vectors, for the shortest chain of instructions.
-  const bool few = D <= 8192 && M * cdiv(D, 256) <= 148 * 8;
-  if (!few && !u_scale && D > 512) {
+  // Few rows: one vector per lane, as many warps to a row as it has vectors, for the shortest chain of instructions, as long
+  // as all rows are at work at the same time (32 warps of this kernel fit an SM).  Measured on B200 (us, this way / rows in
+  // a pipeline): 1024 x 1024 RMS bf16 3.7 / 4.7, layer fp32 5.1 / 8.0; 256 x 4096 4.1 / 5.0 and 6.0 / 8.6; 512 x 4096 7.8 / 6.4
+  // and 11.3 / 12.0; 256 x 8192 9.8 / 6.4 and 15.1 / 12.2.
+  const bool few = D <= 8192 && M * cdiv(D, 256) <= (int64_t)sms * 32;
+  if (!few && !u_scale) {
     const bool layer = a.post.layer || a.pre.layer;
 #define OSDP_FWD(RT, LAYER) launch_fwd_rows<RT, LAYER>(a, sms, s)
     if (resid_dtype == OSDP_DTYPE_FP32) return layer ? OSDP_FWD(float, true) : OSDP_FWD(float, false);
     return layer ? OSDP_FWD(__nv_bfloat16, true) : OSDP_FWD(__nv_bfloat16, false);
 #undef OSDP_FWD
   }
-  if (few)
-    return resid_dtype == OSDP_DTYPE_FP32 ? launch_fwd<float, 1>(a, (int)cdiv(D, 256), s) : launch_fwd<__nv_bfloat16, 1>(a, (int)cdiv(D, 256), s);
-  return resid_dtype == OSDP_DTYPE_FP32 ? launch_fwd<float, 4>(a, (int)cdiv(D, 1024), s) : launch_fwd<__nv_bfloat16, 4>(a, (int)cdiv(D, 1024), s);
+  if (few) return resid_dtype == OSDP_DTYPE_FP32 ? launch_fwd<float, 1>(a, (int)cdiv(D, 256), s) : launch_fwd<__nv_bfloat16, 1>(a, (int)cdiv(D, 256), s);
+  // int8 u for many rows.  Two vectors per lane: 8192 x 2048 RMS 38 us; one 52, four 49 (8192 x 8192: 169, 325, 195).
+  return resid_dtype == OSDP_DTYPE_FP32 ? launch_fwd<float, 2>(a, (int)cdiv(D, 512), s) : launch_fwd<__nv_bfloat16, 2>(a, (int)cdiv(D, 512), s);
 }
 
 int osdp_block_norm_workspace_bytes(int64_t M, int64_t D, size_t *bytes) {
