@@ -145,6 +145,22 @@ def test_gradient_norm_and_clipping(P, dtype, sizes):
         assert torch.equal(opt.grad_norm, first)                     # same gradients, same bits
 
 
+@pytest.mark.parametrize("scale", [1e-12, 1e12, 1e15])
+def test_clipping_of_gradients_far_from_one(P, scale):
+    """The coefficient's square is outside fp32's normal range at the largest norm; v is not."""
+    from paper_2209_13258_b200.optim import AdamW
+    p = torch.nn.Parameter(gen(8)(1 << 20) * 0.05)
+    p.grad = gen(9)(1 << 20) * scale
+    opt = AdamW([p], lr=1e-3, betas=(0.9, 0.999), max_norm=0.1)
+    opt.step()
+    coef = float(opt.grad_norm[1])
+    m, v = states(opt, 0)
+    g = p.grad.double() * coef
+    # m: 1 - beta1, its product with the coefficient, the sum; v: the same and one product each for both g
+    assert bool(((m - 0.1 * g).abs() <= 5 * 2.0 ** -24 * 0.1 * g.abs() + 1e-37).all())
+    assert bool(((v - 0.001 * g * g).abs() <= 5 * 2.0 ** -24 * 0.001 * g * g + 1e-37).all())
+
+
 def test_a_norm_that_is_not_finite_changes_nothing(P):
     from paper_2209_13258_b200.optim import AdamW
     for bad in (float("nan"), float("inf")):
