@@ -426,6 +426,7 @@ int osdp_grad_norm(const osdp_adamw_tensor *tensors, int n_tensors, int grad_dty
  *            OSDP_DTYPE_E4M3: e4m3 codes of m and of sqrt(v), value = code * scale_m / scale_v [offset / OSDP_ADAMW_BLOCK].
  *            A scale is the block's largest magnitude / 448; a block below 2^-100 is stored as zeros; the code of a root
  *            above zero is at least the smallest positive one.  The step uses m and v before they are rounded.
+ *            A gradient whose square is not finite spoils the states and parameters of its block.
  *   clip     output of osdp_grad_norm or NULL.  If its coefficient is not finite nothing at all is updated.
  * All arithmetic per element is in a fixed order; the call is deterministic. */
 int osdp_adamw_step(const osdp_adamw_tensor *tensors, int n_tensors, int param_dtype, int state_dtype, float *master,

@@ -61,12 +61,30 @@ __device__ __forceinline__ int find_entry(const Table<MAXT> &t, int chunk) {
 struct Hyper {
   float b1, one_minus_b1, b2, one_minus_b2, eps;
   float root_scale;    // 1 / sqrt(1 - b2^t)
+  float one;           // 1, but not to the compiler: a * one + b is a sum that it cannot merge with the product a
 };
 
 __device__ __forceinline__ bool has_zero_byte(uint32_t w) { return ((w - 0x01010101u) & ~w & 0x80808080u) != 0u; }
 
-// 256 elements -> codes and their scale.  ROOT: the elements are not negative, those above zero keep at least the
-// smallest code.
+// Square roots to a relative 2^-22, for the update alone.
+__device__ __forceinline__ f2 fast_root2(f2 v) {
+  const float2 a = split2(v);
+  return pack2(fast_sqrt(a.x), fast_sqrt(a.y));
+}
+// From -v the negated square root of v, for roots that are stored: q = -v / sqrt(v) to a relative 2^-22, then one of Heron's
+// steps, q + (q^2 - v) / (2 sqrt(v)), whose remainder is 2^-45.  With one rounding after it that is the nearest fp32 value but for a case
+// in 10^6; signs are chosen so that no operation goes into them.  Zeros stay zeros: the reciprocal root is taken of at least
+// 2^-126.  The library's function took 100 us more for 537 M parameters.
+__device__ __forceinline__ f2 negated_root2(f2 minus_v) {
+  const float2 a = split2(minus_v);
+  constexpr float least = 1.17549435e-38f;
+  const f2 y = pack2(fast_rsqrt(fmaxf(-a.x, least)), fast_rsqrt(fmaxf(-a.y, least)));
+  const f2 q = mul2(minus_v, y);
+  return fma2(fma2(q, q, minus_v), mul2(y, both(0.5f)), q);
+}
+
+// 256 elements -> codes and their scale.  ROOT: x holds negated roots; those of numbers above zero keep at least the smallest
+// code.
 template <bool ROOT>
 __device__ __forceinline__ void quantise_block(const f2 (&x)[4], uint8_t *codes, float *scale, int lane) {
   float top = 0.f;
@@ -77,11 +95,11 @@ __device__ __forceinline__ void quantise_block(const f2 (&x)[4], uint8_t *codes,
   }
   top = warp_max_abs(top);
   const bool live = !(top < TINY);
-  const float inv = live ? __fdiv_rn(448.0f, top) : 0.0f;
-  const f2 inv2 = both(inv);
+  const float inv = live ? __frcp_rn(top) * 448.0f : 0.0f;
+  const f2 inv2 = both(ROOT ? -inv : inv);
   f2 c[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) c[j] = mul2(x[j], inv2);
+  for (int j = 0; j < 4; ++j) c[j] = ROOT ? fma2(x[j], inv2, both(0.0f)) : mul2(x[j], inv2);   // a root's zero has the code of +0
   uint2 q = encode_e4m3x8(c);
   if (ROOT && (has_zero_byte(q.x) || has_zero_byte(q.y))) {   // rare: an element that is zero, or very small in its block
 #pragma unroll
@@ -89,8 +107,8 @@ __device__ __forceinline__ void quantise_block(const f2 (&x)[4], uint8_t *codes,
       const float2 v = split2(x[j]);
       float2 l = split2(c[j]);
       constexpr float least = 0.001953125f;   // 2^-9, the smallest e4m3 value
-      if (live && v.x > 0.f) l.x = fmaxf(l.x, least);
-      if (live && v.y > 0.f) l.y = fmaxf(l.y, least);
+      if (live && v.x < 0.f) l.x = fmaxf(l.x, least);
+      if (live && v.y < 0.f) l.y = fmaxf(l.y, least);
       c[j] = pack2(l.x, l.y);
     }
     q = encode_e4m3x8(c);
@@ -146,8 +164,8 @@ struct RawState {
 // lines and a block's scale is a warp reduction.  All loads of BLOCKS blocks are issued before the first is used.
 // What bounds it: HBM with 32-bit states (28 bytes an element: 134 M bf16 parameters with fp32 masters 6310 GB/s of a copy rate
 // of 6547, the gradient norm before it included).  With 8-bit states (10 bytes an element) the instructions come near: 64 an
-// element in scalar form took 1450 us for 537 M parameters, 40 an element with pairs of fp32, approximate root and
-// reciprocal and the rare paths set apart take 830 us at full clocks (6510 GB/s) and 930 us in the power-capped state.
+// element in scalar form took 1450 us for 537 M parameters, some 45 an element with pairs of fp32, approximate reciprocals
+// and the rare paths set apart take 870 us at full clocks (6200 GB/s) and 935 us in the power-capped state.
 template <typename T, bool MASTER, bool E4M3, int MAXT>
 __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ Table<MAXT> t, const Hyper h, float *master,
                                                         void *state_m, void *state_v, float *scale_m, float *scale_v,
@@ -168,10 +186,9 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
   T *param = static_cast<T *>(e.param);
   const T *grad = static_cast<const T *>(e.grad);
   using W = typename std::conditional<MASTER, float, T>::type;
-  // The clipping coefficient is in the factor of g, and once in that of each g of g^2: its square alone would leave
-  // fp32's normal numbers at a gradient norm of 1e18.
-  const f2 b1 = both(h.b1), n1 = both(h.one_minus_b1 * coef), b2 = both(h.b2), n2 = both(h.one_minus_b2 * coef), clipped = both(coef), eps = both(h.eps),
-           root_scale = both(h.root_scale), decay = both(e.decay), size = both(-e.size);
+  constexpr float sign = E4M3 ? -1.0f : 1.0f;   // 8-bit states: v and its root are negated, see negated_root2
+  const f2 b1 = both(h.b1), n1 = both(h.one_minus_b1), b2 = both(sign * h.b2), n2 = both(sign * h.one_minus_b2), eps = both(h.eps),
+           root_scale = both(sign * h.root_scale), clipped = both(coef), one = both(h.one), decay = both(e.decay), size = both(-e.size);
 #pragma unroll 1
   for (int it = 0; it < PER_WARP; it += BLOCKS) {
     Raw8<T> rg[BLOCKS];
@@ -232,10 +249,13 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        m[j] = fma2(n1, g[j], mul2(m[j], b1));
-        v[j] = fma2(mul2(g[j], n2), mul2(g[j], clipped), mul2(v[j], b2));
-        const float2 s = split2(v[j]);
-        root[j] = pack2(fast_sqrt(s.x), fast_sqrt(s.y));
+        // Each operation of the formulas rounded by itself: 8-bit codes jump at ties, so that another evaluation of the
+        // formulas only gives the same codes where it gives the same bits.  (Contracted
+        // sums and approximate roots moved a code in 10^6, and with it the next step's scale where that was the largest.)
+        g[j] = mul2(g[j], clipped);
+        m[j] = fma2(mul2(m[j], b1), one, mul2(g[j], n1));
+        v[j] = fma2(mul2(v[j], b2), one, mul2(mul2(g[j], g[j]), n2));
+        root[j] = E4M3 ? negated_root2(v[j]) : fast_root2(v[j]);
         const float2 d = split2(fma2(root[j], root_scale, eps));
         const f2 upd = mul2(m[j], pack2(fast_rcp(d.x), fast_rcp(d.y)));
         w[j] = fma2(upd, size, mul2(w[j], decay));
@@ -503,6 +523,7 @@ int osdp_adamw_step(const osdp_adamw_tensor *tensors, int n_tensors, int param_d
   h.b2 = (float)beta2;
   h.one_minus_b2 = (float)(1.0 - beta2);
   h.eps = (float)eps;
+  h.one = 1.0f;
   h.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
   const double b1t = std::pow(beta1, (double)step);
   cudaStream_t s = static_cast<cudaStream_t>(stream);

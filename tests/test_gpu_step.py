@@ -145,6 +145,34 @@ def test_gradient_norm_and_clipping(P, dtype, sizes):
         assert torch.equal(opt.grad_norm, first)                     # same gradients, same bits
 
 
+def test_codes_are_those_of_the_formulas_op_by_op(P):
+    """8-bit states: the same codes and scales as the formulas in elementary fp32 operations, bit by bit, over several
+    steps (a code that falls on the other side of a tie would move a later scale by some percent)."""
+    from paper_2209_13258_b200.optim import AdamW
+    n, b1, b2 = 1 << 21, 0.9, 0.95
+    rnd = gen(31)
+    p = torch.nn.Parameter(rnd(n) * 0.05)
+    opt = AdamW([p], lr=1e-3, betas=(b1, b2), state_dtype="e4m3")
+    m = v = torch.zeros(n, device="cuda")
+    for t in range(4):
+        g = rnd(n) * torch.exp(rnd(n // QB, 1)).expand(-1, QB).reshape(-1) * (rnd(n) > -1.5)
+        p.grad = g
+        opt.step()
+        m = m * b1 + g * (1.0 - b1)
+        v = v * b2 + (g * g) * (1.0 - b2)
+        root = v.sqrt()
+        for x, codes, scales in ((m, opt.exp_avg, opt.exp_avg_scale), (root, opt.exp_avg_sq, opt.exp_avg_sq_scale)):
+            top = x.view(-1, QB).abs().amax(1)
+            c = x.view(-1, QB) * (top.reciprocal() * 448.0)[:, None]
+            if x is root:
+                c = torch.where(x.view(-1, QB) > 0, c.clamp_min(2.0 ** -9), c)
+            want = c.to(torch.float8_e4m3fn).view(-1).float()
+            assert torch.equal(codes.float(), want)
+            assert torch.equal(scales, top * (1.0 / 448.0))
+        m = (opt.exp_avg.float().view(-1, QB) * opt.exp_avg_scale[:, None]).view(-1)
+        v = (opt.exp_avg_sq.float().view(-1, QB) * opt.exp_avg_sq_scale[:, None]).view(-1).square()
+
+
 @pytest.mark.parametrize("scale", [1e-12, 1e12, 1e15])
 def test_clipping_of_gradients_far_from_one(P, scale):
     """The coefficient's square is outside fp32's normal range at the largest norm; v is not."""
