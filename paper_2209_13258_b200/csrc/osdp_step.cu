@@ -74,7 +74,7 @@ __device__ __forceinline__ f2 fast_root2(f2 v) {
 // From -v the negated square root of v, for roots that are stored: q = -v / sqrt(v) to a relative 2^-22, then one of Heron's
 // steps, q + (q^2 - v) / (2 sqrt(v)), whose remainder is 2^-45.  With one rounding after it that is the nearest fp32 value but for a case
 // in 10^6; signs are chosen so that no operation goes into them.  Zeros stay zeros: the reciprocal root is taken of at least
-// 2^-126.  The library's function took 100 us more for 537 M parameters.
+// 2^-126.  The library's function took 60 us more for 537 M parameters.
 __device__ __forceinline__ f2 negated_root2(f2 minus_v) {
   const float2 a = split2(minus_v);
   constexpr float least = 1.17549435e-38f;
@@ -165,7 +165,7 @@ struct RawState {
 // What bounds it: HBM with 32-bit states (28 bytes an element: 134 M bf16 parameters with fp32 masters 6310 GB/s of a copy rate
 // of 6547, the gradient norm before it included).  With 8-bit states (10 bytes an element) the instructions come near: 64 an
 // element in scalar form took 1450 us for 537 M parameters, some 45 an element with pairs of fp32, approximate reciprocals
-// and the rare paths set apart take 870 us at full clocks (6200 GB/s) and 935 us in the power-capped state.
+// and the rare paths set apart take 870 us at full clocks (6200 GB/s) and 974 us in the power-capped state.
 template <typename T, bool MASTER, bool E4M3, int MAXT>
 __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ Table<MAXT> t, const Hyper h, float *master,
                                                         void *state_m, void *state_v, float *scale_m, float *scale_v,

@@ -184,7 +184,7 @@ def test_clipping_of_gradients_far_from_one(P, scale):
     coef = float(opt.grad_norm[1])
     m, v = states(opt, 0)
     g = p.grad.double() * coef
-    # m: 1 - beta1, its product with the coefficient, the sum; v: the same and one product each for both g
+    # roundings: of c g, 1 - beta and its product; in v c g twice and its square
     assert bool(((m - 0.1 * g).abs() <= 5 * 2.0 ** -24 * 0.1 * g.abs() + 1e-37).all())
     assert bool(((v - 0.001 * g * g).abs() <= 5 * 2.0 ** -24 * 0.001 * g * g + 1e-37).all())
 
