@@ -203,12 +203,12 @@ __global__ void __launch_bounds__(1024) block_norm_fwd_kernel(const __grid_const
         for (int q = 0; q < a.warps; ++q)
           top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(buf[first_warp + q])));
       }
-      const float inv = int8_inverse(top);
+      const float scale = int8_scale(top), inv = int8_inverse(scale);
 #pragma unroll
       for (int j = 0; j < V; ++j)
         if (act[j])
-          *reinterpret_cast<uint2 *>(static_cast<int8_t *>(a.u) + row * a.D + (j * TL + tl) * 8) = to_int8x8(v[j], inv);
-      if (tl == 0) a.u_scale[row] = int8_scale(top);
+          *reinterpret_cast<uint2 *>(static_cast<int8_t *>(a.u) + row * a.D + (j * TL + tl) * 8) = to_int8x8(v[j], scale, inv);
+      if (tl == 0) a.u_scale[row] = scale;
     }
   }
   if (a.stats && tl == 0) a.stats[row] = st;

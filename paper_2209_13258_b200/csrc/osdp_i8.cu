@@ -38,13 +38,13 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const __nv_bfloat16 
     asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(TL) : "memory");
     for (int k = 0; k < warps; ++k) top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(red[first_warp + k])));
   }
-  const float inv = int8_inverse(top);
+  const float step = int8_scale(top), inv = int8_inverse(step);
   for (int c = tl * 8; c < K; c += TL * 8) {
     float f[8];
     widen8(__ldg(reinterpret_cast<const uint4 *>(xr + c)), f);
-    *reinterpret_cast<uint2 *>(q + row * K + c) = to_int8x8(f, inv);
+    *reinterpret_cast<uint2 *>(q + row * K + c) = to_int8x8(f, step, inv);
   }
-  if (tl == 0) scale[row] = int8_scale(top);
+  if (tl == 0) scale[row] = step;
 }
 
 // ---- Few tokens: the product is bound by reading W once; mma.sync (int8, exact int32 sums) takes W straight from

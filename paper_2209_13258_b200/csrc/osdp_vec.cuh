@@ -196,17 +196,27 @@ __device__ __forceinline__ float fast_rcp(float x) {
 
 // int8 rows: scale = (largest magnitude) / 127; a row whose largest magnitude is below 2^-100 (its reciprocal could
 // overflow) is stored as zeros with scale 0.  An infinity or a NaN goes into the scale.
-__device__ __forceinline__ float int8_inverse(float top) { return top < 7.888609052210118e-31f ? 0.f : __fdiv_rn(127.0f, top); }
 __device__ __forceinline__ float int8_scale(float top) { return top < 7.888609052210118e-31f ? 0.f : __fdiv_rn(top, 127.0f); }
-// Eight values times `inv`, rounded to the nearest integers (ties to even), as int8.  |value * inv| <= 127 up to
-// rounding; a NaN becomes 0.
-__device__ __forceinline__ uint2 to_int8x8(const float (&f)[8], float inv) {
-  uint32_t w[2] = {0u, 0u};
+__device__ __forceinline__ float int8_inverse(float scale) { return scale == 0.f ? 0.f : __frcp_rn(scale); }
+// Eight values / scale, rounded to the nearest integers (ties to even), as int8; a NaN becomes 0.  `inv` = int8_inverse(scale):
+// value * inv is within 127 * 2^-23 + 2^-24 of the quotient, so that it decides unless it is that close to the middle of
+// two integers; those, one in some thousand vectors, are divided.
+__device__ __forceinline__ uint2 to_int8x8(const float (&f)[8], float scale, float inv) {
+  int q[8];
+  bool middle = false;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const int q = min(127, max(-127, __float2int_rn(f[j] * inv)));
-    w[j >> 2] |= ((uint32_t)q & 0xFFu) << (8 * (j & 3));
+    const float t = f[j] * inv, n = rintf(t);
+    middle |= fabsf(t - n) > 0.4999f;
+    q[j] = (int)n;
   }
+  if (middle) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[j] = __float2int_rn(__fdiv_rn(f[j], scale));
+  }
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int j = 0; j < 8; ++j) w[j >> 2] |= ((uint32_t)min(127, max(-127, q[j])) & 0xFFu) << (8 * (j & 3));
   return make_uint2(w[0], w[1]);
 }
 
