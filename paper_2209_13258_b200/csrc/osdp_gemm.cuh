@@ -25,6 +25,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "osdp_vec.cuh"
+
 namespace osdp {
 
 constexpr int BM = 128;       // tile rows  (UMMA M, cta_group::1)
@@ -365,10 +367,10 @@ __device__ __forceinline__ void dequantise_acc(uint32_t (&v)[32], float row_scal
   for (int g = 0; g < 8; ++g) {
     float4 c = make_float4(0.f, 0.f, 0.f, 0.f);
     if (col + 4 * g < col_end) c = *reinterpret_cast<const float4 *>(col_scale + col + 4 * g);
-    v[4 * g + 0] = __float_as_uint((float)(int)v[4 * g + 0] * row_scale * c.x);
-    v[4 * g + 1] = __float_as_uint((float)(int)v[4 * g + 1] * row_scale * c.y);
-    v[4 * g + 2] = __float_as_uint((float)(int)v[4 * g + 2] * row_scale * c.z);
-    v[4 * g + 3] = __float_as_uint((float)(int)v[4 * g + 3] * row_scale * c.w);
+    v[4 * g + 0] = __float_as_uint(dequantise1((int)v[4 * g + 0], row_scale, c.x));
+    v[4 * g + 1] = __float_as_uint(dequantise1((int)v[4 * g + 1], row_scale, c.y));
+    v[4 * g + 2] = __float_as_uint(dequantise1((int)v[4 * g + 2], row_scale, c.z));
+    v[4 * g + 3] = __float_as_uint(dequantise1((int)v[4 * g + 3], row_scale, c.w));
   }
 }
 
@@ -599,6 +601,17 @@ __device__ __forceinline__ void gelu_array(float (&f)[N], int act) {
     for (int j = 0; j < N; ++j) f[j] = gelu_f(f[j], ACT_GELU_ERF);
   }
 }
+// int8 operands: the activation of the few-token kernel
+template <int N>
+__device__ __forceinline__ void gelu1_array(float (&f)[N], int act) {
+  if (act == ACT_GELU_TANH) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = gelu1(f[j], ACT_GELU_TANH);
+  } else if (act == ACT_GELU_ERF) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) f[j] = gelu1(f[j], ACT_GELU_ERF);
+  }
+}
 template <int N>
 __device__ __forceinline__ void gelu_grad_array(const float (&x)[N], float (&grad)[N], int act) {
   if (act == ACT_GELU_TANH) {
@@ -705,7 +718,7 @@ __device__ __forceinline__ void epilogue8(const Epilogue &e, long long row, int 
 // half as many B bytes cross from L2 to shared memory per flop.
 // I8: int8 operands with a scale per row and per column of the output (bf16 output, whole or concatenated, or summed
 // in tensor memory over all slices).  Tensor-bound like the other types: 8192 x 8192 x 8192 352 us = 3120 TOPS (e4m3: 358 us),
-// 8192 x 32768 x 8192 with bias and GeLU 1430 us = 3080 TOPS, 1690 us in the power-capped state.  A tile of 128 rows takes at
+// 8192 x 32768 x 8192 with bias and GeLU 1480 us = 2970 TOPS (1450 with the approximate tanh).  A tile of 128 rows takes at
 // least 0.29 us per k-block (reading A from shared memory), which is what bounds it with few tokens.
 template <int BN, bool A_MN, bool B_MN, bool CTA2, bool HEAVY = false, int EB = 2, bool I8 = false>
 __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kernel(const __grid_constant__ GemmParams p) {
@@ -1338,7 +1351,8 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
               float f[8];
 #pragma unroll
               for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(v[g * 8 + j]);
-              gelu_array(f, p.epi.act);
+              if (I8) gelu1_array(f, p.epi.act);
+              else gelu_array(f, p.epi.act);
               packed[g] = pack_bf16x8(f);
             }
             const uint32_t dst = stage_begin();

@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
       const int m = i / ROWS, n = unit * ROWS + i % ROWS;
       if (m < M && n < N && in_group % per == 0) {
         const bool f1 = i == in_group / per;
-        const float f = fmaf((float)s * scales[m], f1 ? ws_first : __ldg(a.w_scale + n), f1 ? b_first : a.bias ? __ldg(a.bias + n) : 0.f);
+        const float f = __fadd_rn(dequantise1(s, scales[m], f1 ? ws_first : __ldg(a.w_scale + n)), f1 ? b_first : a.bias ? __ldg(a.bias + n) : 0.f);
         a.out[(long long)m * N + n] = __float2bfloat16_rn(gelu1(f, a.act));
       }
     }

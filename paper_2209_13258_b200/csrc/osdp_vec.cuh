@@ -220,10 +220,22 @@ __device__ __forceinline__ uint2 to_int8x8(const float (&f)[8], float scale, flo
   return make_uint2(w[0], w[1]);
 }
 
-// act(x) with the ABI's activation codes (0 none, 1 GeLU tanh form, 2 GeLU erf form).
+// Epilogue of the int8 products.  Both kernels that have it round every operation by itself, whatever flags they are compiled
+// with, so that a token's outputs do not depend on how many tokens come with it.
+__device__ __forceinline__ float dequantise1(int sum, float row_scale, float col_scale) {
+  return __fmul_rn(__fmul_rn((float)sum, row_scale), col_scale);
+}
+// act(x) with the ABI's activation codes (0 none, 1 GeLU tanh form, 2 GeLU erf form).  0.5 (1 + tanh u) = 1 / (1 + exp(-2 u)): the
+// special-function unit's power of two and reciprocal are good to 2^-22, and a small output keeps its digits.
 __device__ __forceinline__ float gelu1(float x, int act) {
-  if (act == 1) return 0.5f * x * (1.0f + tanhf(0.7978845608028654f * (x + 0.044715f * x * x * x)));
-  if (act == 2) return 0.5f * x * (1.0f + erff(x * 0.7071067811865476f));
+  if (act == 1) {
+    constexpr float k = -2.0f * 1.4426950408889634f * 0.7978845608028654f;   // -2 log2(e) sqrt(2 / pi)
+    float e, h;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(__fmul_rn(x, __fmaf_rn(__fmul_rn(x, x), k * 0.044715f, k))));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(h) : "f"(__fadd_rn(1.0f, e)));
+    return __fmul_rn(x, h);
+  }
+  if (act == 2) return __fmul_rn(__fmul_rn(0.5f, x), __fadd_rn(1.0f, erff(__fmul_rn(x, 0.7071067811865476f))));
   return x;
 }
 

@@ -29,3 +29,41 @@ def test_codes_and_scales(P, M, K):
     want = torch.round(f / scale[:, None])
     off = int((q.float() != want).sum())
     assert off == 0, "%d of %d codes differ" % (off, q.numel())
+
+
+def layer(P, N, K, act, bias=True):
+    from paper_2209_13258_b200.nn import Int8Linear, quantize_int8
+    g = torch.Generator(device="cuda")
+    g.manual_seed(N + K)
+    w8, sw = quantize_int8((torch.randn(N, K, device="cuda", generator=g) * 1.5 / K ** 0.5).bfloat16())
+    b = torch.randn(N, device="cuda", generator=g) * 0.3 if bias else None
+    return Int8Linear(w8, sw, b, act=act), torch.randn(700, K, device="cuda", generator=g).bfloat16()
+
+
+@pytest.mark.parametrize("N,K", [(1024, 2048), (8200, 1040)])
+@pytest.mark.parametrize("act", [0, 1, 2])
+@pytest.mark.parametrize("bias", [False, True])
+def test_a_token_gives_the_same_bits_whatever_comes_with_it(P, N, K, act, bias):
+    """One token, some, and enough for the tile kernel."""
+    lin, x = layer(P, N, K, act, bias)
+    whole = lin(x)
+    for n in (1, 5, 16, 33, 65, 300):
+        assert torch.equal(lin(x[:n]), whole[:n]), n
+
+
+@pytest.mark.parametrize("M", [7, 700])
+@pytest.mark.parametrize("act", [1, 2])
+def test_activation(P, M, act):
+    """Against 64 bits.  The pre-activation has three fp32 roundings (4 * 2^-24 of its terms; GeLU's slope is at most 1.13).
+    The activation: the exponent of its power of two carries three roundings of at most 127, its own error and the
+    reciprocal's are below 2^-22, which is 2^-15 of the value; the erf form 1 + erf loses up to 2^-22 of |z|.  And half a
+    unit in the last place of bf16.  The approximate tanh (2^-11) would be far outside for negative z."""
+    from test_gpu_int8 import half_unit, linear64
+    from paper_2209_13258_b200.nn import quantize_int8
+    lin, x = layer(P, 1024, 2048, act)
+    x = x[:M]
+    q, s = quantize_int8(x)
+    mag, ref = linear64(q, s, lin.weight8, lin.w_scale, lin.bias, act)
+    slack = half_unit(ref) + 2.0 ** -20 * mag + 2.0 ** -15 * ref.abs() + 1e-30
+    off = (lin(x).double() - ref).abs() - slack
+    assert bool((off <= 0).all()), float(off.max())
