@@ -175,6 +175,11 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
   for (int t = 0; t < T8; ++t) x_row[t] = x8 + (long long)min(t * 8 + g, M - 1) * x_pitch;
   const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
   int slot = 0, turn = 0;
+  // Numbers of barriers end at 15: groups of two warps or more are eight at most, a group of one warp needs none.
+  auto group_sync = [&]() {
+    if (WK > 1) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(WK * 32) : "memory");
+    else __syncwarp();
+  };
   // The sums of a unit are added by all threads of the group: `per` adjacent lanes to an output, each a part of the warps.
   constexpr int OUTPUTS = T8 * 8 * ROWS;
   const int in_group = wk * 32 + lane;
@@ -228,7 +233,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
           if (2 * t + h < T8)
             *reinterpret_cast<int2 *>(sums + wk * SH::PITCH + (t * 16 + g + 8 * h) * ROWS + n * 8 + 2 * (lane & 3)) = make_int2(acc[t][n][2 * h], acc[t][n][2 * h + 1]);
     // with two buffers the only barrier of a unit: this buffer is written again only after the next one
-    asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(WK * 32) : "memory");
+    group_sync();
     for (int i = in_group / per; i < OUTPUTS; i += WK * 32 / per) {   // whole warps, or all their lanes, leave together
       int s = 0;
       for (int q = in_group % per; q < WK; q += per) s += sums[q * SH::PITCH + i];
@@ -240,7 +245,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
         a.out[(long long)m * N + n] = __float2bfloat16_rn(gelu1(f, a.act));
       }
     }
-    if (SH::TURNS == 1) asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "r"(WK * 32) : "memory");
+    if (SH::TURNS == 1) group_sync();
   }
   asm volatile("cp.async.wait_group 0;" ::: "memory");
 }

@@ -67,3 +67,17 @@ def test_activation(P, M, act):
     slack = half_unit(ref) + 2.0 ** -20 * mag + 2.0 ** -15 * ref.abs() + 1e-30
     off = (lin(x).double() - ref).abs() - slack
     assert bool((off <= 0).all()), float(off.max())
+
+
+@pytest.mark.parametrize("M,K", [(1, 16), (1, 512), (8, 752), (1, 768), (1, 784), (9, 128), (16, 368), (16, 384), (16, 400)])
+@pytest.mark.parametrize("N", [17760, 17768, 32000, 35536])
+def test_few_tokens_of_a_narrow_model_through_a_wide_layer(P, M, K, N):
+    """Reductions so short that each warp works by itself, outputs so wide that all sixteen of them have work."""
+    from test_gpu_int8 import check, codes, gen, linear64, run
+    g = gen(M + K + N)
+    x8, w8 = codes(g, M, K), codes(g, N, K)
+    sx, sw = torch.rand(M, device="cuda", generator=g) * 0.02 / K ** 0.5, torch.rand(N, device="cuda", generator=g) * 0.02
+    bias = torch.randn(N, device="cuda", generator=g)
+    out = run(P, x8, sx, w8, sw, bias, 0)
+    mag, ref = linear64(x8, sx, w8, sw, bias, 0)
+    check(out, mag, ref, 0)
