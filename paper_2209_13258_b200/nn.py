@@ -12,6 +12,20 @@ import torch
 from . import binding as B
 
 
+def _check_fp32(device, **vectors):
+    """name=(tensor or None, elements).  The kernels read these as fp32 from the address alone: another dtype, device or
+    length would be misread, and read beyond its end."""
+    for name, (v, n) in vectors.items():
+        if v is None:
+            continue
+        if v.dtype is not torch.float32:
+            raise TypeError("%s is %s and has to be fp32: module.to(dtype) casts every floating-point parameter and buffer" % (name, v.dtype))
+        if v.device != device:
+            raise RuntimeError("%s is on %s and its input on %s: they have to be on one CUDA device" % (name, v.device, device))
+        if v.numel() != n or not v.is_contiguous():
+            raise ValueError("%s has to be contiguous with %d elements" % (name, n))
+
+
 class _SplitLinearFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, layer):
@@ -356,7 +370,7 @@ class ResidualNorm(torch.nn.Module):
     the new residual stream, u (bf16): the input of the block after.  ``forward(x, y)`` returns (r, u);
     ``forward(x)`` in front of the first block leaves the y term out; pre=None returns (r, None) behind the last one.
     post / pre: "rms", "layer" or None.  gate: a learned value per channel (``gate_init``), or none with gate=False.
-    Weights, biases and gate are fp32 parameters.
+    Weights, biases and gate are fp32 parameters and have to stay fp32: a module cast by ``to(dtype)`` is refused.
 
     ``forward_int8(x, y)`` (no gradient) returns (r, (u8, scale)): u as int8 with a scale per token, what ``Int8Linear``
     takes, without the bf16 u in between.
@@ -396,6 +410,10 @@ class ResidualNorm(torch.nn.Module):
             raise TypeError("ResidualNorm takes x in its resid_dtype and y in bf16")
         if x.shape[-1] != self.hidden or (y is not None and y.shape != x.shape):
             raise ValueError("x and y are [..., hidden] of the same shape")
+        if y is not None and y.device != x.device:
+            raise RuntimeError("x is on %s and y on %s: they have to be on one CUDA device" % (x.device, y.device))
+        D = self.hidden
+        _check_fp32(x.device, w_post=(self.w_post, D), b_post=(self.b_post, D), gate=(self.gate, D), w_pre=(self.w_pre, D), b_pre=(self.b_pre, D))
 
     def forward(self, x, y=None):
         self._check(x, y)
@@ -438,7 +456,8 @@ class Int8Linear(torch.nn.Module):
     """y = act(x W^T + b) for serving, with int8 weights (a scale per output channel) and int8 activations (a scale per
     token, taken from the token itself); int32 sums, bf16 output.  No gradient.
 
-    weight8 [out, in] int8, w_scale [out] fp32, bias [out] fp32 or None.  ``from_linear`` quantises a trained
+    weight8 [out, in] int8, w_scale [out] fp32, bias [out] fp32 or None (fp32 for good: a module cast by ``to(dtype)`` is
+    refused).  ``from_linear`` quantises a trained
     ``SplitLinear`` (or any bf16 weight).  ``forward`` takes bf16 activations, or the pair (int8, scale) that
     ``ResidualNorm.forward_int8`` and ``quantize_int8`` return.
     """
@@ -483,11 +502,16 @@ class Int8Linear(torch.nn.Module):
         if shape[-1] != K:
             raise ValueError("Int8Linear takes [..., in_features]")
         M = q.numel() // K
+        if self.weight8.dtype is not torch.int8 or self.weight8.device != q.device or self.weight8.numel() != N * K:
+            raise RuntimeError("weight8 has to be [out_features, in_features] int8 on %s, its input's device" % q.device)
+        _check_fp32(q.device, w_scale=(self.w_scale, N), bias=(self.bias, N))
         if not q.is_contiguous():
             q = q.contiguous()
         if s is not None:
             if s.dtype != torch.float32 or s.numel() != M:
                 raise ValueError("one fp32 scale per token")
+            if s.device != q.device:
+                raise RuntimeError("the scales are on %s and the tokens on %s: they have to be on one CUDA device" % (s.device, q.device))
             s = s.contiguous()
         out = torch.empty(shape[:-1] + (N,), dtype=torch.bfloat16, device=q.device)
         B.osdp_split_linear_fwd_i8(q, s, self.weight8, 0, self.w_scale, self.bias, M, N, K, self.k_split, self.split_dim, self.act, out,

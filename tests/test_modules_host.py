@@ -1,0 +1,106 @@
+"""What the norm and int8 modules refuse before any address reaches a kernel.  No GPU: the tensors only say that they are
+on one, and a library call fails the test."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2209_13258_b200.binding as B                                     # noqa: E402
+from paper_2209_13258_b200 import nn as pnn                                    # noqa: E402
+
+BF16, CUDA0 = torch.bfloat16, torch.device("cuda", 0)
+
+
+class OnGpu(torch.Tensor):
+    """A CPU tensor that gives itself out as one on cuda:0."""
+    is_cuda = property(lambda self: True)
+    device = property(lambda self: CUDA0)
+
+
+def gpu(t):
+    return t.as_subclass(OnGpu)
+
+
+def to_gpu(module):
+    """The module's parameters and buffers say that they are on cuda:0."""
+    for group in (module._parameters, module._buffers):
+        for k, v in group.items():
+            if v is not None:
+                group[k] = torch.nn.Parameter(gpu(v.data)) if isinstance(v, torch.nn.Parameter) else gpu(v)
+    return module
+
+
+@pytest.fixture(autouse=True)
+def no_kernel(monkeypatch):
+    def reached(name):
+        def call(*a, **k):
+            raise AssertionError("%s was reached" % name)
+        return call
+    for name in ("osdp_block_norm_fwd", "osdp_split_linear_fwd_i8", "osdp_quantize_rows_i8", "osdp_split_linear_fwd", "osdp_split_mlp_fwd"):
+        monkeypatch.setattr(B, name, reached(name))
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **k: torch.zeros(*a, **k))
+    monkeypatch.setattr(torch, "empty_like", lambda t: torch.zeros(t.shape, dtype=t.dtype))
+    monkeypatch.setattr(B, "new_workspace", lambda n, device=None: torch.zeros(n, dtype=torch.uint8))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+
+
+def norm(**kw):
+    return pnn.ResidualNorm(64, post="layer", pre="layer", device="cpu", **kw)
+
+
+def int8(bias=True):
+    return pnn.Int8Linear(torch.ones(32, 64, dtype=torch.int8), torch.ones(32), torch.zeros(32) if bias else None)
+
+
+X = torch.ones(4, 64, dtype=BF16)
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float16, torch.float64])
+def test_a_cast_norm_is_refused(dtype):
+    m = to_gpu(norm().to(dtype))
+    for call in (lambda: m(gpu(X), gpu(X)), lambda: m(gpu(X)), lambda: m.forward_int8(gpu(X), gpu(X))):
+        with torch.no_grad(), pytest.raises(TypeError, match="fp32"):
+            call()
+
+
+@pytest.mark.parametrize("name", ["w_post", "b_post", "gate", "w_pre", "b_pre"])
+def test_each_vector_of_a_norm_is_looked_at(name):
+    for other, error in ((torch.ones(64, dtype=BF16), TypeError), (torch.ones(56), ValueError), (torch.ones(128)[::2], ValueError)):
+        m = to_gpu(norm())
+        m._parameters[name] = torch.nn.Parameter(gpu(other))
+        with torch.no_grad(), pytest.raises(error, match=name):
+            m(gpu(X), gpu(X))
+    m = to_gpu(norm())
+    m._parameters[name] = torch.nn.Parameter(torch.ones(64))
+    with torch.no_grad(), pytest.raises(RuntimeError, match="device"):
+        m(gpu(X), gpu(X))
+
+
+def test_a_norm_with_its_inputs_on_two_devices_is_refused():
+    with torch.no_grad(), pytest.raises(RuntimeError, match="device"):
+        to_gpu(norm())(gpu(X), X)
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float16])
+def test_a_cast_int8_layer_is_refused(dtype):
+    for bias in (True, False):
+        with pytest.raises(TypeError, match="fp32"):
+            to_gpu(int8(bias).to(dtype))(gpu(X))
+
+
+def test_an_int8_layer_elsewhere_is_refused():
+    codes, scale = X.to(torch.int8), torch.ones(4)
+    with pytest.raises(RuntimeError, match="device"):
+        int8()(gpu(X))
+    for name in ("w_scale", "bias", "weight8"):
+        m = to_gpu(int8())
+        m._buffers[name] = m._buffers[name].clone().as_subclass(torch.Tensor)
+        with pytest.raises(RuntimeError, match="device"):
+            m(gpu(X))
+    with pytest.raises(RuntimeError, match="device"):
+        to_gpu(int8())((gpu(codes), scale))
+
+
+def test_what_is_right_reaches_the_kernel():
+    for call in (lambda: to_gpu(norm())(gpu(X), gpu(X)), lambda: to_gpu(int8())(gpu(X)), lambda: to_gpu(int8())((gpu(X.to(torch.int8)), gpu(torch.ones(4))))):
+        with torch.no_grad(), pytest.raises(AssertionError, match="reached"):
+            call()
