@@ -26,6 +26,15 @@ def _check_fp32(device, **vectors):
             raise ValueError("%s has to be contiguous with %d elements" % (name, n))
 
 
+def _check_flat(device, flat, numel):
+    if flat.dtype is not torch.bfloat16:
+        raise TypeError("the flat parameter buffer is %s and has to be bf16" % flat.dtype)
+    if flat.device != device:
+        raise RuntimeError("the flat parameter buffer is on %s and its input on %s: they have to be on one CUDA device" % (flat.device, device))
+    if flat.numel() < numel or not flat.is_contiguous():
+        raise ValueError("the flat parameter buffer has to be contiguous with %d elements" % numel)
+
+
 class _SplitLinearFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, layer):
@@ -128,6 +137,8 @@ class SplitLinear(torch.nn.Module):
             raise RuntimeError("SplitLinear runs on CUDA only: there is no CPU path")
         if x.dtype != torch.bfloat16:
             raise TypeError("SplitLinear takes bf16 activations")
+        _check_flat(x.device, self.flat, self.w_offset + self.in_features * self.out_features)
+        _check_fp32(x.device, bias=(self.bias, self.out_features))
         return _SplitLinearFn.apply(x, self.weight, self.bias, self)
 
 
@@ -232,6 +243,8 @@ class SplitMLP(torch.nn.Module):
             raise RuntimeError("SplitMLP runs on CUDA only: there is no CPU path")
         if x.dtype != torch.bfloat16:
             raise TypeError("SplitMLP takes bf16 activations")
+        _check_flat(x.device, self.flat_param, 2 * self.hidden * self.ffn)
+        _check_fp32(x.device, b1=(self.b1, self.ffn), b2=(self.b2, self.hidden))
         return _SplitMLPFn.apply(x, self.flat_param, self.b1, self.b2, self)
 
 
@@ -306,6 +319,7 @@ class ZdpLinear(torch.nn.Module):
             raise RuntimeError("ZdpLinear runs on CUDA only: there is no CPU path")
         if x.dtype != torch.bfloat16:
             raise TypeError("ZdpLinear takes bf16 activations")
+        _check_fp32(x.device, bias=(self.bias, self.out_features))
         return _ZdpLinearFn.apply(x, self.shard, self.bias, self, *self.dp_parts)
 
 

@@ -1,4 +1,4 @@
-"""What the norm and int8 modules refuse before any address reaches a kernel.  No GPU: the tensors only say that they are
+"""What the modules refuse before any address reaches a kernel.  No GPU: the tensors only say that they are
 on one, and a library call fails the test."""
 import pytest
 
@@ -100,7 +100,31 @@ def test_an_int8_layer_elsewhere_is_refused():
         to_gpu(int8())((gpu(codes), scale))
 
 
+def split_layers():
+    return [pnn.SplitLinear(64, 32, device="cpu"), pnn.SplitMLP(64, 128, device="cpu")]
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float16, torch.float32])
+def test_a_cast_split_layer_is_refused(dtype):
+    """bf16 flat weights beside fp32 biases: any cast of the whole module spoils one of them."""
+    for m in split_layers():
+        with torch.no_grad(), pytest.raises(TypeError, match="has to be (fp32|bf16)"):
+            to_gpu(m.to(dtype))(gpu(X))
+
+
+def test_a_split_layer_elsewhere_is_refused():
+    for m in split_layers():
+        with torch.no_grad(), pytest.raises(RuntimeError, match="device"):
+            m(gpu(X))
+        for name in [k for k in m._parameters if m._parameters[k] is not None]:
+            m2 = to_gpu(type(m)(64, 128, device="cpu"))
+            m2._parameters[name] = torch.nn.Parameter(m._parameters[name].data.clone().resize_(m2._parameters[name].shape))
+            with torch.no_grad(), pytest.raises(RuntimeError, match="device"):
+                m2(gpu(X))
+
+
 def test_what_is_right_reaches_the_kernel():
-    for call in (lambda: to_gpu(norm())(gpu(X), gpu(X)), lambda: to_gpu(int8())(gpu(X)), lambda: to_gpu(int8())((gpu(X.to(torch.int8)), gpu(torch.ones(4))))):
+    for call in (lambda: to_gpu(split_layers()[0])(gpu(X)), lambda: to_gpu(split_layers()[1])(gpu(X)),
+                 lambda: to_gpu(norm())(gpu(X), gpu(X)), lambda: to_gpu(int8())(gpu(X)), lambda: to_gpu(int8())((gpu(X.to(torch.int8)), gpu(torch.ones(4))))):
         with torch.no_grad(), pytest.raises(AssertionError, match="reached"):
             call()
