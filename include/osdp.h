@@ -445,7 +445,8 @@ int osdp_quantize_rows_i8(const void *x, int64_t M, int64_t K, void *q, float *s
 
 /* x [M,K] and w8_flat (W [N,K] at element = byte offset w_offset) int8; x_scale [M], w_scale [N], bias [N] (or NULL) fp32;
  * out [M,N] bf16.  x_scale NULL: x is [M,K] bf16 and the call quantises it, as osdp_quantize_rows_i8 does, on the way;
- * ws then needs osdp_i8_workspace_bytes(M, K) bytes, otherwise 256 (its status word, as for every tile kernel).
+ * ws then needs osdp_i8_workspace_bytes(M, K) bytes, otherwise 256 (its status word, as for every tile kernel).  The codes lie
+ * in ws until the call's kernels have run: no other call may use it meanwhile, on another stream or by a graph's replay.
  * K and w_offset multiples of 16, N of 8 (16 if the slices cut N), a slice length of K a multiple of 16; K < 131072; M may
  * be 0.  x, w8_flat, out, w_scale and bias 16-byte aligned.  Every slice of the operator in one call, no flags.  No
  * gradient: a model is trained in bf16 and served in int8. */

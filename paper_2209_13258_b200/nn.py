@@ -489,16 +489,8 @@ class Int8Linear(torch.nn.Module):
         self.register_buffer("w_scale", w_scale.contiguous())
         self.register_buffer("bias", bias.contiguous() if bias is not None else None)
         self.act, self.k_split, self.split_dim = int(act), int(k_split), int(split_dim)
-        self._ws, self._ws_tokens = None, 0
-
-    def _workspace(self, M, quantise):
-        if self._ws is not None and (not quantise or M <= self._ws_tokens) and self._ws.device == self.weight8.device:
-            return self._ws
-        rc, need = B.osdp_i8_workspace_bytes(M, self.in_features)
-        if rc:
-            raise B.OsdpError(rc, "osdp_i8_workspace_bytes")
-        self._ws, self._ws_tokens = B.new_workspace(need, device=self.weight8.device), M
-        return self._ws
+        # the tile kernel's status word: all that is kept between calls
+        self.register_buffer("_status", torch.zeros(256, dtype=torch.uint8, device=weight8.device), persistent=False)
 
     @classmethod
     def from_linear(cls, layer, **kw):
@@ -527,7 +519,15 @@ class Int8Linear(torch.nn.Module):
             if s.device != q.device:
                 raise RuntimeError("the scales are on %s and the tokens on %s: they have to be on one CUDA device" % (s.device, q.device))
             s = s.contiguous()
-        out = torch.empty(shape[:-1] + (N,), dtype=torch.bfloat16, device=q.device)
+        else:
+            # This call's own scales (whole 256-byte lines of them) and codes: another stream's call has others, and a
+            # captured graph keeps its own.
+            lines = -(-M // 64) * 256
+            held = torch.empty(lines + M * K, dtype=torch.uint8, device=q.device)
+            s = held.data_ptr()
+            B.osdp_quantize_rows_i8(q, M, K, s + lines, s, check=True)
+            q = s + lines
+        out = torch.empty(shape[:-1] + (N,), dtype=torch.bfloat16, device=self.weight8.device)
         B.osdp_split_linear_fwd_i8(q, s, self.weight8, 0, self.w_scale, self.bias, M, N, K, self.k_split, self.split_dim, self.act, out,
-                                   self._workspace(M, s is None), check=True)
+                                   self._status, check=True)
         return out

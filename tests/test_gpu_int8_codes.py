@@ -81,3 +81,42 @@ def test_few_tokens_of_a_narrow_model_through_a_wide_layer(P, M, K, N):
     out = run(P, x8, sx, w8, sw, bias, 0)
     mag, ref = linear64(x8, sx, w8, sw, bias, 0)
     check(out, mag, ref, 0)
+
+
+def test_a_graph_of_few_tokens_outlives_calls_with_more(P):
+    """Decode graphs beside eager prompts: the graph's codes stay its own, and its replay writes into nobody's memory."""
+    lin, x = layer(P, 1024, 2048, 1)
+    for n in (4, 40):
+        lin, _ = layer(P, 1024, 2048, 1)
+        xs = x[:n].clone()
+        want = lin(xs)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = lin(xs)
+        whole = lin(x)
+        mine = [torch.full((n * 2048 // k,), 7, dtype=torch.uint8, device="cuda") for k in (1, 1, 2, 4, 8) for _ in range(8)]
+        for _ in range(3):
+            out.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+        assert all(bool((t == 7).all()) for t in mine)
+        assert torch.equal(lin(x), whole)
+
+
+def test_two_streams_on_one_layer(P):
+    lin, x = layer(P, 4096, 2048, 0)
+    a, b = x[:4].clone(), x[300:304].clone()
+    wants = lin(a), lin(b)
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for _ in range(200):
+        for k, (s, t) in enumerate(zip(streams, (a, b))):
+            with torch.cuda.stream(s):
+                got[k].append(lin(t))
+    torch.cuda.synchronize()
+    for k in (0, 1):
+        assert all(torch.equal(o, wants[k]) for o in got[k])

@@ -128,3 +128,19 @@ def test_what_is_right_reaches_the_kernel():
                  lambda: to_gpu(norm())(gpu(X), gpu(X)), lambda: to_gpu(int8())(gpu(X)), lambda: to_gpu(int8())((gpu(X.to(torch.int8)), gpu(torch.ones(4))))):
         with torch.no_grad(), pytest.raises(AssertionError, match="reached"):
             call()
+
+
+def test_an_int8_layer_keeps_no_memory_of_its_calls(monkeypatch):
+    """Codes and scales of a call's tokens are the call's: what the layer keeps does not depend on how many came (a captured
+    graph would keep the address of what a later call replaces, and two streams would share it)."""
+    kept, seen = [], []
+    monkeypatch.setattr(B, "osdp_quantize_rows_i8", lambda x, M, K, q, s, **k: seen.append(q))
+    monkeypatch.setattr(B, "osdp_split_linear_fwd_i8", lambda *a, **k: kept.append(a[13]))
+    m = to_gpu(int8())
+    before = {k: v.data_ptr() for k, v in m._buffers.items() if v is not None}
+    for tokens in (4, 300, 2):
+        m(gpu(torch.ones(tokens, 64, dtype=BF16)))
+    assert len(seen) == 3
+    assert all(w.numel() == 256 and w.data_ptr() == kept[0].data_ptr() for w in kept)
+    assert before == {k: v.data_ptr() for k, v in m._buffers.items() if v is not None}
+    assert not [k for k, v in vars(m).items() if torch.is_tensor(v)]
