@@ -366,8 +366,10 @@ class _ResidualNormFn(torch.autograd.Function):
         vec = lambda on: torch.empty(D, dtype=torch.float32, device=dev) if on else None    # noqa: E731
         dw_post, db_post, dgate = vec(need[2] and has_y), vec(need[3] and has_y), vec(need[4] and has_y)
         dw_pre, db_pre = vec(need[5] and pre), vec(need[6] and pre)
+        # this call's own: a backward on another stream may run at the same time, a captured one keeps its own
+        ws = torch.empty(layer._backward_bytes, dtype=torch.uint8, device=dev)
         B.osdp_block_norm_bwd(dr, du, y, r, stats, M, D, layer.resid_dtype, ctx.post, w_post, b_post, gate, layer.alpha, layer.beta,
-                              pre, w_pre if pre else None, dx, dy, dw_post, db_post, dgate, dw_pre, db_pre, layer._workspace(M, dev), check=True)
+                              pre, w_pre if pre else None, dx, dy, dw_post, db_post, dgate, dw_pre, db_pre, ws, check=True)
         return (dx.view(ctx.shape) if dx is not None else None, dy.view(ctx.shape) if dy is not None else None, dw_post, db_post,
                 dgate, dw_pre, db_pre, None)
 
@@ -407,15 +409,9 @@ class ResidualNorm(torch.nn.Module):
         self.w_post, self.b_post = vec(post, 1.0), vec(post == "layer", 0.0)
         self.w_pre, self.b_pre = vec(pre, 1.0), vec(pre == "layer", 0.0)
         self.gate = vec(gate, gate_init)
-        self._ws = None
-
-    def _workspace(self, M, dev):
-        if self._ws is None or self._ws.device != dev:       # its size does not depend on M
-            rc, need = B.osdp_block_norm_workspace_bytes(M, self.hidden)
-            if rc:
-                raise B.OsdpError(rc, "osdp_block_norm_workspace_bytes")
-            self._ws = B.new_workspace(need, device=dev)
-        return self._ws
+        rc, self._backward_bytes = B.osdp_block_norm_workspace_bytes(0, self.hidden)     # (the same for any number of rows)
+        if rc:
+            raise B.OsdpError(rc, "osdp_block_norm_workspace_bytes")
 
     def _check(self, x, y):
         if not x.is_cuda:

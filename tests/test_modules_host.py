@@ -144,3 +144,18 @@ def test_an_int8_layer_keeps_no_memory_of_its_calls(monkeypatch):
     assert all(w.numel() == 256 and w.data_ptr() == kept[0].data_ptr() for w in kept)
     assert before == {k: v.data_ptr() for k, v in m._buffers.items() if v is not None}
     assert not [k for k, v in vars(m).items() if torch.is_tensor(v)]
+
+
+def test_a_norm_keeps_no_memory_of_its_calls(monkeypatch):
+    """The partial sums of a backward call are the call's: two streams would share what the module keeps."""
+    used = []
+    monkeypatch.setattr(B, "osdp_block_norm_fwd", lambda *a, **k: None)
+    monkeypatch.setattr(B, "osdp_block_norm_bwd", lambda *a, **k: used.append(a[23]))
+    m = to_gpu(norm())
+    for tokens in (4, 300):
+        x = gpu(torch.ones(tokens, 64, dtype=BF16)).requires_grad_(True)
+        r, u = m(x, x)
+        (r.sum() + u.sum()).backward()
+    assert len(used) == 2 and used[0].numel() == used[1].numel() == B.osdp_block_norm_workspace_bytes(300, 64)[1]
+    assert used[0].data_ptr() != used[1].data_ptr()
+    assert not [k for k, v in vars(m).items() if torch.is_tensor(v)]
