@@ -489,7 +489,7 @@ def osdp_adamw_step(tensors, n_tensors, param_dtype, state_dtype, master, state_
 
 
 def osdp_quantize_rows_i8(x, M, K, q, scale, stream=None, check=False):
-    rc = lib().osdp_quantize_rows_i8(_ptr(x), int(M), int(K), _ptr(q), _ptr(scale), _stream(stream))
+    rc = lib().osdp_quantize_rows_i8(_ptr(x), M, K, _ptr(q), _ptr(scale), _stream(stream))
     return _ret(rc, check, "osdp_quantize_rows_i8")
 
 
@@ -504,7 +504,6 @@ def osdp_split_linear_fwd_i8(x, x_scale, w8_flat, w_offset, w_scale, bias, M, N,
                              stream=None, check=False):
     """x_scale None: x is bf16 and is quantised by the call."""
     wp, wn = _ws(ws)
-    rc = lib().osdp_split_linear_fwd_i8(_ptr(x), _ptr(x_scale), _ptr(w8_flat), int(w_offset), _ptr(w_scale), _ptr(bias), int(M),
-                                        int(N), int(K), int(k_split), int(split_dim), int(act), _ptr(out), wp, wn,
-                                        _stream(stream))
+    rc = lib().osdp_split_linear_fwd_i8(_ptr(x), _ptr(x_scale), _ptr(w8_flat), w_offset, _ptr(w_scale), _ptr(bias), M, N, K,
+                                        k_split, split_dim, act, _ptr(out), wp, wn, _stream(stream))
     return _ret(rc, check, "osdp_split_linear_fwd_i8")

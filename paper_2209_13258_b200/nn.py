@@ -504,26 +504,29 @@ class Int8Linear(torch.nn.Module):
         if shape[-1] != K:
             raise ValueError("Int8Linear takes [..., in_features]")
         M = q.numel() // K
-        if self.weight8.dtype is not torch.int8 or self.weight8.device != q.device or self.weight8.numel() != N * K:
-            raise RuntimeError("weight8 has to be [out_features, in_features] int8 on %s, its input's device" % q.device)
-        _check_fp32(q.device, w_scale=(self.w_scale, N), bias=(self.bias, N))
+        held = self._buffers          # (an attribute of a module that is a buffer takes several times as long)
+        w8, w_scale, bias, device = held["weight8"], held["w_scale"], held["bias"], q.device
+        if w8.dtype is not torch.int8 or w8.device != device or w8.numel() != N * K:
+            raise RuntimeError("weight8 has to be [out_features, in_features] int8 on %s, its input's device" % device)
+        _check_fp32(device, w_scale=(w_scale, N), bias=(bias, N))
         if not q.is_contiguous():
             q = q.contiguous()
+        stream = B._stream(None)
         if s is not None:
             if s.dtype != torch.float32 or s.numel() != M:
                 raise ValueError("one fp32 scale per token")
-            if s.device != q.device:
-                raise RuntimeError("the scales are on %s and the tokens on %s: they have to be on one CUDA device" % (s.device, q.device))
+            if s.device != device:
+                raise RuntimeError("the scales are on %s and the tokens on %s: they have to be on one CUDA device" % (s.device, device))
             s = s.contiguous()
         else:
             # This call's own scales (whole 256-byte lines of them) and codes: another stream's call has others, and a
             # captured graph keeps its own.
             lines = -(-M // 64) * 256
-            held = torch.empty(lines + M * K, dtype=torch.uint8, device=q.device)
-            s = held.data_ptr()
-            B.osdp_quantize_rows_i8(q, M, K, s + lines, s, check=True)
+            own = torch.empty(lines + M * K, dtype=torch.uint8, device=device)
+            s = own.data_ptr()
+            B.osdp_quantize_rows_i8(q, M, K, s + lines, s, stream, True)
             q = s + lines
-        out = torch.empty(shape[:-1] + (N,), dtype=torch.bfloat16, device=self.weight8.device)
-        B.osdp_split_linear_fwd_i8(q, s, self.weight8, 0, self.w_scale, self.bias, M, N, K, self.k_split, self.split_dim, self.act, out,
-                                   self._status, check=True)
+        out = torch.empty(shape[:-1] + (N,), dtype=torch.bfloat16, device=device)
+        B.osdp_split_linear_fwd_i8(q, s, w8, 0, w_scale, bias, M, N, K, self.k_split, self.split_dim, self.act, out, held["_status"], stream,
+                                   True)
         return out

@@ -41,6 +41,7 @@ def no_kernel(monkeypatch):
     monkeypatch.setattr(torch, "empty_like", lambda t: torch.zeros(t.shape, dtype=t.dtype))
     monkeypatch.setattr(B, "new_workspace", lambda n, device=None: torch.zeros(n, dtype=torch.uint8))
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(B, "_stream", lambda s: 0)
 
 
 def norm(**kw):
@@ -134,7 +135,7 @@ def test_an_int8_layer_keeps_no_memory_of_its_calls(monkeypatch):
     """Codes and scales of a call's tokens are the call's: what the layer keeps does not depend on how many came (a captured
     graph would keep the address of what a later call replaces, and two streams would share it)."""
     kept, seen = [], []
-    monkeypatch.setattr(B, "osdp_quantize_rows_i8", lambda x, M, K, q, s, **k: seen.append(q))
+    monkeypatch.setattr(B, "osdp_quantize_rows_i8", lambda x, M, K, q, s, *a, **k: seen.append(q))
     monkeypatch.setattr(B, "osdp_split_linear_fwd_i8", lambda *a, **k: kept.append(a[13]))
     m = to_gpu(int8())
     before = {k: v.data_ptr() for k, v in m._buffers.items() if v is not None}
