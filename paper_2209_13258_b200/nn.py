@@ -26,6 +26,11 @@ def _check_fp32(device, **vectors):
             raise ValueError("%s has to be contiguous with %d elements" % (name, n))
 
 
+def _elsewhere(x):
+    """Whether x is on another CUDA device than the current one, on whose current stream a call launches."""
+    return x.is_cuda and x.get_device() != torch.cuda.current_device()
+
+
 def _check_flat(device, flat, numel):
     if flat.dtype is not torch.bfloat16:
         raise TypeError("the flat parameter buffer is %s and has to be bf16" % flat.dtype)
@@ -426,6 +431,9 @@ class ResidualNorm(torch.nn.Module):
         _check_fp32(x.device, w_post=(self.w_post, D), b_post=(self.b_post, D), gate=(self.gate, D), w_pre=(self.w_pre, D), b_pre=(self.b_pre, D))
 
     def forward(self, x, y=None):
+        if _elsewhere(x):
+            with torch.cuda.device(x.device):
+                return self.forward(x, y)
         self._check(x, y)
         if y is None and self.alpha == 1.0 and self.pre == B.NORM_NONE:
             return x, None
@@ -434,6 +442,9 @@ class ResidualNorm(torch.nn.Module):
 
     @torch.no_grad()
     def forward_int8(self, x, y=None):
+        if _elsewhere(x):
+            with torch.cuda.device(x.device):
+                return self.forward_int8(x, y)
         self._check(x, y)
         if self.pre == B.NORM_NONE:
             raise ValueError("there is no u to quantise: pre is None")
@@ -455,6 +466,9 @@ def quantize_int8(x):
     K = x.shape[-1]
     if not x.is_cuda or x.dtype != torch.bfloat16:
         raise TypeError("quantize_int8 takes a bf16 CUDA tensor")
+    if _elsewhere(x):
+        with torch.cuda.device(x.device):
+            return quantize_int8(x)
     x2 = x.detach().reshape(-1, K).contiguous()
     q = torch.empty(x2.shape, dtype=torch.int8, device=x.device)
     s = torch.empty(x2.shape[0], dtype=torch.float32, device=x.device)
@@ -499,6 +513,9 @@ class Int8Linear(torch.nn.Module):
         q, s = x if isinstance(x, tuple) else (x, None)
         if q.dtype != (torch.bfloat16 if s is None else torch.int8) or not q.is_cuda:
             raise TypeError("Int8Linear takes bf16 CUDA activations, or a pair (int8, fp32 scale per token)")
+        if _elsewhere(q):
+            with torch.cuda.device(q.device):
+                return self.forward(x)
         K, N = self.in_features, self.out_features
         shape = q.shape
         if shape[-1] != K:

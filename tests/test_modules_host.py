@@ -14,6 +14,7 @@ class OnGpu(torch.Tensor):
     """A CPU tensor that gives itself out as one on cuda:0."""
     is_cuda = property(lambda self: True)
     device = property(lambda self: CUDA0)
+    get_device = lambda self: 0                                                # noqa: E731
 
 
 def gpu(t):
@@ -160,3 +161,29 @@ def test_a_norm_keeps_no_memory_of_its_calls(monkeypatch):
     assert len(used) == 2 and used[0].numel() == used[1].numel() == B.osdp_block_norm_workspace_bytes(300, 64)[1]
     assert used[0].data_ptr() != used[1].data_ptr()
     assert not [k for k, v in vars(m).items() if torch.is_tensor(v)]
+
+
+def test_calls_launch_on_their_tensors_device(monkeypatch):
+    """The current device is another one: its current stream must not get the launch."""
+    now, at = [1], []
+
+    class Device:
+        def __init__(self, device):
+            self.index = torch.device(device).index
+
+        def __enter__(self):
+            self.old, now[0] = now[0], self.index
+
+        def __exit__(self, *a):
+            now[0] = self.old
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    for name in ("osdp_block_norm_fwd", "osdp_split_linear_fwd_i8", "osdp_quantize_rows_i8"):
+        monkeypatch.setattr(B, name, lambda *a, **k: at.append(now[0]))
+    with torch.no_grad():
+        to_gpu(norm())(gpu(X), gpu(X))
+        to_gpu(norm()).forward_int8(gpu(X), gpu(X))
+        to_gpu(int8())(gpu(X))
+        pnn.quantize_int8(gpu(X))
+    assert at == [0] * 5 and now == [1]
