@@ -16,7 +16,8 @@ _TENSOR = np.dtype([("param", np.uint64), ("grad", np.uint64), ("numel", np.int6
                     ("lr", np.float64), ("weight_decay", np.float64)])      # osdp_adamw_tensor
 
 
-_GRAD, _DATA_PTR, _IS_CONTIGUOUS = operator.attrgetter("grad"), torch.Tensor.data_ptr, torch.Tensor.is_contiguous
+_GRAD, _DTYPE = operator.attrgetter("grad"), operator.attrgetter("dtype")
+_DATA_PTR, _NUMEL, _DEVICE, _IS_CONTIGUOUS = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
 
 
 class AdamW(torch.optim.Optimizer):
@@ -93,18 +94,34 @@ class AdamW(torch.optim.Optimizer):
             raise RuntimeError("the states are laid out when the optimiser is built: pass all groups then")
         super().add_param_group(group)
 
+    def _refuse(self, what, tensors, sizes):
+        """Raises for the tensor that is no longer what the kernel is told of it."""
+        for i, (t, n) in enumerate(zip(tensors, sizes)):
+            if t.dtype is not self._torch_dtype:
+                raise TypeError("%s %d is %s, the optimiser was built for %s" % (what, i, t.dtype, self._torch_dtype))
+            if t.get_device() != self._device.index:
+                raise RuntimeError("%s %d is on %s, the optimiser was built on %s" % (what, i, t.device, self._device))
+            if t.numel() != n:
+                raise ValueError("%s %d has %d elements, the optimiser was built for %d" % (what, i, t.numel(), n))
+            if what == "parameter" and not t.is_contiguous():
+                raise ValueError("parameter %d is not contiguous any more" % i)
+
     def _fill(self):
         """The table of this step: addresses as they are now; tensors without a gradient are left out.  Returns its
         length and the copies of gradients that were not contiguous."""
-        params, table = self._params, self._table
-        dtype = self._torch_dtype
-        for p in params:
-            if p.dtype is not dtype:
-                raise TypeError("a parameter's dtype has changed since the optimiser was built")
+        params, table, sizes = self._params, self._table, self._sizes
+        # The kernel has addresses and the lengths recorded when the optimiser was built: whatever else a parameter or a
+        # gradient has become (moved, cast, resized, strided) would be read and written out of its bounds.
+        dtype, device = {self._torch_dtype}, {self._device.index}
+        if set(map(_DTYPE, params)) != dtype or set(map(_DEVICE, params)) != device or list(map(_NUMEL, params)) != sizes or \
+           not all(map(_IS_CONTIGUOUS, params)):
+            self._refuse("parameter", params, sizes)
         grads, at, keep = list(map(_GRAD, params)), None, None
         if type(None) in set(map(type, grads)):
             at = [i for i, g in enumerate(grads) if g is not None]
-            params, grads = [params[i] for i in at], [grads[i] for i in at]
+            params, grads, sizes = [params[i] for i in at], [grads[i] for i in at], [sizes[i] for i in at]
+        if grads and (set(map(_DTYPE, grads)) != dtype or set(map(_DEVICE, grads)) != device or list(map(_NUMEL, grads)) != sizes):
+            self._refuse("gradient", grads, sizes)
         if not all(map(_IS_CONTIGUOUS, grads)):
             keep = grads = [g.contiguous() for g in grads]
         n = len(grads)
