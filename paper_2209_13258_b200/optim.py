@@ -20,6 +20,12 @@ _GRAD, _DTYPE = operator.attrgetter("grad"), operator.attrgetter("dtype")
 _DATA_PTR, _NUMEL, _DEVICE, _IS_CONTIGUOUS = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
 
 
+try:      # one native pass over type, dtype, device, sizes and strides of many tensors, where this torch has it
+    from torch._C._dynamo.guards import TensorGuards as _TensorGuards
+except ImportError:
+    _TensorGuards = None
+
+
 class AdamW(torch.optim.Optimizer):
     """Decoupled weight decay (AdamW) for contiguous CUDA parameters of one dtype, bf16 or fp32.
 
@@ -91,6 +97,8 @@ class AdamW(torch.optim.Optimizer):
 
     def add_param_group(self, group):
         if self._built:
+        # parameters and gradients as one step found them in order; a few times anew, if what comes changes
+        self._guard, self._guards_left = None, 8 if _TensorGuards is not None else 0
             raise RuntimeError("the states are laid out when the optimiser is built: pass all groups then")
         super().add_param_group(group)
 
@@ -119,11 +127,23 @@ class AdamW(torch.optim.Optimizer):
         grads, at, keep = list(map(_GRAD, params)), None, None
         if type(None) in set(map(type, grads)):
             at = [i for i, g in enumerate(grads) if g is not None]
-            params, grads, sizes = [params[i] for i in at], [grads[i] for i in at], [sizes[i] for i in at]
-        if grads and (set(map(_DTYPE, grads)) != dtype or set(map(_DEVICE, grads)) != device or list(map(_NUMEL, grads)) != sizes):
-            self._refuse("gradient", grads, sizes)
-        if not all(map(_IS_CONTIGUOUS, grads)):
-            keep = grads = [g.contiguous() for g in grads]
+        # The kernel has addresses and the lengths recorded when the optimiser was built: whatever else a parameter or a
+        # gradient has become (moved, cast, resized, strided) would be read and written out of its bounds.
+        if self._guard is None or at is not None or not self._guard.check(*params, *grads):
+            dtype, device = {self._torch_dtype}, {self._device.index}
+            if set(map(_DTYPE, params)) != dtype or set(map(_DEVICE, params)) != device or list(map(_NUMEL, params)) != sizes or \
+               not all(map(_IS_CONTIGUOUS, params)):
+                self._refuse("parameter", params, sizes)
+            if at is not None:
+                params, grads, sizes = [params[i] for i in at], [grads[i] for i in at], [sizes[i] for i in at]
+            if grads and (set(map(_DTYPE, grads)) != dtype or set(map(_DEVICE, grads)) != device or list(map(_NUMEL, grads)) != sizes):
+                self._refuse("gradient", grads, sizes)
+            if not all(map(_IS_CONTIGUOUS, grads)):
+                keep = grads = [g.contiguous() for g in grads]
+            elif at is None and self._guards_left:
+                self._guards_left -= 1
+                ts = params + grads
+                self._guard = _TensorGuards(*ts, dynamic_dims_sizes=[list(t.shape) for t in ts], dynamic_dims_strides=[list(t.stride()) for t in ts])
         n = len(grads)
         rates = [(float(g["lr"]), float(g["weight_decay"])) for g in self.param_groups]
         if at is not None or not self._whole or rates != self._rates:
