@@ -16,7 +16,7 @@ _TENSOR = np.dtype([("param", np.uint64), ("grad", np.uint64), ("numel", np.int6
                     ("lr", np.float64), ("weight_decay", np.float64)])      # osdp_adamw_tensor
 
 
-_GRAD, _DTYPE = operator.attrgetter("grad"), operator.attrgetter("dtype")
+_GRAD, _DTYPE, _VERSION = operator.attrgetter("grad"), operator.attrgetter("dtype"), operator.attrgetter("_version")
 _DATA_PTR, _NUMEL, _DEVICE, _IS_CONTIGUOUS = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
 
 
@@ -33,6 +33,10 @@ class AdamW(torch.optim.Optimizer):
                  parameter instead of 8; the second moment is kept as its root).
     master       bf16 parameters only: the step works on fp32 copies of the parameters (4 bytes each) and writes their
                  rounding.  Without it an update below half a unit in the last place of a bf16 parameter is lost.
+                 Parameters that change outside the step (weights loaded, averaged or initialised again: any in-place
+                 operation on them, or new ``.data``) are noticed by the next step, which takes the changed elements over
+                 into the masters.  Writes through ``p.data`` or by another library's kernels leave no trace:
+                 call ``refresh_masters()`` after them.
     max_norm     clips the gradients by their global norm over all parameters of the step, without a host round trip.
                  A step whose norm is not finite changes no parameter and no state (``grad_norm[0]`` says so); it counts as
                  a step all the same, since the host does not wait to learn of it.
@@ -82,6 +86,7 @@ class AdamW(torch.optim.Optimizer):
             self.master = new(total, torch.float32)
             for p, o in zip(self._params, self.offsets):
                 self.master[o:o + p.numel()].copy_(p.detach().reshape(-1))
+        self._seen = self._params_now() if master else None
         self.max_norm = max_norm
         self.grad_norm = new(2, torch.float32)
         self.steps = 0
@@ -92,15 +97,30 @@ class AdamW(torch.optim.Optimizer):
         self._group_of = [i for i, g in enumerate(self.param_groups) for _ in g["params"]]
         self._table = np.zeros(n, dtype=_TENSOR)
         self._whole, self._rates = False, None
+        # parameters and gradients as one step found them in order; a few times anew, if what comes changes
+        self._guard, self._guards_left = None, 8 if _TensorGuards is not None else 0
         self._ws = B.new_workspace(B.osdp_grad_norm_workspace_bytes(n)[1], device=dev)
         self._built = True
 
     def add_param_group(self, group):
         if self._built:
-        # parameters and gradients as one step found them in order; a few times anew, if what comes changes
-        self._guard, self._guards_left = None, 8 if _TensorGuards is not None else 0
             raise RuntimeError("the states are laid out when the optimiser is built: pass all groups then")
         super().add_param_group(group)
+
+    def _params_now(self):
+        """Changes with every in-place operation on a parameter (the step's own kernel leaves it alone) and every move."""
+        return list(map(_VERSION, self._params)), list(map(_DATA_PTR, self._params))
+
+    @torch.no_grad()
+    def refresh_masters(self):
+        """Takes parameters over into the fp32 masters, element by element where a parameter is not its master's
+        rounding: elements that nobody changed keep their masters' digits."""
+        if self.master is None:
+            return
+        for p, o, n in zip(self._params, self.offsets, self._sizes):
+            m, w = self.master[o:o + n], p.detach().reshape(-1)
+            m.copy_(torch.where(m.to(w.dtype) == w, m, w.to(m.dtype)))
+        self._seen = self._params_now()
 
     def _refuse(self, what, tensors, sizes):
         """Raises for the tensor that is no longer what the kernel is told of it."""
@@ -118,12 +138,6 @@ class AdamW(torch.optim.Optimizer):
         """The table of this step: addresses as they are now; tensors without a gradient are left out.  Returns its
         length and the copies of gradients that were not contiguous."""
         params, table, sizes = self._params, self._table, self._sizes
-        # The kernel has addresses and the lengths recorded when the optimiser was built: whatever else a parameter or a
-        # gradient has become (moved, cast, resized, strided) would be read and written out of its bounds.
-        dtype, device = {self._torch_dtype}, {self._device.index}
-        if set(map(_DTYPE, params)) != dtype or set(map(_DEVICE, params)) != device or list(map(_NUMEL, params)) != sizes or \
-           not all(map(_IS_CONTIGUOUS, params)):
-            self._refuse("parameter", params, sizes)
         grads, at, keep = list(map(_GRAD, params)), None, None
         if type(None) in set(map(type, grads)):
             at = [i for i, g in enumerate(grads) if g is not None]
@@ -188,6 +202,8 @@ class AdamW(torch.optim.Optimizer):
 
     def _launch(self, betas, eps):
         n, keep = self._fill()
+        if self.master is not None and self._params_now() != self._seen:
+            self.refresh_masters()
         self.steps += 1
         clip, table = None, self._table.__array_interface__["data"][0]
         if self.max_norm is not None:
@@ -217,3 +233,5 @@ class AdamW(torch.optim.Optimizer):
             if v is not None:
                 getattr(self, k).copy_(v)
         self.steps = int(steps)
+        if self.master is not None:
+            self._seen = self._params_now()
