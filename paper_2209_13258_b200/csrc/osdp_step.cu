@@ -66,7 +66,7 @@ struct Hyper {
 
 __device__ __forceinline__ bool has_zero_byte(uint32_t w) { return ((w - 0x01010101u) & ~w & 0x80808080u) != 0u; }
 
-// Square roots to a relative 2^-22, for the update alone.
+// Square roots to a relative 2^-22, for the update alone (of subnormal numbers too).
 __device__ __forceinline__ f2 fast_root2(f2 v) {
   const float2 a = split2(v);
   return pack2(fast_sqrt(a.x), fast_sqrt(a.y));
@@ -74,7 +74,8 @@ __device__ __forceinline__ f2 fast_root2(f2 v) {
 // From -v the negated square root of v, for roots that are stored: q = -v / sqrt(v) to a relative 2^-22, then one of Heron's
 // steps, q + (q^2 - v) / (2 sqrt(v)), whose remainder is 2^-45.  With one rounding after it that is the nearest fp32 value but for a case
 // in 10^6; signs are chosen so that no operation goes into them.  Zeros stay zeros: the reciprocal root is taken of at least
-// 2^-126.  The library's function took 60 us more for 537 M parameters.
+// 2^-126.  The library's function took 60 us more for 537 M parameters.  Not for v below 2^-100 (root_of_small): the
+// remainder q^2 - v leaves fp32's range there.
 __device__ __forceinline__ f2 negated_root2(f2 minus_v) {
   const float2 a = split2(minus_v);
   constexpr float least = 1.17549435e-38f;
@@ -82,6 +83,7 @@ __device__ __forceinline__ f2 negated_root2(f2 minus_v) {
   const f2 q = mul2(minus_v, y);
   return fma2(fma2(q, q, minus_v), mul2(y, both(0.5f)), q);
 }
+__device__ __forceinline__ float root_of_small(float minus_v, float root) { return minus_v < 0.f && minus_v > -TINY ? -__fsqrt_rn(-minus_v) : root; }
 
 // 256 elements -> codes and their scale.  ROOT: x holds negated roots; those of numbers above zero keep at least the smallest
 // code.
@@ -256,6 +258,24 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
         m[j] = fma2(mul2(m[j], b1), one, mul2(g[j], n1));
         v[j] = fma2(mul2(v[j], b2), one, mul2(mul2(g[j], g[j]), n2));
         root[j] = E4M3 ? negated_root2(v[j]) : fast_root2(v[j]);
+      }
+      if constexpr (E4M3) {
+        float smallest = TINY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float2 x = split2(v[j]);
+          smallest = min_abs3(smallest, x.x, x.y);
+        }
+        if (smallest < TINY) {   // rare, but for zeros
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 x = split2(v[j]), r = split2(root[j]);
+            root[j] = pack2(root_of_small(x.x, r.x), root_of_small(x.y, r.y));
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
         const float2 d = split2(fma2(root[j], root_scale, eps));
         const f2 upd = mul2(m[j], pack2(fast_rcp(d.x), fast_rcp(d.y)));
         w[j] = fma2(upd, size, mul2(w[j], decay));

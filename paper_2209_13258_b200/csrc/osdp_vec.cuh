@@ -177,10 +177,17 @@ __device__ __forceinline__ float max_abs3(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
   return r;
 }
-// Square root and reciprocal of the special-function unit (relative error about 2^-22; denormals count as zero).
+// Smallest of `a` >= 0 and two magnitudes; a NaN loses.
+__device__ __forceinline__ float min_abs3(float a, float b, float c) {
+  float r;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
+  return r;
+}
+// Square root and reciprocals of the special-function unit (relative error about 2^-22; denormals count as zero in the
+// reciprocals).
 __device__ __forceinline__ float fast_sqrt(float x) {
   float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 __device__ __forceinline__ float fast_rsqrt(float x) {

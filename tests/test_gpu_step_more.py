@@ -90,3 +90,55 @@ def test_masters_of_a_loaded_state_are_taken_as_they_are(P):
         opt.step()
         other.step()
         assert torch.equal(opt.master, other.master) and all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+# ---- second moments at the bottom of fp32's range
+
+@pytest.mark.parametrize("state", ["fp32", "e4m3"])
+@pytest.mark.parametrize("size", [1e-14, 1e-16, 1e-18, 1e-19, 2e-20])
+def test_small_second_moments(P, state, size):
+    """eps = 0, so that the update shows the root.  v = 0.001 g^2 has two roundings, in the subnormal range of half of
+    2^-149 each: its root is off by a relative 2^-150 / v and the usual 2^-20."""
+    from paper_2209_13258_b200.optim import AdamW
+    n = 5000
+    p = torch.nn.Parameter(torch.zeros(n, device="cuda"))
+    p.grad = torch.where(torch.arange(n, device="cuda") % 2 == 0, size, -size) * (1 + gen(3)(n).abs())
+    opt = AdamW([p], lr=1.0, betas=(0.9, 0.999), eps=0.0, weight_decay=0.0, state_dtype=state)
+    opt.step()
+    zero = torch.zeros(n, dtype=F64, device="cuda")
+    _, _, v, upd = step64(zero, p.grad.double(), zero, zero, 1, 1.0, 0.9, 0.999, 0.0, 0.0)
+    assert bool(((p.detach().double() + upd).abs() <= upd.abs() * (2.0 ** -20 + 2.0 ** -150 / v)).all())
+    root = states(opt, 0)[1].sqrt()
+    want = v.sqrt()
+    off = want * (2.0 ** -22 + 2.0 ** -150 / v)
+    if state == "e4m3":
+        at = torch.arange(n, device="cuda") // QB
+        off = off + torch.maximum(want * 2.0 ** -4, opt.exp_avg_sq_scale[at].double() * 2.0 ** -10) * 1.0001
+    assert bool(((root - want).abs() <= off).all())
+
+
+def test_codes_of_small_gradients_are_those_of_the_formulas_op_by_op(P):
+    """As test_codes_are_those_of_the_formulas_op_by_op, with second moments on both sides of 2^-126 and of 2^-100."""
+    from paper_2209_13258_b200.optim import AdamW
+    n, b1, b2 = 1 << 20, 0.9, 0.95
+    rnd = gen(32)
+    p = torch.nn.Parameter(rnd(n) * 0.05)
+    opt = AdamW([p], lr=1e-3, betas=(b1, b2), state_dtype="e4m3")
+    m = v = torch.zeros(n, device="cuda")
+    for t in range(4):
+        g = 1e-17 * rnd(n) * torch.exp(2 * rnd(n // QB, 1)).expand(-1, QB).reshape(-1) * (rnd(n) > -1.5)
+        p.grad = g
+        opt.step()
+        m = m * b1 + g * (1.0 - b1)
+        v = v * b2 + (g * g) * (1.0 - b2)
+        root = v.sqrt()
+        for x, codes, scales in ((m, opt.exp_avg, opt.exp_avg_scale), (root, opt.exp_avg_sq, opt.exp_avg_sq_scale)):
+            top = x.view(-1, QB).abs().amax(1)
+            c = x.view(-1, QB) * (top.reciprocal() * 448.0)[:, None]
+            if x is root:
+                c = torch.where(x.view(-1, QB) > 0, c.clamp_min(2.0 ** -9), c)
+            want = c.to(torch.float8_e4m3fn).view(-1).float()
+            assert torch.equal(codes.float(), want)
+            assert torch.equal(scales, top * (1.0 / 448.0))
+        m = (opt.exp_avg.float().view(-1, QB) * opt.exp_avg_scale[:, None]).view(-1)
+        v = (opt.exp_avg_sq.float().view(-1, QB) * opt.exp_avg_sq_scale[:, None]).view(-1).square()
