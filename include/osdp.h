@@ -91,6 +91,7 @@ extern "C" {
 #define OSDP_DTYPE_BF16 0
 #define OSDP_DTYPE_FP32 1
 #define OSDP_DTYPE_E4M3 2             /* optimiser states only: 8-bit codes with a scale per OSDP_ADAMW_BLOCK elements */
+#define OSDP_DTYPE_E4M3_DITHERED 3    /* the same codes, rounded with a dither whatever the betas */
 
 #define OSDP_NORM_NONE 0
 #define OSDP_NORM_RMS 1
@@ -426,6 +427,11 @@ int osdp_grad_norm(const osdp_adamw_tensor *tensors, int n_tensors, int grad_dty
  *            OSDP_DTYPE_E4M3: e4m3 codes of m and of sqrt(v), value = code * scale_m / scale_v [offset / OSDP_ADAMW_BLOCK].
  *            A scale is the block's largest magnitude / 448; a block below 2^-100 is stored as zeros; the code of a root
  *            above zero is at least the smallest positive one.  The step uses m and v before they are rounded.
+ *            A moment whose beta is at most 0.975 is rounded to the nearest code.  Beyond that a step moves it by so little
+ *            that the nearest code would often be the one it has, for good; it is rounded up or down at random, right
+ *            on average.  The bits for it are a function of the element's offset and of `step`: the same call gives
+ *            the same states.  OSDP_DTYPE_E4M3_DITHERED rounds both moments that way whatever the betas (for gradients with
+ *            next to no noise of their own); states of either code can be continued with the other.
  *            A gradient whose square is not finite spoils the states and parameters of its block.
  *   clip     output of osdp_grad_norm or NULL.  If its coefficient is not finite nothing at all is updated.
  * All arithmetic per element is in a fixed order; the call is deterministic. */

@@ -15,7 +15,7 @@ from .binding import (  # noqa: F401
     osdp_plan_cost, osdp_plan_search, osdp_plan_expand_slices, osdp_plan_search_granularity,
     osdp_split_linear_fwd_f8, osdp_split_linear_bwd_f8, osdp_zdp_linear_bwd_slice_scatter,
     osdp_zdp_mlp_fwd_slice, osdp_zdp_mlp_bwd_slice,
-    ADAMW_BLOCK, BLOCK_NORM_MAX_D, DTYPE_E4M3, NORM_LAYER, NORM_NONE, NORM_RMS, AdamWTensor,
+    ADAMW_BLOCK, BLOCK_NORM_MAX_D, DTYPE_E4M3, DTYPE_E4M3_DITHERED, NORM_LAYER, NORM_NONE, NORM_RMS, AdamWTensor,
     osdp_block_norm_fwd, osdp_block_norm_bwd, osdp_block_norm_workspace_bytes,
     osdp_adamw_layout, osdp_adamw_step, osdp_grad_norm, osdp_grad_norm_workspace_bytes,
     osdp_quantize_rows_i8, osdp_split_linear_fwd_i8, osdp_i8_workspace_bytes,

@@ -14,7 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 
 SPLIT_OUT, SPLIT_RED = 0, 1
 ACT_NONE, ACT_GELU_TANH, ACT_GELU_ERF = 0, 1, 2
-DTYPE_BF16, DTYPE_FP32, DTYPE_E4M3 = 0, 1, 2
+DTYPE_BF16, DTYPE_FP32, DTYPE_E4M3, DTYPE_E4M3_DITHERED = 0, 1, 2, 3
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 ADAMW_BLOCK, BLOCK_NORM_MAX_D = 256, 16384
 OP_LINEAR_FWD, OP_LINEAR_BWD, OP_MLP_FWD, OP_MLP_BWD = 0, 1, 2, 3

@@ -9,6 +9,15 @@
 // (448 is the largest e4m3 value).  The second moment is kept as its root, which halves the range that the codes have
 // to cover (2^-9 ... 448 of a root is 10 decades of v), and a root above zero is never rounded to zero: that would turn
 // a small second moment into a huge step.  The step itself uses the unrounded m and v.
+//
+// Rounding to nearest holds a moment where it is as long as a step moves it by less than half a code, 3 to 6 % of it, and
+// beta close to one moves it by 1 - beta at most.  After half of a block's gradients had become five times smaller, their
+// stored root was, 5 / (1 - beta2) and then 50 / (1 - beta2) steps later, too large by a factor of
+//   beta2 0.95: 1.4 and 1.05,  0.97: 3.6 and 1.2,  0.98: 6 and 6,  0.99: 6 and 6.5,  0.999: 5 and 4.5    (normal gradients)
+// while with a dither before the rounding, which makes it right on average, it was 1.10 and 1.02 at every one of them.
+// So a moment whose beta is above DITHER_ABOVE is rounded with the dither.  Nearest is better below: a moment that is
+// renewed within some dozen steps carries the noise of the gradients, which is dither enough, and the codes' own error is half.
+// The dither takes 537 M parameters from 874 to 1035 us for one moment, 1175 for both (instructions).
 #include "../../include/osdp.h"
 
 #include <cmath>
@@ -24,6 +33,7 @@ constexpr int QB = OSDP_ADAMW_BLOCK;       // elements per 8-bit scale; one warp
 constexpr int THREADS = 256;
 constexpr int CHUNK = 4096;                // elements of one tensor that a thread block works on
 constexpr int STATUS_BYTES = 256;
+constexpr double DITHER_ABOVE = 0.975;
 constexpr float TINY = 7.888609052210118e-31f;   // 2^-100: a block whose largest magnitude is below it is stored as zeros
 
 struct Entry {
@@ -62,7 +72,28 @@ struct Hyper {
   float b1, one_minus_b1, b2, one_minus_b2, eps;
   float root_scale;    // 1 / sqrt(1 - b2^t)
   float one;           // 1, but not to the compiler: a * one + b is a sum that it cannot merge with the product a
+  uint32_t seed;       // of the dither: the step's number
+  int dither_m, dither_v;
 };
+
+enum States { F32, CODES, DITHERED };   // fp32; 8-bit codes; 8-bit codes of which m's, v's or both are dithered
+
+// Random bits for eight consecutive elements from their number (the first one's index in the flat states / 8) and the step's:
+// products with odd numbers (2^32 / the golden ratio, / sqrt 2, (sqrt 3 - 1) 2^32) and shifted sums in turn.  Element j of
+// moment k (0 m, 1 v) takes the upper 20 bits of 2 (j + 8 k) + 1 times the result.
+__device__ __forceinline__ uint32_t dither_bits(unsigned long long group, uint32_t seed) {
+  uint32_t x = (uint32_t)group ^ (uint32_t)(group >> 32) * 0xB504F333u ^ seed * 0xBB67AE85u;
+  x = (x ^ x >> 16) * 0xB504F333u;
+  x = (x ^ x >> 15) * 0x9E3779B9u;
+  return (x ^ x >> 16) * 0x9E3779B9u;
+}
+// x (|x| <= 448) to a value of e4m3, up or down with the probabilities that make it x on average.  A code has three
+// mantissa bits below the leading one, 2^-9 at least: magnitudes below 2^-6 are moved up by 2^-6, where that is the step; the
+// dither is added to the bits behind it and what is left of them cut off.
+__device__ __forceinline__ float dither1(float x, uint32_t bits) {
+  const float a = fabsf(x), up = a < 0.015625f ? 0.015625f : 0.f;
+  return copysignf(__uint_as_float((__float_as_uint(a + up) + (bits >> 12)) & 0xFFF00000u) - up, x);
+}
 
 __device__ __forceinline__ bool has_zero_byte(uint32_t w) { return ((w - 0x01010101u) & ~w & 0x80808080u) != 0u; }
 
@@ -87,8 +118,9 @@ __device__ __forceinline__ float root_of_small(float minus_v, float root) { retu
 
 // 256 elements -> codes and their scale.  ROOT: x holds negated roots; those of numbers above zero keep at least the smallest
 // code.
-template <bool ROOT>
-__device__ __forceinline__ void quantise_block(const f2 (&x)[4], uint8_t *codes, float *scale, int lane) {
+// DITHER: rounded with a dither if `dither` is set; `bits` = dither_bits of the lane's elements.
+template <bool ROOT, bool DITHER>
+__device__ __forceinline__ void quantise_block(const f2 (&x)[4], uint8_t *codes, float *scale, int lane, bool dither, uint32_t bits) {
   float top = 0.f;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -102,6 +134,14 @@ __device__ __forceinline__ void quantise_block(const f2 (&x)[4], uint8_t *codes,
   f2 c[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) c[j] = ROOT ? fma2(x[j], inv2, both(0.0f)) : mul2(x[j], inv2);   // a root's zero has the code of +0
+  if (DITHER && dither) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 v = split2(c[j]);
+      const uint32_t n = (ROOT ? 16 : 0) + 4 * j + 1;
+      c[j] = pack2(dither1(v.x, bits * n), dither1(v.y, bits * (n + 2)));
+    }
+  }
   uint2 q = encode_e4m3x8(c);
   if (ROOT && (has_zero_byte(q.x) || has_zero_byte(q.y))) {   // rare: an element that is zero, or very small in its block
 #pragma unroll
@@ -168,10 +208,11 @@ struct RawState {
 // of 6547, the gradient norm before it included).  With 8-bit states (10 bytes an element) the instructions come near: 64 an
 // element in scalar form took 1450 us for 537 M parameters, some 45 an element with pairs of fp32, approximate reciprocals
 // and the rare paths set apart take 870 us at full clocks (6200 GB/s) and 974 us in the power-capped state.
-template <typename T, bool MASTER, bool E4M3, int MAXT>
+template <typename T, bool MASTER, States STATES, int MAXT>
 __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ Table<MAXT> t, const Hyper h, float *master,
                                                         void *state_m, void *state_v, float *scale_m, float *scale_v,
                                                         const float *__restrict__ clip) {
+  constexpr bool E4M3 = STATES != F32, DITHER = STATES == DITHERED;
   constexpr int WARPS = THREADS / 32, PER_WARP = CHUNK / (WARPS * QB), BLOCKS = E4M3 ? PER_WARP : 1;
   pdl_launch_dependents();
   // After the gradient norm the last gradients that it read are still in L2: those first.
@@ -292,8 +333,9 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
       }
       if constexpr (E4M3) {
         const long long sb = (e.state + blk) / QB;
-        quantise_block<false>(m, static_cast<uint8_t *>(state_m) + (e.state + blk), scale_m + sb, lane);
-        quantise_block<true>(root, static_cast<uint8_t *>(state_v) + (e.state + blk), scale_v + sb, lane);
+        const uint32_t bits = DITHER ? dither_bits((unsigned long long)si >> 3, h.seed) : 0u;
+        quantise_block<false, DITHER>(m, static_cast<uint8_t *>(state_m) + (e.state + blk), scale_m + sb, lane, h.dither_m != 0, bits);
+        quantise_block<true, DITHER>(root, static_cast<uint8_t *>(state_v) + (e.state + blk), scale_v + sb, lane, h.dither_v != 0, bits);
       } else {
         store4(static_cast<float *>(state_m) + si, m);
         store4(static_cast<float *>(state_v) + si, v);
@@ -419,7 +461,7 @@ int for_each_table(const osdp_adamw_tensor *t, int n, int dtype, bool with_param
   return OSDP_OK;
 }
 
-template <typename T, bool MASTER, bool E4M3, int MAXT>
+template <typename T, bool MASTER, States STATES, int MAXT>
 int launch_adamw(const osdp_adamw_tensor *t, int n, int dtype, const Hyper &h, double beta1_t, float *master, void *m, void *v,
                  float *sm, float *sv, const float *clip, cudaStream_t stream) {
   return for_each_table<MAXT>(
@@ -429,17 +471,17 @@ int launch_adamw(const osdp_adamw_tensor *t, int n, int dtype, const Hyper &h, d
         e.size = (float)(a.lr / (1.0 - beta1_t));
       },
       [&](const Table<MAXT> &tab) {
-        return launch_overlapped(adamw_kernel<T, MASTER, E4M3, MAXT>, dim3((unsigned)tab.chunks), dim3(THREADS), 0, 1, stream, tab, h,
+        return launch_overlapped(adamw_kernel<T, MASTER, STATES, MAXT>, dim3((unsigned)tab.chunks), dim3(THREADS), 0, 1, stream, tab, h,
                                  master, m, v, sm, sv, clip);
       });
 }
 
-template <typename T, bool MASTER, bool E4M3>
+template <typename T, bool MASTER, States STATES>
 int pick_table(const osdp_adamw_tensor *t, int n, int dtype, const Hyper &h, double b1t, float *master, void *m, void *v, float *sm,
                float *sv, const float *clip, cudaStream_t stream) {
-  if (n <= TABLE_SMALL) return launch_adamw<T, MASTER, E4M3, TABLE_SMALL>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream);
-  if (n <= TABLE_MIDDLE) return launch_adamw<T, MASTER, E4M3, TABLE_MIDDLE>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream);
-  return launch_adamw<T, MASTER, E4M3, TABLE_LARGE>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream);
+  if (n <= TABLE_SMALL) return launch_adamw<T, MASTER, STATES, TABLE_SMALL>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream);
+  if (n <= TABLE_MIDDLE) return launch_adamw<T, MASTER, STATES, TABLE_MIDDLE>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream);
+  return launch_adamw<T, MASTER, STATES, TABLE_LARGE>(t, n, dtype, h, b1t, master, m, v, sm, sv, clip, stream);
 }
 
 template <typename T, int MAXT>
@@ -522,8 +564,8 @@ int osdp_adamw_step(const osdp_adamw_tensor *tensors, int n_tensors, int param_d
                     int64_t step, const float *clip, void *stream) {
   int rc = check_tensors(tensors, n_tensors, param_dtype, true);
   if (rc) return rc;
-  if (state_dtype != OSDP_DTYPE_FP32 && state_dtype != OSDP_DTYPE_E4M3) return OSDP_ERR_UNSUPPORTED;
-  const bool e4m3 = state_dtype == OSDP_DTYPE_E4M3;
+  if (state_dtype != OSDP_DTYPE_FP32 && state_dtype != OSDP_DTYPE_E4M3 && state_dtype != OSDP_DTYPE_E4M3_DITHERED) return OSDP_ERR_UNSUPPORTED;
+  const bool e4m3 = state_dtype != OSDP_DTYPE_FP32, all = state_dtype == OSDP_DTYPE_E4M3_DITHERED;
   if (step < 1 || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 0.0) || !std::isfinite(eps))
     return OSDP_ERR_UNSUPPORTED;
   int64_t total = 0;
@@ -544,14 +586,20 @@ int osdp_adamw_step(const osdp_adamw_tensor *tensors, int n_tensors, int param_d
   h.one_minus_b2 = (float)(1.0 - beta2);
   h.eps = (float)eps;
   h.one = 1.0f;
+  h.seed = (uint32_t)step;
+  h.dither_m = all || beta1 > DITHER_ABOVE;
+  h.dither_v = all || beta2 > DITHER_ABOVE;
+  const States states = !e4m3 ? F32 : h.dither_m || h.dither_v ? DITHERED : CODES;
   h.root_scale = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
   const double b1t = std::pow(beta1, (double)step);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-#define OSDP_STEP(T, MASTER, E4M3) \
-  pick_table<T, MASTER, E4M3>(tensors, n_tensors, param_dtype, h, b1t, master, state_m, state_v, scale_m, scale_v, clip, s)
-  if (param_dtype == OSDP_DTYPE_FP32) return e4m3 ? OSDP_STEP(float, false, true) : OSDP_STEP(float, false, false);
-  if (master) return e4m3 ? OSDP_STEP(__nv_bfloat16, true, true) : OSDP_STEP(__nv_bfloat16, true, false);
-  return e4m3 ? OSDP_STEP(__nv_bfloat16, false, true) : OSDP_STEP(__nv_bfloat16, false, false);
+#define OSDP_STEP(T, MASTER, STATES) \
+  pick_table<T, MASTER, STATES>(tensors, n_tensors, param_dtype, h, b1t, master, state_m, state_v, scale_m, scale_v, clip, s)
+#define OSDP_STEP_OF(T, MASTER) \
+  (states == F32 ? OSDP_STEP(T, MASTER, F32) : states == CODES ? OSDP_STEP(T, MASTER, CODES) : OSDP_STEP(T, MASTER, DITHERED))
+  if (param_dtype == OSDP_DTYPE_FP32) return OSDP_STEP_OF(float, false);
+  return master ? OSDP_STEP_OF(__nv_bfloat16, true) : OSDP_STEP_OF(__nv_bfloat16, false);
+#undef OSDP_STEP_OF
 #undef OSDP_STEP
 }
 

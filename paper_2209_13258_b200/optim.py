@@ -16,6 +16,7 @@ _TENSOR = np.dtype([("param", np.uint64), ("grad", np.uint64), ("numel", np.int6
                     ("lr", np.float64), ("weight_decay", np.float64)])      # osdp_adamw_tensor
 
 
+_STATES = {"fp32": B.DTYPE_FP32, "e4m3": B.DTYPE_E4M3, "e4m3_dithered": B.DTYPE_E4M3_DITHERED}
 _GRAD, _DTYPE, _VERSION = operator.attrgetter("grad"), operator.attrgetter("dtype"), operator.attrgetter("_version")
 _DATA_PTR, _NUMEL, _DEVICE, _IS_CONTIGUOUS = torch.Tensor.data_ptr, torch.Tensor.numel, torch.Tensor.get_device, torch.Tensor.is_contiguous
 
@@ -31,6 +32,9 @@ class AdamW(torch.optim.Optimizer):
 
     state_dtype  "fp32", or "e4m3": both moments as 8-bit codes with one fp32 scale per 256 elements (2.03 bytes per
                  parameter instead of 8; the second moment is kept as its root).
+                 A moment whose beta is at most 0.975 is rounded to the nearest code, others up or down at random
+                 (repeatably: by element and step), since the nearest code would hold them where they are.  "e4m3_dithered":
+                 at random whatever the betas, for gradients with next to no noise of their own.
     master       bf16 parameters only: the step works on fp32 copies of the parameters (4 bytes each) and writes their
                  rounding.  Without it an update below half a unit in the last place of a bf16 parameter is lost.
                  Parameters that change outside the step (weights loaded, averaged or initialised again: any in-place
@@ -44,7 +48,7 @@ class AdamW(torch.optim.Optimizer):
     All parameter groups are stepped together: ``lr`` and ``weight_decay`` may differ between groups, ``betas`` and
     ``eps`` may not.  Parameters whose ``.grad`` is None are left alone.  ``steps`` counts the steps done (one count for
     all parameters: it sets the bias correction).  States are flat over all parameters, each parameter's part starting
-    at a multiple of 256 elements (``offsets``): ``exp_avg``, ``exp_avg_sq`` (with "e4m3" the codes of the second
+    at a multiple of 256 elements (``offsets``): ``exp_avg``, ``exp_avg_sq`` (in 8 bits the codes of the second
     moment's root), ``exp_avg_scale``, ``exp_avg_sq_scale``, ``master``.  A CUDA graph of a step replays that step's
     bias correction, rates and gradients' addresses.  ``grad_norm`` [2]: the last step's norm and
     coefficient, on the device.
@@ -52,8 +56,8 @@ class AdamW(torch.optim.Optimizer):
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_dtype="fp32", master=False,
                  max_norm=None):
-        if state_dtype not in ("fp32", "e4m3"):
-            raise ValueError('state_dtype is "fp32" or "e4m3"')
+        if state_dtype not in _STATES:
+            raise ValueError('state_dtype is "fp32", "e4m3" or "e4m3_dithered"')
         self._built = False
         super().__init__(params, {"lr": lr, "betas": tuple(betas), "eps": eps, "weight_decay": weight_decay})
         self._params = [p for g in self.param_groups for p in g["params"]]
@@ -71,16 +75,17 @@ class AdamW(torch.optim.Optimizer):
             raise ValueError("fp32 parameters are their own master")
         self._torch_dtype, self._device = first.dtype, first.device
         self._dtype = B.DTYPE_FP32 if first.dtype == torch.float32 else B.DTYPE_BF16
-        self._state_dtype = B.DTYPE_E4M3 if state_dtype == "e4m3" else B.DTYPE_FP32
+        self._state_dtype = _STATES[state_dtype]
+        eight = state_dtype != "fp32"
         rc, self.offsets, total = B.osdp_adamw_layout([p.numel() for p in self._params])
         if rc:
             raise B.OsdpError(rc, "osdp_adamw_layout")
         dev = first.device
         new = lambda n, dt: torch.zeros(n, dtype=dt, device=dev)      # noqa: E731
-        sdt = torch.float8_e4m3fn if state_dtype == "e4m3" else torch.float32
+        sdt = torch.float8_e4m3fn if eight else torch.float32
         self.exp_avg, self.exp_avg_sq = new(total, sdt), new(total, sdt)
         blocks = total // B.ADAMW_BLOCK
-        self.exp_avg_scale, self.exp_avg_sq_scale = (new(blocks, torch.float32), new(blocks, torch.float32)) if state_dtype == "e4m3" else (None, None)
+        self.exp_avg_scale, self.exp_avg_sq_scale = (new(blocks, torch.float32), new(blocks, torch.float32)) if eight else (None, None)
         self.master = None
         if master:
             self.master = new(total, torch.float32)
