@@ -5,9 +5,9 @@
 
 A block is  r = x + gate (.) N(MLP(u)),  u' = N'(r): the split MLP (its weights in one flat parameter buffer) between
 fused norms, gate and residual sum (``nn.ResidualNorm``).  All parameters, flat bf16 buffers and fp32 vectors, are
-stepped by ``optim.AdamW``: the bf16 ones with fp32 masters and 8-bit states, gradients clipped on the device.  The
-trained blocks are then run with int8 weights (``nn.Int8Linear``), the norms handing their output over as int8 with a
-scale per token, for a batch and for a single token.  The task is to reproduce a fixed random network of the same form.
+stepped by ``optim.AdamW``: the bf16 ones with fp32 masters and 8-bit states, all gradients clipped by one norm on the
+device.  The trained blocks are then run with int8 weights (``nn.Int8Linear``), the norms handing their output over as
+int8 with a scale per token, for a batch and for a single token.  The task is to reproduce a fixed random network of the same form.
 """
 from __future__ import annotations
 
@@ -21,7 +21,7 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 import paper_2209_13258_b200 as P                                          # noqa: E402
 from paper_2209_13258_b200.nn import Int8Linear, ResidualNorm, SplitMLP    # noqa: E402
-from paper_2209_13258_b200.optim import AdamW                              # noqa: E402
+from paper_2209_13258_b200.optim import AdamW, ClippedStep                 # noqa: E402
 
 
 class Stack(torch.nn.Module):
@@ -79,8 +79,9 @@ def main(argv=None):
         p.requires_grad_(False)
     half = [p for p in student.parameters() if p.dtype == torch.bfloat16]
     full = [p for p in student.parameters() if p.dtype == torch.float32]
-    opts = [AdamW(half, lr=a.lr, weight_decay=0.01, state_dtype="e4m3", master=True, max_norm=1.0),
-            AdamW(full, lr=a.lr, weight_decay=0.0, max_norm=1.0)]
+    # bf16 and fp32 parameters have their own optimisers, and one gradient norm
+    opt = ClippedStep([AdamW(half, lr=a.lr, weight_decay=0.01, state_dtype="e4m3", master=True), AdamW(full, lr=a.lr, weight_decay=0.0)],
+                      max_norm=1.0)
     losses = []
     for step in range(a.steps):
         x = torch.randn(a.tokens, a.hidden, device="cuda")
@@ -88,12 +89,11 @@ def main(argv=None):
             want = teacher(x)
         loss = (student(x) - want).square().mean()
         loss.backward()
-        for o in opts:
-            o.step()
-            o.zero_grad(set_to_none=True)
+        opt.step()
+        opt.zero_grad()
         if step % max(1, a.steps // 10) == 0 or step == a.steps - 1:
             losses.append(float(loss.detach()))
-            print("step %4d  loss %.5f  gradient norm %.4f" % (step, losses[-1], float(opts[0].grad_norm[0])))
+            print("step %4d  loss %.5f  gradient norm %.4f" % (step, losses[-1], float(opt.grad_norm[0])))
     served = Int8Stack(student)
     errors = {}
     for tokens in (64, 1):

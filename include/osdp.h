@@ -416,6 +416,13 @@ int osdp_grad_norm_workspace_bytes(int n_tensors, size_t *bytes);
 int osdp_grad_norm(const osdp_adamw_tensor *tensors, int n_tensors, int grad_dtype, float max_norm, float *out, void *ws,
                    size_t ws_bytes, void *stream);
 
+/* The same in two parts, for a norm over gradients that no single call has: of two dtypes, or of several ranks.
+ * osdp_grad_squares writes the sum of squares of its tensors to *sum (DEVICE); the sums of the parts are brought together
+ * (for ranks: all-reduced), and osdp_clip_coefficient forms out[0], out[1] as above of n_sums of them, added in order. */
+int osdp_grad_squares(const osdp_adamw_tensor *tensors, int n_tensors, int grad_dtype, double *sum, void *ws, size_t ws_bytes,
+                      void *stream);
+int osdp_clip_coefficient(const double *sums, int n_sums, float max_norm, float *out, void *stream);
+
 /* AdamW (decoupled weight decay) over all tensors, one launch per 640 of them; `tensors` is a HOST array that the call
  * does not keep.  Per element, t = step >= 1 and c = clip[1] (1 for clip NULL):
  *     g = c * grad;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
@@ -433,7 +440,7 @@ int osdp_grad_norm(const osdp_adamw_tensor *tensors, int n_tensors, int grad_dty
  *            the same states.  OSDP_DTYPE_E4M3_DITHERED rounds both moments that way whatever the betas (for gradients with
  *            next to no noise of their own); states of either code can be continued with the other.
  *            A gradient whose square is not finite spoils the states and parameters of its block.
- *   clip     output of osdp_grad_norm or NULL.  If its coefficient is not finite nothing at all is updated.
+ *   clip     output of osdp_grad_norm or osdp_clip_coefficient, or NULL.  If its coefficient is not finite nothing at all is updated.
  * All arithmetic per element is in a fixed order; the call is deterministic. */
 int osdp_adamw_step(const osdp_adamw_tensor *tensors, int n_tensors, int param_dtype, int state_dtype, float *master,
                     void *state_m, void *state_v, float *scale_m, float *scale_v, double beta1, double beta2, double eps,

@@ -18,5 +18,6 @@ from .binding import (  # noqa: F401
     ADAMW_BLOCK, BLOCK_NORM_MAX_D, DTYPE_E4M3, DTYPE_E4M3_DITHERED, NORM_LAYER, NORM_NONE, NORM_RMS, AdamWTensor,
     osdp_block_norm_fwd, osdp_block_norm_bwd, osdp_block_norm_workspace_bytes,
     osdp_adamw_layout, osdp_adamw_step, osdp_grad_norm, osdp_grad_norm_workspace_bytes,
+    osdp_grad_squares, osdp_clip_coefficient,
     osdp_quantize_rows_i8, osdp_split_linear_fwd_i8, osdp_i8_workspace_bytes,
 )

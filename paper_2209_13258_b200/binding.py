@@ -30,7 +30,8 @@ EXPORTS = [
     "osdp_split_linear_fwd_f8", "osdp_split_linear_bwd_f8", "osdp_zdp_linear_bwd_slice_scatter",
     "osdp_zdp_mlp_fwd_slice", "osdp_zdp_mlp_bwd_slice",
     "osdp_block_norm_fwd", "osdp_block_norm_bwd", "osdp_block_norm_workspace_bytes",
-    "osdp_adamw_layout", "osdp_adamw_step", "osdp_grad_norm", "osdp_grad_norm_workspace_bytes",
+    "osdp_adamw_layout", "osdp_adamw_step", "osdp_grad_norm", "osdp_grad_norm_workspace_bytes", "osdp_grad_squares",
+    "osdp_clip_coefficient",
     "osdp_quantize_rows_i8", "osdp_split_linear_fwd_i8", "osdp_i8_workspace_bytes",
 ]
 
@@ -115,6 +116,8 @@ def lib():
         L.osdp_adamw_layout.argtypes = [p64, ci, p64, p64]
         L.osdp_grad_norm_workspace_bytes.argtypes = [ci, ctypes.POINTER(sz)]
         L.osdp_grad_norm.argtypes = [vp, ci, ci, f32, vp, vp, sz, vp]
+        L.osdp_grad_squares.argtypes = [vp, ci, ci, vp, vp, sz, vp]
+        L.osdp_clip_coefficient.argtypes = [vp, ci, f32, vp, vp]
         L.osdp_adamw_step.argtypes = [vp, ci, ci, ci, vp, vp, vp, vp, vp, dbl, dbl, dbl, i64, vp, vp]
         L.osdp_i8_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
         L.osdp_quantize_rows_i8.argtypes = [vp, i64, i64, vp, vp, vp]
@@ -477,6 +480,18 @@ def osdp_grad_norm(tensors, n_tensors, grad_dtype, max_norm, out, ws, stream=Non
     wp, wn = _ws(ws)
     rc = lib().osdp_grad_norm(tensors, int(n_tensors), int(grad_dtype), float(max_norm), _ptr(out), wp, wn, _stream(stream))
     return _ret(rc, check, "osdp_grad_norm")
+
+
+def osdp_grad_squares(tensors, n_tensors, grad_dtype, sum, ws, stream=None, check=False):
+    """sum: one fp64 value on the device."""
+    wp, wn = _ws(ws)
+    rc = lib().osdp_grad_squares(tensors, int(n_tensors), int(grad_dtype), _ptr(sum), wp, wn, _stream(stream))
+    return _ret(rc, check, "osdp_grad_squares")
+
+
+def osdp_clip_coefficient(sums, n_sums, max_norm, out, stream=None, check=False):
+    rc = lib().osdp_clip_coefficient(_ptr(sums), int(n_sums), float(max_norm), _ptr(out), _stream(stream))
+    return _ret(rc, check, "osdp_clip_coefficient")
 
 
 def osdp_adamw_step(tensors, n_tensors, param_dtype, state_dtype, master, state_m, state_v, scale_m, scale_v, beta1, beta2, eps,

@@ -350,10 +350,17 @@ __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ 
 constexpr int NORM_BLOCKS = 592;   // 4 per SM
 constexpr int NORM_CHUNK = 16384;  // eight vectors per thread, all loads issued before the first is used
 
+__device__ __forceinline__ void clip_coefficient(double squares, float max_norm, float *out) {
+  const float norm = (float)sqrt(squares);
+  out[0] = norm;
+  // a norm that is not finite has no coefficient: the step that reads NaN changes nothing
+  out[1] = !isfinite(norm) ? __int_as_float(0x7FC00000) : max_norm > 0.f ? fminf(max_norm / (norm + 1e-6f), 1.0f) : 1.0f;
+}
+
 template <typename T, int MAXT>
 __global__ void __launch_bounds__(THREADS) grad_norm_kernel(const __grid_constant__ Table<MAXT> t, float *partial, int first_partial,
                                                             int total_partials, unsigned *ticket, float max_norm,
-                                                            float *__restrict__ out) {
+                                                            float *out, double *squares) {
   __shared__ float red[THREADS / 32];
   __shared__ bool last;
   pdl_launch_dependents();
@@ -406,12 +413,20 @@ __global__ void __launch_bounds__(THREADS) grad_norm_kernel(const __grid_constan
     __syncthreads();
   }
   if (threadIdx.x == 0) {
-    const float norm = (float)sqrt(sum[0]);
-    out[0] = norm;
-    // a norm that is not finite has no coefficient: the step that reads NaN changes nothing
-    out[1] = !isfinite(norm) ? __int_as_float(0x7FC00000) : max_norm > 0.f ? fminf(max_norm / (norm + 1e-6f), 1.0f) : 1.0f;
+    if (squares) *squares = sum[0];
+    else clip_coefficient(sum[0], max_norm, out);
     *ticket = 0u;
   }
+}
+
+// The coefficient of sums of squares that were taken apart (by dtype, by rank).
+__global__ void __launch_bounds__(32) clip_kernel(const double *sums, int n, float max_norm, float *out) {
+  pdl_launch_dependents();
+  pdl_wait();
+  if (threadIdx.x != 0) return;
+  double s = 0.0;
+  for (int k = 0; k < n; ++k) s += sums[k];
+  clip_coefficient(s, max_norm, out);
 }
 
 int check_tensors(const osdp_adamw_tensor *t, int n, int dtype, bool need_param) {
@@ -485,7 +500,7 @@ int pick_table(const osdp_adamw_tensor *t, int n, int dtype, const Hyper &h, dou
 }
 
 template <typename T, int MAXT>
-int launch_norm(const osdp_adamw_tensor *t, int n, int dtype, float max_norm, float *out, float *partial, unsigned *ticket,
+int launch_norm(const osdp_adamw_tensor *t, int n, int dtype, float max_norm, float *out, double *squares, float *partial, unsigned *ticket,
                 cudaStream_t stream) {
   // the number of partial sums has to be known before the first launch
   int total = 0;
@@ -497,20 +512,38 @@ int launch_norm(const osdp_adamw_tensor *t, int n, int dtype, float max_norm, fl
   empty.n = 0;
   empty.chunks = 0;
   if (total == 0)   // no elements at all: the norm is zero
-    return launch_overlapped(grad_norm_kernel<T, MAXT>, dim3(1), dim3(THREADS), 0, 1, stream, empty, partial, 0, 1, ticket, max_norm, out);
+    return launch_overlapped(grad_norm_kernel<T, MAXT>, dim3(1), dim3(THREADS), 0, 1, stream, empty, partial, 0, 1, ticket, max_norm, out, squares);
   int at = 0;
   return for_each_table<MAXT>(t, n, dtype, false, NORM_CHUNK, none, [&](const Table<MAXT> &tab) {
     const int b = blocks(tab.chunks);
     const int first = at;
     at += b;
     return launch_overlapped(grad_norm_kernel<T, MAXT>, dim3((unsigned)b), dim3(THREADS), 0, 1, stream, tab, partial, first, total, ticket,
-                             max_norm, out);
+                             max_norm, out, squares);
   });
 }
 
 size_t norm_workspace(int n) {
   const size_t tables = (size_t)cdiv(n > 0 ? n : 1, TABLE_LARGE);
   return STATUS_BYTES + tables * NORM_BLOCKS * sizeof(float);
+}
+
+// Norm and coefficient into `out`, or the sum of squares into `squares`.
+int norm_of(const osdp_adamw_tensor *tensors, int n_tensors, int dtype, float max_norm, float *out, double *squares, void *ws,
+            size_t ws_bytes, cudaStream_t s) {
+  const int rc = check_tensors(tensors, n_tensors, dtype, false);
+  if (rc) return rc;
+  if ((!out && !squares) || !ws) return OSDP_ERR_NULL_POINTER;
+  if (!aligned_to(ws, 256) || !aligned_to(out, 4) || !aligned_to(squares, 8)) return OSDP_ERR_ALIGNMENT;
+  if (ws_bytes < norm_workspace(n_tensors)) return OSDP_ERR_WORKSPACE_TOO_SMALL;
+  unsigned *ticket = reinterpret_cast<unsigned *>(static_cast<char *>(ws) + 64);
+  float *partial = reinterpret_cast<float *>(static_cast<char *>(ws) + STATUS_BYTES);
+#define OSDP_NORM(T) \
+  (n_tensors <= TABLE_SMALL ? launch_norm<T, TABLE_SMALL>(tensors, n_tensors, dtype, max_norm, out, squares, partial, ticket, s) \
+   : n_tensors <= TABLE_MIDDLE ? launch_norm<T, TABLE_MIDDLE>(tensors, n_tensors, dtype, max_norm, out, squares, partial, ticket, s) \
+                               : launch_norm<T, TABLE_LARGE>(tensors, n_tensors, dtype, max_norm, out, squares, partial, ticket, s))
+  return dtype == OSDP_DTYPE_FP32 ? OSDP_NORM(float) : OSDP_NORM(__nv_bfloat16);
+#undef OSDP_NORM
 }
 
 }  // namespace
@@ -542,21 +575,21 @@ int osdp_grad_norm_workspace_bytes(int n_tensors, size_t *bytes) {
 
 int osdp_grad_norm(const osdp_adamw_tensor *tensors, int n_tensors, int grad_dtype, float max_norm, float *out, void *ws,
                    size_t ws_bytes, void *stream) {
-  const int rc = check_tensors(tensors, n_tensors, grad_dtype, false);
-  if (rc) return rc;
-  if (!out || !ws) return OSDP_ERR_NULL_POINTER;
   if (std::isnan(max_norm)) return OSDP_ERR_UNSUPPORTED;
-  if (!aligned_to(ws, 256) || !aligned_to(out, 4)) return OSDP_ERR_ALIGNMENT;
-  if (ws_bytes < norm_workspace(n_tensors)) return OSDP_ERR_WORKSPACE_TOO_SMALL;
-  unsigned *ticket = reinterpret_cast<unsigned *>(static_cast<char *>(ws) + 64);
-  float *partial = reinterpret_cast<float *>(static_cast<char *>(ws) + STATUS_BYTES);
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-#define OSDP_NORM(T) \
-  (n_tensors <= TABLE_SMALL ? launch_norm<T, TABLE_SMALL>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s) \
-   : n_tensors <= TABLE_MIDDLE ? launch_norm<T, TABLE_MIDDLE>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s) \
-                               : launch_norm<T, TABLE_LARGE>(tensors, n_tensors, grad_dtype, max_norm, out, partial, ticket, s))
-  return grad_dtype == OSDP_DTYPE_FP32 ? OSDP_NORM(float) : OSDP_NORM(__nv_bfloat16);
-#undef OSDP_NORM
+  return norm_of(tensors, n_tensors, grad_dtype, max_norm, out, nullptr, ws, ws_bytes, static_cast<cudaStream_t>(stream));
+}
+
+int osdp_grad_squares(const osdp_adamw_tensor *tensors, int n_tensors, int grad_dtype, double *sum, void *ws, size_t ws_bytes,
+                      void *stream) {
+  return norm_of(tensors, n_tensors, grad_dtype, 0.f, nullptr, sum, ws, ws_bytes, static_cast<cudaStream_t>(stream));
+}
+
+int osdp_clip_coefficient(const double *sums, int n_sums, float max_norm, float *out, void *stream) {
+  if (n_sums < 0 || n_sums > (1 << 20)) return OSDP_ERR_BAD_SHAPE;
+  if (!out || (n_sums > 0 && !sums)) return OSDP_ERR_NULL_POINTER;
+  if (std::isnan(max_norm)) return OSDP_ERR_UNSUPPORTED;
+  if (!aligned_to(sums, 8) || !aligned_to(out, 4)) return OSDP_ERR_ALIGNMENT;
+  return launch_overlapped(clip_kernel, dim3(1), dim3(32), 0, 1, static_cast<cudaStream_t>(stream), sums, n_sums, max_norm, out);
 }
 
 int osdp_adamw_step(const osdp_adamw_tensor *tensors, int n_tensors, int param_dtype, int state_dtype, float *master,

@@ -298,8 +298,8 @@ class ZdpLinear(torch.nn.Module):
 
     Parameters: `shard` (bf16, this rank's part of every ZDP slice), `dp_parts` (the DP slices' compact matrices),
     `bias` (fp32, replicated).  After backward their `.grad` hold this rank's part of the gradient summed over
-    ranks (bf16 for the weights, fp32 for the bias), ready for a sharded optimiser step.  Every rank passes its
-    own tokens.  Collectives run on the layer's communication stream, overlapped with the slice GEMMs.
+    ranks (bf16 for the weights, fp32 for the bias), ready for a sharded optimiser step (``optim.ClippedStep`` clips by
+    the norm over all ranks, with ``shard`` in a group marked as sharded).  Every rank passes its own tokens.  Collectives run on the layer's communication stream, overlapped with the slice GEMMs.
     """
 
     def __init__(self, in_features, out_features, bias=True, k_split=1, split_dim=B.SPLIT_OUT, act=B.ACT_NONE,

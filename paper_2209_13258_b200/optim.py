@@ -41,12 +41,14 @@ class AdamW(torch.optim.Optimizer):
                  operation on them, or new ``.data``) are noticed by the next step, which takes the changed elements over
                  into the masters.  Writes through ``p.data`` or by another library's kernels leave no trace:
                  call ``refresh_masters()`` after them.
-    max_norm     clips the gradients by their global norm over all parameters of the step, without a host round trip.
+    max_norm     clips the gradients by their norm over all parameters of the step, without a host round trip.  That is
+                 this optimiser's norm on this rank: parameters of two dtypes, or sharded over ranks, have to be clipped
+                 together, or their parts are scaled differently (and replicated parameters drift apart): ``ClippedStep``.
                  A step whose norm is not finite changes no parameter and no state (``grad_norm[0]`` says so); it counts as
                  a step all the same, since the host does not wait to learn of it.
 
     All parameter groups are stepped together: ``lr`` and ``weight_decay`` may differ between groups, ``betas`` and
-    ``eps`` may not.  Parameters whose ``.grad`` is None are left alone.  ``steps`` counts the steps done (one count for
+    ``eps`` may not.  A group with ``"sharded": True`` says that every rank has other elements of its parameters.  Parameters whose ``.grad`` is None are left alone.  ``steps`` counts the steps done (one count for
     all parameters: it sets the bias correction).  States are flat over all parameters, each parameter's part starting
     at a multiple of 256 elements (``offsets``): ``exp_avg``, ``exp_avg_sq`` (in 8 bits the codes of the second
     moment's root), ``exp_avg_scale``, ``exp_avg_sq_scale``, ``master``.  A CUDA graph of a step replays that step's
@@ -100,6 +102,8 @@ class AdamW(torch.optim.Optimizer):
         # parameters in order
         self._sizes = [p.numel() for p in self._params]
         self._group_of = [i for i, g in enumerate(self.param_groups) for _ in g["params"]]
+        self.sharded = np.array([bool(g.get("sharded", False)) for g in self.param_groups for _ in g["params"]])
+        self._clip = None       # coefficient from outside, while a ClippedStep steps
         self._table = np.zeros(n, dtype=_TENSOR)
         self._whole, self._rates = False, None
         # parameters and gradients as one step found them in order; a few times anew, if what comes changes
@@ -141,7 +145,7 @@ class AdamW(torch.optim.Optimizer):
 
     def _fill(self):
         """The table of this step: addresses as they are now; tensors without a gradient are left out.  Returns its
-        length and the copies of gradients that were not contiguous."""
+        length, the copies of gradients that were not contiguous, and the indices of its parameters (None: all)."""
         params, table, sizes = self._params, self._table, self._sizes
         grads, at, keep = list(map(_GRAD, params)), None, None
         if type(None) in set(map(type, grads)):
@@ -174,7 +178,7 @@ class AdamW(torch.optim.Optimizer):
             self._whole, self._rates = at is None, rates
         table["param"][:n] = list(map(_DATA_PTR, params))
         table["grad"][:n] = list(map(_DATA_PTR, grads))
-        return n, keep
+        return n, keep, at
 
     def step(self, closure=None):
         if self._optimizer_step_pre_hooks or self._optimizer_step_post_hooks:
@@ -206,16 +210,26 @@ class AdamW(torch.optim.Optimizer):
         return loss
 
     def _launch(self, betas, eps):
-        n, keep = self._fill()
+        n, keep, _ = self._fill()
         if self.master is not None and self._params_now() != self._seen:
             self.refresh_masters()
         self.steps += 1
-        clip, table = None, self._table.__array_interface__["data"][0]
-        if self.max_norm is not None:
+        clip, table = self._clip, self._table.__array_interface__["data"][0]
+        if clip is None and self.max_norm is not None:
             clip = self.grad_norm
             B.osdp_grad_norm(table, n, self._dtype, self.max_norm, clip, self._ws, check=True)
         B.osdp_adamw_step(table, n, self._dtype, self._state_dtype, self.master, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale,
                           self.exp_avg_sq_scale, betas[0], betas[1], eps, self.steps, clip, check=True)
+
+    def _squares(self, replicated, sharded):
+        """Sums of squares of the gradients of replicated and of sharded parameters into two fp64 values on the device
+        (None: that part is not wanted)."""
+        n, keep, at = self._fill()
+        flags = self.sharded if at is None else self.sharded[at]
+        for to, which in ((replicated, ~flags), (sharded, flags)):
+            if to is not None:
+                part = np.ascontiguousarray(self._table[:n][which])
+                B.osdp_grad_squares(part.__array_interface__["data"][0], len(part), self._dtype, to, self._ws, check=True)
 
     def __getstate__(self):
         raise TypeError("an AdamW is copied or saved through state_dict()")     # torch's copy would leave the flat states out
@@ -240,3 +254,64 @@ class AdamW(torch.optim.Optimizer):
         self.steps = int(steps)
         if self.master is not None:
             self._seen = self._params_now()
+
+
+class ClippedStep:
+    """Steps several ``AdamW`` optimisers with their gradients clipped by ONE norm: over all their parameters, whatever their
+    dtypes, and over the ranks of a process group.
+
+        opt = ClippedStep([AdamW(bf16_params, ...), AdamW(fp32_params, ...)], max_norm=1.0)
+        loss.backward(); opt.step(); opt.zero_grad()
+
+    comm      rank, world and all_reduce(tensor) of the ranks (``zdp.DistComm``), or None: one process.  Parameters in groups
+              with ``"sharded": True`` (``ZdpLinear.shard``) have other elements on every rank: their sums of squares are
+              added over ranks.  All others are replicated with the same gradients everywhere (``ZdpLinear.dp_parts``,
+              biases): rank 0's are counted.  So every rank has the same coefficient, bit by bit.  Every rank calls
+              ``step()``: it is a collective.
+    max_norm  as in AdamW; the optimisers themselves have none.  A norm that is not finite changes nothing on any rank.
+
+    ``grad_norm`` [2]: the last step's norm and coefficient, on the device.  The norm is taken before the optimisers' own
+    hooks run.
+    """
+
+    def __init__(self, optimizers, max_norm, comm=None):
+        self.optimizers, self.max_norm, self.comm = list(optimizers), float(max_norm), comm
+        if not self.optimizers or not all(isinstance(o, AdamW) for o in self.optimizers):
+            raise TypeError("ClippedStep takes AdamW optimisers")
+        if any(o.max_norm is not None for o in self.optimizers):
+            raise ValueError("the optimisers of a ClippedStep have no max_norm of their own")
+        self._device = self.optimizers[0]._device
+        if any(o._device != self._device for o in self.optimizers):
+            raise RuntimeError("the optimisers of a ClippedStep are on one device")
+        if comm is None and any(o.sharded.any() for o in self.optimizers):
+            raise ValueError("sharded parameters are clipped over the ranks of a comm")
+        self.grad_norm = torch.zeros(2, dtype=torch.float32, device=self._device)
+        self._sums = torch.zeros(2 * len(self.optimizers), dtype=torch.float64, device=self._device)
+
+    def _local_sums(self):
+        """This rank's sums of squares: of what is replicated (rank 0 alone, zeros elsewhere), then of what is sharded."""
+        k, at = len(self.optimizers), self._sums.data_ptr()
+        first = self.comm is None or self.comm.rank == 0
+        if not first:
+            self._sums.zero_()      # the last all-reduce's results
+        for i, o in enumerate(self.optimizers):
+            o._squares(at + 8 * i if first else None, at + 8 * (k + i) if self.comm is not None else None)
+        return self._sums
+
+    @torch.no_grad()
+    def step(self):
+        with torch.cuda.device(self._device):
+            sums = self._local_sums()
+            if self.comm is not None:
+                self.comm.all_reduce(sums, tag="grad_norm")
+            B.osdp_clip_coefficient(sums, sums.numel() if self.comm is not None else len(self.optimizers), self.max_norm, self.grad_norm, check=True)
+            for o in self.optimizers:
+                o._clip = self.grad_norm
+                try:
+                    o.step()
+                finally:
+                    o._clip = None
+
+    def zero_grad(self, set_to_none=True):
+        for o in self.optimizers:
+            o.zero_grad(set_to_none=set_to_none)

@@ -216,3 +216,87 @@ def test_second_moments_follow_gradients_that_become_smaller(P, b2, state, noise
     for part in (quiet, ~quiet):
         ratio = float(root[part].square().mean().sqrt() / v[part].mean().sqrt())
         assert abs(ratio - 1) < 0.06, ratio
+
+
+# ---- one norm over several optimisers and ranks
+
+def check_clipped(ps, opts, coef):
+    """First moments after one step from zero: (1 - beta1) c g."""
+    for p, o, i in ((p, o, i) for o in opts for i, p in enumerate(o._params)):
+        g = p.grad.double() * coef
+        assert bool(((states(o, i)[0] - 0.1 * g).abs() <= 4 * 2.0 ** -24 * g.abs() + 1e-37).all())
+
+
+@pytest.mark.parametrize("scale", [1 / 3, 3.0])
+def test_one_norm_over_two_dtypes(P, scale):
+    from paper_2209_13258_b200.optim import AdamW, ClippedStep
+    half, full = make([5000, 70001, 8], torch.bfloat16, 3), make([5000, 17, 300], torch.float32, 4)
+    for p in full:
+        p.grad *= 20
+    ps = half + full
+    norm = math.sqrt(sum(float(p.grad.double().square().sum()) for p in ps))
+    opts = [AdamW(half, lr=1e-3, master=True), AdamW(full, lr=1e-3)]
+    both = ClippedStep(opts, max_norm=norm * scale)
+    both.step()
+    got = both.grad_norm.tolist()
+    assert abs(got[0] - norm) <= 2e-6 * norm
+    assert abs(got[1] - min(1.0, scale)) <= 3e-6
+    check_clipped(ps, opts, got[1])
+    assert all(o.steps == 1 for o in opts)
+    both.zero_grad()
+    assert all(p.grad is None for p in ps)
+
+
+class Pair:
+    """The all-reduce of two ranks that run one after the other: adds what the other one brings."""
+    world = 2
+
+    def __init__(self, rank):
+        self.rank, self.other = rank, None
+
+    def all_reduce(self, t, tag=None):
+        t.add_(self.other)
+
+
+def two_ranks(step=True):
+    from paper_2209_13258_b200.optim import AdamW, ClippedStep
+    ranks = []
+    for r in (0, 1):
+        shard, whole = make([40000, 300], torch.bfloat16, 10 + r), make([5000], torch.bfloat16, 3)
+        bias = make([1000], torch.float32, 4)
+        for p in shard:
+            p.grad *= 1 + 9 * r                       # the ranks' own norms differ by far
+        opts = [AdamW([{"params": shard, "sharded": True}, {"params": whole}], lr=1e-2, master=True), AdamW(bias, lr=1e-2)]
+        ranks.append((shard, whole + bias, opts, ClippedStep(opts, max_norm=0.5, comm=Pair(r))))
+    return ranks
+
+
+def step_both(ranks):
+    sums = [c._local_sums().clone() for *_, c in ranks]
+    for r, (*_, c) in enumerate(ranks):
+        c.comm.other = sums[1 - r]
+        c.step()
+
+
+def test_one_norm_over_ranks_with_replicated_parameters_beside_shards(P):
+    ranks = two_ranks()
+    for k in range(3):
+        step_both(ranks)
+        sharded = sum(float(p.grad.double().square().sum()) for shard, *_ in ranks for p in shard)
+        norm = math.sqrt(sharded + sum(float(p.grad.double().square().sum()) for p in ranks[0][1]))
+        for shard, rep, opts, c in ranks:
+            assert abs(float(c.grad_norm[0]) - norm) <= 2e-6 * norm
+            if k == 0:
+                check_clipped(shard + rep, opts, float(c.grad_norm[1]))
+        assert torch.equal(ranks[0][3].grad_norm, ranks[1][3].grad_norm)
+        assert all(torch.equal(p, q) for p, q in zip(ranks[0][1], ranks[1][1]))     # replicated parameters stay the same
+
+
+def test_a_norm_that_is_not_finite_on_one_rank_changes_nothing_on_any(P):
+    ranks = two_ranks()
+    step_both(ranks)
+    ranks[1][0][0].grad[123] = float("nan")
+    before = [p.detach().clone() for shard, rep, *_ in ranks for p in shard + rep]
+    step_both(ranks)
+    assert all(torch.equal(p, q) for p, q in zip(before, (p for shard, rep, *_ in ranks for p in shard + rep)))
+    assert all(math.isnan(float(c.grad_norm[1])) for *_, c in ranks)

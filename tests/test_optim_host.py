@@ -11,9 +11,8 @@ from paper_2209_13258_b200 import optim                                        #
 from test_modules_host import OnGpu, gpu                                       # noqa: E402
 
 
-@pytest.fixture(autouse=True)
-def calls(monkeypatch):
-    """The tables that reach the step, one list of (param, grad, numel) per call."""
+def patch(monkeypatch):
+    """Returns the list that gets the tables that reach the step, one list of (param, grad, numel) per call."""
     seen = []
     zeros = torch.zeros
 
@@ -28,6 +27,11 @@ def calls(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(optim, "_DEVICE", lambda t: t.get_device())
     return seen
+
+
+@pytest.fixture(autouse=True)
+def calls(monkeypatch):
+    return patch(monkeypatch)
 
 
 def make(*sizes, dtype=torch.float32, **kw):
@@ -80,3 +84,118 @@ def test_a_parameter_that_moved_in_memory_is_followed(calls):
     ps[0].grad = None
     opt.step()
     assert calls[1] == [(ps[1].data_ptr(), ps[1].grad.data_ptr(), 300)]
+
+
+# ---- one norm over several optimisers and ranks
+
+def fake_squares(monkeypatch, log=None):
+    def squares(table, n, dtype, to, ws, **k):
+        t = (B.AdamWTensor * max(n, 1)).from_address(table)
+        c = {B.DTYPE_FP32: ctypes.c_float, B.DTYPE_BF16: ctypes.c_uint16}[dtype]
+        total = 0.0
+        for e in t[:n]:
+            a = list((c * e.numel).from_address(e.grad))
+            if dtype == B.DTYPE_BF16:
+                a = torch.tensor(a, dtype=torch.int32).to(torch.uint16).view(torch.bfloat16).double().tolist()
+            total += sum(v * v for v in a)
+        ctypes.c_double.from_address(to).value = total
+
+    def coefficient(sums, n, max_norm, out, **k):
+        norm = float(sums[:n].sum()) ** 0.5
+        out[0], out[1] = norm, min(1.0, max_norm / (norm + 1e-6))
+
+    monkeypatch.setattr(B, "osdp_grad_squares", squares)
+    monkeypatch.setattr(B, "osdp_clip_coefficient", coefficient)
+
+
+class NoDevice:
+    def __init__(self, *a):
+        pass
+
+    __enter__ = __exit__ = lambda self, *a: None                               # noqa: E731
+
+
+def test_a_clipped_step_hands_one_coefficient_to_all(calls, monkeypatch):
+    fake_squares(monkeypatch)
+    monkeypatch.setattr(torch.cuda, "device", NoDevice)
+    clips = []
+    monkeypatch.setattr(B, "osdp_adamw_step", lambda *a, **k: clips.append(a[13]))
+    _, a = make(100, 300)
+    _, b = make(50, dtype=torch.bfloat16)
+    c = optim.ClippedStep([a, b], max_norm=2.0)
+    c.step()
+    assert abs(float(c.grad_norm[0]) - 450 ** 0.5) < 1e-5
+    assert len(clips) == 2 and all(v is c.grad_norm for v in clips)
+    a.step()
+    assert clips[2] is None            # by itself an optimiser does not clip
+
+
+def test_a_clipped_step_refuses():
+    _, a = make(100)
+    _, own = make(100, max_norm=1.0)
+    ps, _ = make(100)
+    shard = optim.AdamW([{"params": ps, "sharded": True}])
+    with pytest.raises(ValueError, match="max_norm"):
+        optim.ClippedStep([a, own], 1.0)
+    with pytest.raises(ValueError, match="comm"):
+        optim.ClippedStep([a, shard], 1.0)
+    with pytest.raises(TypeError):
+        optim.ClippedStep([], 1.0)
+    with pytest.raises(TypeError):
+        optim.ClippedStep([a, torch.optim.SGD([torch.nn.Parameter(torch.ones(1))], lr=1.0)], 1.0)
+
+
+WORKER = """
+import os, sys
+sys.path[:0] = [%r, %r]
+import pytest, torch, torch.distributed as dist
+import test_optim_host as T
+from test_modules_host import gpu
+from paper_2209_13258_b200 import binding as B, optim
+from paper_2209_13258_b200.zdp import DistComm
+dist.init_process_group("gloo")
+rank = dist.get_rank()
+mp = pytest.MonkeyPatch()
+T.patch(mp)
+T.fake_squares(mp)
+mp.setattr(torch.cuda, "device", T.NoDevice)
+shard = torch.nn.Parameter(gpu(torch.ones(100)))
+shard.grad = gpu(torch.full((100,), 3.0 if rank else 0.1))
+both = torch.nn.Parameter(gpu(torch.ones(50)))
+both.grad = gpu(torch.full((50,), 0.7))
+half = torch.nn.Parameter(gpu(torch.ones(20, dtype=torch.bfloat16)))
+half.grad = gpu(torch.full((20,), 0.5, dtype=torch.bfloat16))
+c = optim.ClippedStep([optim.AdamW([{"params": [both]}, {"params": [shard], "sharded": True}]), optim.AdamW([half])], 1.0, comm=DistComm())
+for _ in range(3):
+    c.step()
+    want = (100 * 9.0 + 100 * 0.1 ** 2 + 50 * 0.49 + 20 * 0.25) ** 0.5
+    assert abs(float(c.grad_norm[0]) - want) < 1e-4 * want, (rank, c.grad_norm)
+    print("rank", rank, c.grad_norm.tolist())
+dist.barrier()
+dist.destroy_process_group()
+"""
+
+
+def test_two_gloo_ranks_get_one_coefficient():
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    procs = [subprocess.Popen([sys.executable, "-c", WORKER % (os.path.dirname(here), here)], stdout=subprocess.PIPE, stderr=subprocess.PIPE, text=True,
+                              env=dict(os.environ, RANK=str(r), WORLD_SIZE="2", MASTER_ADDR="127.0.0.1", MASTER_PORT="29755")) for r in (0, 1)]
+    outs = [p.communicate(timeout=180) for p in procs]
+    for p, (_, err) in zip(procs, outs):
+        assert p.returncode == 0, err[-3000:]
+    lines = [[line.split("]")[0].split("[")[1] for line in o.splitlines() if line.startswith("rank")] for o, _ in outs]
+    assert len(lines[0]) == 3 and lines[0] == lines[1]
+
+
+def test_squares_and_coefficient_refuse():
+    """The library's own checks stand before any launch: made-up addresses are never read."""
+    A, need = 1 << 20, B.osdp_grad_norm_workspace_bytes(1)[1]
+    t = (B.AdamWTensor * 1)()
+    t[0].grad, t[0].numel = A, 100
+    go = lambda t=t, n=1, dt=1, out=A, ws=(A, need): B.osdp_grad_squares(t, n, dt, out, ws, stream=0)          # noqa: E731
+    assert [go(out=None), go(ws=None), go(ws=(A + 8, need)), go(ws=(A, 256)), go(dt=2), go(n=-1), go(out=A + 4)] == [1, 1, 4, 5, 6, 2, 4]
+    co = lambda sums=A, n=2, mx=1.0, out=A: B.osdp_clip_coefficient(sums, n, mx, out, stream=0)                # noqa: E731
+    assert [co(sums=None), co(out=None), co(n=-1), co(mx=float("nan")), co(sums=A + 4), co(out=A + 2)] == [1, 1, 2, 6, 4, 4]
