@@ -10,9 +10,9 @@ namespace osdp {
 constexpr int COLSUM_ROWS_PER_CHUNK = 1024;   // fixed, so that a column's summation order never depends on k
 
 // g[m, j] = dy[m, c0 + j] * act'(z[m, c0 + j]),  j in [0, ncols), ncols % 8 == 0.
-__global__ void __launch_bounds__(256) act_backward_kernel(const __nv_bfloat16 *__restrict__ dy, long long ld_dy,
-                                                           const __nv_bfloat16 *__restrict__ z, long long ld_z,
-                                                           __nv_bfloat16 *__restrict__ g, long long ld_g,
+__global__ void __launch_bounds__(256) act_backward_kernel(const __nv_bfloat16 *dy, long long ld_dy,
+                                                           const __nv_bfloat16 *z, long long ld_z,
+                                                           __nv_bfloat16 *g, long long ld_g,
                                                            long long M, int c0, int ncols, int act) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");   // inputs may come from the previous kernel on the stream
@@ -37,9 +37,9 @@ __global__ void __launch_bounds__(256) act_backward_kernel(const __nv_bfloat16 *
 // multiples of 8, g 16-byte aligned).  A thread owns 8 adjacent columns (one 16-byte load per row) and
 // every 32nd row of the chunk; row order inside a chunk: row lane ty sums rows ty, ty+32, ...; then the
 // 32 row lanes are added in ascending order.  The order never depends on how the operator is split.
-__global__ void __launch_bounds__(256) colsum_partial_kernel(const __nv_bfloat16 *__restrict__ g, long long ld,
+__global__ void __launch_bounds__(256) colsum_partial_kernel(const __nv_bfloat16 *g, long long ld,
                                                              long long M, int c0, int ncols,
-                                                             float *__restrict__ partial, int ld_partial) {
+                                                             float *partial, int ld_partial) {
   __shared__ float red[32][64 + 1];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -88,8 +88,8 @@ __global__ void __launch_bounds__(256) colsum_partial_kernel(const __nv_bfloat16
 }
 
 // out[c0 + c] = sum over chunks (ascending) of partial[chunk, c].
-__global__ void __launch_bounds__(256) colsum_final_kernel(const float *__restrict__ partial, int ld_partial,
-                                                           int nchunks, int ncols, float *__restrict__ out) {
+__global__ void __launch_bounds__(256) colsum_final_kernel(const float *partial, int ld_partial,
+                                                           int nchunks, int ncols, float *out) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int c = blockIdx.x * blockDim.x + threadIdx.x;

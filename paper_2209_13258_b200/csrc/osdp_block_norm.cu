@@ -57,7 +57,7 @@ struct FwdArgs {
 
 __device__ __forceinline__ void weights8(const float *w, int col, float fill, float (&f)[8]) {
   if (w) {
-    const float4 a = __ldg(reinterpret_cast<const float4 *>(w + col)), b = __ldg(reinterpret_cast<const float4 *>(w + col + 4));
+    const float4 a = *reinterpret_cast<const float4 *>(w + col), b = *reinterpret_cast<const float4 *>(w + col + 4);
     f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
     f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
   } else {
@@ -808,13 +808,13 @@ __global__ void __launch_bounds__(32 * bwd_warps(LAYER), 1) block_norm_bwd_kerne
   const f2 alpha = both(a.alpha);
   // a row's statistics are read a step before they are used
   const bool has_stats = FULL || a.stats;
-  float4 next_st = (has_stats && n > 0) ? __ldg(a.stats + first) : make_float4(0.f, 0.f, 0.f, 0.f);
+  float4 next_st = (has_stats && n > 0) ? a.stats[first] : make_float4(0.f, 0.f, 0.f, 0.f);
   int st_a = 0, st_b = sh.stages - 1;     // ring stages of row i and of row i - 1 (then refilled)
   long long at = first * a.D - row_step;  // first channel of row i - 1
   for (long long i = 0; i <= n_steps; ++i, at += row_step) {
     if (i < n) {
       const float4 st = next_st;
-      if (has_stats && i + 1 < n) next_st = __ldg(a.stats + first + (i + 1) * step);
+      if (has_stats && i + 1 < n) next_st = a.stats[first + (i + 1) * step];
       if (has_post) {
         ip[0] = st.y;
         mp[0] = st.x;

@@ -1304,7 +1304,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
               tmem_ld_wait();
               if (SL::NBUF == 1 && (c + 1 == (wg + 1) * ((BN + 63) / 64 / EG) || cbase + 64 >= w.col_end)) release_accumulator();
               if (I8) {
-                const float rs = row < w.row_end ? __ldg(p.epi.row_scale + row) : 0.f;
+                const float rs = row < w.row_end ? p.epi.row_scale[row] : 0.f;
                 dequantise_acc(lo, rs, p.epi.col_scale, cbase, w.col_end);
                 if (BN >= 64) dequantise_acc(hi, rs, p.epi.col_scale, cbase + 32, w.col_end);
               } else {

@@ -14,8 +14,7 @@ namespace {
 
 // One row per team of warps: the row's largest magnitude, then its codes.  The row is read twice by its own threads;
 // the second read comes from L1 / L2.  One token of 8192: 2.7 us, next to nothing but the launch.
-__global__ void __launch_bounds__(256) quantize_rows_kernel(const __nv_bfloat16 *__restrict__ x, long long M, int K, int8_t *__restrict__ q,
-                                                            float *__restrict__ scale, int warps) {
+__global__ void __launch_bounds__(256) quantize_rows_kernel(const __nv_bfloat16 *x, long long M, int K, int8_t *q, float *scale, int warps) {
   __shared__ float red[8];
   pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -28,7 +27,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const __nv_bfloat16 
   uint32_t bits = 0u;
   for (int c = tl * 8; c < K; c += TL * 8) {
     float f[8];
-    widen8(__ldg(reinterpret_cast<const uint4 *>(xr + c)), f);
+    widen8(*reinterpret_cast<const uint4 *>(xr + c), f);
 #pragma unroll
     for (int k = 0; k < 8; ++k) bits = max(bits, __float_as_uint(f[k]) & 0x7FFFFFFFu);
   }
@@ -41,7 +40,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const __nv_bfloat16 
   const float step = int8_scale(top), inv = int8_inverse(step);
   for (int c = tl * 8; c < K; c += TL * 8) {
     float f[8];
-    widen8(__ldg(reinterpret_cast<const uint4 *>(xr + c)), f);
+    widen8(*reinterpret_cast<const uint4 *>(xr + c), f);
     *reinterpret_cast<uint2 *>(q + row * K + c) = to_int8x8(f, step, inv);
   }
   if (tl == 0) scale[row] = step;
@@ -163,7 +162,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
     const int pieces = K / 16;
     for (int i = threadIdx.x; i < M * pieces; i += blockDim.x) {
       const int m = i / pieces, c = i - m * pieces;
-      *reinterpret_cast<uint4 *>(xs + m * (K + 64) + c * 16) = __ldg(reinterpret_cast<const uint4 *>(a.x + (long long)m * K + c * 16));
+      *reinterpret_cast<uint4 *>(xs + m * (K + 64) + c * 16) = *reinterpret_cast<const uint4 *>(a.x + (long long)m * K + c * 16);
     }
   }
   __syncthreads();
@@ -188,7 +187,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
   for (int unit = first; unit < units; unit += stride, turn = (turn + 1) % SH::TURNS) {
     // what the epilogue needs of this thread's first output's column, while the products run
     const int n_first = min(unit * ROWS + (in_group / per) % ROWS, N - 1);
-    const float ws_first = __ldg(a.w_scale + n_first), b_first = a.bias ? __ldg(a.bias + n_first) : 0.f;
+    const float ws_first = a.w_scale[n_first], b_first = a.bias ? a.bias[n_first] : 0.f;
     int acc[MT][NT][4];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -241,7 +240,7 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, 1) few_tokens_kernel(const __g
       const int m = i / ROWS, n = unit * ROWS + i % ROWS;
       if (m < M && n < N && in_group % per == 0) {
         const bool f1 = i == in_group / per;
-        const float f = __fadd_rn(dequantise1(s, scales[m], f1 ? ws_first : __ldg(a.w_scale + n)), f1 ? b_first : a.bias ? __ldg(a.bias + n) : 0.f);
+        const float f = __fadd_rn(dequantise1(s, scales[m], f1 ? ws_first : a.w_scale[n]), f1 ? b_first : a.bias ? a.bias[n] : 0.f);
         a.out[(long long)m * N + n] = __float2bfloat16_rn(gelu1(f, a.act));
       }
     }

@@ -211,7 +211,7 @@ struct RawState {
 template <typename T, bool MASTER, States STATES, int MAXT>
 __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ Table<MAXT> t, const Hyper h, float *master,
                                                         void *state_m, void *state_v, float *scale_m, float *scale_v,
-                                                        const float *__restrict__ clip) {
+                                                        const float *clip) {
   constexpr bool E4M3 = STATES != F32, DITHER = STATES == DITHERED;
   constexpr int WARPS = THREADS / 32, PER_WARP = CHUNK / (WARPS * QB), BLOCKS = E4M3 ? PER_WARP : 1;
   pdl_launch_dependents();

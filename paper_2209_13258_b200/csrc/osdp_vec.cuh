@@ -8,6 +8,9 @@
 
 namespace osdp {
 
+// A kernel that is launched over the end of the one before it may find written by that one whatever it reads after pdl_wait():
+// inputs, scales, statistics, parameters that a step has just changed.  Such data is read with ordinary loads, never
+// through the read-only path (whose data must not change while the kernel runs, and it runs before the wait).
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
