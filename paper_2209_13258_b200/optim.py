@@ -181,18 +181,6 @@ class AdamW(torch.optim.Optimizer):
         return n, keep, at
 
     def step(self, closure=None):
-        if self._optimizer_step_pre_hooks or self._optimizer_step_post_hooks:
-            for hook in self._optimizer_step_pre_hooks.values():
-                hook(self, (closure,), {})
-            loss = self._step(closure)
-            for hook in self._optimizer_step_post_hooks.values():
-                hook(self, (closure,), {})
-            return loss
-        return self._step(closure)
-
-    step.hooked = True       # the hooks are called here: torch's wrapper around step costs more than the launch
-
-    def _step(self, closure):
         loss = None
         if closure is not None:
             with torch.enable_grad():

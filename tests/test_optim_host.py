@@ -199,3 +199,37 @@ def test_squares_and_coefficient_refuse():
     assert [go(out=None), go(ws=None), go(ws=(A + 8, need)), go(ws=(A, 256)), go(dt=2), go(n=-1), go(out=A + 4)] == [1, 1, 4, 5, 6, 2, 4]
     co = lambda sums=A, n=2, mx=1.0, out=A: B.osdp_clip_coefficient(sums, n, mx, out, stream=0)                # noqa: E731
     assert [co(sums=None), co(out=None), co(n=-1), co(mx=float("nan")), co(sums=A + 4), co(out=A + 2)] == [1, 1, 2, 6, 4, 4]
+
+
+# ---- torch's conventions
+
+def test_hooks_are_called_as_torch_calls_them(calls):
+    """Global and own hooks, in torch's order and with torch's arguments; a pre-hook may replace the arguments."""
+    from torch.optim.optimizer import register_optimizer_step_post_hook, register_optimizer_step_pre_hook
+    ps, opt = make(100)
+    seen, ran = [], []
+    closure = lambda: ran.append("given") or 1.0                               # noqa: E731
+    other = lambda: ran.append("other") or 2.0                                 # noqa: E731
+    handles = [register_optimizer_step_pre_hook(lambda o, a, k: seen.append(("global pre", o is opt, a, k))),
+               register_optimizer_step_post_hook(lambda o, a, k: seen.append(("global post", o is opt, a, k))),
+               opt.register_step_pre_hook(lambda o, a, k: seen.append(("pre", o is opt, a, k)) or ((o, other), k)),
+               opt.register_step_post_hook(lambda o, a, k: seen.append(("post", o is opt, a, k)))]
+    try:
+        assert opt.step(closure) == 2.0
+    finally:
+        for h in handles:
+            h.remove()
+    assert ran == ["other"] and len(calls) == 1
+    assert seen == [("global pre", True, (opt, closure), {}), ("pre", True, (opt, closure), {}), ("post", True, (opt, other), {}),
+                    ("global post", True, (opt, other), {})]
+    opt.register_step_pre_hook(lambda o, a, k: 3)
+    with pytest.raises(RuntimeError):
+        opt.step()
+
+
+def test_a_step_shows_in_a_profile(calls):
+    ps, opt = make(100)
+    opt.step()
+    with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CPU]) as prof:
+        opt.step()
+    assert any("Optimizer.step#AdamW" in e.key for e in prof.key_averages())
