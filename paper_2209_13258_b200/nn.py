@@ -339,8 +339,9 @@ class _ResidualNormFn(torch.autograd.Function):
         y2 = y.reshape(M, D).contiguous() if y is not None else None
         need_grad = any(ctx.needs_input_grad)
         pre = layer.pre != B.NORM_NONE
-        r = None if y is None and layer.alpha == 1.0 else torch.empty_like(x2)
-        u = torch.empty(M, D, dtype=torch.bfloat16, device=x.device) if pre else None
+        # in the caller's shape: a view made here could not be changed in place under autograd
+        r = None if y is None and layer.alpha == 1.0 else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        u = torch.empty(x.shape, dtype=torch.bfloat16, device=x.device) if pre else None
         post = layer.post if y is not None else B.NORM_NONE
         if y is None:
             w_post = b_post = gate = None
@@ -351,7 +352,7 @@ class _ResidualNormFn(torch.autograd.Function):
             ctx.layer, ctx.M, ctx.post, ctx.shape = layer, M, post, x.shape
             ctx.save_for_backward(y2, (x2 if r is None else r) if pre else None, stats, w_post, b_post, gate, w_pre)
         ctx.set_materialize_grads(False)
-        return (r.view(x.shape) if r is not None else None), (u.view(x.shape) if pre else None)
+        return r, u
 
     @staticmethod
     def backward(ctx, dr, du):

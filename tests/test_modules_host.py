@@ -187,3 +187,24 @@ def test_calls_launch_on_their_tensors_device(monkeypatch):
         to_gpu(int8())(gpu(X))
         pnn.quantize_int8(gpu(X))
     assert at == [0] * 5 and now == [1]
+
+
+@pytest.mark.parametrize("pre", [None, "rms"])
+def test_outputs_of_a_norm_can_be_changed_in_place(monkeypatch, pre):
+    """Under autograd too.  r is an input of the norm behind it, so a change before that norm's backward is reported there
+    (by torch's version count); behind the last block nothing needs it."""
+    monkeypatch.setattr(B, "osdp_block_norm_fwd", lambda *a, **k: None)
+    monkeypatch.setattr(B, "osdp_block_norm_bwd", lambda *a, **k: None)
+    m = to_gpu(pnn.ResidualNorm(64, post="rms", pre=pre, device="cpu"))
+    x = gpu(torch.ones(2, 3, 64, dtype=BF16)).requires_grad_(True)
+    r, u = m(x, x)
+    assert r.shape == x.shape and r.is_contiguous()
+    if pre:
+        u.mul_(2.0)
+        u.sum().backward(retain_graph=True)
+    r.add_(1.0)
+    if pre:
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            r.sum().backward()
+    else:
+        r.sum().backward()
