@@ -8,6 +8,7 @@ the CUDA kernels behind ``osdp_split_linear_fwd`` / ``osdp_split_linear_bwd``.  
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -64,6 +65,7 @@ class _SplitLinearFn(torch.autograd.Function):
         return out.reshape(*x.shape[:-1], N)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         layer, M = ctx.layer, ctx.M
         x2, z, weight = ctx.saved_tensors
@@ -169,6 +171,7 @@ class _SplitMLPFn(torch.autograd.Function):
         return out.reshape(*x.shape[:-1], H)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         layer, M = ctx.layer, ctx.M
         H, F, k = layer.hidden, layer.ffn, layer.k_split
@@ -269,6 +272,7 @@ class _ZdpLinearFn(torch.autograd.Function):
         return out.reshape(*x.shape[:-1], impl.N)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         layer, M = ctx.layer, ctx.M
         impl = layer.impl
@@ -355,6 +359,7 @@ class _ResidualNormFn(torch.autograd.Function):
         return r, u
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dr, du):
         layer, M = ctx.layer, ctx.M
         D = layer.hidden

@@ -208,3 +208,17 @@ def test_outputs_of_a_norm_can_be_changed_in_place(monkeypatch, pre):
             r.sum().backward()
     else:
         r.sum().backward()
+
+
+def test_second_derivatives_are_refused(monkeypatch):
+    """The backward passes are the library's calls, which autograd cannot differentiate: without the refusal the gradient of a
+    gradient came out as if it did not depend on anything."""
+    for name in ("osdp_block_norm_fwd", "osdp_block_norm_bwd", "osdp_split_linear_fwd", "osdp_split_linear_bwd", "osdp_split_mlp_fwd", "osdp_split_mlp_bwd"):
+        monkeypatch.setattr(B, name, lambda *a, **k: None)
+    monkeypatch.setattr(torch, "zeros_like", lambda t: torch.zeros(t.shape, dtype=t.dtype))
+    calls = [(to_gpu(norm()), lambda m, x: m(x, x)[0])] + [(to_gpu(m), lambda m, x: m(x)) for m in split_layers()]
+    for m, call in calls:
+        x = gpu(X.clone()).requires_grad_(True)
+        (g,) = torch.autograd.grad(call(m, x).float().square().sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            g.float().square().sum().backward()
