@@ -482,9 +482,21 @@ def quantize_int8(x):
     return q.view(x.shape), s.view(x.shape[:-1])
 
 
+class _Int8LinearFn(torch.autograd.Function):
+    """Int8Linear on an input that has a gradient: says so when that is asked for, instead of cutting the graph."""
+
+    @staticmethod
+    def forward(ctx, x, layer):
+        return layer._product(x, None)
+
+    @staticmethod
+    def backward(ctx, dy):
+        raise RuntimeError("Int8Linear has no gradient: train the layer it was made from")
+
+
 class Int8Linear(torch.nn.Module):
     """y = act(x W^T + b) for serving, with int8 weights (a scale per output channel) and int8 activations (a scale per
-    token, taken from the token itself); int32 sums, bf16 output.  No gradient.
+    token, taken from the token itself); int32 sums, bf16 output.  No gradient: a backward pass through it raises.
 
     weight8 [out, in] int8, w_scale [out] fp32, bias [out] fp32 or None (fp32 for good: a module cast by ``to(dtype)`` is
     refused).  ``from_linear`` quantises a trained
@@ -522,6 +534,11 @@ class Int8Linear(torch.nn.Module):
         if _elsewhere(q):
             with torch.cuda.device(q.device):
                 return self.forward(x)
+        if q.requires_grad and torch.is_grad_enabled():
+            return _Int8LinearFn.apply(q, self)
+        return self._product(q, s)
+
+    def _product(self, q, s):
         K, N = self.in_features, self.out_features
         shape = q.shape
         if shape[-1] != K:

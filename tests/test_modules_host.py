@@ -222,3 +222,15 @@ def test_second_derivatives_are_refused(monkeypatch):
         (g,) = torch.autograd.grad(call(m, x).float().square().sum(), x, create_graph=True)
         with pytest.raises(RuntimeError, match="once_differentiable"):
             g.float().square().sum().backward()
+
+
+def test_a_backward_pass_through_int8_is_refused(monkeypatch):
+    monkeypatch.setattr(B, "osdp_split_linear_fwd_i8", lambda *a, **k: None)
+    monkeypatch.setattr(B, "osdp_quantize_rows_i8", lambda *a, **k: None)
+    m = to_gpu(int8())
+    x = gpu(X.clone()).requires_grad_(True)
+    with pytest.raises(RuntimeError, match="no gradient"):
+        (m(x) + x[..., :32]).sum().backward()
+    with torch.no_grad():
+        assert not m(x).requires_grad
+    assert not m(gpu(X)).requires_grad and not m(x.detach()).requires_grad
