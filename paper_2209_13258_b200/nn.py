@@ -458,13 +458,13 @@ class ResidualNorm(torch.nn.Module):
         M = x.numel() // D
         x2 = x.reshape(M, D).contiguous()
         y2 = y.reshape(M, D).contiguous() if y is not None else None
-        r = torch.empty_like(x2)
+        r = None if y is None and self.alpha == 1.0 else torch.empty_like(x2)      # (x itself, as in forward)
         u = torch.empty(M, D, dtype=torch.int8, device=x.device)
         s = torch.empty(M, dtype=torch.float32, device=x.device)
         post, w_post, b_post, gate = (self.post, self.w_post, self.b_post, self.gate) if y is not None else (B.NORM_NONE, None, None, None)
         B.osdp_block_norm_fwd(x2, y2, M, D, self.resid_dtype, post, w_post, b_post, self.eps, gate, self.alpha, self.beta, self.pre,
                               self.w_pre, self.b_pre, self.eps, r, u, s, None, check=True)
-        return r.view(x.shape), (u.view(x.shape), s.view(x.shape[:-1]))
+        return (x if r is None else r.view(x.shape)), (u.view(x.shape), s.view(x.shape[:-1]))
 
 
 def quantize_int8(x):

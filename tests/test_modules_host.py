@@ -234,3 +234,12 @@ def test_a_backward_pass_through_int8_is_refused(monkeypatch):
     with torch.no_grad():
         assert not m(x).requires_grad
     assert not m(gpu(X)).requires_grad and not m(x.detach()).requires_grad
+
+
+def test_the_first_norm_in_int8_writes_no_copy_of_x(monkeypatch):
+    written = []
+    monkeypatch.setattr(B, "osdp_block_norm_fwd", lambda *a, **k: written.append(a[16]))
+    x = gpu(X)
+    assert to_gpu(norm()).forward_int8(x)[0] is x and written == [None]
+    assert to_gpu(norm(alpha=0.5)).forward_int8(x)[0] is not x and written[1] is not None
+    assert to_gpu(norm()).forward_int8(x, x)[0] is not x and written[2] is not None
