@@ -153,11 +153,11 @@ class AdamW(torch.optim.Optimizer):
         length, the copies of gradients that were not contiguous, and the indices of its parameters (None: all)."""
         params, table, sizes = self._params, self._table, self._sizes
         grads, at, keep = list(map(_GRAD, params)), None, None
-        if type(None) in set(map(type, grads)):
-            at = [i for i, g in enumerate(grads) if g is not None]
         # The kernel has addresses and the lengths recorded when the optimiser was built: whatever else a parameter or a
         # gradient has become (moved, cast, resized, strided) would be read and written out of its bounds.
-        if self._guard is None or at is not None or not self._guard.check(*params, *grads):
+        if self._guard is None or not self._guard.check(*params, *grads):
+            if type(None) in set(map(type, grads)):
+                at = [i for i, g in enumerate(grads) if g is not None]
             dtype, device = {self._torch_dtype}, {self._device.index}
             if set(map(_DTYPE, params)) != dtype or set(map(_DEVICE, params)) != device or list(map(_NUMEL, params)) != sizes or \
                not all(map(_IS_CONTIGUOUS, params)):
@@ -217,13 +217,14 @@ class AdamW(torch.optim.Optimizer):
         n, keep, _ = self._fill()
         if self.master is not None and self._params_now() != self._seen:
             self.refresh_masters()
-        self.steps += 1
+        step = self.steps + 1
         clip, table = self._clip, self._table.__array_interface__["data"][0]
         if clip is None and self.max_norm is not None:
             clip = self.grad_norm
             B.osdp_grad_norm(table, n, self._dtype, self.max_norm, clip, self._ws, check=True)
         B.osdp_adamw_step(table, n, self._dtype, self._state_dtype, self.master, self.exp_avg, self.exp_avg_sq, self.exp_avg_scale,
-                          self.exp_avg_sq_scale, betas[0], betas[1], eps, self.steps, clip, check=True)
+                          self.exp_avg_sq_scale, betas[0], betas[1], eps, step, clip, check=True)
+        self.steps = step        # (not of a step that was refused)
 
     def _squares(self, replicated, sharded):
         """Sums of squares of the gradients of replicated and of sharded parameters into two fp64 values on the device

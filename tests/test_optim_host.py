@@ -233,3 +233,31 @@ def test_a_step_shows_in_a_profile(calls):
     with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CPU]) as prof:
         opt.step()
     assert any("Optimizer.step#AdamW" in e.key for e in prof.key_averages())
+
+
+@pytest.mark.parametrize("name", ["osdp_adamw_step", "osdp_grad_norm"])
+def test_a_step_that_the_library_refuses_is_not_counted(calls, monkeypatch, name):
+    """The count sets the bias correction: a refused step (here: its betas) has not happened."""
+    ps, opt = make(100, max_norm=1.0)
+    opt.step()
+
+    def refuse(*a, **k):
+        raise B.OsdpError(6, name)
+
+    with monkeypatch.context() as m:
+        m.setattr(B, name, refuse)
+        with pytest.raises(B.OsdpError):
+            opt.step()
+    assert opt.steps == 1
+    opt.step()
+    assert opt.steps == 2
+
+
+def test_gradients_come_and_go(calls):
+    """The look at what came last time must not take a missing gradient for one that fits."""
+    ps, opt = make(100, 300)
+    for want in ([0, 1], [0, 1], [0], [0, 1], [1], []):
+        for i, p in enumerate(ps):
+            p.grad = gpu(torch.ones(p.shape)) if i in want else None
+        opt.step()
+        assert [c[0] for c in calls[-1]] == [ps[i].data_ptr() for i in want]
