@@ -53,8 +53,9 @@ class AdamW(torch.optim.Optimizer):
                  a step all the same, since the host does not wait to learn of it.
 
     All parameter groups are stepped together: ``lr`` and ``weight_decay`` may differ between groups, ``betas`` and
-    ``eps`` may not.  A group with ``"sharded": True`` says that every rank has other elements of its parameters.  Parameters whose ``.grad`` is None are left alone.  ``steps`` counts the steps done (one count for
-    all parameters: it sets the bias correction).  States are flat over all parameters, each parameter's part starting
+    ``eps`` may not.  A group with ``"sharded": True`` says that every rank has other elements of its parameters.
+    Parameters whose ``.grad`` is None are left alone.  ``steps`` counts the steps done (one count for all parameters: it
+    sets the bias correction).  States are flat over all parameters, each parameter's part starting
     at a multiple of 256 elements (``offsets``): ``exp_avg``, ``exp_avg_sq`` (in 8 bits the codes of the second
     moment's root), ``exp_avg_scale``, ``exp_avg_sq_scale``, ``master``.  A CUDA graph of a step replays that step's
     bias correction, rates and gradients' addresses.  ``grad_norm`` [2]: the last step's norm and
@@ -110,7 +111,9 @@ class AdamW(torch.optim.Optimizer):
         self.sharded = np.array([bool(g.get("sharded", False)) for g in self.param_groups for _ in g["params"]])
         self._clip = None       # coefficient from outside, while a ClippedStep steps
         self._table = np.zeros(n, dtype=_TENSOR)
+        self._table_at = self._table.ctypes.data
         self._whole, self._rates = False, None
+        self._written = None, None      # the addresses that the table's first entries hold
         # parameters and gradients as one step found them in order; a few times anew, if what comes changes
         self._guard, self._guards_left = None, 8 if _TensorGuards is not None else 0
         self._ws = B.new_workspace(B.osdp_grad_norm_workspace_bytes(n)[1], device=dev)
@@ -181,8 +184,12 @@ class AdamW(torch.optim.Optimizer):
             table["lr"][:n] = [rates[self._group_of[i]][0] for i in which]
             table["weight_decay"][:n] = [rates[self._group_of[i]][1] for i in which]
             self._whole, self._rates = at is None, rates
-        table["param"][:n] = list(map(_DATA_PTR, params))
-        table["grad"][:n] = list(map(_DATA_PTR, grads))
+        at_params, at_grads = list(map(_DATA_PTR, params)), list(map(_DATA_PTR, grads))
+        if at_params != self._written[0]:      # (comparing lists takes a tenth of writing a column)
+            table["param"][:n] = at_params
+        if at_grads != self._written[1]:
+            table["grad"][:n] = at_grads
+        self._written = at_params, at_grads
         return n, keep, at
 
     def _step(self, closure=None):
@@ -218,7 +225,7 @@ class AdamW(torch.optim.Optimizer):
         if self.master is not None and self._params_now() != self._seen:
             self.refresh_masters()
         step = self.steps + 1
-        clip, table = self._clip, self._table.__array_interface__["data"][0]
+        clip, table = self._clip, self._table_at
         if clip is None and self.max_norm is not None:
             clip = self.grad_norm
             B.osdp_grad_norm(table, n, self._dtype, self.max_norm, clip, self._ws, check=True)
@@ -234,7 +241,7 @@ class AdamW(torch.optim.Optimizer):
         for to, which in ((replicated, ~flags), (sharded, flags)):
             if to is not None:
                 part = np.ascontiguousarray(self._table[:n][which])
-                B.osdp_grad_squares(part.__array_interface__["data"][0], len(part), self._dtype, to, self._ws, check=True)
+                B.osdp_grad_squares(part.ctypes.data, len(part), self._dtype, to, self._ws, check=True)
 
     def __getstate__(self):
         raise TypeError("an AdamW is copied or saved through state_dict()")     # torch's copy would leave the flat states out
