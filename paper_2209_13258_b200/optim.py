@@ -32,6 +32,10 @@ except ImportError:
     _TensorGuards = None
 
 
+def _guard_of(tensors):
+    return _TensorGuards(*tensors, dynamic_dims_sizes=[list(t.shape) for t in tensors], dynamic_dims_strides=[list(t.stride()) for t in tensors])
+
+
 class AdamW(torch.optim.Optimizer):
     """Decoupled weight decay (AdamW) for contiguous CUDA parameters of one dtype, bf16 or fp32.
 
@@ -115,7 +119,7 @@ class AdamW(torch.optim.Optimizer):
         self._whole, self._rates = False, None
         self._written = None, None      # the addresses that the table's first entries hold
         # parameters and gradients as one step found them in order; a few times anew, if what comes changes
-        self._guard, self._guards_left = None, 8 if _TensorGuards is not None else 0
+        self._guard, self._guards_left = None, 9 if _TensorGuards is not None else 0
         self._ws = B.new_workspace(B.osdp_grad_norm_workspace_bytes(n)[1], device=dev)
         self._built = True
 
@@ -173,8 +177,8 @@ class AdamW(torch.optim.Optimizer):
                 keep = grads = [g.contiguous() for g in grads]
             elif at is None and self._guards_left:
                 self._guards_left -= 1
-                ts = params + grads
-                self._guard = _TensorGuards(*ts, dynamic_dims_sizes=[list(t.shape) for t in ts], dynamic_dims_strides=[list(t.stride()) for t in ts])
+                if self._guards_left < 8:       # (not in the first step, which is long enough)
+                    self._guard = _guard_of(params + grads)
         n = len(grads)
         rates = [(float(g["lr"]), float(g["weight_decay"])) for g in self.param_groups]
         if at is not None or not self._whole or rates != self._rates:
