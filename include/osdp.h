@@ -364,8 +364,9 @@ int osdp_split_mlp_bwd(const void *dy, const void *x, const void *w_flat, int64_
  *   w_* NULL: ones; b_* NULL: zeros (b_* must be NULL for OSDP_NORM_RMS); gate NULL: ones.
  *   r may be NULL (not written) and may be x itself; r and u must not overlap y otherwise.
  *   u_scale NULL: u is bf16.  u_scale [M] fp32: u is int8, the row divided by its scale = max |u| / 127 and rounded to
- *   the nearest integer, ties to even: the input that osdp_split_linear_fwd_i8 takes.  A row without a magnitude
- *   has scale 0 and zeros; a row with an infinity or a NaN has a scale that is not finite (the products come out NaN).
+ *   the nearest integer, ties to even (both divisions as fp32 rounds them): the input that osdp_split_linear_fwd_i8 takes.  A
+ *   row whose largest magnitude is below 2^-100 has scale 0 and zeros; a row with an infinity or a NaN has a scale that is
+ *   not finite and zeros (the products come out NaN).
  *   stats [M,4] fp32 or NULL: mean and 1 / sqrt(...) of N_post, then of N_pre (mean 0 for RMS; 0, 0 for an absent norm):
  *   what the backward needs.
  * D is a multiple of 8 and at most OSDP_BLOCK_NORM_MAX_D; M may be 0 (nothing is launched).  bf16 matrices, stats and vectors

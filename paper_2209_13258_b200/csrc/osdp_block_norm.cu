@@ -2,8 +2,9 @@
 //   p = N_post(y),  r = alpha x + beta gate (.) p,  u = N_pre(r).
 // HBM-bound: the forward reads x, y and writes r, u once; the backward reads y, r, du, dr and writes dx, dy once, the
 // sums over rows (weights' gradients) are kept in registers over all rows of a thread block.  Measured on B200 against a
-// copy rate of 6547 GB/s: 16384 x 8192 RMS bf16 forward 164 us (6550 GB/s of what has to move), backward 257 us (6270); layer
-// norm on an fp32 stream, 8192 x 2048, forward 48 us (4170), backward 91 us (3320): there the instructions count.
+// copy rate of 6547 GB/s, at full clocks: 16384 x 8192 RMS bf16 forward 161 us (6690 GB/s of what has to move), backward 261 us
+// (6170); in a loop under the power cap 185 and 301.  Layer norm on an fp32 stream, 8192 x 2048, forward 48 us (4170), backward 89
+// (3400): latency, 43 % of the issue slots are taken.
 #include "../../include/osdp.h"
 
 #include <atomic>
@@ -1171,7 +1172,8 @@ int osdp_block_norm_fwd(const void *x, const void *y, int64_t M, int64_t D, int 
 #undef OSDP_FWD
   }
   if (few) return resid_dtype == OSDP_DTYPE_FP32 ? launch_fwd<float, 1>(a, (int)cdiv(D, 256), s) : launch_fwd<__nv_bfloat16, 1>(a, (int)cdiv(D, 256), s);
-  // int8 u for many rows.  Two vectors per lane: 8192 x 2048 RMS 38 us; one 52, four 49 (8192 x 8192: 169, 325, 195).
+  // int8 u for many rows.  Two vectors per lane: 8192 x 2048 RMS 43 us (8192 x 8192: 177); one and four took 1.4 and 1.3
+  // (1.9 and 1.2) times as long.
   return resid_dtype == OSDP_DTYPE_FP32 ? launch_fwd<float, 2>(a, (int)cdiv(D, 512), s) : launch_fwd<__nv_bfloat16, 2>(a, (int)cdiv(D, 512), s);
 }
 

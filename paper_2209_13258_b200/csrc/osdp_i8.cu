@@ -13,7 +13,8 @@ namespace osdp {
 namespace {
 
 // One row per team of warps: the row's largest magnitude, then its codes.  The row is read twice by its own threads;
-// the second read comes from L1 / L2.  One token of 8192: 2.7 us, next to nothing but the launch.
+// the second read comes from L1 / L2.  One token of 8192: 2.9 us, next to nothing but the launch; 8192 x 8192 59 us of 31 that its
+// bytes take: the two loops' loads wait for one another.
 __global__ void __launch_bounds__(256) quantize_rows_kernel(const __nv_bfloat16 *x, long long M, int K, int8_t *q, float *scale, int warps) {
   __shared__ float red[8];
   pdl_launch_dependents();
@@ -59,8 +60,9 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const __nv_bfloat16 
 // The four words of a piece are used as operands of two mma whose k order is a permutation of the real one, the same
 // for W and X, which a sum over k does not notice.
 //
-// Measured on B200, one token, 8192 x 8192 (67 MB of W): 15.0 us, 4470 GB/s, where the bare stream takes 13 us (a read
-// that short does not reach the copy rate); 32768 x 8192: 45.9 us, 5850 GB/s; 8 tokens 53 us, 16 tokens 68 us.
+// Measured on B200 on ready-made codes (bf16 tokens: the quantiser's launch comes before), one token, 8192 x 8192 (67 MB of W):
+// 15.6 us, 4300 GB/s, where the bare stream takes 13 us (a read that short does not reach the copy rate); 32768 x 8192: 45.5 us,
+// 5900 GB/s; 8 tokens 54 us, 16 tokens 70 us.  With bf16 tokens 8192 x 8192 takes 20 us.
 __device__ __forceinline__ void mma_s8(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])

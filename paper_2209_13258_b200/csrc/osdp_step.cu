@@ -13,7 +13,7 @@
 // Rounding to nearest holds a moment where it is as long as a step moves it by less than half a code, 3 to 6 % of it, and
 // beta close to one moves it by 1 - beta at most.  After half of a block's gradients had become five times smaller, their
 // stored root was, 5 / (1 - beta2) and then 50 / (1 - beta2) steps later, too large by a factor of
-//   beta2 0.95: 1.4 and 1.05,  0.97: 3.6 and 1.2,  0.98: 6 and 6,  0.99: 6 and 6.5,  0.999: 5 and 4.5    (normal gradients)
+//   beta2 0.95: 1.5 and 1.05,  0.97: 3.6 and 1.2,  0.98: 6.3 and 5.9,  0.99: 5.8 and 6.5    (normal gradients; 0.999 no better)
 // while with a dither before the rounding, which makes it right on average, it was 1.10 and 1.02 at every one of them.
 // So a moment whose beta is above DITHER_ABOVE is rounded with the dither.  Nearest is better below: a moment that is
 // renewed within some dozen steps carries the noise of the gradients, which is dither enough, and the codes' own error is half.
@@ -207,7 +207,7 @@ struct RawState {
 // What bounds it: HBM with 32-bit states (28 bytes an element: 134 M bf16 parameters with fp32 masters 6310 GB/s of a copy rate
 // of 6547, the gradient norm before it included).  With 8-bit states (10 bytes an element) the instructions come near: 64 an
 // element in scalar form took 1450 us for 537 M parameters, some 45 an element with pairs of fp32, approximate reciprocals
-// and the rare paths set apart take 870 us at full clocks (6200 GB/s) and 974 us in the power-capped state.
+// and the rare paths set apart take 868 us at full clocks (6220 GB/s) and 1010 us in the power-capped state.
 template <typename T, bool MASTER, States STATES, int MAXT>
 __global__ void __launch_bounds__(THREADS) adamw_kernel(const __grid_constant__ Table<MAXT> t, const Hyper h, float *master,
                                                         void *state_m, void *state_v, float *scale_m, float *scale_v,

@@ -502,6 +502,7 @@ class Int8Linear(torch.nn.Module):
     refused).  ``from_linear`` quantises a trained
     ``SplitLinear`` (or any bf16 weight).  ``forward`` takes bf16 activations, or the pair (int8, scale) that
     ``ResidualNorm.forward_int8`` and ``quantize_int8`` return.
+    Nothing of a call is kept: calls on several streams and replays of captured graphs do not meet.
     """
 
     def __init__(self, weight8, w_scale, bias=None, act=B.ACT_NONE, k_split=1, split_dim=B.SPLIT_OUT):
