@@ -540,8 +540,8 @@ class Int8Linear(torch.nn.Module):
         return self._product(q, s)
 
     def _check(self, q, w8, w_scale, bias):
-        if w8.dtype is not torch.int8 or w8.device != q.device or w8.numel() != self.out_features * self.in_features:
-            raise RuntimeError("weight8 has to be [out_features, in_features] int8 on %s, its input's device" % q.device)
+        if w8.dtype is not torch.int8 or w8.device != q.device or w8.numel() != self.out_features * self.in_features or not w8.is_contiguous():
+            raise RuntimeError("weight8 has to be contiguous [out_features, in_features] int8 on %s, its input's device" % q.device)
         _check_fp32(q.device, w_scale=(w_scale, self.out_features), bias=(bias, self.out_features))
 
     def _product(self, q, s):
@@ -552,9 +552,9 @@ class Int8Linear(torch.nn.Module):
         M = q.numel() // K
         held = self._buffers          # (an attribute of a module that is a buffer takes several times as long)
         w8, w_scale, bias, device = held["weight8"], held["w_scale"], held["bias"], q.device
-        if w8.dtype is not torch.int8 or w8.device != device or w8.numel() != N * K or w_scale.dtype is not torch.float32 or \
-           w_scale.device != device or w_scale.numel() != N or (bias is not None and (bias.dtype is not torch.float32 or bias.device != device or
-                                                                                     bias.numel() != N)):
+        if w8.dtype is not torch.int8 or w8.device != device or w8.numel() != N * K or not w8.is_contiguous() or \
+           w_scale.dtype is not torch.float32 or w_scale.device != device or w_scale.numel() != N or not w_scale.is_contiguous() or \
+           (bias is not None and (bias.dtype is not torch.float32 or bias.device != device or bias.numel() != N or not bias.is_contiguous())):
             self._check(q, w8, w_scale, bias)
         if not q.is_contiguous():
             q = q.contiguous()

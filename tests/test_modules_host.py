@@ -243,3 +243,17 @@ def test_the_first_norm_in_int8_writes_no_copy_of_x(monkeypatch):
     assert to_gpu(norm()).forward_int8(x)[0] is x and written == [None]
     assert to_gpu(norm(alpha=0.5)).forward_int8(x)[0] is not x and written[1] is not None
     assert to_gpu(norm()).forward_int8(x, x)[0] is not x and written[2] is not None
+
+
+def test_an_int8_layer_looks_at_lengths_and_layouts():
+    """Buffers that a program has put in place of the layer's own."""
+    for name, other in (("w_scale", torch.ones(1).expand(32)), ("bias", torch.ones(64)[::2]), ("w_scale", torch.ones(16)), ("bias", torch.ones(8))):
+        m = to_gpu(int8())
+        m._buffers[name] = gpu(other)
+        with pytest.raises(ValueError, match=name):
+            m(gpu(X))
+    for other in (torch.ones(64, 32, dtype=torch.int8).t(), torch.ones(16, 64, dtype=torch.int8), torch.ones(1, 64, dtype=torch.int8).expand(32, 64)):
+        m = to_gpu(int8())
+        m._buffers["weight8"] = gpu(other)
+        with pytest.raises(RuntimeError, match="weight8"):
+            m(gpu(X))
