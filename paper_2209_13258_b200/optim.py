@@ -113,6 +113,8 @@ class AdamW(torch.optim.Optimizer):
         self._sizes = [p.numel() for p in self._params]
         self._group_of = [i for i, g in enumerate(self.param_groups) for _ in g["params"]]
         self.sharded = np.array([bool(g.get("sharded", False)) for g in self.param_groups for _ in g["params"]])
+        if max_norm is not None and self.sharded.any():
+            raise ValueError("sharded parameters are clipped by the norm over all ranks: ClippedStep")
         self._clip = None       # coefficient from outside, while a ClippedStep steps
         self._table = np.zeros(n, dtype=_TENSOR)
         self._table_at = self._table.ctypes.data

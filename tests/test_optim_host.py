@@ -261,3 +261,10 @@ def test_gradients_come_and_go(calls):
             p.grad = gpu(torch.ones(p.shape)) if i in want else None
         opt.step()
         assert [c[0] for c in calls[-1]] == [ps[i].data_ptr() for i in want]
+
+
+def test_sharded_parameters_are_not_clipped_by_one_ranks_norm():
+    ps, _ = make(100)
+    with pytest.raises(ValueError, match="ClippedStep"):
+        optim.AdamW([{"params": ps, "sharded": True}], max_norm=1.0)
+    optim.AdamW([{"params": ps, "sharded": False}], max_norm=1.0)
