@@ -97,6 +97,9 @@ extern "C" {
 #define OSDP_NORM_RMS 1
 #define OSDP_NORM_LAYER 2
 
+#define OSDP_SCORE_SOFTMAX 0
+#define OSDP_SCORE_SIGMOID 1
+
 #define OSDP_OP_LINEAR_FWD 0
 #define OSDP_OP_LINEAR_BWD 1
 #define OSDP_OP_MLP_FWD 2
@@ -468,6 +471,73 @@ int osdp_i8_workspace_bytes(int64_t M, int64_t K, size_t *bytes);
 int osdp_split_linear_fwd_i8(const void *x, const float *x_scale, const void *w8_flat, int64_t w_offset, const float *w_scale,
                              const float *bias, int64_t M, int64_t N, int64_t K, int k_split, int split_dim, int act, void *out,
                              void *ws, size_t ws_bytes, void *stream);
+
+/* ---- A mixture of experts around the linear layers.  (Addition beside the paper's method: the layer whose operators are the
+ * largest of all.)  T tokens choose top_k of E experts each; the experts' weights [E, N, K] lie in the flat parameter
+ * buffer, one expert after another.  1 <= E <= OSDP_MAX_EXPERTS, 1 <= top_k <= min(E, OSDP_MAX_TOP_K), T >= 0, T top_k <= 2^30.
+ *
+ * osdp_route_fwd: which experts a token goes to, and with what weights.  With l = logits[t, :]
+ *     s = softmax(l) or 1 / (1 + exp(-l));   c = s + bias
+ *     n_groups > top_groups: the experts form n_groups groups of E / n_groups neighbours; a group's score is the sum of its
+ *         group_take (1 or 2; 1 where a group is one expert) largest c, and only experts of the top_groups best groups may be chosen
+ *     idx[t, j]: the top_k largest c in descending order;   weights[t, j] = scale * s_idx / (renorm ? sum of the chosen s : 1)
+ * The choice is that of exact arithmetic; equal scores go to the lower index (groups likewise).  logits [T, E] bf16 or fp32,
+ * ld elements from row to row; bias [E] fp32 or NULL; idx [T, top_k] int32, weights [T, top_k] fp32.
+ * A logit of minus infinity has score 0 (also a row of nothing else), and a NaN is chosen as minus infinity is.  Renormalised
+ * weights depend on the chosen logits only, also where their scores leave fp32's range; if all of them are minus infinity the
+ * weights are 0.  idx is always made of top_k different experts.  n_groups <= 32 divides E, top_groups * (E / n_groups) >= top_k.
+ *
+ * osdp_route_bwd: dlogits [T, E] (dtype of the logits, ld_dlogits elements from row to row, all of it written) from dweights
+ * [T, top_k] fp32 and the idx of the forward.  The choice itself and the bias have no gradient.  An index outside 0 .. E - 1
+ * counts as no choice, the same index twice as two choices. */
+#define OSDP_MAX_EXPERTS 1024
+#define OSDP_MAX_TOP_K 16
+int osdp_route_fwd(const void *logits, int64_t ld, int logits_dtype, const float *bias, int64_t T, int E, int top_k, int score,
+                   int n_groups, int top_groups, int group_take, int renorm, double scale, int32_t *idx, float *weights, void *stream);
+int osdp_route_bwd(const float *dweights, const void *logits, int64_t ld, int logits_dtype, const int32_t *idx, int64_t T, int E,
+                   int top_k, int score, int renorm, double scale, void *dlogits, int64_t ld_dlogits, void *stream);
+
+/* The experts' rows.  Every (token, choice) is a row; rows are sorted by expert, in the order of t * top_k + j within one.  An
+ * expert's rows start at a multiple of OSDP_EXPERT_ROWS; the rows up to the next expert's are zero, rows behind the last
+ * expert's are neither read into any result nor written.
+ * osdp_expert_rows (host only): how many rows are enough however the choices fall, and the plan's length in int32.
+ * osdp_expert_plan: from idx [T, top_k] (of any origin; an index outside 0 .. E - 1 has no row) the plan, 16-byte aligned:
+ *     plan[0 .. E]: where the experts' rows start (plan[E]: where the last one's end), plan[E + 1 .. 2 E]: how many rows each
+ *     has; what follows is for the library's kernels;     pos[t, j]: the row of the choice, -1 for none.
+ * Deterministic; T = 0 writes a plan of no rows.  A plan belongs to its T, top_k and E: the calls below take all four. */
+#define OSDP_EXPERT_ROWS 64
+int osdp_expert_rows(int64_t T, int top_k, int E, int64_t *rows, int64_t *plan_ints);
+int osdp_expert_plan(const int32_t *idx, int64_t T, int top_k, int E, int32_t *plan, int32_t *pos, void *stream);
+
+/* osdp_expert_dispatch: rows[pos[t, j]] = weights[t, j] * x[t] (weights NULL: ones), zeros between the experts; with dweights
+ * (and y_rows) also dweights[t, j] = sum over channels of x[t] * y_rows[pos[t, j]] (0 for a choice without a row).
+ * osdp_expert_combine: out[t] = sum over j, in order, of weights[t, j] * rows[pos[t, j]] (weights NULL: ones).
+ * Each is the other's backward: of combine, dispatch with x = dout, the same weights and the rows that were combined; of dispatch without
+ * weights, combine without weights.  x, out [T, D], rows, y_rows [rows, D] bf16, 16-byte aligned, D a multiple of 8; weights,
+ * dweights [T, top_k] fp32; sums in fp32.  rows must not overlap x or y_rows. */
+int osdp_expert_dispatch(const void *x, const int32_t *plan, const int32_t *pos, const float *weights, const void *y_rows, int64_t T,
+                         int top_k, int E, int64_t D, void *rows, float *dweights, void *stream);
+int osdp_expert_combine(const void *rows, const int32_t *plan, const int32_t *pos, const float *weights, int64_t T, int top_k, int E,
+                        int64_t D, void *out, void *stream);
+
+/* The experts' products: for every row r of expert e
+ *     out[r] = act(rows[r] W_e^T + bias_e),    z_save[r] (or NULL) = the argument of act
+ * and their gradients: with G = dY (.) act'(Z)
+ *     dx[r] = G[r] W_e;   dW_e = sum over its rows of G[r]^T rows[r] (zero for an expert without rows);   dbias_e = sum of G[r]
+ * rows [rows, K], out, z_save, dy [rows, N], dx [rows, K] bf16; W [E, N, K] bf16 at element w_offset of w_flat; bias, dbias
+ * [E, N] fp32; dW [E, N, K] at dw_offset of dw_flat, bf16 or fp32 (dw_dtype; OSDP_FLAG_ACCUMULATE_DW adds to it).  N, K
+ * and the offsets are multiples of 8.  dx, dw_flat and dbias may be NULL (not wanted).  z_saved is read with an activation only.
+ * Rows between the experts: written as zeros; `rows` and dy have to be finite there and one of the two zero, as every call here
+ * leaves them.  dbias is summed from the unrounded G, in a fixed order; no atomics anywhere: the same call gives the same bits.
+ * The host does not learn how many rows an expert has: nothing synchronises, and a captured call follows the plan's
+ * contents.  ws: osdp_expert_linear_workspace_bytes(...) bytes (op OSDP_OP_LINEAR_FWD or _BWD), its first 256 zeroed once; no
+ * two calls that may run at the same time may share it. */
+int osdp_expert_linear_workspace_bytes(int64_t T, int top_k, int E, int64_t N, int64_t K, int act, int op, size_t *bytes);
+int osdp_expert_linear_fwd(const void *rows, const int32_t *plan, const void *w_flat, int64_t w_offset, const float *bias, int64_t T,
+                           int top_k, int E, int64_t N, int64_t K, int act, void *out, void *z_save, void *ws, size_t ws_bytes, void *stream);
+int osdp_expert_linear_bwd(const void *dy, const void *rows, const int32_t *plan, const void *w_flat, int64_t w_offset,
+                           const void *z_saved, int64_t T, int top_k, int E, int64_t N, int64_t K, int act, void *dx, void *dw_flat,
+                           int64_t dw_offset, int dw_dtype, int flags, float *dbias, void *ws, size_t ws_bytes, void *stream);
 
 /* Failure detection (no counterpart in the paper, which does not discuss faults: the slices of Section
  * 3.3 "executed sequentially" are pipelines of asynchronous copies and tensor-core work whose stages

@@ -20,4 +20,7 @@ from .binding import (  # noqa: F401
     osdp_adamw_layout, osdp_adamw_step, osdp_grad_norm, osdp_grad_norm_workspace_bytes,
     osdp_grad_squares, osdp_clip_coefficient,
     osdp_quantize_rows_i8, osdp_split_linear_fwd_i8, osdp_i8_workspace_bytes,
+    EXPERT_ROWS, MAX_EXPERTS, MAX_TOP_K, SCORE_SIGMOID, SCORE_SOFTMAX,
+    osdp_route_fwd, osdp_route_bwd, osdp_expert_rows, osdp_expert_plan, osdp_expert_dispatch, osdp_expert_combine,
+    osdp_expert_linear_workspace_bytes, osdp_expert_linear_fwd, osdp_expert_linear_bwd,
 )

@@ -17,6 +17,8 @@ ACT_NONE, ACT_GELU_TANH, ACT_GELU_ERF = 0, 1, 2
 DTYPE_BF16, DTYPE_FP32, DTYPE_E4M3, DTYPE_E4M3_DITHERED = 0, 1, 2, 3
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 ADAMW_BLOCK, BLOCK_NORM_MAX_D = 256, 16384
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+EXPERT_ROWS, MAX_EXPERTS, MAX_TOP_K = 64, 1024, 16
 OP_LINEAR_FWD, OP_LINEAR_BWD, OP_MLP_FWD, OP_MLP_BWD = 0, 1, 2, 3
 FLAG_ACCUMULATE_DW, FLAG_CARRY_BF16, FLAG_RECOMPUTE, FLAG_PAIR_SLICES, FLAG_SLICE_MAJOR = 1, 2, 4, 8, 16
 
@@ -33,6 +35,8 @@ EXPORTS = [
     "osdp_adamw_layout", "osdp_adamw_step", "osdp_grad_norm", "osdp_grad_norm_workspace_bytes", "osdp_grad_squares",
     "osdp_clip_coefficient",
     "osdp_quantize_rows_i8", "osdp_split_linear_fwd_i8", "osdp_i8_workspace_bytes",
+    "osdp_route_fwd", "osdp_route_bwd", "osdp_expert_rows", "osdp_expert_plan", "osdp_expert_dispatch", "osdp_expert_combine",
+    "osdp_expert_linear_workspace_bytes", "osdp_expert_linear_fwd", "osdp_expert_linear_bwd",
 ]
 
 _lib = None
@@ -122,6 +126,15 @@ def lib():
         L.osdp_i8_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
         L.osdp_quantize_rows_i8.argtypes = [vp, i64, i64, vp, vp, vp]
         L.osdp_split_linear_fwd_i8.argtypes = [vp, vp, vp, i64, vp, vp, i64, i64, i64, ci, ci, ci, vp, vp, sz, vp]
+        L.osdp_route_fwd.argtypes = [vp, i64, ci, vp, i64, ci, ci, ci, ci, ci, ci, ci, dbl, vp, vp, vp]
+        L.osdp_route_bwd.argtypes = [vp, vp, i64, ci, vp, i64, ci, ci, ci, ci, dbl, vp, i64, vp]
+        L.osdp_expert_rows.argtypes = [i64, ci, ci, p64, p64]
+        L.osdp_expert_plan.argtypes = [vp, i64, ci, ci, vp, vp, vp]
+        L.osdp_expert_dispatch.argtypes = [vp, vp, vp, vp, vp, i64, ci, ci, i64, vp, vp, vp]
+        L.osdp_expert_combine.argtypes = [vp, vp, vp, vp, i64, ci, ci, i64, vp, vp]
+        L.osdp_expert_linear_workspace_bytes.argtypes = [i64, ci, ci, i64, i64, ci, ci, ctypes.POINTER(sz)]
+        L.osdp_expert_linear_fwd.argtypes = [vp, vp, vp, i64, vp, i64, ci, ci, i64, i64, ci, vp, vp, vp, sz, vp]
+        L.osdp_expert_linear_bwd.argtypes = [vp, vp, vp, vp, i64, vp, i64, ci, ci, i64, i64, ci, vp, vp, i64, ci, ci, vp, vp, sz, vp]
         for name in EXPORTS:
             getattr(L, name)
             if name not in ("osdp_status_string",):
@@ -522,3 +535,61 @@ def osdp_split_linear_fwd_i8(x, x_scale, w8_flat, w_offset, w_scale, bias, M, N,
     rc = lib().osdp_split_linear_fwd_i8(_ptr(x), _ptr(x_scale), _ptr(w8_flat), w_offset, _ptr(w_scale), _ptr(bias), M, N, K,
                                         k_split, split_dim, act, _ptr(out), wp, wn, _stream(stream))
     return _ret(rc, check, "osdp_split_linear_fwd_i8")
+
+
+def osdp_route_fwd(logits, ld, logits_dtype, bias, T, E, top_k, score, n_groups, top_groups, group_take, renorm, scale, idx, weights,
+                   stream=None, check=False):
+    rc = lib().osdp_route_fwd(_ptr(logits), ld, logits_dtype, _ptr(bias), T, E, top_k, score, n_groups, top_groups, group_take, renorm, scale,
+                              _ptr(idx), _ptr(weights), _stream(stream))
+    return _ret(rc, check, "osdp_route_fwd")
+
+
+def osdp_route_bwd(dweights, logits, ld, logits_dtype, idx, T, E, top_k, score, renorm, scale, dlogits, ld_dlogits, stream=None, check=False):
+    rc = lib().osdp_route_bwd(_ptr(dweights), _ptr(logits), ld, logits_dtype, _ptr(idx), T, E, top_k, score, renorm, scale, _ptr(dlogits),
+                              ld_dlogits, _stream(stream))
+    return _ret(rc, check, "osdp_route_bwd")
+
+
+def osdp_expert_rows(T, top_k, E):
+    """Returns (status, rows that are enough however the choices fall, int32 words of a plan)."""
+    a, b = ctypes.c_int64(), ctypes.c_int64()
+    rc = lib().osdp_expert_rows(int(T), int(top_k), int(E), ctypes.byref(a), ctypes.byref(b))
+    return rc, a.value, b.value
+
+
+def osdp_expert_plan(idx, T, top_k, E, plan, pos, stream=None, check=False):
+    rc = lib().osdp_expert_plan(_ptr(idx), T, top_k, E, _ptr(plan), _ptr(pos), _stream(stream))
+    return _ret(rc, check, "osdp_expert_plan")
+
+
+def osdp_expert_dispatch(x, plan, pos, weights, y_rows, T, top_k, E, D, rows, dweights, stream=None, check=False):
+    rc = lib().osdp_expert_dispatch(_ptr(x), _ptr(plan), _ptr(pos), _ptr(weights), _ptr(y_rows), T, top_k, E, D, _ptr(rows), _ptr(dweights),
+                                    _stream(stream))
+    return _ret(rc, check, "osdp_expert_dispatch")
+
+
+def osdp_expert_combine(rows, plan, pos, weights, T, top_k, E, D, out, stream=None, check=False):
+    rc = lib().osdp_expert_combine(_ptr(rows), _ptr(plan), _ptr(pos), _ptr(weights), T, top_k, E, D, _ptr(out), _stream(stream))
+    return _ret(rc, check, "osdp_expert_combine")
+
+
+def osdp_expert_linear_workspace_bytes(T, top_k, E, N, K, act, op):
+    """Returns (status, bytes)."""
+    n = ctypes.c_size_t()
+    rc = lib().osdp_expert_linear_workspace_bytes(int(T), int(top_k), int(E), int(N), int(K), int(act), int(op), ctypes.byref(n))
+    return rc, n.value
+
+
+def osdp_expert_linear_fwd(rows, plan, w_flat, w_offset, bias, T, top_k, E, N, K, act, out, z_save, ws, stream=None, check=False):
+    wp, wn = _ws(ws)
+    rc = lib().osdp_expert_linear_fwd(_ptr(rows), _ptr(plan), _ptr(w_flat), w_offset, _ptr(bias), T, top_k, E, N, K, act, _ptr(out),
+                                      _ptr(z_save), wp, wn, _stream(stream))
+    return _ret(rc, check, "osdp_expert_linear_fwd")
+
+
+def osdp_expert_linear_bwd(dy, rows, plan, w_flat, w_offset, z_saved, T, top_k, E, N, K, act, dx, dw_flat, dw_offset, dw_dtype, flags, dbias, ws,
+                           stream=None, check=False):
+    wp, wn = _ws(ws)
+    rc = lib().osdp_expert_linear_bwd(_ptr(dy), _ptr(rows), _ptr(plan), _ptr(w_flat), w_offset, _ptr(z_saved), T, top_k, E, N, K, act, _ptr(dx),
+                                      _ptr(dw_flat), dw_offset, dw_dtype, flags, _ptr(dbias), wp, wn, _stream(stream))
+    return _ret(rc, check, "osdp_expert_linear_bwd")

@@ -11,9 +11,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libosdp.so")
 # Approximate functions and flushed denormals are fine for the GEMMs' epilogues; the optimiser's states, the norms'
 # statistics and the int8 scales are computed with IEEE division and square root.
-FAST_MATH_SOURCES = ["osdp_api.cu", "osdp_plan.cu"]
-SOURCES = FAST_MATH_SOURCES + ["osdp_step.cu", "osdp_block_norm.cu", "osdp_i8.cu"]
-HEADERS = ["osdp_gemm.cuh", "osdp_aux.cuh", "osdp_vec.cuh", "osdp_internal.h", "osdp_i8.h",
+FAST_MATH_SOURCES = ["osdp_api.cu", "osdp_plan.cu", "osdp_experts.cu"]
+SOURCES = FAST_MATH_SOURCES + ["osdp_step.cu", "osdp_block_norm.cu", "osdp_i8.cu", "osdp_route.cu"]
+HEADERS = ["osdp_gemm.cuh", "osdp_aux.cuh", "osdp_vec.cuh", "osdp_internal.h", "osdp_i8.h", "osdp_experts.h",
            os.path.join("..", "..", "include", "osdp.h")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -1137,6 +1137,10 @@ int bwd_impl(const void *dy, const void *x, const void *w_flat, int64_t w_offset
 namespace osdp {
 int report_cuda(cudaError_t e) { return e == cudaSuccess ? OSDP_OK : cuda_fail(e); }
 int sm_count(int *sms) { return device_sms(sms); }
+int encode_map3d(CUtensorMap *map, CUtensorMapDataType dt, const void *base, const cuuint64_t (&dims)[3], const cuuint64_t (&strides)[2],
+                 const cuuint32_t (&box)[3], bool swizzle) {
+  return encode3d(map, dt, base, dims, strides, box, swizzle);
+}
 }  // namespace osdp
 
 extern "C" {

@@ -96,6 +96,10 @@ struct GemmParams {
   int a_rows;                // int8: rows of A's box (BM, or the matrix's own, rounded up to 8, where it has fewer)
   Epilogue epi;
   int *status;               // device status word or null
+  // Experts' products (GRP below): the plan's offsets and counts, tiles of this launch's height before each expert, and the
+  // number of experts.
+  const int *seg_offsets, *seg_counts, *seg_tiles;
+  int experts;
 };
 
 // ------------------------------------------------------------------------------------------------
@@ -468,6 +472,8 @@ struct Work {
   int a_row, b_col;          // TMA coordinates (slice-relative where that dimension is sliced)
   int carry_in, carry_out;
   int first_of_slice;        // MODE_RED: this CTA's first tile of slice s
+  int k0;                    // GRP_RED: where the reduction starts (a row of the experts' rows)
+  int valid_end;             // GRP_ROWS: the expert's rows end here; from here to row_end zeros are written
 };
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -533,6 +539,68 @@ __device__ __forceinline__ bool get_work(const GemmParams &p, int i, int bid, in
   w.carry_in = (p.mode == MODE_RED) && !p.carry_bf16 && (s > 0);
   w.carry_out = (p.mode == MODE_RED) && !p.carry_bf16 && (s + w.s_count - 1 < p.k_total - 1);
   return true;
+}
+
+// The products of a mixture of experts.  Rows are sorted by expert, each expert's from a multiple of 64, so that a box of 32
+// rows and a k-block of 64 rows belong to one expert.  The expert is the slice coordinate of the weights' maps.
+//   GRP_ROWS  OUT[r, :] = A[r, :] B_e(r)^T: tiles of an expert's rows; a tile's rows behind the expert's own are computed
+//             from whatever is there and not stored.
+//   GRP_RED   OUT_e = A[rows of e, :]^T B[rows of e, :]: the tiles of every expert, over its rows.  An expert without rows takes
+//             one k-block behind the last row, which the copies fill with zeros.
+// How many rows an expert has is only known on the device: every role walks the plan's tables in the same way (w.s stays
+// where the tile before was found).
+enum : int { GRP_NONE = 0, GRP_ROWS = 1, GRP_RED = 2 };
+
+template <int TM, int BN, int GRP>
+__device__ __forceinline__ bool get_work_of_experts(const GemmParams &p, int i, int bid, int G, Work &w) {
+  const int tiles_n = ceil_div(p.Q, BN);
+  const long long t = (long long)bid + (long long)i * G;
+  if (i == 0) w.s = 0;
+  int tl, tiles_m;
+  if (GRP == GRP_ROWS) {
+    const int E = p.experts;
+    if (t >= (long long)p.seg_tiles[E] * tiles_n) return false;
+    while (t >= (long long)p.seg_tiles[w.s + 1] * tiles_n) ++w.s;
+    tl = (int)(t - (long long)p.seg_tiles[w.s] * tiles_n);
+    tiles_m = p.seg_tiles[w.s + 1] - p.seg_tiles[w.s];
+  } else {
+    tiles_m = ceil_div(p.P, TM);
+    const long long each = (long long)tiles_m * tiles_n;
+    if (t >= each * p.experts) return false;
+    w.s = (int)(t / each);
+    tl = (int)(t - w.s * each);
+  }
+  constexpr int GM = GROUP_M * BM / TM;
+  const int group = GM * tiles_n;
+  const int g = tl / group;
+  const int first_m = g * GM;
+  const int gm = min(GM, tiles_m - first_m);
+  const int tm = first_m + (tl - g * group) % gm;
+  const int tn = (tl - g * group) / gm;
+  const int off = p.seg_offsets[w.s], end = p.seg_offsets[w.s + 1];
+  w.s_count = 1;
+  w.b_col = w.col0 = tn * BN;
+  w.col_end = p.Q;
+  w.carry_in = w.carry_out = w.first_of_slice = 0;
+  if (GRP == GRP_ROWS) {
+    w.a_row = w.row0 = off + tm * TM;
+    w.row_end = end;
+    w.valid_end = off + p.seg_counts[w.s];
+    w.k0 = 0;
+    w.kblocks = ceil_div(p.R, p.bk);
+  } else {
+    w.a_row = w.row0 = tm * TM;
+    w.row_end = w.valid_end = p.P;
+    w.k0 = end > off ? off : p.R;
+    w.kblocks = max(1, (end - off) / p.bk);
+  }
+  return true;
+}
+
+template <int TM, int BN, int GRP>
+__device__ __forceinline__ bool next_work(const GemmParams &p, int i, int bid, int G, Work &w) {
+  if constexpr (GRP != GRP_NONE) return get_work_of_experts<TM, BN, GRP>(p, i, bid, G, w);
+  else return get_work<TM, BN>(p, i, bid, G, w);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -720,7 +788,7 @@ __device__ __forceinline__ void epilogue8(const Epilogue &e, long long row, int 
 // in tensor memory over all slices).  Tensor-bound like the other types: 8192 x 8192 x 8192 352 us = 3120 TOPS (e4m3: 358 us),
 // 8192 x 32768 x 8192 with bias and GeLU 1480 us = 2970 TOPS (1450 with the approximate tanh).  A tile of 128 rows takes at
 // least 0.29 us per k-block (reading A from shared memory), which is what bounds it with few tokens.
-template <int BN, bool A_MN, bool B_MN, bool CTA2, bool HEAVY = false, int EB = 2, bool I8 = false>
+template <int BN, bool A_MN, bool B_MN, bool CTA2, bool HEAVY = false, int EB = 2, bool I8 = false, int GRP = GRP_NONE>
 __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kernel(const __grid_constant__ GemmParams p) {
   using SL = SmemLayout<BN, CTA2, HEAVY>;
   constexpr int BKE = 128 / EB;   // reduction elements per k-block
@@ -809,17 +877,17 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
     uint32_t armed = 0, armed_phase = 0;   // per-round bookkeeping for the unwind path
     bool ok = true;
     Work w;
-    for (int i = 0; ok && get_work<TM, BN>(p, i, bid, G, w); ++i) {
+    for (int i = 0; ok && next_work<TM, BN, GRP>(p, i, bid, G, w); ++i) {
       w.a_row += (int)rank * BM;            // this CTA's rows of the pair's tile
       w.b_col += (int)rank * SL::GB_ROWS * (CTA2 ? 1 : 0);   // ... and its half of each 256-column group of B
       int tile_left = w.kblocks;            // k-blocks of this tile still to load (a round never spans two tiles)
       for (int sl = 0; sl < w.s_count && ok; ++sl) {
       const int ss = w.s + sl;               // the slice whose operand boxes are loaded now
       const bool tail = (ss == p.k_total - 1);
-      const CUtensorMap *amap = (a_sliced && !tail) ? &p.a_main : &p.a_tail;
-      const CUtensorMap *bmap = (b_sliced && !tail) ? &p.b_main : &p.b_tail;
+      const CUtensorMap *amap = (a_sliced && !tail) || GRP != GRP_NONE ? &p.a_main : &p.a_tail;
+      const CUtensorMap *bmap = (b_sliced && !tail) || GRP != GRP_NONE ? &p.b_main : &p.b_tail;
       const int a_sc = (a_sliced && !tail) ? ss * p.a_sc_mul : 0;
-      const int b_sc = (b_sliced && !tail) ? ss * p.b_sc_mul : 0;
+      const int b_sc = GRP == GRP_ROWS ? w.s : (b_sliced && !tail) ? ss * p.b_sc_mul : 0;
       const int nkb = (p.mode == MODE_RED) ? ceil_div(min(p.L, p.R - ss * p.L), BKE) : w.kblocks;
       for (int kb = 0; kb < nkb; ++kb) {
         if (sub == 0) {
@@ -835,7 +903,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
           const uint32_t sa = smem_base + (uint32_t)(grp * unit + sub) * SL::STAGE_BYTES;
           const uint32_t sb = sa + SL::A_BYTES;
           const uint32_t fb = full_bar(grp);
-          const int kc = kb * BKE;
+          const int kc = kb * BKE + (GRP == GRP_RED ? w.k0 : 0);
           auto tma_load = [&](uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2) {
             if (CTA2) tma_load_3d_pair(dst, map, fb, c0, c1, c2);
             else tma_load_3d(dst, map, fb, c0, c1, c2);
@@ -899,7 +967,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
       uint32_t phase = 0;
       bool ok = true;
       Work w;
-      for (int i = 0; ok && get_work<TM, BN>(p, i, bid, G, w); ++i) {
+      for (int i = 0; ok && next_work<TM, BN, GRP>(p, i, bid, G, w); ++i) {
         const int buf = i % SL::NBUF;
         const uint32_t bphase = (uint32_t)(i / SL::NBUF) & 1u;
         ok = mbar_wait(tempty_bar(buf), bphase ^ 1u, abort_flag, p.status, STATUS_TIMEOUT_MMA);
@@ -965,7 +1033,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
     uint32_t n_cload = 0;   // carry boxes loaded by this warp
     bool ok = true;
     Work w;
-    for (int i = 0; ok && get_work<TM, BN>(p, i, bid, G, w); ++i) {
+    for (int i = 0; ok && next_work<TM, BN, GRP>(p, i, bid, G, w); ++i) {
       w.a_row += (int)rank * BM;
       w.row0 += (int)rank * BM;
       if (i == 0 && p.tma_epilogue && p.epi.gz && lane == 0)   // this CTA's first tile: while its main loop runs
@@ -1029,9 +1097,12 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
         }
       } else if (wrow0 < w.row_end) {
         const bool tail = (w.s == p.k_total - 1);
-        const int sc = (out_sliced && !tail) ? w.s * p.out_sc_mul : 0;
-        const CUtensorMap *omap = (out_sliced && !tail) ? &p.out_main : &p.out_tail;
-        const CUtensorMap *zmap = (out_sliced && !tail) ? &p.z_main : &p.z_tail;
+        const int sc = GRP == GRP_RED ? w.s : (out_sliced && !tail) ? w.s * p.out_sc_mul : 0;
+        const CUtensorMap *omap = (out_sliced && !tail) || GRP != GRP_NONE ? &p.out_main : &p.out_tail;
+        const CUtensorMap *zmap = (out_sliced && !tail) || GRP != GRP_NONE ? &p.z_main : &p.z_tail;
+        const float *bias = p.epi.bias;
+        if (GRP == GRP_ROWS && bias) bias += (long long)w.s * p.Q;
+        const bool empty_row = GRP == GRP_ROWS && row >= w.valid_end;   // written as zeros
         const int r_in = w.a_row + quarter * 32;
         // One staged box: wait until the buffer's previous box has been read, fill it, hand it to TMA.
         auto stage_begin = [&]() -> uint32_t {
@@ -1315,12 +1386,12 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
               for (int j = 0; j < 32; ++j) { v[j] = lo[j]; v[32 + j] = hi[j]; }
             }
             uint4 packed[8];
-            if (p.epi.bias && !skip_bias) {
+            if (bias && !skip_bias) {
 #pragma unroll
               for (int g = 0; g < 8; ++g) {
                 if (cbase + g * 8 < w.col_end) {
-                  const float4 b0 = *reinterpret_cast<const float4 *>(p.epi.bias + cbase + g * 8);
-                  const float4 b1 = *reinterpret_cast<const float4 *>(p.epi.bias + cbase + g * 8 + 4);
+                  const float4 b0 = *reinterpret_cast<const float4 *>(bias + cbase + g * 8);
+                  const float4 b1 = *reinterpret_cast<const float4 *>(bias + cbase + g * 8 + 4);
                   v[g * 8 + 0] = __float_as_uint(__uint_as_float(v[g * 8 + 0]) + b0.x);
                   v[g * 8 + 1] = __float_as_uint(__uint_as_float(v[g * 8 + 1]) + b0.y);
                   v[g * 8 + 2] = __float_as_uint(__uint_as_float(v[g * 8 + 2]) + b0.z);
@@ -1339,6 +1410,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
 #pragma unroll
                 for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(v[g * 8 + j]);
                 packed[g] = pack_bf16x8(f);
+                if (empty_row) packed[g] = make_uint4(0u, 0u, 0u, 0u);
               }
               const uint32_t dstz = stage_begin();
 #pragma unroll
@@ -1354,6 +1426,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
               if (I8) gelu1_array(f, p.epi.act);
               else gelu_array(f, p.epi.act);
               packed[g] = pack_bf16x8(f);
+              if (empty_row) packed[g] = make_uint4(0u, 0u, 0u, 0u);
             }
             const uint32_t dst = stage_begin();
 #pragma unroll
@@ -1384,7 +1457,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
 // Diagnostic: one warp waits, with the same bounded wait the GEMM uses, on a barrier that nothing
 // ever signals.  The wait gives up after limit_ns, records STATUS_TIMEOUT_PROBE and the kernel returns.
 enum : int { STATUS_TIMEOUT_PROBE = 199 };
-__global__ void wait_probe_kernel(int *status, unsigned long long limit_ns) {
+static __global__ void wait_probe_kernel(int *status, unsigned long long limit_ns) {
   __shared__ __align__(8) unsigned long long bar;
   __shared__ int abort_flag;
   if (threadIdx.x == 0) {

@@ -1,6 +1,7 @@
 // Host-side helpers shared by the library's translation units.  Not part of the C ABI.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -10,6 +11,10 @@ namespace osdp {
 int report_cuda(cudaError_t e);
 // Number of SMs of the current device (cached per device).
 int sm_count(int *sms);
+
+// A 3-D tensor map (strides in bytes); swizzle: 128-byte, else none.
+int encode_map3d(CUtensorMap *map, CUtensorMapDataType dt, const void *base, const cuuint64_t (&dims)[3], const cuuint64_t (&strides)[2],
+                 const cuuint32_t (&box)[3], bool swizzle);
 
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline bool aligned_to(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
