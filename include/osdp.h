@@ -513,8 +513,9 @@ int osdp_expert_plan(const int32_t *idx, int64_t T, int top_k, int E, int32_t *p
  * (and y_rows) also dweights[t, j] = sum over channels of x[t] * y_rows[pos[t, j]] (0 for a choice without a row).
  * osdp_expert_combine: out[t] = sum over j, in order, of weights[t, j] * rows[pos[t, j]] (weights NULL: ones).
  * Each is the other's backward: of combine, dispatch with x = dout, the same weights and the rows that were combined; of dispatch without
- * weights, combine without weights.  x, out [T, D], rows, y_rows [rows, D] bf16, 16-byte aligned, D a multiple of 8; weights,
- * dweights [T, top_k] fp32; sums in fp32.  rows must not overlap x or y_rows. */
+ * weights, combine without weights.  x, out [T, D], rows, y_rows [rows, D] bf16, 16-byte aligned, D a multiple of 8 and at most
+ * OSDP_EXPERT_MAX_D; weights, dweights [T, top_k] fp32; sums in fp32.  rows must not overlap x or y_rows. */
+#define OSDP_EXPERT_MAX_D 262144
 int osdp_expert_dispatch(const void *x, const int32_t *plan, const int32_t *pos, const float *weights, const void *y_rows, int64_t T,
                          int top_k, int E, int64_t D, void *rows, float *dweights, void *stream);
 int osdp_expert_combine(const void *rows, const int32_t *plan, const int32_t *pos, const float *weights, int64_t T, int top_k, int E,

@@ -16,11 +16,11 @@ constexpr uint32_t ALL = 0xFFFFFFFFu;
 // ------------------------------------------------------------------------------------------------
 // Routing.  One warp per token; lane l holds experts l, l + 32, ... in registers.
 //
-// The choice has to be the one of exact arithmetic: another expert is another result.  Without a bias the scores are a
-// monotone function of the logits, so the experts are chosen by the logits themselves.  With a bias (and for the sums of the
-// groups) scores are formed in fp32, and where two of those that decide are closer than their rounding the row is done again
-// in fp64: some rows in a thousand, so that the price of a batch in fp64 is not paid.
-
+// The choice has to be the one of exact arithmetic: another expert is another result.  It is made twice at most.  First in
+// fp32 with approximate scores: a key is the score's order-preserving bits with the place in the lane's registers in the lowest
+// ones, a lane sorts its keys once, and an expert is found by one maximum over the lanes' first keys.  Where two scores
+// that decide are closer than all these roundings (and are not the same logit with the same bias), the row is done again
+// in fp64; that is one row in some hundred.
 struct RouteArgs {
   const void *logits;
   long long ld, T;
@@ -45,7 +45,6 @@ __device__ __forceinline__ unsigned long long key_of(double x) {
   if ((u & 0x7FFFFFFFFFFFFFFFull) > 0x7FF0000000000000ull) return 0x000FFFFFFFFFFFFFull;
   return (u >> 63) ? ~u : u | 0x8000000000000000ull;
 }
-__device__ __forceinline__ uint32_t warp_top(uint32_t k) { return __reduce_max_sync(ALL, k); }
 __device__ __forceinline__ unsigned long long warp_top(unsigned long long k) {
   const uint32_t hi = __reduce_max_sync(ALL, (uint32_t)(k >> 32));
   const uint32_t lo = __reduce_max_sync(ALL, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
@@ -53,139 +52,244 @@ __device__ __forceinline__ unsigned long long warp_top(unsigned long long k) {
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float((key >> 31) ? key & 0x7FFFFFFFu : ~key); }
 
-__device__ __forceinline__ float exp_of(float x) { return expf(x); }
-__device__ __forceinline__ double exp_of(double x) { return exp(x); }
 template <typename R>
 __device__ __forceinline__ R sum_of(R v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(ALL, v, o);
   return v;
 }
-
-// Chooses the row's experts: lane j < k leaves with the j-th in `mine`.  Returns false where R is too short to say.
-// `room` [E] of R: this warp's shared memory.
-template <typename R, int V, typename L>
-__device__ __noinline__ bool choose(const RouteArgs &a, const L *row, const float (&l)[V], R *room, int lane, int &mine) {
-  using Key = decltype(key_of(R(0)));
-  const R low = -(R)INFINITY;
-  const bool grouped = a.top_groups < a.groups;
-  Key key[V];
-  R c[V];
-  float far = 0.f;                    // largest |bias|: what a score's rounding is relative to, beside the score
-  if (a.bias || grouped) {
-    if (a.score == OSDP_SCORE_SOFTMAX) {
-      uint32_t top = 0;
+template <int V>
+__device__ __forceinline__ float largest(const float (&l)[V]) {   // of the row; lanes past its end hold minus infinity
+  uint32_t top = 0;
 #pragma unroll
-      for (int v = 0; v < V; ++v) top = max(top, v * 32 + lane < a.E ? key_of(l[v]) : 0u);
-      const R high = (R)value_of(__reduce_max_sync(ALL, top));
-      R total = 0;
+  for (int v = 0; v < V; ++v) top = max(top, key_of(l[v]));
+  return value_of(__reduce_max_sync(ALL, top));
+}
+
+// Which groups may be chosen from: bit g * per of the result, `per` lanes for each group.  c: the row's scores in `room`, NaN as
+// minus infinity; border: the last group that is taken and the first that is not.
+template <typename R>
+__device__ __forceinline__ uint32_t choose_groups(const RouteArgs &a, const R *room, int lane, int &per, R &sum, bool &in) {
+  const R low = -(R)INFINITY;
+  const int size = a.E / a.groups;
+  per = 32;
+  while (per * a.groups > 32) per >>= 1;
+  const int g = lane / per;
+  R first = low, second = low;
+  if (g < a.groups) {
+    for (int e = g * size + lane % per; e < (g + 1) * size; e += per) {
+      const R x = room[e];
+      second = max(second, min(first, x));
+      first = max(first, x);
+    }
+  }
+  for (int o = 1; o < per; o <<= 1) {
+    const R f = __shfl_xor_sync(ALL, first, o), s = __shfl_xor_sync(ALL, second, o);
+    second = max(max(second, s), min(first, f));
+    first = max(first, f);
+  }
+  sum = a.take > 1 && size > 1 ? first + second : first;
+  if (sum != sum) sum = low;
+  int rank = 0;
+  for (int h = 0; h < a.groups; ++h) {
+    const R other = __shfl_sync(ALL, sum, h * per);
+    rank += other > sum || (other == sum && h < g) ? 1 : 0;
+  }
+  in = g < a.groups && rank < a.top_groups;
+  return __ballot_sync(ALL, in && lane % per == 0);
+}
+
+constexpr float HALF_ULP = 5.9604645e-8f;
+__device__ __forceinline__ float fast_exp(float x) {   // 2^-22 and the rounding of the product: 1.5 |x| 2^-24
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * 1.4426950408889634f));
+  return e;
+}
+
+// Chooses the row's experts by their approximate scores: lane j < k leaves with the j-th in `mine`, its logit in `lj`.
+// Returns false where two scores are too close to say.  `room` [E]: this warp's shared memory.
+template <int V, typename L>
+__device__ __forceinline__ bool choose_fast(const RouteArgs &a, const L *row, const float (&l)[V], float *room, int lane, int &mine, float &lj) {
+  const bool grouped = a.top_groups < a.groups, soft = a.score == OSDP_SCORE_SOFTMAX;
+  uint32_t key[V];
+  float c[V];
+  float high = 0.f, inv = 1.f;
+  bool sure = true;
+  if (a.bias || grouped) {
+    if (soft) {
+      high = largest(l);
+      float total = 0.f;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        c[v] = v * 32 + lane < a.E && l[v] != -INFINITY ? exp_of((R)l[v] - high) : (R)0;
+        c[v] = l[v] == -INFINITY ? 0.f : fast_exp(l[v] - high);
         total += c[v];
       }
-      total = sum_of(total);
-      const R inv = total > (R)0 ? (R)1 / total : total;   // (a row of minus infinities: all scores are zero)
+      total = warp_sum(total);
+      inv = total > 0.f ? fast_rcp(total) : total;       // (a row of minus infinities: all scores are zero)
 #pragma unroll
       for (int v = 0; v < V; ++v) c[v] *= inv;
     } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v) c[v] = (R)1 / ((R)1 + exp_of(-(R)l[v]));
+      for (int v = 0; v < V; ++v) c[v] = fast_rcp(1.0f + fast_exp(-l[v]));
     }
+    float far = 0.f;
     if (a.bias) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const float b = v * 32 + lane < a.E ? a.bias[v * 32 + lane] : 0.f;
-        c[v] += (R)b;
+        c[v] += b;
         far = fmaxf(far, fabsf(b));
       }
-      if (sizeof(R) == 4) far = __uint_as_float(__reduce_max_sync(ALL, __float_as_uint(far)));
+    }
+    if (grouped) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (v * 32 + lane < a.E) room[v * 32 + lane] = fmaxf(c[v], -INFINITY);
+      __syncwarp();
+      int per;
+      float sum;
+      bool in;
+      const uint32_t taken = choose_groups(a, room, lane, per, sum, in);
+      // Two scores each.  128 half units: as much as a score's exponent can cost before nothing is left of the score.
+      const float last = value_of(~__reduce_max_sync(ALL, in ? ~key_of(sum) : 0u));
+      const float next = value_of(__reduce_max_sync(ALL, lane / per < a.groups && !in ? key_of(sum) : 0x007FFFFFu));
+      far = __uint_as_float(__reduce_max_sync(ALL, __float_as_uint(far)));
+      if (last - next <= 2.0f * 128.0f * HALF_ULP * (fabsf(last) + 2.0f * far)) sure = false;
+      const int size = a.E / a.groups;
+      const uint32_t magic = (1048576u + size - 1) / size;      // e / size for e < 1024
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] = (taken >> (((uint32_t)(v * 32 + lane) * magic >> 20) * per)) & 1u;
+      __syncwarp();
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) key[v] = 1u;
+    }
+    if (!a.bias) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) c[v] = l[v];
+    }
+  } else {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      key[v] = 1u;
+      c[v] = l[v];                      // without a bias the scores are in the order of the logits
     }
   }
 #pragma unroll
-  for (int v = 0; v < V; ++v) key[v] = v * 32 + lane < a.E ? (a.bias ? key_of(c[v]) : (Key)key_of((R)l[v])) : (Key)0;
-  // How far the fp32 scores may be off, relative to themselves and the bias: the sigmoid's exponential (two units in the last
-  // place), sum, quotient and the bias are 7 roundings of 2^-24; a softmax has up to 37 in its total, and its exponent's
-  // rounding counts |l - max| times (beyond 80 nothing is left of a score).
-  const float off = (a.score == OSDP_SCORE_SIGMOID ? 8.0f : 128.0f) * 5.9604645e-8f;
-  bool sure = true;
-  if (grouped) {
+  for (int v = 0; v < V; ++v) key[v] = key[v] && v * 32 + lane < a.E ? (key_of(c[v]) & ~(uint32_t)(V - 1)) | (uint32_t)(V - 1 - v) : 0u;
+  // descending (a bitonic network)
+#pragma unroll
+  for (int n = 2; n <= V; n *= 2)
+#pragma unroll
+    for (int o = n / 2; o > 0; o /= 2)
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if ((v & o) == 0) {
+          const uint32_t hi = max(key[v], key[v | o]), lo = min(key[v], key[v | o]);
+          key[v] = (v & n) == 0 ? hi : lo;
+          key[v | o] = (v & n) == 0 ? lo : hi;
+        }
+  // one more than are wanted, to see how far away it is
+  uint32_t got = 0;
+  for (int j = 0; j <= a.k; ++j) {
+    const uint32_t best = __reduce_max_sync(ALL, key[0]);
+    if (best == 0) break;             // (only behind the last one wanted: the groups have enough experts)
+    const int owner = __ffs(__ballot_sync(ALL, key[0] == best)) - 1;      // equal keys: the same register, the lower lane
+    if (lane == j) {
+      got = best;
+      mine = (V - 1 - (int)(best & (V - 1))) * 32 + owner;
+    }
+    if (lane == owner) {
+#pragma unroll
+      for (int v = 0; v + 1 < V; ++v) key[v] = key[v + 1];
+      key[V - 1] = 0;
+    }
+  }
+  float bj = 0.f, off = 0.f;
+  const float value = value_of(got & ~(uint32_t)(V - 1));
+  if (mine >= 0) {
+    lj = widen(row[mine]);
+    off = 2.0f * V * fabsf(value);                                          // the bits that the place took
+    if (a.bias) {
+      bj = a.bias[mine];
+      // the score: exponent (1.5 times its size), exponential and reciprocal 4 each, a softmax's total up to 37; and the sum with the bias
+      const float s = fabsf(value - bj);
+      off += fabsf(value) + fabsf(bj) + (soft ? s * (1.5f * (high - lj) + 46.0f) : s * ((1.0f - fminf(s, 1.0f) + 0.01f) * (1.5f * fabsf(lj) + 6.0f) + 6.0f));
+    }
+  }
+  const int after = __shfl_down_sync(ALL, mine, 1);
+  const float less = __shfl_down_sync(ALL, value, 1), less_off = __shfl_down_sync(ALL, off, 1), less_l = __shfl_down_sync(ALL, lj, 1),
+              less_b = __shfl_down_sync(ALL, bj, 1);
+  // as close as that: the same in exact arithmetic only if it is the same logit and the same bias
+  if (lane < a.k && after >= 0 && value - less <= HALF_ULP * (off + less_off) && (lj != less_l || bj != less_b)) sure = false;
+  return __all_sync(ALL, sure);
+}
+
+// The same in fp64, score by score.
+template <int V, typename L>
+__device__ __noinline__ void choose_exactly(const RouteArgs &a, const L *row, double *room, int lane, int &mine) {
+  unsigned long long key[V];
+  double c[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) c[v] = v * 32 + lane < a.E ? (double)widen(row[v * 32 + lane]) : -(double)INFINITY;
+#pragma unroll
+  for (int v = 0; v < V; ++v) key[v] = v * 32 + lane < a.E ? key_of(c[v]) : 0ull;
+  if (a.bias || a.top_groups < a.groups) {
+    if (a.score == OSDP_SCORE_SOFTMAX) {
+      unsigned long long top = 0;
+#pragma unroll
+      for (int v = 0; v < V; ++v) top = key[v] > top ? key[v] : top;
+      top = warp_top(top);
+      const double high = __longlong_as_double((long long)((top >> 63) ? top & 0x7FFFFFFFFFFFFFFFull : ~top));
+      double total = 0.0;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        c[v] = c[v] == -(double)INFINITY ? 0.0 : exp(c[v] - high);
+        total += c[v];
+      }
+      total = sum_of(total);
+#pragma unroll
+      for (int v = 0; v < V; ++v) c[v] = total == 0.0 ? 0.0 : c[v] / total;
+    } else {
+#pragma unroll
+      for (int v = 0; v < V; ++v) c[v] = 1.0 / (1.0 + exp(-c[v]));
+    }
+    if (a.bias) {
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (v * 32 + lane < a.E) {
+          c[v] += (double)a.bias[v * 32 + lane];
+          key[v] = key_of(c[v]);
+        }
+    }
+  }
+  if (a.top_groups < a.groups) {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (v * 32 + lane < a.E) room[v * 32 + lane] = c[v] == c[v] ? c[v] : -(double)INFINITY;
+    __syncwarp();
+    int per;
+    double sum;
+    bool in;
+    const uint32_t taken = choose_groups(a, room, lane, per, sum, in);
     const int size = a.E / a.groups;
 #pragma unroll
     for (int v = 0; v < V; ++v)
-      if (v * 32 + lane < a.E) room[v * 32 + lane] = c[v] == c[v] ? c[v] : low;
-    __syncwarp();
-    // `per` lanes for each group
-    int per = 32;
-    while (per * a.groups > 32) per >>= 1;
-    const int g = lane / per;
-    R first = low, second = low;
-    if (g < a.groups) {
-      for (int e = lane % per; e < size; e += per) {
-        const R x = room[g * size + e];
-        second = x > first ? first : (x > second ? x : second);
-        first = x > first ? x : first;
-      }
-    }
-    for (int o = 1; o < per; o <<= 1) {
-      const R f = __shfl_xor_sync(ALL, first, o), s = __shfl_xor_sync(ALL, second, o);
-      const R less = f > first ? first : f;
-      second = s > second ? s : second;
-      second = less > second ? less : second;
-      first = f > first ? f : first;
-    }
-    R sum = a.take > 1 && size > 1 ? first + second : first;
-    if (sum != sum) sum = low;
-    int rank = 0;
-    for (int h = 0; h < a.groups; ++h) {
-      const R other = __shfl_sync(ALL, sum, h * per);
-      rank += other > sum || (other == sum && h < g) ? 1 : 0;
-    }
-    const bool in = g < a.groups && rank < a.top_groups;
-    const uint32_t taken = __ballot_sync(ALL, in && lane % per == 0);
-    if (sizeof(R) == 4) {
-      // the last group that is taken against the first that is not
-      const float last = value_of(~__reduce_max_sync(ALL, in ? ~key_of((float)sum) : 0u));
-      const float next = value_of(__reduce_max_sync(ALL, g < a.groups && !in ? key_of((float)sum) : 0x007FFFFFu));
-      if (last - next <= 2.0f * off * (fabsf(last) + 2.0f * far)) sure = false;
-    }
-    const uint32_t magic = (1048576u + size - 1) / size;      // e / size for e < 1024
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const uint32_t mine_g = (uint32_t)(v * 32 + lane) * magic >> 20;
-      if (v * 32 + lane < a.E && !((taken >> (mine_g * per)) & 1u)) key[v] = 0;
-    }
-    __syncwarp();
+      if (!((taken >> ((v * 32 + lane) / size * per)) & 1u)) key[v] = 0ull;
   }
-  // one more than are wanted, to see how far away it is
-  float value = 0.f;
-  for (int j = 0; j <= a.k; ++j) {
-    Key best = 0;
+  for (int j = 0; j < a.k; ++j) {
+    unsigned long long best = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) best = key[v] > best ? key[v] : best;
     best = warp_top(best);
-    if (best == 0) break;             // (only behind the last one wanted: the groups have enough experts)
     int e = 1 << 20;
 #pragma unroll
     for (int v = V - 1; v >= 0; --v) e = key[v] == best ? v * 32 + lane : e;
     e = __reduce_min_sync(ALL, e);
 #pragma unroll
-    for (int v = 0; v < V; ++v) key[v] = v * 32 + lane == e ? (Key)0 : key[v];
-    if (lane == j) {
-      mine = e;
-      if (sizeof(R) == 4) value = value_of((uint32_t)best);
-    }
-    if (!a.bias && j + 1 == a.k) break;
+    for (int v = 0; v < V; ++v) key[v] = v * 32 + lane == e ? 0ull : key[v];
+    if (lane == j) mine = e;
   }
-  if (sizeof(R) == 4 && a.bias) {
-    const int after = __shfl_down_sync(ALL, mine, 1);
-    const float less = __shfl_down_sync(ALL, value, 1);
-    // as close as that: the same in exact arithmetic only if it is the same logit and the same bias
-    if (lane < a.k && after >= 0 && value - less <= off * (fabsf(value) + fabsf(less) + 2.0f * far) &&
-        (widen(row[mine]) != widen(row[after]) || a.bias[mine] != a.bias[after]))
-      sure = false;
-  }
-  return __all_sync(ALL, sure);
 }
 
 // The weights' parts of the chosen experts, lanes 0 .. k - 1 (their logits in `l`): r_j = s_j / sum s, formed from the chosen
@@ -201,7 +305,7 @@ __device__ __forceinline__ float share_of(const RouteArgs &a, float l, bool on, 
 }
 
 template <typename L, int V>
-__global__ void __launch_bounds__(256) route_fwd_kernel(const __grid_constant__ RouteArgs a) {
+__global__ void __launch_bounds__(256, V <= 8 ? 4 : 1) route_fwd_kernel(const __grid_constant__ RouteArgs a) {
   extern __shared__ double rooms[];
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31;
@@ -214,22 +318,19 @@ __global__ void __launch_bounds__(256) route_fwd_kernel(const __grid_constant__ 
 #pragma unroll
   for (int v = 0; v < V; ++v) l[v] = v * 32 + lane < a.E ? widen(row[v * 32 + lane]) : -INFINITY;
   int mine = -1;
-  if (!choose<float, V, L>(a, row, l, reinterpret_cast<float *>(room), lane, mine)) {
-    __syncwarp();
-    choose<double, V, L>(a, row, l, room, lane, mine);
+  float lj = -INFINITY;
+  if (!choose_fast<V, L>(a, row, l, reinterpret_cast<float *>(room), lane, mine, lj)) {
+    choose_exactly<V, L>(a, row, room, lane, mine);
+    if (lane < a.k) lj = widen(row[mine]);
   }
   const bool on = lane < a.k;
-  const float lj = on ? widen(row[mine]) : -INFINITY;
   float w;
   if (a.renorm) {
     w = share_of(a, lj, on, lane);
   } else if (a.score == OSDP_SCORE_SIGMOID) {
     w = 1.0f / (1.0f + expf(-lj));
   } else {
-    uint32_t top = 0;
-#pragma unroll
-    for (int v = 0; v < V; ++v) top = max(top, key_of(l[v]));
-    const float high = value_of(__reduce_max_sync(ALL, top));
+    const float high = largest(l);
     float total = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) total += l[v] == -INFINITY ? 0.f : expf(l[v] - high);
@@ -338,12 +439,11 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_bwd_kernel(const __gri
 // ------------------------------------------------------------------------------------------------
 // The plan: a stable counting sort of the T k choices by expert.  One launch of a cluster: a warp counts a contiguous part
 // of the choices into its own table, the tables' prefix sums over warps and (through distributed shared memory) over the
-// cluster's blocks say where each warp's rows of each expert start, and a second pass hands them out in order.  No
-// atomics between warps: the same choices give the same plan.
+// cluster's blocks say where each warp's rows of each expert start, and a second pass hands them out in order: the same
+// choices give the same plan.
 struct PlanArgs {
   const int32_t *idx;
-  long long n;
-  int E;
+  int n, E;
   int32_t *plan, *pos;
 };
 constexpr int PLAN_WARPS = 32;
@@ -367,48 +467,51 @@ __device__ __forceinline__ int peer_int(const int *p, uint32_t cta) {
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
   return (int)v;
 }
-// Inclusive sums over the block's 1024 threads.
-__device__ __forceinline__ int block_scan(int v, int *warps) {
+// Inclusive sums of N values over the block's 1024 threads.
+template <int N>
+__device__ __forceinline__ void block_scan(int (&v)[N], int (*warps)[PLAN_WARPS]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int w[N];
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(ALL, v, o);
-    if (lane >= o) v += u;
-  }
-  if (lane == 31) warps[warp] = v;
+  for (int o = 1; o < 32; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = __shfl_up_sync(ALL, v[i], o);
+      if (lane >= o) v[i] += u;
+    }
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (lane == 31) warps[i][warp] = v[i];
   __syncthreads();
-  int before = 0;
-  for (int w = 0; w < warp; ++w) before += warps[w];
-  __syncthreads();
-  return v + before;
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = lane < warp ? warps[i][lane] : 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] += __reduce_add_sync(ALL, w[i]);
 }
 
 __global__ void __launch_bounds__(32 * PLAN_WARPS, 1) expert_plan_kernel(const __grid_constant__ PlanArgs a) {
-  extern __shared__ int tables[];              // [PLAN_WARPS][E], then this block's totals [E]
-  __shared__ int sums[PLAN_WARPS];
+  extern __shared__ int tables[];              // [PLAN_WARPS][E], then this block's totals [E], then where its rows start [E]
+  __shared__ int sums[4][PLAN_WARPS];
   const int E = a.E, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
-  int *totals = tables + PLAN_WARPS * E;
+  int *totals = tables + PLAN_WARPS * E, *starts = totals + E;
   const uint32_t rank = cta_rank_in_cluster(), ctas = ctas_in_cluster();
   pdl_launch_dependents();
   for (int i = tid; i < PLAN_WARPS * E; i += blockDim.x) tables[i] = 0;
   __syncthreads();
   pdl_wait();
   int *mine = tables + warp * E;
-  const long long parts = (long long)ctas * PLAN_WARPS;
-  const long long part = ((a.n + parts - 1) / parts + 31) / 32 * 32;
-  const long long begin = ((long long)rank * PLAN_WARPS + warp) * part, end = min(a.n, begin + part);
+  const int parts = (int)ctas * PLAN_WARPS, part = ((a.n + parts - 1) / parts + 31) / 32 * 32;
+  const int begin = (int)min((long long)((int)rank * PLAN_WARPS + warp) * part, (long long)a.n), end = min(a.n, begin + part);
   constexpr int AHEAD = 4;
-  auto expert_at = [&](long long i) { return i < end ? a.idx[i] : -1; };
-  for (long long i0 = begin; i0 < end; i0 += 32 * AHEAD) {
+  const int bits = 32 - __clz(E - 1);          // (0 for one expert)
+  auto expert_at = [&](int i) { return i < end ? a.idx[i] : -1; };
+  for (int i0 = begin; i0 < end; i0 += 32 * AHEAD) {
     int e[AHEAD];
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) e[q] = expert_at(i0 + 32 * q + lane);
 #pragma unroll
-    for (int q = 0; q < AHEAD; ++q) {
-      const uint32_t same = __match_any_sync(ALL, e[q]);
-      if (e[q] >= 0 && e[q] < E && lane == __ffs(same) - 1) mine[e[q]] += __popc(same);
-      __syncwarp();
-    }
+    for (int q = 0; q < AHEAD; ++q)
+      if (e[q] >= 0 && e[q] < E) atomicAdd(mine + e[q], 1);
   }
   __syncthreads();
   if (tid < E) {
@@ -430,50 +533,55 @@ __global__ void __launch_bounds__(32 * PLAN_WARPS, 1) expert_plan_kernel(const _
     }
   }
   const int padded = (count + OSDP_EXPERT_ROWS - 1) / OSDP_EXPERT_ROWS * OSDP_EXPERT_ROWS;
-  const int offset = block_scan(padded, sums) - padded;
-  if (tid < E)
-    for (int w = 0; w < PLAN_WARPS; ++w) tables[w * E + tid] += offset + before;
-  if (rank == 0) {
+  const int t128 = (count + 127) / 128, t256 = (count + 255) / 256, live = count > 0 ? 1 : 0;
+  int upto[4] = {padded, t128, t256, live};
+  block_scan(upto, sums);
+  const int offset = upto[0] - padded;
+  if (tid < E) starts[tid] = offset + before;
+  if (rank == 0 && tid < E) {
     int32_t *p = a.plan;
-    const int t128 = (count + 127) / 128, t256 = (count + 255) / 256, live = count > 0 ? 1 : 0;
-    const int s128 = block_scan(t128, sums), s256 = block_scan(t256, sums), at = block_scan(live, sums);
-    if (tid < E) {
-      p[PLAN_OFFSETS + tid] = offset;
-      p[plan_counts(E) + tid] = count;
-      p[plan_tiles128(E) + tid] = s128 - t128;
-      p[plan_tiles256(E) + tid] = s256 - t256;
-      if (live) p[plan_live(E) + at - 1] = tid;
-      if (tid == E - 1) {
-        p[PLAN_OFFSETS + E] = offset + padded;
-        p[plan_tiles128(E) + E] = s128;
-        p[plan_tiles256(E) + E] = s256;
-        p[plan_n_live(E)] = at;
-      }
+    p[PLAN_OFFSETS + tid] = offset;
+    p[plan_counts(E) + tid] = count;
+    p[plan_tiles128(E) + tid] = upto[1] - t128;
+    p[plan_tiles256(E) + tid] = upto[2] - t256;
+    if (live) p[plan_live(E) + upto[3] - 1] = tid;
+    if (tid == E - 1) {
+      p[PLAN_OFFSETS + E] = upto[0];
+      p[plan_tiles128(E) + E] = upto[1];
+      p[plan_tiles256(E) + E] = upto[2];
+      p[plan_n_live(E)] = upto[3];
     }
   }
   __syncthreads();
-  for (long long i0 = begin; i0 < end; i0 += 32 * AHEAD) {
+  for (int i0 = begin; i0 < end; i0 += 32 * AHEAD) {
     int e[AHEAD];
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) e[q] = expert_at(i0 + 32 * q + lane);
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) {
-      const long long i = i0 + 32 * q + lane;
-      const uint32_t same = __match_any_sync(ALL, e[q]);
+      const int i = i0 + 32 * q + lane;
       const bool in = e[q] >= 0 && e[q] < E;
+      // the lanes with the same expert, bit by bit of its number (match.any takes 64 cycles of the whole SM: 131072 choices of
+      // 256 experts 36 us with it, of which the two passes' 16 matches a warp were 30)
+      uint32_t same = __ballot_sync(ALL, in);
+      for (int b = 0; b < bits; ++b) {
+        const uint32_t has = __ballot_sync(ALL, (e[q] >> b) & 1);
+        same &= (e[q] >> b) & 1 ? has : ~has;
+      }
       const int first = in ? mine[e[q]] : 0;
       __syncwarp();
       if (in && lane == __ffs(same) - 1) mine[e[q]] = first + __popc(same);
       __syncwarp();
-      if (i < end) a.pos[i] = in ? first + __popc(same & ((1u << lane) - 1u)) : -1;
+      if (i < end) a.pos[i] = in ? starts[e[q]] + first + __popc(same & ((1u << lane) - 1u)) : -1;
     }
   }
   cluster_sync();        // nobody leaves while another block may still read its totals
 }
 
 // ------------------------------------------------------------------------------------------------
-// Dispatch, combine.  A thread has eight channels of one token: it reads the token's piece once and writes it to the k rows,
-// or adds the k rows' pieces in order of the choices.  Bound by memory.
+// Dispatch, combine.  A block takes CHUNK neighbouring pieces of eight channels; a thread has PER of them, reads a token's piece
+// once and writes it to the k rows, or adds the k rows' pieces in order of the choices.  Bound by memory: the pieces of a
+// thread are independent, all their loads are on the way together, and the one division is made per block.
 struct RowsArgs {
   const __nv_bfloat16 *x;        // dispatch: [T, D]; combine: rows
   const int32_t *plan, *pos;
@@ -484,6 +592,7 @@ struct RowsArgs {
   long long T;
   int k, E, D;
   long long token_blocks;        // dispatch: the blocks behind these clear the rows between the experts
+  uint32_t magic;                // 2^32 / (D / 8), rounded up; 0 for D = 8
   int team;                      // dispatch with dweights: warps to a (token, choice)
 };
 
@@ -494,33 +603,55 @@ __device__ __forceinline__ void clear_between(const RowsArgs &a, int e) {
   for (long long i = threadIdx.x; i < n; i += blockDim.x) p[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
+// Pieces of a thread.  More of them, or fewer threads on an SM, and the pieces' addresses and sums cost more than the loads gain:
+// combine of two rows 16384 x 8192 135 us with 2 pieces and 5 blocks on an SM (4 and 2: 164, 1 and 8: 138; floor 123), of eight
+// rows 8192 x 2048 48 us with one piece and 6 blocks (4 and 1: 53; floor 46); dispatch does not mind.
+template <int K>
+struct Combine {
+  static constexpr int PER = K <= 2 ? 2 : 1, BLOCKS = K <= 2 ? 5 : 6, CHUNK = 256 * PER;
+};
+constexpr int PER = 2, CHUNK = 256 * PER;       // dispatch
+
+// Token and first channel of piece `i` of a chunk that starts `lead` pieces into token t0.  Exact: lead + i < D / 8 + CHUNK, and that
+// times D / 8 is below 2^32.
+__device__ __forceinline__ void locate(const RowsArgs &a, long long t0, uint32_t at, long long &t, int &c) {
+  const uint32_t pieces = (uint32_t)a.D >> 3, q = a.magic ? __umulhi(at, a.magic) : at;
+  t = t0 + q;
+  c = (int)((at - q * pieces) << 3);
+}
+
+template <bool WEIGHTED>
 __global__ void __launch_bounds__(256) dispatch_kernel(const __grid_constant__ RowsArgs a) {
   pdl_launch_dependents();
   pdl_wait();
   if (blockIdx.x >= a.token_blocks) return clear_between(a, (int)(blockIdx.x - a.token_blocks));
-  const int pieces = a.D >> 3;
-  const long long n = a.T * pieces, stride = a.token_blocks * blockDim.x;
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += stride) {
-    const long long t = i / pieces;
-    const int c = (int)(i - t * pieces) << 3;
-    const uint4 v = load16(a.x + t * a.D + c);
-    const int32_t *pos = a.pos + t * a.k;
-    if (!a.weights) {
-      for (int j = 0; j < a.k; ++j) {
-        const long long r = pos[j];
-        if (r >= 0) *reinterpret_cast<uint4 *>(a.out + r * a.D + c) = v;
-      }
-    } else {
-      float f[8];
-      widen8(v, f);
-      for (int j = 0; j < a.k; ++j) {
-        const long long r = pos[j];
-        const float w = a.weights[t * a.k + j];
-        float g[8];
+  const long long start = (long long)blockIdx.x * CHUNK, n = a.T * (a.D >> 3) - start;
+  const long long t0 = start / (a.D >> 3);
+  const uint32_t lead = (uint32_t)(start - t0 * (a.D >> 3));
+  uint4 v[PER];
+  long long t[PER];
+  int c[PER];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) g[q] = f[q] * w;
-        if (r >= 0) *reinterpret_cast<uint4 *>(a.out + r * a.D + c) = narrow8(g);
+  for (int u = 0; u < PER; ++u) {
+    const int i = (int)threadIdx.x + u * 256;
+    locate(a, t0, lead + i, t[u], c[u]);
+    v[u] = i < n ? load16(a.x + t[u] * a.D + c[u]) : make_uint4(0u, 0u, 0u, 0u);
+  }
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    if ((int)threadIdx.x + u * 256 >= n) break;
+    for (int j = 0; j < a.k; ++j) {
+      const long long r = a.pos[t[u] * a.k + j];
+      uint4 w = v[u];
+      if (WEIGHTED) {
+        const float f = a.weights[t[u] * a.k + j];
+        float g[8];
+        widen8(v[u], g);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) g[q] *= f;
+        w = narrow8(g);
       }
+      if (r >= 0) *reinterpret_cast<uint4 *>(a.out + r * a.D + c[u]) = w;
     }
   }
 }
@@ -566,37 +697,49 @@ __global__ void __launch_bounds__(256) dispatch_dot_kernel(const __grid_constant
   if (there && tl == 0) a.dweights[slot] = dot;
 }
 
-__global__ void __launch_bounds__(256) combine_kernel(const __grid_constant__ RowsArgs a) {
+// K: rows that a thread has on the way for each of its pieces (k itself up to 2).
+template <int K>
+__global__ void __launch_bounds__(256, Combine<K>::BLOCKS) combine_kernel(const __grid_constant__ RowsArgs a) {
   pdl_launch_dependents();
   pdl_wait();
-  const int pieces = a.D >> 3;
-  const long long n = a.T * pieces, stride = (long long)gridDim.x * blockDim.x;
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += stride) {
-    const long long t = i / pieces;
-    const int c = (int)(i - t * pieces) << 3;
-    float sum[8];
+  constexpr int AT_ONCE = Combine<K>::PER;
+  const long long start = (long long)blockIdx.x * Combine<K>::CHUNK, n = a.T * (a.D >> 3) - start;
+  const long long t0 = start / (a.D >> 3);
+  const uint32_t lead = (uint32_t)(start - t0 * (a.D >> 3));
+  long long t[AT_ONCE];
+  int c[AT_ONCE];
+  float sum[AT_ONCE][8];
 #pragma unroll
-    for (int q = 0; q < 8; ++q) sum[q] = 0.f;
-    constexpr int AHEAD = 4;
-    for (int j0 = 0; j0 < a.k; j0 += AHEAD) {
-      uint4 v[AHEAD];
-      float w[AHEAD];
+  for (int u = 0; u < AT_ONCE; ++u) {
+    locate(a, t0, lead + threadIdx.x + u * 256, t[u], c[u]);
 #pragma unroll
-      for (int q = 0; q < AHEAD; ++q) {
-        const long long r = j0 + q < a.k ? a.pos[t * a.k + j0 + q] : -1;
-        v[q] = r >= 0 ? load16(a.x + r * a.D + c) : make_uint4(0u, 0u, 0u, 0u);
-        w[q] = r < 0 ? 0.f : a.weights ? a.weights[t * a.k + j0 + q] : 1.0f;
-      }
-#pragma unroll
-      for (int q = 0; q < AHEAD; ++q) {
-        float f[8];
-        widen8(v[q], f);
-#pragma unroll
-        for (int h = 0; h < 8; ++h) sum[h] = fmaf(w[q], f[h], sum[h]);
-      }
-    }
-    *reinterpret_cast<uint4 *>(a.out + t * a.D + c) = narrow8(sum);
+    for (int q = 0; q < 8; ++q) sum[u][q] = 0.f;
   }
+  for (int j0 = 0; j0 < a.k; j0 += K) {
+    uint4 v[AT_ONCE][K];
+    float w[AT_ONCE][K];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+      for (int q = 0; q < K; ++q) {
+        const bool there = (int)threadIdx.x + u * 256 < n && (K <= 2 || j0 + q < a.k);
+        const long long slot = t[u] * a.k + j0 + q, r = there ? a.pos[slot] : -1;
+        v[u][q] = r >= 0 ? load16(a.x + r * a.D + c[u]) : make_uint4(0u, 0u, 0u, 0u);
+        w[u][q] = r < 0 ? 0.f : a.weights ? a.weights[slot] : 1.0f;
+      }
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u)
+#pragma unroll
+      for (int q = 0; q < K; ++q) {
+        float f[8];
+        widen8(v[u][q], f);
+#pragma unroll
+        for (int h = 0; h < 8; ++h) sum[u][h] = fmaf(w[u][q], f[h], sum[u][h]);
+      }
+  }
+#pragma unroll
+  for (int u = 0; u < AT_ONCE; ++u)
+    if ((int)threadIdx.x + u * 256 < n) *reinterpret_cast<uint4 *>(a.out + t[u] * a.D + c[u]) = narrow8(sum[u]);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -637,10 +780,14 @@ int launch_route(const RouteArgs &a, cudaStream_t stream) {
 int check_rows(int64_t T, int top_k, int E, int64_t D) {
   const int rc = check_choices(T, top_k, E);
   if (rc) return rc;
-  if (D <= 0 || D > ((int64_t)1 << 24)) return OSDP_ERR_BAD_SHAPE;
+  if (D <= 0 || D > OSDP_EXPERT_MAX_D || T * (D / 8) > ((int64_t)1 << 40)) return OSDP_ERR_BAD_SHAPE;
   return (D & 7) ? OSDP_ERR_ALIGNMENT : OSDP_OK;
 }
 
+}  // namespace
+
+namespace {
+uint32_t piece_magic(int64_t D) { return D > 8 ? (uint32_t)((((uint64_t)1 << 32) + D / 8 - 1) / (D / 8)) : 0u; }
 }  // namespace
 
 int64_t expert_rows(int64_t T, int top_k, int E) {
@@ -705,12 +852,12 @@ extern "C" int osdp_expert_plan(const int32_t *idx, int64_t T, int top_k, int E,
   if (rc) return rc;
   if (!plan || (T > 0 && (!idx || !pos))) return OSDP_ERR_NULL_POINTER;
   if (!aligned_to(idx, 4) || !aligned_to(plan, 16) || !aligned_to(pos, 4)) return OSDP_ERR_ALIGNMENT;
-  const size_t smem = (size_t)(PLAN_WARPS + 1) * E * sizeof(int);
+  const size_t smem = (size_t)(PLAN_WARPS + 2) * E * sizeof(int);
   if (smem > 40 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(expert_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (PLAN_WARPS + 1) * OSDP_MAX_EXPERTS * 4);
+    const cudaError_t e = cudaFuncSetAttribute(expert_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (PLAN_WARPS + 2) * OSDP_MAX_EXPERTS * 4);
     if (e != cudaSuccess) return report_cuda(e);
   }
-  const PlanArgs a{idx, (long long)(T * top_k), E, plan, pos};
+  const PlanArgs a{idx, (int)(T * top_k), E, plan, pos};
   // one block up to a choice per thread, a cluster of eight beyond
   const int ctas = T * top_k <= 32 * PLAN_WARPS ? 1 : 8;
   return launch_overlapped(expert_plan_kernel, dim3(ctas), dim3(32 * PLAN_WARPS), smem, ctas, static_cast<cudaStream_t>(stream), a);
@@ -726,7 +873,7 @@ extern "C" int osdp_expert_dispatch(const void *x, const int32_t *plan, const in
       !aligned_to(weights, 4) || !aligned_to(dweights, 4))
     return OSDP_ERR_ALIGNMENT;
   RowsArgs a{static_cast<const __nv_bfloat16 *>(x), plan, pos, weights, static_cast<const __nv_bfloat16 *>(y_rows), static_cast<__nv_bfloat16 *>(rows),
-             dweights, (long long)T, top_k, E, (int)D, 0, 1};
+             dweights, (long long)T, top_k, E, (int)D, 0, piece_magic(D), 1};
   if (dweights) {
     int sms = 0;
     const int src = sm_count(&sms);
@@ -737,8 +884,9 @@ extern "C" int osdp_expert_dispatch(const void *x, const int32_t *plan, const in
     a.token_blocks = cdiv(T * top_k, 8 / a.team);
     return launch_overlapped(dispatch_dot_kernel, dim3((unsigned)(a.token_blocks + E)), dim3(256), 0, 1, static_cast<cudaStream_t>(stream), a);
   }
-  a.token_blocks = cdiv(T * (D / 8), 256);
-  return launch_overlapped(dispatch_kernel, dim3((unsigned)(a.token_blocks + E)), dim3(256), 0, 1, static_cast<cudaStream_t>(stream), a);
+  a.token_blocks = cdiv(T * (D / 8), CHUNK);
+  return launch_overlapped(weights ? dispatch_kernel<true> : dispatch_kernel<false>, dim3((unsigned)(a.token_blocks + E)), dim3(256), 0, 1,
+                           static_cast<cudaStream_t>(stream), a);
 }
 
 extern "C" int osdp_expert_combine(const void *rows, const int32_t *plan, const int32_t *pos, const float *weights, int64_t T, int top_k, int E,
@@ -749,6 +897,9 @@ extern "C" int osdp_expert_combine(const void *rows, const int32_t *plan, const 
   if (!rows || !pos || !plan || !out) return OSDP_ERR_NULL_POINTER;
   if (!aligned_to(rows, 16) || !aligned_to(out, 16) || !aligned_to(plan, 16) || !aligned_to(pos, 4) || !aligned_to(weights, 4)) return OSDP_ERR_ALIGNMENT;
   const RowsArgs a{static_cast<const __nv_bfloat16 *>(rows), plan, pos, weights, nullptr, static_cast<__nv_bfloat16 *>(out), nullptr, (long long)T,
-                   top_k, E, (int)D, 0, 1};
-  return launch_overlapped(combine_kernel, dim3((unsigned)cdiv(T * (D / 8), 256)), dim3(256), 0, 1, static_cast<cudaStream_t>(stream), a);
+                   top_k, E, (int)D, 0, piece_magic(D), 1};
+  const dim3 grid((unsigned)cdiv(T * (D / 8), top_k <= 2 ? Combine<2>::CHUNK : Combine<4>::CHUNK));
+  if (top_k == 1) return launch_overlapped(combine_kernel<1>, grid, dim3(256), 0, 1, static_cast<cudaStream_t>(stream), a);
+  if (top_k == 2) return launch_overlapped(combine_kernel<2>, grid, dim3(256), 0, 1, static_cast<cudaStream_t>(stream), a);
+  return launch_overlapped(combine_kernel<4>, grid, dim3(256), 0, 1, static_cast<cudaStream_t>(stream), a);
 }
