@@ -16,34 +16,34 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------
 // G = dY (.) act'(Z) and the sums of G's columns for each expert, in one pass (bound by memory).  A block takes 64 columns of
-// 256 of an expert's rows; the blocks' sums are added in a fixed order by a second kernel.  The sums are of the unrounded G.
+// 128 of an expert's rows; the blocks' sums are added in a fixed order by a second kernel.  The sums are of the unrounded G.
 // Rows between two experts become zero, whatever dY and Z hold there.
 struct GradArgs {
   const __nv_bfloat16 *dy, *z;
   __nv_bfloat16 *g;             // null: column sums of dY alone
   const int32_t *plan;
-  float *partial;               // [tiles of 256 rows][N], or null
+  float *partial;               // [tiles of 128 rows][N], or null
   int E, N, act;
 };
-constexpr int GRAD_ROWS = 256;
+constexpr int GRAD_ROWS = 128;
 
-// act'(x): 0.5 (1 + tanh u) = h = 1 / (1 + e), e = exp(-2 u), and act' = h + 2 x h (1 - h) u', 1 - h = e h: no difference of numbers
-// that are close, and the special-function unit's 2^-22 (tanh.approx has 2^-11, too coarse for sums kept in fp32).
-__device__ __forceinline__ float gelu_grad1(float x, int act) {
-  if (act == ACT_GELU_TANH) {
-    constexpr float a = 0.7978845608028654f, k = -2.0f * 1.4426950408889634f * a;
-    const float x2 = x * x;
-    float e, h;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fminf(x * fmaf(x2, k * 0.044715f, k), 126.0f)));
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(h) : "f"(1.0f + e));
-    const float du = fmaf(x2, 2.0f * a * 0.134145f, 2.0f * a);
-    return fmaf(x * h, (e * h) * du, h);
-  }
-  if (act == ACT_GELU_ERF) {
-    const float h = 0.5f * erfcf(-0.7071067811865476f * x);
-    return fmaf(x, 0.3989422804014327f * __expf(-0.5f * x * x), h);
-  }
-  return 1.0f;
+// act'(x) of the tanh form: 0.5 (1 + tanh u) = h = 1 / (1 + exp(-2 u)), and act' = h + 2 x h (1 - h) u'.  The special-function unit's 2^-22
+// (tanh.approx has 2^-11, too coarse for sums that are kept in fp32); two elements in an instruction.
+__device__ __forceinline__ f2 gelu_tanh_grad2(f2 x) {
+  constexpr float a = 0.7978845608028654f, k = -2.0f * 1.4426950408889634f * a;
+  const f2 one = both(1.0f), x2 = mul2(x, x);
+  const float2 arg = split2(mul2(x, fma2(x2, both(k * 0.044715f), both(k))));
+  float e0, e1, h0, h1;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(arg.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(arg.y));
+  const float2 d = split2(add2(pack2(e0, e1), one));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(h0) : "f"(d.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(h1) : "f"(d.y));
+  const f2 h = pack2(h0, h1), rest = fma2(h, both(-1.0f), one), du = fma2(x2, both(2.0f * a * 0.134145f), both(2.0f * a));
+  return fma2(mul2(mul2(x, h), rest), du, h);
+}
+__device__ __forceinline__ float gelu_erf_grad(float x) {
+  return fmaf(x, 0.3989422804014327f * __expf(-0.5f * x * x), 0.5f * erfcf(-0.7071067811865476f * x));
 }
 
 __device__ __forceinline__ int expert_of_tile(const int32_t *first, int E, int tile) {   // first[e] <= tile < first[e + 1]
@@ -56,20 +56,20 @@ __device__ __forceinline__ int expert_of_tile(const int32_t *first, int E, int t
   return lo;
 }
 
-__global__ void __launch_bounds__(256) expert_grad_kernel(const __grid_constant__ GradArgs a) {
+__global__ void __launch_bounds__(256, 4) expert_grad_kernel(const __grid_constant__ GradArgs a) {
   __shared__ float red[32][64 + 1];
   pdl_launch_dependents();
   const int cols = (a.N + 63) / 64;
   const int tile = (int)(blockIdx.x / cols), col = (int)(blockIdx.x % cols) * 64 + (threadIdx.x & 7) * 8, ty = threadIdx.x >> 3;
   pdl_wait();
-  const int32_t *tiles = a.plan + plan_tiles256(a.E);
+  const int32_t *tiles = a.plan + plan_tiles128(a.E);
   if (tile >= tiles[a.E]) return;
   const int e = expert_of_tile(tiles, a.E, tile);
   const int off = a.plan[PLAN_OFFSETS + e], first = (tile - tiles[e]) * GRAD_ROWS;
   const int count = a.plan[plan_counts(a.E) + e] - first, padded = a.plan[PLAN_OFFSETS + e + 1] - off - first;
-  float acc[8];
+  f2 acc[4];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+  for (int j = 0; j < 4; ++j) acc[j] = both(0.f);
   if (col < a.N) {
     constexpr int EACH = GRAD_ROWS / 32;
     const long long at = ((long long)off + first) * a.N + col;
@@ -83,27 +83,34 @@ __global__ void __launch_bounds__(256) expert_grad_kernel(const __grid_constant_
 #pragma unroll
     for (int q = 0; q < EACH; ++q) {
       const int r = ty + 32 * q;
-      float f[8];
-      widen8(d[q], f);
+      f2 f[4];
+      widen4(d[q], f);
       if (a.g) {
-        float x[8];
-        widen8(z[q], x);
+        f2 x[4];
+        widen4(z[q], x);
         if (a.act == ACT_GELU_TANH) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] *= gelu_grad1(x[j], ACT_GELU_TANH);
+          for (int j = 0; j < 4; ++j) f[j] = mul2(f[j], gelu_tanh_grad2(x[j]));
         } else {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) f[j] *= gelu_grad1(x[j], ACT_GELU_ERF);
+          for (int j = 0; j < 4; ++j) {
+            const float2 v = split2(x[j]);
+            f[j] = mul2(f[j], pack2(gelu_erf_grad(v.x), gelu_erf_grad(v.y)));
+          }
         }
-        if (r < min(padded, GRAD_ROWS)) *reinterpret_cast<uint4 *>(a.g + at + (long long)r * a.N) = narrow8(f);
+        if (r < min(padded, GRAD_ROWS)) *reinterpret_cast<uint4 *>(a.g + at + (long long)r * a.N) = narrow4(f);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] += f[j];
+      for (int j = 0; j < 4; ++j) acc[j] = add2(acc[j], f[j]);
     }
   }
   if (!a.partial) return;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) red[ty][(threadIdx.x & 7) * 8 + j] = acc[j];
+  for (int j = 0; j < 4; ++j) {
+    const float2 v = split2(acc[j]);
+    red[ty][(threadIdx.x & 7) * 8 + 2 * j] = v.x;
+    red[ty][(threadIdx.x & 7) * 8 + 2 * j + 1] = v.y;
+  }
   __syncthreads();
   const int c = (int)(blockIdx.x % cols) * 64 + threadIdx.x;
   if (threadIdx.x < 64 && c < a.N) {
@@ -120,7 +127,7 @@ __global__ void __launch_bounds__(128) expert_bias_kernel(const float *partial, 
   const int e = (int)blockIdx.y, c = (int)(blockIdx.x * blockDim.x + threadIdx.x);
   pdl_wait();
   if (c >= N) return;
-  const int32_t *tiles = plan + plan_tiles256(E);
+  const int32_t *tiles = plan + plan_tiles128(E);
   float s = 0.f;
   for (int t = tiles[e]; t < tiles[e + 1]; ++t) s += partial[(long long)t * N + c];
   db[(long long)e * N + c] = s;
@@ -145,7 +152,7 @@ struct PreparedGemm {
   ExpertGemm key;
   GemmParams p;
   int bn;
-  bool pair, heavy;
+  bool pair;
   int64_t items;
 };
 // Prepared launches (encoded tensor maps, tile choice) of this thread, as for the other products: they hold addresses and
@@ -188,27 +195,26 @@ int launch_tiles(const GemmParams &p, int64_t items, int sms, cudaStream_t strea
   return launch_overlapped(kernel, dim3((unsigned)(CTA2 ? 2 * n : n)), dim3(SL::THREADS), SL::TOTAL, CTA2 ? 2 : 1, stream, p);
 }
 
+// Eight epilogue warps everywhere (four but for the widest tile elsewhere): tiles are short, and what is drained from one has to
+// be out before the next one is done.
 int launch_prepared(const PreparedGemm &s, int sms, cudaStream_t stream) {
   const GemmParams &p = s.p;
   if (s.key.grp == GRP_RED) {
     if (s.pair && s.bn == 512) return launch_tiles<512, true, true, true, false, GRP_RED>(p, s.items, sms, stream);
-    if (s.pair) return launch_tiles<256, true, true, true, false, GRP_RED>(p, s.items, sms, stream);
-    if (s.bn == 256) return launch_tiles<256, true, true, false, false, GRP_RED>(p, s.items, sms, stream);
-    return launch_tiles<128, true, true, false, false, GRP_RED>(p, s.items, sms, stream);
+    if (s.pair) return launch_tiles<256, true, true, true, true, GRP_RED>(p, s.items, sms, stream);
+    if (s.bn == 256) return launch_tiles<256, true, true, false, true, GRP_RED>(p, s.items, sms, stream);
+    return launch_tiles<128, true, true, false, true, GRP_RED>(p, s.items, sms, stream);
   }
   if (s.key.b_mn) {
     if (s.pair && s.bn == 512) return launch_tiles<512, false, true, true, false, GRP_ROWS>(p, s.items, sms, stream);
-    if (s.pair) return launch_tiles<256, false, true, true, false, GRP_ROWS>(p, s.items, sms, stream);
-    if (s.bn == 256) return launch_tiles<256, false, true, false, false, GRP_ROWS>(p, s.items, sms, stream);
-    return launch_tiles<128, false, true, false, false, GRP_ROWS>(p, s.items, sms, stream);
+    if (s.pair) return launch_tiles<256, false, true, true, true, GRP_ROWS>(p, s.items, sms, stream);
+    if (s.bn == 256) return launch_tiles<256, false, true, false, true, GRP_ROWS>(p, s.items, sms, stream);
+    return launch_tiles<128, false, true, false, true, GRP_ROWS>(p, s.items, sms, stream);
   }
   if (s.pair && s.bn == 512) return launch_tiles<512, false, false, true, false, GRP_ROWS>(p, s.items, sms, stream);
-  if (s.pair && s.heavy) return launch_tiles<256, false, false, true, true, GRP_ROWS>(p, s.items, sms, stream);
-  if (s.pair) return launch_tiles<256, false, false, true, false, GRP_ROWS>(p, s.items, sms, stream);
-  if (s.bn == 256 && s.heavy) return launch_tiles<256, false, false, false, true, GRP_ROWS>(p, s.items, sms, stream);
-  if (s.bn == 256) return launch_tiles<256, false, false, false, false, GRP_ROWS>(p, s.items, sms, stream);
-  if (s.bn == 128 && s.heavy) return launch_tiles<128, false, false, false, true, GRP_ROWS>(p, s.items, sms, stream);
-  return launch_tiles<128, false, false, false, false, GRP_ROWS>(p, s.items, sms, stream);
+  if (s.pair) return launch_tiles<256, false, false, true, true, GRP_ROWS>(p, s.items, sms, stream);
+  if (s.bn == 256) return launch_tiles<256, false, false, false, true, GRP_ROWS>(p, s.items, sms, stream);
+  return launch_tiles<128, false, false, false, true, GRP_ROWS>(p, s.items, sms, stream);
 }
 
 int map3(CUtensorMap *m, const void *base, int eb, int64_t inner, int64_t rows, int64_t deep, int box_inner, int box_rows) {
@@ -273,7 +279,8 @@ int launch_expert_gemm(const ExpertGemm &c, cudaStream_t stream) {
     if (!rc && c.z_save) rc = map3(&p.z_main, c.z_save, 2, p.Q, c.R, 1, 64, 32);
   }
   if (rc) return rc;
-  p.a_tail = p.a_main; p.b_tail = p.b_main; p.out_tail = p.out_main; p.z_tail = p.z_main; p.carry_map = p.out_main;
+  p.a_tail = p.a_main;
+  p.b_tail = p.b_main; p.out_tail = p.out_main; p.z_tail = p.z_main; p.carry_map = p.out_main;
   p.mode = MODE_NONE;
   p.L = 0; p.k_total = 1; p.s_begin = 0; p.s_end = 1;
   p.red_group = 1;
@@ -297,10 +304,10 @@ int launch_expert_gemm(const ExpertGemm &c, cudaStream_t stream) {
   p.experts = c.E;
   slot.pair = pair;
   slot.bn = bn;
-  slot.heavy = c.act != ACT_NONE;
   // at most: every expert that can have rows leaves one tile partly filled
   const int tm = pair ? 256 : 128;
   slot.items = red ? tiles(tm, bn) : (n / tm + used) * cdiv(p.Q, bn);
+  if (slot.items >= (1 << 24)) return OSDP_ERR_BAD_SHAPE;      // what the kernel's tile arithmetic is exact for
   slot.valid = true;
   return launch_prepared(slot, sms, stream);
 }
@@ -361,6 +368,9 @@ extern "C" int osdp_expert_linear_fwd(const void *rows, const int32_t *plan, con
     return OSDP_ERR_ALIGNMENT;
   rc = check_workspace(ws, ws_bytes, w);
   if (rc) return rc;
+  if (expert_few_rows(T, top_k, E, N, K))
+    return launch_expert_few(rows, plan, static_cast<const __nv_bfloat16 *>(w_flat) + w_offset, bias, T, top_k, E, N, K, act, out, z_save,
+                             static_cast<cudaStream_t>(stream));
   ExpertGemm c;
   memset(&c, 0, sizeof(c));
   c.a = rows;

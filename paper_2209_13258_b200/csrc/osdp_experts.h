@@ -21,5 +21,9 @@ __host__ __device__ constexpr int plan_length(int E) { return (5 * E + 4 + 3) / 
 int64_t expert_rows(int64_t T, int top_k, int E);
 // The checks that every call over the experts' rows makes of T, top_k and E.
 int expert_check(int64_t T, int top_k, int E);
+// The products of few rows for each expert (osdp_expert_few.cu): whether they go there, and the launch.
+bool expert_few_rows(int64_t T, int top_k, int E, int64_t N, int64_t K);
+int launch_expert_few(const void *rows, const int32_t *plan, const void *w, const float *bias, int64_t T, int top_k, int E, int64_t N, int64_t K, int act,
+                      void *out, void *z_save, cudaStream_t stream);
 
 }  // namespace osdp

@@ -474,6 +474,7 @@ struct Work {
   int first_of_slice;        // MODE_RED: this CTA's first tile of slice s
   int k0;                    // GRP_RED: where the reduction starts (a row of the experts' rows)
   int valid_end;             // GRP_ROWS: the expert's rows end here; from here to row_end zeros are written
+  int first_tile, next_tile; // GRP_*: the tiles of expert s
 };
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
@@ -547,36 +548,55 @@ __device__ __forceinline__ bool get_work(const GemmParams &p, int i, int bid, in
 //             from whatever is there and not stored.
 //   GRP_RED   OUT_e = A[rows of e, :]^T B[rows of e, :]: the tiles of every expert, over its rows.  An expert without rows takes
 //             one k-block behind the last row, which the copies fill with zeros.
-// How many rows an expert has is only known on the device: every role walks the plan's tables in the same way (w.s stays
-// where the tile before was found).
+// How many rows an expert has is only known on the device: every role walks the plan's tables in the same way, on from where
+// the tile before was found (bf16 operands only: a k-block is 64 rows).
 enum : int { GRP_NONE = 0, GRP_ROWS = 1, GRP_RED = 2 };
+
+// a / b and the remainder for 0 <= a < 2^24, 0 < b: by the reciprocal, put right by one (an integer division takes tens of
+// instructions, in every role and for every tile)
+__device__ __forceinline__ int quotient(int a, int b, int &rest) {
+  int q = (int)((float)a * __frcp_rn((float)b));
+  rest = a - q * b;
+  if (rest < 0) { --q; rest += b; }
+  else if (rest >= b) { ++q; rest -= b; }
+  return q;
+}
 
 template <int TM, int BN, int GRP>
 __device__ __forceinline__ bool get_work_of_experts(const GemmParams &p, int i, int bid, int G, Work &w) {
-  const int tiles_n = ceil_div(p.Q, BN);
-  const long long t = (long long)bid + (long long)i * G;
-  if (i == 0) w.s = 0;
-  int tl, tiles_m;
+  const int tiles_n = ceil_div(p.Q, BN), E = p.experts;
+  const int t = bid + i * G;             // (the host sees to it that there are fewer than 2^24 tiles)
+  if (i == 0) w.s = w.first_tile = 0;
+  int tiles_m;
   if (GRP == GRP_ROWS) {
-    const int E = p.experts;
-    if (t >= (long long)p.seg_tiles[E] * tiles_n) return false;
-    while (t >= (long long)p.seg_tiles[w.s + 1] * tiles_n) ++w.s;
-    tl = (int)(t - (long long)p.seg_tiles[w.s] * tiles_n);
+    if (i == 0) w.next_tile = p.seg_tiles[1] * tiles_n;
+    while (t >= w.next_tile) {
+      if (++w.s == E) return false;
+      w.first_tile = w.next_tile;
+      w.next_tile = p.seg_tiles[w.s + 1] * tiles_n;
+    }
     tiles_m = p.seg_tiles[w.s + 1] - p.seg_tiles[w.s];
   } else {
     tiles_m = ceil_div(p.P, TM);
-    const long long each = (long long)tiles_m * tiles_n;
-    if (t >= each * p.experts) return false;
-    w.s = (int)(t / each);
-    tl = (int)(t - w.s * each);
+    if (i == 0) w.next_tile = tiles_m * tiles_n;
+    while (t >= w.next_tile) {
+      if (++w.s == E) return false;
+      w.first_tile = w.next_tile;
+      w.next_tile += tiles_m * tiles_n;
+    }
   }
   constexpr int GM = GROUP_M * BM / TM;
-  const int group = GM * tiles_n;
-  const int g = tl / group;
-  const int first_m = g * GM;
-  const int gm = min(GM, tiles_m - first_m);
-  const int tm = first_m + (tl - g * group) % gm;
-  const int tn = (tl - g * group) / gm;
+  const int tl = t - w.first_tile;
+  int tm = 0, tn, in_group = tl;
+  int gm = tiles_m;
+  if (tiles_m > GM) {
+    const int g = quotient(tl, GM * tiles_n, in_group);
+    tm = g * GM;
+    gm = min(GM, tiles_m - tm);
+  }
+  int m;
+  tn = quotient(in_group, gm, m);
+  tm += m;
   const int off = p.seg_offsets[w.s], end = p.seg_offsets[w.s + 1];
   w.s_count = 1;
   w.b_col = w.col0 = tn * BN;
@@ -587,12 +607,12 @@ __device__ __forceinline__ bool get_work_of_experts(const GemmParams &p, int i, 
     w.row_end = end;
     w.valid_end = off + p.seg_counts[w.s];
     w.k0 = 0;
-    w.kblocks = ceil_div(p.R, p.bk);
+    w.kblocks = (p.R + 63) >> 6;
   } else {
     w.a_row = w.row0 = tm * TM;
     w.row_end = w.valid_end = p.P;
     w.k0 = end > off ? off : p.R;
-    w.kblocks = max(1, (end - off) / p.bk);
+    w.kblocks = max(1, (end - off) >> 6);
   }
   return true;
 }
@@ -812,7 +832,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
 
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
-  const int unit = (SL::UNIT > 1 && p.round_kblocks > 1) ? SL::UNIT : 1;   // k-blocks per barrier round
+  const int unit = GRP != GRP_NONE ? SL::UNIT : (SL::UNIT > 1 && p.round_kblocks > 1) ? SL::UNIT : 1;   // k-blocks per barrier round
   const int groups = SL::STAGES / unit;                                     // rounds in the ring
 
   // Programmatic dependent launch: the next kernel on the stream may be scheduled as soon as this
@@ -865,7 +885,79 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
   // lock step (warp 0 arms the stage's barrier and loads A, warp 3 loads B) so that two threads issue
   // them in parallel.  Otherwise warp 0 does it all (measured: the split costs 1-2 % there).
   constexpr bool SPLIT_PRODUCER = A_MN && B_MN;
-  if (warp == 0 || (SPLIT_PRODUCER && warp == 3)) {
+  if (GRP != GRP_NONE && (warp == 0 || (SPLIT_PRODUCER && warp == 3))) {
+    // ------------------------------------------------------------------ TMA producer(s) of the experts' products
+    // The tiles of these are often short (few rows to an expert, few k-blocks to its gradient), and the thread that
+    // issues the copies then sets the pace: it runs alone, and what it does per k-block is the copies.
+    if (lane == 0) {
+      const bool load_a = (warp == 0), load_b = !SPLIT_PRODUCER || warp == 3;
+      constexpr int UNIT = SL::UNIT, ROUNDS = SL::STAGES / SL::UNIT;
+      constexpr uint32_t TX = SL::STAGE_BYTES * (CTA2 ? 2u : 1u);
+      int grp = 0;
+      uint32_t phase = 0, armed = 0, armed_phase = 0;
+      bool ok = true;
+      Work w;
+      for (int i = 0; ok && next_work<TM, BN, GRP>(p, i, bid, G, w); ++i) {
+        const int a_row = w.a_row + (int)rank * BM, b_col = w.b_col + (CTA2 ? (int)rank * SL::GB_ROWS : 0);
+        const int b_sc = GRP == GRP_ROWS ? w.s : 0;
+        int kc = w.k0;
+        for (int kb = 0; kb < w.kblocks; kb += UNIT) {
+          const int n_sub = min(UNIT, w.kblocks - kb);
+          const uint32_t fb = full_bar(grp);
+          ok = mbar_wait(empty_bar(grp), phase ^ 1u, abort_flag, p.status, STATUS_TIMEOUT_PRODUCER);
+          if (!ok) break;
+          if (load_a && (!CTA2 || rank == 0)) mbar_expect_tx(fb, (uint32_t)n_sub * TX);
+          armed |= 1u << grp;
+          armed_phase = (armed_phase & ~(1u << grp)) | (phase << grp);
+          uint32_t sa = smem_base + (uint32_t)(grp * UNIT) * SL::STAGE_BYTES;
+#pragma unroll
+          for (int sub = 0; sub < UNIT; ++sub) {
+            if (sub < n_sub) {
+              auto tma_load = [&](uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2) {
+                if (CTA2) tma_load_3d_pair(dst, map, fb, c0, c1, c2);
+                else tma_load_3d(dst, map, fb, c0, c1, c2);
+              };
+              if (load_a) {
+                if (A_MN) {
+#pragma unroll
+                  for (int j = 0; j < BM / CW; ++j) tma_load(sa + j * (BKE * 128), &p.a_main, a_row + j * CW, kc, 0);
+                } else {
+                  tma_load(sa, &p.a_main, kc, a_row, 0);
+                }
+              }
+              if (load_b) {
+                const uint32_t sb = sa + SL::A_BYTES;
+                if (B_MN) {
+#pragma unroll
+                  for (int j = 0; j < (BNL + CW - 1) / CW; ++j) {
+                    constexpr int CPG = (SL::GB_ROWS + CW - 1) / CW;
+                    tma_load(sb + j * (BKE * 128), &p.b_main, b_col + (j / CPG) * 256 + (j % CPG) * CW, kc, b_sc);
+                  }
+                } else {
+#pragma unroll
+                  for (int g = 0; g < SL::NG; ++g) tma_load(sb + g * (SL::GB_ROWS * 128), &p.b_main, kc, b_col + g * 256, b_sc);
+                }
+              }
+              kc += BKE;
+              sa += SL::STAGE_BYTES;
+            }
+          }
+          if (++grp == ROUNDS) { grp = 0; phase ^= 1u; }
+        }
+      }
+      if (!ok && rank == 0 && load_a) {
+        // Unwinding: let the copies already issued land before the CTA's shared memory goes away.
+        for (int st = 0; st < ROUNDS; ++st) {
+          if (!((armed >> st) & 1u)) continue;
+          const unsigned long long t0 = globaltimer_ns();
+          while (!mbar_try_wait(full_bar(st), (armed_phase >> st) & 1u)) {
+            if (globaltimer_ns() - t0 > 2000000ull) break;   // 2 ms
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else if (GRP == GRP_NONE && (warp == 0 || (SPLIT_PRODUCER && warp == 3))) {
     // ------------------------------------------------------------------ TMA producer(s)
     const bool load_a = (warp == 0);
     const bool load_b = SPLIT_PRODUCER ? (warp == 3) : true;
@@ -884,10 +976,10 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
       for (int sl = 0; sl < w.s_count && ok; ++sl) {
       const int ss = w.s + sl;               // the slice whose operand boxes are loaded now
       const bool tail = (ss == p.k_total - 1);
-      const CUtensorMap *amap = (a_sliced && !tail) || GRP != GRP_NONE ? &p.a_main : &p.a_tail;
-      const CUtensorMap *bmap = (b_sliced && !tail) || GRP != GRP_NONE ? &p.b_main : &p.b_tail;
+      const CUtensorMap *amap = (a_sliced && !tail) ? &p.a_main : &p.a_tail;
+      const CUtensorMap *bmap = (b_sliced && !tail) ? &p.b_main : &p.b_tail;
       const int a_sc = (a_sliced && !tail) ? ss * p.a_sc_mul : 0;
-      const int b_sc = GRP == GRP_ROWS ? w.s : (b_sliced && !tail) ? ss * p.b_sc_mul : 0;
+      const int b_sc = (b_sliced && !tail) ? ss * p.b_sc_mul : 0;
       const int nkb = (p.mode == MODE_RED) ? ceil_div(min(p.L, p.R - ss * p.L), BKE) : w.kblocks;
       for (int kb = 0; kb < nkb; ++kb) {
         if (sub == 0) {
@@ -903,7 +995,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
           const uint32_t sa = smem_base + (uint32_t)(grp * unit + sub) * SL::STAGE_BYTES;
           const uint32_t sb = sa + SL::A_BYTES;
           const uint32_t fb = full_bar(grp);
-          const int kc = kb * BKE + (GRP == GRP_RED ? w.k0 : 0);
+          const int kc = kb * BKE;
           auto tma_load = [&](uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2) {
             if (CTA2) tma_load_3d_pair(dst, map, fb, c0, c1, c2);
             else tma_load_3d(dst, map, fb, c0, c1, c2);
@@ -1038,6 +1130,8 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
       w.row0 += (int)rank * BM;
       if (i == 0 && p.tma_epilogue && p.epi.gz && lane == 0)   // this CTA's first tile: while its main loop runs
         tma_prefetch_l2_3d(&p.gz_pf_map, w.b_col, w.a_row + quarter * 32, 0);
+      if (GRP == GRP_ROWS && p.epi.bias && lane < BN / 32 && w.col0 + lane * 32 < w.col_end)   // while the main loop runs
+        asm volatile("prefetch.global.L1 [%0];" ::"l"(p.epi.bias + (long long)w.s * p.Q + w.col0 + lane * 32) : "memory");
       const int buf = i % SL::NBUF;
       const uint32_t bphase = (uint32_t)(i / SL::NBUF) & 1u;
       ok = mbar_wait(tfull_bar(buf), bphase, abort_flag, p.status, STATUS_TIMEOUT_EPILOGUE);
