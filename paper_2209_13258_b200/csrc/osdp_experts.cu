@@ -15,17 +15,17 @@ namespace osdp {
 namespace {
 
 // ------------------------------------------------------------------------------------------------
-// G = dY (.) act'(Z) and the sums of G's columns for each expert, in one pass (bound by memory).  A block takes 64 columns of
-// 128 of an expert's rows; the blocks' sums are added in a fixed order by a second kernel.  The sums are of the unrounded G.
+// G = dY (.) act'(Z) and the sums of G's columns for each expert, in one pass (bound by memory).  A block takes 256 columns
+// of 64 rows, which are one expert's; the blocks' sums are added in a fixed order by a second kernel.  The sums are of the unrounded G.
 // Rows between two experts become zero, whatever dY and Z hold there.
 struct GradArgs {
   const __nv_bfloat16 *dy, *z;
   __nv_bfloat16 *g;             // null: column sums of dY alone
   const int32_t *plan;
-  float *partial;               // [tiles of 128 rows][N], or null
+  float *partial;               // [parts of 64 rows][N], or null
   int E, N, act;
 };
-constexpr int GRAD_ROWS = 128;
+constexpr int GRAD_ROWS = OSDP_EXPERT_ROWS, GRAD_COLS = 256;
 
 // act'(x) of the tanh form: 0.5 (1 + tanh u) = h = 1 / (1 + exp(-2 u)), and act' = h + 2 x h (1 - h) u'.  The special-function unit's 2^-22
 // (tanh.approx has 2^-11, too coarse for sums that are kept in fp32); two elements in an instruction.
@@ -46,90 +46,84 @@ __device__ __forceinline__ float gelu_erf_grad(float x) {
   return fmaf(x, 0.3989422804014327f * __expf(-0.5f * x * x), 0.5f * erfcf(-0.7071067811865476f * x));
 }
 
-__device__ __forceinline__ int expert_of_tile(const int32_t *first, int E, int tile) {   // first[e] <= tile < first[e + 1]
-  int lo = 0, hi = E - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (first[mid] <= tile) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
-}
-
-__global__ void __launch_bounds__(256, 4) expert_grad_kernel(const __grid_constant__ GradArgs a) {
-  __shared__ float red[32][64 + 1];
+__global__ void __launch_bounds__(256, 2) expert_grad_kernel(const __grid_constant__ GradArgs a) {
+  __shared__ float red[8][GRAD_COLS];
   pdl_launch_dependents();
-  const int cols = (a.N + 63) / 64;
-  const int tile = (int)(blockIdx.x / cols), col = (int)(blockIdx.x % cols) * 64 + (threadIdx.x & 7) * 8, ty = threadIdx.x >> 3;
+  const int cols = (a.N + GRAD_COLS - 1) / GRAD_COLS, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int part = (int)(blockIdx.x / cols), c0 = (int)(blockIdx.x % cols) * GRAD_COLS, col = c0 + lane * 8;
   pdl_wait();
-  const int32_t *tiles = a.plan + plan_tiles128(a.E);
-  if (tile >= tiles[a.E]) return;
-  const int e = expert_of_tile(tiles, a.E, tile);
-  const int off = a.plan[PLAN_OFFSETS + e], first = (tile - tiles[e]) * GRAD_ROWS;
-  const int count = a.plan[plan_counts(a.E) + e] - first, padded = a.plan[PLAN_OFFSETS + e + 1] - off - first;
+  // Rows warp, warp + 8, ... of the block's 64.  They are there whoever's they are, so that the plan is looked up while they
+  // are on their way.
+  constexpr int EACH = GRAD_ROWS / 8;
+  const long long at = ((long long)part * GRAD_ROWS + warp) * a.N + col;
+  uint4 d[EACH], z[EACH];
+  if (col < a.N) {
+#pragma unroll
+    for (int q = 0; q < EACH; ++q) {
+      d[q] = load16(a.dy + at + (long long)q * 8 * a.N);
+      if (a.g) z[q] = load16(a.z + at + (long long)q * 8 * a.N);
+    }
+  }
+  // the expert whose rows these are: offsets[e] <= row < offsets[e + 1]
+  const int32_t *offsets = a.plan + PLAN_OFFSETS;
+  int e = -1;
+  for (int i = lane; i - lane < a.E; i += 32) e += __popc(__ballot_sync(0xFFFFFFFFu, i < a.E && offsets[i] <= part * GRAD_ROWS));
+  if (part * GRAD_ROWS >= offsets[a.E]) return;
+  const int count = a.plan[plan_counts(a.E) + e] - (part * GRAD_ROWS - offsets[e]) - warp;
   f2 acc[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) acc[j] = both(0.f);
   if (col < a.N) {
-    constexpr int EACH = GRAD_ROWS / 32;
-    const long long at = ((long long)off + first) * a.N + col;
-    uint4 d[EACH], z[EACH];
 #pragma unroll
     for (int q = 0; q < EACH; ++q) {
-      const int r = ty + 32 * q;
-      d[q] = r < count ? load16(a.dy + at + (long long)r * a.N) : make_uint4(0u, 0u, 0u, 0u);
-      if (a.g) z[q] = r < count ? load16(a.z + at + (long long)r * a.N) : make_uint4(0u, 0u, 0u, 0u);
-    }
-#pragma unroll
-    for (int q = 0; q < EACH; ++q) {
-      const int r = ty + 32 * q;
       f2 f[4];
-      widen4(d[q], f);
-      if (a.g) {
-        f2 x[4];
-        widen4(z[q], x);
-        if (a.act == ACT_GELU_TANH) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) f[j] = mul2(f[j], gelu_tanh_grad2(x[j]));
-        } else {
+      for (int j = 0; j < 4; ++j) f[j] = both(0.f);
+      if (8 * q < count) {
+        widen4(d[q], f);
+        if (a.g) {
+          f2 x[4];
+          widen4(z[q], x);
+          if (a.act == ACT_GELU_TANH) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 v = split2(x[j]);
-            f[j] = mul2(f[j], pack2(gelu_erf_grad(v.x), gelu_erf_grad(v.y)));
+            for (int j = 0; j < 4; ++j) f[j] = mul2(f[j], gelu_tanh_grad2(x[j]));
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float2 v = split2(x[j]);
+              f[j] = mul2(f[j], pack2(gelu_erf_grad(v.x), gelu_erf_grad(v.y)));
+            }
           }
         }
-        if (r < min(padded, GRAD_ROWS)) *reinterpret_cast<uint4 *>(a.g + at + (long long)r * a.N) = narrow4(f);
       }
+      if (a.g) *reinterpret_cast<uint4 *>(a.g + at + (long long)q * 8 * a.N) = narrow4(f);
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[j] = add2(acc[j], f[j]);
     }
   }
   if (!a.partial) return;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float2 v = split2(acc[j]);
-    red[ty][(threadIdx.x & 7) * 8 + 2 * j] = v.x;
-    red[ty][(threadIdx.x & 7) * 8 + 2 * j + 1] = v.y;
-  }
+  for (int j = 0; j < 4; ++j) *reinterpret_cast<float2 *>(&red[warp][lane * 8 + 2 * j]) = split2(acc[j]);
   __syncthreads();
-  const int c = (int)(blockIdx.x % cols) * 64 + threadIdx.x;
-  if (threadIdx.x < 64 && c < a.N) {
+  const int c = c0 + threadIdx.x;
+  if (c < a.N) {
     float s = 0.f;
 #pragma unroll
-    for (int t = 0; t < 32; ++t) s += red[t][threadIdx.x];
-    a.partial[(long long)tile * a.N + c] = s;
+    for (int w = 0; w < 8; ++w) s += red[w][threadIdx.x];
+    a.partial[(long long)part * a.N + c] = s;
   }
 }
 
-// db[e, c]: the tiles' sums of expert e in order.
+// db[e, c]: the parts' sums of expert e in order.
 __global__ void __launch_bounds__(128) expert_bias_kernel(const float *partial, const int32_t *plan, int E, int N, float *db) {
   pdl_launch_dependents();
   const int e = (int)blockIdx.y, c = (int)(blockIdx.x * blockDim.x + threadIdx.x);
   pdl_wait();
   if (c >= N) return;
-  const int32_t *tiles = plan + plan_tiles128(E);
+  const int first = plan[PLAN_OFFSETS + e] / GRAD_ROWS, last = plan[PLAN_OFFSETS + e + 1] / GRAD_ROWS;
   float s = 0.f;
-  for (int t = tiles[e]; t < tiles[e + 1]; ++t) s += partial[(long long)t * N + c];
+#pragma unroll 8
+  for (int t = first; t < last; ++t) s += partial[(long long)t * N + c];
   db[(long long)e * N + c] = s;
 }
 
@@ -323,15 +317,15 @@ int expert_workspace(int64_t T, int top_k, int E, int64_t N, int64_t K, int act,
   if (N <= 0 || K <= 0 || N > ((int64_t)1 << 24) || K > ((int64_t)1 << 24)) return OSDP_ERR_BAD_SHAPE;
   if ((N & 7) || (K & 7)) return OSDP_ERR_ALIGNMENT;
   if (act != OSDP_ACT_NONE && act != OSDP_ACT_GELU_TANH && act != OSDP_ACT_GELU_ERF) return OSDP_ERR_UNSUPPORTED;
-  const int64_t n = T * top_k, used = n < E ? n : E, R = expert_rows(T, top_k, E);
+  const int64_t R = expert_rows(T, top_k, E);
   if (R >= ((int64_t)1 << 31) - 256) return OSDP_ERR_BAD_SHAPE;
   auto up = [](size_t v) { return (v + 255) / 256 * 256; };
   w->partial = w->g = w->total = 256;
   if (op == OSDP_OP_LINEAR_FWD) return OSDP_OK;
   if (op != OSDP_OP_LINEAR_BWD) return OSDP_ERR_UNSUPPORTED;
-  const int64_t blocks = (n / GRAD_ROWS + used) * cdiv(N, 64);
+  const int64_t blocks = (R / GRAD_ROWS) * cdiv(N, GRAD_COLS);
   if (blocks >= ((int64_t)1 << 31)) return OSDP_ERR_BAD_SHAPE;
-  w->g = w->partial + up((size_t)(n / GRAD_ROWS + used) * N * 4);
+  w->g = w->partial + up((size_t)(R / GRAD_ROWS) * N * 4);
   w->total = w->g + (act == OSDP_ACT_NONE ? 0 : up((size_t)R * N * 2));
   return OSDP_OK;
 }
@@ -399,7 +393,7 @@ extern "C" int osdp_expert_linear_bwd(const void *dy, const void *rows, const in
   rc = check_workspace(ws, ws_bytes, w);
   if (rc) return rc;
   cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-  const int64_t R = expert_rows(T, top_k, E), n = T * top_k, used = n < E ? n : E;
+  const int64_t R = expert_rows(T, top_k, E);
   void *dw = nullptr;
   const size_t dw_bytes = (size_t)E * N * K * (dw_dtype == OSDP_DTYPE_FP32 ? 4 : 2);
   if (dw_flat) dw = static_cast<char *>(dw_flat) + dw_offset * (dw_dtype == OSDP_DTYPE_FP32 ? 4 : 2);
@@ -416,7 +410,7 @@ extern "C" int osdp_expert_linear_bwd(const void *dy, const void *rows, const in
     __nv_bfloat16 *stage = act != OSDP_ACT_NONE ? reinterpret_cast<__nv_bfloat16 *>(wsb + w.g) : nullptr;
     const GradArgs a{static_cast<const __nv_bfloat16 *>(dy), static_cast<const __nv_bfloat16 *>(z_saved), stage, plan, dbias ? partial : nullptr, E,
                      (int)N, act};
-    rc = launch_overlapped(expert_grad_kernel, dim3((unsigned)((n / GRAD_ROWS + used) * cdiv(N, 64))), dim3(256), 0, 1, stream, a);
+    rc = launch_overlapped(expert_grad_kernel, dim3((unsigned)((R / GRAD_ROWS) * cdiv(N, GRAD_COLS))), dim3(256), 0, 1, stream, a);
     if (rc) return rc;
     if (stage) g = stage;
   }

@@ -884,7 +884,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
   // With both operands MN-major a stage takes four to six copies; two warps then walk the ring in
   // lock step (warp 0 arms the stage's barrier and loads A, warp 3 loads B) so that two threads issue
   // them in parallel.  Otherwise warp 0 does it all (measured: the split costs 1-2 % there).
-  constexpr bool SPLIT_PRODUCER = A_MN && B_MN;
+  constexpr bool SPLIT_PRODUCER = B_MN && (A_MN || GRP != GRP_NONE);
   if (GRP != GRP_NONE && (warp == 0 || (SPLIT_PRODUCER && warp == 3))) {
     // ------------------------------------------------------------------ TMA producer(s) of the experts' products
     // The tiles of these are often short (few rows to an expert, few k-blocks to its gradient), and the thread that
