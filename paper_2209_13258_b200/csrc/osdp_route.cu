@@ -12,6 +12,7 @@ namespace osdp {
 namespace {
 
 constexpr uint32_t ALL = 0xFFFFFFFFu;
+constexpr int ROUTE_WARPS = 8;
 
 // ------------------------------------------------------------------------------------------------
 // Routing.  One warp per token; lane l holds experts l, l + 32, ... in registers.
@@ -19,8 +20,9 @@ constexpr uint32_t ALL = 0xFFFFFFFFu;
 // The choice has to be the one of exact arithmetic: another expert is another result.  It is made twice at most.  First in
 // fp32 with approximate scores: a key is the score's order-preserving bits with the place in the lane's registers in the lowest
 // ones, a lane sorts its keys once, and an expert is found by one maximum over the lanes' first keys.  Where two scores
-// that decide are closer than all these roundings (and are not the same logit with the same bias), the row is done again
-// in fp64; that is one row in some hundred.
+// that decide are closer than all these roundings (and are not the same logit with the same bias), the scores in question are
+// taken again in fp64; that is one row in some hundred, and it is kept short (a whole row in fp64 made the last of
+// 16384 rows of 256 experts 10 us late).
 struct RouteArgs {
   const void *logits;
   long long ld, T;
@@ -29,6 +31,9 @@ struct RouteArgs {
   float scale;
   int32_t *idx;
   float *weights;
+  // of the groups: experts of one, 2^20 / that rounded up (a quotient e / size for e < 1024), log2 of the lanes that look at one
+  int size, lanes_log2;
+  uint32_t magic;
 };
 
 __device__ __forceinline__ float widen(float v) { return v; }
@@ -36,28 +41,11 @@ __device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162floa
 
 // Order-preserving keys; 0 is below every key.  NaN counts as minus infinity, -0 as 0.
 __device__ __forceinline__ uint32_t key_of(float x) {
-  const uint32_t u = __float_as_uint(x + 0.0f);
-  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0x007FFFFFu;
-  return (u >> 31) ? ~u : u | 0x80000000u;
-}
-__device__ __forceinline__ unsigned long long key_of(double x) {
-  const unsigned long long u = (unsigned long long)__double_as_longlong(x + 0.0);
-  if ((u & 0x7FFFFFFFFFFFFFFFull) > 0x7FF0000000000000ull) return 0x000FFFFFFFFFFFFFull;
-  return (u >> 63) ? ~u : u | 0x8000000000000000ull;
-}
-__device__ __forceinline__ unsigned long long warp_top(unsigned long long k) {
-  const uint32_t hi = __reduce_max_sync(ALL, (uint32_t)(k >> 32));
-  const uint32_t lo = __reduce_max_sync(ALL, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
-  return ((unsigned long long)hi << 32) | lo;
+  const int32_t u = __float_as_int(fmaxf(x, -INFINITY) + 0.0f);
+  return (uint32_t)u ^ ((uint32_t)(u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float((key >> 31) ? key & 0x7FFFFFFFu : ~key); }
 
-template <typename R>
-__device__ __forceinline__ R sum_of(R v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(ALL, v, o);
-  return v;
-}
 template <int V>
 __device__ __forceinline__ float largest(const float (&l)[V]) {   // of the row; lanes past its end hold minus infinity
   uint32_t top = 0;
@@ -66,19 +54,16 @@ __device__ __forceinline__ float largest(const float (&l)[V]) {   // of the row;
   return value_of(__reduce_max_sync(ALL, top));
 }
 
-// Which groups may be chosen from: bit g * per of the result, `per` lanes for each group.  c: the row's scores in `room`, NaN as
-// minus infinity; border: the last group that is taken and the first that is not.
-template <typename R>
-__device__ __forceinline__ uint32_t choose_groups(const RouteArgs &a, const R *room, int lane, int &per, R &sum, bool &in) {
+// Which groups may be chosen from: bit g << lanes_log2 of the result.  score_of: an expert's score, NaN as minus infinity.
+template <typename R, typename F>
+__device__ __forceinline__ uint32_t choose_groups(const RouteArgs &a, F score_of, int lane, R &sum, bool &in) {
   const R low = -(R)INFINITY;
-  const int size = a.E / a.groups;
-  per = 32;
-  while (per * a.groups > 32) per >>= 1;
-  const int g = lane / per;
+  const int per = 1 << a.lanes_log2, g = lane >> a.lanes_log2, sub = lane & (per - 1);
   R first = low, second = low;
   if (g < a.groups) {
-    for (int e = g * size + lane % per; e < (g + 1) * size; e += per) {
-      const R x = room[e];
+#pragma unroll(sizeof(R) == 4 ? 4 : 1)
+    for (int e = sub; e < a.size; e += per) {
+      const R x = score_of(g * a.size + e);
       second = max(second, min(first, x));
       first = max(first, x);
     }
@@ -88,15 +73,15 @@ __device__ __forceinline__ uint32_t choose_groups(const RouteArgs &a, const R *r
     second = max(max(second, s), min(first, f));
     first = max(first, f);
   }
-  sum = a.take > 1 && size > 1 ? first + second : first;
+  sum = a.take > 1 && a.size > 1 ? first + second : first;
   if (sum != sum) sum = low;
   int rank = 0;
   for (int h = 0; h < a.groups; ++h) {
-    const R other = __shfl_sync(ALL, sum, h * per);
+    const R other = __shfl_sync(ALL, sum, h << a.lanes_log2);
     rank += other > sum || (other == sum && h < g) ? 1 : 0;
   }
   in = g < a.groups && rank < a.top_groups;
-  return __ballot_sync(ALL, in && lane % per == 0);
+  return __ballot_sync(ALL, in && sub == 0);
 }
 
 constexpr float HALF_ULP = 5.9604645e-8f;
@@ -106,77 +91,165 @@ __device__ __forceinline__ float fast_exp(float x) {   // 2^-22 and the rounding
   return e;
 }
 
-// Chooses the row's experts by their approximate scores: lane j < k leaves with the j-th in `mine`, its logit in `lj`.
-// Returns false where two scores are too close to say.  `room` [E]: this warp's shared memory.
+// The row's scores in fp64, one at a time.  Compact loops: they are cold when they are needed.
+template <typename L>
+struct Exact {
+  const RouteArgs &a;
+  const L *row;
+  double high, total;
+
+  __device__ Exact(const RouteArgs &args, const L *r, int lane) : a(args), row(r), high(0.0), total(1.0) {
+    if (a.score != OSDP_SCORE_SOFTMAX || !(a.bias || a.top_groups < a.groups)) return;
+    uint32_t top = 0;
+    for (int e = lane; e < a.E; e += 32) top = max(top, key_of(widen(row[e])));
+    high = (double)value_of(__reduce_max_sync(ALL, top));
+    total = 0.0;
+#pragma unroll 1
+    for (int e = lane; e < a.E; e += 32) {
+      const double l = (double)widen(row[e]);
+      total += l == -(double)INFINITY ? 0.0 : exp(l - high);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(ALL, total, o);
+  }
+  __device__ double score(int e) const {
+    const double l = (double)widen(row[e]);
+    double s;
+    if (a.score == OSDP_SCORE_SOFTMAX) s = l == -(double)INFINITY && total == total ? 0.0 : exp(l - high) / total;
+    else s = 1.0 / (1.0 + exp(-l));
+    if (a.bias) s += (double)a.bias[e];
+    return s == s ? s : -(double)INFINITY;
+  }
+  // what experts are chosen by
+  __device__ double rank_by(int e) const {
+    if (a.bias) return score(e);
+    const double l = (double)widen(row[e]);
+    return l == l ? l : -(double)INFINITY;
+  }
+};
+
+template <typename L>
+__device__ __noinline__ uint32_t exact_groups(const RouteArgs &a, const L *row, int lane) {
+  const Exact<L> exact(a, row, lane);
+  double sum;
+  bool in;
+  return choose_groups<double>(a, [&](int e) { return exact.score(e); }, lane, sum, in);
+}
+
+// Lanes 0 .. m hold candidates, behind which nothing can be chosen: the k best of them, in order.
+template <typename L>
+__device__ __noinline__ void exact_order(const RouteArgs &a, const L *row, int lane, int m, int &mine) {
+  const Exact<L> exact(a, row, lane);
+  const double key = lane <= m ? exact.rank_by(mine) : 0.0;
+  int rank = 0, from = 0;
+#pragma unroll 1
+  for (int i = 0; i <= m; ++i) {
+    const double other = __shfl_sync(ALL, key, i);
+    const int e = __shfl_sync(ALL, mine, i);
+    rank += other > key || (other == key && e < mine) ? 1 : 0;
+  }
+#pragma unroll 1
+  for (int j = 0; j < a.k; ++j) {
+    const int owner = __ffs(__ballot_sync(ALL, lane <= m && rank == j)) - 1;
+    if (lane == j) from = owner;
+  }
+  mine = __shfl_sync(ALL, mine, from);
+}
+
+// Everything in question: the experts of the groups in `taken`, one after the other.
+template <typename L>
+__device__ __noinline__ void exact_all(const RouteArgs &a, const L *row, uint32_t taken, int lane, int &mine) {
+  const Exact<L> exact(a, row, lane);
+  double last = (double)INFINITY;
+  int last_e = -1;
+#pragma unroll 1
+  for (int j = 0; j < a.k; ++j) {     // the best of those behind the last one
+    double best = -(double)INFINITY;
+    int best_e = 1 << 20;
+#pragma unroll 1
+    for (int e = lane; e < a.E; e += 32) {
+      if (!((taken >> (((uint32_t)e * a.magic >> 20) << a.lanes_log2)) & 1u)) continue;
+      const double x = exact.rank_by(e);
+      const bool behind = j == 0 || x < last || (x == last && e > last_e);
+      if (behind && (x > best || (x == best && e < best_e))) {
+        best = x;
+        best_e = e;
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const double x = __shfl_xor_sync(ALL, best, o);
+      const int e = __shfl_xor_sync(ALL, best_e, o);
+      if (x > best || (x == best && e < best_e)) {
+        best = x;
+        best_e = e;
+      }
+    }
+    last = best;
+    last_e = best_e;
+    if (lane == j) mine = best_e;
+  }
+}
+
+// Chooses the row's experts: lane j < k leaves with the j-th in `mine`, its logit in `lj`.
+// `list` [32 V]: this warp's shared memory.
 template <int V, typename L>
-__device__ __forceinline__ bool choose_fast(const RouteArgs &a, const L *row, const float (&l)[V], float *room, int lane, int &mine, float &lj) {
+__device__ __forceinline__ void choose(const RouteArgs &a, const L *row, const float (&l)[V], uint32_t *list, int lane, int &mine, float &lj) {
   const bool grouped = a.top_groups < a.groups, soft = a.score == OSDP_SCORE_SOFTMAX;
-  uint32_t key[V];
+  uint32_t key[V], taken = ALL;
   float c[V];
-  float high = 0.f, inv = 1.f;
-  bool sure = true;
+  float high = 0.f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) c[v] = l[v];                 // without a bias the scores are in the order of the logits
   if (a.bias || grouped) {
+    float s[V], far = 0.f;
     if (soft) {
       high = largest(l);
       float total = 0.f;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        c[v] = l[v] == -INFINITY ? 0.f : fast_exp(l[v] - high);
-        total += c[v];
+        s[v] = l[v] == -INFINITY ? 0.f : fast_exp(l[v] - high);
+        total += s[v];
       }
       total = warp_sum(total);
-      inv = total > 0.f ? fast_rcp(total) : total;       // (a row of minus infinities: all scores are zero)
+      const float inv = total > 0.f ? fast_rcp(total) : total;       // (a row of minus infinities: all scores are zero)
 #pragma unroll
-      for (int v = 0; v < V; ++v) c[v] *= inv;
+      for (int v = 0; v < V; ++v) s[v] *= inv;
     } else {
 #pragma unroll
-      for (int v = 0; v < V; ++v) c[v] = fast_rcp(1.0f + fast_exp(-l[v]));
+      for (int v = 0; v < V; ++v) s[v] = fast_rcp(1.0f + fast_exp(-l[v]));
     }
-    float far = 0.f;
     if (a.bias) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const float b = v * 32 + lane < a.E ? a.bias[v * 32 + lane] : 0.f;
-        c[v] += b;
+        c[v] = s[v] += b;
         far = fmaxf(far, fabsf(b));
       }
     }
     if (grouped) {
 #pragma unroll
       for (int v = 0; v < V; ++v)
-        if (v * 32 + lane < a.E) room[v * 32 + lane] = fmaxf(c[v], -INFINITY);
+        list[v * 32 + lane] = __float_as_uint(fmaxf(s[v], -INFINITY));
       __syncwarp();
-      int per;
       float sum;
       bool in;
-      const uint32_t taken = choose_groups(a, room, lane, per, sum, in);
-      // Two scores each.  128 half units: as much as a score's exponent can cost before nothing is left of the score.
+      taken = choose_groups<float>(a, [&](int e) { return __uint_as_float(list[e]); }, lane, sum, in);
       const float last = value_of(~__reduce_max_sync(ALL, in ? ~key_of(sum) : 0u));
-      const float next = value_of(__reduce_max_sync(ALL, lane / per < a.groups && !in ? key_of(sum) : 0x007FFFFFu));
+      const float next = value_of(__reduce_max_sync(ALL, (lane >> a.lanes_log2) < a.groups && !in ? key_of(sum) : 0x007FFFFFu));
       far = __uint_as_float(__reduce_max_sync(ALL, __float_as_uint(far)));
-      if (last - next <= 2.0f * 128.0f * HALF_ULP * (fabsf(last) + 2.0f * far)) sure = false;
-      const int size = a.E / a.groups;
-      const uint32_t magic = (1048576u + size - 1) / size;      // e / size for e < 1024
-#pragma unroll
-      for (int v = 0; v < V; ++v) key[v] = (taken >> (((uint32_t)(v * 32 + lane) * magic >> 20) * per)) & 1u;
+      // Two sums of two scores.  A sigmoid is off by 4.4 half units of 1 at most, and the sums by theirs and the bias's; a softmax by
+      // 128 of its own size (its exponent counts 1.5 times, and beyond 80 nothing is left of it).
+      const float off = soft ? 256.0f * (fabsf(last) + 2.0f * far) : 24.0f + 4.0f * far + 2.0f * fabsf(last);
+      if (last - next <= HALF_ULP * off) taken = exact_groups(a, row, lane);
       __syncwarp();
-    } else {
-#pragma unroll
-      for (int v = 0; v < V; ++v) key[v] = 1u;
-    }
-    if (!a.bias) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) c[v] = l[v];
-    }
-  } else {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      key[v] = 1u;
-      c[v] = l[v];                      // without a bias the scores are in the order of the logits
     }
   }
 #pragma unroll
-  for (int v = 0; v < V; ++v) key[v] = key[v] && v * 32 + lane < a.E ? (key_of(c[v]) & ~(uint32_t)(V - 1)) | (uint32_t)(V - 1 - v) : 0u;
+  for (int v = 0; v < V; ++v) {
+    const bool on = v * 32 + lane < a.E && (!grouped || ((taken >> (((uint32_t)(v * 32 + lane) * a.magic >> 20) << a.lanes_log2)) & 1u));
+    key[v] = on ? (key_of(c[v]) & ~(uint32_t)(V - 1)) | (uint32_t)(V - 1 - v) : 0u;
+  }
   // descending (a bitonic network)
 #pragma unroll
   for (int n = 2; n <= V; n *= 2)
@@ -189,107 +262,63 @@ __device__ __forceinline__ bool choose_fast(const RouteArgs &a, const L *row, co
           key[v] = (v & n) == 0 ? hi : lo;
           key[v | o] = (v & n) == 0 ? lo : hi;
         }
-  // one more than are wanted, to see how far away it is
-  uint32_t got = 0;
-  for (int j = 0; j <= a.k; ++j) {
-    const uint32_t best = __reduce_max_sync(ALL, key[0]);
-    if (best == 0) break;             // (only behind the last one wanted: the groups have enough experts)
-    const int owner = __ffs(__ballot_sync(ALL, key[0] == best)) - 1;      // equal keys: the same register, the lower lane
-    if (lane == j) {
-      got = best;
-      mine = (V - 1 - (int)(best & (V - 1))) * 32 + owner;
-    }
-    if (lane == owner) {
+  // A lane's keys wait in shared memory but for the first.
 #pragma unroll
-      for (int v = 0; v + 1 < V; ++v) key[v] = key[v + 1];
-      key[V - 1] = 0;
-    }
-  }
-  float bj = 0.f, off = 0.f;
-  const float value = value_of(got & ~(uint32_t)(V - 1));
-  if (mine >= 0) {
-    lj = widen(row[mine]);
-    off = 2.0f * V * fabsf(value);                                          // the bits that the place took
-    if (a.bias) {
-      bj = a.bias[mine];
-      // the score: exponent (1.5 times its size), exponential and reciprocal 4 each, a softmax's total up to 37; and the sum with the bias
-      const float s = fabsf(value - bj);
-      off += fabsf(value) + fabsf(bj) + (soft ? s * (1.5f * (high - lj) + 46.0f) : s * ((1.0f - fminf(s, 1.0f) + 0.01f) * (1.5f * fabsf(lj) + 6.0f) + 6.0f));
-    }
-  }
-  const int after = __shfl_down_sync(ALL, mine, 1);
-  const float less = __shfl_down_sync(ALL, value, 1), less_off = __shfl_down_sync(ALL, off, 1), less_l = __shfl_down_sync(ALL, lj, 1),
-              less_b = __shfl_down_sync(ALL, bj, 1);
-  // as close as that: the same in exact arithmetic only if it is the same logit and the same bias
-  if (lane < a.k && after >= 0 && value - less <= HALF_ULP * (off + less_off) && (lj != less_l || bj != less_b)) sure = false;
-  return __all_sync(ALL, sure);
-}
-
-// The same in fp64, score by score.
-template <int V, typename L>
-__device__ __noinline__ void choose_exactly(const RouteArgs &a, const L *row, double *room, int lane, int &mine) {
-  unsigned long long key[V];
-  double c[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) c[v] = v * 32 + lane < a.E ? (double)widen(row[v * 32 + lane]) : -(double)INFINITY;
-#pragma unroll
-  for (int v = 0; v < V; ++v) key[v] = v * 32 + lane < a.E ? key_of(c[v]) : 0ull;
-  if (a.bias || a.top_groups < a.groups) {
-    if (a.score == OSDP_SCORE_SOFTMAX) {
-      unsigned long long top = 0;
-#pragma unroll
-      for (int v = 0; v < V; ++v) top = key[v] > top ? key[v] : top;
-      top = warp_top(top);
-      const double high = __longlong_as_double((long long)((top >> 63) ? top & 0x7FFFFFFFFFFFFFFFull : ~top));
-      double total = 0.0;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        c[v] = c[v] == -(double)INFINITY ? 0.0 : exp(c[v] - high);
-        total += c[v];
+  for (int v = 1; v < V; ++v) list[v * 32 + lane] = key[v];
+  uint32_t got = 0, head = key[0];
+  int next = lane + 32;
+  auto take = [&](int from, int to) {        // lane j gets the j-th
+    for (int j = from; j < to; ++j) {
+      const uint32_t best = __reduce_max_sync(ALL, head);
+      if (best == 0) break;             // (only behind the last one wanted: the groups have enough experts)
+      const int owner = __ffs(__ballot_sync(ALL, head == best)) - 1;      // equal keys: the same register, the lower lane
+      if (lane == j) {
+        got = best;
+        mine = owner + (V - 1 - (int)(best & (V - 1))) * 32;
       }
-      total = sum_of(total);
-#pragma unroll
-      for (int v = 0; v < V; ++v) c[v] = total == 0.0 ? 0.0 : c[v] / total;
-    } else {
-#pragma unroll
-      for (int v = 0; v < V; ++v) c[v] = 1.0 / (1.0 + exp(-c[v]));
+      if (lane == owner) {
+        head = next < V * 32 ? list[next] : 0u;
+        next += 32;
+      }
     }
-    if (a.bias) {
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (v * 32 + lane < a.E) {
-          c[v] += (double)a.bias[v * 32 + lane];
-          key[v] = key_of(c[v]);
-        }
+  };
+  // whether lane j's expert and the next lane's are too close to say: bits of lanes
+  auto close = [&](bool equal_too) {
+    float bj = 0.f, off = 0.f;
+    const float value = value_of(got & ~(uint32_t)(V - 1));
+    if (mine >= 0) {
+      lj = widen(row[mine]);
+      off = 2.0f * V * fabsf(value);                                          // the bits that the place took
+      if (a.bias) {
+        bj = a.bias[mine];
+        // the score (see above, here relative to itself) and its sum with the bias
+        const float s = fabsf(value - bj);
+        off += fabsf(value) + fabsf(bj) + (soft ? s * (1.5f * (high - lj) + 46.0f) : s * ((1.0f - fminf(s, 1.0f) + 0.01f) * (1.5f * fabsf(lj) + 6.0f) + 6.0f));
+      }
+    }
+    const int after = __shfl_down_sync(ALL, mine, 1);
+    const float less = __shfl_down_sync(ALL, value, 1), less_off = __shfl_down_sync(ALL, off, 1), less_l = __shfl_down_sync(ALL, lj, 1),
+                less_b = __shfl_down_sync(ALL, bj, 1);
+    // as close as that: the same in exact arithmetic only if it is the same logit and the same bias
+    return __ballot_sync(ALL, lane < 31 && mine >= 0 && after >= 0 && value - less <= HALF_ULP * (off + less_off) && (equal_too || lj != less_l || bj != less_b));
+  };
+  take(0, a.k + 1);     // one more than are wanted, to see how far away it is
+  if ((close(false) & ((1u << a.k) - 1u)) == 0) return;
+  // the candidates end at the first gap behind the last one wanted
+  for (int many = a.k + 1; many < 32;) {
+    const int more = min(many + 4, 32);
+    take(many, more);
+    many = more;
+    const uint32_t there = __ballot_sync(ALL, mine >= 0);
+    const uint32_t gaps = ~close(true) & ~((1u << (a.k - 1)) - 1u) & (there >> 1);      // (the last candidate's gap is not known yet)
+    if (gaps || __popc(there) < many) {
+      exact_order(a, row, lane, gaps ? __ffs(gaps) - 1 : __popc(there) - 1, mine);
+      if (lane < a.k) lj = widen(row[mine]);
+      return;
     }
   }
-  if (a.top_groups < a.groups) {
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (v * 32 + lane < a.E) room[v * 32 + lane] = c[v] == c[v] ? c[v] : -(double)INFINITY;
-    __syncwarp();
-    int per;
-    double sum;
-    bool in;
-    const uint32_t taken = choose_groups(a, room, lane, per, sum, in);
-    const int size = a.E / a.groups;
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (!((taken >> ((v * 32 + lane) / size * per)) & 1u)) key[v] = 0ull;
-  }
-  for (int j = 0; j < a.k; ++j) {
-    unsigned long long best = 0;
-#pragma unroll
-    for (int v = 0; v < V; ++v) best = key[v] > best ? key[v] : best;
-    best = warp_top(best);
-    int e = 1 << 20;
-#pragma unroll
-    for (int v = V - 1; v >= 0; --v) e = key[v] == best ? v * 32 + lane : e;
-    e = __reduce_min_sync(ALL, e);
-#pragma unroll
-    for (int v = 0; v < V; ++v) key[v] = v * 32 + lane == e ? 0ull : key[v];
-    if (lane == j) mine = e;
-  }
+  exact_all(a, row, taken, lane, mine);
+  if (lane < a.k) lj = widen(row[mine]);
 }
 
 // The weights' parts of the chosen experts, lanes 0 .. k - 1 (their logits in `l`): r_j = s_j / sum s, formed from the chosen
@@ -306,23 +335,19 @@ __device__ __forceinline__ float share_of(const RouteArgs &a, float l, bool on, 
 
 template <typename L, int V>
 __global__ void __launch_bounds__(256, V <= 8 ? 4 : 1) route_fwd_kernel(const __grid_constant__ RouteArgs a) {
-  extern __shared__ double rooms[];
+  __shared__ uint32_t lists[ROUTE_WARPS * 32 * V];
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31;
   const long long t = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   pdl_wait();
   if (t >= a.T) return;
-  double *room = rooms + (threadIdx.x >> 5) * a.E;
   const L *row = static_cast<const L *>(a.logits) + t * a.ld;
   float l[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) l[v] = v * 32 + lane < a.E ? widen(row[v * 32 + lane]) : -INFINITY;
   int mine = -1;
   float lj = -INFINITY;
-  if (!choose_fast<V, L>(a, row, l, reinterpret_cast<float *>(room), lane, mine, lj)) {
-    choose_exactly<V, L>(a, row, room, lane, mine);
-    if (lane < a.k) lj = widen(row[mine]);
-  }
+  choose<V, L>(a, row, l, lists + (threadIdx.x >> 5) * 32 * V, lane, mine, lj);
   const bool on = lane < a.k;
   float w;
   if (a.renorm) {
@@ -358,8 +383,6 @@ struct RouteBackArgs {
 
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
-
-constexpr int ROUTE_WARPS = 8;
 
 template <typename L>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_bwd_kernel(const __grid_constant__ RouteBackArgs b) {
@@ -761,14 +784,7 @@ int check_routing(int64_t T, int E, int top_k, int64_t ld, int dtype, int score,
 template <typename L>
 int launch_route(const RouteArgs &a, cudaStream_t stream) {
   const dim3 grid((unsigned)cdiv(a.T, ROUTE_WARPS)), block(32 * ROUTE_WARPS);
-  const size_t smem = a.groups > a.top_groups ? (size_t)ROUTE_WARPS * a.E * sizeof(double) : 0;   // at most 64 KB: below
-  auto go = [&](auto kernel) -> int {
-    if (smem > 48 * 1024) {
-      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ROUTE_WARPS * OSDP_MAX_EXPERTS * (int)sizeof(double));
-      if (e != cudaSuccess) return report_cuda(e);
-    }
-    return launch_overlapped(kernel, grid, block, smem, 1, stream, a);
-  };
+  auto go = [&](auto kernel) { return launch_overlapped(kernel, grid, block, 0, 1, stream, a); };
   if (a.E <= 32) return go(route_fwd_kernel<L, 1>);
   if (a.E <= 64) return go(route_fwd_kernel<L, 2>);
   if (a.E <= 128) return go(route_fwd_kernel<L, 4>);
@@ -812,8 +828,10 @@ extern "C" int osdp_route_fwd(const void *logits, int64_t ld, int logits_dtype, 
   if (!logits || !idx || !weights) return OSDP_ERR_NULL_POINTER;
   if (!aligned_to(logits, logits_dtype == OSDP_DTYPE_FP32 ? 4 : 2) || !aligned_to(bias, 4) || !aligned_to(idx, 4) || !aligned_to(weights, 4))
     return OSDP_ERR_ALIGNMENT;
-  const RouteArgs a{logits, (long long)ld, (long long)T, bias, E, top_k, score, n_groups, top_groups, group_take, renorm ? 1 : 0, (float)scale,
-                    idx, weights};
+  RouteArgs a{logits, (long long)ld, (long long)T, bias, E, top_k, score, n_groups, top_groups, group_take, renorm ? 1 : 0, (float)scale,
+              idx, weights, E / n_groups, 5, 0u};
+  while ((n_groups << a.lanes_log2) > 32) --a.lanes_log2;
+  a.magic = ((1u << 20) + a.size - 1) / a.size;
   return logits_dtype == OSDP_DTYPE_FP32 ? launch_route<float>(a, static_cast<cudaStream_t>(stream))
                                          : launch_route<__nv_bfloat16>(a, static_cast<cudaStream_t>(stream));
 }
@@ -829,7 +847,7 @@ extern "C" int osdp_route_bwd(const float *dweights, const void *logits, int64_t
   if (!aligned_to(logits, es) || !aligned_to(dlogits, es) || !aligned_to(dweights, 4) || !aligned_to(idx, 4)) return OSDP_ERR_ALIGNMENT;
   RouteBackArgs b{};
   b.r = RouteArgs{logits, (long long)ld, (long long)T, nullptr, E, top_k, score, 1, 1, 1, renorm ? 1 : 0, (float)scale, const_cast<int32_t *>(idx),
-                  nullptr};
+                  nullptr, E, 5, 0u};
   b.dweights = dweights;
   b.dlogits = dlogits;
   b.ld_out = (long long)ld_dlogits;
