@@ -614,16 +614,20 @@ struct RowsArgs {
   float *dweights;
   long long T;
   int k, E, D;
-  long long token_blocks;        // dispatch: the blocks behind these clear the rows between the experts
   uint32_t magic;                // 2^32 / (D / 8), rounded up; 0 for D = 8
+  int clear_experts, clear_blocks;   // dispatch: experts that have rows (at most), blocks for the rows behind one's
   int team;                      // dispatch with dweights: warps to a (token, choice)
 };
 
-__device__ __forceinline__ void clear_between(const RowsArgs &a, int e) {
+// The first clear_experts * clear_blocks blocks: zeros in the rows between the experts that have any.
+__device__ __forceinline__ void clear_between(const RowsArgs &a) {
+  const int i_live = (int)blockIdx.x / a.clear_blocks, part = (int)blockIdx.x - i_live * a.clear_blocks;
+  if (i_live >= a.plan[plan_n_live(a.E)]) return;
+  const int e = a.plan[plan_live(a.E) + i_live];
   const long long first = a.plan[PLAN_OFFSETS + e] + a.plan[plan_counts(a.E) + e];
   const long long n = (a.plan[PLAN_OFFSETS + e + 1] - first) * (a.D >> 3);
   uint4 *p = reinterpret_cast<uint4 *>(a.out + first * a.D);
-  for (long long i = threadIdx.x; i < n; i += blockDim.x) p[i] = make_uint4(0u, 0u, 0u, 0u);
+  for (long long i = part * 256 + threadIdx.x; i < n; i += a.clear_blocks * 256) p[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
 // Pieces of a thread.  More of them, or fewer threads on an SM, and the pieces' addresses and sums cost more than the loads gain:
@@ -647,8 +651,9 @@ template <bool WEIGHTED>
 __global__ void __launch_bounds__(256) dispatch_kernel(const __grid_constant__ RowsArgs a) {
   pdl_launch_dependents();
   pdl_wait();
-  if (blockIdx.x >= a.token_blocks) return clear_between(a, (int)(blockIdx.x - a.token_blocks));
-  const long long start = (long long)blockIdx.x * CHUNK, n = a.T * (a.D >> 3) - start;
+  const long long block = (long long)blockIdx.x - a.clear_experts * a.clear_blocks;
+  if (block < 0) return clear_between(a);
+  const long long start = block * CHUNK, n = a.T * (a.D >> 3) - start;
   const long long t0 = start / (a.D >> 3);
   const uint32_t lead = (uint32_t)(start - t0 * (a.D >> 3));
   uint4 v[PER];
@@ -684,10 +689,11 @@ __global__ void __launch_bounds__(256) dispatch_dot_kernel(const __grid_constant
   __shared__ float part[8];
   pdl_launch_dependents();
   pdl_wait();
-  if (blockIdx.x >= a.token_blocks) return clear_between(a, (int)(blockIdx.x - a.token_blocks));
+  const long long block = (long long)blockIdx.x - a.clear_experts * a.clear_blocks;
+  if (block < 0) return clear_between(a);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, teams = 8 / a.team, team = warp / a.team;
   const int tl = (warp - team * a.team) * 32 + lane, TL = a.team * 32;
-  const long long slot = (long long)blockIdx.x * teams + team;
+  const long long slot = block * teams + team;
   const bool there = slot < a.T * a.k;
   const long long t = there ? slot / a.k : 0;
   const long long r = there ? a.pos[slot] : -1;
@@ -696,18 +702,30 @@ __global__ void __launch_bounds__(256) dispatch_dot_kernel(const __grid_constant
     const float w = a.weights ? a.weights[slot] : 1.0f;
     const __nv_bfloat16 *x = a.x + t * a.D, *y = a.y + r * a.D;
     __nv_bfloat16 *out = a.out + r * a.D;
-    for (int c = tl * 8; c < a.D; c += TL * 8) {
-      float f[8], h[8];
-      widen8(*reinterpret_cast<const uint4 *>(x + c), f);
-      widen8(load16(y + c), h);
-      float s = 0.f;
+    constexpr int AHEAD = 4;           // pieces of a lane on the way together
+    for (int c = tl * 8; c < a.D; c += AHEAD * TL * 8) {
+      uint4 xv[AHEAD], yv[AHEAD];
 #pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        s = fmaf(f[q], h[q], s);
-        f[q] *= w;
+      for (int u = 0; u < AHEAD; ++u) {
+        const int at = c + u * TL * 8;
+        xv[u] = at < a.D ? *reinterpret_cast<const uint4 *>(x + at) : make_uint4(0u, 0u, 0u, 0u);
+        yv[u] = at < a.D ? load16(y + at) : make_uint4(0u, 0u, 0u, 0u);
       }
-      dot += s;
-      *reinterpret_cast<uint4 *>(out + c) = narrow8(f);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int at = c + u * TL * 8;
+        float f[8], h[8];
+        widen8(xv[u], f);
+        widen8(yv[u], h);
+        float s = 0.f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          s = fmaf(f[q], h[q], s);
+          f[q] *= w;
+        }
+        dot += s;
+        if (at < a.D) *reinterpret_cast<uint4 *>(out + at) = narrow8(f);
+      }
     }
   }
   dot = warp_sum(dot);
@@ -891,19 +909,22 @@ extern "C" int osdp_expert_dispatch(const void *x, const int32_t *plan, const in
       !aligned_to(weights, 4) || !aligned_to(dweights, 4))
     return OSDP_ERR_ALIGNMENT;
   RowsArgs a{static_cast<const __nv_bfloat16 *>(x), plan, pos, weights, static_cast<const __nv_bfloat16 *>(y_rows), static_cast<__nv_bfloat16 *>(rows),
-             dweights, (long long)T, top_k, E, (int)D, 0, piece_magic(D), 1};
+             dweights, (long long)T, top_k, E, (int)D, piece_magic(D), 0, 1, 1};
+  int sms = 0;
+  const int src = sm_count(&sms);
+  if (src) return src;
+  // up to 63 rows behind each expert's: four pieces to a thread, where that does not make more blocks than the GPU has room for
+  a.clear_blocks = (int)cdiv((OSDP_EXPERT_ROWS - 1) * (D / 8), 1024);
+  a.clear_experts = (int)(T * top_k < E ? T * top_k : E);
+  if (a.clear_blocks > 4 * sms / a.clear_experts) a.clear_blocks = 4 * sms / a.clear_experts > 0 ? 4 * sms / a.clear_experts : 1;
+  const int64_t clear = (int64_t)a.clear_experts * a.clear_blocks;
   if (dweights) {
-    int sms = 0;
-    const int src = sm_count(&sms);
-    if (src) return src;
     // as many warps to a row as it has pieces for, more where there are few rows
     a.team = 1;
     while (a.team < 8 && a.team * 256 < D && (T * top_k * a.team < (int64_t)sms * 16 || a.team * 2048 < D)) a.team *= 2;
-    a.token_blocks = cdiv(T * top_k, 8 / a.team);
-    return launch_overlapped(dispatch_dot_kernel, dim3((unsigned)(a.token_blocks + E)), dim3(256), 0, 1, static_cast<cudaStream_t>(stream), a);
+    return launch_overlapped(dispatch_dot_kernel, dim3((unsigned)(cdiv(T * top_k, 8 / a.team) + clear)), dim3(256), 0, 1, static_cast<cudaStream_t>(stream), a);
   }
-  a.token_blocks = cdiv(T * (D / 8), CHUNK);
-  return launch_overlapped(weights ? dispatch_kernel<true> : dispatch_kernel<false>, dim3((unsigned)(a.token_blocks + E)), dim3(256), 0, 1,
+  return launch_overlapped(weights ? dispatch_kernel<true> : dispatch_kernel<false>, dim3((unsigned)(cdiv(T * (D / 8), CHUNK) + clear)), dim3(256), 0, 1,
                            static_cast<cudaStream_t>(stream), a);
 }
 
@@ -915,7 +936,7 @@ extern "C" int osdp_expert_combine(const void *rows, const int32_t *plan, const 
   if (!rows || !pos || !plan || !out) return OSDP_ERR_NULL_POINTER;
   if (!aligned_to(rows, 16) || !aligned_to(out, 16) || !aligned_to(plan, 16) || !aligned_to(pos, 4) || !aligned_to(weights, 4)) return OSDP_ERR_ALIGNMENT;
   const RowsArgs a{static_cast<const __nv_bfloat16 *>(rows), plan, pos, weights, nullptr, static_cast<__nv_bfloat16 *>(out), nullptr, (long long)T,
-                   top_k, E, (int)D, 0, piece_magic(D), 1};
+                   top_k, E, (int)D, piece_magic(D), 0, 1, 1};
   const dim3 grid((unsigned)cdiv(T * (D / 8), top_k <= 2 ? Combine<2>::CHUNK : Combine<4>::CHUNK));
   if (top_k == 1) return launch_overlapped(combine_kernel<1>, grid, dim3(256), 0, 1, static_cast<cudaStream_t>(stream), a);
   if (top_k == 2) return launch_overlapped(combine_kernel<2>, grid, dim3(256), 0, 1, static_cast<cudaStream_t>(stream), a);
