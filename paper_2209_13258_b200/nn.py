@@ -577,3 +577,203 @@ class Int8Linear(torch.nn.Module):
         B.osdp_split_linear_fwd_i8(q, s, w8, 0, w_scale, bias, M, N, K, self.k_split, self.split_dim, self.act, out, held["_status"], stream,
                                    True)
         return out
+
+
+class _RouteFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, router):
+        T, E, k = logits.shape[0], router.experts, router.top_k
+        idx = torch.empty(T, k, dtype=torch.int32, device=logits.device)
+        weights = torch.empty(T, k, dtype=torch.float32, device=logits.device)
+        dt = B.DTYPE_FP32 if logits.dtype is torch.float32 else B.DTYPE_BF16
+        B.osdp_route_fwd(logits, max(logits.stride(0), E), dt, router.bias, T, E, k, router.score, router.groups, router.top_groups,
+                         router.group_take, router.renormalise, router.scale, idx, weights, check=True)
+        ctx.router = router
+        ctx.save_for_backward(logits, idx)
+        ctx.mark_non_differentiable(idx)
+        ctx.set_materialize_grads(False)
+        return weights, idx
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dweights, _):
+        if dweights is None:
+            return None, None
+        r = ctx.router
+        logits, idx = ctx.saved_tensors
+        T, E = logits.shape
+        out = torch.empty(T, E, dtype=logits.dtype, device=logits.device)
+        dt = B.DTYPE_FP32 if logits.dtype is torch.float32 else B.DTYPE_BF16
+        B.osdp_route_bwd(dweights.contiguous(), logits, max(logits.stride(0), E), dt, idx, T, E, r.top_k, r.score, r.renormalise, r.scale, out, E,
+                         check=True)
+        return out, None
+
+
+class ExpertRouter(torch.nn.Module):
+    """Which experts a token goes to: ``forward(logits)`` of [..., experts] logits (bf16 or fp32) returns (weights, idx), the weights
+    [..., top_k] fp32 with a gradient into the logits, and the experts [..., top_k] int32, best first.
+
+    score: "softmax" or "sigmoid".  renormalise: the weights of a token are made to add up to `scale`.  groups, top_groups,
+    group_take: the experts form `groups` groups of neighbours, and only those of the `top_groups` best may be chosen, a group
+    being as good as the sum of its `group_take` (1 or 2) best.  bias=True: a buffer `bias` [experts] fp32, zero at first, is added
+    to the scores for the choice alone, to balance the load (it has no gradient, and has to stay fp32).
+    """
+
+    def __init__(self, experts, top_k, score="softmax", renormalise=True, scale=1.0, groups=1, top_groups=None, group_take=1, bias=False,
+                 device="cuda"):
+        super().__init__()
+        scores = {"softmax": B.SCORE_SOFTMAX, "sigmoid": B.SCORE_SIGMOID}
+        if score not in scores:
+            raise ValueError('score is "softmax" or "sigmoid"')
+        if not 1 <= experts <= B.MAX_EXPERTS or not 1 <= top_k <= min(experts, B.MAX_TOP_K):
+            raise ValueError("1 to %d experts, of which a token chooses at most %d" % (B.MAX_EXPERTS, B.MAX_TOP_K))
+        top_groups = groups if top_groups is None else top_groups
+        if not 1 <= groups <= 32 or experts % groups or not 1 <= top_groups <= groups or top_groups * (experts // groups) < top_k:
+            raise ValueError("up to 32 groups of equal size, of which the best have at least top_k experts")
+        if group_take not in (1, 2):
+            raise ValueError("a group is judged by its best expert or by its best two")
+        self.experts, self.top_k, self.score = int(experts), int(top_k), scores[score]
+        self.renormalise, self.scale = bool(renormalise), float(scale)
+        self.groups, self.top_groups, self.group_take = int(groups), int(top_groups), int(group_take)
+        self.register_buffer("bias", torch.zeros(self.experts, dtype=torch.float32, device=device) if bias else None)
+
+    def forward(self, logits):
+        if not logits.is_cuda:
+            raise RuntimeError("ExpertRouter runs on CUDA only: there is no CPU path")
+        if logits.dtype not in (torch.bfloat16, torch.float32):
+            raise TypeError("ExpertRouter takes bf16 or fp32 logits")
+        if logits.shape[-1] != self.experts:
+            raise ValueError("ExpertRouter takes [..., experts]")
+        if _elsewhere(logits):
+            with torch.cuda.device(logits.device):
+                return self.forward(logits)
+        _check_fp32(logits.device, bias=(self.bias, self.experts))
+        flat = logits.reshape(-1, self.experts)
+        if flat.stride(-1) != 1 or (flat.shape[0] > 1 and flat.stride(0) < self.experts):
+            flat = flat.contiguous()
+        weights, idx = _RouteFn.apply(flat, self)
+        shape = logits.shape[:-1] + (self.top_k,)
+        return weights.view(shape), idx.view(shape)
+
+
+class _ExpertMLPFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weights, flat, b1, b2, idx, layer):
+        E, H, F, T, k = layer.experts, layer.hidden, layer.ffn, idx.shape[0], idx.shape[1]
+        need = any(ctx.needs_input_grad)
+        dev = x.device
+        new = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device=dev)     # noqa: E731
+        rc, R, ints = B.osdp_expert_rows(T, k, E)
+        if rc:
+            raise B.OsdpError(rc, "osdp_expert_rows")
+        plan, pos = torch.empty(ints, dtype=torch.int32, device=dev), torch.empty(T, k, dtype=torch.int32, device=dev)
+        stream, status = B._stream(None), layer._status
+        B.osdp_expert_plan(idx, T, k, E, plan, pos, stream, True)
+        xs, h, y, out = new(R, H), new(R, F), new(R, H), new(T, H)
+        z = new(R, F) if need and layer.act != B.ACT_NONE else None
+        B.osdp_expert_dispatch(x, plan, pos, None, None, T, k, E, H, xs, None, stream, True)
+        B.osdp_expert_linear_fwd(xs, plan, flat, layer.off_w1, b1, T, k, E, F, H, layer.act, h, z, status, stream, True)
+        B.osdp_expert_linear_fwd(h, plan, flat, layer.off_w2, b2, T, k, E, H, F, B.ACT_NONE, y, None, status, stream, True)
+        B.osdp_expert_combine(y, plan, pos, weights, T, k, E, H, out, stream, True)
+        if need:
+            ctx.layer = layer
+            ctx.save_for_backward(weights, flat, plan, pos, xs, z, h, y)
+        return out
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout):
+        layer = ctx.layer
+        weights, flat, plan, pos, xs, z, h, y = ctx.saved_tensors
+        E, H, F, T, k = layer.experts, layer.hidden, layer.ffn, pos.shape[0], pos.shape[1]
+        need_x, need_w, need_flat, need_b1, need_b2 = ctx.needs_input_grad[:5]
+        dev = dout.device
+        new = lambda on, dtype, *shape: torch.empty(shape, dtype=dtype, device=dev) if on else None      # noqa: E731
+        half, full = torch.bfloat16, torch.float32
+        R = xs.shape[0]
+        dys, dw = new(True, half, R, H), new(need_w, full, T, k)
+        stream = B._stream(None)
+        B.osdp_expert_dispatch(dout.contiguous(), plan, pos, weights, y if need_w else None, T, k, E, H, dys, dw, stream, True)
+        first = need_x or need_flat or need_b1             # something before the second product has a gradient
+        dflat = torch.empty_like(flat) if need_flat else None           # both products' gradients fill it
+        dh, dxs = new(first, half, R, F), new(need_x, half, R, H)
+        db1, db2, dx = new(need_b1, full, E, F), new(need_b2, full, E, H), new(need_x, half, T, H)
+        bytes2 = B.osdp_expert_linear_workspace_bytes(T, k, E, H, F, B.ACT_NONE, B.OP_LINEAR_BWD)[1]
+        bytes1 = B.osdp_expert_linear_workspace_bytes(T, k, E, F, H, layer.act, B.OP_LINEAR_BWD)[1]
+        # this call's own: a backward on another stream may run at the same time, a captured one keeps its own
+        ws = torch.empty(max(bytes1, bytes2), dtype=torch.uint8, device=dev)
+        ws[:256].zero_()
+        if first or need_b2:
+            B.osdp_expert_linear_bwd(dys, h, plan, flat, layer.off_w2, None, T, k, E, H, F, B.ACT_NONE, dh, dflat, layer.off_w2, B.DTYPE_BF16, 0, db2, ws,
+                                     stream, True)
+        if first:
+            B.osdp_expert_linear_bwd(dh, xs, plan, flat, layer.off_w1, z, T, k, E, F, H, layer.act, dxs, dflat, layer.off_w1, B.DTYPE_BF16, 0, db1, ws,
+                                     stream, True)
+        if need_x:
+            B.osdp_expert_combine(dxs, plan, pos, None, T, k, E, H, dx, stream, True)
+        return dx, dw, dflat, db1, db2, None, None
+
+
+class ExpertMLP(torch.nn.Module):
+    """A mixture of MLP blocks in the place of one: y[t] = sum over j of weights[t, j] * (act(x[t] W1_e^T + b1_e) W2_e^T + b2_e), e = idx[t, j],
+    with the weights and experts of an ``ExpertRouter``: ``mlp(x, *router(logits))``.
+
+    W1 [experts, ffn, hidden] and W2 [experts, hidden, ffn] live in one flat bf16 parameter buffer (`flat_param`, W1 first), the biases
+    [experts, ffn] and [experts, hidden] are fp32.  Rows are sorted by expert on the device, every expert's product runs in the same
+    launch, and nothing waits for the host to learn who got how many.  An index outside the experts drops that choice.
+    """
+
+    def __init__(self, hidden, ffn, experts, bias=True, act=B.ACT_GELU_TANH, device="cuda"):
+        super().__init__()
+        if hidden % 8 or ffn % 8 or hidden <= 0 or ffn <= 0:
+            raise ValueError("hidden and ffn must be multiples of 8")
+        if not 1 <= experts <= B.MAX_EXPERTS:
+            raise ValueError("1 to %d experts" % B.MAX_EXPERTS)
+        self.hidden, self.ffn, self.experts, self.act = int(hidden), int(ffn), int(experts), int(act)
+        self.off_w1, self.off_w2 = 0, self.experts * self.hidden * self.ffn
+        w = torch.empty(2 * self.off_w2, dtype=torch.bfloat16, device=device)
+        torch.nn.init.normal_(w, std=0.02)
+        self.flat_param = torch.nn.Parameter(w)
+        mk = lambda n: torch.nn.Parameter(torch.zeros(self.experts, n, dtype=torch.float32, device=device)) if bias else None      # noqa: E731
+        self.b1, self.b2 = mk(self.ffn), mk(self.hidden)
+        # the tile kernels' status word: all that is kept between calls
+        self.register_buffer("_status", torch.zeros(256, dtype=torch.uint8, device=device), persistent=False)
+        rc, _ = B.osdp_expert_linear_workspace_bytes(1, 1, self.experts, self.ffn, self.hidden, self.act, B.OP_LINEAR_BWD)
+        if rc:
+            raise B.OsdpError(rc, "ExpertMLP")
+
+    @property
+    def flat(self):
+        return self.flat_param
+
+    @property
+    def w1(self):
+        return self.flat_param[:self.off_w2].view(self.experts, self.ffn, self.hidden)
+
+    @property
+    def w2(self):
+        return self.flat_param[self.off_w2:].view(self.experts, self.hidden, self.ffn)
+
+    def forward(self, x, weights, idx):
+        if not x.is_cuda:
+            raise RuntimeError("ExpertMLP runs on CUDA only: there is no CPU path")
+        if x.dtype != torch.bfloat16:
+            raise TypeError("ExpertMLP takes bf16 activations")
+        if weights.dtype != torch.float32 or idx.dtype != torch.int32:
+            raise TypeError("the weights are fp32 and the experts int32, as ExpertRouter returns them")
+        if x.shape[-1] != self.hidden or weights.shape != idx.shape or weights.shape[:-1] != x.shape[:-1]:
+            raise ValueError("ExpertMLP takes x [..., hidden] and weights, idx [..., top_k]")
+        if weights.device != x.device or idx.device != x.device:
+            raise RuntimeError("x, its weights and its experts have to be on one CUDA device")
+        if _elsewhere(x):
+            with torch.cuda.device(x.device):
+                return self.forward(x, weights, idx)
+        _check_flat(x.device, self.flat_param, 2 * self.off_w2)
+        _check_fp32(x.device, b1=(self.b1, self.experts * self.ffn), b2=(self.b2, self.experts * self.hidden))
+        if self._status.device != x.device:
+            raise RuntimeError("the module is on %s and its input on %s: they have to be on one CUDA device" % (self._status.device, x.device))
+        k = idx.shape[-1]
+        T = idx.numel() // k if k else 0
+        out = _ExpertMLPFn.apply(x.reshape(T, self.hidden).contiguous(), weights.reshape(T, k).contiguous(), self.flat_param, self.b1, self.b2,
+                                 idx.reshape(T, k).contiguous(), self)
+        return out.view(x.shape)
