@@ -46,7 +46,7 @@ __device__ __forceinline__ float gelu_erf_grad(float x) {
   return fmaf(x, 0.3989422804014327f * __expf(-0.5f * x * x), 0.5f * erfcf(-0.7071067811865476f * x));
 }
 
-__global__ void __launch_bounds__(256, 2) expert_grad_kernel(const __grid_constant__ GradArgs a) {
+__global__ void __launch_bounds__(256, 4) expert_grad_kernel(const __grid_constant__ GradArgs a) {
   __shared__ float red[8][GRAD_COLS];
   pdl_launch_dependents();
   const int cols = (a.N + GRAD_COLS - 1) / GRAD_COLS, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -56,14 +56,16 @@ __global__ void __launch_bounds__(256, 2) expert_grad_kernel(const __grid_consta
   // are on their way.
   constexpr int EACH = GRAD_ROWS / 8;
   const long long at = ((long long)part * GRAD_ROWS + warp) * a.N + col;
-  uint4 d[EACH], z[EACH];
-  if (col < a.N) {
+  constexpr int HALF = EACH / 2;         // at a time: twice the blocks on an SM
+  uint4 d[HALF], z[HALF];
+  auto load = [&](int h) {
 #pragma unroll
-    for (int q = 0; q < EACH; ++q) {
-      d[q] = load16(a.dy + at + (long long)q * 8 * a.N);
-      if (a.g) z[q] = load16(a.z + at + (long long)q * 8 * a.N);
+    for (int q = 0; q < HALF; ++q) {
+      d[q] = load16(a.dy + at + (long long)(h * HALF + q) * 8 * a.N);
+      if (a.g) z[q] = load16(a.z + at + (long long)(h * HALF + q) * 8 * a.N);
     }
-  }
+  };
+  if (col < a.N) load(0);
   // the expert whose rows these are: offsets[e] <= row < offsets[e + 1]
   const int32_t *offsets = a.plan + PLAN_OFFSETS;
   int e = -1;
@@ -76,14 +78,15 @@ __global__ void __launch_bounds__(256, 2) expert_grad_kernel(const __grid_consta
   if (col < a.N) {
 #pragma unroll
     for (int q = 0; q < EACH; ++q) {
+      if (q > 0 && q % HALF == 0) load(q / HALF);
       f2 f[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) f[j] = both(0.f);
       if (8 * q < count) {
-        widen4(d[q], f);
+        widen4(d[q % HALF], f);
         if (a.g) {
           f2 x[4];
-          widen4(z[q], x);
+          widen4(z[q % HALF], x);
           if (a.act == ACT_GELU_TANH) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) f[j] = mul2(f[j], gelu_tanh_grad2(x[j]));

@@ -291,9 +291,9 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const L *row, const f
       off = 2.0f * V * fabsf(value);                                          // the bits that the place took
       if (a.bias) {
         bj = a.bias[mine];
-        // the score (see above, here relative to itself) and its sum with the bias
+        // the score (see above, here relative to itself; beyond 100 nothing is left of it) and its sum with the bias
         const float s = fabsf(value - bj);
-        off += fabsf(value) + fabsf(bj) + (soft ? s * (1.5f * (high - lj) + 46.0f) : s * ((1.0f - fminf(s, 1.0f) + 0.01f) * (1.5f * fabsf(lj) + 6.0f) + 6.0f));
+        off += fabsf(value) + fabsf(bj) + (soft ? s * (1.5f * fminf(high - lj, 100.0f) + 46.0f) : s * ((1.0f - fminf(s, 1.0f) + 0.01f) * (1.5f * fminf(fabsf(lj), 100.0f) + 6.0f) + 6.0f));
       }
     }
     const int after = __shfl_down_sync(ALL, mine, 1);

@@ -222,3 +222,17 @@ def test_training_with_the_optimiser():
         assert p.grad is not None and bool(torch.isfinite(p.grad).all()) and bool(p.grad.float().abs().max() > 0)
     opt.step()
     assert all(not torch.equal(a, b) for a, b in zip(before, (*m.parameters(), *gate.parameters())))
+
+
+def test_example_with_experts():
+    """It runs, and gradients reach every parameter."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import residual_blocks
+    losses, _ = residual_blocks.main(["--hidden", "128", "--ffn", "256", "--blocks", "2", "--tokens", "300", "--steps", "3", "--experts", "6"])
+    assert len(losses) == 3 and all(math.isfinite(v) for v in losses)
+    net = residual_blocks.Stack(128, 256, 2, experts=6)
+    net(torch.randn(300, 128, device="cuda")).square().mean().backward()
+    for n, p in net.named_parameters():
+        assert p.grad is not None and bool(torch.isfinite(p.grad).all()) and bool(p.grad.float().abs().max() > 0), n

@@ -271,6 +271,18 @@ def test_products_backward(T, k, E, how, N, K, act):
     Problem(T, k, E, how, N, K).check_backward(act, dw_dtype=torch.float32 if act == P.ACT_GELU_TANH else BF16)
 
 
+@pytest.mark.parametrize("T", [5, 300])
+def test_nobody_is_chosen(T):
+    """Every choice is dropped: no row is written, and all gradients of the weights are zero."""
+    p = Problem(T, 2, 6, "even", 136, 72)
+    idx = torch.full((T, 2), 6, dtype=torch.int32, device="cuda")
+    p.plan, p.pos, p.R = make_plan(idx, 6)
+    out, _ = p.forward(P.ACT_GELU_TANH)
+    assert p.R == len(out) and bool((out == MARK).all())
+    dx, dw, db = p.backward(P.ACT_GELU_TANH)
+    assert bool((dx == MARK).all()) and bool((dw[64:] == 0).all()) and bool((db == 0).all())
+
+
 def test_gradients_are_added_and_left_out():
     p = Problem(300, 2, 5, "skewed", 264, 136)
     for dtype in (torch.float32, BF16):

@@ -104,6 +104,23 @@ def test_scores_that_fp32_cannot_tell_apart(score, groups, top, take):
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,k,groups,top", [(32, 2, 1, 1), (64, 16, 4, 3), (128, 8, 1, 1), (1000, 5, 1, 1), (1024, 16, 32, 8)])
+def test_masked_experts_among_scores_that_fp32_cannot_tell_apart(score, E, k, groups, top):
+    """A masked expert's score is its bias exactly, an expert's beside it the same but for what fp32 cannot hold; more of them
+    than a warp has lanes."""
+    g = torch.Generator(device="cuda").manual_seed(E)
+    row = torch.randn(1, E, device="cuda", generator=g)
+    row[0, ::3] = -math.inf
+    s = torch.softmax(row.to(D64), 1) if score == "softmax" else torch.sigmoid(row.to(D64))
+    bias = (0.75 - s[0]).float()
+    bias[::3] = 0.75
+    l = row.repeat(16, 1)
+    l[1::2] += 1e-7 * torch.randn(8, E, device="cuda", generator=g)
+    for take in (1, 2):
+        check(l, bias, k, score, groups=groups, top=top, take=take, renorm=False)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("renorm", [True, False])
 @pytest.mark.parametrize("groups,top", [(1, 1), (4, 2)])
 @pytest.mark.parametrize("bias", [False, True])
