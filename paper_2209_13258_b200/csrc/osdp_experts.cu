@@ -248,10 +248,11 @@ int launch_expert_gemm(const ExpertGemm &c, cudaStream_t stream) {
   p.P = (int)(red ? c.N : c.R);
   p.Q = (int)(red ? c.K : (c.b_mn ? c.K : c.N));
   p.R = (int)(red ? c.R : (c.b_mn ? c.N : c.K));
-  // Tiles, were the choices spread evenly (only the device knows): for an expert's rows, half a tile more than they fill.
+  // Tiles, were the choices spread evenly (only the device knows): one for each expert that has rows, or half a tile more than the
+  // rows fill.
   auto tiles = [&](int tm, int bn) {
-    const int64_t m = red ? cdiv(c.N, tm) * c.E : n / tm + cdiv(used, 2);
-    return (m > 0 ? m : 1) * cdiv(p.Q, bn);
+    const int64_t full = n / tm + cdiv(used, 2), m = red ? cdiv(c.N, tm) * c.E : (full > used ? full : used);
+    return m * cdiv(p.Q, bn);
   };
   // CTA pairs on 256 rows where the experts fill most of such a tile, and there are tiles for a third of the SMs.
   const bool pair = tiles(256, 256) >= sms / 3 && (red || n >= 160 * used);
