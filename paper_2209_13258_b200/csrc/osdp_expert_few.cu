@@ -238,15 +238,16 @@ int launch_few(FewArgs a, int64_t live, cudaStream_t stream) {
 
 }  // namespace
 
-// The tile kernel streams the weights as well where it has a tile for each SM, but a k-block takes it 0.2 us, and it has an
-// epilogue at the end.  Measured on B200 (us, few / tile), T x top_k of E, K -> N: 1 x 2 of 8, 2048 -> 8192 17.1 / 17.2, 8192 -> 2048 19.4 / 36.7,
-// 1024 -> 1024 3.7 / 8.8; 4 x 4 of 64, 1024 -> 1024 14.1 / 15.8; 1 x 8 of 64, 2048 -> 2048 20.5 / 22.5; 8 x 2 of 8, 8192 -> 8192 161 / 160.
-// With more than eight rows to an expert only where there are few tiles: 16 x 2 of 2, 8192 -> 2048 26 / 36.5, 64 x 2 of 16, 512 -> 512
-// 5.8 / 8.2; but 32 x 2 of 4, 2048 -> 2048 15.7 / 14.7, 64 x 2 of 16, 2048 -> 2048 38 / 31.
+// The tile kernel streams the weights as well where it has a tile for each SM, but a k-block takes it 0.2 us, and it has some 5 us
+// before its first and behind its last.  Measured on B200 (us, few / tile), T x top_k of E, K -> N.  Up to eight rows to an expert:
+// 1 x 2 of 8, 2048 -> 8192 17.1 / 17.2, 8192 -> 2048 19.4 / 36.7, 1024 -> 1024 3.7 / 8.8; 4 x 4 of 64, 1024 -> 1024 10.2 / 15.8;
+// 1 x 8 of 64, 2048 -> 2048 20.4 / 22.5; 8 x 2 of 8, 8192 -> 8192 159 / 160.  With more, where the tiles are few: 16 x 2 of 2,
+// 8192 -> 2048 20.7 / 36.5; or the weights: 100 of 16, 512 -> 512 4.6 / 7.6; 56 x 2 of 55, 192 -> 408 5.2 / 11.4; 79 x 2 of 68, 400 -> 480
+// 9.2 / 14.4; but 37 x 2 of 16, 1032 -> 2064 22.9 / 19.7, 64 x 2 of 16, 2048 -> 2048 38 / 29, 32 x 2 of 64, 1024 -> 1024 33 / 26.
 bool expert_few_rows(int64_t T, int top_k, int E, int64_t N, int64_t K) {
   const int64_t n = T * top_k, used = n < E ? n : E;
   if (used * cdiv(N, ROWS) >= ((int64_t)1 << 30)) return false;
-  return T <= 8 || (n <= 16 * used && used * cdiv(N, 128) <= 64);
+  return T <= 8 || (n <= 16 * used && (used * cdiv(N, 128) <= 64 || used * N * K < (1 << 24)));
 }
 
 int launch_expert_few(const void *rows, const int32_t *plan, const void *w, const float *bias, int64_t T, int top_k, int E, int64_t N, int64_t K, int act,
