@@ -913,8 +913,8 @@ extern "C" int osdp_expert_dispatch(const void *x, const int32_t *plan, const in
   int sms = 0;
   const int src = sm_count(&sms);
   if (src) return src;
-  // up to 63 rows behind each expert's: four pieces to a thread, where that does not make more blocks than the GPU has room for
-  a.clear_blocks = (int)cdiv((OSDP_EXPERT_ROWS - 1) * (D / 8), 1024);
+  // up to 63 rows behind each expert's: eight pieces to a thread, where that does not make more blocks than the GPU has room for
+  a.clear_blocks = (int)cdiv((OSDP_EXPERT_ROWS - 1) * (D / 8), 2048);
   a.clear_experts = (int)(T * top_k < E ? T * top_k : E);
   if (a.clear_blocks > 4 * sms / a.clear_experts) a.clear_blocks = 4 * sms / a.clear_experts > 0 ? 4 * sms / a.clear_experts : 1;
   const int64_t clear = (int64_t)a.clear_experts * a.clear_blocks;
