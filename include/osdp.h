@@ -540,6 +540,19 @@ int osdp_expert_linear_bwd(const void *dy, const void *rows, const int32_t *plan
                            const void *z_saved, int64_t T, int top_k, int E, int64_t N, int64_t K, int act, void *dx, void *dw_flat,
                            int64_t dw_offset, int dw_dtype, int flags, float *dbias, void *ws, size_t ws_bytes, void *stream);
 
+/* The mixture-of-experts calls above with their arguments in memory: words[0] says which, then every argument in its order as
+ * one 8-byte word (pointers, integers and sizes as int64, doubles as they are).  For callers whose foreign-function interface
+ * takes its time for every argument: through ctypes 16 arguments take 2.1 us, one 0.45 us.  Returns what the call returns;
+ * an integer that an int argument cannot hold is refused as the call refuses a nonsensical one.  words need no alignment. */
+#define OSDP_CALL_ROUTE_FWD 0
+#define OSDP_CALL_ROUTE_BWD 1
+#define OSDP_CALL_EXPERT_PLAN 2
+#define OSDP_CALL_EXPERT_DISPATCH 3
+#define OSDP_CALL_EXPERT_COMBINE 4
+#define OSDP_CALL_EXPERT_LINEAR_FWD 5
+#define OSDP_CALL_EXPERT_LINEAR_BWD 6
+int osdp_call(const void *words);
+
 /* Failure detection (no counterpart in the paper, which does not discuss faults: the slices of Section
  * 3.3 "executed sequentially" are pipelines of asynchronous copies and tensor-core work whose stages
  * wait on one another, and every such wait here is bounded).  Synchronises `stream`, copies the device

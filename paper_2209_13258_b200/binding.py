@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 
@@ -36,7 +37,7 @@ EXPORTS = [
     "osdp_clip_coefficient",
     "osdp_quantize_rows_i8", "osdp_split_linear_fwd_i8", "osdp_i8_workspace_bytes",
     "osdp_route_fwd", "osdp_route_bwd", "osdp_expert_rows", "osdp_expert_plan", "osdp_expert_dispatch", "osdp_expert_combine",
-    "osdp_expert_linear_workspace_bytes", "osdp_expert_linear_fwd", "osdp_expert_linear_bwd",
+    "osdp_expert_linear_workspace_bytes", "osdp_expert_linear_fwd", "osdp_expert_linear_bwd", "osdp_call",
 ]
 
 _lib = None
@@ -126,15 +127,9 @@ def lib():
         L.osdp_i8_workspace_bytes.argtypes = [i64, i64, ctypes.POINTER(sz)]
         L.osdp_quantize_rows_i8.argtypes = [vp, i64, i64, vp, vp, vp]
         L.osdp_split_linear_fwd_i8.argtypes = [vp, vp, vp, i64, vp, vp, i64, i64, i64, ci, ci, ci, vp, vp, sz, vp]
-        L.osdp_route_fwd.argtypes = [vp, i64, ci, vp, i64, ci, ci, ci, ci, ci, ci, ci, dbl, vp, vp, vp]
-        L.osdp_route_bwd.argtypes = [vp, vp, i64, ci, vp, i64, ci, ci, ci, ci, dbl, vp, i64, vp]
         L.osdp_expert_rows.argtypes = [i64, ci, ci, p64, p64]
-        L.osdp_expert_plan.argtypes = [vp, i64, ci, ci, vp, vp, vp]
-        L.osdp_expert_dispatch.argtypes = [vp, vp, vp, vp, vp, i64, ci, ci, i64, vp, vp, vp]
-        L.osdp_expert_combine.argtypes = [vp, vp, vp, vp, i64, ci, ci, i64, vp, vp]
         L.osdp_expert_linear_workspace_bytes.argtypes = [i64, ci, ci, i64, i64, ci, ci, ctypes.POINTER(sz)]
-        L.osdp_expert_linear_fwd.argtypes = [vp, vp, vp, i64, vp, i64, ci, ci, i64, i64, ci, vp, vp, vp, sz, vp]
-        L.osdp_expert_linear_bwd.argtypes = [vp, vp, vp, vp, i64, vp, i64, ci, ci, i64, i64, ci, vp, vp, i64, ci, ci, vp, vp, sz, vp]
+        L.osdp_call.argtypes = [ctypes.c_char_p]
         for name in EXPORTS:
             getattr(L, name)
             if name not in ("osdp_status_string",):
@@ -537,17 +532,34 @@ def osdp_split_linear_fwd_i8(x, x_scale, w8_flat, w_offset, w_scale, bias, M, N,
     return _ret(rc, check, "osdp_split_linear_fwd_i8")
 
 
+# The mixture-of-experts calls go through osdp_call: their arguments packed as words (ctypes takes 0.1 us for each, and the
+# smallest of these calls a few us in all).  q: an integer, Q: an address, d: a double.
+_entry = None
+_ROUTE_FWD, _ROUTE_BWD, _PLAN, _DISPATCH, _COMBINE, _LINEAR_FWD, _LINEAR_BWD = (struct.Struct("=q" + f).pack for f in (
+    "QqqQqqqqqqqqdQQQ", "QQqqQqqqqqdQqQ", "QqqqQQQ", "QQQQQqqqqQQQ", "QQQQqqqqQQ", "QQQqQqqqqqqQQQQQ", "QQQQqQqqqqqqQQqqqQQQQ"))
+
+
+def _load_entry():
+    global _entry
+    _entry = lib().osdp_call
+    return _entry
+
+
+def _word(t):
+    return 0 if t is None else t if type(t) is int else int(t) if isinstance(t, int) else t.data_ptr()
+
+
 def osdp_route_fwd(logits, ld, logits_dtype, bias, T, E, top_k, score, n_groups, top_groups, group_take, renorm, scale, idx, weights,
                    stream=None, check=False):
-    rc = lib().osdp_route_fwd(_ptr(logits), ld, logits_dtype, _ptr(bias), T, E, top_k, score, n_groups, top_groups, group_take, renorm, scale,
-                              _ptr(idx), _ptr(weights), _stream(stream))
-    return _ret(rc, check, "osdp_route_fwd")
+    rc = (_entry or _load_entry())(_ROUTE_FWD(0, _word(logits), ld, logits_dtype, _word(bias), T, E, top_k, score, n_groups, top_groups, group_take,
+                                              renorm, scale, _word(idx), _word(weights), _stream(stream) or 0))
+    return _ret(rc, check, "osdp_route_fwd") if rc else 0
 
 
 def osdp_route_bwd(dweights, logits, ld, logits_dtype, idx, T, E, top_k, score, renorm, scale, dlogits, ld_dlogits, stream=None, check=False):
-    rc = lib().osdp_route_bwd(_ptr(dweights), _ptr(logits), ld, logits_dtype, _ptr(idx), T, E, top_k, score, renorm, scale, _ptr(dlogits),
-                              ld_dlogits, _stream(stream))
-    return _ret(rc, check, "osdp_route_bwd")
+    rc = (_entry or _load_entry())(_ROUTE_BWD(1, _word(dweights), _word(logits), ld, logits_dtype, _word(idx), T, E, top_k, score, renorm, scale,
+                                              _word(dlogits), ld_dlogits, _stream(stream) or 0))
+    return _ret(rc, check, "osdp_route_bwd") if rc else 0
 
 
 def osdp_expert_rows(T, top_k, E):
@@ -558,19 +570,19 @@ def osdp_expert_rows(T, top_k, E):
 
 
 def osdp_expert_plan(idx, T, top_k, E, plan, pos, stream=None, check=False):
-    rc = lib().osdp_expert_plan(_ptr(idx), T, top_k, E, _ptr(plan), _ptr(pos), _stream(stream))
-    return _ret(rc, check, "osdp_expert_plan")
+    rc = (_entry or _load_entry())(_PLAN(2, _word(idx), T, top_k, E, _word(plan), _word(pos), _stream(stream) or 0))
+    return _ret(rc, check, "osdp_expert_plan") if rc else 0
 
 
 def osdp_expert_dispatch(x, plan, pos, weights, y_rows, T, top_k, E, D, rows, dweights, stream=None, check=False):
-    rc = lib().osdp_expert_dispatch(_ptr(x), _ptr(plan), _ptr(pos), _ptr(weights), _ptr(y_rows), T, top_k, E, D, _ptr(rows), _ptr(dweights),
-                                    _stream(stream))
-    return _ret(rc, check, "osdp_expert_dispatch")
+    rc = (_entry or _load_entry())(_DISPATCH(3, _word(x), _word(plan), _word(pos), _word(weights), _word(y_rows), T, top_k, E, D, _word(rows),
+                                             _word(dweights), _stream(stream) or 0))
+    return _ret(rc, check, "osdp_expert_dispatch") if rc else 0
 
 
 def osdp_expert_combine(rows, plan, pos, weights, T, top_k, E, D, out, stream=None, check=False):
-    rc = lib().osdp_expert_combine(_ptr(rows), _ptr(plan), _ptr(pos), _ptr(weights), T, top_k, E, D, _ptr(out), _stream(stream))
-    return _ret(rc, check, "osdp_expert_combine")
+    rc = (_entry or _load_entry())(_COMBINE(4, _word(rows), _word(plan), _word(pos), _word(weights), T, top_k, E, D, _word(out), _stream(stream) or 0))
+    return _ret(rc, check, "osdp_expert_combine") if rc else 0
 
 
 def osdp_expert_linear_workspace_bytes(T, top_k, E, N, K, act, op):
@@ -582,14 +594,14 @@ def osdp_expert_linear_workspace_bytes(T, top_k, E, N, K, act, op):
 
 def osdp_expert_linear_fwd(rows, plan, w_flat, w_offset, bias, T, top_k, E, N, K, act, out, z_save, ws, stream=None, check=False):
     wp, wn = _ws(ws)
-    rc = lib().osdp_expert_linear_fwd(_ptr(rows), _ptr(plan), _ptr(w_flat), w_offset, _ptr(bias), T, top_k, E, N, K, act, _ptr(out),
-                                      _ptr(z_save), wp, wn, _stream(stream))
-    return _ret(rc, check, "osdp_expert_linear_fwd")
+    rc = (_entry or _load_entry())(_LINEAR_FWD(5, _word(rows), _word(plan), _word(w_flat), w_offset, _word(bias), T, top_k, E, N, K, act, _word(out),
+                                               _word(z_save), wp or 0, wn, _stream(stream) or 0))
+    return _ret(rc, check, "osdp_expert_linear_fwd") if rc else 0
 
 
 def osdp_expert_linear_bwd(dy, rows, plan, w_flat, w_offset, z_saved, T, top_k, E, N, K, act, dx, dw_flat, dw_offset, dw_dtype, flags, dbias, ws,
                            stream=None, check=False):
     wp, wn = _ws(ws)
-    rc = lib().osdp_expert_linear_bwd(_ptr(dy), _ptr(rows), _ptr(plan), _ptr(w_flat), w_offset, _ptr(z_saved), T, top_k, E, N, K, act, _ptr(dx),
-                                      _ptr(dw_flat), dw_offset, dw_dtype, flags, _ptr(dbias), wp, wn, _stream(stream))
-    return _ret(rc, check, "osdp_expert_linear_bwd")
+    rc = (_entry or _load_entry())(_LINEAR_BWD(6, _word(dy), _word(rows), _word(plan), _word(w_flat), w_offset, _word(z_saved), T, top_k, E, N, K, act,
+                                               _word(dx), _word(dw_flat), dw_offset, dw_dtype, flags, _word(dbias), wp or 0, wn, _stream(stream) or 0))
+    return _ret(rc, check, "osdp_expert_linear_bwd") if rc else 0

@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libosdp.so")
 # Approximate functions and flushed denormals are fine for the GEMMs' epilogues; the optimiser's states, the norms'
 # statistics and the int8 scales are computed with IEEE division and square root.
 FAST_MATH_SOURCES = ["osdp_api.cu", "osdp_plan.cu", "osdp_experts.cu"]
-SOURCES = FAST_MATH_SOURCES + ["osdp_step.cu", "osdp_block_norm.cu", "osdp_i8.cu", "osdp_route.cu", "osdp_expert_few.cu"]
+SOURCES = FAST_MATH_SOURCES + ["osdp_step.cu", "osdp_block_norm.cu", "osdp_i8.cu", "osdp_route.cu", "osdp_expert_few.cu", "osdp_call.cu"]
 HEADERS = ["osdp_gemm.cuh", "osdp_aux.cuh", "osdp_vec.cuh", "osdp_internal.h", "osdp_i8.h", "osdp_experts.h",
            os.path.join("..", "..", "include", "osdp.h")]
 

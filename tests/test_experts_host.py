@@ -124,5 +124,20 @@ def test_mlp_module_refuses():
         m(torch.zeros(4, 16, dtype=torch.bfloat16), torch.zeros(4, 2), torch.zeros(4, 2, dtype=torch.int32))
 
 
+def test_calls_as_words():
+    """The binding packs its arguments; what the packed entry point itself refuses, and that integers are not cut."""
+    import struct
+    from paper_2209_13258_b200 import binding as B
+    call = B.lib().osdp_call
+    assert call(None) == NULL
+    for which in (-1, 7, 1 << 40):
+        assert call(struct.pack("=25q", which, *[0] * 24)) == UNSUPPORTED
+    assert route(k=(1 << 32) + 2) == SHAPE and route(score=1 << 32) == UNSUPPORTED and fwd(k=(1 << 32) + 2) == SHAPE and bwd(flags=1 << 32) == UNSUPPORTED
+    with pytest.raises(struct.error):
+        route(T=1 << 64)
+    with pytest.raises(P.OsdpError):
+        P.osdp_expert_plan(None, 4, 2, 8, A, A, stream=0, check=True)
+
+
 def test_rows_in_an_expert_order():
     assert P.EXPERT_ROWS == 64 and P.MAX_EXPERTS == 1024 and P.MAX_TOP_K == 16
