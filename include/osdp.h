@@ -489,7 +489,7 @@ int osdp_split_linear_fwd_i8(const void *x, const float *x_scale, const void *w8
  *
  * osdp_route_bwd: dlogits [T, E] (dtype of the logits, ld_dlogits elements from row to row, all of it written) from dweights
  * [T, top_k] fp32 and the idx of the forward.  The choice itself and the bias have no gradient.  An index outside 0 .. E - 1
- * counts as no choice, the same index twice as two choices. */
+ * counts as no choice, the same index twice as two choices.  dlogits must not overlap the logits. */
 #define OSDP_MAX_EXPERTS 1024
 #define OSDP_MAX_TOP_K 16
 int osdp_route_fwd(const void *logits, int64_t ld, int logits_dtype, const float *bias, int64_t T, int E, int top_k, int score,

@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(256, V <= 8 ? 4 : 1) route_fwd_kernel(const __
 // Backward of the routing.  Renormalised, with r_j = s_j / sum of the chosen s and g_j = scale dw_j:
 //   softmax: dl_j = r_j (g_j - sum_i g_i r_i);  sigmoid: the same times (1 - s_j);  other logits have no gradient.
 // Not renormalised: sigmoid dl_j = g_j s_j (1 - s_j);  softmax dl_e = s_e (g_e - sum_i g_i s_i) for every e (g_e = 0 where
-// the expert was not chosen), the one case that reads all logits.
+// the expert was not chosen), the one case that reads all logits: a kernel of its own.
 struct RouteBackArgs {
   RouteArgs r;
   const float *dweights;
@@ -384,6 +384,29 @@ struct RouteBackArgs {
 __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
 
+// The choices of a token: lane j < k has the j-th expert (-1: none) and g_j.
+template <typename L>
+__device__ __forceinline__ void load_choices(const RouteBackArgs &b, long long t, bool there, int lane, int &e, float &g) {
+  const RouteArgs &a = b.r;
+  e = lane < a.k && there ? a.idx[t * a.k + lane] : -1;
+  if (e < 0 || e >= a.E) e = -1;           // a choice that is none has no gradient
+  g = e >= 0 ? b.dweights[t * a.k + lane] * a.scale : 0.f;
+}
+// A token that was given the same expert twice: one gradient, the sum, on the lane that `first` names.
+__device__ __forceinline__ float sum_of_same(int k, int e, float d, int &first) {
+  float sum = 0.f;
+  first = 32;
+  for (int j = k - 1; j >= 0; --j) {
+    const int ej = __shfl_sync(ALL, e, j);
+    const float dj = __shfl_sync(ALL, d, j);
+    sum += ej == e ? dj : 0.f;
+    first = ej == e ? j : first;
+  }
+  return sum;
+}
+
+// The gradient is zero but for the chosen.  Bound by latency: choices, their logits, stores behind the zeros (16384 x 256 fp32
+// 7.5 us, floor 2.8; two tokens to a warp 8.9).
 template <typename L>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_bwd_kernel(const __grid_constant__ RouteBackArgs b) {
   pdl_launch_dependents();
@@ -392,71 +415,70 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_bwd_kernel(const __gri
   const long long t0 = (long long)blockIdx.x * ROUTE_WARPS, t = t0 + (threadIdx.x >> 5);
   L *out = static_cast<L *>(b.dlogits);
   pdl_wait();
-  const bool all = a.score == OSDP_SCORE_SOFTMAX && !a.renorm;
-  const bool on = lane < a.k && t < a.T;
-  int e = on ? a.idx[t * a.k + lane] : -1;
-  if (e < 0 || e >= a.E) e = -1;           // a choice that is none has no gradient
-  const float g = on && e >= 0 ? b.dweights[t * a.k + lane] * a.scale : 0.f;
-  const L *row = static_cast<const L *>(a.logits) + (t < a.T ? t : 0) * a.ld;
-  const float l = e >= 0 ? widen(row[e]) : -INFINITY;
-  if (!all) {
-    // eight whole rows are a multiple of 16 bytes
-    if (b.dense) {
-      const int rows = (int)min((long long)ROUTE_WARPS, a.T - t0);
-      const int bytes = rows * a.E * (int)sizeof(L);
-      char *base = reinterpret_cast<char *>(out + t0 * a.E);
-      for (int i = threadIdx.x * 16; i + 16 <= bytes; i += blockDim.x * 16) *reinterpret_cast<uint4 *>(base + i) = make_uint4(0u, 0u, 0u, 0u);
-      const int rest = bytes & ~15;
-      if (rest + (int)threadIdx.x * (int)sizeof(L) < bytes) put(reinterpret_cast<L *>(base + rest) + threadIdx.x, 0.f);
-    } else if (t < a.T) {
-      for (int i = lane; i < a.E; i += 32) put(out + t * b.ld_out + i, 0.f);
-    }
-    float d;
-    const float s = a.score == OSDP_SCORE_SIGMOID ? 1.0f / (1.0f + expf(-l)) : 0.f;
-    if (a.renorm) {
-      const float r = share_of(a, l, e >= 0, lane);
-      d = r * (g - warp_sum(e >= 0 ? g * r : 0.f)) * (1.0f - s);
-    } else {
-      d = g * s * (1.0f - s);
-    }
-    // a token that was given the same expert twice: one gradient, the sum
-    const uint32_t same = __match_any_sync(ALL, e);
-    float sum = 0.f;
-    for (int j = 0; j < a.k; ++j) {
-      const float dj = __shfl_sync(ALL, d, j);
-      sum += (same >> j) & 1u ? dj : 0.f;
-    }
-    __syncthreads();                       // the rows are clear
-    if (e >= 0 && lane == __ffs(same) - 1) put(out + t * b.ld_out + e, sum);
-    return;
+  int e, first;
+  float g;
+  load_choices<L>(b, t, t < a.T, lane, e, g);
+  const float l = e >= 0 ? widen(static_cast<const L *>(a.logits)[t * a.ld + e]) : -INFINITY;
+  // eight whole rows are a multiple of 16 bytes
+  if (b.dense) {
+    const int rows = (int)min((long long)ROUTE_WARPS, a.T - t0);
+    const int bytes = rows * a.E * (int)sizeof(L);
+    char *base = reinterpret_cast<char *>(out + t0 * a.E);
+    for (int i = threadIdx.x * 16; i + 16 <= bytes; i += blockDim.x * 16) *reinterpret_cast<uint4 *>(base + i) = make_uint4(0u, 0u, 0u, 0u);
+    const int rest = bytes & ~15;
+    if (rest + (int)threadIdx.x * (int)sizeof(L) < bytes) put(reinterpret_cast<L *>(base + rest) + threadIdx.x, 0.f);
+  } else if (t < a.T) {
+    for (int i = lane; i < a.E; i += 32) put(out + t * b.ld_out + i, 0.f);
   }
+  const float s = a.score == OSDP_SCORE_SIGMOID ? 1.0f / (1.0f + expf(-l)) : 0.f;
+  float d;
+  if (a.renorm) {
+    const float r = share_of(a, l, e >= 0, lane);
+    d = r * (g - warp_sum(e >= 0 ? g * r : 0.f)) * (1.0f - s);
+  } else {
+    d = g * s * (1.0f - s);
+  }
+  d = sum_of_same(a.k, e, d, first);
+  __syncthreads();                       // the rows are clear
+  if (e >= 0 && lane == first) put(out + t * b.ld_out + e, d);
+}
+
+// A softmax that is not renormalised: every logit has a gradient.  s_e (0 - mean) everywhere, then the chosen ones (16384 x 256
+// fp32 9.0 us, floor 5.3).
+template <typename L, int V>
+__global__ void __launch_bounds__(32 * ROUTE_WARPS) route_bwd_dense_kernel(const __grid_constant__ RouteBackArgs b) {
+  pdl_launch_dependents();
+  const RouteArgs &a = b.r;
+  const int lane = threadIdx.x & 31;
+  const long long t = (long long)blockIdx.x * ROUTE_WARPS + (threadIdx.x >> 5);
+  pdl_wait();
   if (t >= a.T) return;
-  float high = -INFINITY, total = 0.f;
-  {
-    uint32_t top = 0;
-    for (int i = lane; i < a.E; i += 32) top = max(top, key_of(widen(row[i])));
-    high = value_of(__reduce_max_sync(ALL, top));
-    for (int i = lane; i < a.E; i += 32) {
-      const float x = widen(row[i]);
-      total += x == -INFINITY ? 0.f : expf(x - high);
-    }
-    total = warp_sum(total);
+  const L *row = static_cast<const L *>(a.logits) + t * a.ld;
+  L *out = static_cast<L *>(b.dlogits) + t * b.ld_out;
+  float s[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) s[v] = v * 32 + lane < a.E ? widen(row[v * 32 + lane]) : -INFINITY;
+  int e, first;
+  float g;
+  load_choices<L>(b, t, true, lane, e, g);
+  const float l = e >= 0 ? widen(row[e]) : -INFINITY;
+  const float high = largest(s);
+  float total = 0.f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    s[v] = s[v] == -INFINITY ? 0.f : expf(s[v] - high);
+    total += s[v];
   }
+  total = warp_sum(total);
   const float inv = total == 0.f ? 0.f : 1.0f / total;
-  const float mean = warp_sum(e >= 0 && l != -INFINITY ? g * (expf(l - high) * inv) : 0.f);
-  for (int i0 = 0; i0 < a.E; i0 += 32) {
-    const int i = i0 + lane;
-    float ge = 0.f;
-    for (int j = 0; j < a.k; ++j) {
-      const int ej = __shfl_sync(ALL, e, j);
-      const float gj = __shfl_sync(ALL, g, j);
-      ge += ej == i ? gj : 0.f;
-    }
-    if (i < a.E) {
-      const float x = widen(row[i]);
-      put(out + t * b.ld_out + i, (x == -INFINITY ? 0.f : expf(x - high) * inv) * (ge - mean));
-    }
-  }
+  const float mine = l == -INFINITY ? 0.f : expf(l - high) * inv;
+  const float mean = warp_sum(e >= 0 ? g * mine : 0.f);
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+    if (v * 32 + lane < a.E) put(out + v * 32 + lane, s[v] * inv * (0.f - mean));
+  const float sum = sum_of_same(a.k, e, g, first);
+  __syncwarp();
+  if (e >= 0 && lane == first) put(out + e, mine * (sum - mean));
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -811,6 +833,22 @@ int launch_route(const RouteArgs &a, cudaStream_t stream) {
   return go(route_fwd_kernel<L, 32>);
 }
 
+template <typename L>
+int launch_route_bwd(const RouteBackArgs &b, cudaStream_t stream) {
+  const RouteArgs &a = b.r;
+  const dim3 block(32 * ROUTE_WARPS);
+  if (a.score != OSDP_SCORE_SOFTMAX || a.renorm)
+    return launch_overlapped(route_bwd_kernel<L>, dim3((unsigned)cdiv(a.T, ROUTE_WARPS)), block, 0, 1, stream, b);
+  const dim3 grid((unsigned)cdiv(a.T, ROUTE_WARPS));
+  auto go = [&](auto kernel) { return launch_overlapped(kernel, grid, block, 0, 1, stream, b); };
+  if (a.E <= 32) return go(route_bwd_dense_kernel<L, 1>);
+  if (a.E <= 64) return go(route_bwd_dense_kernel<L, 2>);
+  if (a.E <= 128) return go(route_bwd_dense_kernel<L, 4>);
+  if (a.E <= 256) return go(route_bwd_dense_kernel<L, 8>);
+  if (a.E <= 512) return go(route_bwd_dense_kernel<L, 16>);
+  return go(route_bwd_dense_kernel<L, 32>);
+}
+
 int check_rows(int64_t T, int top_k, int E, int64_t D) {
   const int rc = check_choices(T, top_k, E);
   if (rc) return rc;
@@ -870,9 +908,8 @@ extern "C" int osdp_route_bwd(const float *dweights, const void *logits, int64_t
   b.dlogits = dlogits;
   b.ld_out = (long long)ld_dlogits;
   b.dense = ld_dlogits == E && aligned_to(dlogits, 16) ? 1 : 0;
-  const dim3 grid((unsigned)cdiv(T, ROUTE_WARPS)), block(32 * ROUTE_WARPS);
-  if (logits_dtype == OSDP_DTYPE_FP32) return launch_overlapped(route_bwd_kernel<float>, grid, block, 0, 1, static_cast<cudaStream_t>(stream), b);
-  return launch_overlapped(route_bwd_kernel<__nv_bfloat16>, grid, block, 0, 1, static_cast<cudaStream_t>(stream), b);
+  return logits_dtype == OSDP_DTYPE_FP32 ? launch_route_bwd<float>(b, static_cast<cudaStream_t>(stream))
+                                         : launch_route_bwd<__nv_bfloat16>(b, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int osdp_expert_rows(int64_t T, int top_k, int E, int64_t *rows, int64_t *plan_ints) {
