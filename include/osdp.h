@@ -42,7 +42,7 @@
  *    few microseconds of enqueueing (the GPU work is not serialised).  Make the first call on a
  *    device outside any stream capture.  On the host, every thread that calls the library keeps a
  *    table of its most recent launches' prepared kernel parameters (encoded tensor maps, tile
- *    choice; about 0.4 MB per thread), so that a loop issuing the same calls step after step does
+ *    choice; about 0.5 MB per thread), so that a loop issuing the same calls step after step does
  *    not encode them again; it holds addresses and shapes only and never touches device memory.
  *  - bf16 tensors are row-major, 16-byte aligned; N and K must be multiples of 8.
  *  - W lives inside a flat bf16 parameter buffer `w_flat` at ELEMENT offset `w_offset`

@@ -254,10 +254,12 @@ int launch_expert_gemm(const ExpertGemm &c, cudaStream_t stream) {
     const int64_t full = n / tm + cdiv(used, 2), m = red ? cdiv(c.N, tm) * c.E : (full > used ? full : used);
     return m * cdiv(p.Q, bn);
   };
-  // CTA pairs on 256 rows where the experts fill most of such a tile, and there are tiles for a third of the SMs.
-  const bool pair = tiles(256, 256) >= sms / 3 && (red || n >= 160 * used);
+  // CTA pairs on 256 rows where the experts fill most of such a tile (a weight gradient: its matrix), and there are tiles for a third
+  // of the SMs; outputs of at most 128 columns take single CTAs, which waste half as much of a tile.
+  const bool narrow = p.Q <= 128;
+  const bool pair = !narrow && tiles(256, 256) >= sms / 3 && (red ? c.N > 128 : n >= 160 * used);
   int bn = 128;
-  if (pair || tiles(128, 256) >= (int64_t)sms * 4 / 5) bn = 256;
+  if (pair || (!narrow && tiles(128, 256) >= (int64_t)sms * 4 / 5)) bn = 256;
   const double len = red ? (double)n / (double)used : (double)p.R;
   if (pair && c.act == ACT_NONE) {
     // the wider tile: as for the other products (its epilogue does not overlap the next tile)
