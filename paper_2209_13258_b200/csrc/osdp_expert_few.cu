@@ -55,8 +55,10 @@ __global__ void __launch_bounds__(32 * WARPS, 1) expert_few_kernel(const __grid_
   const int group = warp / WK, wk = warp % WK, groups = WARPS / WK;
   pdl_wait();
   const int32_t *live = a.plan + plan_live(a.E), *offsets = a.plan + PLAN_OFFSETS, *counts = a.plan + plan_counts(a.E);
-  const int each = (N + ROWS - 1) / ROWS, units = a.plan[plan_n_live(a.E)] * each;
+  const int each = (N + ROWS - 1) / ROWS;
   const int first = (int)blockIdx.x + group * (int)gridDim.x, stride = groups * (int)gridDim.x;
+  // the first unit's expert and whether there is one: both looked up at once
+  const int first_e = live[min(first / each, a.E - 1)], units = a.plan[plan_n_live(a.E)] * each;
 
   const int all_stages = (K + KSTAGE - 1) / KSTAGE, share = (all_stages + WK - 1) / WK;
   const int k_first = wk * share * KSTAGE, n_st = min(max(all_stages - wk * share, 0), share);
@@ -65,14 +67,14 @@ __global__ void __launch_bounds__(32 * WARPS, 1) expert_few_kernel(const __grid_
   constexpr int COPIES = 4;                     // of 4 rows, 8 pieces of 16 bytes each
   const int c_row = lane >> 3, c_piece = lane & 7;
   const __nv_bfloat16 *f_w[COPIES];
-  auto f_rows = [&]() {       // rows past the end read the last one: in bounds, and their sums are not stored
+  auto f_rows = [&](bool start) {       // rows past the end read the last one: in bounds, and their sums are not stored
     if (f_unit >= units) return;
-    const int i = f_unit / each, e = live[i], n0 = (f_unit - i * each) * ROWS;
+    const int i = f_unit / each, e = start ? first_e : live[i], n0 = (f_unit - i * each) * ROWS;
     f_left = (counts[e] + SH::TOKENS - 1) / SH::TOKENS;
 #pragma unroll
     for (int n = 0; n < COPIES; ++n) f_w[n] = a.w + ((long long)e * N + min(n0 + n * 4 + c_row, N - 1)) * K + (k_first + c_piece * 8);
   };
-  f_rows();
+  f_rows(true);
   uint8_t *ring = smem + warp * (STAGES * STAGE);
   // 16-byte piece c of row r lies at place c ^ 4 (r & 1), so that the eight lanes that read together (two rows, four pieces
   // each) hit all banks
@@ -94,7 +96,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) expert_few_kernel(const __grid_
           for (int n = 0; n < COPIES; ++n) f_w[n] -= (n_st - 1) * KSTAGE;
         } else {
           f_unit += stride;
-          f_rows();
+          f_rows(false);
         }
       }
     }
