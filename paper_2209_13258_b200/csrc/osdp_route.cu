@@ -199,13 +199,13 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const L *row, const f
   const bool grouped = a.top_groups < a.groups, soft = a.score == OSDP_SCORE_SOFTMAX;
   uint32_t key[V], taken = ALL;
   float c[V];
-  float high = 0.f;
+  float slack = 0.f;                  // half units of 1 that a score with a bias may be off, beside those of itself
 #pragma unroll
   for (int v = 0; v < V; ++v) c[v] = l[v];                 // without a bias the scores are in the order of the logits
   if (a.bias || grouped) {
-    float s[V], far = 0.f;
+    float s[V], far = 0.f, inv = 1.f;
     if (soft) {
-      high = largest(l);
+      const float high = largest(l);
       float total = 0.f;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
@@ -213,7 +213,7 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const L *row, const f
         total += s[v];
       }
       total = warp_sum(total);
-      const float inv = total > 0.f ? fast_rcp(total) : total;       // (a row of minus infinities: all scores are zero)
+      inv = total > 0.f ? fast_rcp(total) : total;       // (a row of minus infinities: all scores are zero)
 #pragma unroll
       for (int v = 0; v < V; ++v) s[v] *= inv;
     } else {
@@ -227,6 +227,11 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const L *row, const f
         c[v] = s[v] += b;
         far = fmaxf(far, fabsf(b));
       }
+      far = __uint_as_float(__reduce_max_sync(ALL, __float_as_uint(far)));
+      // A sigmoid is off by 4.4 half units at most: s (1 - s) (1.5 |l| + 4) for its exponential, 3 s for sum and reciprocal.  A
+      // softmax by 46 of its own, of which `inv` is the largest: exponent 1.5 times its size, which e^-x more than takes back,
+      // exponential and reciprocal 4 each, its total up to 37.  The sum with the bias counts it once.
+      slack = far + (soft ? 46.0f * inv : 5.0f);
     }
     if (grouped) {
 #pragma unroll
@@ -238,7 +243,6 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const L *row, const f
       taken = choose_groups<float>(a, [&](int e) { return __uint_as_float(list[e]); }, lane, sum, in);
       const float last = value_of(~__reduce_max_sync(ALL, in ? ~key_of(sum) : 0u));
       const float next = value_of(__reduce_max_sync(ALL, (lane >> a.lanes_log2) < a.groups && !in ? key_of(sum) : 0x007FFFFFu));
-      far = __uint_as_float(__reduce_max_sync(ALL, __float_as_uint(far)));
       // Two sums of two scores.  A sigmoid is off by 4.4 half units of 1 at most, and the sums by theirs and the bias's; a softmax by
       // 128 of its own size (its exponent counts 1.5 times, and beyond 80 nothing is left of it).
       const float off = soft ? 256.0f * (fabsf(last) + 2.0f * far) : 24.0f + 4.0f * far + 2.0f * fabsf(last);
@@ -283,19 +287,15 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const L *row, const f
       }
     }
   };
-  // whether lane j's expert and the next lane's are too close to say: bits of lanes
+  // Whether lane j's expert and the next lane's are too close to say: bits of lanes.  How far a score may be off is a bound for the
+  // row, and grows with nothing but the score: where a gap is, it lies between all before it and all behind it, the experts
+  // that were never looked at among them.  The bits that the place took are 2 V half units of the score.
   auto close = [&](bool equal_too) {
-    float bj = 0.f, off = 0.f;
-    const float value = value_of(got & ~(uint32_t)(V - 1));
+    float bj = 0.f;
+    const float value = value_of(got & ~(uint32_t)(V - 1)), off = fmaf(a.bias ? 2.0f * V + 1.0f : 2.0f * V, fabsf(value), slack);
     if (mine >= 0) {
       lj = widen(row[mine]);
-      off = 2.0f * V * fabsf(value);                                          // the bits that the place took
-      if (a.bias) {
-        bj = a.bias[mine];
-        // the score (see above, here relative to itself; beyond 100 nothing is left of it) and its sum with the bias
-        const float s = fabsf(value - bj);
-        off += fabsf(value) + fabsf(bj) + (soft ? s * (1.5f * fminf(high - lj, 100.0f) + 46.0f) : s * ((1.0f - fminf(s, 1.0f) + 0.01f) * (1.5f * fminf(fabsf(lj), 100.0f) + 6.0f) + 6.0f));
-      }
+      if (a.bias) bj = a.bias[mine];
     }
     const int after = __shfl_down_sync(ALL, mine, 1);
     const float less = __shfl_down_sync(ALL, value, 1), less_off = __shfl_down_sync(ALL, off, 1), less_l = __shfl_down_sync(ALL, lj, 1),

@@ -103,6 +103,26 @@ def test_scores_that_fp32_cannot_tell_apart(score, groups, top, take):
     check(l, bias, 8, score, groups=groups, top=top, take=take)
 
 
+@pytest.mark.parametrize("E,k", [(8, 1), (64, 3), (256, 8), (1000, 16)])
+def test_scores_of_different_make_at_the_border(E, k):
+    """Scores that are nearly all bias beside scores that have none: their roundings differ by far, and a chain of near ties
+    may pass from one kind to the other."""
+    g = torch.Generator(device="cuda").manual_seed(E + k)
+    for turn in range(20):
+        l = 3.0 * torch.randn(64, E, device="cuda", generator=g)
+        l[:, turn % E] += 9.0                                    # one large share
+        s = torch.softmax(l.to(D64), 1)
+        bias = (0.5 - s.median(0)[0]).float()
+        bias[::2] = (s.max(1)[0].median() - s[:, ::2].median(0)[0]).float()
+        # logits such that a row's scores meet: l = log of what is missing to 0.5, one Newton step in 64 bits
+        near = (0.6 - bias.to(D64)).clamp_min(1e-9)
+        rows = torch.log(near / near.sum()).float().repeat(64, 1)
+        rows += 2.0 ** -22 * torch.randn(64, E, device="cuda", generator=g)
+        check(rows, bias, k, "softmax")
+        check(l, bias, k, "softmax", spread=80.0)
+        check(l, bias, k, "sigmoid", spread=80.0)
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("E,k,groups,top", [(32, 2, 1, 1), (64, 16, 4, 3), (128, 8, 1, 1), (1000, 5, 1, 1), (1024, 16, 32, 8)])
 def test_masked_experts_among_scores_that_fp32_cannot_tell_apart(score, E, k, groups, top):
