@@ -225,13 +225,12 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const L *row, const f
       for (int v = 0; v < V; ++v) {
         const float b = v * 32 + lane < a.E ? a.bias[v * 32 + lane] : 0.f;
         c[v] = s[v] += b;
-        far = fmaxf(far, fabsf(b));
+        far = fmaxf(far, fabsf(b) < 1e30f ? fabsf(b) : 0.f);           // (beyond, a bias is a mask: nothing is close to it)
       }
-      far = __uint_as_float(__reduce_max_sync(ALL, __float_as_uint(far)));
       // A sigmoid is off by 4.4 half units at most: s (1 - s) (1.5 |l| + 4) for its exponential, 3 s for sum and reciprocal.  A
       // softmax by 46 of its own, of which `inv` is the largest: exponent 1.5 times its size, which e^-x more than takes back,
-      // exponential and reciprocal 4 each, its total up to 37.  The sum with the bias counts it once.
-      slack = far + (soft ? 46.0f * inv : 5.0f);
+      // exponential and reciprocal 4 each, its total up to 37.  The sum with the bias adds one of its own.
+      slack = soft ? 46.0f * inv : 5.0f;
     }
     if (grouped) {
 #pragma unroll
@@ -243,6 +242,7 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const L *row, const f
       taken = choose_groups<float>(a, [&](int e) { return __uint_as_float(list[e]); }, lane, sum, in);
       const float last = value_of(~__reduce_max_sync(ALL, in ? ~key_of(sum) : 0u));
       const float next = value_of(__reduce_max_sync(ALL, (lane >> a.lanes_log2) < a.groups && !in ? key_of(sum) : 0x007FFFFFu));
+      far = __uint_as_float(__reduce_max_sync(ALL, __float_as_uint(far)));
       // Two sums of two scores.  A sigmoid is off by 4.4 half units of 1 at most, and the sums by theirs and the bias's; a softmax by
       // 128 of its own size (its exponent counts 1.5 times, and beyond 80 nothing is left of it).
       const float off = soft ? 256.0f * (fabsf(last) + 2.0f * far) : 24.0f + 4.0f * far + 2.0f * fabsf(last);

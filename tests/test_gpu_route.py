@@ -103,6 +103,19 @@ def test_scores_that_fp32_cannot_tell_apart(score, groups, top, take):
     check(l, bias, 8, score, groups=groups, top=top, take=take)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("groups,top,take", [(1, 1, 1), (8, 3, 2)])
+@pytest.mark.parametrize("mask", [-math.inf, torch.finfo(torch.float32).min, -1e9, 1e9])
+def test_experts_masked_by_the_bias(score, groups, top, take, mask):
+    g = torch.Generator(device="cuda").manual_seed(11)
+    l = torch.randn(300, 64, device="cuda", generator=g)
+    bias = 0.1 * torch.randn(64, device="cuda", generator=g)
+    for some in (slice(0, 64, 3), slice(5, 64), slice(0, 64), slice(7, 8)):
+        b = bias.clone()
+        b[some] = mask
+        check(l, b, 6, score, groups=groups, top=top, take=take)
+
+
 @pytest.mark.parametrize("E,k", [(8, 1), (64, 3), (256, 8), (1000, 16)])
 def test_scores_of_different_make_at_the_border(E, k):
     """Scores that are nearly all bias beside scores that have none: their roundings differ by far, and a chain of near ties
