@@ -290,7 +290,8 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const L *row, const f
   // Whether lane j's expert and the next lane's are too close to say: bits of lanes.  How far a score may be off is a bound for the
   // row, and grows with nothing but the score: where a gap is, it lies between all before it and all behind it, the experts
   // that were never looked at among them.  The bits that the place took are 2 V half units of the score.
-  auto close = [&](bool equal_too) {
+  // `unequal`: those of them that are not the same in exact arithmetic for having the same logit and the same bias.
+  auto close = [&](uint32_t &unequal) {
     float bj = 0.f;
     const float value = value_of(got & ~(uint32_t)(V - 1)), off = fmaf(a.bias ? 2.0f * V + 1.0f : 2.0f * V, fabsf(value), slack);
     if (mine >= 0) {
@@ -300,21 +301,27 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const L *row, const f
     const int after = __shfl_down_sync(ALL, mine, 1);
     const float less = __shfl_down_sync(ALL, value, 1), less_off = __shfl_down_sync(ALL, off, 1), less_l = __shfl_down_sync(ALL, lj, 1),
                 less_b = __shfl_down_sync(ALL, bj, 1);
-    // as close as that: the same in exact arithmetic only if it is the same logit and the same bias
-    return __ballot_sync(ALL, lane < 31 && mine >= 0 && after >= 0 && value - less <= HALF_ULP * (off + less_off) && (equal_too || lj != less_l || bj != less_b));
+    const bool near = lane < 31 && mine >= 0 && after >= 0 && value - less <= HALF_ULP * (off + less_off);
+    unequal = __ballot_sync(ALL, near && (lj != less_l || bj != less_b));
+    return __ballot_sync(ALL, near);
   };
   take(0, a.k + 1);     // one more than are wanted, to see how far away it is
-  if ((close(false) & ((1u << a.k) - 1u)) == 0) return;
-  // the candidates end at the first gap behind the last one wanted
+  uint32_t unequal;
+  if (((close(unequal) >> (a.k - 1)) & 1u) == 0 && (unequal & ((1u << a.k) - 1u)) == 0) return;
+  // The candidates end at the first gap behind the last one wanted.  (Also where it has an equal behind it: what comes after
+  // that one may be neither equal nor far away.)
   for (int many = a.k + 1; many < 32;) {
     const int more = min(many + 4, 32);
     take(many, more);
     many = more;
     const uint32_t there = __ballot_sync(ALL, mine >= 0);
-    const uint32_t gaps = ~close(true) & ~((1u << (a.k - 1)) - 1u) & (there >> 1);      // (the last candidate's gap is not known yet)
+    const uint32_t gaps = ~close(unequal) & ~((1u << (a.k - 1)) - 1u) & (there >> 1);      // (the last candidate's gap is not known yet)
     if (gaps || __popc(there) < many) {
-      exact_order(a, row, lane, gaps ? __ffs(gaps) - 1 : __popc(there) - 1, mine);
-      if (lane < a.k) lj = widen(row[mine]);
+      const int m = gaps ? __ffs(gaps) - 1 : __popc(there) - 1;
+      if (unequal & ((1u << m) - 1u)) {          // (equal ones are in order)
+        exact_order(a, row, lane, m, mine);
+        if (lane < a.k) lj = widen(row[mine]);
+      }
       return;
     }
   }

@@ -104,6 +104,20 @@ def test_scores_that_fp32_cannot_tell_apart(score, groups, top, take):
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("E,k,groups,top", [(300, 4, 3, 1), (256, 2, 1, 1), (60, 6, 1, 1), (1024, 16, 8, 2), (64, 8, 4, 3), (512, 1, 1, 1)])
+def test_equal_scores_among_near_ones(E, k, groups, top, dtype, score):
+    """Few different logits, and biases of some ten neighbouring numbers: an expert's equal may stand beside it and a better
+    one behind that."""
+    g = torch.Generator(device="cuda").manual_seed(E + k)
+    for turn in range(6):
+        l = (2.0 * torch.randn(400, E, device="cuda", generator=g)).round().div(2.0).to(dtype)
+        for bias in (0.5 - 1e-6 * torch.rand(E, device="cuda", generator=g), 2.0 ** -24 * torch.randint(0, 3, (E,), device="cuda", generator=g), None):
+            check(l if bias is not None else l + 2.0 ** -21 * torch.randint(0, 3, l.shape, device="cuda", generator=g).to(dtype), bias, k, score,
+                  groups=groups, top=top, take=1 + turn % 2)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("groups,top,take", [(1, 1, 1), (8, 3, 2)])
 @pytest.mark.parametrize("mask", [-math.inf, torch.finfo(torch.float32).min, -1e9, 1e9])
 def test_experts_masked_by_the_bias(score, groups, top, take, mask):
