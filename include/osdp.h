@@ -481,9 +481,11 @@ int osdp_split_linear_fwd_i8(const void *x, const float *x_scale, const void *w8
  *     n_groups > top_groups: the experts form n_groups groups of E / n_groups neighbours; a group's score is the sum of its
  *         group_take (1 or 2; 1 where a group is one expert) largest c, and only experts of the top_groups best groups may be chosen
  *     idx[t, j]: the top_k largest c in descending order;   weights[t, j] = scale * s_idx / (renorm ? sum of the chosen s : 1)
- * The choice is that of exact arithmetic; equal scores go to the lower index (groups likewise).  logits [T, E] bf16 or fp32,
- * ld elements from row to row; bias [E] fp32 or NULL; idx [T, top_k] int32, weights [T, top_k] fp32.
- * A logit of minus infinity has score 0 (also a row of nothing else), and a NaN is chosen as minus infinity is.  Renormalised
+ * The choice is that of c in 64 bits, and without a bias that of the logits, in whose order the scores are.  Of equal c the larger
+ * logit comes first (a sigmoid is 1 in 64 bits from a logit of 37 on), unless the bias is 2^20 or more in magnitude: a mask,
+ * behind which all are equal.  Then the lower index.  Groups go by their sums in 64 bits, equal ones by the lower index.
+ * logits [T, E] bf16 or fp32, ld elements from row to row; bias [E] fp32 or NULL; idx [T, top_k] int32, weights [T, top_k] fp32.
+ * A logit of minus infinity has score 0 (also a row of nothing else), and a c that is NaN counts as minus infinity.  Renormalised
  * weights depend on the chosen logits only, also where their scores leave fp32's range; if all of them are minus infinity the
  * weights are 0.  idx is always made of top_k different experts.  n_groups <= 32 divides E, top_groups * (E / n_groups) >= top_k.
  *

@@ -17,7 +17,7 @@ constexpr int ROUTE_WARPS = 8;
 // ------------------------------------------------------------------------------------------------
 // Routing.  One warp per token; lane l holds experts l, l + 32, ... in registers.
 //
-// The choice has to be the one of exact arithmetic: another expert is another result.  It is made twice at most.  First in
+// The choice has to be the one of 64 bits: another expert is another result.  It is made twice at most.  First in
 // fp32 with approximate scores: a key is the score's order-preserving bits with the place in the lane's registers in the lowest
 // ones, a lane sorts its keys once, and an expert is found by one maximum over the lanes' first keys.  Where two scores
 // that decide are closer than all these roundings (and are not the same logit with the same bias), the scores in question are
@@ -92,6 +92,16 @@ __device__ __forceinline__ float fast_exp(float x) {   // 2^-22 and the rounding
   return e;
 }
 
+constexpr float MASK_BIAS = 1048576.0f;
+struct Rank {
+  double key;
+  float then;
+  __device__ bool above(const Rank &o) const { return key > o.key || (key == o.key && then > o.then); }
+  __device__ bool same(const Rank &o) const { return key == o.key && then == o.then; }
+};
+__device__ __forceinline__ Rank shfl_rank(const Rank &r, int from) { return {__shfl_sync(ALL, r.key, from), __shfl_sync(ALL, r.then, from)}; }
+__device__ __forceinline__ Rank shfl_xor_rank(const Rank &r, int o) { return {__shfl_xor_sync(ALL, r.key, o), __shfl_xor_sync(ALL, r.then, o)}; }
+
 // The row's scores in fp64, one at a time.  Compact loops: they are cold when they are needed.
 template <typename L>
 struct Exact {
@@ -121,11 +131,14 @@ struct Exact {
     if (a.bias) s += (double)a.bias[e];
     return s == s ? s : -(double)INFINITY;
   }
-  // what experts are chosen by
-  __device__ double rank_by(int e) const {
-    if (a.bias) return score(e);
-    const double l = (double)widen(row[e]);
-    return l == l ? l : -(double)INFINITY;
+  // What experts are chosen by: the larger first number, of equal ones the larger second.  fp64's sigmoid is 1 from a logit of 37 on and
+  // its softmax 0 from 746 below the largest, so that scores of one bias can be equal where the logits, in whose order exact
+  // ones are, still differ.  A bias of 2^20 or more is a mask, behind which all are equal.
+  __device__ Rank rank_by(int e) const {
+    const float l = fmaxf(widen(row[e]), -INFINITY);
+    if (!a.bias) return {(double)l, 0.f};
+    const double s = score(e);
+    return {s, fabsf(a.bias[e]) < MASK_BIAS && s > -(double)INFINITY ? l : -INFINITY};
   }
 };
 
@@ -141,13 +154,13 @@ __device__ __noinline__ uint32_t exact_groups(const RouteArgs &a, const L *row, 
 template <typename L>
 __device__ __noinline__ void exact_order(const RouteArgs &a, const L *row, int lane, int m, int &mine) {
   const Exact<L> exact(a, row, lane);
-  const double key = lane <= m ? exact.rank_by(mine) : 0.0;
+  const Rank key = lane <= m ? exact.rank_by(mine) : Rank{0.0, 0.f};
   int rank = 0, from = 0;
 #pragma unroll 1
   for (int i = 0; i <= m; ++i) {
-    const double other = __shfl_sync(ALL, key, i);
+    const Rank other = shfl_rank(key, i);
     const int e = __shfl_sync(ALL, mine, i);
-    rank += other > key || (other == key && e < mine) ? 1 : 0;
+    rank += other.above(key) || (other.same(key) && e < mine) ? 1 : 0;
   }
 #pragma unroll 1
   for (int j = 0; j < a.k; ++j) {
@@ -161,27 +174,28 @@ __device__ __noinline__ void exact_order(const RouteArgs &a, const L *row, int l
 template <typename L>
 __device__ __noinline__ void exact_all(const RouteArgs &a, const L *row, uint32_t taken, int lane, int &mine) {
   const Exact<L> exact(a, row, lane);
-  double last = (double)INFINITY;
+  const Rank lowest{-(double)INFINITY, -INFINITY};
+  Rank last = lowest;
   int last_e = -1;
 #pragma unroll 1
   for (int j = 0; j < a.k; ++j) {     // the best of those behind the last one
-    double best = -(double)INFINITY;
+    Rank best = lowest;
     int best_e = 1 << 20;
 #pragma unroll 1
     for (int e = lane; e < a.E; e += 32) {
       if (!((taken >> (((uint32_t)e * a.magic >> 20) << a.lanes_log2)) & 1u)) continue;
-      const double x = exact.rank_by(e);
-      const bool behind = j == 0 || x < last || (x == last && e > last_e);
-      if (behind && (x > best || (x == best && e < best_e))) {
+      const Rank x = exact.rank_by(e);
+      const bool behind = j == 0 || last.above(x) || (last.same(x) && e > last_e);
+      if (behind && (x.above(best) || (x.same(best) && e < best_e))) {
         best = x;
         best_e = e;
       }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-      const double x = __shfl_xor_sync(ALL, best, o);
+      const Rank x = shfl_xor_rank(best, o);
       const int e = __shfl_xor_sync(ALL, best_e, o);
-      if (x > best || (x == best && e < best_e)) {
+      if (x.above(best) || (x.same(best) && e < best_e)) {
         best = x;
         best_e = e;
       }
@@ -290,7 +304,7 @@ __device__ __forceinline__ void choose(const RouteArgs &a, const L *row, const f
   // Whether lane j's expert and the next lane's are too close to say: bits of lanes.  How far a score may be off is a bound for the
   // row, and grows with nothing but the score: where a gap is, it lies between all before it and all behind it, the experts
   // that were never looked at among them.  The bits that the place took are 2 V half units of the score.
-  // `unequal`: those of them that are not the same in exact arithmetic for having the same logit and the same bias.
+  // `unequal`: those of them that are not the same anyway, for having the same logit and the same bias.
   auto close = [&](uint32_t &unequal) {
     float bj = 0.f;
     const float value = value_of(got & ~(uint32_t)(V - 1)), off = fmaf(a.bias ? 2.0f * V + 1.0f : 2.0f * V, fabsf(value), slack);
