@@ -452,13 +452,14 @@ __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_bwd_kernel(const __gri
   } else if (t < a.T) {
     for (int i = lane; i < a.E; i += 32) put(out + t * b.ld_out + i, 0.f);
   }
-  const float s = a.score == OSDP_SCORE_SIGMOID ? 1.0f / (1.0f + expf(-l)) : 0.f;
+  // 1 - s by its own formula: as a difference it loses the digits of a confident expert, and all of them from a logit of 17 on
+  const float rest = a.score == OSDP_SCORE_SIGMOID ? 1.0f / (1.0f + expf(l)) : 1.0f;
   float d;
   if (a.renorm) {
     const float r = share_of(a, l, e >= 0, lane);
-    d = r * (g - warp_sum(e >= 0 ? g * r : 0.f)) * (1.0f - s);
+    d = r * (g - warp_sum(e >= 0 ? g * r : 0.f)) * rest;
   } else {
-    d = g * s * (1.0f - s);
+    d = g * (1.0f / (1.0f + expf(-l))) * rest;
   }
   d = sum_of_same(a.k, e, d, first);
   __syncthreads();                       // the rows are clear
