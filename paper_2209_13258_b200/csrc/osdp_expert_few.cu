@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) expert_few_kernel(const __grid_
               const float s = acc[t][j] + (bias ? bias[n] : 0.f);
               const long long at = (off + t0 + tok) * N + n;
               if (a.z) a.z[at] = __float2bfloat16_rn(s);
-              a.out[at] = __float2bfloat16_rn(gelu1(s, a.act));
+              a.out[at] = __float2bfloat16_rn(expert_gelu1(s, a.act));
             }
           }
         continue;
@@ -192,7 +192,7 @@ __global__ void __launch_bounds__(32 * WARPS, 1) expert_few_kernel(const __grid_
           if (bias) s += bias[n];
           const long long at = (off + t0 + o / ROWS) * N + n;
           if (a.z) a.z[at] = __float2bfloat16_rn(s);
-          a.out[at] = __float2bfloat16_rn(gelu1(s, a.act));
+          a.out[at] = __float2bfloat16_rn(expert_gelu1(s, a.act));
         }
       }
     }

@@ -753,15 +753,29 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float (&f)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The tanh form, two elements in an instruction where there is one.
-__device__ __forceinline__ void gelu_tanh_pairs(float (&f)[8]) {
+// The experts' activation, expert_gelu1's operations; the tanh form two elements in an instruction where there is one.
+// (tanh.approx would take one special function in place of two, but its 2^-11 are of 1 + tanh's terms, not of the sum:
+// at -3 a fifth of the output.)
+__device__ __forceinline__ void expert_gelu_array(float (&f)[8], int act) {
+  if (act == ACT_GELU_TANH) {
+    constexpr float k = -2.0f * 1.4426950408889634f * 0.7978845608028654f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const f2 x = pack2(f[2 * j], f[2 * j + 1]), half = mul2(x, both(0.5f));
-    const float2 u = split2(mul2(x, fma2(mul2(x, x), both(0.7978845608028654f * 0.044715f), both(0.7978845608028654f))));
-    const float2 y = split2(fma2(half, pack2(tanh_fast(u.x), tanh_fast(u.y)), half));
-    f[2 * j] = y.x;
-    f[2 * j + 1] = y.y;
+    for (int j = 0; j < 4; ++j) {
+      const f2 x = pack2(f[2 * j], f[2 * j + 1]);
+      const float2 arg = split2(mul2(x, fma2(mul2(x, x), both(k * 0.044715f), both(k))));
+      float e0, e1, h0, h1;
+      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(arg.x));
+      asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(arg.y));
+      const float2 d = split2(add2(both(1.0f), pack2(e0, e1)));
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(h0) : "f"(d.x));
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(h1) : "f"(d.y));
+      const float2 y = split2(mul2(x, pack2(h0, h1)));
+      f[2 * j] = y.x;
+      f[2 * j + 1] = y.y;
+    }
+  } else if (act == ACT_GELU_ERF) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = expert_gelu1(f[j], ACT_GELU_ERF);
   }
 }
 // 32 accumulators -> bf16, or zeros
@@ -1570,7 +1584,7 @@ __global__ void __launch_bounds__((BN > 256 || HEAVY) ? 384 : 256, 1) gemm_kerne
 #pragma unroll
               for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(v[g * 8 + j]);
               if (I8) gelu1_array(f, p.epi.act);
-              else if (GRP != GRP_NONE && p.epi.act == ACT_GELU_TANH) gelu_tanh_pairs(f);
+              else if (GRP != GRP_NONE) expert_gelu_array(f, p.epi.act);
               else gelu_array(f, p.epi.act);
               packed[g] = pack_bf16x8(f);
               if (empty_row) packed[g] = make_uint4(0u, 0u, 0u, 0u);

@@ -255,6 +255,13 @@ __device__ __forceinline__ float gelu1(float x, int act) {
   return x;
 }
 
+// The same for the experts' products, whose erf form keeps the digits of a small output too: 1 + erf(y) = erfc(-y).  Both of their
+// kernels have it, so that a token's activation does not depend on how many tokens come with it.
+__device__ __forceinline__ float expert_gelu1(float x, int act) {
+  if (act == 2) return __fmul_rn(__fmul_rn(0.5f, x), erfcf(__fmul_rn(x, -0.7071067811865476f)));
+  return gelu1(x, act);
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
