@@ -588,7 +588,8 @@ class _RouteFn(torch.autograd.Function):
         dt = B.DTYPE_FP32 if logits.dtype is torch.float32 else B.DTYPE_BF16
         B.osdp_route_fwd(logits, max(logits.stride(0), E), dt, router.bias, T, E, k, router.score, router.groups, router.top_groups,
                          router.group_take, router.renormalise, router.scale, idx, weights, check=True)
-        ctx.router = router
+        # what this forward did: a schedule may change the module before the backward
+        ctx.did = router.score, router.renormalise, router.scale
         ctx.save_for_backward(logits, idx)
         ctx.mark_non_differentiable(idx)
         ctx.set_materialize_grads(False)
@@ -599,12 +600,12 @@ class _RouteFn(torch.autograd.Function):
     def backward(ctx, dweights, _):
         if dweights is None:
             return None, None
-        r = ctx.router
+        score, renormalise, scale = ctx.did
         logits, idx = ctx.saved_tensors
         T, E = logits.shape
         out = torch.empty(T, E, dtype=logits.dtype, device=logits.device)
         dt = B.DTYPE_FP32 if logits.dtype is torch.float32 else B.DTYPE_BF16
-        B.osdp_route_bwd(dweights.contiguous(), logits, max(logits.stride(0), E), dt, idx, T, E, r.top_k, r.score, r.renormalise, r.scale, out, E,
+        B.osdp_route_bwd(dweights.contiguous(), logits, max(logits.stride(0), E), dt, idx, T, E, idx.shape[1], score, renormalise, scale, out, E,
                          check=True)
         return out, None
 
@@ -667,23 +668,23 @@ class _ExpertMLPFn(torch.autograd.Function):
         if rc:
             raise B.OsdpError(rc, "osdp_expert_rows")
         plan, pos = torch.empty(ints, dtype=torch.int32, device=dev), torch.empty(T, k, dtype=torch.int32, device=dev)
-        stream, status = B._stream(None), layer._status
+        stream, status, act = B._stream(None), layer._status, layer.act
         B.osdp_expert_plan(idx, T, k, E, plan, pos, stream, True)
         xs, h, y, out = new(R, H), new(R, F), new(R, H), new(T, H)
-        z = new(R, F) if need and layer.act != B.ACT_NONE else None
+        z = new(R, F) if need and act != B.ACT_NONE else None
         B.osdp_expert_dispatch(x, plan, pos, None, None, T, k, E, H, xs, None, stream, True)
-        B.osdp_expert_linear_fwd(xs, plan, flat, layer.off_w1, b1, T, k, E, F, H, layer.act, h, z, status, stream, True)
+        B.osdp_expert_linear_fwd(xs, plan, flat, layer.off_w1, b1, T, k, E, F, H, act, h, z, status, stream, True)
         B.osdp_expert_linear_fwd(h, plan, flat, layer.off_w2, b2, T, k, E, H, F, B.ACT_NONE, y, None, status, stream, True)
         B.osdp_expert_combine(y, plan, pos, weights, T, k, E, H, out, stream, True)
         if need:
-            ctx.layer = layer
+            ctx.layer, ctx.act = layer, act
             ctx.save_for_backward(weights, flat, plan, pos, xs, z, h, y)
         return out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dout):
-        layer = ctx.layer
+        layer, act = ctx.layer, ctx.act
         weights, flat, plan, pos, xs, z, h, y = ctx.saved_tensors
         E, H, F, T, k = layer.experts, layer.hidden, layer.ffn, pos.shape[0], pos.shape[1]
         need_x, need_w, need_flat, need_b1, need_b2 = ctx.needs_input_grad[:5]
@@ -699,7 +700,7 @@ class _ExpertMLPFn(torch.autograd.Function):
         dh, dxs = new(first, half, R, F), new(need_x, half, R, H)
         db1, db2, dx = new(need_b1, full, E, F), new(need_b2, full, E, H), new(need_x, half, T, H)
         bytes2 = B.osdp_expert_linear_workspace_bytes(T, k, E, H, F, B.ACT_NONE, B.OP_LINEAR_BWD)[1]
-        bytes1 = B.osdp_expert_linear_workspace_bytes(T, k, E, F, H, layer.act, B.OP_LINEAR_BWD)[1]
+        bytes1 = B.osdp_expert_linear_workspace_bytes(T, k, E, F, H, act, B.OP_LINEAR_BWD)[1]
         # this call's own: a backward on another stream may run at the same time, a captured one keeps its own
         ws = torch.empty(max(bytes1, bytes2), dtype=torch.uint8, device=dev)
         ws[:256].zero_()
@@ -707,7 +708,7 @@ class _ExpertMLPFn(torch.autograd.Function):
             B.osdp_expert_linear_bwd(dys, h, plan, flat, layer.off_w2, None, T, k, E, H, F, B.ACT_NONE, dh, dflat, layer.off_w2, B.DTYPE_BF16, 0, db2, ws,
                                      stream, True)
         if first:
-            B.osdp_expert_linear_bwd(dh, xs, plan, flat, layer.off_w1, z, T, k, E, F, H, layer.act, dxs, dflat, layer.off_w1, B.DTYPE_BF16, 0, db1, ws,
+            B.osdp_expert_linear_bwd(dh, xs, plan, flat, layer.off_w1, z, T, k, E, F, H, act, dxs, dflat, layer.off_w1, B.DTYPE_BF16, 0, db1, ws,
                                      stream, True)
         if need_x:
             B.osdp_expert_combine(dxs, plan, pos, None, T, k, E, H, dx, stream, True)
