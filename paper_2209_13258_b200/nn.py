@@ -661,7 +661,7 @@ class _ExpertMLPFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weights, flat, b1, b2, idx, layer):
         E, H, F, T, k = layer.experts, layer.hidden, layer.ffn, idx.shape[0], idx.shape[1]
-        need = any(ctx.needs_input_grad)
+        need_x, need_w, need_flat, need_b1 = ctx.needs_input_grad[:4]
         dev = x.device
         new = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device=dev)     # noqa: E731
         rc, R, ints = B.osdp_expert_rows(T, k, E)
@@ -671,14 +671,15 @@ class _ExpertMLPFn(torch.autograd.Function):
         stream, status, act = B._stream(None), layer._status, layer.act
         B.osdp_expert_plan(idx, T, k, E, plan, pos, stream, True)
         xs, h, y, out = new(R, H), new(R, F), new(R, H), new(T, H)
-        z = new(R, F) if need and act != B.ACT_NONE else None
+        z = new(R, F) if (need_x or need_flat or need_b1) and act != B.ACT_NONE else None
         B.osdp_expert_dispatch(x, plan, pos, None, None, T, k, E, H, xs, None, stream, True)
         B.osdp_expert_linear_fwd(xs, plan, flat, layer.off_w1, b1, T, k, E, F, H, act, h, z, status, stream, True)
         B.osdp_expert_linear_fwd(h, plan, flat, layer.off_w2, b2, T, k, E, H, F, B.ACT_NONE, y, None, status, stream, True)
         B.osdp_expert_combine(y, plan, pos, weights, T, k, E, H, out, stream, True)
-        if need:
-            ctx.layer, ctx.act = layer, act
-            ctx.save_for_backward(weights, flat, plan, pos, xs, z, h, y)
+        if any(ctx.needs_input_grad):
+            # each product's rows for its weights' gradient alone, the combined ones for that of the tokens' weights
+            ctx.layer, ctx.act, ctx.rows = layer, act, R
+            ctx.save_for_backward(weights, flat, plan, pos, xs if need_flat else None, z, h if need_flat else None, y if need_w else None)
         return out
 
     @staticmethod
@@ -691,10 +692,10 @@ class _ExpertMLPFn(torch.autograd.Function):
         dev = dout.device
         new = lambda on, dtype, *shape: torch.empty(shape, dtype=dtype, device=dev) if on else None      # noqa: E731
         half, full = torch.bfloat16, torch.float32
-        R = xs.shape[0]
+        R = ctx.rows
         dys, dw = new(True, half, R, H), new(need_w, full, T, k)
         stream = B._stream(None)
-        B.osdp_expert_dispatch(dout.contiguous(), plan, pos, weights, y if need_w else None, T, k, E, H, dys, dw, stream, True)
+        B.osdp_expert_dispatch(dout.contiguous(), plan, pos, weights, y, T, k, E, H, dys, dw, stream, True)
         first = need_x or need_flat or need_b1             # something before the second product has a gradient
         dflat = torch.empty_like(flat) if need_flat else None           # both products' gradients fill it
         dh, dxs = new(first, half, R, F), new(need_x, half, R, H)

@@ -41,3 +41,30 @@ def test_an_activation_changed_after_the_forward():
         m.act = act
         grads.append(torch.autograd.grad(out.float().square().sum(), [x, w, m.flat_param]))
     assert all(torch.equal(a, b) for a, b in zip(*grads))
+
+
+def kept(m, *args):
+    """Bytes of what the forward keeps for the backward, inputs and parameters aside."""
+    seen = {}
+    known = {t.untyped_storage().data_ptr() for t in (*args, *m.parameters())}
+
+    def pack(t):
+        if t.untyped_storage().data_ptr() not in known:
+            seen[t.untyped_storage().data_ptr()] = t.untyped_storage().nbytes()
+        return t
+    with torch.autograd.graph.saved_tensors_hooks(pack, lambda t: t):
+        out = m(*args)
+    out.float().sum().backward()
+    return sum(seen.values())
+
+
+def test_only_what_the_gradients_need_is_kept():
+    torch.manual_seed(3)
+    m = ExpertMLP(64, 128, 4)
+    x, w, i = batch(T=500)
+    rows = P.osdp_expert_rows(500, 2, 4)[1]
+    whole = kept(m, x, w, i)
+    assert whole - kept(m, x, w.detach(), i) == rows * 64 * 2               # the combined rows: the gradient of the weights
+    m.flat_param.requires_grad_(False)
+    assert whole - kept(m, x, w, i) == rows * (64 + 128) * 2                # both products' rows: the experts' gradients
+    assert x.grad is not None and m.b1.grad is not None and m.flat_param.grad is not None
