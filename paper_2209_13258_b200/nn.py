@@ -697,7 +697,10 @@ class _ExpertMLPFn(torch.autograd.Function):
         stream = B._stream(None)
         B.osdp_expert_dispatch(dout.contiguous(), plan, pos, weights, y, T, k, E, H, dys, dw, stream, True)
         first = need_x or need_flat or need_b1             # something before the second product has a gradient
-        dflat = torch.empty_like(flat) if need_flat else None           # both products' gradients fill it
+        # both products' gradients fill it; what a larger buffer holds behind the experts has none
+        dflat = torch.empty_like(flat) if need_flat else None
+        if need_flat and flat.numel() > 2 * layer.off_w2:
+            dflat.view(-1)[2 * layer.off_w2:].zero_()
         dh, dxs = new(first, half, R, F), new(need_x, half, R, H)
         db1, db2, dx = new(need_b1, full, E, F), new(need_b2, full, E, H), new(need_x, half, T, H)
         bytes2 = B.osdp_expert_linear_workspace_bytes(T, k, E, H, F, B.ACT_NONE, B.OP_LINEAR_BWD)[1]

@@ -68,3 +68,15 @@ def test_only_what_the_gradients_need_is_kept():
     m.flat_param.requires_grad_(False)
     assert whole - kept(m, x, w, i) == rows * (64 + 128) * 2                # both products' rows: the experts' gradients
     assert x.grad is not None and m.b1.grad is not None and m.flat_param.grad is not None
+
+
+def test_a_larger_flat_buffer_has_a_gradient_of_zeros_behind_the_experts():
+    torch.manual_seed(4)
+    m = ExpertMLP(64, 128, 4)
+    n = m.flat_param.numel()
+    filled = torch.full((4 * n,), 7.0, dtype=BF16, device="cuda")      # what a new allocation may find
+    del filled
+    m.flat_param.data = torch.cat([m.flat_param.data, torch.ones(3 * n, dtype=BF16, device="cuda")])
+    x, w, i = batch()
+    m(x, w, i).float().sum().backward()
+    assert m.flat_param.grad.shape == (4 * n,) and bool((m.flat_param.grad[n:] == 0).all()) and bool((m.flat_param.grad[:n] != 0).any())
