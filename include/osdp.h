@@ -533,8 +533,9 @@ int osdp_expert_combine(const void *rows, const int32_t *plan, const int32_t *po
  * Rows between the experts: written as zeros; `rows` and dy have to be finite there and one of the two zero, as every call here
  * leaves them.  dbias is summed from the unrounded G, in a fixed order; no atomics anywhere: the same call gives the same bits.
  * The host does not learn how many rows an expert has: nothing synchronises, and a captured call follows the plan's
- * contents.  ws: osdp_expert_linear_workspace_bytes(...) bytes (op OSDP_OP_LINEAR_FWD or _BWD), its first 256 zeroed once; no
- * two calls that may run at the same time may share it. */
+ * contents.  ws: osdp_expert_linear_workspace_bytes(...) bytes (op OSDP_OP_LINEAR_FWD or _BWD), its first 256 zeroed once.  Forward
+ * calls use these 256 bytes only, for the status word, and may share them; a backward's workspace belongs to one call at a time.
+ * No output may overlap an input, or another output. */
 int osdp_expert_linear_workspace_bytes(int64_t T, int top_k, int E, int64_t N, int64_t K, int act, int op, size_t *bytes);
 int osdp_expert_linear_fwd(const void *rows, const int32_t *plan, const void *w_flat, int64_t w_offset, const float *bias, int64_t T,
                            int top_k, int E, int64_t N, int64_t K, int act, void *out, void *z_save, void *ws, size_t ws_bytes, void *stream);
@@ -562,6 +563,11 @@ int osdp_call(const void *words);
  * inside a kernel ran out) and clears it.  Every device-side wait in this library is bounded; none can
  * hang the GPU.  This is the one call that synchronises. */
 int osdp_read_device_status(void *ws, int *status, void *stream);
+
+/* The status word at the start of `ws`, if it is set, goes into the one at the start of `into` (kept if that is set already): for
+ * callers whose workspaces do not outlive the call, several of which may be joined into one word at the same time.
+ * Asynchronous on `stream`. */
+int osdp_join_status(const void *ws, void *into, void *stream);
 
 /* Diagnostic for the failure-detection path (no counterpart in the paper): launches one warp that
  * waits, with the bounded wait every kernel of this library uses, on a barrier nothing signals.

@@ -10,7 +10,7 @@ from .binding import (  # noqa: F401
     osdp_last_cuda_error, osdp_read_device_status, osdp_slice_range, osdp_split_linear_bwd,
     osdp_split_linear_bwd_slice, osdp_split_linear_fwd, osdp_split_linear_fwd_slice,
     osdp_split_linear_workspace_bytes, osdp_split_mlp_bwd, osdp_split_mlp_fwd, osdp_status_string,
-    osdp_version, new_workspace, osdp_bias_grad_noalloc, osdp_debug_wait_probe, osdp_suggest_granularity,
+    osdp_version, new_workspace, osdp_bias_grad_noalloc, osdp_debug_wait_probe, osdp_join_status, osdp_suggest_granularity,
     osdp_zdp_shard_layout, osdp_zdp_linear_fwd_slice, osdp_zdp_linear_bwd_slice,
     osdp_plan_cost, osdp_plan_search, osdp_plan_expand_slices, osdp_plan_search_granularity,
     osdp_split_linear_fwd_f8, osdp_split_linear_bwd_f8, osdp_zdp_linear_bwd_slice_scatter,

@@ -27,7 +27,7 @@ EXPORTS = [
     "osdp_version", "osdp_status_string", "osdp_last_cuda_error", "osdp_slice_range",
     "osdp_split_linear_workspace_bytes", "osdp_split_linear_fwd", "osdp_split_linear_fwd_slice",
     "osdp_split_linear_bwd", "osdp_split_linear_bwd_slice", "osdp_split_mlp_fwd", "osdp_split_mlp_bwd",
-    "osdp_read_device_status", "osdp_bias_grad_noalloc", "osdp_debug_wait_probe", "osdp_suggest_granularity",
+    "osdp_read_device_status", "osdp_join_status", "osdp_bias_grad_noalloc", "osdp_debug_wait_probe", "osdp_suggest_granularity",
     "osdp_zdp_shard_layout", "osdp_zdp_linear_fwd_slice", "osdp_zdp_linear_bwd_slice",
     "osdp_plan_cost", "osdp_plan_search", "osdp_plan_expand_slices", "osdp_plan_search_granularity",
     "osdp_split_linear_fwd_f8", "osdp_split_linear_bwd_f8", "osdp_zdp_linear_bwd_slice_scatter",
@@ -89,6 +89,7 @@ def lib():
                                          ci, vp, vp, vp, sz, vp]
         L.osdp_read_device_status.argtypes = [vp, ctypes.POINTER(ci), vp]
         L.osdp_bias_grad_noalloc.argtypes = [vp, i64, i64, vp, vp]
+        L.osdp_join_status.argtypes = [vp, vp, vp]
         L.osdp_debug_wait_probe.argtypes = [vp, i64, vp]
         L.osdp_suggest_granularity.argtypes = [i64, i64, i64, ci, ci, ci, ci, sz, ci, ctypes.POINTER(ci)]
         p64 = ctypes.POINTER(i64)
@@ -273,6 +274,12 @@ def osdp_read_device_status(ws, stream=None):
     st = ctypes.c_int(0)
     rc = lib().osdp_read_device_status(wp, ctypes.byref(st), _stream(stream))
     return rc, st.value
+
+
+def osdp_join_status(ws, into, stream=None, check=False):
+    """The status word of `ws`, if it is set, goes into that of `into`."""
+    rc = lib().osdp_join_status(_ws(ws)[0], _ws(into)[0], _stream(stream))
+    return _ret(rc, check, "osdp_join_status")
 
 
 def osdp_bias_grad_noalloc(dy, M, N, dbias, stream=None, check=False):

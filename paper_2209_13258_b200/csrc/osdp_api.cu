@@ -1134,6 +1134,15 @@ int bwd_impl(const void *dy, const void *x, const void *w_flat, int64_t w_offset
 // C ABI
 
 // What the other translation units of the library need from this one (osdp_internal.h).
+namespace {
+// Several of these may run at once for the same `into`: a mark is never written over.
+__global__ void join_status_kernel(const int *ws, int *into) {
+  pdl_launch_dependents();
+  pdl_wait();
+  if (threadIdx.x == 0 && *ws != 0) atomicCAS(into, 0, *ws);
+}
+}  // namespace
+
 namespace osdp {
 int report_cuda(cudaError_t e) { return e == cudaSuccess ? OSDP_OK : cuda_fail(e); }
 int sm_count(int *sms) { return device_sms(sms); }
@@ -1727,6 +1736,13 @@ int osdp_zdp_mlp_bwd_slice(const void *dy, const void *x, const void *w1_slice, 
   return mlp_bwd_impl(dy, x, w1_slice, 0, b1, 0, z1_saved, M, hidden, ffn, k_split, act, dx,
                       want_dw ? const_cast<void *>(w1_slice) : nullptr, 0, 0, dw_dtype, flags, db1, db2, ws, ws_bytes,
                       stream, &cs);
+}
+
+int osdp_join_status(const void *ws, void *into, void *stream) {
+  if (!ws || !into) return OSDP_ERR_NULL_POINTER;
+  if (!aligned_to(ws, 4) || !aligned_to(into, 4)) return OSDP_ERR_ALIGNMENT;
+  return launch_overlapped(join_status_kernel, dim3(1), dim3(32), 0, 1, static_cast<cudaStream_t>(stream), static_cast<const int *>(ws),
+                           static_cast<int *>(into));
 }
 
 int osdp_debug_wait_probe(void *ws, int64_t limit_us, void *stream_) {

@@ -678,7 +678,7 @@ class _ExpertMLPFn(torch.autograd.Function):
         B.osdp_expert_combine(y, plan, pos, weights, T, k, E, H, out, stream, True)
         if any(ctx.needs_input_grad):
             # each product's rows for its weights' gradient alone, the combined ones for that of the tokens' weights
-            ctx.layer, ctx.act, ctx.rows = layer, act, R
+            ctx.layer, ctx.act, ctx.rows, ctx.status = layer, act, R, status
             ctx.save_for_backward(weights, flat, plan, pos, xs if need_flat else None, z, h if need_flat else None, y if need_w else None)
         return out
 
@@ -714,6 +714,8 @@ class _ExpertMLPFn(torch.autograd.Function):
         if first:
             B.osdp_expert_linear_bwd(dh, xs, plan, flat, layer.off_w1, z, T, k, E, F, H, act, dxs, dflat, layer.off_w1, B.DTYPE_BF16, 0, db1, ws,
                                      stream, True)
+        if first or need_b2:
+            B.osdp_join_status(ws, ctx.status, stream, True)        # the workspace goes, a wait that ran out stays known
         if need_x:
             B.osdp_expert_combine(dxs, plan, pos, None, T, k, E, H, dx, stream, True)
         return dx, dw, dflat, db1, db2, None, None
@@ -741,7 +743,7 @@ class ExpertMLP(torch.nn.Module):
         self.flat_param = torch.nn.Parameter(w)
         mk = lambda n: torch.nn.Parameter(torch.zeros(self.experts, n, dtype=torch.float32, device=device)) if bias else None      # noqa: E731
         self.b1, self.b2 = mk(self.ffn), mk(self.hidden)
-        # the tile kernels' status word: all that is kept between calls
+        # the tile kernels' status word, forward and backward: all that is kept between calls
         self.register_buffer("_status", torch.zeros(256, dtype=torch.uint8, device=device), persistent=False)
         rc, _ = B.osdp_expert_linear_workspace_bytes(1, 1, self.experts, self.ffn, self.hidden, self.act, B.OP_LINEAR_BWD)
         if rc:

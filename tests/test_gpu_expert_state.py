@@ -1,12 +1,14 @@
-"""What the mixture-of-experts modules keep between forward and backward."""
+"""What the mixture-of-experts modules keep between forward and backward, and what is left of a wait that ran out."""
 import pytest
 import torch
 
 import paper_2209_13258_b200 as P
+from paper_2209_13258_b200 import binding as B
 from paper_2209_13258_b200.nn import ExpertMLP, ExpertRouter
 
 pytestmark = pytest.mark.gpu
 BF16 = torch.bfloat16
+TIMEOUT = 8
 
 
 def batch(T=60, H=64, E=4, k=2, grad=True):
@@ -80,3 +82,37 @@ def test_a_larger_flat_buffer_has_a_gradient_of_zeros_behind_the_experts():
     x, w, i = batch()
     m(x, w, i).float().sum().backward()
     assert m.flat_param.grad.shape == (4 * n,) and bool((m.flat_param.grad[n:] == 0).all()) and bool((m.flat_param.grad[:n] != 0).any())
+
+
+def test_a_wait_that_runs_out_in_the_backward_leaves_its_trace(monkeypatch):
+    """The module's status word has it, as it has the forward's; it is cleared by being read."""
+    torch.manual_seed(5)
+    m = ExpertMLP(64, 128, 4)
+    x, w, i = batch()
+    read = lambda: P.osdp_read_device_status(m._status)                                              # noqa: E731
+    m(x, w, i).float().sum().backward()
+    assert read() == (0, 0)
+    call = B.osdp_expert_linear_bwd
+    for which in (0, 1):                    # each of the backward's two products
+        calls = []
+
+        def broken(*args):
+            rc = call(*args)
+            if len(calls) == which:         # ws, stream, check come last
+                P.osdp_debug_wait_probe(args[-3], 1000, args[-2])
+            calls.append(rc)
+            return rc
+        monkeypatch.setattr(B, "osdp_expert_linear_bwd", broken)
+        m(x, w, i).float().sum().backward()
+        monkeypatch.setattr(B, "osdp_expert_linear_bwd", call)
+        assert len(calls) == 2 and read() == (0, TIMEOUT) and read() == (0, 0)
+
+
+def test_status_words_meet():
+    a, b = P.new_workspace(256), P.new_workspace(256)
+    P.osdp_join_status(a, b, check=True)
+    assert P.osdp_read_device_status(b) == (0, 0)
+    P.osdp_debug_wait_probe(a, 1000)
+    P.osdp_join_status(a, b, check=True)
+    P.osdp_join_status(P.new_workspace(256), b, check=True)          # one without a mark leaves the other's
+    assert P.osdp_read_device_status(b) == (0, TIMEOUT) and P.osdp_read_device_status(a) == (0, TIMEOUT) and P.osdp_read_device_status(b) == (0, 0)
