@@ -210,6 +210,16 @@ __global__ void __launch_bounds__(32 * WARPS, 1) expert_few_kernel(const __grid_
   asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
+// Warps to a unit: as few as keep most of the warps busy, with at most 2048 of K for each and two stages at least.  One token, two
+// experts 2048 -> 8192: 1 / 2 / 4 / 16 warps 24.4 / 17.0 / 17.4 / 21.3 us; 8192 -> 2048 (a quarter of the units): 99 / 52 / 29 / 20 us,
+// with 8 19.4; eight tokens, eight experts 8192 -> 8192: 209 / 174 / 161 / 171 us.
+int warps_to_unit(int64_t live, int64_t N, int64_t K, int sms) {
+  int wk = 1;
+  while (wk < WARPS && (live * cdiv(N, ROWS) * wk < (int64_t)sms * WARPS * 6 / 7 || K > 2048 * wk)) wk *= 2;
+  while (wk > 1 && cdiv(K, KSTAGE) < 2 * wk) wk /= 2;
+  return wk;
+}
+
 template <int T8>
 int launch_few(FewArgs a, int64_t live, cudaStream_t stream) {
   using SH = FewShape<T8>;
@@ -227,12 +237,7 @@ int launch_few(FewArgs a, int64_t live, cudaStream_t stream) {
     if (e != cudaSuccess) return report_cuda(e);
     ready[dev].store(true, std::memory_order_release);
   }
-  // Warps to a unit: as few as keep most of the warps busy, with at most 2048 of K for each and two stages at least.  One token, two
-  // experts 2048 -> 8192: 1 / 2 / 4 / 16 warps 24.4 / 17.0 / 17.4 / 21.3 us; 8192 -> 2048 (a quarter of the units): 99 / 52 / 29 / 20 us,
-  // with 8 19.4; eight tokens, eight experts 8192 -> 8192: 209 / 174 / 161 / 171 us.
-  a.wk = 1;
-  while (a.wk < WARPS && (live * cdiv(a.N, ROWS) * a.wk < (int64_t)sms * WARPS * 6 / 7 || a.K > 2048 * a.wk)) a.wk *= 2;
-  while (a.wk > 1 && cdiv(a.K, KSTAGE) < 2 * a.wk) a.wk /= 2;
+  a.wk = warps_to_unit(live, a.N, a.K, sms);
   int64_t blocks = live * cdiv(a.N, ROWS);
   if (blocks > sms) blocks = sms;
   return launch_overlapped(expert_few_kernel<T8>, dim3((unsigned)blocks), dim3(32 * WARPS), (size_t)SH::SMEM, 1, stream, a);
@@ -246,10 +251,19 @@ int launch_few(FewArgs a, int64_t live, cudaStream_t stream) {
 // 1 x 8 of 64, 2048 -> 2048 20.4 / 22.5; 8 x 2 of 8, 8192 -> 8192 159 / 160.  With more, where the tiles are few: 16 x 2 of 2,
 // 8192 -> 2048 20.7 / 36.5; or the weights: 100 of 16, 512 -> 512 4.6 / 7.6; 56 x 2 of 55, 192 -> 408 5.2 / 11.4; 79 x 2 of 68, 400 -> 480
 // 9.2 / 14.4; but 37 x 2 of 16, 1032 -> 2064 22.9 / 19.7, 64 x 2 of 16, 2048 -> 2048 38 / 29, 32 x 2 of 64, 1024 -> 1024 33 / 26.
+//
+// Only the device knows how many rows an expert has.  Should all tokens choose the same ones, these are read once for every 16
+// tokens by a few warps, 0.55 us for 64 of K a warp, while the tile kernel takes no longer than otherwise.  More than 40 such steps
+// in the worst case (at most twice the tile kernel's time) are not risked: 512 x 1 of 32, 8192 -> 256 takes 75 / 42 with even
+// choices and 520 / 33 if all are one; 200 x 1 of 20, 1024 -> 520 10.4 / 9.3 and 38 / 8.7; but 79 x 2 of 68 21.8 / 12.1, 64 x 2 of 16, 2048 -> 128
+// 5.7 / 12.0 and 10.5 / 11.7.
 bool expert_few_rows(int64_t T, int top_k, int E, int64_t N, int64_t K) {
   const int64_t n = T * top_k, used = n < E ? n : E;
   if (used * cdiv(N, ROWS) >= ((int64_t)1 << 30)) return false;
-  return T <= 8 || (n <= 16 * used && (used * cdiv(N, 128) <= 64 || used * N * K < (1 << 24)));
+  if (T <= 8) return true;
+  int sms = 0;
+  if (n > 16 * used || (used * cdiv(N, 128) > 64 && used * N * K >= (1 << 24)) || sm_count(&sms)) return false;
+  return cdiv(T, 16) * cdiv(cdiv(K, KSTAGE), warps_to_unit(used, N, K, sms)) <= 40;
 }
 
 int launch_expert_few(const void *rows, const int32_t *plan, const void *w, const float *bias, int64_t T, int top_k, int E, int64_t N, int64_t K, int act,

@@ -22,11 +22,15 @@ STREAMED = [
     (8, 8, 8, "even", 4096, 4104),      # WK 4, a group walks several outputs
     (8, 16, 16, "one", 1024, 520),      # WK 2: 128 rows of one expert, 16 readings of its weights
     (8, 2, 3, "one", 40, 3336),         # WK 16: 16 rows of one expert, two readings
-    (200, 1, 20, "one", 520, 1024),     # WK 4, 16 rows to a reading: 200 rows of one expert
-    (200, 1, 20, "skewed", 520, 1024),
-    (200, 1, 20, "holes", 136, 4096),   # WK 16
-    (33, 1, 3, "skewed", 200, 2600),    # WK 16: 3 ... 3 2 0 0
-    (100, 2, 16, "skewed", 8, 12000),   # WK 16, 12 stages, half an output
+    (33, 1, 3, "skewed", 200, 2600),    # WK 16: 3 ... 3 2 0 0; from here on 16 rows to a reading
+    (100, 1, 16, "one", 512, 512),      # WK 4: 100 rows of one expert, seven readings
+    (64, 2, 16, "one", 128, 2048),      # WK 16: 128 rows, eight readings
+    (64, 2, 16, "skewed", 128, 2048),
+    (79, 2, 68, "one", 480, 400),       # WK 1, 7 stages: 158 rows, ten readings
+    (79, 2, 68, "holes", 480, 400),
+    (48, 2, 16, "skewed", 8, 12000),    # WK 16, 12 stages, half an output
+    (512, 1, 32, "one", 256, 8192),     # too many readings in the worst case: the tile kernel
+    (200, 1, 20, "one", 136, 4096),
 ]
 
 
