@@ -92,16 +92,6 @@ __device__ __forceinline__ float fast_exp(float x) {   // 2^-22 and the rounding
   return e;
 }
 
-constexpr float MASK_BIAS = 1048576.0f;
-struct Rank {
-  double key;
-  float then;
-  __device__ bool above(const Rank &o) const { return key > o.key || (key == o.key && then > o.then); }
-  __device__ bool same(const Rank &o) const { return key == o.key && then == o.then; }
-};
-__device__ __forceinline__ Rank shfl_rank(const Rank &r, int from) { return {__shfl_sync(ALL, r.key, from), __shfl_sync(ALL, r.then, from)}; }
-__device__ __forceinline__ Rank shfl_xor_rank(const Rank &r, int o) { return {__shfl_xor_sync(ALL, r.key, o), __shfl_xor_sync(ALL, r.then, o)}; }
-
 // The row's scores in fp64, one at a time.  Compact loops: they are cold when they are needed.
 template <typename L>
 struct Exact {
@@ -131,15 +121,23 @@ struct Exact {
     if (a.bias) s += (double)a.bias[e];
     return s == s ? s : -(double)INFINITY;
   }
-  // What experts are chosen by: the larger first number, of equal ones the larger second.  fp64's sigmoid is 1 from a logit of 37 on and
-  // its softmax 0 from 746 below the largest, so that scores of one bias can be equal where the logits, in whose order exact
-  // ones are, still differ.  A bias of 2^20 or more is a mask, behind which all are equal.
-  __device__ Rank rank_by(int e) const {
-    const float l = fmaxf(widen(row[e]), -INFINITY);
-    if (!a.bias) return {(double)l, 0.f};
-    const double s = score(e);
-    return {s, fabsf(a.bias[e]) < MASK_BIAS && s > -(double)INFINITY ? l : -INFINITY};
+  // what experts are chosen by
+  __device__ double rank_by(int e) const {
+    if (a.bias) return score(e);
+    const double l = (double)widen(row[e]);
+    return l == l ? l : -(double)INFINITY;
   }
+  // Which of two experts with equal numbers `key` comes first.  fp64's sigmoid is 1 from a logit of 37 on and its softmax 0 from 746
+  // below the largest: scores with one bias can be equal where the logits, in whose order exact ones are, still differ.  A
+  // bias of 2^20 or more is a mask, behind which all are equal.
+  __device__ bool first_of_equal(int e, int f, double key) const {
+    if (a.bias && key > -(double)INFINITY) {
+      const float x = logit_behind(e), y = logit_behind(f);
+      if (x != y) return x > y;
+    }
+    return e < f;
+  }
+  __device__ float logit_behind(int e) const { return fabsf(a.bias[e]) < 1048576.0f ? widen(row[e]) : -INFINITY; }
 };
 
 template <typename L>
@@ -154,13 +152,13 @@ __device__ __noinline__ uint32_t exact_groups(const RouteArgs &a, const L *row, 
 template <typename L>
 __device__ __noinline__ void exact_order(const RouteArgs &a, const L *row, int lane, int m, int &mine) {
   const Exact<L> exact(a, row, lane);
-  const Rank key = lane <= m ? exact.rank_by(mine) : Rank{0.0, 0.f};
+  const double key = lane <= m ? exact.rank_by(mine) : 0.0;
   int rank = 0, from = 0;
 #pragma unroll 1
   for (int i = 0; i <= m; ++i) {
-    const Rank other = shfl_rank(key, i);
+    const double other = __shfl_sync(ALL, key, i);
     const int e = __shfl_sync(ALL, mine, i);
-    rank += other.above(key) || (other.same(key) && e < mine) ? 1 : 0;
+    rank += other > key || (other == key && lane <= m && i != lane && exact.first_of_equal(e, mine, key)) ? 1 : 0;
   }
 #pragma unroll 1
   for (int j = 0; j < a.k; ++j) {
@@ -174,28 +172,27 @@ __device__ __noinline__ void exact_order(const RouteArgs &a, const L *row, int l
 template <typename L>
 __device__ __noinline__ void exact_all(const RouteArgs &a, const L *row, uint32_t taken, int lane, int &mine) {
   const Exact<L> exact(a, row, lane);
-  const Rank lowest{-(double)INFINITY, -INFINITY};
-  Rank last = lowest;
+  double last = (double)INFINITY;
   int last_e = -1;
 #pragma unroll 1
   for (int j = 0; j < a.k; ++j) {     // the best of those behind the last one
-    Rank best = lowest;
-    int best_e = 1 << 20;
+    double best = -(double)INFINITY;
+    int best_e = -1;
 #pragma unroll 1
     for (int e = lane; e < a.E; e += 32) {
       if (!((taken >> (((uint32_t)e * a.magic >> 20) << a.lanes_log2)) & 1u)) continue;
-      const Rank x = exact.rank_by(e);
-      const bool behind = j == 0 || last.above(x) || (last.same(x) && e > last_e);
-      if (behind && (x.above(best) || (x.same(best) && e < best_e))) {
+      const double x = exact.rank_by(e);
+      const bool behind = j == 0 || x < last || (x == last && e != last_e && exact.first_of_equal(last_e, e, x));
+      if (behind && (best_e < 0 || x > best || (x == best && exact.first_of_equal(e, best_e, x)))) {
         best = x;
         best_e = e;
       }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-      const Rank x = shfl_xor_rank(best, o);
+      const double x = __shfl_xor_sync(ALL, best, o);
       const int e = __shfl_xor_sync(ALL, best_e, o);
-      if (x.above(best) || (x.same(best) && e < best_e)) {
+      if (e >= 0 && (best_e < 0 || x > best || (x == best && exact.first_of_equal(e, best_e, x)))) {
         best = x;
         best_e = e;
       }
