@@ -18,6 +18,8 @@ namespace {
 // G = dY (.) act'(Z) and the sums of G's columns for each expert, in one pass (bound by memory).  A block takes 256 columns
 // of 64 rows, which are one expert's; the blocks' sums are added in a fixed order by a second kernel.  The sums are of the unrounded G.
 // Rows between two experts become zero, whatever dY and Z hold there.
+// G itself is rounded to bf16, as the operand that both products take: dX and dW are then off by 0.0023 in the norm where their own
+// rounding leaves 0.0017 (without an activation G is dY, which is bf16 as it comes).
 struct GradArgs {
   const __nv_bfloat16 *dy, *z;
   __nv_bfloat16 *g;             // null: column sums of dY alone
@@ -255,14 +257,24 @@ int launch_expert_gemm(const ExpertGemm &c, cudaStream_t stream) {
     return m * cdiv(p.Q, bn);
   };
   // CTA pairs on 256 rows where the experts fill most of such a tile (a weight gradient: its matrix), and there are tiles for a third
-  // of the SMs; outputs of at most 128 columns take single CTAs, which waste half as much of a tile.
+  // of the SMs; outputs of at most 128 columns take single CTAs, which waste half as much of a tile.  256 columns where there are
+  // tiles for most SMs.  Measured (us; single 128, single 256, pair 256, pair 512; * is the choice), T x top_k of E, K -> N:
+  //   forward  300 x 2 of 8, 1024 -> 2048    13.6* 14.6  15.8  19.2    input   600 x 2 of 4, 2048 -> 1024   14.2* 13.6  12.8  21.9
+  //   forward  2000 x 2 of 8, 2048 -> 512    14.9* 19.0  25.6  29.0    input   2000 x 2 of 8, 2048 -> 512   17.2  15.3  17.9* 22.8
+  //   forward  4096 x 2 of 64, 2048 -> 1024  66.7  64.6* 67.3  66.2    input   4096 x 2 of 64, 2048 -> 1024 68.7  62.6* 68.1  67.7
+  //   forward  8192 x 2 of 8, 2048 -> 1024   78.6  64.4  55.6* 57.5    input   8192 x 2 of 8, 2048 -> 8192  525   456   398   385*
+  //   forward  8192 x 2 of 8, 2048 -> 8192   504   416   380*  393     weights 100 x 2 of 4, 1024 -> 1024    5.2   5.4   6.6*  8.0
+  //   forward  2000 x 2 of 8, 1024 -> 1024   16.9  14.0  24.1  21.7*   weights 600 x 2 of 4, 2048 -> 1024   11.9  11.1  10.2  11.7*
+  //   weights  64 x 2 of 16, 2048 -> 8192    132   103   101*  123     weights 8192 x 2 of 8, 512 -> 2048   50.1  44.3  37.6  39.4*
+  // (The rule is off where a few hundred rows of an expert make one short wave of wide tiles: the sixth line.)
   const bool narrow = p.Q <= 128;
   const bool pair = !narrow && tiles(256, 256) >= sms / 3 && (red ? c.N > 128 : n >= 160 * used);
   int bn = 128;
   if (pair || (!narrow && tiles(128, 256) >= (int64_t)sms * 4 / 5)) bn = 256;
   const double len = red ? (double)n / (double)used : (double)p.R;
   if (pair && c.act == ACT_NONE) {
-    // the wider tile: as for the other products (its epilogue does not overlap the next tile)
+    // The wider tile (its epilogue does not overlap the next tile): waves times us for a unit of the reduction, and 5 us for what
+    // does not overlap, once in the run or once a tile; rates and epilogue as measured for the other products.
     const double t_n = (double)cdiv(tiles(256, 256), sms / 2) * (6.5e-3 * len) + 5.0;
     const double t_w = (double)cdiv(tiles(256, 512), sms / 2) * (11.5e-3 * len + 5.0);
     if (t_w < 0.97 * t_n) bn = 512;

@@ -21,9 +21,11 @@ constexpr int ROUTE_WARPS = 8;
 // fp32 with approximate scores: a key is the score's order-preserving bits with the place in the lane's registers in the lowest
 // ones, a lane sorts its keys once, and an expert is found by one maximum over the lanes' first keys.  Where two scores
 // that decide are closer than all these roundings (and are not the same logit with the same bias), the scores in question are
-// taken again in fp64; that is one row in some hundred, and it is kept short (a whole row in fp64 made the last of
-// 16384 rows of 256 experts 10 us late).  Bound by instructions, some 1100 a row: 16384 rows of 256 experts, sigmoid, bias, 4 of 8
-// groups, 8 choices 24 us (17 MB of logits: 2.7 us); 128 experts, 4 choices, without a bias 9.8 us; one row 1.8 us.
+// taken again in fp64.  That is kept short (a whole row in fp64 made the last of 16384 rows of 256 experts 10 us late), for how many
+// rows it is depends on the logits: with sigmoid, 256 experts, groups and a bias of zeros 0.2 % at a spread of 1.2, 2.2 % at 0.02, 9 % at
+// 0.005, and 24.1, 26 and 29 us; with a bias of 0.05 randn 0.2 % at most.  Bound by instructions, some 1100 a row: 16384 rows of 256
+// experts, sigmoid, bias, 4 of 8 groups, 8 choices 24 us (17 MB of logits: 2.7 us); 128 experts, 4 choices, without a bias 9.8 us; one
+// row 1.8 us.
 struct RouteArgs {
   const void *logits;
   long long ld, T;
@@ -425,7 +427,7 @@ __device__ __forceinline__ float sum_of_same(int k, int e, float d, int &first) 
 }
 
 // The gradient is zero but for the chosen.  Bound by latency: choices, their logits, stores behind the zeros (16384 x 256 fp32
-// 7.5 us, floor 2.8; two tokens to a warp 8.9).
+// 7.1 us, floor 2.8; two tokens to a warp 8.9).
 template <typename L>
 __global__ void __launch_bounds__(32 * ROUTE_WARPS) route_bwd_kernel(const __grid_constant__ RouteBackArgs b) {
   pdl_launch_dependents();
